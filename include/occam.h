@@ -405,6 +405,166 @@ int occam_compact_noalloc(const occam_batch* batch, const uint8_t* keep, int32_t
                           int64_t capacity_rows, int32_t* out_index, int32_t* count_out, int64_t* out_off,
                           occam_stream_t stream);
 
+/* ------------------------------------------------------------------ after pruning: rotary positions
+ * Kept rows keep the (time, height, width) positions they had before pruning,
+ * so a pruned prefix is turned by positions given per row and axis. */
+
+/* Element types of the entry points below. */
+enum { OCCAM_BF16 = 0, OCCAM_F16 = 1, OCCAM_F32 = 2 };
+/* Which two of a head's first `rot` values make pair i: HALF (i, i + rot/2), ADJACENT (2i, 2i + 1). */
+enum { OCCAM_ROPE_HALF = 0, OCCAM_ROPE_ADJACENT = 1 };
+
+/* One tensor of an occam_rope call: [rows, heads, dim] values, dense in dim;
+ * strides in elements. dst may be src with the same strides (in place);
+ * otherwise the two must not overlap. */
+typedef struct occam_rope_tensor {
+  const void* src;
+  void* dst;
+  int32_t heads;
+  int64_t src_row, src_head; /* strides of src */
+  int64_t dst_row, dst_head; /* strides of dst */
+} occam_rope_tensor;
+
+/* Rotary positions with several axes. For row n, pair i of rot/2 and every
+ * head, with the angle t = positions[axis[i]][n] * inv_freq[i]:
+ *   (a, b) -> (a cos t - b sin t, b cos t + a sin t);
+ * values rot .. dim-1 are copied. inverse != 0 turns by -t: the transpose,
+ * hence the gradient with respect to the input (and the inverse). The angle
+ * is formed in two fp32 terms, so large positions (up to 2^24) lose nothing.
+ * positions: `axes` (1..8) rows of int32, pos_stride elements apart; inv_freq
+ * [rot/2] fp32; axis [rot/2] int32, each in [0, axes) (an entry outside is
+ * read as 0); all device. tensors: n_tensors (1..2, host array; queries and keys in one
+ * launch). dtype OCCAM_BF16, OCCAM_F16 or OCCAM_F32; any alignment of the
+ * element type. dim even, 2..1024; rot even, 2..dim; rows 0..2^31-1. */
+int occam_rope(int32_t dtype, int64_t rows, int32_t dim, int32_t rot, int32_t pairing, int32_t inverse,
+               const int32_t* positions, int64_t pos_stride, int32_t axes, const float* inv_freq,
+               const int32_t* axis, int32_t n_tensors, const occam_rope_tensor* tensors, occam_stream_t stream);
+
+/* ------------------------------------------------------------------ after pruning: a paged cache held in 8 bits
+ * Keys and values of kept rows, held as e4m3 codes (1 sign, 4 exponent, 3
+ * mantissa bits; largest value 448) with one fp32 scale for each block of
+ * tokens and head: value = code * scale. A page holds page_tokens tokens of
+ * one sequence in every layer; the block of (layer, page, head) is
+ * page_tokens x dim codes, contiguous. Sequence slot s lists its pages in
+ * table[s], holds length[s] tokens (token p in slot p % page_tokens of page
+ * table[s][p / page_tokens]), and a page may belong to several sequences;
+ * refs counts them. A page that is not full belongs to one sequence only.
+ * Table entries that name no page are -1. All state is on the device and only the calls below
+ * write it: nothing needs a host synchronisation, and every call can be
+ * captured into a CUDA graph. Page indices are given out lowest free page
+ * first, in call order, so they do not depend on timing.
+ *
+ * seqs (and src, dst) are device arrays of n distinct slots, n <= max_seqs.
+ * A slot, offset or page outside its range, a slot listed twice (extend,
+ * fork, compact) or a count that does not fit records OCCAM_ERR_INVALID_ARG
+ * in the status word, too few free pages (or table columns) record
+ * OCCAM_ERR_CAPACITY; an extend, fork or compact call that records an error
+ * changes nothing. */
+typedef struct occam_cache {
+  int32_t layers;
+  int32_t pages;       /* pages of the pool (each in all layers), at most 2^24 */
+  int32_t heads;       /* key / value heads */
+  int32_t dim;         /* 64 or 128 */
+  int32_t page_tokens; /* 16, 32, 64 or 128 */
+  int32_t max_seqs;    /* sequence slots, at most 65535 */
+  int32_t max_pages;   /* pages a sequence can hold */
+  void* k;             /* [layers, pages, heads, page_tokens, dim] codes, 16-byte aligned */
+  void* v;
+  float* k_scale;      /* [layers, pages, heads] */
+  float* v_scale;
+  int32_t* table;      /* [max_seqs, max_pages] page or -1 */
+  int32_t* length;     /* [max_seqs] tokens */
+  int32_t* refs;       /* [pages] sequences that hold the page; 0: free */
+} occam_cache;
+
+/* Scratch of the cache calls (workspace convention as above: 256-byte
+ * aligned, zero-filled before first use, status word at its start).
+ * max_tokens: the most keep flags one occam_cache_compact call passes. */
+int occam_cache_workspace_size(const occam_cache* cache, int64_t max_tokens, size_t* bytes);
+
+/* Makes room: sequence seqs[i] grows by counts[i] >= 0 tokens (device int32). Pages
+ * are taken as needed and length is raised; the new tokens' codes are to be
+ * written by occam_cache_append, layer by layer. */
+int occam_cache_extend(const occam_cache* cache, int32_t n, const int32_t* seqs, const int32_t* counts,
+                       void* workspace, size_t workspace_bytes, occam_stream_t stream);
+
+/* Writes the last tokens of each sequence in one layer. Rows row_off[i] ..
+ * row_off[i+1] of k and v ([total_rows, heads, dim] bf16 or f16, rows
+ * k_row / v_row elements apart) are the keys and values of the last
+ * row_off[i+1] - row_off[i] tokens of sequence seqs[i] (row_off [n+1] int64,
+ * device: out_off of occam_prune fits). Per block and head the scale is the
+ * smallest power of two s >= 2^-100 with |x| <= 448 s for every finite new
+ * value, so that codes keep their relative precision and a change of scale is
+ * a shift of the exponent; a block that holds older tokens keeps at least its
+ * scale, and when it grows their codes are rounded again to the new one.
+ * Codes are rounded to nearest, ties to even; infinities become +-448 s, NaN
+ * stays NaN. Repeating a call changes nothing. Rows must be 16-byte aligned. */
+int occam_cache_append(const occam_cache* cache, int32_t layer, int32_t dtype, int64_t total_rows, const void* k,
+                       int64_t k_row, const void* v, int64_t v_row, int32_t n, const int32_t* seqs,
+                       const int64_t* row_off, void* workspace, size_t workspace_bytes, occam_stream_t stream);
+
+/* Attention over the cache. Rows row_off[i] .. row_off[i+1] of q ([total_rows,
+ * heads, dim] bf16 or f16, rows q_row elements apart) are the queries of
+ * the last tokens of sequence seqs[i], whose keys and values are in the cache
+ * already; query head h reads key head h / (heads / cache heads). causal: the
+ * query of token p sees tokens 0..p; else all of the sequence. keep (NULL:
+ * none; uint8, device) hides tokens: token p of sequence i is seen if
+ * keep[keep_off[i] + p] != 0 or p is past the flags (keep_off[i+1] -
+ * keep_off[i] of them; keep_off [n+1] int64, device), so a prefix can be
+ * pruned for one question without moving it. Hidden tokens and slots past the length may hold anything.
+ *   out [total_rows, heads, dim] (q's type, dense) = sum_k p_k v_k / sum_k p_k,
+ *   p_k = exp(scale q.k - max), scale 0: 1/sqrt(dim);
+ *   lse [total_rows, heads] fp32 (NULL to skip) = log sum_k exp(scale q.k).
+ * A row that sees no token gives 0 and -inf. Scores, statistics and sums are
+ * in fp32; probabilities are rounded to f16 for the product with the codes.
+ * Scales of v within a sequence may span a factor of 2^60. max_rows: the
+ * largest row_off[i+1] - row_off[i] (it chooses the kernels; results are right for any
+ * value). heads <= 64 * cache heads. */
+typedef struct occam_attend_args {
+  int32_t layer;
+  int32_t dtype;
+  int32_t heads;
+  int32_t causal;
+  int64_t total_rows;
+  int64_t q_row;
+  const void* q;
+  void* out;
+  float* lse;
+  int32_t n;
+  int32_t max_rows;
+  const int32_t* seqs;
+  const int64_t* row_off;
+  float scale;
+  const uint8_t* keep;
+  const int64_t* keep_off;
+  int64_t total_keep; /* entries of keep */
+} occam_attend_args;
+int occam_cache_attend(const occam_cache* cache, const occam_attend_args* args, void* workspace,
+                       size_t workspace_bytes, occam_stream_t stream);
+
+/* Sequence dst[i], which must be empty, becomes a copy of src[i] (a src may
+ * be listed more than once, but not as a dst): full pages are shared, a last page that is not
+ * full is copied in every layer. */
+int occam_cache_fork(const occam_cache* cache, int32_t n, const int32_t* src, const int32_t* dst, void* workspace,
+                     size_t workspace_bytes, occam_stream_t stream);
+
+/* Prunes sequences in place: token p of sequence seqs[i] stays if
+ * keep[keep_off[i] + p] != 0 or p is past the flags (as in occam_cache_attend;
+ * keep2 and row_off of a prune call fit), in order. Leading full pages
+ * that keep every token stay as they are; the other kept tokens move to new
+ * pages, whose blocks get the scale of their own values (as in
+ * occam_cache_append) in layers layer_begin .. layer_end-1 -- the other
+ * layers' codes are not moved: give every layer that holds the sequence.
+ * New pages are taken before the old ones are given back. */
+int occam_cache_compact(const occam_cache* cache, int32_t layer_begin, int32_t layer_end, int32_t n,
+                        const int32_t* seqs, const uint8_t* keep, const int64_t* keep_off, int64_t total_keep,
+                        void* workspace, size_t workspace_bytes, occam_stream_t stream);
+
+/* Empties sequences: their pages lose a reference, their table rows become
+ * -1 and their lengths 0. An empty sequence stays empty. */
+int occam_cache_release(const occam_cache* cache, int32_t n, const int32_t* seqs, void* workspace,
+                        size_t workspace_bytes, occam_stream_t stream);
+
 /* Diagnostic of the bounded device-side waits (no fault, trap or hang). One
  * warp waits, each time for about limit_ns (1 .. 1e9), on an mbarrier that
  * nothing completes (the tensor-core kernels' timer-bounded wait and the

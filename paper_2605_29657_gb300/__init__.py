@@ -41,3 +41,14 @@ from ._lib import (  # noqa: F401
     occam_version,
     occam_workspace_size,
 )
+from ._cache import (  # noqa: F401
+    PagedCache,
+    occam_cache_append,
+    occam_cache_attend,
+    occam_cache_compact,
+    occam_cache_extend,
+    occam_cache_fork,
+    occam_cache_release,
+    occam_rope,
+    rope_axes,
+)

@@ -1,0 +1,282 @@
+"""What follows pruning: rotary positions with several axes, and a paged
+cache held in 8 bits with the calls that fill it, attend over it and manage
+its pages (include/occam.h). Argument marshalling only, as in _lib."""
+
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from ._lib import (
+    OCCAM_ERR_INVALID_ARG,
+    CAttendArgs,
+    CCache,
+    CRopeTensor,
+    OccamError,
+    _check,
+    _dev_tensor,
+    _ptr,
+    _stream,
+    library,
+    occam_get_status,
+)
+
+_DTYPE = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+_PAIRING = {"half": 0, "adjacent": 1}
+E4M3 = torch.float8_e4m3fn
+
+
+def _bad(msg: str):
+    raise OccamError(OCCAM_ERR_INVALID_ARG, msg)
+
+
+def _rows_tensor(t, name: str, dtypes, heads: int | None = None, dim: int | None = None) -> torch.Tensor:
+    """A CUDA tensor [rows, heads, dim] whose heads are dense; rows may be strided."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        _bad(f"{name} must be a CUDA tensor")
+    if t.dtype not in dtypes:
+        _bad(f"{name} must be one of {[str(d) for d in dtypes]}, got {t.dtype}")
+    if t.dim() != 3 or (heads is not None and t.shape[1] != heads) or (dim is not None and t.shape[2] != dim):
+        _bad(f"{name} must be [rows, {heads or 'heads'}, {dim or 'dim'}], got {list(t.shape)}")
+    if t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2])):
+        _bad(f"{name} must be dense in its last two dimensions")
+    return t
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    """Elements from one row to the next (a single row has none: its own size)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+# ------------------------------------------------------------------ rotary positions
+
+def rope_axes(sections, interleaved: bool = False, device="cuda") -> torch.Tensor:
+    """The axis of each pair, int32 [sum(sections)]. sections[a] pairs turn
+    with axis a: in consecutive runs, or interleaved (pair i with axis i %
+    axes as long as that axis has pairs left, then axis 0)."""
+    n = sum(sections)
+    if not interleaved:
+        axis = [a for a, s in enumerate(sections) for _ in range(s)]
+    else:
+        axis = [0] * n
+        for a in range(1, len(sections)):
+            for i in range(a, len(sections) * sections[a], len(sections)):
+                if i >= n:
+                    _bad("an interleaved section reaches past the pairs")
+                axis[i] = a
+    return torch.tensor(axis, dtype=torch.int32, device=device)
+
+
+def occam_rope(q, k, positions, inv_freq, axis, pairing: str = "half", inverse: bool = False, out_q=None, out_k=None,
+               stream=None):
+    """Turns q [rows, heads, dim] and k (None: q alone) by their positions
+    [axes, rows] int32: pair i by positions[axis[i]] * inv_freq[i]; pairs are
+    (i, i + rot/2) for "half" and (2i, 2i + 1) for "adjacent", rot = 2 *
+    len(inv_freq). inverse: by the negative angle, the gradient's map. q and k may be
+    strided in rows and heads (views of one projection). Results are new
+    dense tensors unless out_q / out_k are given (q itself: in place). Returns (q, k)."""
+    if pairing not in _PAIRING:
+        _bad(f"pairing must be one of {sorted(_PAIRING)}")
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.dtype not in _DTYPE:
+        _bad("q must be [rows, heads, dim] bfloat16, float16 or float32")
+    rows, _, dim = q.shape
+    _dev_tensor(inv_freq, torch.float32, "inv_freq")
+    _dev_tensor(axis, torch.int32, "axis")
+    if inv_freq.dim() != 1 or axis.shape != inv_freq.shape:
+        _bad("inv_freq and axis must be [pairs]")
+    if not isinstance(positions, torch.Tensor) or not positions.is_cuda or positions.dtype != torch.int32 or \
+            positions.dim() != 2 or positions.shape[1] != rows or (rows > 1 and positions.stride(1) != 1):
+        _bad("positions must be a CUDA int32 tensor [axes, rows], dense in rows")
+    ins, outs = [q] if k is None else [q, k], [out_q] if k is None else [out_q, out_k]
+    tensors, results = (CRopeTensor * 2)(), []
+    for i, (x, o) in enumerate(zip(ins, outs)):
+        name = "qk"[i]
+        if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dtype != q.dtype or x.dim() != 3 or \
+                x.shape[0] != rows or x.shape[2] != dim:
+            _bad(f"{name} must be a CUDA tensor [{rows}, heads, {dim}] {q.dtype}")
+        if o is None:
+            o = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        if not isinstance(o, torch.Tensor) or not o.is_cuda or o.shape != x.shape or o.dtype != x.dtype:
+            _bad(f"out_{name} must be like {name}")
+        if x.numel() and (x.stride(2) != 1 or o.stride(2) != 1):
+            _bad(f"{name} must be dense in its last dimension")
+        tensors[i] = CRopeTensor(_ptr(x), _ptr(o), x.shape[1], x.stride(0), x.stride(1), o.stride(0), o.stride(1))
+        results.append(o)
+    _check(library().occam_rope(_DTYPE[q.dtype], rows, dim, 2 * inv_freq.numel(), _PAIRING[pairing], int(bool(inverse)),
+                                _ptr(positions), positions.stride(0), positions.shape[0], _ptr(inv_freq), _ptr(axis),
+                                len(results), tensors, _stream(stream)), "occam_rope")
+    return results[0], (results[1] if k is not None else None)
+
+
+# ------------------------------------------------------------------ the cache
+
+class PagedCache:
+    """A pool of pages for `layers` layers, held as e4m3 codes with an fp32
+    scale per (layer, page, head), and the tables of `max_seqs` sequences.
+
+    k, v [layers, pages, heads, page_tokens, dim] float8_e4m3fn; k_scale,
+    v_scale [layers, pages, heads]; table [max_seqs, max_pages] int32 (-1: no
+    page); length [max_seqs]; refs [pages]. One workspace (ws) serves one
+    call at a time: for calls in flight on several streams give each its own
+    (alloc_workspace)."""
+
+    def __init__(self, layers: int, pages: int, heads: int, dim: int, max_seqs: int, max_pages: int,
+                 page_tokens: int = 64, max_tokens: int | None = None, device="cuda"):
+        shape = (layers, pages, heads, page_tokens, dim)
+        self._set(torch.zeros(shape, dtype=torch.uint8, device=device).view(E4M3),
+                  torch.zeros(shape, dtype=torch.uint8, device=device).view(E4M3),
+                  torch.ones(shape[:3], dtype=torch.float32, device=device),
+                  torch.ones(shape[:3], dtype=torch.float32, device=device),
+                  torch.full((max_seqs, max_pages), -1, dtype=torch.int32, device=device),
+                  torch.zeros(max_seqs, dtype=torch.int32, device=device),
+                  torch.zeros(pages, dtype=torch.int32, device=device), max_tokens)
+
+    @classmethod
+    def wrap(cls, k, v, k_scale, v_scale, table, length, refs, max_tokens: int | None = None) -> "PagedCache":
+        """A cache over existing tensors (nothing is copied)."""
+        self = cls.__new__(cls)
+        self._set(k, v, k_scale, v_scale, table, length, refs, max_tokens)
+        return self
+
+    def _set(self, k, v, k_scale, v_scale, table, length, refs, max_tokens):
+        _dev_tensor(k, E4M3, "k"); _dev_tensor(v, E4M3, "v")
+        _dev_tensor(k_scale, torch.float32, "k_scale"); _dev_tensor(v_scale, torch.float32, "v_scale")
+        _dev_tensor(table, torch.int32, "table"); _dev_tensor(length, torch.int32, "length")
+        _dev_tensor(refs, torch.int32, "refs")
+        if k.dim() != 5 or v.shape != k.shape or k_scale.shape != k.shape[:3] or v_scale.shape != k.shape[:3]:
+            _bad("k and v must be [layers, pages, heads, page_tokens, dim], their scales [layers, pages, heads]")
+        if table.dim() != 2 or length.shape != table.shape[:1] or refs.shape != k.shape[1:2]:
+            _bad("table must be [max_seqs, max_pages], length [max_seqs], refs [pages]")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.table, self.length, self.refs = table, length, refs
+        self.layers, self.pages, self.heads, self.page_tokens, self.dim = k.shape
+        self.max_seqs, self.max_pages = table.shape
+        # flags one compact call may pass: by default a token of every page of the pool
+        self.max_tokens = self.pages * self.page_tokens if max_tokens is None else int(max_tokens)
+        self.device = k.device
+        self._c = CCache(self.layers, self.pages, self.heads, self.dim, self.page_tokens, self.max_seqs, self.max_pages,
+                         _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(table), _ptr(length), _ptr(refs))
+        self._ref = ctypes.byref(self._c)
+        self.ws = self.alloc_workspace()
+
+    def alloc_workspace(self) -> torch.Tensor:
+        """A workspace of the cache calls, zero-filled and 256-byte aligned."""
+        n = ctypes.c_size_t(0)
+        _check(library().occam_cache_workspace_size(self._ref, self.max_tokens, ctypes.byref(n)),
+               "occam_cache_workspace_size")
+        ws = torch.zeros(n.value + 256, dtype=torch.uint8, device=self.device)
+        off = (-ws.data_ptr()) % 256
+        return ws[off:off + n.value]
+
+    def status(self, stream=None, ws=None) -> int:
+        """Reads and clears the status word (synchronises the stream)."""
+        return occam_get_status(self.ws if ws is None else ws, stream)
+
+
+def _cache_args(cache, ws):
+    if not isinstance(cache, PagedCache):
+        _bad("cache must be a PagedCache")
+    return cache.ws if ws is None else ws
+
+
+def _slots(t, name: str, n: int | None = None) -> torch.Tensor:
+    _dev_tensor(t, torch.int32, name)
+    if t.dim() != 1 or (n is not None and t.shape[0] != n):
+        _bad(f"{name} must be a vector" + ("" if n is None else f" of {n}"))
+    return t
+
+
+def _offsets(t, name: str, n: int) -> torch.Tensor:
+    _dev_tensor(t, torch.int64, name)
+    if t.dim() != 1 or t.shape[0] != n + 1:
+        _bad(f"{name} must have one entry more than there are sequences")
+    return t
+
+
+def occam_cache_extend(cache: PagedCache, seqs, counts, ws=None, stream=None) -> None:
+    """Sequence seqs[i] grows by counts[i] tokens: pages are taken and lengths raised."""
+    ws = _cache_args(cache, ws)
+    _slots(seqs, "seqs"); _slots(counts, "counts", seqs.shape[0])
+    _check(library().occam_cache_extend(cache._ref, seqs.shape[0], _ptr(seqs), _ptr(counts), _ptr(ws), ws.numel(),
+                                        _stream(stream)), "occam_cache_extend")
+
+
+def occam_cache_append(cache: PagedCache, layer: int, k, v, seqs, row_off, ws=None, stream=None) -> None:
+    """Writes rows row_off[i] .. row_off[i+1] of k and v [rows, heads, dim]
+    (bfloat16 or float16, rows may be strided) as the last tokens of sequence
+    seqs[i] in one layer."""
+    ws = _cache_args(cache, ws)
+    _rows_tensor(k, "k", (torch.bfloat16, torch.float16), cache.heads, cache.dim)
+    _rows_tensor(v, "v", (k.dtype,), cache.heads, cache.dim)
+    if v.shape[0] != k.shape[0]:
+        _bad("k and v must have as many rows")
+    n = _slots(seqs, "seqs").shape[0]
+    _offsets(row_off, "row_off", n)
+    _check(library().occam_cache_append(cache._ref, int(layer), _DTYPE[k.dtype], k.shape[0], _ptr(k), _row_stride(k),
+                                        _ptr(v), _row_stride(v), n, _ptr(seqs), _ptr(row_off), _ptr(ws), ws.numel(),
+                                        _stream(stream)), "occam_cache_append")
+
+
+def occam_cache_attend(cache: PagedCache, layer: int, q, seqs, row_off, max_rows: int, scale: float = 0.0,
+                       causal: bool = True, keep=None, keep_off=None, out=None, lse=None, ws=None, stream=None):
+    """Attention of the rows of q [rows, heads, dim] (the last tokens of their
+    sequences; rows may be strided) over the cache. max_rows: the most rows of one
+    sequence. scale 0: 1 / sqrt(dim). keep / keep_off: uint8 flags that hide
+    tokens. Returns (out, lse [rows, heads] natural logarithm)."""
+    ws = _cache_args(cache, ws)
+    _rows_tensor(q, "q", (torch.bfloat16, torch.float16), None, cache.dim)
+    rows, heads, dim = q.shape
+    n = _slots(seqs, "seqs").shape[0]
+    _offsets(row_off, "row_off", n)
+    total_keep = 0
+    if keep is not None:
+        _dev_tensor(keep, torch.uint8, "keep")
+        if keep_off is None:
+            _bad("keep needs keep_off")
+        _offsets(keep_off, "keep_off", n)
+        total_keep = keep.numel()
+    if out is None:
+        out = torch.empty((rows, heads, dim), dtype=q.dtype, device=q.device)
+    elif _dev_tensor(out, q.dtype, "out").shape != q.shape:
+        _bad("out must be like q")
+    if lse is None:
+        lse = torch.empty((rows, heads), dtype=torch.float32, device=q.device)
+    elif _dev_tensor(lse, torch.float32, "lse").shape != q.shape[:2]:
+        _bad("lse must be [rows, heads]")
+    a = CAttendArgs(int(layer), _DTYPE[q.dtype], heads, int(bool(causal)), rows, _row_stride(q), _ptr(q), _ptr(out),
+                    _ptr(lse), n, int(max_rows), _ptr(seqs), _ptr(row_off), float(scale), _ptr(keep),
+                    _ptr(keep_off) if keep is not None else None, total_keep)
+    _check(library().occam_cache_attend(cache._ref, ctypes.byref(a), _ptr(ws), ws.numel(), _stream(stream)),
+           "occam_cache_attend")
+    return out, lse
+
+
+def occam_cache_fork(cache: PagedCache, src, dst, ws=None, stream=None) -> None:
+    """Sequence dst[i] (empty) becomes a copy of src[i]; full pages are shared."""
+    ws = _cache_args(cache, ws)
+    _slots(src, "src"); _slots(dst, "dst", src.shape[0])
+    _check(library().occam_cache_fork(cache._ref, src.shape[0], _ptr(src), _ptr(dst), _ptr(ws), ws.numel(),
+                                      _stream(stream)), "occam_cache_fork")
+
+
+def occam_cache_compact(cache: PagedCache, seqs, keep, keep_off, layers: tuple[int, int] | None = None, ws=None,
+                        stream=None) -> None:
+    """Keeps the tokens of each sequence whose flag keep[keep_off[i] + p] is
+    set (and those past the flags), in order; layers: the range of layers whose
+    codes move (default: all)."""
+    ws = _cache_args(cache, ws)
+    n = _slots(seqs, "seqs").shape[0]
+    _dev_tensor(keep, torch.uint8, "keep")
+    _offsets(keep_off, "keep_off", n)
+    l0, l1 = (0, cache.layers) if layers is None else layers
+    _check(library().occam_cache_compact(cache._ref, int(l0), int(l1), n, _ptr(seqs), _ptr(keep), _ptr(keep_off),
+                                         keep.numel(), _ptr(ws), ws.numel(), _stream(stream)), "occam_cache_compact")
+
+
+def occam_cache_release(cache: PagedCache, seqs, ws=None, stream=None) -> None:
+    """Empties sequences; their pages lose a reference."""
+    ws = _cache_args(cache, ws)
+    _slots(seqs, "seqs")
+    _check(library().occam_cache_release(cache._ref, seqs.shape[0], _ptr(seqs), _ptr(ws), ws.numel(),
+                                         _stream(stream)), "occam_cache_release")

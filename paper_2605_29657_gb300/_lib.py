@@ -85,6 +85,27 @@ class CPruneOut(ctypes.Structure):
     ]
 
 
+class CRopeTensor(ctypes.Structure):
+    _fields_ = [("src", _p), ("dst", _p), ("heads", _i32),
+                ("src_row", _i64), ("src_head", _i64), ("dst_row", _i64), ("dst_head", _i64)]
+
+
+class CCache(ctypes.Structure):
+    _fields_ = [
+        ("layers", _i32), ("pages", _i32), ("heads", _i32), ("dim", _i32), ("page_tokens", _i32),
+        ("max_seqs", _i32), ("max_pages", _i32),
+        ("k", _p), ("v", _p), ("k_scale", _p), ("v_scale", _p), ("table", _p), ("length", _p), ("refs", _p),
+    ]
+
+
+class CAttendArgs(ctypes.Structure):
+    _fields_ = [
+        ("layer", _i32), ("dtype", _i32), ("heads", _i32), ("causal", _i32), ("total_rows", _i64), ("q_row", _i64),
+        ("q", _p), ("out", _p), ("lse", _p), ("n", _i32), ("max_rows", _i32), ("seqs", _p), ("row_off", _p),
+        ("scale", ctypes.c_float), ("keep", _p), ("keep_off", _p), ("total_keep", _i64),
+    ]
+
+
 _lib = None
 
 
@@ -129,7 +150,18 @@ def library() -> ctypes.CDLL:
         lib.occam_selftest_wait.argtypes = [ctypes.c_uint64, _p, _p]
         lib.occam_last_call_kernels.argtypes = []
         lib.occam_set_stage2_route.argtypes = [_i32, P(_i32)]
-        for name in ("occam_last_call_kernels", "occam_selftest_wait", "occam_pool_scores", "occam_mean_reference", "occam_budget_keep", "occam_construct_registers", "occam_calibrate_lambda2", "occam_workspace_size", "occam_get_status", "occam_score_stage1",
+        _ws = [_p, ctypes.c_size_t, _p]
+        lib.occam_rope.argtypes = [_i32, _i64, _i32, _i32, _i32, _i32, _p, _i64, _i32, _p, _p, _i32, P(CRopeTensor), _p]
+        lib.occam_cache_workspace_size.argtypes = [P(CCache), _i64, P(ctypes.c_size_t)]
+        lib.occam_cache_extend.argtypes = [P(CCache), _i32, _p, _p] + _ws
+        lib.occam_cache_append.argtypes = [P(CCache), _i32, _i32, _i64, _p, _i64, _p, _i64, _i32, _p, _p] + _ws
+        lib.occam_cache_attend.argtypes = [P(CCache), P(CAttendArgs)] + _ws
+        lib.occam_cache_fork.argtypes = [P(CCache), _i32, _p, _p] + _ws
+        lib.occam_cache_compact.argtypes = [P(CCache), _i32, _i32, _i32, _p, _p, _p, _i64] + _ws
+        lib.occam_cache_release.argtypes = [P(CCache), _i32, _p] + _ws
+        for name in ("occam_rope", "occam_cache_workspace_size", "occam_cache_extend", "occam_cache_append",
+                     "occam_cache_attend", "occam_cache_fork", "occam_cache_compact", "occam_cache_release",
+                     "occam_last_call_kernels", "occam_selftest_wait", "occam_pool_scores", "occam_mean_reference", "occam_budget_keep", "occam_construct_registers", "occam_calibrate_lambda2", "occam_workspace_size", "occam_get_status", "occam_score_stage1",
                      "occam_threshold",
                      "occam_score_stage2", "occam_compact", "occam_prune", "occam_prune_traced",
                      "occam_compact_noalloc", "occam_prune_staged", "occam_set_stage2_route"):

@@ -1,0 +1,573 @@
+// attend.cu -- attention over the paged 8-bit cache for few query rows per key
+// head (single tokens, a few speculative ones), and the C-ABI entry.
+//
+// With m the running maximum of s_k = scale * s(q) * ks(k) * (q . codes_k),
+// in log2 units, one pass keeps l = sum 2^(s_k - m) and O = sum 2^(s_k - m) v_k
+// and rescales both when m grows. Bound by HBM: the codes are read once, 1
+// byte a value. Each warp runs its own key tiles of 32 keys, straight from
+// global memory into the registers of its matrix instructions, with no shared memory
+// and no barrier between tiles; the next keys' loads are issued as soon as
+// the present ones are used up.
+//  - S^T = K Q^T and O^T = V^T P^T (m16n8k16, f16 operands, fp32 sums): keys and
+//    dims fill the 16 rows, up to 8 query rows the 8 columns, so one token of a
+//    group of 8 heads wastes nothing. The order of the summed index is free, so
+//    each lane's 16 bytes of a key row are the operands of four steps as
+//    they come; v's codes of two keys are interleaved by byte permutes; P is
+//    transposed by movmatrix.
+//  - e4m3 codes convert to f16 exactly. Query rows are brought to f16 by a power of two of
+//    their own (bf16's 8 bits fit; what falls below 2^-38 of a row's largest
+//    value is lost), undone in fp32.
+//  - a NaN value counts for the rows that see its token only: in tiles that
+//    some row does not see whole, NaN codes are left out of the product and the
+//    first such token of each dim is noted for the rows past it.
+//  - the scales of v enter P relative to a running reference, so that P stays
+//    in f16's range whatever the scales are.
+#include <algorithm>
+#include <cmath>
+
+#include "attend.cuh"
+#include "nvtx.cuh"
+
+using namespace occam;
+
+namespace {
+
+constexpr int kTile = 32;   // keys of a unit
+constexpr int kWarps = 4;
+constexpr int kThreads = kWarps * 32;
+constexpr float kRhoKeep = 1.f / 64.f;           // P is scaled down by v's scales at most this far
+constexpr float kRhoSpan = 8.6736174e-19f;       // 2^-60
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                        uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
+  uint32_t d;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float q_value(uint16_t x, int bf16) {
+  return bf16 ? __uint_as_float((uint32_t)x << 16) : __half2float(__ushort_as_half(x));
+}
+__device__ __forceinline__ uint16_t out_bits(float x, int bf16) {
+  return bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(x)) : __half_as_ushort(__float2half_rn(x));
+}
+
+// N 4-byte words of 16 bytes each, or zeros
+template <int WORDS>
+__device__ __forceinline__ void load_codes(uint32_t (&r)[WORDS], const uint8_t* p, bool there) {
+#pragma unroll
+  for (int i = 0; i < WORDS; ++i) r[i] = 0;
+  if (there) {
+    if constexpr (WORDS == 4) {
+      const uint4 x = ldg_stream(p);
+      r[0] = x.x;
+      r[1] = x.y;
+      r[2] = x.z;
+      r[3] = x.w;
+    } else {
+      asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "l"(p));
+    }
+  }
+}
+
+// A key tile's addresses and flags, found one tile ahead of its codes
+struct TileMeta {
+  int page[2];
+  uint32_t seen;  // bit k: key k of the tile may be seen
+};
+
+// Takes NaN codes (of either sign) out of a word of values of one key, dims d .. d+3, and
+// notes the key as the first of those dims.
+__device__ __forceinline__ void note_nans(uint32_t& w, int key, int d, int* first) {
+  const uint32_t hit = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+  if (hit) {
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+      if ((hit >> (8 * b + 7)) & 1) {
+        atomicMin(&first[d + b], key);
+        w &= ~(0xffu << (8 * b));
+      }
+  }
+}
+
+// NQ: tiles of 8 query rows
+template <int D, int NQ>
+__global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(AttendParams p) {
+  constexpr int R = 8 * NQ;
+  constexpr int KC = D / 64;      // 16-byte pieces of a key row a lane holds
+  constexpr int VW = D / 32;      // 4-byte words of a value row a lane holds
+  constexpr int MT = D / 16;      // tiles of 16 dims
+  __shared__ int64_t sh[kWarps + 4];
+  __shared__ float sh_m[kWarps][R], sh_l[kWarps][R];
+  __shared__ int sh_last;
+  __shared__ int sh_nan[D];  // first token with a NaN in that dim, of those taken out
+  extern __shared__ float sh_o[];  // [kWarps][R][D]
+
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int g = lane >> 2, t = lane & 3;
+  for (int d = threadIdx.x; d < D; d += kThreads) sh_nan[d] = 0x7fffffff;
+  Stretch w;
+  if (!attend_stretch<R, kTile, kThreads>(p, kWarps, sh, w)) return;
+
+  int i = w.seq;
+  SeqInfo s = attend_seq(p, i);
+  int64_t hu = head_units<R, kTile>(p, s);
+  if (hu == 0) return;
+  int h = (int)(w.in_seq / hu), rt = 0;
+  int64_t in_item = w.in_seq - h * hu;
+  int tiles = key_tiles<R, kTile>(p, s, 0);
+  while (in_item >= tiles) {
+    in_item -= tiles;
+    tiles = key_tiles<R, kTile>(p, s, ++rt);
+  }
+
+  for (int64_t u = w.u0; u < w.u1;) {
+    const int ta = (int)in_item, tb = (int)min((int64_t)tiles, ta + (w.u1 - u));
+    const int rows = s.rows * p.G - rt * R;  // rows of this tile that exist, from 0
+    const int32_t* table = p.c.table + (int64_t)s.seq * p.c.max_pages;
+    const uint8_t* flags = nullptr;
+    int n_flags = 0;
+    if (p.keep) {
+      const int64_t k0 = p.keep_off[i], k1 = p.keep_off[i + 1];
+      if (k0 >= 0 && k1 >= k0 && k1 <= p.total_keep) {
+        flags = p.keep + k0;
+        n_flags = (int)min(k1 - k0, (int64_t)s.len);
+      } else {
+        set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
+      }
+    }
+
+    // the query rows as f16, scaled by a power of two each
+    uint32_t qf[NQ][4 * KC][2];
+    float qscale[NQ][2];  // of rows 2t and 2t + 1
+    int limit[NQ][2];     // keys those rows see
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) {
+      const int r = nq * 8 + g;
+      float x[KC][16];
+      float amax = 0.f;
+      const int row = rt * R + r, j = row / p.G;
+      const uint16_t* q = p.q + (s.row0 + j) * p.q_row + (int64_t)(h * p.G + row - j * p.G) * D;
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        uint4 v[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+        if (r < rows) {
+          v[0] = *reinterpret_cast<const uint4*>(q + (t + 4 * c) * 16);
+          v[1] = *reinterpret_cast<const uint4*>(q + (t + 4 * c) * 16 + 8);
+        }
+        const uint16_t* b = reinterpret_cast<const uint16_t*>(v);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          x[c][k] = q_value(b[k], p.bf16);
+          amax = fmaxf(amax, finite_abs(x[c][k]));
+        }
+      }
+      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+      // largest value in [2^14, 2^15): far from f16's end, small values far from its lower end
+      int e = (__float_as_int(amax) >> 23) - 127 - 14;
+      e = amax == 0.f ? 0 : max(e, -112);
+      const float up = __int_as_float((127 - e) << 23);
+#pragma unroll
+      for (int c = 0; c < KC; ++c)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          qf[nq][c * 4 + k][0] = pack_f16(x[c][4 * k] * up, x[c][4 * k + 1] * up);
+          qf[nq][c * 4 + k][1] = pack_f16(x[c][4 * k + 2] * up, x[c][4 * k + 3] * up);
+        }
+      const float down = __int_as_float((127 + e) << 23) * p.scale_log2;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        qscale[nq][k] = __shfl_sync(0xffffffffu, down, (2 * t + k) * 4);
+        const int rr = nq * 8 + 2 * t + k;
+        limit[nq][k] = rr >= rows ? 0 : p.causal ? s.len - s.rows + (rt * R + rr) / p.G + 1 : s.len;
+      }
+    }
+    // keys that every row of the tile sees
+    const int common = p.causal ? s.len - s.rows + (rt * R) / p.G + 1 : s.len;
+
+    float o[NQ][MT][4], m[NQ][2], l[NQ][2];
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq) {
+#pragma unroll
+      for (int k = 0; k < MT; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[nq][k][e] = 0.f;
+      m[nq][0] = m[nq][1] = -INFINITY;
+      l[nq][0] = l[nq][1] = 0.f;
+    }
+    float rho = 0.f, rho_max = 0.f;  // O is held in units of rho
+
+    const int64_t layer_page = (int64_t)p.layer * p.c.pages;
+    const int tmask = p.c.T - 1;
+    auto meta_of = [&](int tile) {
+      TileMeta x;
+      const int key = tile * kTile;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int first = key + 16 * k;
+        x.page[k] = first < s.len ? table[first >> p.c.log2T] : 0;
+      }
+      bool see = key + lane < s.len;
+      if (key + lane < n_flags) see = flags[key + lane] != 0;
+      x.seen = see;
+      return x;
+    };
+    // the ballot is taken one tile later, when the flag has arrived
+    auto settle = [&](TileMeta& x) {
+      x.seen = __ballot_sync(0xffffffffu, x.seen != 0);
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        if ((unsigned)x.page[k] >= (unsigned)p.c.pages) {
+          set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
+          x.page[k] = 0;
+          x.seen &= k ? 0x0000ffffu : 0xffff0000u;
+        }
+    };
+    uint32_t kr[4][KC][4];     // rows g, g + 8, g + 16, g + 24
+    uint32_t vr[2][4][VW];     // rows 2t, 2t + 1, 2t + 8, 2t + 9 of each 16 keys
+    float ks[2], vs[2];
+    auto block_of = [&](const TileMeta& x, int k) { return (layer_page + x.page[k]) * p.c.heads + h; };
+    auto load_k = [&](const TileMeta& x, int tile) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int64_t b = block_of(x, k);
+        ks[k] = p.c.k_scale[b];
+        const uint8_t* base = p.c.k + (b * p.c.T + ((tile * kTile + 16 * k) & tmask)) * D + t * 16;
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+          for (int c = 0; c < KC; ++c)
+            load_codes<4>(kr[2 * k + r][c], base + (g + 8 * r) * D + 64 * c, (x.seen >> (16 * k + 8 * r + g)) & 1);
+      }
+    };
+    auto load_v = [&](const TileMeta& x, int tile) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int64_t b = block_of(x, k);
+        vs[k] = p.c.v_scale[b];
+        const uint8_t* base = p.c.v + (b * p.c.T + ((tile * kTile + 16 * k) & tmask)) * D + g * (4 * VW);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int row = 2 * t + (r & 1) + 8 * (r >> 1);
+          load_codes<VW>(vr[k][r], base + row * D, (x.seen >> (16 * k + row)) & 1);
+        }
+      }
+    };
+
+    int tile = ta + (int)((warp - (int)(u % kWarps) + kWarps) % kWarps);
+    TileMeta cur, nxt;
+    if (tile < tb) {
+      cur = meta_of(tile);
+      settle(cur);
+      load_k(cur, tile);
+      load_v(cur, tile);
+      nxt = meta_of(min(tile + kWarps, tb - 1));
+    }
+    for (; tile < tb; tile += kWarps) {
+      const bool more = tile + kWarps < tb;
+      settle(nxt);
+      const TileMeta after = meta_of(min(tile + 2 * kWarps, tb - 1));
+      // scores
+      float sc[NQ][2][4];
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[nq][k][e] = 0.f;
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int c = 0; c < KC; ++c)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const uint32_t lo = kr[2 * k][c][x], hi = kr[2 * k + 1][c][x];
+            const uint32_t a0 = e4m3x2_f16x2(lo), a2 = e4m3x2_f16x2_hi(lo);
+            const uint32_t a1 = e4m3x2_f16x2(hi), a3 = e4m3x2_f16x2_hi(hi);
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq) mma_f16(sc[nq][k], a0, a1, a2, a3, qf[nq][c * 4 + x][0], qf[nq][c * 4 + x][1]);
+          }
+      const float ksc[2] = {ks[0], ks[1]};
+      const uint32_t seen = cur.seen;
+      if (more) load_k(nxt, tile + kWarps);
+      // softmax: lane holds rows 2t, 2t + 1 of keys g, g + 8 of each 16
+      const bool open = seen == 0xffffffffu && (tile + 1) * kTile <= common;
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[nq][k][e] *= ksc[k] * qscale[nq][e & 1];
+        if (!open) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int key = 16 * k + 8 * (e >> 1) + g;
+              const bool see = ((seen >> key) & 1) && tile * kTile + key < limit[nq][e & 1];
+              sc[nq][k][e] = see ? sc[nq][k][e] : -INFINITY;
+            }
+        }
+        float grow[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float x = fmaxf(fmaxf(sc[nq][0][e], sc[nq][0][e + 2]), fmaxf(sc[nq][1][e], sc[nq][1][e + 2]));
+          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+          const float mn = fmaxf(m[nq][e], x);
+          const float ref = mn == -INFINITY ? 0.f : mn;  // nothing seen yet: every p is 0
+          grow[e] = fast_exp2(m[nq][e] - ref);
+          m[nq][e] = mn;
+          l[nq][e] *= grow[e];
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+              const float pr = fast_exp2(sc[nq][k][e + 2 * b] - ref);
+              sc[nq][k][e + 2 * b] = pr;
+              l[nq][e] += pr;
+            }
+        }
+        if (__any_sync(0xffffffffu, grow[0] != 1.f || grow[1] != 1.f)) {
+#pragma unroll
+          for (int k = 0; k < MT; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[nq][k][e] *= grow[e & 1];
+        }
+      }
+      if (!open) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int x = 0; x < VW; ++x)
+              note_nans(vr[k][r][x], tile * kTile + 16 * k + 2 * t + (r & 1) + 8 * (r >> 1), g * (4 * VW) + 4 * x, sh_nan);
+      }
+      // O^T += V^T P^T, 16 keys at a time
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if ((seen >> (16 * k)) & 0xffff) {
+          const float v = vs[k];
+          if (v > rho || v < rho * kRhoKeep) {  // the same in every lane
+            float to = v > rho ? v : fmaxf(v, rho_max * kRhoSpan);
+            if (to != rho && to > 0.f) {
+              const float f = rho / to;
+#pragma unroll
+              for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                for (int x = 0; x < MT; ++x)
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) o[nq][x][e] *= f;
+              rho = to;
+              rho_max = fmaxf(rho_max, to);
+            }
+          }
+          const float ratio = rho > 0.f ? v / rho : 0.f;
+          uint32_t b0[NQ], b1[NQ];
+#pragma unroll
+          for (int nq = 0; nq < NQ; ++nq) {
+            b0[nq] = transpose8x8(pack_f16(sc[nq][k][0] * ratio, sc[nq][k][1] * ratio));
+            b1[nq] = transpose8x8(pack_f16(sc[nq][k][2] * ratio, sc[nq][k][3] * ratio));
+          }
+#pragma unroll
+          for (int x = 0; x < VW; ++x) {
+            const uint32_t w0 = vr[k][0][x], w1 = vr[k][1][x], w2 = vr[k][2][x], w3 = vr[k][3][x];
+            // two keys' bytes 0, 1 and 2, 3 side by side
+            const uint32_t p0 = __byte_perm(w0, w1, 0x5140), p1 = __byte_perm(w0, w1, 0x7362);
+            const uint32_t p2 = __byte_perm(w2, w3, 0x5140), p3 = __byte_perm(w2, w3, 0x7362);
+            const uint32_t a0 = e4m3x2_f16x2(p0), a1 = e4m3x2_f16x2_hi(p0), a2 = e4m3x2_f16x2(p2), a3 = e4m3x2_f16x2_hi(p2);
+            const uint32_t c0 = e4m3x2_f16x2(p1), c1 = e4m3x2_f16x2_hi(p1), c2 = e4m3x2_f16x2(p3), c3 = e4m3x2_f16x2_hi(p3);
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq) {
+              mma_f16(o[nq][2 * x], a0, a1, a2, a3, b0[nq], b1[nq]);
+              mma_f16(o[nq][2 * x + 1], c0, c1, c2, c3, b0[nq], b1[nq]);
+            }
+          }
+        }
+      }
+      if (more) load_v(nxt, tile + kWarps);
+      cur = nxt;
+      nxt = after;
+    }
+
+    // the warps' results meet in shared memory
+#pragma unroll
+    for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float x = l[nq][e];
+        x += __shfl_xor_sync(0xffffffffu, x, 4);
+        x += __shfl_xor_sync(0xffffffffu, x, 8);
+        x += __shfl_xor_sync(0xffffffffu, x, 16);
+        const int r = nq * 8 + 2 * t + e;
+        if (g == 0) {
+          sh_m[warp][r] = m[nq][e];
+          sh_l[warp][r] = x;
+        }
+        // dims 16 g' .. of row r: tile k holds dims D/8 g + 2k and + 2k + 1
+        float* dst = sh_o + (warp * R + r) * D + g * (D / 8);
+#pragma unroll
+        for (int k = 0; k < MT; k += 2)
+          *reinterpret_cast<float4*>(dst + 2 * k) =
+              make_float4(o[nq][k][e] * rho, o[nq][k][e + 2] * rho, o[nq][k + 1][e] * rho, o[nq][k + 1][e + 2] * rho);
+      }
+    __syncthreads();
+    const bool whole = ta == 0 && tb == tiles;
+    const int slot = ta > 0 ? 0 : 1;
+    float* po = p.part_o + ((int64_t)blockIdx.x * 2 + slot) * kAttendRows * D;
+    float2* pml = p.part_ml + ((int64_t)blockIdx.x * 2 + slot) * kAttendRows;
+    const int live = min(rows, R);
+    for (int e = threadIdx.x; e < live * D; e += kThreads) {
+      const int r = e / D, d = e % D;
+      float mx = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < kWarps; ++k) mx = fmaxf(mx, sh_m[k][r]);
+      const float ref = mx == -INFINITY ? 0.f : mx;
+      float sum = 0.f, acc = 0.f;
+#pragma unroll
+      for (int k = 0; k < kWarps; ++k) {
+        const float f = fast_exp2(sh_m[k][r] - ref);
+        sum += sh_l[k][r] * f;
+        acc += sh_o[(k * R + r) * D + d] * f;
+      }
+      const int row = rt * R + r, j = row / p.G;
+      if (sh_nan[d] < (p.causal ? s.len - s.rows + j + 1 : s.len)) acc = __int_as_float(0x7fc00000);
+      if (whole) {
+        const int64_t to = (s.row0 + j) * p.H + h * p.G + row - j * p.G;
+        p.out[to * D + d] = out_bits(sum == 0.f ? 0.f : acc / sum, p.bf16);
+        if (d == 0 && p.lse) p.lse[to] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.69314718056f;
+      } else {
+        po[r * D + d] = acc;
+        if (d == 0) pml[r] = make_float2(mx, sum);
+      }
+    }
+    if (!whole) {
+      __threadfence();
+      __syncthreads();
+      const int64_t item = u - ta;  // the item's first unit
+      const int first = cta_of(w.units, w.ctas, item), last = cta_of(w.units, w.ctas, item + tiles - 1);
+      if (threadIdx.x == 0) sh_last = atomicAdd(&p.counters[first], 1) == last - first;
+      __syncthreads();
+      if (sh_last) {
+        __threadfence();
+        if (threadIdx.x == 0) p.counters[first] = 0;
+        for (int e = threadIdx.x; e < live * D; e += kThreads) {
+          const int r = e / D, d = e % D;
+          float mx = -INFINITY, sum = 0.f, acc = 0.f;
+          for (int c = first; c <= last; ++c) {
+            const int64_t at = ((int64_t)c * 2 + (c == first ? 1 : 0)) * kAttendRows + r;
+            const float2 ml = __ldcg(&p.part_ml[at]);
+            const float x = __ldcg(&p.part_o[at * D + d]);
+            const float mn = fmaxf(mx, ml.x), ref = mn == -INFINITY ? 0.f : mn;
+            const float f0 = fast_exp2(mx - ref), f1 = fast_exp2(ml.x - ref);
+            sum = sum * f0 + ml.y * f1;
+            acc = acc * f0 + x * f1;
+            mx = mn;
+          }
+          const int row = rt * R + r, j = row / p.G;
+          const int64_t to = (s.row0 + j) * p.H + h * p.G + row - j * p.G;
+          p.out[to * D + d] = out_bits(sum == 0.f ? 0.f : acc / sum, p.bf16);
+          if (d == 0 && p.lse) p.lse[to] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.69314718056f;
+        }
+      }
+    }
+    __syncthreads();  // the shared results are free again
+    for (int d = threadIdx.x; d < D; d += kThreads) sh_nan[d] = 0x7fffffff;
+
+    u += tb - ta;
+    in_item = 0;
+    if (u < w.u1) {
+      const int nrt = (s.rows * p.G + R - 1) / R;
+      if (++rt == nrt) {
+        rt = 0;
+        if (++h == p.c.heads) {
+          h = 0;
+          do {
+            s = attend_seq(p, ++i);
+          } while (s.rows == 0);
+        }
+      }
+      tiles = key_tiles<R, kTile>(p, s, rt);
+    }
+  }
+}
+
+template <int D, int NQ>
+int launch_rows(const AttendParams& p, cudaStream_t st) {
+  const size_t smem = (size_t)kWarps * 8 * NQ * D * 4;
+  const int grid = std::min(cache_sms() * (NQ == 1 ? 3 : 2), kAttendCtas);
+  attend_rows_kernel<D, NQ><<<grid, kThreads, smem, st>>>(p);
+  count_launch();
+  return cudaGetLastError() == cudaSuccess ? OCCAM_OK : OCCAM_ERR_CUDA;
+}
+
+}  // namespace
+
+#define OCCAM_TRY(x)                 \
+  do {                               \
+    int _rc = (x);                   \
+    if (_rc != OCCAM_OK) return _rc; \
+  } while (0)
+
+extern "C" int occam_cache_attend(const occam_cache* cache, const occam_attend_args* a, void* workspace,
+                                  size_t workspace_bytes, occam_stream_t stream) {
+  const NvtxRange nvtx("occam_cache_attend");
+  launch_counter() = 0;
+  OCCAM_TRY(check_cache(cache));
+  if (!a) return OCCAM_ERR_INVALID_ARG;
+  if (a->dtype != OCCAM_BF16 && a->dtype != OCCAM_F16) return OCCAM_ERR_UNSUPPORTED;
+  if (a->layer < 0 || a->layer >= cache->layers || a->total_rows < 0 || a->total_rows > 0x7fffffff || a->n < 0 ||
+      a->n > cache->max_seqs || a->max_rows < 0 || a->heads < 1 || a->heads % cache->heads != 0 || !(a->scale >= 0.f) ||
+      !(a->scale < INFINITY))
+    return OCCAM_ERR_INVALID_ARG;
+  const int G = a->heads / cache->heads;
+  if (G > 64 || a->total_rows * G > 0x7fffffff) return OCCAM_ERR_UNSUPPORTED;
+  if (a->keep && (!a->keep_off || a->total_keep < 0)) return OCCAM_ERR_INVALID_ARG;
+  CacheWs w;
+  OCCAM_TRY(check_cache_ws(cache, 0, workspace, workspace_bytes, &w));
+  if (a->n == 0 || a->total_rows == 0) return OCCAM_OK;
+  if (!a->q || !a->out || !a->seqs || !a->row_off || !aligned16(a->q) || !aligned16(a->out) || (a->q_row & 7) ||
+      a->q_row < (int64_t)a->heads * cache->dim)
+    return OCCAM_ERR_INVALID_ARG;
+  AttendParams p{};
+  p.c = cache_dev(cache, workspace, w);
+  p.layer = a->layer;
+  p.n = a->n;
+  p.H = a->heads;
+  p.G = G;
+  p.causal = a->causal ? 1 : 0;
+  p.bf16 = a->dtype == OCCAM_BF16;
+  p.row_lo = 0;
+  p.row_hi = 0x7fffffff;
+  p.total_rows = a->total_rows;
+  p.q_row = a->q_row;
+  p.total_keep = a->total_keep;
+  p.q = static_cast<const uint16_t*>(a->q);
+  p.out = static_cast<uint16_t*>(a->out);
+  p.lse = a->lse;
+  p.seqs = a->seqs;
+  p.row_off = a->row_off;
+  p.keep = a->keep;
+  p.keep_off = a->keep_off;
+  const double scale = a->scale > 0.f ? (double)a->scale : 1.0 / std::sqrt((double)cache->dim);
+  p.scale_log2 = (float)(scale * 1.4426950408889634);
+  p.counters = ws_at<int32_t>(workspace, w.counters);
+  p.part_o = ws_at<float>(workspace, w.part_o);
+  p.part_ml = ws_at<float2>(workspace, w.part_ml);
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  const bool few = (int64_t)a->max_rows * G <= 8;
+  if (cache->dim == 128) return few ? launch_rows<128, 1>(p, st) : launch_rows<128, 2>(p, st);
+  return few ? launch_rows<64, 1>(p, st) : launch_rows<64, 2>(p, st);
+}

@@ -1,0 +1,139 @@
+// attend.cuh -- parameters and work partition shared by the attention kernels
+// over the paged cache (internal header).
+//
+// The work is a line of units: for each sequence, key head and tile of query
+// rows (token j, query head g of the key head's group: row j G + g) the key
+// tiles that the tile's last row can see. Every CTA takes an equal stretch of
+// the line. An item (sequence, head, row tile) that lies in one CTA's
+// stretch is finished there; one that is split leaves a partial result
+// (unnormalised sums, running maximum, sum) per CTA, and the CTA that
+// arrives last adds them in order -- always the same order, so results do not depend on timing.
+#pragma once
+
+#include "cache.cuh"
+
+namespace occam {
+
+struct AttendParams {
+  CacheDev c;
+  int layer, n, H, G, causal, bf16;
+  int row_lo, row_hi;  // sequences with row_lo < rows * G <= row_hi are this launch's
+  int64_t total_rows, q_row, total_keep;
+  const uint16_t* q;
+  uint16_t* out;
+  float* lse;
+  const int32_t* seqs;
+  const int64_t* row_off;
+  const uint8_t* keep;
+  const int64_t* keep_off;
+  float scale_log2;
+  int32_t* counters;
+  float* part_o;
+  float2* part_ml;
+};
+
+struct SeqInfo {
+  int64_t row0;
+  int rows, len, seq;
+};
+
+// Sequence i's rows and length; rows = 0 if it is not this launch's or if its offsets do
+// not fit (recorded).
+__device__ __forceinline__ SeqInfo attend_seq(const AttendParams& p, int i) {
+  SeqInfo s;
+  s.row0 = p.row_off[i];
+  const int64_t r1 = p.row_off[i + 1];
+  s.seq = p.seqs[i];
+  s.rows = 0;
+  s.len = 0;
+  if ((unsigned)s.seq < (unsigned)p.c.max_seqs) {
+    const int len = p.c.length[s.seq];
+    if (s.row0 >= 0 && r1 >= s.row0 && r1 <= p.total_rows && len <= p.c.max_pages * p.c.T && r1 - s.row0 <= len) {
+      s.len = len;
+      const int64_t m = (r1 - s.row0) * p.G;
+      if (m > p.row_lo && m <= p.row_hi) s.rows = (int)(r1 - s.row0);
+      return s;
+    }
+  }
+  set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
+  return s;
+}
+
+// Key tiles of KT keys that row tile rt (R rows) of a sequence can see, at least one.
+template <int R, int KT>
+__device__ __forceinline__ int key_tiles(const AttendParams& p, const SeqInfo& s, int rt) {
+  int keys = s.len;
+  if (p.causal) keys = s.len - s.rows + min((rt + 1) * R - 1, s.rows * p.G - 1) / p.G + 1;
+  return (keys + KT - 1) / KT;
+}
+template <int R, int KT>
+__device__ __forceinline__ int64_t head_units(const AttendParams& p, const SeqInfo& s) {
+  if (s.rows == 0) return 0;
+  const int nrt = (s.rows * p.G + R - 1) / R;
+  if (!p.causal) return (int64_t)nrt * ((s.len + KT - 1) / KT);
+  int64_t u = 0;
+  for (int rt = 0; rt < nrt; ++rt) u += key_tiles<R, KT>(p, s, rt);
+  return u;
+}
+
+// The stretch [u0, u1) of the CTA and the sequence its first unit is in.
+struct Stretch {
+  int64_t units, u0, u1, in_seq;  // in_seq: u0 relative to the sequence's first unit
+  int ctas, seq;
+};
+
+__device__ __forceinline__ int64_t cta_begin(int64_t units, int ctas, int c) { return units * c / ctas; }
+__device__ __forceinline__ int cta_of(int64_t units, int ctas, int64_t u) {
+  int c = (int)(u * ctas / units);
+  while (c + 1 < ctas && cta_begin(units, ctas, c + 1) <= u) ++c;
+  while (c > 0 && cta_begin(units, ctas, c) > u) --c;
+  return c;
+}
+
+// Block-wide (NT threads, all of them); sh: NT / 32 + 4 int64 of shared memory. False: no work for this CTA.
+template <int R, int KT, int NT>
+__device__ __forceinline__ bool attend_stretch(const AttendParams& p, int min_units, int64_t* sh, Stretch& w) {
+  constexpr int NWARP = NT / 32;
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+  const int per = (p.n + NT - 1) / NT;
+  const int i0 = min(t * per, p.n), i1 = min(i0 + per, p.n);
+  int64_t mine = 0;
+  for (int i = i0; i < i1; ++i) mine += p.c.heads * head_units<R, KT>(p, attend_seq(p, i));
+  int64_t incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t x = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += x;
+  }
+  if (lane == 31) sh[warp] = incl;
+  __syncthreads();
+  int64_t before = 0, total = 0;
+#pragma unroll
+  for (int k = 0; k < NWARP; ++k) {
+    if (k < warp) before += sh[k];
+    total += sh[k];
+  }
+  w.units = total;
+  const int64_t most = (total + min_units - 1) / min_units;
+  w.ctas = (int)min((int64_t)gridDim.x, most > 0 ? most : 1);
+  if (total == 0 || (int)blockIdx.x >= w.ctas) return false;
+  w.u0 = cta_begin(total, w.ctas, blockIdx.x);
+  w.u1 = cta_begin(total, w.ctas, blockIdx.x + 1);
+  int64_t at = before + incl - mine;
+  if (w.u0 >= at && w.u0 < at + mine) {
+    int i = i0;
+    for (;; ++i) {
+      const int64_t u = p.c.heads * head_units<R, KT>(p, attend_seq(p, i));
+      if (w.u0 < at + u || i + 1 >= i1) break;
+      at += u;
+    }
+    sh[NWARP] = i;
+    sh[NWARP + 1] = w.u0 - at;
+  }
+  __syncthreads();
+  w.seq = (int)sh[NWARP];
+  w.in_seq = sh[NWARP + 1];
+  return true;
+}
+
+}  // namespace occam

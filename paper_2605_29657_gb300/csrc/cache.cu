@@ -1,0 +1,862 @@
+// cache.cu -- the paged 8-bit cache: occam_cache_append and the page calls
+// (extend, fork, compact, release). The page bookkeeping is a one-CTA kernel
+// per call: reference counts are scanned for free pages (lowest first) and
+// handed out in call order by prefix sums, so page indices do not depend on
+// timing. The codes move in grid-wide kernels behind it.
+#include <algorithm>
+#include <cstring>
+
+#include "cache.cuh"
+#include "nvtx.cuh"
+
+using namespace occam;
+
+int occam::cache_sms() {
+  constexpr int kMaxDevices = 64;
+  static int sms[kMaxDevices];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 148;
+  if (sms[dev] == 0) {
+    int n = 0;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) n = 148;
+    sms[dev] = n;  // the same value from every thread
+  }
+  return sms[dev];
+}
+
+namespace {
+
+constexpr int kPlanThreads = 1024;
+
+// ---------------------------------------------------------------- append
+// One CTA per (touched page, head, K or V): the new rows' values of the block
+// stay in registers between the block's maximum and the rounding, so they are
+// read once. Bound by HBM (2 bytes read and 1 written a value).
+struct AppendParams {
+  CacheDev c;
+  int layer, n, dim;
+  int64_t total_rows, k_row, v_row;
+  const void* k;
+  const void* v;
+  const int32_t* seqs;
+  const int64_t* row_off;
+};
+
+// The first index whose slot count passes w: sequence i's pages occupy slots
+// [row_off[i] / T + 2 i, row_off[i+1] / T + 2 (i + 1)), at least as many as
+// the pages its rows can touch. One warp searches 32 ways at a time.
+__device__ __forceinline__ int slot_sequence(const int64_t* row_off, int n, int log2T, int64_t w) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, hi = n;  // slot(lo) <= w < slot(hi)
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 31) / 32;
+    const int i = min(lo + (lane + 1) * step, hi);
+    const bool past = i >= hi || (row_off[i] >> log2T) + 2 * (int64_t)i > w;
+    const unsigned b = __ballot_sync(0xffffffffu, past);
+    const int f = __ffs(b) - 1;  // some lane always reaches hi
+    const int nh = min(lo + (f + 1) * step, hi);
+    lo = lo + f * step;
+    hi = nh;
+  }
+  return lo;
+}
+
+template <bool BF16>
+__device__ __forceinline__ void unpack8(uint4 r, float (&x)[8]) {
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (BF16) {
+      x[2 * i] = bf16_lo(w[i]);
+      x[2 * i + 1] = bf16_hi(w[i]);
+    } else {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      x[2 * i] = f.x;
+      x[2 * i + 1] = f.y;
+    }
+  }
+}
+
+// MAXV: 8-value vectors a thread holds (128 threads; page_tokens * dim / 8 / 128 at most)
+template <bool BF16, int MAXV>
+__global__ void __launch_bounds__(128) append_kernel(AppendParams p) {
+  __shared__ float red[4];
+  const int T = p.c.T, D = p.dim, H = p.c.heads;
+  const int64_t item = blockIdx.x;
+  const int kv = (int)(item & 1);
+  const int64_t rest = item >> 1;
+  const int h = (int)(rest % H);
+  const int64_t w = rest / H;
+  const int i = slot_sequence(p.row_off, p.n, p.c.log2T, w);
+  const int64_t r0 = p.row_off[i], r1 = p.row_off[i + 1];
+  const int local = (int)(w - ((r0 >> p.c.log2T) + 2 * (int64_t)i));
+  const int seq = p.seqs[i];
+  int len = -1;
+  if ((unsigned)seq < (unsigned)p.c.max_seqs) len = p.c.length[seq];
+  if (local < 0) return;  // rows before row_off[0] belong to no sequence
+  const bool good = r0 >= 0 && r1 >= r0 && r1 <= p.total_rows && len >= r1 - r0 &&
+                    len <= (int64_t)p.c.max_pages * T;
+  if (!good) {
+    if (threadIdx.x == 0) set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
+    return;
+  }
+  const int start = len - (int)(r1 - r0);  // position of row r0
+  const int slot = (start >> p.c.log2T) + local;
+  const int t0 = max(start - slot * T, 0), t1 = min(len - slot * T, T);  // new tokens of this page
+  if (t1 <= t0) return;
+  const int page = p.c.table[(int64_t)seq * p.c.max_pages + slot];
+  if ((unsigned)page >= (unsigned)p.c.pages) {
+    if (threadIdx.x == 0) set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
+    return;
+  }
+  const int64_t block = ((int64_t)p.layer * p.c.pages + page) * H + h;
+  uint8_t* codes = (kv ? p.c.v : p.c.k) + block * T * D;
+  float* scale = (kv ? p.c.v_scale : p.c.k_scale) + block;
+  const int64_t ld = kv ? p.v_row : p.k_row;
+  const uint16_t* src = static_cast<const uint16_t*>(kv ? p.v : p.k) + (r0 + (int64_t)slot * T - start) * ld + (int64_t)h * D;
+  const int vpr = D / 8;  // vectors of a row
+  const int nv = (t1 - t0) * vpr;
+  uint4 x[MAXV];
+  float amax = 0.f;
+#pragma unroll
+  for (int q = 0; q < MAXV; ++q) {
+    const int e = q * 128 + threadIdx.x;
+    if (e < nv) x[q] = ldg_stream(src + (int64_t)(t0 + e / vpr) * ld + (e % vpr) * 8);
+  }
+#pragma unroll
+  for (int q = 0; q < MAXV; ++q) {
+    const int e = q * 128 + threadIdx.x;
+    if (e < nv) {
+      float f[8];
+      unpack8<BF16>(x[q], f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) amax = fmaxf(amax, finite_abs(f[j]));
+    }
+  }
+  amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = amax;
+  const float was = t0 > 0 ? *scale : 0.f;
+  __syncthreads();
+  amax = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  const float need = block_scale(amax);
+  const float now = was > need ? was : need;  // older tokens keep at least their scale
+  if (t0 > 0 && now > was) {
+    // the held codes, rounded again to the larger scale
+    const float ratio = was / now;
+    for (int e = threadIdx.x; e < t0 * D / 16; e += 128) {
+      uint4 r = reinterpret_cast<uint4*>(codes)[e];
+      uint32_t* rw = reinterpret_cast<uint32_t*>(&r);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float f[4];
+        codes4_f32(rw[j], f);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) f[m] *= ratio;
+        rw[j] = f32_codes4(f);
+      }
+      reinterpret_cast<uint4*>(codes)[e] = r;
+    }
+  }
+  const bool exact = is_pow2(now);
+  const float inv = exact ? 1.f / now : 0.f;
+#pragma unroll
+  for (int q = 0; q < MAXV; ++q) {
+    const int e = q * 128 + threadIdx.x;
+    if (e < nv) {
+      float f[8];
+      unpack8<BF16>(x[q], f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = exact ? f[j] * inv : f[j] / now;
+      const float lo[4] = {f[0], f[1], f[2], f[3]}, hi[4] = {f[4], f[5], f[6], f[7]};
+      uint2 out;
+      out.x = f32_codes4(lo);
+      out.y = f32_codes4(hi);
+      *reinterpret_cast<uint2*>(codes + (int64_t)(t0 + e / vpr) * D + (e % vpr) * 8) = out;
+    }
+  }
+  __syncthreads();  // `was` has been read by every thread
+  if (threadIdx.x == 0) *scale = now;
+}
+
+// ---------------------------------------------------------------- page bookkeeping (one CTA)
+
+// Marks the n slots of `seqs`; true (block-wide) if all are in range and listed once.
+__device__ bool mark_slots(const CacheDev& c, const int32_t* seqs, int n, int32_t* marks) {
+  int bad = 0;
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    const int s = seqs[i];
+    if ((unsigned)s >= (unsigned)c.max_seqs || atomicAdd(&marks[s], 1) != 0) bad = 1;
+  }
+  return __syncthreads_or(bad) == 0;
+}
+__device__ void unmark_slots(const CacheDev& c, const int32_t* seqs, int n, int32_t* marks) {
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    const int s = seqs[i];
+    if ((unsigned)s < (unsigned)c.max_seqs) marks[s] = 0;
+  }
+}
+
+// Writes the lowest `want` free pages, ascending, to list; returns how many
+// there are (want, or fewer if the pool has fewer). tmp: 33 ints of shared memory.
+__device__ int find_free(const CacheDev& c, int want, int32_t* list, int* tmp) {
+  int found = 0;
+  const bool vec = (reinterpret_cast<uintptr_t>(c.refs) & 15) == 0;
+  for (int base = 0; base < c.pages && found < want; base += 4 * kPlanThreads) {
+    const int p = base + 4 * threadIdx.x;
+    int r[4] = {1, 1, 1, 1};
+    if (vec && p + 4 <= c.pages) {
+      const int4 q = *reinterpret_cast<const int4*>(c.refs + p);
+      r[0] = q.x;
+      r[1] = q.y;
+      r[2] = q.z;
+      r[3] = q.w;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (p + j < c.pages) r[j] = c.refs[p + j];
+    }
+    int f = 0, total = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f += r[j] == 0;
+    int at = found + block_exclusive_scan(f, tmp, &total);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (r[j] == 0) {
+        if (at < want) list[at] = p + j;
+        ++at;
+      }
+    found += total;
+  }
+  __syncthreads();  // the list is complete for every thread of the block
+  return min(found, want);
+}
+
+struct PlanParams {
+  CacheDev c;
+  int n;
+  const int32_t* a;  // extend: seqs; fork: src; compact: seqs
+  const int32_t* b;  // extend: counts; fork: dst
+  int32_t* marks;
+  int32_t* free_list;
+  int2* new_pages;   // fork: (from, to) of a copied page, or (-1, -1)
+  // compact
+  int32_t* count;
+  int32_t* lead;
+  int32_t* head;
+  int32_t* old_table;
+};
+
+__device__ __forceinline__ int pages_of(int tokens, const CacheDev& c) { return (tokens + c.T - 1) >> c.log2T; }
+
+__global__ void __launch_bounds__(kPlanThreads) extend_kernel(PlanParams p) {
+  __shared__ int tmp[33];
+  const CacheDev& c = p.c;
+  const bool fine = mark_slots(c, p.a, p.n, p.marks);
+  int bad = 0, full = 0;
+  int64_t total = 0;
+  if (fine) {
+    for (int base = 0; base < p.n; base += kPlanThreads) {
+      const int i = base + threadIdx.x;
+      int need = 0, t = 0;
+      if (i < p.n) {
+        const int s = p.a[i], add = p.b[i], len = c.length[s];
+        const int64_t to = (int64_t)len + add;
+        if (add < 0 || len < 0 || len > c.max_pages * c.T) {
+          bad = 1;
+        } else if (to > (int64_t)c.max_pages * c.T) {
+          full = 1;
+        } else {
+          need = pages_of((int)to, c) - pages_of(len, c);
+          // tokens go into a page of the sequence's own
+          if (add > 0 && (len & (c.T - 1))) {
+            const int pg = c.table[(int64_t)s * c.max_pages + (len >> c.log2T)];
+            if ((unsigned)pg >= (unsigned)c.pages || c.refs[pg] != 1) bad = 1;
+          }
+        }
+      }
+      block_exclusive_scan(need, tmp, &t);
+      total += t;
+    }
+  }
+  bad = __syncthreads_or(bad || !fine);
+  full = __syncthreads_or(full) || total > c.pages;
+  const bool ok = !bad && !full && find_free(c, (int)total, p.free_list, tmp) == (int)total;
+  if (ok) {
+    int at = 0;
+    for (int base = 0; base < p.n; base += kPlanThreads) {
+      const int i = base + threadIdx.x;
+      int need = 0, have = 0, s = 0, t = 0, to = 0;
+      if (i < p.n) {
+        s = p.a[i];
+        const int len = c.length[s];
+        to = len + p.b[i];
+        have = pages_of(len, c);
+        need = pages_of(to, c) - have;
+      }
+      int rank = at + block_exclusive_scan(need, tmp, &t);
+      at += t;
+      for (int j = 0; j < need; ++j) {
+        const int pg = p.free_list[rank + j];
+        c.table[(int64_t)s * c.max_pages + have + j] = pg;
+        c.refs[pg] = 1;
+      }
+      if (i < p.n) c.length[s] = to;
+    }
+  } else if (threadIdx.x == 0) {
+    set_status(c.status, bad ? OCCAM_ERR_INVALID_ARG : OCCAM_ERR_CAPACITY);
+  }
+  unmark_slots(c, p.a, p.n, p.marks);
+}
+
+__global__ void __launch_bounds__(kPlanThreads) fork_kernel(PlanParams p) {
+  __shared__ int tmp[33];
+  const CacheDev& c = p.c;
+  const bool fine = mark_slots(c, p.b, p.n, p.marks);
+  int bad = 0;
+  int64_t total = 0;
+  if (fine) {
+    for (int base = 0; base < p.n; base += kPlanThreads) {
+      const int i = base + threadIdx.x;
+      int need = 0, t = 0;
+      if (i < p.n) {
+        const int a = p.a[i], b = p.b[i];
+        p.new_pages[i] = make_int2(-1, -1);
+        if ((unsigned)a >= (unsigned)c.max_seqs || p.marks[a] != 0 || c.length[b] != 0 || c.length[a] < 0 ||
+            c.length[a] > c.max_pages * c.T)
+          bad = 1;
+        else
+          need = (c.length[a] & (c.T - 1)) != 0;
+      }
+      block_exclusive_scan(need, tmp, &t);
+      total += t;
+    }
+    // every page that is shared or copied must be one
+    if (!__syncthreads_or(bad)) {
+      const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+      for (int i = warp; i < p.n; i += kPlanThreads / 32) {
+        const int a = p.a[i], m = pages_of(c.length[a], c);
+        for (int j = lane; j < m; j += 32)
+          if ((unsigned)c.table[(int64_t)a * c.max_pages + j] >= (unsigned)c.pages) bad = 1;
+      }
+    }
+  }
+  bad = __syncthreads_or(bad || !fine);
+  const bool ok = !bad && total <= c.pages && find_free(c, (int)total, p.free_list, tmp) == (int)total;
+  if (ok) {
+    int at = 0;
+    for (int base = 0; base < p.n; base += kPlanThreads) {
+      const int i = base + threadIdx.x;
+      int need = 0, t = 0, a = 0, b = 0, len = 0;
+      if (i < p.n) {
+        a = p.a[i];
+        b = p.b[i];
+        len = c.length[a];
+        need = (len & (c.T - 1)) != 0;
+      }
+      const int rank = at + block_exclusive_scan(need, tmp, &t);
+      at += t;
+      if (need) {
+        const int pg = p.free_list[rank], j = len >> c.log2T;
+        p.new_pages[i] = make_int2(c.table[(int64_t)a * c.max_pages + j], pg);
+        c.table[(int64_t)b * c.max_pages + j] = pg;
+        c.refs[pg] = 1;
+      }
+      if (i < p.n) c.length[b] = len;
+    }
+    // full pages are shared: a warp per pair
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int i = warp; i < p.n; i += kPlanThreads / 32) {
+      const int a = p.a[i], b = p.b[i], m = c.length[a] >> c.log2T;
+      for (int j = lane; j < m; j += 32) {
+        const int pg = c.table[(int64_t)a * c.max_pages + j];
+        c.table[(int64_t)b * c.max_pages + j] = pg;
+        atomicAdd(&c.refs[pg], 1);
+      }
+    }
+  } else {
+    for (int i = threadIdx.x; i < p.n; i += blockDim.x) p.new_pages[i] = make_int2(-1, -1);
+    if (threadIdx.x == 0) set_status(c.status, bad ? OCCAM_ERR_INVALID_ARG : OCCAM_ERR_CAPACITY);
+  }
+  unmark_slots(c, p.b, p.n, p.marks);
+}
+
+// Copies the pages fork_kernel listed: grid (pairs, layers, 2 * chunks), 16 KB a CTA.
+constexpr int kCopyChunk = 16384;
+__global__ void __launch_bounds__(256) copy_pages_kernel(CacheDev c, const int2* pairs, int page_bytes) {
+  const int2 ft = pairs[blockIdx.x];
+  if (ft.x < 0) return;
+  const int layer = blockIdx.y, kv = blockIdx.z & 1, chunk = blockIdx.z >> 1;
+  const int64_t from = (int64_t)layer * c.pages + ft.x, to = (int64_t)layer * c.pages + ft.y;
+  uint8_t* base = kv ? c.v : c.k;
+  const uint4* src = reinterpret_cast<const uint4*>(base + from * page_bytes);
+  uint4* dst = reinterpret_cast<uint4*>(base + to * page_bytes);
+  const int e0 = chunk * (kCopyChunk / 16) + threadIdx.x, n = page_bytes / 16;
+  uint4 x[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    if (e0 + q * 256 < n) x[q] = ldg_stream(src + e0 + q * 256);
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    if (e0 + q * 256 < n) stg_stream(dst + e0 + q * 256, x[q]);
+  if (chunk == 0) {
+    float* sc = kv ? c.v_scale : c.k_scale;
+    for (int h = threadIdx.x; h < c.heads; h += 256) sc[to * c.heads + h] = sc[from * c.heads + h];
+  }
+}
+
+__global__ void __launch_bounds__(256) release_kernel(CacheDev c, int n, const int32_t* seqs) {
+  const int i = blockIdx.y;
+  const int s = seqs[i];
+  if ((unsigned)s >= (unsigned)c.max_seqs) {
+    if (threadIdx.x == 0 && blockIdx.x == 0) set_status(c.status, OCCAM_ERR_INVALID_ARG);
+    return;
+  }
+  const int j = blockIdx.x * 256 + threadIdx.x;
+  if (j < c.max_pages) {
+    // taking the entry makes a slot listed twice give its pages back once
+    int32_t* e = &c.table[(int64_t)s * c.max_pages + j];
+    if (*e != -1) {
+      const int pg = atomicExch(e, -1);
+      if (pg != -1) {
+        if ((unsigned)pg >= (unsigned)c.pages)
+          set_status(c.status, OCCAM_ERR_INVALID_ARG);
+        else
+          atomicSub(&c.refs[pg], 1);
+      }
+    }
+  }
+  if (j == 0) c.length[s] = 0;
+}
+
+// ---------------------------------------------------------------- compact
+struct CountParams {
+  CacheDev c;
+  const int32_t* seqs;
+  const uint8_t* keep;
+  const int64_t* keep_off;
+  int64_t total_keep;
+  int32_t* count;
+  int32_t* lead;
+  int2* info;  // (listed tokens, flags)
+  int32_t* list;
+};
+
+// One CTA per sequence: the positions of its kept flagged tokens, in order, to
+// list[keep_off[i] ..], their number and the number of leading full pages
+// that keep every token. count = -1 marks bad offsets.
+__global__ void __launch_bounds__(1024) compact_count_kernel(CountParams p) {
+  __shared__ int tmp[33];
+  __shared__ int first;
+  const int i = blockIdx.x;
+  const int s = p.seqs[i];
+  const int64_t k0 = p.keep_off[i], k1 = p.keep_off[i + 1];
+  const int len = (unsigned)s < (unsigned)p.c.max_seqs ? p.c.length[s] : -1;
+  if (len < 0 || len > p.c.max_pages * p.c.T || k0 < 0 || k1 < k0 || k1 > p.total_keep) {
+    if (threadIdx.x == 0) p.count[i] = -1;
+    return;
+  }
+  const int flags = (int)(k1 - k0 < len ? k1 - k0 : len);
+  if (threadIdx.x == 0) first = len;  // first dropped position
+  __syncthreads();
+  int n = 0, mine = len;
+  for (int base = 0; base < flags; base += 1024) {
+    const int pos = base + threadIdx.x;
+    const int k = pos < flags && p.keep[k0 + pos] != 0;
+    if (pos < flags && !k) mine = min(mine, pos);
+    int t = 0;
+    const int at = n + block_exclusive_scan(k, tmp, &t);
+    if (k) p.list[k0 + at] = pos;
+    n += t;
+  }
+  mine = __reduce_min_sync(0xffffffffu, mine);
+  if ((threadIdx.x & 31) == 0) atomicMin(&first, mine);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    p.count[i] = n + (len - flags);  // tokens past the flags stay
+    p.info[i] = make_int2(n, flags);
+    p.lead[i] = first >> p.c.log2T;
+  }
+}
+
+// New page tables: head[i] = index of sequence i's first new page in free_list.
+__global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(PlanParams p) {
+  __shared__ int tmp[33];
+  const CacheDev& c = p.c;
+  const bool fine = mark_slots(c, p.a, p.n, p.marks);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int bad = 0;
+  int64_t total = 0;
+  if (fine) {
+    for (int base = 0; base < p.n; base += kPlanThreads) {
+      const int i = base + threadIdx.x;
+      int need = 0, t = 0;
+      if (i < p.n) {
+        if (p.count[i] < 0)
+          bad = 1;
+        else
+          need = max(pages_of(p.count[i], c) - p.lead[i], 0);
+      }
+      const int at = (int)min(total, (int64_t)0x3fffffff) + block_exclusive_scan(need, tmp, &t);
+      if (i < p.n) p.head[i] = at;
+      total += t;
+    }
+    if (!__syncthreads_or(bad)) {
+      for (int i = warp; i < p.n; i += kPlanThreads / 32) {
+        const int s = p.a[i], m = pages_of(c.length[s], c);
+        for (int j = lane; j < m; j += 32)
+          if ((unsigned)c.table[(int64_t)s * c.max_pages + j] >= (unsigned)c.pages) bad = 1;
+      }
+    }
+  }
+  bad = __syncthreads_or(bad || !fine);
+  const bool ok = !bad && total <= c.pages && find_free(c, (int)total, p.free_list, tmp) == (int)total;
+  if (ok) {
+    // pages leave their sequence before new ones come in: the new ones were
+    // free at the start of the call, so the two sets do not meet
+    for (int i = warp; i < p.n; i += kPlanThreads / 32) {
+      const int s = p.a[i], lead = p.lead[i], m = pages_of(c.length[s], c);
+      const int to = pages_of(p.count[i], c), head = p.head[i];
+      for (int j = lane; j < max(m, to); j += 32) {
+        int32_t* e = &c.table[(int64_t)s * c.max_pages + j];
+        if (j < m) {
+          const int pg = *e;
+          p.old_table[(int64_t)i * c.max_pages + j] = pg;
+          if (j >= lead) atomicSub(&c.refs[pg], 1);
+        }
+        if (j >= lead) {
+          const bool fresh = j < to;
+          const int pg = fresh ? p.free_list[head + j - lead] : -1;
+          *e = pg;
+          if (fresh) atomicAdd(&c.refs[pg], 1);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) c.length[s] = p.count[i];
+    }
+    if (threadIdx.x == 0) p.head[p.n] = (int)total;
+  } else {
+    if (threadIdx.x == 0) {
+      p.head[p.n] = 0;  // nothing to move
+      set_status(c.status, bad ? OCCAM_ERR_INVALID_ARG : OCCAM_ERR_CAPACITY);
+    }
+  }
+  unmark_slots(c, p.a, p.n, p.marks);
+}
+
+struct MoveParams {
+  CacheDev c;
+  int n, dim, layer0, layers;
+  const int32_t* free_list;
+  const int32_t* head;
+  const int32_t* lead;
+  const int32_t* count;
+  const int32_t* old_table;
+  const int2* info;
+  const int32_t* list;
+  const int64_t* keep_off;
+};
+
+// One CTA per (new page, layer, K or V, group of heads), a block of codes at
+// a time: the kept rows are gathered once, their common scale found, the codes
+// rounded to it (a shift of the exponent where both scales are powers of
+// two) and written once. Bound by HBM.
+// MAXV: 16-code vectors a thread holds (128 threads).
+constexpr int kMoveHeads = 4;
+template <int MAXV>
+__global__ void __launch_bounds__(128) compact_move_kernel(MoveParams p) {
+  __shared__ int2 src[128];  // page and slot of each token
+  __shared__ float red[2][4];
+  const int T = p.c.T, D = p.dim, H = p.c.heads, vpr = D / 16;
+  const int hg = (H + kMoveHeads - 1) / kMoveHeads;
+  const int64_t items = (int64_t)p.head[p.n] * p.layers * 2 * hg;
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    int64_t rest = item;
+    const int g = (int)(rest % hg);
+    rest /= hg;
+    const int kv = (int)(rest & 1);
+    rest >>= 1;
+    const int layer = p.layer0 + (int)(rest % p.layers);
+    const int fresh = (int)(rest / p.layers);
+    // the sequence whose new pages include this one (head is ascending)
+    int lo = 0, hi = p.n;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (p.head[mid] <= fresh) lo = mid; else hi = mid;
+    }
+    const int i = lo;
+    const int first = (p.lead[i] + fresh - p.head[i]) * T;  // new position of the page's first token
+    const int tokens = min(p.count[i] - first, T);
+    __syncthreads();
+    if ((int)threadIdx.x < tokens) {
+      // kept flagged tokens come from the list, tokens past the flags in order
+      const int q = first + threadIdx.x;
+      const int2 info = p.info[i];  // listed tokens, flags
+      const int pos = q < info.x ? p.list[p.keep_off[i] + q] : info.y + q - info.x;
+      src[threadIdx.x] = make_int2(p.old_table[(int64_t)i * p.c.max_pages + (pos >> p.c.log2T)], pos & (T - 1));
+    }
+    __syncthreads();
+    const uint8_t* from = kv ? p.c.v : p.c.k;
+    uint8_t* to = kv ? p.c.v : p.c.k;
+    float* sc = kv ? p.c.v_scale : p.c.k_scale;
+    const int64_t layer_page = (int64_t)layer * p.c.pages;
+    const int64_t new_block = (layer_page + p.free_list[fresh]) * H;
+    const int nv = tokens * vpr;
+    for (int h = g * kMoveHeads; h < min((g + 1) * kMoveHeads, H); ++h) {
+      uint4 x[MAXV];
+      float s[MAXV];
+      float amax = 0.f;
+#pragma unroll
+      for (int q = 0; q < MAXV; ++q) {
+        const int e = q * 128 + threadIdx.x;
+        if (e < nv) {
+          const int2 ps = src[e / vpr];
+          const int64_t block = (layer_page + ps.x) * H + h;
+          x[q] = ldg_stream(from + (block * T + ps.y) * D + (e % vpr) * 16);
+          s[q] = sc[block];
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < MAXV; ++q) {
+        const int e = q * 128 + threadIdx.x;
+        if (e < nv) {
+          const uint32_t* w = reinterpret_cast<const uint32_t*>(&x[q]);
+          float m = 0.f;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float f[4];
+            codes4_f32(w[j], f);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) m = fmaxf(m, fabsf(f[k]));  // a NaN code is passed over
+          }
+          amax = fmaxf(amax, finite_abs(m * s[q]));
+        }
+      }
+      amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
+      if ((threadIdx.x & 31) == 0) red[h & 1][threadIdx.x >> 5] = amax;
+      __syncthreads();
+      const float* r = red[h & 1];
+      const float now = block_scale(fmaxf(fmaxf(r[0], r[1]), fmaxf(r[2], r[3])));
+      const float inv = 1.f / now;  // exact: now is a power of two
+      uint8_t* out = to + (new_block + h) * T * D;
+#pragma unroll
+      for (int q = 0; q < MAXV; ++q) {
+        const int e = q * 128 + threadIdx.x;
+        if (e < nv) {
+          uint32_t* w = reinterpret_cast<uint32_t*>(&x[q]);
+          if (s[q] != now) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              float f[4];
+              codes4_f32(w[j], f);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) f[k] = f[k] * s[q] * inv;
+              w[j] = f32_codes4(f);
+            }
+          }
+          stg_stream(out + e * 16, x[q]);
+        }
+      }
+      if (threadIdx.x == 0) sc[new_block + h] = now;
+    }
+  }
+}
+
+int last_error() { return cudaGetLastError() == cudaSuccess ? OCCAM_OK : OCCAM_ERR_CUDA; }
+
+PlanParams plan_params(const occam_cache* c, void* ws, const CacheWs& w, int n) {
+  PlanParams p{};
+  p.c = cache_dev(c, ws, w);
+  p.n = n;
+  p.marks = ws_at<int32_t>(ws, w.marks);
+  p.free_list = ws_at<int32_t>(ws, w.free_list);
+  p.new_pages = ws_at<int2>(ws, w.new_pages);
+  p.count = ws_at<int32_t>(ws, w.count);
+  p.lead = ws_at<int32_t>(ws, w.lead);
+  p.head = ws_at<int32_t>(ws, w.head);
+  p.old_table = ws_at<int32_t>(ws, w.old_table);
+  return p;
+}
+
+template <bool BF16>
+void launch_append(const AppendParams& p, unsigned grid, cudaStream_t st) {
+  const int vecs = p.c.T * p.dim / 8 / 128;
+  if (vecs <= 2)
+    append_kernel<BF16, 2><<<grid, 128, 0, st>>>(p);
+  else if (vecs == 4)
+    append_kernel<BF16, 4><<<grid, 128, 0, st>>>(p);
+  else if (vecs == 8)
+    append_kernel<BF16, 8><<<grid, 128, 0, st>>>(p);
+  else
+    append_kernel<BF16, 16><<<grid, 128, 0, st>>>(p);
+}
+
+}  // namespace
+
+#define OCCAM_TRY(x)                 \
+  do {                               \
+    int _rc = (x);                   \
+    if (_rc != OCCAM_OK) return _rc; \
+  } while (0)
+
+extern "C" {
+
+int occam_cache_workspace_size(const occam_cache* cache, int64_t max_tokens, size_t* bytes) {
+  if (!bytes || max_tokens < 0) return OCCAM_ERR_INVALID_ARG;
+  OCCAM_TRY(check_cache(cache));
+  *bytes = cache_ws(cache, max_tokens).total;
+  return OCCAM_OK;
+}
+
+int occam_cache_extend(const occam_cache* cache, int32_t n, const int32_t* seqs, const int32_t* counts,
+                       void* workspace, size_t workspace_bytes, occam_stream_t stream) {
+  const NvtxRange nvtx("occam_cache_extend");
+  launch_counter() = 0;
+  OCCAM_TRY(check_cache(cache));
+  if (n < 0 || n > cache->max_seqs || (n > 0 && (!seqs || !counts))) return OCCAM_ERR_INVALID_ARG;
+  CacheWs w;
+  OCCAM_TRY(check_cache_ws(cache, 0, workspace, workspace_bytes, &w));
+  if (n == 0) return OCCAM_OK;
+  PlanParams p = plan_params(cache, workspace, w, n);
+  p.a = seqs;
+  p.b = counts;
+  extend_kernel<<<1, kPlanThreads, 0, reinterpret_cast<cudaStream_t>(stream)>>>(p);
+  count_launch();
+  return last_error();
+}
+
+int occam_cache_append(const occam_cache* cache, int32_t layer, int32_t dtype, int64_t total_rows, const void* k,
+                       int64_t k_row, const void* v, int64_t v_row, int32_t n, const int32_t* seqs,
+                       const int64_t* row_off, void* workspace, size_t workspace_bytes, occam_stream_t stream) {
+  const NvtxRange nvtx("occam_cache_append");
+  launch_counter() = 0;
+  OCCAM_TRY(check_cache(cache));
+  if (dtype != OCCAM_BF16 && dtype != OCCAM_F16) return OCCAM_ERR_UNSUPPORTED;
+  if (layer < 0 || layer >= cache->layers || total_rows < 0 || total_rows > 0x7fffffff || n < 0 || n > cache->max_seqs)
+    return OCCAM_ERR_INVALID_ARG;
+  CacheWs w;
+  OCCAM_TRY(check_cache_ws(cache, 0, workspace, workspace_bytes, &w));
+  if (n == 0 || total_rows == 0) return OCCAM_OK;
+  const int64_t row = (int64_t)cache->heads * cache->dim;
+  if (!k || !v || !seqs || !row_off || !aligned16(k) || !aligned16(v) || k_row < row || v_row < row || (k_row & 7) || (v_row & 7))
+    return OCCAM_ERR_INVALID_ARG;
+  AppendParams p{};
+  p.c = cache_dev(cache, workspace, w);
+  p.layer = layer;
+  p.n = n;
+  p.dim = cache->dim;
+  p.total_rows = total_rows;
+  p.k_row = k_row;
+  p.v_row = v_row;
+  p.k = k;
+  p.v = v;
+  p.seqs = seqs;
+  p.row_off = row_off;
+  const int64_t grid = (total_rows / cache->page_tokens + 2 * (int64_t)n) * cache->heads * 2;
+  if (grid > 0x7fffffff) return OCCAM_ERR_UNSUPPORTED;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  if (dtype == OCCAM_BF16)
+    launch_append<true>(p, (unsigned)grid, st);
+  else
+    launch_append<false>(p, (unsigned)grid, st);
+  count_launch();
+  return last_error();
+}
+
+int occam_cache_fork(const occam_cache* cache, int32_t n, const int32_t* src, const int32_t* dst, void* workspace,
+                     size_t workspace_bytes, occam_stream_t stream) {
+  const NvtxRange nvtx("occam_cache_fork");
+  launch_counter() = 0;
+  OCCAM_TRY(check_cache(cache));
+  if (n < 0 || n > cache->max_seqs || (n > 0 && (!src || !dst))) return OCCAM_ERR_INVALID_ARG;
+  CacheWs w;
+  OCCAM_TRY(check_cache_ws(cache, 0, workspace, workspace_bytes, &w));
+  if (n == 0) return OCCAM_OK;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  PlanParams p = plan_params(cache, workspace, w, n);
+  p.a = src;
+  p.b = dst;
+  fork_kernel<<<1, kPlanThreads, 0, st>>>(p);
+  count_launch();
+  const int page_bytes = cache->heads * cache->page_tokens * cache->dim;
+  const int chunks = (page_bytes + kCopyChunk - 1) / kCopyChunk;
+  copy_pages_kernel<<<dim3((unsigned)n, (unsigned)cache->layers, (unsigned)(2 * chunks)), 256, 0, st>>>(p.c, p.new_pages, page_bytes);
+  count_launch();
+  return last_error();
+}
+
+int occam_cache_compact(const occam_cache* cache, int32_t layer_begin, int32_t layer_end, int32_t n,
+                        const int32_t* seqs, const uint8_t* keep, const int64_t* keep_off, int64_t total_keep,
+                        void* workspace, size_t workspace_bytes, occam_stream_t stream) {
+  const NvtxRange nvtx("occam_cache_compact");
+  launch_counter() = 0;
+  OCCAM_TRY(check_cache(cache));
+  if (layer_begin < 0 || layer_end < layer_begin || layer_end > cache->layers || n < 0 || n > cache->max_seqs ||
+      total_keep < 0 || (n > 0 && (!seqs || !keep_off)) || (total_keep > 0 && !keep))
+    return OCCAM_ERR_INVALID_ARG;
+  CacheWs w;
+  OCCAM_TRY(check_cache_ws(cache, total_keep, workspace, workspace_bytes, &w));
+  if (n == 0) return OCCAM_OK;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  PlanParams p = plan_params(cache, workspace, w, n);
+  p.a = seqs;
+  CountParams q{};
+  q.c = p.c;
+  q.seqs = seqs;
+  q.keep = keep;
+  q.keep_off = keep_off;
+  q.total_keep = total_keep;
+  q.count = p.count;
+  q.lead = p.lead;
+  q.info = p.new_pages;
+  q.list = ws_at<int32_t>(workspace, w.list);
+  compact_count_kernel<<<n, 1024, 0, st>>>(q);
+  count_launch();
+  compact_plan_kernel<<<1, kPlanThreads, 0, st>>>(p);
+  count_launch();
+  if (layer_end > layer_begin) {
+    MoveParams m{};
+    m.c = p.c;
+    m.n = n;
+    m.dim = cache->dim;
+    m.layer0 = layer_begin;
+    m.layers = layer_end - layer_begin;
+    m.free_list = p.free_list;
+    m.head = p.head;
+    m.lead = p.lead;
+    m.count = p.count;
+    m.old_table = p.old_table;
+    m.info = p.new_pages;
+    m.list = q.list;
+    m.keep_off = keep_off;
+    const int vecs = cache->page_tokens * cache->dim / 16 / 128;
+    const unsigned grid = (unsigned)cache_sms() * 12;
+    if (vecs <= 1)
+      compact_move_kernel<1><<<grid, 128, 0, st>>>(m);
+    else if (vecs == 2)
+      compact_move_kernel<2><<<grid, 128, 0, st>>>(m);
+    else if (vecs == 4)
+      compact_move_kernel<4><<<grid, 128, 0, st>>>(m);
+    else
+      compact_move_kernel<8><<<grid, 128, 0, st>>>(m);
+    count_launch();
+  }
+  return last_error();
+}
+
+int occam_cache_release(const occam_cache* cache, int32_t n, const int32_t* seqs, void* workspace,
+                        size_t workspace_bytes, occam_stream_t stream) {
+  const NvtxRange nvtx("occam_cache_release");
+  launch_counter() = 0;
+  OCCAM_TRY(check_cache(cache));
+  if (n < 0 || n > cache->max_seqs || (n > 0 && !seqs)) return OCCAM_ERR_INVALID_ARG;
+  CacheWs w;
+  OCCAM_TRY(check_cache_ws(cache, 0, workspace, workspace_bytes, &w));
+  if (n == 0) return OCCAM_OK;
+  release_kernel<<<dim3((unsigned)((cache->max_pages + 255) / 256), (unsigned)n), 256, 0,
+                   reinterpret_cast<cudaStream_t>(stream)>>>(cache_dev(cache, workspace, w), n, seqs);
+  count_launch();
+  return last_error();
+}
+
+}  // extern "C"
