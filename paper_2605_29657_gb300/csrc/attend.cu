@@ -26,6 +26,7 @@
 #include <cmath>
 
 #include "attend.cuh"
+#include "attend_tc.cuh"
 #include "nvtx.cuh"
 
 using namespace occam;
@@ -35,6 +36,7 @@ namespace {
 constexpr int kTile = 32;   // keys of a unit
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
+constexpr int kFewRows = 32;  // query rows of a key head this file's kernel is used for
 constexpr float kRhoKeep = 1.f / 64.f;           // P is scaled down by v's scales at most this far
 constexpr float kRhoSpan = 8.6736174e-19f;       // 2^-60
 
@@ -120,15 +122,9 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
 
   int i = w.seq;
   SeqInfo s = attend_seq(p, i);
-  int64_t hu = head_units<R, kTile>(p, s);
-  if (hu == 0) return;
-  int h = (int)(w.in_seq / hu), rt = 0;
-  int64_t in_item = w.in_seq - h * hu;
-  int tiles = key_tiles<R, kTile>(p, s, 0);
-  while (in_item >= tiles) {
-    in_item -= tiles;
-    tiles = key_tiles<R, kTile>(p, s, ++rt);
-  }
+  int h = w.head, rt = w.row_tile;
+  int64_t in_item = w.tile;
+  int tiles = key_tiles<R, kTile>(p, s, rt);
 
   for (int64_t u = w.u0; u < w.u1;) {
     const int ta = (int)in_item, tb = (int)min((int64_t)tiles, ta + (w.u1 - u));
@@ -155,7 +151,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
       const int r = nq * 8 + g;
       float x[KC][16];
       float amax = 0.f;
-      const int row = rt * R + r, j = row / p.G;
+      const int row = rt * R + r, j = div_group(p, row);
       const uint16_t* q = p.q + (s.row0 + j) * p.q_row + (int64_t)(h * p.G + row - j * p.G) * D;
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
@@ -189,11 +185,11 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
       for (int k = 0; k < 2; ++k) {
         qscale[nq][k] = __shfl_sync(0xffffffffu, down, (2 * t + k) * 4);
         const int rr = nq * 8 + 2 * t + k;
-        limit[nq][k] = rr >= rows ? 0 : p.causal ? s.len - s.rows + (rt * R + rr) / p.G + 1 : s.len;
+        limit[nq][k] = rr >= rows ? 0 : p.causal ? s.len - s.rows + div_group(p, rt * R + rr) + 1 : s.len;
       }
     }
     // keys that every row of the tile sees
-    const int common = p.causal ? s.len - s.rows + (rt * R) / p.G + 1 : s.len;
+    const int common = p.causal ? s.len - s.rows + div_group(p, rt * R) + 1 : s.len;
 
     float o[NQ][MT][4], m[NQ][2], l[NQ][2];
 #pragma unroll
@@ -442,7 +438,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
         sum += sh_l[k][r] * f;
         acc += sh_o[(k * R + r) * D + d] * f;
       }
-      const int row = rt * R + r, j = row / p.G;
+      const int row = rt * R + r, j = div_group(p, row);
       if (sh_nan[d] < (p.causal ? s.len - s.rows + j + 1 : s.len)) acc = __int_as_float(0x7fc00000);
       if (whole) {
         const int64_t to = (s.row0 + j) * p.H + h * p.G + row - j * p.G;
@@ -476,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
             acc = acc * f0 + x * f1;
             mx = mn;
           }
-          const int row = rt * R + r, j = row / p.G;
+          const int row = rt * R + r, j = div_group(p, row);
           const int64_t to = (s.row0 + j) * p.H + h * p.G + row - j * p.G;
           p.out[to * D + d] = out_bits(sum == 0.f ? 0.f : acc / sum, p.bf16);
           if (d == 0 && p.lse) p.lse[to] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.69314718056f;
@@ -547,6 +543,11 @@ extern "C" int occam_cache_attend(const occam_cache* cache, const occam_attend_a
   p.n = a->n;
   p.H = a->heads;
   p.G = G;
+  // ceil(2^(31 + s) / G) with 2^s >= G: exact for 31-bit numbers
+  uint32_t sh = 0;
+  while ((1 << sh) < G) ++sh;
+  p.g_shift = 31 + sh;
+  p.g_mul = (uint32_t)(((uint64_t(1) << p.g_shift) + G - 1) / G);
   p.causal = a->causal ? 1 : 0;
   p.bf16 = a->dtype == OCCAM_BF16;
   p.row_lo = 0;
@@ -567,7 +568,17 @@ extern "C" int occam_cache_attend(const occam_cache* cache, const occam_attend_a
   p.part_o = ws_at<float>(workspace, w.part_o);
   p.part_ml = ws_at<float2>(workspace, w.part_ml);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  const bool few = (int64_t)a->max_rows * G <= 8;
+  // Sequences with more than kFewRows query rows a key head go to the
+  // tensor-core kernel, the others are this file's; one launch where the rows allow only one of them.
+  const int64_t most = (int64_t)a->max_rows * G;
+  if (most > kFewRows) {
+    p.row_lo = a->n == 1 ? 0 : kFewRows;
+    OCCAM_TRY(launch_attend_tc(p, cache->dim, st));
+    if (a->n == 1) return OCCAM_OK;  // whatever its rows are
+    p.row_lo = 0;
+    p.row_hi = kFewRows;
+  }
+  const bool few = most <= 8;
   if (cache->dim == 128) return few ? launch_rows<128, 1>(p, st) : launch_rows<128, 2>(p, st);
   return few ? launch_rows<64, 1>(p, st) : launch_rows<64, 2>(p, st);
 }

@@ -27,6 +27,7 @@ struct AttendParams {
   const uint8_t* keep;
   const int64_t* keep_off;
   float scale_log2;
+  uint32_t g_mul, g_shift;  // x / G = x g_mul >> g_shift for 0 <= x < 2^31
   int32_t* counters;
   float* part_o;
   float2* part_ml;
@@ -59,31 +60,57 @@ __device__ __forceinline__ SeqInfo attend_seq(const AttendParams& p, int i) {
   return s;
 }
 
+__device__ __forceinline__ int div_group(const AttendParams& p, int x) {
+  return (int)(((uint64_t)(uint32_t)x * p.g_mul) >> p.g_shift);
+}
+
 // Key tiles of KT keys that row tile rt (R rows) of a sequence can see, at least one.
 template <int R, int KT>
 __device__ __forceinline__ int key_tiles(const AttendParams& p, const SeqInfo& s, int rt) {
   int keys = s.len;
-  if (p.causal) keys = s.len - s.rows + min((rt + 1) * R - 1, s.rows * p.G - 1) / p.G + 1;
+  if (p.causal) keys = s.len - s.rows + div_group(p, min((rt + 1) * R - 1, s.rows * p.G - 1)) + 1;
   return (keys + KT - 1) / KT;
+}
+// sum of floor((a i + b) / m) over i = 0 .. n-1 (a, b >= 0): quotients are taken
+// out, and the lattice points under the rest of the line are counted along
+// the other axis
+static __device__ __noinline__ int64_t floor_sum(int64_t n, int64_t m, int64_t a, int64_t b) {
+  int64_t sum = 0;
+  for (;;) {
+    sum += (a / m) * (n * (n - 1) / 2) + (b / m) * n;
+    a %= m;
+    b %= m;
+    const int64_t y = a * n + b;
+    if (y < m) return sum;
+    n = y / m;
+    b = y % m;
+    const int64_t t = m;
+    m = a;
+    a = t;
+  }
+}
+// Key tiles of the first nrt row tiles of a sequence's head. Row tile rt < the last sees
+// base + 1 + floor(((rt + 1) R - 1) / G) keys.
+template <int R, int KT>
+__device__ __forceinline__ int64_t tiles_before(const AttendParams& p, const SeqInfo& s, int nrt) {
+  if (!p.causal) return (int64_t)nrt * ((s.len + KT - 1) / KT);
+  return floor_sum(nrt, (int64_t)p.G * KT, R, R - 1 + (int64_t)p.G * (s.len - s.rows + KT));
 }
 template <int R, int KT>
 __device__ __forceinline__ int64_t head_units(const AttendParams& p, const SeqInfo& s) {
   if (s.rows == 0) return 0;
   const int nrt = (s.rows * p.G + R - 1) / R;
-  if (!p.causal) return (int64_t)nrt * ((s.len + KT - 1) / KT);
-  int64_t u = 0;
-  for (int rt = 0; rt < nrt; ++rt) u += key_tiles<R, KT>(p, s, rt);
-  return u;
+  return (nrt > 1 ? tiles_before<R, KT>(p, s, nrt - 1) : 0) + key_tiles<R, KT>(p, s, nrt - 1);
 }
 
-// The stretch [u0, u1) of the CTA and the sequence its first unit is in.
+// The stretch [u0, u1) of the CTA and the item its first unit is in.
 struct Stretch {
-  int64_t units, u0, u1, in_seq;  // in_seq: u0 relative to the sequence's first unit
-  int ctas, seq;
+  int64_t units, u0, u1;
+  int ctas, seq, head, row_tile, tile;  // tile: u0's key tile in the item
 };
 
 __device__ __forceinline__ int64_t cta_begin(int64_t units, int ctas, int c) { return units * c / ctas; }
-__device__ __forceinline__ int cta_of(int64_t units, int ctas, int64_t u) {
+static __device__ __noinline__ int cta_of(int64_t units, int ctas, int64_t u) {
   int c = (int)(u * ctas / units);
   while (c + 1 < ctas && cta_begin(units, ctas, c + 1) <= u) ++c;
   while (c > 0 && cta_begin(units, ctas, c) > u) --c;
@@ -121,18 +148,31 @@ __device__ __forceinline__ bool attend_stretch(const AttendParams& p, int min_un
   w.u1 = cta_begin(total, w.ctas, blockIdx.x + 1);
   int64_t at = before + incl - mine;
   if (w.u0 >= at && w.u0 < at + mine) {
-    int i = i0;
-    for (;; ++i) {
-      const int64_t u = p.c.heads * head_units<R, KT>(p, attend_seq(p, i));
-      if (w.u0 < at + u || i + 1 >= i1) break;
-      at += u;
+    for (int i = i0; i < i1; ++i) {
+      const SeqInfo s = attend_seq(p, i);
+      const int64_t hu = head_units<R, KT>(p, s);
+      if (w.u0 < at + p.c.heads * hu) {
+        const int64_t off = w.u0 - at;
+        const int64_t h = off / hu, in_head = off - h * hu;
+        int lo = 0, hi = (s.rows * p.G + R - 1) / R;  // the last row tile that begins at or before in_head
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (tiles_before<R, KT>(p, s, mid) <= in_head) lo = mid; else hi = mid;
+        }
+        sh[NWARP] = i;
+        sh[NWARP + 1] = h;
+        sh[NWARP + 2] = lo;
+        sh[NWARP + 3] = in_head - (lo ? tiles_before<R, KT>(p, s, lo) : 0);
+        break;
+      }
+      at += p.c.heads * hu;
     }
-    sh[NWARP] = i;
-    sh[NWARP + 1] = w.u0 - at;
   }
   __syncthreads();
   w.seq = (int)sh[NWARP];
-  w.in_seq = sh[NWARP + 1];
+  w.head = (int)sh[NWARP + 1];
+  w.row_tile = (int)sh[NWARP + 2];
+  w.tile = (int)sh[NWARP + 3];
   return true;
 }
 

@@ -1,0 +1,981 @@
+// attend_tc.cu -- attention over the paged 8-bit cache for many query rows per
+// key head (questions, prefixes), on the fifth-generation tensor cores.
+//
+// The same running softmax as attend.cu, for 256 query rows (token, head of
+// the group) against tiles of 128 keys. Bound by the tensor cores and the
+// exponentials: 4 D operations and one exponential a (row, key).
+// One CTA an SM, 16 warps in four roles:
+//  - warps 8-11 fetch the codes of a key tile, a page's rows at a time, and
+//    write them to shared memory as f16 (exact) in the matrix layout (128-byte
+//    swizzle), two stages deep, the next tile's loads in flight meanwhile;
+//  - one thread of warp 12 issues the products: S = Q K^T into tensor memory,
+//    O += P V with P read from tensor memory, for two row tiles of 128 in turn,
+//    so that one tile's softmax runs under the other's products;
+//  - warps 0-3 and 4-7 hold a row a thread: scores from tensor memory, maximum,
+//    exponentials, P back over the scores as f16.
+// O stays in tensor memory. It is rescaled only where a row's maximum grew by more than
+// 2^8 since its last reference, or where v's scale left the window that P
+// is held in; both references are undone at the end.
+// Which tile comes next is decided by the fetching warps (tiles without a seen key are left out; a tile whose
+// scales of v lie more than 2^6 apart is taken 16 keys at a time), told to the others through
+// a ring of step records.
+#include <algorithm>
+#include <atomic>
+#include <type_traits>
+
+#include "attend.cuh"
+#include "attend_tc.cuh"
+#include "tc5.cuh"
+
+using namespace occam;
+
+namespace {
+
+constexpr int kR = 256;        // query rows of an item
+constexpr int kK = 128;        // keys of a tile
+constexpr int kGroup = 16;     // keys that share a page at least
+constexpr int kThreads = 512;
+constexpr int kRing = 4;
+constexpr int kRegSoftmax = 136, kRegFetch = 160, kRegIssue = 80;  // 2 x 136 + 160 + 80 = 4 x 128
+constexpr uint64_t kWaitNs = 2000000000ull;
+constexpr float kLazy = 8.f;             // log2 growth of a maximum before O is rescaled
+constexpr float kLeast = 1.2e-38f;       // a score's factor: never 0, so that a hidden key's -inf stays
+constexpr float kRhoKeep = 1.f / 64.f;
+constexpr float kRhoSpan = 8.6736174e-19f;  // 2^-60
+
+struct Step {
+  int tile;
+  int end;            // 1: no more steps of this segment (an item, or the CTA's part of one); 2: nor segments
+  int row_tiles;      // 1 or 2
+  uint32_t seen[4];   // bit k: key k of the tile may be seen
+  float ks[8];        // scale of k, per 16 keys
+  float lr[8];        // log2(scale of v / rho)
+  float rr[8];        // rho / scale of v
+  float fall;         // O's factor: rho before / rho now
+  float rho;
+};
+
+struct Shared {
+  uint64_t q_full, k_full[2], k_free[2], v_full[2], v_free[2], s_full[2], p_full[2], o_done[2], step_full[kRing],
+      step_free[kRing], meet, drain;
+  Step step[kRing];
+  int64_t scan[kThreads / 32 + 4];
+  uint32_t tmem;
+  int stop;            // a wait ran out
+  int last;
+  int any_nan[4];
+  int nan_first[4][128];
+};
+
+__device__ __forceinline__ uint64_t desc_kmajor(uint32_t saddr) { return tc::sdesc_sw128(saddr); }
+// rows of the summed index, 64 columns (128 bytes) a block, blocks 16 KB apart
+__device__ __forceinline__ uint64_t desc_mnmajor(uint32_t saddr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr >> 4) & 0x3FFF);
+  d |= (uint64_t)(16384 >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+// f16 operands, fp32 sums; B with the summed index along its rows if trans_b
+__host__ __device__ constexpr uint32_t idesc_f16(int M, int N, bool trans_b) {
+  return (1u << 4) | ((trans_b ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+// A from tensor memory
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t accum) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b), "r"(idesc), "r"(accum)
+      : "memory");
+}
+// one lane of a converged warp
+__device__ __forceinline__ bool elect_one() {
+  uint32_t yes;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+  return yes != 0;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(*reinterpret_cast<uint64_t*>(&d))
+      : "l"(*reinterpret_cast<uint64_t*>(&a)), "l"(*reinterpret_cast<uint64_t*>(&b)), "l"(*reinterpret_cast<uint64_t*>(&c)));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(*reinterpret_cast<uint64_t*>(&d))
+      : "l"(*reinterpret_cast<uint64_t*>(&a)), "l"(*reinterpret_cast<uint64_t*>(&b)));
+  return d;
+}
+// waits for this thread's tensor-memory loads; v is only there afterwards
+__device__ __forceinline__ void wait_ld(uint32_t (&v)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]),
+                 "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]),
+                 "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]),
+                 "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])
+               :
+               : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+      "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+      : "memory");
+}
+
+// The item (sequence, head, row tile) a role is at, and its walk along the CTA's stretch.
+struct Walk {
+  SeqInfo s;
+  int i, h, rt, tiles, ta, tb;
+  int64_t u;
+};
+__device__ __forceinline__ void walk_begin(const AttendParams& p, const Stretch& w, Walk& x) {
+  x.i = w.seq;
+  x.s = attend_seq(p, x.i);
+  x.h = w.head;
+  x.rt = w.row_tile;
+  x.tiles = key_tiles<kR, kK>(p, x.s, x.rt);
+  x.u = w.u0;
+  x.ta = w.tile;
+  x.tb = (int)min((int64_t)x.tiles, x.ta + (w.u1 - x.u));
+}
+// False at the end of the stretch.
+__device__ __forceinline__ bool walk_next(const AttendParams& p, const Stretch& w, Walk& x) {
+  x.u += x.tb - x.ta;
+  if (x.u >= w.u1) return false;
+  const int nrt = (x.s.rows * p.G + kR - 1) / kR;
+  if (++x.rt == nrt) {
+    x.rt = 0;
+    if (++x.h == p.c.heads) {
+      x.h = 0;
+      do {
+        x.s = attend_seq(p, ++x.i);
+      } while (x.s.rows == 0);
+    }
+  }
+  x.tiles = key_tiles<kR, kK>(p, x.s, x.rt);
+  x.ta = 0;
+  x.tb = (int)min((int64_t)x.tiles, w.u1 - x.u);
+  return true;
+}
+__device__ __forceinline__ int row_tiles(const AttendParams& p, const Walk& x) {
+  return x.s.rows * p.G - x.rt * kR > 128 ? 2 : 1;
+}
+
+// ---------------------------------------------------------------- fetching warps
+__device__ __forceinline__ uint32_t pick(const uint32_t (&v)[4], int k) {
+  const uint32_t lo = k & 1 ? v[1] : v[0], hi = k & 1 ? v[3] : v[2];
+  return k & 2 ? hi : lo;
+}
+
+// What a warp knows of a key tile; lane l holds the page and scales of group l & 7.
+struct Tile {
+  int tile, page;
+  float ks, vs;
+  uint32_t seen[4];
+};
+
+template <int D>
+struct Fetch {
+  static constexpr int LPR = D / 16;           // lanes of a key row
+  static constexpr int RPP = 128 / LPR;        // rows of a pass (of the four warps)
+  static constexpr int PASSES = 128 / RPP;     // 8 (D = 128) or 4
+
+  const AttendParams& p;
+  const Walk& x;
+  const int lane, warp;
+  const int32_t* table;
+  const uint8_t* flags;
+  int n_flags;
+
+  __device__ Fetch(const AttendParams& p_, const Walk& x_, int lane_, int warp_) : p(p_), x(x_), lane(lane_), warp(warp_) {}
+
+  __device__ __forceinline__ void item() {
+    table = p.c.table + (int64_t)x.s.seq * p.c.max_pages;
+    flags = nullptr;
+    n_flags = 0;
+    if (p.keep) {
+      const int64_t k0 = p.keep_off[x.i], k1 = p.keep_off[x.i + 1];
+      if (k0 >= 0 && k1 >= k0 && k1 <= p.total_keep) {
+        flags = p.keep + k0;
+        n_flags = (int)min(k1 - k0, (int64_t)x.s.len);
+      } else {
+        set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
+      }
+    }
+  }
+  // page and raw flags (loads in flight)
+  __device__ __forceinline__ Tile look(int tile) const {
+    Tile t;
+    t.tile = tile;
+    const int first = tile * kK + (lane & 7) * kGroup;
+    t.page = first < x.s.len ? table[first >> p.c.log2T] : 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int key = tile * kK + 32 * k + lane;
+      bool see = key < x.s.len;
+      if (key < n_flags) see = flags[key] != 0;
+      t.seen[k] = see;
+    }
+    t.ks = t.vs = 0.f;
+    return t;
+  }
+  // masks, and the scales (loads in flight)
+  __device__ __forceinline__ void settle(Tile& t) const {
+    const bool bad = (unsigned)t.page >= (unsigned)p.c.pages;
+    if (bad) {
+      set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
+      t.page = 0;
+    }
+    const unsigned wrong = __ballot_sync(0xffffffffu, bad) & 0xff;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      t.seen[k] = __ballot_sync(0xffffffffu, t.seen[k] != 0);
+      if ((wrong >> (2 * k)) & 1) t.seen[k] &= 0xffff0000u;
+      if ((wrong >> (2 * k + 1)) & 1) t.seen[k] &= 0x0000ffffu;
+    }
+    const int64_t b = ((int64_t)p.layer * p.c.pages + t.page) * p.c.heads + x.h;
+    t.ks = p.c.k_scale[b];
+    t.vs = p.c.v_scale[b];
+  }
+  __device__ __forceinline__ int row_of(int pass) const { return pass * RPP + warp * (32 / LPR) + lane / LPR; }
+  __device__ __forceinline__ void load(uint4 (&r)[PASSES], const uint8_t* codes, const Tile& t) const {
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      const int row = row_of(i);
+      const int page = __shfl_sync(0xffffffffu, t.page, row / kGroup);
+      const uint32_t word = t.seen[i * RPP / 32 + (RPP > 32 ? row % RPP / 32 : 0)];
+      r[i] = make_uint4(0, 0, 0, 0);
+      if ((word >> (row & 31)) & 1) {
+        const int64_t b = ((int64_t)p.layer * p.c.pages + page) * p.c.heads + x.h;
+        r[i] = ldg_stream(codes + (b * p.c.T + ((t.tile * kK + row) & (p.c.T - 1))) * D + (lane % LPR) * 16);
+      }
+    }
+  }
+  // codes to f16 in the swizzled matrix layout: [D / 64][128 keys][64 dims]
+  __device__ __forceinline__ void store(const uint4 (&r)[PASSES], unsigned char* base) const {
+    const int c = lane % LPR, half = c >> 2, idx = 2 * (c & 3);
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      const int row = row_of(i);
+      unsigned char* line = base + half * 16384 + row * 128;
+      uint4 a, b;
+      a.x = e4m3x2_f16x2(r[i].x);
+      a.y = e4m3x2_f16x2_hi(r[i].x);
+      a.z = e4m3x2_f16x2(r[i].y);
+      a.w = e4m3x2_f16x2_hi(r[i].y);
+      b.x = e4m3x2_f16x2(r[i].z);
+      b.y = e4m3x2_f16x2_hi(r[i].z);
+      b.z = e4m3x2_f16x2(r[i].w);
+      b.w = e4m3x2_f16x2_hi(r[i].w);
+      // the two halves of a row start at the same bank: their lanes write
+      // their even and odd pieces in opposite order
+      const bool odd_first = half != 0;
+      const int i0 = (idx + (odd_first ? 1 : 0)) ^ (row & 7), i1 = (idx + (odd_first ? 0 : 1)) ^ (row & 7);
+      *reinterpret_cast<uint4*>(line + i0 * 16) = odd_first ? b : a;
+      *reinterpret_cast<uint4*>(line + i1 * 16) = odd_first ? a : b;
+    }
+  }
+  // whether this lane's group has a seen key; the largest and least (positive) scale of v of such groups
+  __device__ __forceinline__ bool range(const Tile& t, float& hi, float& lo) const {
+    const bool has = (pick(t.seen, (lane & 7) >> 1) >> (16 * (lane & 1))) & 0xffffu;
+    hi = has ? t.vs : 0.f;
+    lo = has && t.vs > 0.f ? t.vs : INFINITY;
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) {
+      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    }
+    return has;
+  }
+  __device__ __forceinline__ bool nans(const uint4 (&r)[PASSES]) const {
+    uint32_t hit = 0;
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      const uint32_t w[4] = {r[i].x, r[i].y, r[i].z, r[i].w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) hit |= (w[k] & 0x7f7f7f7fu) + 0x01010101u;
+    }
+    return (hit & 0x80808080u) != 0;
+  }
+  // NaN values that some row does not see: taken out of the matrix (this lane's own pieces), the token noted
+  __device__ __forceinline__ void note(int tile, unsigned char* base, int* first, int* any) const {
+    *any = 1;
+    const int c = lane % LPR;
+#pragma unroll 1
+    for (int i = 0; i < PASSES; ++i) {
+      const int row = row_of(i);
+#pragma unroll 1
+      for (int b = 0; b < 16; ++b) {
+        const int idx = (2 * (c & 3) + (b >> 3)) ^ (row & 7);
+        uint16_t* x = reinterpret_cast<uint16_t*>(base + (c >> 2) * 16384 + row * 128 + idx * 16 + (b & 7) * 2);
+        if ((*x & 0x7fff) > 0x7c00) {
+          atomicMin(&first[c * 16 + b], tile * kK + row);
+          *x = 0;
+        }
+      }
+    }
+  }
+};
+
+// a bounded wait on a barrier phase; false (recorded) if it ran out or another role gave up
+__device__ __forceinline__ bool wait_long(uint64_t* bar, uint32_t parity, volatile int* stop, int32_t* status) {
+  const uint64_t t0 = tc::globaltimer();
+  while (!tc::bar_try(bar, parity)) {
+    if (*stop || tc::globaltimer() - t0 > kWaitNs) {
+      *stop = 1;
+      set_status(status, OCCAM_ERR_TIMEOUT);
+      return false;
+    }
+  }
+  return true;
+}
+#define TC_WAIT(bar, parity)                                                                               \
+  if (!tc::bar_try(&(bar), (parity)) && !wait_long(&(bar), (parity), &sh.stop, p.c.status)) return;
+// the 256 softmax threads meet
+#define TC_MEET()                        \
+  do {                                   \
+    tc::bar_arrive(&sh.meet);            \
+    TC_WAIT(sh.meet, met & 1)            \
+    ++met;                               \
+  } while (0)
+
+template <int D>
+__device__ __forceinline__ void fetch_role(const AttendParams& p, const Stretch& w, Shared& sh, unsigned char* k_smem,
+                                           unsigned char* v_smem) {
+  constexpr int kBytes = kK * D * 2;
+  const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
+  Walk x;
+  walk_begin(p, w, x);
+  Fetch<D> f(p, x, lane, warp);
+  uint32_t n = 0, j = 0, seg = 0;  // step records, data steps, segments so far
+  for (bool again = true; again;) {
+    f.item();
+    const int common = p.causal ? x.s.len - x.s.rows + div_group(p, x.rt * kR) + 1 : x.s.len;
+    float rho = 0.f, rho_max = 0.f;
+    int* first = sh.nan_first[seg & 3];
+    int* any = &sh.any_nan[seg & 3];
+    // tiles in the order of their stages: codes (cur), masks and scales (nxt), page and flags (far)
+    Tile cur, nxt, far;
+    uint4 kr[Fetch<D>::PASSES], vr[Fetch<D>::PASSES];
+    const int end = x.tb - 1;
+    int groups = 0;      // groups of the present tile still to be taken one by one
+    uint32_t whole[4];   // the present tile's mask, while it is taken so
+    far = f.look(x.ta);
+    nxt = far;
+    f.settle(nxt);
+    cur = nxt;
+    cur.tile = x.ta - 1;
+    far = f.look(min(x.ta + 1, end));
+    float fall = 1.f;
+    bool have = false;
+    for (bool more = true; more;) {
+      const int st = j & 1;
+      // the step after cur (tiles without a seen key are passed over)
+      Tile next = cur;
+      if (groups) {
+        const int g = __ffs(groups) - 1;
+        groups &= groups - 1;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) next.seen[k] = (g >> 1) == k ? whole[k] & (0xffffu << (16 * (g & 1))) : 0u;
+      } else {
+        more = false;
+        while (next.tile < end) {
+          next = nxt;
+          if (next.tile < end) {
+            nxt = far;
+            f.settle(nxt);
+            far = f.look(min(nxt.tile + 1, end));
+          }
+          if (next.seen[0] | next.seen[1] | next.seen[2] | next.seen[3]) {
+            more = true;
+            break;
+          }
+        }
+        if (!more && !have) more = true;  // nothing is seen: one step of hidden keys gives the rows their zeros
+        if (more) {
+          // scales of v too far apart for one reference: the groups with a seen key one by one
+          float hi, lo;
+          const bool has = f.range(next, hi, lo);
+          if (lo < hi * kRhoKeep) {
+            const int with = (int)(__ballot_sync(0xffffffffu, has) & 0xff), g = __ffs(with) - 1;
+            groups = with & (with - 1);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              whole[k] = next.seen[k];
+              next.seen[k] = (g >> 1) == k ? whole[k] & (0xffffu << (16 * (g & 1))) : 0u;
+            }
+          }
+        }
+      }
+      if (have) {
+        // the step's record
+        if (n >= kRing) TC_WAIT(sh.step_free[n % kRing], ((n / kRing) - 1) & 1);
+        if (warp == 0) {
+          Step& s = sh.step[n % kRing];
+          if (lane < 8) {
+            // hidden groups take no part; a scale of 0 makes values of 0 (their codes are cleared below)
+            const uint32_t word = pick(cur.seen, lane >> 1);
+            const bool has = (word >> (16 * (lane & 1))) & 0xffffu, real = has && cur.vs != 0.f;
+            s.ks[lane] = has ? cur.ks : 1.f;
+            s.lr[lane] = real ? (cur.vs == rho ? 0.f : log2f(cur.vs / rho)) : 0.f;
+            s.rr[lane] = real ? rho / cur.vs : 1.f;
+          }
+          if (lane < 4) s.seen[lane] = pick(cur.seen, lane);
+          if (lane == 0) {
+            s.tile = cur.tile;
+            s.end = 0;
+            s.row_tiles = row_tiles(p, x);
+            s.fall = fall;
+            s.rho = rho;
+          }
+          __syncwarp();
+          if (lane == 0) tc::bar_arrive(&sh.step_full[n % kRing]);
+        }
+        ++n;
+        // keys
+        if (j >= 2) TC_WAIT(sh.k_free[st], ((j >> 1) - 1) & 1);
+        f.store(kr, k_smem + st * kBytes);
+        tc::fence_proxy_async();
+        tc::bar_arrive(&sh.k_full[st]);
+      }
+      if (more) f.load(kr, p.c.k, next);
+      if (have) {
+        // values
+        if (j >= 2) TC_WAIT(sh.v_free[st], ((j >> 1) - 1) & 1);
+        if (__any_sync(0xffffffffu, cur.vs == 0.f)) {
+#pragma unroll
+          for (int i = 0; i < Fetch<D>::PASSES; ++i)
+            if (__shfl_sync(0xffffffffu, cur.vs, f.row_of(i) / kGroup) == 0.f) vr[i] = make_uint4(0, 0, 0, 0);
+        }
+        f.store(vr, v_smem + st * kBytes);
+        const bool open = (cur.seen[0] & cur.seen[1] & cur.seen[2] & cur.seen[3]) == 0xffffffffu && (cur.tile + 1) * kK <= common;
+        if (!open && f.nans(vr)) f.note(cur.tile, v_smem + st * kBytes, first, any);
+        tc::fence_proxy_async();
+        tc::bar_arrive(&sh.v_full[st]);
+        ++j;
+      }
+      if (more) {
+        f.load(vr, p.c.v, next);
+        // v's reference of the next step, and O's factor
+        float hi, lo;
+        f.range(next, hi, lo);
+        fall = 1.f;
+        if (hi > rho || lo < rho * kRhoKeep) {
+          const float to = hi > rho ? hi : fmaxf(hi, rho_max * kRhoSpan);
+          fall = rho / to;
+          rho = to;
+          rho_max = fmaxf(rho_max, to);
+        }
+      }
+      cur = next;
+      have = true;
+    }
+    // the end of the segment
+    if (n >= kRing) TC_WAIT(sh.step_free[n % kRing], ((n / kRing) - 1) & 1);
+    again = walk_next(p, w, x);
+    if (warp == 0 && lane == 0) {
+      sh.step[n % kRing].end = again ? 1 : 2;
+      sh.step[n % kRing].rho = rho;
+      tc::bar_arrive(&sh.step_full[n % kRing]);
+    }
+    ++n;
+    ++seg;
+  }
+}
+
+// ---------------------------------------------------------------- the issuing thread
+// The whole warp walks through the steps (so that descriptors and branches are
+// the same for every lane); one elected lane issues.
+template <int D>
+__device__ __forceinline__ void mma_role(const AttendParams& p, Shared& sh, uint32_t q_smem, uint32_t k_smem,
+                                         uint32_t v_smem, uint32_t tmem) {
+  constexpr int kBytes = kK * D * 2;
+  constexpr uint32_t id_s = idesc_f16(128, 128, false), id_o = idesc_f16(128, D, true);
+  const uint64_t dq = desc_kmajor(q_smem), dk = desc_kmajor(k_smem), dv = desc_mnmajor(v_smem);
+  // (a descriptor's address field counts 16 bytes)
+  auto scores = [&](auto tt, uint32_t st) {
+    constexpr int t = decltype(tt)::value;
+    if (elect_one()) {
+      const uint64_t kd = dk + st * (kBytes >> 4), qd = dq + t * (kBytes >> 4);
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+        constexpr int kBlock = 16384 >> 4;
+        const int o = (k >> 2) * kBlock + (k & 3) * 2;
+        tc::mma_bf16(tmem + t * 128, qd + o, kd + o, id_s, k > 0);
+      }
+      tc::mma_commit(&sh.s_full[t]);
+    }
+    __syncwarp();
+  };
+  auto values = [&](auto tt, uint32_t st, bool begin) {
+    constexpr int t = decltype(tt)::value;
+    if (elect_one()) {
+      const uint64_t vd = dv + st * (kBytes >> 4);
+#pragma unroll
+      for (int k = 0; k < kK / 16; ++k)
+        mma_ts(tmem + 256 + t * 128, tmem + t * 128 + 64 + k * 8, vd + k * (2048 >> 4), id_o, k > 0 ? 1u : (begin ? 0u : 1u));
+      tc::mma_commit(&sh.o_done[t]);
+    }
+    __syncwarp();
+  };
+  using T0 = std::integral_constant<int, 0>;
+  using T1 = std::integral_constant<int, 1>;
+  uint32_t n = 0, j = 0, it0 = 0, it1 = 0;  // step records, steps, products of each row tile
+  int end = 0;
+  for (uint32_t seg = 0; end != 2; ++seg) {
+    TC_WAIT(sh.q_full, seg & 1);
+    bool two = false;
+    end = 0;
+    // pass k: O += P V of step k - 1, S of step k, a row tile after the other
+    for (uint32_t k = 0; !end; ++k) {
+      if (k > 0) {
+        TC_WAIT(sh.p_full[0], it0 & 1);
+        ++it0;
+        TC_WAIT(sh.v_full[(j - 1) & 1], ((j - 1) >> 1) & 1);
+        tc::fence_after();
+        values(T0{}, (j - 1) & 1, k == 1);
+      }
+      TC_WAIT(sh.step_full[n % kRing], (n / kRing) & 1);
+      end = sh.step[n % kRing].end;
+      if (!end) {
+        two = sh.step[n % kRing].row_tiles == 2;
+        TC_WAIT(sh.k_full[j & 1], (j >> 1) & 1);
+        tc::fence_after();
+        scores(T0{}, j & 1);
+      }
+      if (two) {
+        if (k > 0) {
+          TC_WAIT(sh.p_full[1], it1 & 1);
+          ++it1;
+          tc::fence_after();
+          values(T1{}, (j - 1) & 1, k == 1);
+        }
+        if (!end) scores(T1{}, j & 1);
+      }
+      if (elect_one()) {
+        if (k > 0) tc::mma_commit(&sh.v_free[(j - 1) & 1]);
+        if (!end) tc::mma_commit(&sh.k_free[j & 1]);
+        tc::bar_arrive(&sh.step_free[n % kRing]);
+      }
+      __syncwarp();
+      ++n;
+      if (!end) ++j;
+    }
+  }
+}
+
+// ---------------------------------------------------------------- a row a thread
+// The warp's 32 query rows (from row `first` of the item's tile) as f16 in the
+// matrix layout, each scaled by a power of two of its own; lane l gets row l's scale
+// (with the softmax's). D / 8 lanes take a row; the copies are all in flight at
+// once, and each lane converts in place what it copied.
+template <int D, bool BF16>
+__device__ __forceinline__ float load_queries(const AttendParams& p, const Walk& x, int first, unsigned char* q_smem, int lane) {
+  constexpr int LPR = D / 8, RPI = 32 / LPR, N = 32 / RPI;
+  const int c = lane % LPR, sub = lane / LPR, rows = x.s.rows * p.G;
+  unsigned char* mine = q_smem + (c >> 3) * 16384;
+  auto piece = [&](int i) {
+    const int r = (first & 127) + i * RPI + sub;
+    return mine + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+  };
+#pragma unroll 1
+  for (int i = 0; i < N; ++i) {
+    const int at = x.rt * kR + first + i * RPI + sub, tok = div_group(p, at);
+    const uint16_t* src = at < rows ? p.q + (x.s.row0 + tok) * p.q_row + (int64_t)(x.h * p.G + at - tok * p.G) * D + c * 8 : p.q;
+    tc::cp_async16(piece(i), src, at < rows ? 16 : 0);
+  }
+  cp_async_commit();
+  cp_async_wait<0>();
+  float scale = 0.f;
+#pragma unroll 1
+  for (int i = 0; i < N; ++i) {
+    uint4* at = reinterpret_cast<uint4*>(piece(i));
+    const uint4 v = *at;
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    float f[8], amax = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (BF16) {
+        f[2 * k] = bf16_lo(w[k]);
+        f[2 * k + 1] = bf16_hi(w[k]);
+      } else {
+        const float2 h2 = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
+        f[2 * k] = h2.x;
+        f[2 * k + 1] = h2.y;
+      }
+      amax = tc::fmax3(amax, fabsf(f[2 * k]), fabsf(f[2 * k + 1]));
+    }
+#pragma unroll
+    for (int o = 1; o < LPR; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    // largest value in [2^14, 2^15), as in attend.cu
+    int e = (__float_as_int(amax) >> 23) - 127 - 14;
+    e = amax == 0.f ? 0 : max(e, -112);
+    const float up = __int_as_float((127 - e) << 23);
+    *at = make_uint4(pack_f16(f[0] * up, f[1] * up), pack_f16(f[2] * up, f[3] * up), pack_f16(f[4] * up, f[5] * up),
+                     pack_f16(f[6] * up, f[7] * up));
+    const float down = __shfl_sync(0xffffffffu, __int_as_float((127 + e) << 23), (lane % RPI) * LPR);
+    if (lane / RPI == i) scale = down;
+  }
+  return scale * p.scale_log2;
+}
+
+template <bool BF16>
+__device__ __forceinline__ uint32_t out_pair(float a, float b) {
+  if (BF16) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+  return pack_f16(a, b);
+}
+
+// 16 values of a result row
+template <bool BF16>
+__device__ __forceinline__ void write16(uint16_t* to, const float (&v)[16]) {
+  uint4* out = reinterpret_cast<uint4*>(to);
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    out[k] = make_uint4(out_pair<BF16>(v[8 * k], v[8 * k + 1]), out_pair<BF16>(v[8 * k + 2], v[8 * k + 3]),
+                        out_pair<BF16>(v[8 * k + 4], v[8 * k + 5]), out_pair<BF16>(v[8 * k + 6], v[8 * k + 7]));
+}
+
+template <int D, bool BF16>
+__device__ __forceinline__ void softmax_role(const AttendParams& p, const Stretch& w, Shared& sh, unsigned char* q_smem,
+                                             uint32_t tmem, int t) {
+  const int r = threadIdx.x & 127, lane = threadIdx.x & 31;
+  const uint32_t lanes = (uint32_t)(r & ~31) << 16;
+  const uint32_t s_at = tmem + t * 128 + lanes, o_at = tmem + 256 + t * 128 + lanes;
+  Walk x;
+  walk_begin(p, w, x);
+  uint32_t n = 0, it = 0, seg = 0, met = 0;
+  do {
+    const bool mine = t < row_tiles(p, x);
+    const int row = t * 128 + r, at = x.rt * kR + row;
+    const bool there = at < x.s.rows * p.G;
+    float qscale = 0.f;
+    if (mine) qscale = load_queries<D, BF16>(p, x, row & ~31, q_smem + t * kK * D * 2, lane);
+    tc::fence_proxy_async();
+    tc::bar_arrive(&sh.q_full);
+    const int limit = !there ? 0 : p.causal ? x.s.len - x.s.rows + div_group(p, at) + 1 : x.s.len;  // keys this row sees
+    const int common = p.causal ? x.s.len - x.s.rows + div_group(p, x.rt * kR + t * 128) + 1 : x.s.len;
+    float ref = -INFINITY, top = -INFINITY, l = 0.f, rho = 0.f;
+    for (bool begin = true;; begin = false) {
+      TC_WAIT(sh.step_full[n % kRing], (n / kRing) & 1);
+      const Step& st = sh.step[n % kRing];
+      const bool end = st.end != 0;
+      if (end) rho = st.rho;
+      if (!end && mine) {
+        TC_WAIT(sh.s_full[t], it & 1);
+        tc::fence_after();
+        const int tile = st.tile;
+        const bool open = (st.seen[0] & st.seen[1] & st.seen[2] & st.seen[3]) == 0xffffffffu && (tile + 1) * kK <= common;
+        // scores of 32 keys, hidden ones -inf (rolled loops: the roles together have to stay within the instruction cache)
+        const int lim = limit - tile * kK;
+        auto chunk = [&](uint32_t(&v)[32], int q) {
+          tc::tmem_ld32(s_at + 32 * q, v);
+          wait_ld(v);
+          if (!open) {
+            const int m = lim - 32 * q;
+            const uint32_t see = st.seen[q] & (m >= 32 ? 0xffffffffu : m <= 0 ? 0u : (1u << m) - 1u);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) v[k] = (see >> k) & 1 ? v[k] : 0xff800000u;
+          }
+        };
+        uint32_t v[32];
+        float m = top;
+#pragma unroll 1
+        for (int q = 0; q < 4; ++q) {
+          chunk(v, q);
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            float x0 = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < 16; k += 2)
+              x0 = tc::fmax3(x0, __uint_as_float(v[16 * g + k]), __uint_as_float(v[16 * g + k + 1]));
+            m = fmaxf(m, x0 * fmaxf(st.ks[2 * q + g] * qscale, kLeast));
+          }
+        }
+        top = m;
+        float fall = st.fall;
+        bool move = fall != 1.f;
+        if (m > ref + kLazy || ref == -INFINITY) {
+          const float to = m;
+          if (to != ref) {
+            fall *= ref == -INFINITY ? 0.f : fast_exp2(ref - to);
+            l *= ref == -INFINITY ? 0.f : fast_exp2(ref - to);
+            move = true;
+            ref = to;
+          }
+        }
+        // O in units of the new references (nothing is there before the first product)
+        if (!begin && __any_sync(0xffffffffu, move)) {
+          TC_WAIT(sh.o_done[t], (it - 1) & 1);
+          tc::fence_after();
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t o[32];
+            tc::tmem_ld32(o_at + 32 * c, o);
+            wait_ld(o);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * fall);
+            tc::tmem_st32(o_at + 32 * c, o);
+          }
+        }
+        const float base = ref == -INFINITY ? 0.f : ref;
+        // backwards, so that P (columns 64 + 16 q) only goes over scores that have been read
+#pragma unroll 1
+        for (int q = 3; q >= 0; --q) {
+          chunk(v, q);
+          uint32_t pk[16];
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            const float f = fmaxf(st.ks[2 * q + g] * qscale, kLeast), add = st.lr[2 * q + g] - base;
+            const float2 ff = make_float2(f, f), aa = make_float2(add, add);
+            float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              float2 x2 = fma2(make_float2(__uint_as_float(v[16 * g + 2 * k]), __uint_as_float(v[16 * g + 2 * k + 1])), ff, aa);
+              x2.x = fast_exp2(x2.x);
+              x2.y = fast_exp2(x2.y);
+              sum = add2(sum, x2);
+              pk[8 * g + k] = pack_f16(x2.x, x2.y);
+            }
+            l = fmaf(sum.x + sum.y, st.rr[2 * q + g], l);
+          }
+          tmem_st16(s_at + 64 + 16 * q, pk);
+        }
+        tc::tmem_wait_st();
+        tc::fence_before();
+        tc::bar_arrive(&sh.p_full[t]);
+        ++it;
+      }
+      __syncwarp();
+      if (lane == 0) tc::bar_arrive(&sh.step_free[n % kRing]);
+      ++n;
+      if (end) break;
+    }
+
+    // the row's result
+    const bool done = x.ta == 0 && x.tb == x.tiles;
+    const int slot = x.ta > 0 ? 0 : 1;
+    const int tok = div_group(p, at);
+    const int64_t to = (x.s.row0 + tok) * p.H + x.h * p.G + at - tok * p.G;
+    const int64_t mypart = ((int64_t)blockIdx.x * 2 + slot) * kR + row;
+    if (mine) {
+      TC_WAIT(sh.o_done[t], (it - 1) & 1);
+      tc::fence_after();
+      const float scale = l == 0.f ? 0.f : done ? rho / l : rho;
+      uint16_t* out = p.out + to * D;
+      float* part = p.part_o + mypart * D;
+#pragma unroll 1
+      for (int c = 0; c < D; c += 16) {
+        uint32_t o[16];
+        tmem_ld16(o_at + c, o);
+        if (there) {
+          float v[16];
+#pragma unroll
+          for (int k = 0; k < 16; ++k) v[k] = l == 0.f ? 0.f : __uint_as_float(o[k]) * scale;
+          if (done) {
+            write16<BF16>(out + c, v);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              reinterpret_cast<float4*>(part + c)[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+          }
+        }
+      }
+      if (there && sh.any_nan[seg & 3]) {
+#pragma unroll 1
+        for (int d = 0; d < D; ++d)
+          if (sh.nan_first[seg & 3][d] < limit) {
+            if (done)
+              out[d] = BF16 ? 0x7fc0 : 0x7e00;
+            else
+              part[d] = __int_as_float(0x7fc00000);
+          }
+      }
+      tc::fence_before();
+      if (there) {
+        if (done) {
+          if (p.lse) p.lse[to] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.69314718056f;
+        } else {
+          p.part_ml[mypart] = make_float2(l == 0.f ? -INFINITY : ref, l);
+        }
+      }
+    }
+    if (!done) {
+      __threadfence();
+      TC_MEET();
+      const int64_t first_u = x.u - x.ta;
+      const int first = cta_of(w.units, w.ctas, first_u), last = cta_of(w.units, w.ctas, first_u + x.tiles - 1);
+      if (threadIdx.x == 0) sh.last = atomicAdd(&p.counters[first], 1) == last - first;
+      TC_MEET();
+      if (sh.last) {
+        __threadfence();
+        if (threadIdx.x == 0) p.counters[first] = 0;
+        if (mine && there) {
+          float mx = -INFINITY;
+#pragma unroll 1
+          for (int c = first; c <= last; ++c)
+            mx = fmaxf(mx, __ldcg(&p.part_ml[((int64_t)c * 2 + (c == first ? 1 : 0)) * kR + row]).x);
+          const float base = mx == -INFINITY ? 0.f : mx;
+          float sum = 0.f;
+#pragma unroll 1
+          for (int c = first; c <= last; ++c) {
+            const float2 ml = __ldcg(&p.part_ml[((int64_t)c * 2 + (c == first ? 1 : 0)) * kR + row]);
+            sum += ml.y * fast_exp2(ml.x - base);
+          }
+          const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll 1
+          for (int k = 0; k < D; k += 16) {
+            float acc[16];
+#pragma unroll
+            for (int q = 0; q < 16; ++q) acc[q] = 0.f;
+#pragma unroll 1
+            for (int c = first; c <= last; ++c) {
+              const int64_t from = ((int64_t)c * 2 + (c == first ? 1 : 0)) * kR + row;
+              const float g = fast_exp2(__ldcg(&p.part_ml[from]).x - base);
+              const float4* po = reinterpret_cast<const float4*>(p.part_o + from * D + k);
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                const float4 v = __ldcg(po + q);
+                acc[4 * q] = fmaf(v.x, g, acc[4 * q]);
+                acc[4 * q + 1] = fmaf(v.y, g, acc[4 * q + 1]);
+                acc[4 * q + 2] = fmaf(v.z, g, acc[4 * q + 2]);
+                acc[4 * q + 3] = fmaf(v.w, g, acc[4 * q + 3]);
+              }
+            }
+#pragma unroll
+            for (int q = 0; q < 16; ++q) acc[q] = sum == 0.f ? 0.f : acc[q] * inv;
+            write16<BF16>(p.out + to * D + k, acc);
+          }
+          if (p.lse) p.lse[to] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.69314718056f;
+        }
+      }
+    }
+    // The notes of the segment before are cleared: its other row tile has read
+    // them (it came to this segment's products), and the fetching warps, two tiles ahead
+    // at most, are not yet three segments on.
+    const uint32_t old = (seg + 3) & 3;
+    if (t == 0 && sh.any_nan[old]) {
+      if (r < D) sh.nan_first[old][r] = 0x7fffffff;
+      __syncwarp();
+    }
+    ++seg;
+  } while (walk_next(p, w, x));
+}
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(AttendParams p) {
+  constexpr int kBytes = kK * D * 2;
+  extern __shared__ unsigned char dyn[];
+  __shared__ Shared sh;
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn) + 1023) & ~(uintptr_t)1023);
+  const int warp = threadIdx.x >> 5;
+  Stretch w;
+  if (!attend_stretch<kR, kK, kThreads>(p, 1, sh.scan, w)) return;
+  if (threadIdx.x == 0) {
+    sh.stop = 0;
+    tc::bar_init(&sh.q_full, 256);
+    tc::bar_init(&sh.meet, 256);
+    tc::bar_init(&sh.drain, 1);
+    for (int k = 0; k < 2; ++k) {
+      tc::bar_init(&sh.k_full[k], 128);
+      tc::bar_init(&sh.v_full[k], 128);
+      tc::bar_init(&sh.k_free[k], 1);
+      tc::bar_init(&sh.v_free[k], 1);
+      tc::bar_init(&sh.s_full[k], 1);
+      tc::bar_init(&sh.p_full[k], 128);
+      tc::bar_init(&sh.o_done[k], 1);
+    }
+    for (int k = 0; k < kRing; ++k) {
+      tc::bar_init(&sh.step_full[k], 1);
+      tc::bar_init(&sh.step_free[k], 9);  // eight softmax warps and the issuing thread
+    }
+    tc::bar_fence_init();
+  }
+  if (threadIdx.x < 4) sh.any_nan[threadIdx.x] = 0;
+  for (int d = threadIdx.x; d < 4 * 128; d += kThreads) (&sh.nan_first[0][0])[d] = 0x7fffffff;
+  if (warp == 12) tc::tmem_alloc(&sh.tmem, 512);
+  tc::fence_before();
+  __syncthreads();
+  tc::fence_after();
+  const uint32_t tmem = sh.tmem;
+  unsigned char* q_smem = smem;
+  unsigned char* k_smem = smem + 2 * kBytes;
+  unsigned char* v_smem = smem + 4 * kBytes;
+  // registers: 512 threads start with 128 each, four warpgroups split them
+  if (warp < 8) {
+    tc::setmaxnreg_inc<kRegSoftmax>();
+    softmax_role<D, BF16>(p, w, sh, q_smem, tmem, warp >> 2);
+  } else if (warp < 12) {
+    tc::setmaxnreg_inc<kRegFetch>();
+    fetch_role<D>(p, w, sh, k_smem, v_smem);
+  } else {
+    tc::setmaxnreg_dec<kRegIssue>();
+    if (warp == 12)
+      mma_role<D>(p, sh, tc::su32(q_smem), tc::su32(k_smem), tc::su32(v_smem), tmem);
+  }
+  __syncthreads();
+  // after a wait that ran out products may still be in flight
+  if (sh.stop && threadIdx.x == 384) {
+    tc::mma_commit(&sh.drain);
+    tc::bar_wait(&sh.drain, 0, nullptr, kWaitNs);
+  }
+  __syncthreads();
+  if (warp == 12) tc::tmem_dealloc(tmem, 512);
+}
+
+// Once per device: the shared memory, and that the register split adds up --
+// setmaxnreg.inc waits for registers that only the launch's own can give.
+template <int D, bool BF16>
+int prepare(int smem) {
+  static std::atomic<uint64_t> ready{0};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return OCCAM_ERR_CUDA;
+  if ((ready.load(std::memory_order_acquire) >> dev) & 1) return OCCAM_OK;
+  cudaFuncAttributes at;
+  if (cudaFuncGetAttributes(&at, attend_tc_kernel<D, BF16>) != cudaSuccess) return OCCAM_ERR_CUDA;
+  if (at.numRegs * kThreads < 256 * kRegSoftmax + 128 * (kRegFetch + kRegIssue)) return OCCAM_ERR_UNSUPPORTED;
+  if (cudaFuncSetAttribute(attend_tc_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+    return OCCAM_ERR_CUDA;
+  ready.fetch_or(uint64_t(1) << dev, std::memory_order_release);
+  return OCCAM_OK;
+}
+
+template <int D, bool BF16>
+int launch(const AttendParams& p, cudaStream_t st) {
+  const int smem = 6 * kK * D * 2 + 1024;
+  const int rc = prepare<D, BF16>(smem);
+  if (rc != OCCAM_OK) return rc;
+  attend_tc_kernel<D, BF16><<<std::min(cache_sms(), kAttendTcCtas), kThreads, smem, st>>>(p);
+  count_launch();
+  return cudaGetLastError() == cudaSuccess ? OCCAM_OK : OCCAM_ERR_CUDA;
+}
+
+}  // namespace
+
+int occam::launch_attend_tc(const AttendParams& p, int dim, cudaStream_t st) {
+  if (dim == 128) return p.bf16 ? launch<128, true>(p, st) : launch<128, false>(p, st);
+  return p.bf16 ? launch<64, true>(p, st) : launch<64, false>(p, st);
+}

@@ -10,9 +10,13 @@
 namespace occam {
 
 // Attention workspace: at most kAttendCtas CTAs leave two partial results of
-// up to kAttendRows rows each.
+// up to kAttendRows rows each (the tensor-core kernel: kAttendTcCtas, 256 rows).
 constexpr int kAttendCtas = 1024;
 constexpr int kAttendRows = 16;
+constexpr int kAttendTcCtas = 160;
+constexpr size_t kAttendPartRows =
+    2 * ((size_t)kAttendCtas * kAttendRows > (size_t)kAttendTcCtas * 256 ? (size_t)kAttendCtas * kAttendRows
+                                                                         : (size_t)kAttendTcCtas * 256);
 
 inline size_t cache_align(size_t x) { return (x + 255) / 256 * 256; }
 
@@ -41,8 +45,8 @@ inline CacheWs cache_ws(const occam_cache* c, int64_t max_tokens) {
   w.new_pages = take((size_t)c->max_seqs * 8);
   w.free_list = take((size_t)c->pages * 4);
   w.old_table = take((size_t)c->max_seqs * c->max_pages * 4);
-  w.part_o = take((size_t)2 * kAttendCtas * kAttendRows * c->dim * 4);
-  w.part_ml = take((size_t)2 * kAttendCtas * kAttendRows * 8);
+  w.part_o = take(kAttendPartRows * c->dim * 4);
+  w.part_ml = take(kAttendPartRows * 8);
   w.list = take((size_t)max_tokens * 4);  // last: its size is the caller's
   w.total = off;
   return w;
