@@ -60,6 +60,8 @@ struct Shared {
       step_free[kRing], meet, drain;
   Step step[kRing];
   int64_t scan[kThreads / 32 + 4];
+  volatile int64_t u0, u1, units;   // the CTA's stretch (see Stretch)
+  volatile int ctas, seq, head, row_tile, tile;
   uint32_t tmem;
   int stop;            // a wait ran out
   int last;
@@ -149,7 +151,7 @@ struct Walk {
   int i, h, rt, tiles, ta, tb;
   int64_t u;
 };
-__device__ __forceinline__ void walk_begin(const AttendParams& p, const Stretch& w, Walk& x) {
+__device__ __forceinline__ void walk_begin(const AttendParams& p, const Shared& w, Walk& x) {
   x.i = w.seq;
   x.s = attend_seq(p, x.i);
   x.h = w.head;
@@ -160,7 +162,7 @@ __device__ __forceinline__ void walk_begin(const AttendParams& p, const Stretch&
   x.tb = (int)min((int64_t)x.tiles, x.ta + (w.u1 - x.u));
 }
 // False at the end of the stretch.
-__device__ __forceinline__ bool walk_next(const AttendParams& p, const Stretch& w, Walk& x) {
+__device__ __forceinline__ bool walk_next(const AttendParams& p, const Shared& w, Walk& x) {
   x.u += x.tb - x.ta;
   if (x.u >= w.u1) return false;
   const int nrt = (x.s.rows * p.G + kR - 1) / kR;
@@ -183,32 +185,59 @@ __device__ __forceinline__ int row_tiles(const AttendParams& p, const Walk& x) {
 }
 
 // ---------------------------------------------------------------- fetching warps
+// 16 bytes, or zeros if !there
+__device__ __forceinline__ uint4 load_if(const uint8_t* p, uint32_t there) {
+  uint4 r;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.u32 p, %5, 0;\n\t"
+      "mov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
+      "@p ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+      : "=&r"(r.x), "=&r"(r.y), "=&r"(r.z), "=&r"(r.w)
+      : "l"(p), "r"(there));
+  return r;
+}
+
 __device__ __forceinline__ uint32_t pick(const uint32_t (&v)[4], int k) {
   const uint32_t lo = k & 1 ? v[1] : v[0], hi = k & 1 ? v[3] : v[2];
   return k & 2 ? hi : lo;
 }
 
-// What a warp knows of a key tile; lane l holds the page and scales of group l & 7.
+// What a warp knows of a key tile; lane l holds the place and scales of group l & 7 (16 keys).
 struct Tile {
-  int tile, page;
+  int tile;
+  int64_t at;   // the group's first code in its page (while the tile is only looked at: the page)
   float ks, vs;
   uint32_t seen[4];
 };
 
+// A pass of the four warps takes RPP key rows, LPR lanes a row, 16 codes a lane. Row 16 q + r
+// of every pass has the same r & 7, so a lane's swizzled places are the same in each.
 template <int D>
 struct Fetch {
-  static constexpr int LPR = D / 16;           // lanes of a key row
-  static constexpr int RPP = 128 / LPR;        // rows of a pass (of the four warps)
-  static constexpr int PASSES = 128 / RPP;     // 8 (D = 128) or 4
+  static constexpr int LPR = D / 16;
+  static constexpr int RPP = 128 / LPR;     // 16 (D = 128) or 32 rows
+  static constexpr int PASSES = 128 / RPP;
 
   const AttendParams& p;
   const Walk& x;
-  const int lane, warp;
+  const int lane, row0, c;  // row of pass 0, piece of the row
+  int place0, place1;       // this lane's two 16-byte pieces in a matrix, pass 0
+  uint32_t swap;            // all ones: the odd piece is written first
   const int32_t* table;
   const uint8_t* flags;
   int n_flags;
 
-  __device__ Fetch(const AttendParams& p_, const Walk& x_, int lane_, int warp_) : p(p_), x(x_), lane(lane_), warp(warp_) {}
+  __device__ Fetch(const AttendParams& p_, const Walk& x_, int lane_, int warp)
+      : p(p_), x(x_), lane(lane_), row0(warp * (32 / LPR) + lane_ / LPR), c(lane_ % LPR) {
+    // [D / 64][128 keys][64 dims], 128-byte swizzle. The two halves of a row start at the same
+    // bank: their lanes write their even and odd pieces in opposite order.
+    const int odd = c >> 2;
+    swap = 0u - (uint32_t)odd;
+    const int base = odd * 16384 + row0 * 128, idx = 2 * (c & 3);
+    place0 = base + (((idx + odd) ^ (row0 & 7)) << 4);
+    place1 = base + (((idx + 1 - odd) ^ (row0 & 7)) << 4);
+  }
 
   __device__ __forceinline__ void item() {
     table = p.c.table + (int64_t)x.s.seq * p.c.max_pages;
@@ -225,75 +254,59 @@ struct Fetch {
     }
   }
   // page and raw flags (loads in flight)
-  __device__ __forceinline__ Tile look(int tile) const {
-    Tile t;
+  __device__ __forceinline__ void look(Tile& t, int tile) const {
     t.tile = tile;
     const int first = tile * kK + (lane & 7) * kGroup;
-    t.page = first < x.s.len ? table[first >> p.c.log2T] : 0;
+    int page = 0;
+    if (first < x.s.len) page = table[first >> p.c.log2T];
+    t.at = page;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const int key = tile * kK + 32 * k + lane;
-      bool see = key < x.s.len;
-      if (key < n_flags) see = flags[key] != 0;
+      uint32_t see = key < x.s.len;
+      if (key < n_flags) see = flags[key];
       t.seen[k] = see;
     }
-    t.ks = t.vs = 0.f;
-    return t;
   }
-  // masks, and the scales (loads in flight)
+  // masks, places, and the scales (loads in flight)
   __device__ __forceinline__ void settle(Tile& t) const {
-    const bool bad = (unsigned)t.page >= (unsigned)p.c.pages;
-    if (bad) {
-      set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
-      t.page = 0;
-    }
+    int64_t page = t.at;
+    const bool bad = (uint64_t)page >= (uint64_t)p.c.pages;
     const unsigned wrong = __ballot_sync(0xffffffffu, bad) & 0xff;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      t.seen[k] = __ballot_sync(0xffffffffu, t.seen[k] != 0);
-      if ((wrong >> (2 * k)) & 1) t.seen[k] &= 0xffff0000u;
-      if ((wrong >> (2 * k + 1)) & 1) t.seen[k] &= 0x0000ffffu;
-    }
-    const int64_t b = ((int64_t)p.layer * p.c.pages + t.page) * p.c.heads + x.h;
-    t.ks = p.c.k_scale[b];
-    t.vs = p.c.v_scale[b];
-  }
-  __device__ __forceinline__ int row_of(int pass) const { return pass * RPP + warp * (32 / LPR) + lane / LPR; }
-  __device__ __forceinline__ void load(uint4 (&r)[PASSES], const uint8_t* codes, const Tile& t) const {
+    for (int k = 0; k < 4; ++k) t.seen[k] = __ballot_sync(0xffffffffu, t.seen[k] != 0);
+    if (wrong) {
+      set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
+      if (bad) page = 0;
 #pragma unroll
-    for (int i = 0; i < PASSES; ++i) {
-      const int row = row_of(i);
-      const int page = __shfl_sync(0xffffffffu, t.page, row / kGroup);
-      const uint32_t word = t.seen[i * RPP / 32 + (RPP > 32 ? row % RPP / 32 : 0)];
-      r[i] = make_uint4(0, 0, 0, 0);
-      if ((word >> (row & 31)) & 1) {
-        const int64_t b = ((int64_t)p.layer * p.c.pages + page) * p.c.heads + x.h;
-        r[i] = ldg_stream(codes + (b * p.c.T + ((t.tile * kK + row) & (p.c.T - 1))) * D + (lane % LPR) * 16);
+      for (int k = 0; k < 4; ++k) {
+        if ((wrong >> (2 * k)) & 1) t.seen[k] &= 0xffff0000u;
+        if ((wrong >> (2 * k + 1)) & 1) t.seen[k] &= 0x0000ffffu;
       }
     }
+    const int64_t b = ((int64_t)p.layer * p.c.pages + page) * p.c.heads + x.h;
+    t.ks = p.c.k_scale[b];
+    t.vs = p.c.v_scale[b];
+    t.at = ((b << p.c.log2T) + (((lane & 7) * kGroup) & (p.c.T - 1))) * D;
   }
-  // codes to f16 in the swizzled matrix layout: [D / 64][128 keys][64 dims]
-  __device__ __forceinline__ void store(const uint4 (&r)[PASSES], unsigned char* base) const {
-    const int c = lane % LPR, half = c >> 2, idx = 2 * (c & 3);
+  __device__ __forceinline__ void load(uint4 (&r)[PASSES], const uint8_t* codes, const Tile& t) const {
+    const uint8_t* mine = codes + (row0 & 15) * D + c * 16;
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
-      const int row = row_of(i);
-      unsigned char* line = base + half * 16384 + row * 128;
-      uint4 a, b;
-      a.x = e4m3x2_f16x2(r[i].x);
-      a.y = e4m3x2_f16x2_hi(r[i].x);
-      a.z = e4m3x2_f16x2(r[i].y);
-      a.w = e4m3x2_f16x2_hi(r[i].y);
-      b.x = e4m3x2_f16x2(r[i].z);
-      b.y = e4m3x2_f16x2_hi(r[i].z);
-      b.z = e4m3x2_f16x2(r[i].w);
-      b.w = e4m3x2_f16x2_hi(r[i].w);
-      // the two halves of a row start at the same bank: their lanes write
-      // their even and odd pieces in opposite order
-      const bool odd_first = half != 0;
-      const int i0 = (idx + (odd_first ? 1 : 0)) ^ (row & 7), i1 = (idx + (odd_first ? 0 : 1)) ^ (row & 7);
-      *reinterpret_cast<uint4*>(line + i0 * 16) = odd_first ? b : a;
-      *reinterpret_cast<uint4*>(line + i1 * 16) = odd_first ? a : b;
+      const int64_t at = __shfl_sync(0xffffffffu, t.at, i * (RPP / 16) + (row0 >> 4));
+      r[i] = load_if(mine + at, t.seen[i * RPP / 32] & (1u << (row0 + i * RPP % 32)));
+    }
+  }
+  // codes to f16 in the matrix layout
+  __device__ __forceinline__ void store(const uint4 (&r)[PASSES], unsigned char* base) const {
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      const uint32_t w0 = (r[i].x & ~swap) | (r[i].z & swap), w1 = (r[i].y & ~swap) | (r[i].w & swap);
+      const uint32_t w2 = (r[i].z & ~swap) | (r[i].x & swap), w3 = (r[i].w & ~swap) | (r[i].y & swap);
+      *reinterpret_cast<uint4*>(base + place0 + i * (RPP * 128)) =
+          make_uint4(e4m3x2_f16x2(w0), e4m3x2_f16x2_hi(w0), e4m3x2_f16x2(w1), e4m3x2_f16x2_hi(w1));
+      *reinterpret_cast<uint4*>(base + place1 + i * (RPP * 128)) =
+          make_uint4(e4m3x2_f16x2(w2), e4m3x2_f16x2_hi(w2), e4m3x2_f16x2(w3), e4m3x2_f16x2_hi(w3));
     }
   }
   // whether this lane's group has a seen key; the largest and least (positive) scale of v of such groups
@@ -318,20 +331,28 @@ struct Fetch {
     }
     return (hit & 0x80808080u) != 0;
   }
-  // NaN values that some row does not see: taken out of the matrix (this lane's own pieces), the token noted
-  __device__ __forceinline__ void note(int tile, unsigned char* base, int* first, int* any) const {
-    *any = 1;
-    const int c = lane % LPR;
+  // The rare cases work on the matrix, on this lane's own pieces, in rolled loops.
+  // Values of scale 0 are 0.
+  __device__ __forceinline__ void clear(const Tile& t, unsigned char* base) const {
 #pragma unroll 1
     for (int i = 0; i < PASSES; ++i) {
-      const int row = row_of(i);
+      if (__shfl_sync(0xffffffffu, t.vs, i * (RPP / 16) + (row0 >> 4)) == 0.f) {
+        *reinterpret_cast<uint4*>(base + place0 + i * (RPP * 128)) = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(base + place1 + i * (RPP * 128)) = make_uint4(0, 0, 0, 0);
+      }
+    }
+  }
+  // NaN values that some row does not see are taken out and the token noted.
+  __device__ __forceinline__ void note(int tile, unsigned char* base, int* first, int* any) const {
+    *any = 1;
+#pragma unroll 1
+    for (int i = 0; i < PASSES; ++i) {
 #pragma unroll 1
       for (int b = 0; b < 16; ++b) {
-        const int idx = (2 * (c & 3) + (b >> 3)) ^ (row & 7);
-        uint16_t* x = reinterpret_cast<uint16_t*>(base + (c >> 2) * 16384 + row * 128 + idx * 16 + (b & 7) * 2);
-        if ((*x & 0x7fff) > 0x7c00) {
-          atomicMin(&first[c * 16 + b], tile * kK + row);
-          *x = 0;
+        uint16_t* v = reinterpret_cast<uint16_t*>(base + ((b >> 3) != (int)(swap & 1) ? place1 : place0) + i * (RPP * 128)) + (b & 7);
+        if ((*v & 0x7fff) > 0x7c00) {
+          atomicMin(&first[c * 16 + b], tile * kK + row0 + i * RPP);
+          *v = 0;
         }
       }
     }
@@ -350,6 +371,9 @@ __device__ __forceinline__ bool wait_long(uint64_t* bar, uint32_t parity, volati
   }
   return true;
 }
+// Hides a flag's value from the compiler, so that what follows exists once and
+// not in a copy for each case.
+#define TC_ONCE(flag) asm volatile("" : "+r"(flag))
 #define TC_WAIT(bar, parity)                                                                               \
   if (!tc::bar_try(&(bar), (parity)) && !wait_long(&(bar), (parity), &sh.stop, p.c.status)) return;
 // the 256 softmax threads meet
@@ -361,18 +385,18 @@ __device__ __forceinline__ bool wait_long(uint64_t* bar, uint32_t parity, volati
   } while (0)
 
 template <int D>
-__device__ __forceinline__ void fetch_role(const AttendParams& p, const Stretch& w, Shared& sh, unsigned char* k_smem,
+__device__ __forceinline__ void fetch_role(const AttendParams& p, Shared& sh, unsigned char* k_smem,
                                            unsigned char* v_smem) {
   constexpr int kBytes = kK * D * 2;
   const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
   Walk x;
-  walk_begin(p, w, x);
+  walk_begin(p, sh, x);
   Fetch<D> f(p, x, lane, warp);
   uint32_t n = 0, j = 0, seg = 0;  // step records, data steps, segments so far
   for (bool again = true; again;) {
     f.item();
     const int common = p.causal ? x.s.len - x.s.rows + div_group(p, x.rt * kR) + 1 : x.s.len;
-    float rho = 0.f, rho_max = 0.f;
+    float rho = 0.f, rho_next = 0.f, rho_max = 0.f;
     int* first = sh.nan_first[seg & 3];
     int* any = &sh.any_nan[seg & 3];
     // tiles in the order of their stages: codes (cur), masks and scales (nxt), page and flags (far)
@@ -381,56 +405,71 @@ __device__ __forceinline__ void fetch_role(const AttendParams& p, const Stretch&
     const int end = x.tb - 1;
     int groups = 0;      // groups of the present tile still to be taken one by one
     uint32_t whole[4];   // the present tile's mask, while it is taken so
-    far = f.look(x.ta);
+    f.look(far, x.ta);
     nxt = far;
     f.settle(nxt);
     cur = nxt;
     cur.tile = x.ta - 1;
-    far = f.look(min(x.ta + 1, end));
+    f.look(far, min(x.ta + 1, end));
     float fall = 1.f;
-    bool have = false;
-    for (bool more = true; more;) {
-      const int st = j & 1;
+    int have = 0, more = 1;
+#pragma unroll 1
+    while (more) {
+      TC_ONCE(have);
+      int st = j & 1;
+      TC_ONCE(st);
       // the step after cur (tiles without a seen key are passed over)
       Tile next = cur;
+      int only = -1;  // the group that is taken alone
       if (groups) {
-        const int g = __ffs(groups) - 1;
+        only = __ffs(groups) - 1;
         groups &= groups - 1;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) next.seen[k] = (g >> 1) == k ? whole[k] & (0xffffu << (16 * (g & 1))) : 0u;
       } else {
-        more = false;
+        more = 0;
         while (next.tile < end) {
           next = nxt;
           if (next.tile < end) {
             nxt = far;
             f.settle(nxt);
-            far = f.look(min(nxt.tile + 1, end));
+            f.look(far, min(nxt.tile + 1, end));
           }
           if (next.seen[0] | next.seen[1] | next.seen[2] | next.seen[3]) {
-            more = true;
+            more = 1;
             break;
           }
         }
-        if (!more && !have) more = true;  // nothing is seen: one step of hidden keys gives the rows their zeros
-        if (more) {
+        if (!have) more = 1;  // nothing is seen: one step of hidden keys gives the rows their zeros
+      }
+      float fall_next = 1.f;
+      if (more) {
+        float hi, lo;
+        const bool has = f.range(next, hi, lo);
+        if (only < 0 && lo < hi * kRhoKeep) {
           // scales of v too far apart for one reference: the groups with a seen key one by one
-          float hi, lo;
-          const bool has = f.range(next, hi, lo);
-          if (lo < hi * kRhoKeep) {
-            const int with = (int)(__ballot_sync(0xffffffffu, has) & 0xff), g = __ffs(with) - 1;
-            groups = with & (with - 1);
+          const int with = (int)(__ballot_sync(0xffffffffu, has) & 0xff);
+          only = __ffs(with) - 1;
+          groups = with & (with - 1);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              whole[k] = next.seen[k];
-              next.seen[k] = (g >> 1) == k ? whole[k] & (0xffffu << (16 * (g & 1))) : 0u;
-            }
-          }
+          for (int k = 0; k < 4; ++k) whole[k] = next.seen[k];
+        }
+        if (only >= 0) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) next.seen[k] = (only >> 1) == k ? whole[k] & (0xffffu << (16 * (only & 1))) : 0u;
+          hi = __shfl_sync(0xffffffffu, next.vs, only);
+          lo = hi > 0.f ? hi : INFINITY;
+        }
+        // v's reference of that step, and O's factor
+        if (hi > rho_next || lo < rho_next * kRhoKeep) {
+          const float to = hi > rho_next ? hi : fmaxf(hi, rho_max * kRhoSpan);
+          fall_next = rho_next / to;
+          rho_next = to;
+          rho_max = fmaxf(rho_max, to);
         }
       }
+      TC_ONCE(have);
       if (have) {
         // the step's record
-        if (n >= kRing) TC_WAIT(sh.step_free[n % kRing], ((n / kRing) - 1) & 1);
+        TC_WAIT(sh.step_free[n % kRing], ((n / kRing) & 1) ^ 1);
         if (warp == 0) {
           Step& s = sh.step[n % kRing];
           if (lane < 8) {
@@ -454,46 +493,38 @@ __device__ __forceinline__ void fetch_role(const AttendParams& p, const Stretch&
         }
         ++n;
         // keys
-        if (j >= 2) TC_WAIT(sh.k_free[st], ((j >> 1) - 1) & 1);
+        TC_WAIT(sh.k_free[st], ((j >> 1) & 1) ^ 1);
         f.store(kr, k_smem + st * kBytes);
         tc::fence_proxy_async();
         tc::bar_arrive(&sh.k_full[st]);
       }
+      TC_ONCE(more);
       if (more) f.load(kr, p.c.k, next);
+      TC_ONCE(have);
       if (have) {
         // values
-        if (j >= 2) TC_WAIT(sh.v_free[st], ((j >> 1) - 1) & 1);
-        if (__any_sync(0xffffffffu, cur.vs == 0.f)) {
-#pragma unroll
-          for (int i = 0; i < Fetch<D>::PASSES; ++i)
-            if (__shfl_sync(0xffffffffu, cur.vs, f.row_of(i) / kGroup) == 0.f) vr[i] = make_uint4(0, 0, 0, 0);
-        }
-        f.store(vr, v_smem + st * kBytes);
+        TC_WAIT(sh.v_free[st], ((j >> 1) & 1) ^ 1);
+        unsigned char* v_at = v_smem + st * kBytes;
+        f.store(vr, v_at);
         const bool open = (cur.seen[0] & cur.seen[1] & cur.seen[2] & cur.seen[3]) == 0xffffffffu && (cur.tile + 1) * kK <= common;
-        if (!open && f.nans(vr)) f.note(cur.tile, v_smem + st * kBytes, first, any);
+        if (!open && f.nans(vr)) f.note(cur.tile, v_at, first, any);
+        if (__any_sync(0xffffffffu, cur.vs == 0.f)) f.clear(cur, v_at);
         tc::fence_proxy_async();
         tc::bar_arrive(&sh.v_full[st]);
         ++j;
       }
+      TC_ONCE(more);
       if (more) {
         f.load(vr, p.c.v, next);
-        // v's reference of the next step, and O's factor
-        float hi, lo;
-        f.range(next, hi, lo);
-        fall = 1.f;
-        if (hi > rho || lo < rho * kRhoKeep) {
-          const float to = hi > rho ? hi : fmaxf(hi, rho_max * kRhoSpan);
-          fall = rho / to;
-          rho = to;
-          rho_max = fmaxf(rho_max, to);
-        }
+        rho = rho_next;
+        fall = fall_next;
       }
       cur = next;
-      have = true;
+      have = 1;
     }
     // the end of the segment
-    if (n >= kRing) TC_WAIT(sh.step_free[n % kRing], ((n / kRing) - 1) & 1);
-    again = walk_next(p, w, x);
+    TC_WAIT(sh.step_free[n % kRing], ((n / kRing) & 1) ^ 1);
+    again = walk_next(p, sh, x);
     if (warp == 0 && lane == 0) {
       sh.step[n % kRing].end = again ? 1 : 2;
       sh.step[n % kRing].rho = rho;
@@ -660,13 +691,13 @@ __device__ __forceinline__ void write16(uint16_t* to, const float (&v)[16]) {
 }
 
 template <int D, bool BF16>
-__device__ __forceinline__ void softmax_role(const AttendParams& p, const Stretch& w, Shared& sh, unsigned char* q_smem,
+__device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, unsigned char* q_smem,
                                              uint32_t tmem, int t) {
   const int r = threadIdx.x & 127, lane = threadIdx.x & 31;
   const uint32_t lanes = (uint32_t)(r & ~31) << 16;
   const uint32_t s_at = tmem + t * 128 + lanes, o_at = tmem + 256 + t * 128 + lanes;
   Walk x;
-  walk_begin(p, w, x);
+  walk_begin(p, sh, x);
   uint32_t n = 0, it = 0, seg = 0, met = 0;
   do {
     const bool mine = t < row_tiles(p, x);
@@ -827,7 +858,7 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, const Stretc
       __threadfence();
       TC_MEET();
       const int64_t first_u = x.u - x.ta;
-      const int first = cta_of(w.units, w.ctas, first_u), last = cta_of(w.units, w.ctas, first_u + x.tiles - 1);
+      const int first = cta_of(sh.units, sh.ctas, first_u), last = cta_of(sh.units, sh.ctas, first_u + x.tiles - 1);
       if (threadIdx.x == 0) sh.last = atomicAdd(&p.counters[first], 1) == last - first;
       TC_MEET();
       if (sh.last) {
@@ -882,7 +913,7 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, const Stretc
       __syncwarp();
     }
     ++seg;
-  } while (walk_next(p, w, x));
+  } while (walk_next(p, sh, x));
 }
 
 template <int D, bool BF16>
@@ -890,11 +921,19 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(AttendParams p) 
   constexpr int kBytes = kK * D * 2;
   extern __shared__ unsigned char dyn[];
   __shared__ Shared sh;
-  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn) + 1023) & ~(uintptr_t)1023);
+  unsigned char* smem = dyn + ((1024 - (tc::su32(dyn) & 1023)) & 1023);  // (an offset: the pointer stays one to shared memory)
   const int warp = threadIdx.x >> 5;
   Stretch w;
   if (!attend_stretch<kR, kK, kThreads>(p, 1, sh.scan, w)) return;
   if (threadIdx.x == 0) {
+    sh.u0 = w.u0;
+    sh.u1 = w.u1;
+    sh.units = w.units;
+    sh.ctas = w.ctas;
+    sh.seq = w.seq;
+    sh.head = w.head;
+    sh.row_tile = w.row_tile;
+    sh.tile = w.tile;
     sh.stop = 0;
     tc::bar_init(&sh.q_full, 256);
     tc::bar_init(&sh.meet, 256);
@@ -927,10 +966,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(AttendParams p) 
   // registers: 512 threads start with 128 each, four warpgroups split them
   if (warp < 8) {
     tc::setmaxnreg_inc<kRegSoftmax>();
-    softmax_role<D, BF16>(p, w, sh, q_smem, tmem, warp >> 2);
+    softmax_role<D, BF16>(p, sh, q_smem, tmem, warp >> 2);
   } else if (warp < 12) {
     tc::setmaxnreg_inc<kRegFetch>();
-    fetch_role<D>(p, w, sh, k_smem, v_smem);
+    fetch_role<D>(p, sh, k_smem, v_smem);
   } else {
     tc::setmaxnreg_dec<kRegIssue>();
     if (warp == 12)
