@@ -5,6 +5,7 @@ its pages (include/occam.h). Argument marshalling only, as in _lib."""
 from __future__ import annotations
 
 import ctypes
+import struct
 
 import torch
 
@@ -17,18 +18,31 @@ from ._lib import (
     _check,
     _dev_tensor,
     _ptr,
-    _stream,
     library,
     occam_get_status,
 )
 
 _DTYPE = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+_ROWS = {torch.bfloat16: 0, torch.float16: 1}  # element types of cache rows
 _PAIRING = {"half": 0, "adjacent": 1}
 E4M3 = torch.float8_e4m3fn
+
+# occam_rope_tensor and occam_attend_args as packed bytes: a decode step makes
+# these calls once a layer, and filling a ctypes structure field by field takes longer
+_ROPE_TENSOR = struct.Struct("@PPiqqqq")
+_ATTEND_ARGS = struct.Struct("@iiiiqqPPPiiPPfPPq")
+assert _ROPE_TENSOR.size == ctypes.sizeof(CRopeTensor) and _ATTEND_ARGS.size == ctypes.sizeof(CAttendArgs)
 
 
 def _bad(msg: str):
     raise OccamError(OCCAM_ERR_INVALID_ARG, msg)
+
+
+def _on(stream, device) -> int:
+    """The stream's handle; the device's current one by default."""
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _rows_tensor(t, name: str, dtypes, heads: int | None = None, dim: int | None = None) -> torch.Tensor:
@@ -37,10 +51,13 @@ def _rows_tensor(t, name: str, dtypes, heads: int | None = None, dim: int | None
         _bad(f"{name} must be a CUDA tensor")
     if t.dtype not in dtypes:
         _bad(f"{name} must be one of {[str(d) for d in dtypes]}, got {t.dtype}")
-    if t.dim() != 3 or (heads is not None and t.shape[1] != heads) or (dim is not None and t.shape[2] != dim):
-        _bad(f"{name} must be [rows, {heads or 'heads'}, {dim or 'dim'}], got {list(t.shape)}")
-    if t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2])):
-        _bad(f"{name} must be dense in its last two dimensions")
+    shape = t.shape
+    if len(shape) != 3 or (heads is not None and shape[1] != heads) or (dim is not None and shape[2] != dim):
+        _bad(f"{name} must be [rows, {heads or 'heads'}, {dim or 'dim'}], got {list(shape)}")
+    if not t.is_contiguous():
+        _, h, d = t.stride()
+        if t.numel() and (d != 1 or (shape[1] > 1 and h != shape[2])):
+            _bad(f"{name} must be dense in its last two dimensions")
     return t
 
 
@@ -78,9 +95,10 @@ def occam_rope(q, k, positions, inv_freq, axis, pairing: str = "half", inverse: 
     dense tensors unless out_q / out_k are given (q itself: in place). Returns (q, k)."""
     if pairing not in _PAIRING:
         _bad(f"pairing must be one of {sorted(_PAIRING)}")
-    if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.dtype not in _DTYPE:
-        _bad("q must be [rows, heads, dim] bfloat16, float16 or float32")
+    if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dim() != 3 or q.dtype not in _DTYPE:
+        _bad("q must be a CUDA tensor [rows, heads, dim] of bfloat16, float16 or float32")
     rows, _, dim = q.shape
+    dtype = q.dtype
     _dev_tensor(inv_freq, torch.float32, "inv_freq")
     _dev_tensor(axis, torch.int32, "axis")
     if inv_freq.dim() != 1 or axis.shape != inv_freq.shape:
@@ -88,25 +106,38 @@ def occam_rope(q, k, positions, inv_freq, axis, pairing: str = "half", inverse: 
     if not isinstance(positions, torch.Tensor) or not positions.is_cuda or positions.dtype != torch.int32 or \
             positions.dim() != 2 or positions.shape[1] != rows or (rows > 1 and positions.stride(1) != 1):
         _bad("positions must be a CUDA int32 tensor [axes, rows], dense in rows")
-    ins, outs = [q] if k is None else [q, k], [out_q] if k is None else [out_q, out_k]
-    tensors, results = (CRopeTensor * 2)(), []
-    for i, (x, o) in enumerate(zip(ins, outs)):
-        name = "qk"[i]
-        if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dtype != q.dtype or x.dim() != 3 or \
-                x.shape[0] != rows or x.shape[2] != dim:
-            _bad(f"{name} must be a CUDA tensor [{rows}, heads, {dim}] {q.dtype}")
-        if o is None:
-            o = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        if not isinstance(o, torch.Tensor) or not o.is_cuda or o.shape != x.shape or o.dtype != x.dtype:
+    packed, out_q = _rope_tensor(q, out_q, "q", rows, dim, dtype)
+    n = 1
+    if k is not None:
+        more, out_k = _rope_tensor(k, out_k, "k", rows, dim, dtype)
+        packed += more
+        n = 2
+    elif out_k is not None:
+        _bad("out_k without k")
+    rc = library().occam_rope(_DTYPE[dtype], rows, dim, 2 * inv_freq.shape[0], _PAIRING[pairing], int(bool(inverse)),
+                              positions.data_ptr(), positions.stride(0), positions.shape[0], inv_freq.data_ptr(),
+                              axis.data_ptr(), n, packed, _on(stream, q.device))
+    _check(rc, "occam_rope")
+    return out_q, out_k
+
+
+def _rope_tensor(x, out, name, rows, dim, dtype):
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dtype != dtype or x.dim() != 3 or x.shape[0] != rows or \
+            x.shape[2] != dim:
+        _bad(f"{name} must be a CUDA tensor [{rows}, heads, {dim}] {dtype}")
+    row, head, one = x.stride()
+    if out is None:
+        out = torch.empty(x.shape, dtype=dtype, device=x.device)
+        heads = x.shape[1]
+        out_row, out_head, out_one = heads * dim, dim, 1
+    else:
+        if not isinstance(out, torch.Tensor) or not out.is_cuda or out.shape != x.shape or out.dtype != dtype:
             _bad(f"out_{name} must be like {name}")
-        if x.numel() and (x.stride(2) != 1 or o.stride(2) != 1):
-            _bad(f"{name} must be dense in its last dimension")
-        tensors[i] = CRopeTensor(_ptr(x), _ptr(o), x.shape[1], x.stride(0), x.stride(1), o.stride(0), o.stride(1))
-        results.append(o)
-    _check(library().occam_rope(_DTYPE[q.dtype], rows, dim, 2 * inv_freq.numel(), _PAIRING[pairing], int(bool(inverse)),
-                                _ptr(positions), positions.stride(0), positions.shape[0], _ptr(inv_freq), _ptr(axis),
-                                len(results), tensors, _stream(stream)), "occam_rope")
-    return results[0], (results[1] if k is not None else None)
+        heads = x.shape[1]
+        out_row, out_head, out_one = out.stride()
+    if (one != 1 or out_one != 1) and x.numel():
+        _bad(f"{name} must be dense in its last dimension")
+    return _ROPE_TENSOR.pack(x.data_ptr(), out.data_ptr(), heads, row, head, out_row, out_head), out
 
 
 # ------------------------------------------------------------------ the cache
@@ -159,6 +190,7 @@ class PagedCache:
                          _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(table), _ptr(length), _ptr(refs))
         self._ref = ctypes.byref(self._c)
         self.ws = self.alloc_workspace()
+        self._ws = (self.ws.data_ptr(), self.ws.numel())
 
     def alloc_workspace(self) -> torch.Tensor:
         """A workspace of the cache calls, zero-filled and 256-byte aligned."""
@@ -174,48 +206,42 @@ class PagedCache:
         return occam_get_status(self.ws if ws is None else ws, stream)
 
 
-def _cache_args(cache, ws):
+def _workspace(cache, ws):
     if not isinstance(cache, PagedCache):
         _bad("cache must be a PagedCache")
-    return cache.ws if ws is None else ws
+    return cache._ws if ws is None else (ws.data_ptr(), ws.numel())
 
 
-def _slots(t, name: str, n: int | None = None) -> torch.Tensor:
-    _dev_tensor(t, torch.int32, name)
-    if t.dim() != 1 or (n is not None and t.shape[0] != n):
-        _bad(f"{name} must be a vector" + ("" if n is None else f" of {n}"))
-    return t
-
-
-def _offsets(t, name: str, n: int) -> torch.Tensor:
-    _dev_tensor(t, torch.int64, name)
-    if t.dim() != 1 or t.shape[0] != n + 1:
-        _bad(f"{name} must have one entry more than there are sequences")
+def _vector(t, dtype, n: int | None, name: str) -> torch.Tensor:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or t.dim() != 1 or \
+            (n is not None and t.shape[0] != n) or not t.is_contiguous():
+        _bad(f"{name} must be a dense CUDA vector of {dtype}" + ("" if n is None else f" with {n} entries"))
     return t
 
 
 def occam_cache_extend(cache: PagedCache, seqs, counts, ws=None, stream=None) -> None:
     """Sequence seqs[i] grows by counts[i] tokens: pages are taken and lengths raised."""
-    ws = _cache_args(cache, ws)
-    _slots(seqs, "seqs"); _slots(counts, "counts", seqs.shape[0])
-    _check(library().occam_cache_extend(cache._ref, seqs.shape[0], _ptr(seqs), _ptr(counts), _ptr(ws), ws.numel(),
-                                        _stream(stream)), "occam_cache_extend")
+    wp, wn = _workspace(cache, ws)
+    n = _vector(seqs, torch.int32, None, "seqs").shape[0]
+    _vector(counts, torch.int32, n, "counts")
+    _check(library().occam_cache_extend(cache._ref, n, _ptr(seqs), _ptr(counts), wp, wn,
+                                        _on(stream, cache.device)), "occam_cache_extend")
 
 
 def occam_cache_append(cache: PagedCache, layer: int, k, v, seqs, row_off, ws=None, stream=None) -> None:
     """Writes rows row_off[i] .. row_off[i+1] of k and v [rows, heads, dim]
     (bfloat16 or float16, rows may be strided) as the last tokens of sequence
     seqs[i] in one layer."""
-    ws = _cache_args(cache, ws)
-    _rows_tensor(k, "k", (torch.bfloat16, torch.float16), cache.heads, cache.dim)
+    wp, wn = _workspace(cache, ws)
+    _rows_tensor(k, "k", _ROWS, cache.heads, cache.dim)
     _rows_tensor(v, "v", (k.dtype,), cache.heads, cache.dim)
     if v.shape[0] != k.shape[0]:
         _bad("k and v must have as many rows")
-    n = _slots(seqs, "seqs").shape[0]
-    _offsets(row_off, "row_off", n)
+    n = _vector(seqs, torch.int32, None, "seqs").shape[0]
+    _vector(row_off, torch.int64, n + 1, "row_off")
     _check(library().occam_cache_append(cache._ref, int(layer), _DTYPE[k.dtype], k.shape[0], _ptr(k), _row_stride(k),
-                                        _ptr(v), _row_stride(v), n, _ptr(seqs), _ptr(row_off), _ptr(ws), ws.numel(),
-                                        _stream(stream)), "occam_cache_append")
+                                        _ptr(v), _row_stride(v), n, _ptr(seqs), _ptr(row_off), wp, wn,
+                                        _on(stream, cache.device)), "occam_cache_append")
 
 
 def occam_cache_attend(cache: PagedCache, layer: int, q, seqs, row_off, max_rows: int, scale: float = 0.0,
@@ -224,17 +250,17 @@ def occam_cache_attend(cache: PagedCache, layer: int, q, seqs, row_off, max_rows
     sequences; rows may be strided) over the cache. max_rows: the most rows of one
     sequence. scale 0: 1 / sqrt(dim). keep / keep_off: uint8 flags that hide
     tokens. Returns (out, lse [rows, heads] natural logarithm)."""
-    ws = _cache_args(cache, ws)
-    _rows_tensor(q, "q", (torch.bfloat16, torch.float16), None, cache.dim)
+    wp, wn = _workspace(cache, ws)
+    _rows_tensor(q, "q", _ROWS, None, cache.dim)
     rows, heads, dim = q.shape
-    n = _slots(seqs, "seqs").shape[0]
-    _offsets(row_off, "row_off", n)
+    n = _vector(seqs, torch.int32, None, "seqs").shape[0]
+    _vector(row_off, torch.int64, n + 1, "row_off")
     total_keep = 0
     if keep is not None:
         _dev_tensor(keep, torch.uint8, "keep")
         if keep_off is None:
             _bad("keep needs keep_off")
-        _offsets(keep_off, "keep_off", n)
+        _vector(keep_off, torch.int64, n + 1, "keep_off")
         total_keep = keep.numel()
     if out is None:
         out = torch.empty((rows, heads, dim), dtype=q.dtype, device=q.device)
@@ -244,20 +270,24 @@ def occam_cache_attend(cache: PagedCache, layer: int, q, seqs, row_off, max_rows
         lse = torch.empty((rows, heads), dtype=torch.float32, device=q.device)
     elif _dev_tensor(lse, torch.float32, "lse").shape != q.shape[:2]:
         _bad("lse must be [rows, heads]")
-    a = CAttendArgs(int(layer), _DTYPE[q.dtype], heads, int(bool(causal)), rows, _row_stride(q), _ptr(q), _ptr(out),
-                    _ptr(lse), n, int(max_rows), _ptr(seqs), _ptr(row_off), float(scale), _ptr(keep),
-                    _ptr(keep_off) if keep is not None else None, total_keep)
-    _check(library().occam_cache_attend(cache._ref, ctypes.byref(a), _ptr(ws), ws.numel(), _stream(stream)),
-           "occam_cache_attend")
+    try:
+        a = _ATTEND_ARGS.pack(layer, _ROWS[q.dtype], heads, 1 if causal else 0, rows, _row_stride(q), q.data_ptr(),
+                              out.data_ptr(), lse.data_ptr(), n, max_rows, seqs.data_ptr(), row_off.data_ptr(), scale,
+                              0 if keep is None else keep.data_ptr(), 0 if keep is None else keep_off.data_ptr(),
+                              total_keep)
+    except struct.error as e:
+        _bad(f"layer, max_rows or scale: {e}")
+    _check(library().occam_cache_attend(cache._ref, a, wp, wn, _on(stream, cache.device)), "occam_cache_attend")
     return out, lse
 
 
 def occam_cache_fork(cache: PagedCache, src, dst, ws=None, stream=None) -> None:
     """Sequence dst[i] (empty) becomes a copy of src[i]; full pages are shared."""
-    ws = _cache_args(cache, ws)
-    _slots(src, "src"); _slots(dst, "dst", src.shape[0])
-    _check(library().occam_cache_fork(cache._ref, src.shape[0], _ptr(src), _ptr(dst), _ptr(ws), ws.numel(),
-                                      _stream(stream)), "occam_cache_fork")
+    wp, wn = _workspace(cache, ws)
+    n = _vector(src, torch.int32, None, "src").shape[0]
+    _vector(dst, torch.int32, n, "dst")
+    _check(library().occam_cache_fork(cache._ref, n, _ptr(src), _ptr(dst), wp, wn,
+                                      _on(stream, cache.device)), "occam_cache_fork")
 
 
 def occam_cache_compact(cache: PagedCache, seqs, keep, keep_off, layers: tuple[int, int] | None = None, ws=None,
@@ -265,18 +295,18 @@ def occam_cache_compact(cache: PagedCache, seqs, keep, keep_off, layers: tuple[i
     """Keeps the tokens of each sequence whose flag keep[keep_off[i] + p] is
     set (and those past the flags), in order; layers: the range of layers whose
     codes move (default: all)."""
-    ws = _cache_args(cache, ws)
-    n = _slots(seqs, "seqs").shape[0]
+    wp, wn = _workspace(cache, ws)
+    n = _vector(seqs, torch.int32, None, "seqs").shape[0]
     _dev_tensor(keep, torch.uint8, "keep")
-    _offsets(keep_off, "keep_off", n)
+    _vector(keep_off, torch.int64, n + 1, "keep_off")
     l0, l1 = (0, cache.layers) if layers is None else layers
     _check(library().occam_cache_compact(cache._ref, int(l0), int(l1), n, _ptr(seqs), _ptr(keep), _ptr(keep_off),
-                                         keep.numel(), _ptr(ws), ws.numel(), _stream(stream)), "occam_cache_compact")
+                                         keep.numel(), wp, wn, _on(stream, cache.device)), "occam_cache_compact")
 
 
 def occam_cache_release(cache: PagedCache, seqs, ws=None, stream=None) -> None:
     """Empties sequences; their pages lose a reference."""
-    ws = _cache_args(cache, ws)
-    _slots(seqs, "seqs")
-    _check(library().occam_cache_release(cache._ref, seqs.shape[0], _ptr(seqs), _ptr(ws), ws.numel(),
-                                         _stream(stream)), "occam_cache_release")
+    wp, wn = _workspace(cache, ws)
+    n = _vector(seqs, torch.int32, None, "seqs").shape[0]
+    _check(library().occam_cache_release(cache._ref, n, _ptr(seqs), wp, wn,
+                                         _on(stream, cache.device)), "occam_cache_release")

@@ -151,11 +151,11 @@ def library() -> ctypes.CDLL:
         lib.occam_last_call_kernels.argtypes = []
         lib.occam_set_stage2_route.argtypes = [_i32, P(_i32)]
         _ws = [_p, ctypes.c_size_t, _p]
-        lib.occam_rope.argtypes = [_i32, _i64, _i32, _i32, _i32, _i32, _p, _i64, _i32, _p, _p, _i32, P(CRopeTensor), _p]
+        lib.occam_rope.argtypes = [_i32, _i64, _i32, _i32, _i32, _i32, _p, _i64, _i32, _p, _p, _i32, ctypes.c_char_p, _p]
         lib.occam_cache_workspace_size.argtypes = [P(CCache), _i64, P(ctypes.c_size_t)]
         lib.occam_cache_extend.argtypes = [P(CCache), _i32, _p, _p] + _ws
         lib.occam_cache_append.argtypes = [P(CCache), _i32, _i32, _i64, _p, _i64, _p, _i64, _i32, _p, _p] + _ws
-        lib.occam_cache_attend.argtypes = [P(CCache), P(CAttendArgs)] + _ws
+        lib.occam_cache_attend.argtypes = [P(CCache), ctypes.c_char_p] + _ws
         lib.occam_cache_fork.argtypes = [P(CCache), _i32, _p, _p] + _ws
         lib.occam_cache_compact.argtypes = [P(CCache), _i32, _i32, _i32, _p, _p, _p, _i64] + _ws
         lib.occam_cache_release.argtypes = [P(CCache), _i32, _p] + _ws

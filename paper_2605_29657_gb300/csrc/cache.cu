@@ -34,7 +34,7 @@ constexpr int kPlanThreads = 1024;
 // read once. Bound by HBM (2 bytes read and 1 written a value).
 struct AppendParams {
   CacheDev c;
-  int layer, n, dim;
+  int layer, n;
   int64_t total_rows, k_row, v_row;
   const void* k;
   const void* v;
@@ -77,11 +77,29 @@ __device__ __forceinline__ void unpack8(uint4 r, float (&x)[8]) {
   }
 }
 
-// MAXV: 8-value vectors a thread holds (128 threads; page_tokens * dim / 8 / 128 at most)
-template <bool BF16, int MAXV>
+// the largest finite |value| of 8 elements, as a float
+template <bool BF16>
+__device__ __forceinline__ float amax8(uint4 r) {
+  const uint32_t w[4] = {r.x & 0x7fff7fffu, r.y & 0x7fff7fffu, r.z & 0x7fff7fffu, r.w & 0x7fff7fffu};
+  // magnitudes order as integers
+  uint32_t m = __vmaxu2(__vmaxu2(w[0], w[1]), __vmaxu2(w[2], w[3]));
+  m = max(m >> 16, m & 0xffffu);
+  if (m >= (BF16 ? 0x7f80u : 0x7c00u)) {  // an infinity or NaN among them
+    m = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t a = w[k] >> 16, b = w[k] & 0xffffu, end = BF16 ? 0x7f80u : 0x7c00u;
+      m = max(m, max(a < end ? a : 0u, b < end ? b : 0u));
+    }
+  }
+  return BF16 ? __uint_as_float(m << 16) : __half2float(__ushort_as_half((unsigned short)m));
+}
+
+// MAXV: 8-value vectors a thread holds (128 threads; page_tokens * D / 8 / 128 at most)
+template <bool BF16, int D, int MAXV>
 __global__ void __launch_bounds__(128) append_kernel(AppendParams p) {
   __shared__ float red[4];
-  const int T = p.c.T, D = p.dim, H = p.c.heads;
+  const int T = p.c.T, H = p.c.heads;
   const int64_t item = blockIdx.x;
   const int kv = (int)(item & 1);
   const int64_t rest = item >> 1;
@@ -114,7 +132,7 @@ __global__ void __launch_bounds__(128) append_kernel(AppendParams p) {
   float* scale = (kv ? p.c.v_scale : p.c.k_scale) + block;
   const int64_t ld = kv ? p.v_row : p.k_row;
   const uint16_t* src = static_cast<const uint16_t*>(kv ? p.v : p.k) + (r0 + (int64_t)slot * T - start) * ld + (int64_t)h * D;
-  const int vpr = D / 8;  // vectors of a row
+  constexpr int vpr = D / 8;  // vectors of a row
   const int nv = (t1 - t0) * vpr;
   uint4 x[MAXV];
   float amax = 0.f;
@@ -126,12 +144,7 @@ __global__ void __launch_bounds__(128) append_kernel(AppendParams p) {
 #pragma unroll
   for (int q = 0; q < MAXV; ++q) {
     const int e = q * 128 + threadIdx.x;
-    if (e < nv) {
-      float f[8];
-      unpack8<BF16>(x[q], f);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) amax = fmaxf(amax, finite_abs(f[j]));
-    }
+    if (e < nv) amax = fmaxf(amax, amax8<BF16>(x[q]));
   }
   amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = amax;
@@ -546,7 +559,7 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(PlanParams p
 
 struct MoveParams {
   CacheDev c;
-  int n, dim, layer0, layers;
+  int n, layer0, layers;
   const int32_t* free_list;
   const int32_t* head;
   const int32_t* lead;
@@ -563,11 +576,12 @@ struct MoveParams {
 // two) and written once. Bound by HBM.
 // MAXV: 16-code vectors a thread holds (128 threads).
 constexpr int kMoveHeads = 4;
-template <int MAXV>
+template <int D, int MAXV>
 __global__ void __launch_bounds__(128) compact_move_kernel(MoveParams p) {
   __shared__ int2 src[128];  // page and slot of each token
   __shared__ float red[2][4];
-  const int T = p.c.T, D = p.dim, H = p.c.heads, vpr = D / 16;
+  constexpr int vpr = D / 16;
+  const int T = p.c.T, H = p.c.heads;
   const int hg = (H + kMoveHeads - 1) / kMoveHeads;
   const int64_t items = (int64_t)p.head[p.n] * p.layers * 2 * hg;
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
@@ -678,17 +692,31 @@ PlanParams plan_params(const occam_cache* c, void* ws, const CacheWs& w, int n) 
   return p;
 }
 
-template <bool BF16>
+template <bool BF16, int D>
 void launch_append(const AppendParams& p, unsigned grid, cudaStream_t st) {
-  const int vecs = p.c.T * p.dim / 8 / 128;
+  const int vecs = p.c.T * D / 8 / 128;
   if (vecs <= 2)
-    append_kernel<BF16, 2><<<grid, 128, 0, st>>>(p);
+    append_kernel<BF16, D, 2><<<grid, 128, 0, st>>>(p);
   else if (vecs == 4)
-    append_kernel<BF16, 4><<<grid, 128, 0, st>>>(p);
+    append_kernel<BF16, D, 4><<<grid, 128, 0, st>>>(p);
   else if (vecs == 8)
-    append_kernel<BF16, 8><<<grid, 128, 0, st>>>(p);
+    append_kernel<BF16, D, 8><<<grid, 128, 0, st>>>(p);
   else
-    append_kernel<BF16, 16><<<grid, 128, 0, st>>>(p);
+    append_kernel<BF16, D, 16><<<grid, 128, 0, st>>>(p);
+}
+
+template <int D>
+void launch_move(const MoveParams& m, cudaStream_t st) {
+  const int vecs = m.c.T * D / 16 / 128;
+  const unsigned grid = (unsigned)cache_sms() * 12;
+  if (vecs <= 1)
+    compact_move_kernel<D, 1><<<grid, 128, 0, st>>>(m);
+  else if (vecs == 2)
+    compact_move_kernel<D, 2><<<grid, 128, 0, st>>>(m);
+  else if (vecs == 4)
+    compact_move_kernel<D, 4><<<grid, 128, 0, st>>>(m);
+  else
+    compact_move_kernel<D, 8><<<grid, 128, 0, st>>>(m);
 }
 
 }  // namespace
@@ -744,7 +772,6 @@ int occam_cache_append(const occam_cache* cache, int32_t layer, int32_t dtype, i
   p.c = cache_dev(cache, workspace, w);
   p.layer = layer;
   p.n = n;
-  p.dim = cache->dim;
   p.total_rows = total_rows;
   p.k_row = k_row;
   p.v_row = v_row;
@@ -755,10 +782,10 @@ int occam_cache_append(const occam_cache* cache, int32_t layer, int32_t dtype, i
   const int64_t grid = (total_rows / cache->page_tokens + 2 * (int64_t)n) * cache->heads * 2;
   if (grid > 0x7fffffff) return OCCAM_ERR_UNSUPPORTED;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  if (dtype == OCCAM_BF16)
-    launch_append<true>(p, (unsigned)grid, st);
+  if (cache->dim == 128)
+    dtype == OCCAM_BF16 ? launch_append<true, 128>(p, (unsigned)grid, st) : launch_append<false, 128>(p, (unsigned)grid, st);
   else
-    launch_append<false>(p, (unsigned)grid, st);
+    dtype == OCCAM_BF16 ? launch_append<true, 64>(p, (unsigned)grid, st) : launch_append<false, 64>(p, (unsigned)grid, st);
   count_launch();
   return last_error();
 }
@@ -818,7 +845,6 @@ int occam_cache_compact(const occam_cache* cache, int32_t layer_begin, int32_t l
     MoveParams m{};
     m.c = p.c;
     m.n = n;
-    m.dim = cache->dim;
     m.layer0 = layer_begin;
     m.layers = layer_end - layer_begin;
     m.free_list = p.free_list;
@@ -829,16 +855,10 @@ int occam_cache_compact(const occam_cache* cache, int32_t layer_begin, int32_t l
     m.info = p.new_pages;
     m.list = q.list;
     m.keep_off = keep_off;
-    const int vecs = cache->page_tokens * cache->dim / 16 / 128;
-    const unsigned grid = (unsigned)cache_sms() * 12;
-    if (vecs <= 1)
-      compact_move_kernel<1><<<grid, 128, 0, st>>>(m);
-    else if (vecs == 2)
-      compact_move_kernel<2><<<grid, 128, 0, st>>>(m);
-    else if (vecs == 4)
-      compact_move_kernel<4><<<grid, 128, 0, st>>>(m);
+    if (cache->dim == 128)
+      launch_move<128>(m, st);
     else
-      compact_move_kernel<8><<<grid, 128, 0, st>>>(m);
+      launch_move<64>(m, st);
     count_launch();
   }
   return last_error();
