@@ -4,10 +4,9 @@
 // With m the running maximum of s_k = scale * s(q) * ks(k) * (q . codes_k),
 // in log2 units, one pass keeps l = sum 2^(s_k - m) and O = sum 2^(s_k - m) v_k
 // and rescales both when m grows. Bound by HBM: the codes are read once, 1
-// byte a value. Each warp runs its own key tiles of 32 keys, straight from
-// global memory into the registers of its matrix instructions, with no shared memory
-// and no barrier between tiles; the next keys' loads are issued as soon as
-// the present ones are used up.
+// byte a value. Each warp runs its own key tiles of 32 keys with no barrier
+// between them; two tiles' copies to shared memory are always under way, each lane
+// copying just the pieces that its own matrix instructions take.
 //  - S^T = K Q^T and O^T = V^T P^T (m16n8k16, f16 operands, fp32 sums): keys and
 //    dims fill the 16 rows, up to 8 query rows the 8 columns, so one token of a
 //    group of 8 heads wastes nothing. The order of the summed index is free, so
@@ -23,6 +22,7 @@
 //  - the scales of v enter P relative to a running reference, so that P stays
 //    in f16's range whatever the scales are.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "attend.cuh"
@@ -34,6 +34,7 @@ using namespace occam;
 namespace {
 
 constexpr int kTile = 32;   // keys of a unit
+constexpr int kOver = 3;    // beginning and ending an item takes as long as this many units
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr int kFewRows = 32;  // query rows of a key head this file's kernel is used for
@@ -63,28 +64,32 @@ __device__ __forceinline__ uint16_t out_bits(float x, int bf16) {
   return bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(x)) : __half_as_ushort(__float2half_rn(x));
 }
 
-// N 4-byte words of 16 bytes each, or zeros
+// BYTES (16 or 8) from global to this lane's place in shared memory, zeros if !there
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t dst, const uint8_t* src, uint32_t there) {
+  const int n = there ? BYTES : 0;
+  if constexpr (BYTES == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
 template <int WORDS>
-__device__ __forceinline__ void load_codes(uint32_t (&r)[WORDS], const uint8_t* p, bool there) {
-#pragma unroll
-  for (int i = 0; i < WORDS; ++i) r[i] = 0;
-  if (there) {
-    if constexpr (WORDS == 4) {
-      const uint4 x = ldg_stream(p);
-      r[0] = x.x;
-      r[1] = x.y;
-      r[2] = x.z;
-      r[3] = x.w;
-    } else {
-      asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "l"(p));
-    }
-  }
+__device__ __forceinline__ void read_codes(uint32_t (&r)[WORDS], uint32_t src) {
+  if constexpr (WORDS == 4)
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(src) : "memory");
+  else
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(src) : "memory");
 }
 
-// A key tile's addresses and flags, found one tile ahead of its codes
+// A key tile's place: known one tile before its copies are issued
 struct TileMeta {
-  int page[2];
-  uint32_t seen;  // bit k: key k of the tile may be seen
+  int page[2];    // of each 16 keys
+  uint32_t seen;  // bit k: key k of the tile may be seen (before settle(): this lane's flag)
+};
+// What the products need of a tile whose copies are under way
+struct TileScales {
+  uint32_t seen;
+  float ks[2], vs[2];
 };
 
 // Takes NaN codes (of either sign) out of a word of values of one key, dims d .. d+3, and
@@ -112,22 +117,29 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
   __shared__ float sh_m[kWarps][R], sh_l[kWarps][R];
   __shared__ int sh_last;
   __shared__ int sh_nan[D];  // first token with a NaN in that dim, of those taken out
-  extern __shared__ float sh_o[];  // [kWarps][R][D]
+  // Each warp's copies: two slots of keys and two of values, every piece read by the lane that
+  // copied it (so nothing but the lane's own copies is waited for, and no two
+  // lanes meet in a bank). At the end of a segment the warp's sums take their place.
+  constexpr int KP = 4 * KC;                              // pieces of keys a lane holds a tile
+  constexpr int kWarpBytes = 2 * 32 * (KP * 16 + 8 * 4 * VW);
+  static_assert(kWarpBytes >= R * D * 4, "a warp's sums fit its copies' place");
+  extern __shared__ __align__(128) unsigned char sh_dyn[];
+  float* sh_o = reinterpret_cast<float*>(sh_dyn);         // row r of warp w: (w kWarpBytes / 4) + r D
+  constexpr int kWarpFloats = kWarpBytes / 4;
 
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, t = lane & 3;
+  const uint32_t k_at = smem_u32(sh_dyn) + warp * kWarpBytes + lane * 16;
+  const uint32_t v_at = smem_u32(sh_dyn) + warp * kWarpBytes + 2 * KP * 512 + lane * (4 * VW);
   for (int d = threadIdx.x; d < D; d += kThreads) sh_nan[d] = 0x7fffffff;
   Stretch w;
-  if (!attend_stretch<R, kTile, kThreads>(p, kWarps, sh, w)) return;
+  if (!attend_stretch<R, kTile, kOver, kThreads>(p, kOver + kWarps, sh, w)) return;
 
-  int i = w.seq;
-  SeqInfo s = attend_seq(p, i);
-  int h = w.head, rt = w.row_tile;
-  int64_t in_item = w.tile;
-  int tiles = key_tiles<R, kTile>(p, s, rt);
-
-  for (int64_t u = w.u0; u < w.u1;) {
-    const int ta = (int)in_item, tb = (int)min((int64_t)tiles, ta + (w.u1 - u));
+  Walk x0;
+  if (!walk_begin<R, kTile, kOver>(p, w, x0)) return;
+  do {
+    const SeqInfo s = x0.s;
+    const int i = x0.i, h = x0.h, rt = x0.rt, tiles = x0.tiles, ta = x0.ta, tb = x0.tb;
     const int rows = s.rows * p.G - rt * R;  // rows of this tile that exist, from 0
     const int32_t* table = p.c.table + (int64_t)s.seq * p.c.max_pages;
     const uint8_t* flags = nullptr;
@@ -229,51 +241,77 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
           x.seen &= k ? 0x0000ffffu : 0xffff0000u;
         }
     };
-    uint32_t kr[4][KC][4];     // rows g, g + 8, g + 16, g + 24
-    uint32_t vr[2][4][VW];     // rows 2t, 2t + 1, 2t + 8, 2t + 9 of each 16 keys
-    float ks[2], vs[2];
-    auto block_of = [&](const TileMeta& x, int k) { return (layer_page + x.page[k]) * p.c.heads + h; };
-    auto load_k = [&](const TileMeta& x, int tile) {
+    // K: rows g, g + 8, g + 16, g + 24 in KC pieces; V: rows 2t, 2t + 1, 2t + 8, 2t + 9 of each 16 keys
+    auto scales = [&](const TileMeta& x) {
+      TileScales r;
+      r.seen = x.seen;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const int64_t b = block_of(x, k);
-        ks[k] = p.c.k_scale[b];
-        const uint8_t* base = p.c.k + (b * p.c.T + ((tile * kTile + 16 * k) & tmask)) * D + t * 16;
+        const int64_t b = (layer_page + x.page[k]) * p.c.heads + h;
+        r.ks[k] = p.c.k_scale[b];
+        r.vs[k] = p.c.v_scale[b];
+      }
+      return r;
+    };
+    auto copy_k = [&](const TileMeta& x, int tile, int slot) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int64_t b = (layer_page + x.page[k]) * p.c.heads + h;
+        const uint8_t* base = p.c.k + ((b << p.c.log2T) + ((tile * kTile + 16 * k) & tmask)) * D + g * D + t * 16;
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
           for (int c = 0; c < KC; ++c)
-            load_codes<4>(kr[2 * k + r][c], base + (g + 8 * r) * D + 64 * c, (x.seen >> (16 * k + 8 * r + g)) & 1);
+            copy_async<16>(k_at + (slot * KP + (2 * k + r) * KC + c) * 512, base + 8 * r * D + 64 * c,
+                           x.seen & (1u << (16 * k + 8 * r + g)));
       }
     };
-    auto load_v = [&](const TileMeta& x, int tile) {
+    auto copy_v = [&](const TileMeta& x, int tile, int slot) {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const int64_t b = block_of(x, k);
-        vs[k] = p.c.v_scale[b];
-        const uint8_t* base = p.c.v + (b * p.c.T + ((tile * kTile + 16 * k) & tmask)) * D + g * (4 * VW);
+        const int64_t b = (layer_page + x.page[k]) * p.c.heads + h;
+        const uint8_t* base = p.c.v + ((b << p.c.log2T) + ((tile * kTile + 16 * k) & tmask)) * D + 2 * t * D + g * (4 * VW);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int row = 2 * t + (r & 1) + 8 * (r >> 1);
-          load_codes<VW>(vr[k][r], base + row * D, (x.seen >> (16 * k + row)) & 1);
+          const int row = (r & 1) + 8 * (r >> 1);
+          copy_async<4 * VW>(v_at + (slot * 8 + 4 * k + r) * (32 * 4 * VW), base + row * D, x.seen & (1u << (16 * k + 2 * t + row)));
         }
       }
     };
 
-    int tile = ta + (int)((warp - (int)(u % kWarps) + kWarps) % kWarps);
-    TileMeta cur, nxt;
+    // Two tiles' copies are under way ahead of the one in hand; keys and values
+    // of a tile are a group of copies each, waited for in order (a group may be empty).
+    int tile = ta + warp;
+    TileScales cur, nxt, far;
+    TileMeta ahead;
+    const int end = tb - 1;
+    auto fetch = [&](int to) {
+      TileMeta x = ahead;
+      settle(x);
+      ahead = meta_of(min(to + kWarps, end));
+      return x;
+    };
     if (tile < tb) {
-      cur = meta_of(tile);
-      settle(cur);
-      load_k(cur, tile);
-      load_v(cur, tile);
-      nxt = meta_of(min(tile + kWarps, tb - 1));
+      ahead = meta_of(tile);
+      TileMeta x = fetch(tile);
+      cur = scales(x);
+      copy_k(x, tile, 0);
+      cp_async_commit();
+      copy_v(x, tile, 0);
+      cp_async_commit();
+      x = fetch(min(tile + kWarps, end));
+      nxt = scales(x);
+      if (tile + kWarps < tb) copy_k(x, tile + kWarps, 1);
+      cp_async_commit();
+      if (tile + kWarps < tb) copy_v(x, tile + kWarps, 1);
+      cp_async_commit();
     }
+    int slot = 0;
     for (; tile < tb; tile += kWarps) {
-      const bool more = tile + kWarps < tb;
-      settle(nxt);
-      const TileMeta after = meta_of(min(tile + 2 * kWarps, tb - 1));
+      const int later = tile + 2 * kWarps;
+      TileMeta x2 = fetch(min(later, end));
       // scores
+      cp_async_wait<3>();
       float sc[NQ][2][4];
 #pragma unroll
       for (int nq = 0; nq < NQ; ++nq)
@@ -284,18 +322,23 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int c = 0; c < KC; ++c)
+        for (int c = 0; c < KC; ++c) {
+          uint32_t kr[2][4];
+          read_codes<4>(kr[0], k_at + (slot * KP + 2 * k * KC + c) * 512);
+          read_codes<4>(kr[1], k_at + (slot * KP + (2 * k + 1) * KC + c) * 512);
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            const uint32_t lo = kr[2 * k][c][x], hi = kr[2 * k + 1][c][x];
+            const uint32_t lo = kr[0][x], hi = kr[1][x];
             const uint32_t a0 = e4m3x2_f16x2(lo), a2 = e4m3x2_f16x2_hi(lo);
             const uint32_t a1 = e4m3x2_f16x2(hi), a3 = e4m3x2_f16x2_hi(hi);
 #pragma unroll
             for (int nq = 0; nq < NQ; ++nq) mma_f16(sc[nq][k], a0, a1, a2, a3, qf[nq][c * 4 + x][0], qf[nq][c * 4 + x][1]);
           }
-      const float ksc[2] = {ks[0], ks[1]};
+        }
       const uint32_t seen = cur.seen;
-      if (more) load_k(nxt, tile + kWarps);
+      far = scales(x2);
+      if (later < tb) copy_k(x2, later, slot);
+      cp_async_commit();
       // softmax: lane holds rows 2t, 2t + 1 of keys g, g + 8 of each 16
       const bool open = seen == 0xffffffffu && (tile + 1) * kTile <= common;
 #pragma unroll
@@ -303,7 +346,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sc[nq][k][e] *= ksc[k] * qscale[nq][e & 1];
+          for (int e = 0; e < 4; ++e) sc[nq][k][e] *= cur.ks[k] * qscale[nq][e & 1];
         if (!open) {
 #pragma unroll
           for (int k = 0; k < 2; ++k)
@@ -342,20 +385,22 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
             for (int e = 0; e < 4; ++e) o[nq][k][e] *= grow[e & 1];
         }
       }
-      if (!open) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int x = 0; x < VW; ++x)
-              note_nans(vr[k][r][x], tile * kTile + 16 * k + 2 * t + (r & 1) + 8 * (r >> 1), g * (4 * VW) + 4 * x, sh_nan);
-      }
+      cp_async_wait<3>();
       // O^T += V^T P^T, 16 keys at a time
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         if ((seen >> (16 * k)) & 0xffff) {
-          const float v = vs[k];
+          const float v = cur.vs[k];
+          uint32_t vr[4][VW];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            read_codes<VW>(vr[r], v_at + (slot * 8 + 4 * k + r) * (32 * 4 * VW));
+            if (!open) {
+#pragma unroll
+              for (int x = 0; x < VW; ++x)
+                note_nans(vr[r][x], tile * kTile + 16 * k + 2 * t + (r & 1) + 8 * (r >> 1), g * (4 * VW) + 4 * x, sh_nan);
+            }
+          }
           if (v > rho || v < rho * kRhoKeep) {  // the same in every lane
             float to = v > rho ? v : fmaxf(v, rho_max * kRhoSpan);
             if (to != rho && to > 0.f) {
@@ -379,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
           }
 #pragma unroll
           for (int x = 0; x < VW; ++x) {
-            const uint32_t w0 = vr[k][0][x], w1 = vr[k][1][x], w2 = vr[k][2][x], w3 = vr[k][3][x];
+            const uint32_t w0 = vr[0][x], w1 = vr[1][x], w2 = vr[2][x], w3 = vr[3][x];
             // two keys' bytes 0, 1 and 2, 3 side by side
             const uint32_t p0 = __byte_perm(w0, w1, 0x5140), p1 = __byte_perm(w0, w1, 0x7362);
             const uint32_t p2 = __byte_perm(w2, w3, 0x5140), p3 = __byte_perm(w2, w3, 0x7362);
@@ -393,12 +438,16 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
           }
         }
       }
-      if (more) load_v(nxt, tile + kWarps);
+      if (later < tb) copy_v(x2, later, slot);
+      cp_async_commit();
       cur = nxt;
-      nxt = after;
+      nxt = far;
+      slot ^= 1;
     }
+    cp_async_wait<0>();
 
-    // the warps' results meet in shared memory
+    // the warps' results meet in shared memory (every lane's copies have been read)
+    __syncwarp();
 #pragma unroll
     for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
@@ -413,7 +462,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
           sh_l[warp][r] = x;
         }
         // dims 16 g' .. of row r: tile k holds dims D/8 g + 2k and + 2k + 1
-        float* dst = sh_o + (warp * R + r) * D + g * (D / 8);
+        float* dst = sh_o + warp * kWarpFloats + r * D + g * (D / 8);
 #pragma unroll
         for (int k = 0; k < MT; k += 2)
           *reinterpret_cast<float4*>(dst + 2 * k) =
@@ -421,9 +470,9 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
       }
     __syncthreads();
     const bool whole = ta == 0 && tb == tiles;
-    const int slot = ta > 0 ? 0 : 1;
-    float* po = p.part_o + ((int64_t)blockIdx.x * 2 + slot) * kAttendRows * D;
-    float2* pml = p.part_ml + ((int64_t)blockIdx.x * 2 + slot) * kAttendRows;
+    const int part = ta > 0 ? 0 : 1;
+    float* po = p.part_o + ((int64_t)blockIdx.x * 2 + part) * kAttendRows * D;
+    float2* pml = p.part_ml + ((int64_t)blockIdx.x * 2 + part) * kAttendRows;
     const int live = min(rows, R);
     for (int e = threadIdx.x; e < live * D; e += kThreads) {
       const int r = e / D, d = e % D;
@@ -436,7 +485,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
       for (int k = 0; k < kWarps; ++k) {
         const float f = fast_exp2(sh_m[k][r] - ref);
         sum += sh_l[k][r] * f;
-        acc += sh_o[(k * R + r) * D + d] * f;
+        acc += sh_o[k * kWarpFloats + r * D + d] * f;
       }
       const int row = rt * R + r, j = div_group(p, row);
       if (sh_nan[d] < (p.causal ? s.len - s.rows + j + 1 : s.len)) acc = __int_as_float(0x7fc00000);
@@ -452,8 +501,8 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
     if (!whole) {
       __threadfence();
       __syncthreads();
-      const int64_t item = u - ta;  // the item's first unit
-      const int first = cta_of(w.units, w.ctas, item), last = cta_of(w.units, w.ctas, item + tiles - 1);
+      const int2 who = item_ctas<kOver>(w, x0);
+      const int first = who.x, last = who.y;
       if (threadIdx.x == 0) sh_last = atomicAdd(&p.counters[first], 1) == last - first;
       __syncthreads();
       if (sh_last) {
@@ -481,28 +530,20 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
     }
     __syncthreads();  // the shared results are free again
     for (int d = threadIdx.x; d < D; d += kThreads) sh_nan[d] = 0x7fffffff;
-
-    u += tb - ta;
-    in_item = 0;
-    if (u < w.u1) {
-      const int nrt = (s.rows * p.G + R - 1) / R;
-      if (++rt == nrt) {
-        rt = 0;
-        if (++h == p.c.heads) {
-          h = 0;
-          do {
-            s = attend_seq(p, ++i);
-          } while (s.rows == 0);
-        }
-      }
-      tiles = key_tiles<R, kTile>(p, s, rt);
-    }
-  }
+  } while (walk_next<R, kTile, kOver>(p, w, x0));
 }
 
 template <int D, int NQ>
 int launch_rows(const AttendParams& p, cudaStream_t st) {
-  const size_t smem = (size_t)kWarps * 8 * NQ * D * 4;
+  constexpr int smem = kWarps * 128 * D;  // two slots of 32 keys and values a warp
+  static std::atomic<uint64_t> ready{0};  // devices whose shared memory limit is raised
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return OCCAM_ERR_CUDA;
+  if (!((ready.load(std::memory_order_acquire) >> dev) & 1)) {
+    if (cudaFuncSetAttribute(attend_rows_kernel<D, NQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+      return OCCAM_ERR_CUDA;
+    ready.fetch_or(uint64_t(1) << dev, std::memory_order_release);
+  }
   const int grid = std::min(cache_sms() * (NQ == 1 ? 3 : 2), kAttendCtas);
   attend_rows_kernel<D, NQ><<<grid, kThreads, smem, st>>>(p);
   count_launch();

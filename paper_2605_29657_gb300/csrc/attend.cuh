@@ -8,6 +8,8 @@
 // stretch is finished there; one that is split leaves a partial result
 // (unnormalised sums, running maximum, sum) per CTA, and the CTA that
 // arrives last adds them in order -- always the same order, so results do not depend on timing.
+// An item's units are preceded by OVER empty ones: what beginning and ending an
+// item costs, in key tiles, so that CTAs with many short items get fewer tiles.
 #pragma once
 
 #include "cache.cuh"
@@ -89,24 +91,24 @@ static __device__ __noinline__ int64_t floor_sum(int64_t n, int64_t m, int64_t a
     a = t;
   }
 }
-// Key tiles of the first nrt row tiles of a sequence's head. Row tile rt < the last sees
+// Units of the first nrt row tiles of a sequence's head. Row tile rt < the last sees
 // base + 1 + floor(((rt + 1) R - 1) / G) keys.
-template <int R, int KT>
-__device__ __forceinline__ int64_t tiles_before(const AttendParams& p, const SeqInfo& s, int nrt) {
-  if (!p.causal) return (int64_t)nrt * ((s.len + KT - 1) / KT);
-  return floor_sum(nrt, (int64_t)p.G * KT, R, R - 1 + (int64_t)p.G * (s.len - s.rows + KT));
+template <int R, int KT, int OVER>
+__device__ __forceinline__ int64_t units_before(const AttendParams& p, const SeqInfo& s, int nrt) {
+  if (!p.causal) return (int64_t)nrt * ((s.len + KT - 1) / KT + OVER);
+  return (int64_t)nrt * OVER + floor_sum(nrt, (int64_t)p.G * KT, R, R - 1 + (int64_t)p.G * (s.len - s.rows + KT));
 }
-template <int R, int KT>
+template <int R, int KT, int OVER>
 __device__ __forceinline__ int64_t head_units(const AttendParams& p, const SeqInfo& s) {
   if (s.rows == 0) return 0;
   const int nrt = (s.rows * p.G + R - 1) / R;
-  return (nrt > 1 ? tiles_before<R, KT>(p, s, nrt - 1) : 0) + key_tiles<R, KT>(p, s, nrt - 1);
+  return (nrt > 1 ? units_before<R, KT, OVER>(p, s, nrt - 1) : 0) + OVER + key_tiles<R, KT>(p, s, nrt - 1);
 }
 
 // The stretch [u0, u1) of the CTA and the item its first unit is in.
 struct Stretch {
   int64_t units, u0, u1;
-  int ctas, seq, head, row_tile, tile;  // tile: u0's key tile in the item
+  int ctas, seq, head, row_tile, in_item;  // in_item: u0's place in the item
 };
 
 __device__ __forceinline__ int64_t cta_begin(int64_t units, int ctas, int c) { return units * c / ctas; }
@@ -118,14 +120,14 @@ static __device__ __noinline__ int cta_of(int64_t units, int ctas, int64_t u) {
 }
 
 // Block-wide (NT threads, all of them); sh: NT / 32 + 4 int64 of shared memory. False: no work for this CTA.
-template <int R, int KT, int NT>
+template <int R, int KT, int OVER, int NT>
 __device__ __forceinline__ bool attend_stretch(const AttendParams& p, int min_units, int64_t* sh, Stretch& w) {
   constexpr int NWARP = NT / 32;
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   const int per = (p.n + NT - 1) / NT;
   const int i0 = min(t * per, p.n), i1 = min(i0 + per, p.n);
   int64_t mine = 0;
-  for (int i = i0; i < i1; ++i) mine += p.c.heads * head_units<R, KT>(p, attend_seq(p, i));
+  for (int i = i0; i < i1; ++i) mine += p.c.heads * head_units<R, KT, OVER>(p, attend_seq(p, i));
   int64_t incl = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -150,19 +152,19 @@ __device__ __forceinline__ bool attend_stretch(const AttendParams& p, int min_un
   if (w.u0 >= at && w.u0 < at + mine) {
     for (int i = i0; i < i1; ++i) {
       const SeqInfo s = attend_seq(p, i);
-      const int64_t hu = head_units<R, KT>(p, s);
+      const int64_t hu = head_units<R, KT, OVER>(p, s);
       if (w.u0 < at + p.c.heads * hu) {
         const int64_t off = w.u0 - at;
         const int64_t h = off / hu, in_head = off - h * hu;
         int lo = 0, hi = (s.rows * p.G + R - 1) / R;  // the last row tile that begins at or before in_head
         while (hi - lo > 1) {
           const int mid = (lo + hi) >> 1;
-          if (tiles_before<R, KT>(p, s, mid) <= in_head) lo = mid; else hi = mid;
+          if (units_before<R, KT, OVER>(p, s, mid) <= in_head) lo = mid; else hi = mid;
         }
         sh[NWARP] = i;
         sh[NWARP + 1] = h;
         sh[NWARP + 2] = lo;
-        sh[NWARP + 3] = in_head - (lo ? tiles_before<R, KT>(p, s, lo) : 0);
+        sh[NWARP + 3] = in_head - (lo ? units_before<R, KT, OVER>(p, s, lo) : 0);
         break;
       }
       at += p.c.heads * hu;
@@ -172,8 +174,55 @@ __device__ __forceinline__ bool attend_stretch(const AttendParams& p, int min_un
   w.seq = (int)sh[NWARP];
   w.head = (int)sh[NWARP + 1];
   w.row_tile = (int)sh[NWARP + 2];
-  w.tile = (int)sh[NWARP + 3];
+  w.in_item = (int)sh[NWARP + 3];
   return true;
+}
+
+// The segment (an item's key tiles ta .. tb-1, those in the CTA's stretch) a role is at.
+struct Walk {
+  SeqInfo s;
+  int64_t item;  // the item's first unit
+  int i, h, rt, tiles, ta, tb;
+};
+// False if no tile of the item lies in the stretch.
+template <int R, int KT, int OVER, class W>
+__device__ __forceinline__ bool walk_set(const AttendParams& p, const W& w, Walk& x, int in_item) {
+  x.tiles = key_tiles<R, KT>(p, x.s, x.rt);
+  x.ta = max(in_item - OVER, 0);
+  x.tb = (int)max(min(w.u1 - x.item - OVER, (int64_t)x.tiles), (int64_t)0);
+  return x.ta < x.tb;
+}
+// The next segment; false at the end of the stretch.
+template <int R, int KT, int OVER, class W>
+__device__ __forceinline__ bool walk_next(const AttendParams& p, const W& w, Walk& x) {
+  x.item += OVER + x.tiles;
+  if (x.item + OVER >= w.u1) return false;
+  const int nrt = (x.s.rows * p.G + R - 1) / R;
+  if (++x.rt == nrt) {
+    x.rt = 0;
+    if (++x.h == p.c.heads) {
+      x.h = 0;
+      do {
+        x.s = attend_seq(p, ++x.i);
+      } while (x.s.rows == 0);
+    }
+  }
+  return walk_set<R, KT, OVER>(p, w, x, 0);
+}
+// The first segment; false if the stretch has none.
+template <int R, int KT, int OVER, class W>
+__device__ __forceinline__ bool walk_begin(const AttendParams& p, const W& w, Walk& x) {
+  x.i = w.seq;
+  x.s = attend_seq(p, x.i);
+  x.h = w.head;
+  x.rt = w.row_tile;
+  x.item = w.u0 - w.in_item;
+  return walk_set<R, KT, OVER>(p, w, x, w.in_item) || walk_next<R, KT, OVER>(p, w, x);
+}
+// The first and the last CTA with tiles of the item.
+template <int OVER, class W>
+__device__ __forceinline__ int2 item_ctas(const W& w, const Walk& x) {
+  return make_int2(cta_of(w.units, w.ctas, x.item + OVER), cta_of(w.units, w.ctas, x.item + OVER + x.tiles - 1));
 }
 
 }  // namespace occam

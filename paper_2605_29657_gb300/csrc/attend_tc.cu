@@ -33,6 +33,7 @@ namespace {
 
 constexpr int kR = 256;        // query rows of an item
 constexpr int kK = 128;        // keys of a tile
+constexpr int kOver = 4;       // beginning and ending an item takes as long as this many tiles
 constexpr int kGroup = 16;     // keys that share a page at least
 constexpr int kThreads = 512;
 constexpr int kRing = 4;
@@ -61,7 +62,7 @@ struct Shared {
   Step step[kRing];
   int64_t scan[kThreads / 32 + 4];
   volatile int64_t u0, u1, units;   // the CTA's stretch (see Stretch)
-  volatile int ctas, seq, head, row_tile, tile;
+  volatile int ctas, seq, head, row_tile, in_item;
   uint32_t tmem;
   int stop;            // a wait ran out
   int last;
@@ -145,41 +146,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16
       : "memory");
 }
 
-// The item (sequence, head, row tile) a role is at, and its walk along the CTA's stretch.
-struct Walk {
-  SeqInfo s;
-  int i, h, rt, tiles, ta, tb;
-  int64_t u;
-};
-__device__ __forceinline__ void walk_begin(const AttendParams& p, const Shared& w, Walk& x) {
-  x.i = w.seq;
-  x.s = attend_seq(p, x.i);
-  x.h = w.head;
-  x.rt = w.row_tile;
-  x.tiles = key_tiles<kR, kK>(p, x.s, x.rt);
-  x.u = w.u0;
-  x.ta = w.tile;
-  x.tb = (int)min((int64_t)x.tiles, x.ta + (w.u1 - x.u));
-}
-// False at the end of the stretch.
-__device__ __forceinline__ bool walk_next(const AttendParams& p, const Shared& w, Walk& x) {
-  x.u += x.tb - x.ta;
-  if (x.u >= w.u1) return false;
-  const int nrt = (x.s.rows * p.G + kR - 1) / kR;
-  if (++x.rt == nrt) {
-    x.rt = 0;
-    if (++x.h == p.c.heads) {
-      x.h = 0;
-      do {
-        x.s = attend_seq(p, ++x.i);
-      } while (x.s.rows == 0);
-    }
-  }
-  x.tiles = key_tiles<kR, kK>(p, x.s, x.rt);
-  x.ta = 0;
-  x.tb = (int)min((int64_t)x.tiles, w.u1 - x.u);
-  return true;
-}
 __device__ __forceinline__ int row_tiles(const AttendParams& p, const Walk& x) {
   return x.s.rows * p.G - x.rt * kR > 128 ? 2 : 1;
 }
@@ -390,7 +356,7 @@ __device__ __forceinline__ void fetch_role(const AttendParams& p, Shared& sh, un
   constexpr int kBytes = kK * D * 2;
   const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
   Walk x;
-  walk_begin(p, sh, x);
+  if (!walk_begin<kR, kK, kOver>(p, sh, x)) return;
   Fetch<D> f(p, x, lane, warp);
   uint32_t n = 0, j = 0, seg = 0;  // step records, data steps, segments so far
   for (bool again = true; again;) {
@@ -524,7 +490,7 @@ __device__ __forceinline__ void fetch_role(const AttendParams& p, Shared& sh, un
     }
     // the end of the segment
     TC_WAIT(sh.step_free[n % kRing], ((n / kRing) & 1) ^ 1);
-    again = walk_next(p, sh, x);
+    again = walk_next<kR, kK, kOver>(p, sh, x);
     if (warp == 0 && lane == 0) {
       sh.step[n % kRing].end = again ? 1 : 2;
       sh.step[n % kRing].rho = rho;
@@ -697,7 +663,7 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
   const uint32_t lanes = (uint32_t)(r & ~31) << 16;
   const uint32_t s_at = tmem + t * 128 + lanes, o_at = tmem + 256 + t * 128 + lanes;
   Walk x;
-  walk_begin(p, sh, x);
+  if (!walk_begin<kR, kK, kOver>(p, sh, x)) return;
   uint32_t n = 0, it = 0, seg = 0, met = 0;
   do {
     const bool mine = t < row_tiles(p, x);
@@ -857,8 +823,8 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
     if (!done) {
       __threadfence();
       TC_MEET();
-      const int64_t first_u = x.u - x.ta;
-      const int first = cta_of(sh.units, sh.ctas, first_u), last = cta_of(sh.units, sh.ctas, first_u + x.tiles - 1);
+      const int2 who = item_ctas<kOver>(sh, x);
+      const int first = who.x, last = who.y;
       if (threadIdx.x == 0) sh.last = atomicAdd(&p.counters[first], 1) == last - first;
       TC_MEET();
       if (sh.last) {
@@ -913,7 +879,7 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
       __syncwarp();
     }
     ++seg;
-  } while (walk_next(p, sh, x));
+  } while (walk_next<kR, kK, kOver>(p, sh, x));
 }
 
 template <int D, bool BF16>
@@ -924,7 +890,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(AttendParams p) 
   unsigned char* smem = dyn + ((1024 - (tc::su32(dyn) & 1023)) & 1023);  // (an offset: the pointer stays one to shared memory)
   const int warp = threadIdx.x >> 5;
   Stretch w;
-  if (!attend_stretch<kR, kK, kThreads>(p, 1, sh.scan, w)) return;
+  if (!attend_stretch<kR, kK, kOver, kThreads>(p, kOver + 1, sh.scan, w)) return;
+  {
+    Walk x;
+    if (!walk_begin<kR, kK, kOver>(p, w, x)) return;  // no tile in the stretch: every role has at least one from here on
+  }
   if (threadIdx.x == 0) {
     sh.u0 = w.u0;
     sh.u1 = w.u1;
@@ -933,7 +903,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(AttendParams p) 
     sh.seq = w.seq;
     sh.head = w.head;
     sh.row_tile = w.row_tile;
-    sh.tile = w.tile;
+    sh.in_item = w.in_item;
     sh.stop = 0;
     tc::bar_init(&sh.q_full, 256);
     tc::bar_init(&sh.meet, 256);
