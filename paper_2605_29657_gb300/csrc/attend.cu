@@ -21,9 +21,13 @@
 //    first such token of each dim is noted for the rows past it.
 //  - the scales of v enter P relative to a running reference, so that P stays
 //    in f16's range whatever the scales are.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <mutex>
 
 #include "attend.cuh"
 #include "attend_tc.cuh"
@@ -35,6 +39,7 @@ namespace {
 
 constexpr int kTile = 32;   // keys of a unit
 constexpr int kOver = 3;    // beginning and ending an item takes as long as this many units
+constexpr int kShared = 0;  // sixteenths of the work left to CTAs that become free
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr int kFewRows = 32;  // query rows of a key head this file's kernel is used for
@@ -64,14 +69,27 @@ __device__ __forceinline__ uint16_t out_bits(float x, int bf16) {
   return bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(x)) : __half_as_ushort(__float2half_rn(x));
 }
 
-// BYTES (16 or 8) from global to this lane's place in shared memory, zeros if !there
-template <int BYTES>
-__device__ __forceinline__ void copy_async(uint32_t dst, const uint8_t* src, uint32_t there) {
-  const int n = there ? BYTES : 0;
-  if constexpr (BYTES == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-  else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+// Rows of 128 (64) bytes lie in shared memory with the 128-byte (64-byte) swizzle.
+// piece: where a row's 16-byte piece c is. order: the rows and pieces that
+// neighbouring lanes take, so that eight lanes always meet eight different banks' groups.
+template <int D>
+__device__ __forceinline__ int piece(int row, int c) { return D == 128 ? c ^ (row & 7) : c ^ ((row >> 1) & 3); }
+template <int D>
+__device__ __forceinline__ int order(int g) { return D == 128 ? (g >> 1) | ((g & 1) << 2) : g; }
+template <int D>
+__device__ __forceinline__ int value_place(int row, int g) {
+  return D == 128 ? piece<D>(row, order<D>(g)) * 16 : piece<D>(row, g >> 1) * 16 + (g & 1) * 8;
+}
+// 16 bytes from global to shared memory, zeros if !there
+__device__ __forceinline__ void copy_async16(uint32_t dst, const uint8_t* src, uint32_t there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+// a box of rows from row `row` on
+__device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, int row, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+      "l"(map), "r"(0), "r"(row), "r"(smem_u32(bar))
+      : "memory");
 }
 template <int WORDS>
 __device__ __forceinline__ void read_codes(uint32_t (&r)[WORDS], uint32_t src) {
@@ -106,37 +124,46 @@ __device__ __forceinline__ void note_nans(uint32_t& w, int key, int d, int* firs
   }
 }
 
-// NQ: tiles of 8 query rows
-template <int D, int NQ>
-__global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(AttendParams p) {
+// NQ: tiles of 8 query rows. TMA: whole tiles come by tensor copies; else row by
+// row, leaving out hidden rows.
+template <int D, int NQ, bool TMA>
+__global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
+    attend_rows_kernel(AttendParams p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
   constexpr int R = 8 * NQ;
   constexpr int KC = D / 64;      // 16-byte pieces of a key row a lane holds
   constexpr int VW = D / 32;      // 4-byte words of a value row a lane holds
   constexpr int MT = D / 16;      // tiles of 16 dims
   __shared__ int64_t sh[kWarps + 4];
   __shared__ float sh_m[kWarps][R], sh_l[kWarps][R];
-  __shared__ int sh_last;
+  __shared__ int sh_last, sh_next;
   __shared__ int sh_nan[D];  // first token with a NaN in that dim, of those taken out
-  // Each warp's copies: two slots of keys and two of values, every piece read by the lane that
-  // copied it (so nothing but the lane's own copies is waited for, and no two
-  // lanes meet in a bank). At the end of a segment the warp's sums take their place.
-  constexpr int KP = 4 * KC;                              // pieces of keys a lane holds a tile
-  constexpr int kWarpBytes = 2 * 32 * (KP * 16 + 8 * 4 * VW);
+  // Each warp's copies: two slots of keys and two of values, 32 rows each. At the end
+  // of a segment the warp's sums take their place.
+  constexpr int kSlot = kTile * D, kWarpBytes = 4 * kSlot;
   static_assert(kWarpBytes >= R * D * 4, "a warp's sums fit its copies' place");
-  extern __shared__ __align__(128) unsigned char sh_dyn[];
-  float* sh_o = reinterpret_cast<float*>(sh_dyn);         // row r of warp w: (w kWarpBytes / 4) + r D
+  __shared__ uint64_t sh_bar[kWarps][4];
+  extern __shared__ __align__(1024) unsigned char sh_dyn[];
+  unsigned char* sh_slots = sh_dyn + ((1024 - (smem_u32(sh_dyn) & 1023)) & 1023);
+  float* sh_o = reinterpret_cast<float*>(sh_slots);       // row r of warp w: (w kWarpBytes / 4) + r D
   constexpr int kWarpFloats = kWarpBytes / 4;
 
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int g = lane >> 2, t = lane & 3;
-  const uint32_t k_at = smem_u32(sh_dyn) + warp * kWarpBytes + lane * 16;
-  const uint32_t v_at = smem_u32(sh_dyn) + warp * kWarpBytes + 2 * KP * 512 + lane * (4 * VW);
+  const uint32_t k_at = smem_u32(sh_slots) + warp * kWarpBytes, v_at = k_at + 2 * kSlot;
+  uint64_t* bars = sh_bar[warp];  // keys of slot 0, 1, values of slot 0, 1
+  uint32_t turn = 0;              // tiles this warp has taken
+  if (TMA && threadIdx.x < kWarps * 4) mbar_init(&sh_bar[0][0] + threadIdx.x, 1);
+  if (TMA) fence_mbar_init();
   for (int d = threadIdx.x; d < D; d += kThreads) sh_nan[d] = 0x7fffffff;
+  Line line;
+  const LinePart part0 = attend_line<R, kTile, kOver, kThreads>(p, kOver + kWarps, kAttendCtas, kShared, sh, line);
+  // (every CTA takes part in the last count below)
+  for (int c = line.units > 0 ? (int)blockIdx.x : line.total; c < line.total;) {
   Stretch w;
-  if (!attend_stretch<R, kTile, kOver, kThreads>(p, kOver + kWarps, sh, w)) return;
-
+  attend_find<R, kTile, kOver, kThreads>(p, line, part0, c, sh, w);
+  if (threadIdx.x == 0) sh_next = line.total > line.first ? line.first + atomicAdd(p.tickets, 1) : line.total;
   Walk x0;
-  if (!walk_begin<R, kTile, kOver>(p, w, x0)) return;
+  if (walk_begin<R, kTile, kOver>(p, w, x0))
   do {
     const SeqInfo s = x0.s;
     const int i = x0.i, h = x0.h, rt = x0.rt, tiles = x0.tiles, ta = x0.ta, tb = x0.tb;
@@ -154,7 +181,112 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
       }
     }
 
-    // the query rows as f16, scaled by a power of two each
+    const int64_t layer_page = (int64_t)p.layer * p.c.pages;
+    const int tmask = p.c.T - 1;
+    auto meta_of = [&](int tile) {
+      TileMeta x;
+      const int key = tile * kTile;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int first = key + 16 * k;
+        x.page[k] = first < s.len ? table[first >> p.c.log2T] : 0;
+      }
+      bool see = key + lane < s.len;
+      if (key + lane < n_flags) see = flags[key + lane] != 0;
+      x.seen = see;
+      return x;
+    };
+    // the ballot is taken one tile later, when the flag has arrived
+    auto settle = [&](TileMeta& x) {
+      x.seen = __ballot_sync(0xffffffffu, x.seen != 0);
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        if ((unsigned)x.page[k] >= (unsigned)p.c.pages) {
+          set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
+          x.page[k] = 0;
+          x.seen &= k ? 0x0000ffffu : 0xffff0000u;
+        }
+    };
+    auto scales = [&](const TileMeta& x) {
+      TileScales r;
+      r.seen = x.seen;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int64_t b = (layer_page + x.page[k]) * p.c.heads + h;
+        r.ks[k] = p.c.k_scale[b];
+        r.vs[k] = p.c.v_scale[b];
+      }
+      return r;
+    };
+    // 32 rows of codes (keys or values) of a tile to the slot at `dst`
+    auto copy = [&](const CUtensorMap& map, const uint8_t* codes, const TileMeta& x, int tile, uint32_t dst, uint64_t* bar) {
+      if constexpr (TMA) {
+        if (lane == 0) {
+          if (p.c.T >= kTile) {
+            mbar_arrive_expect_tx(bar, kTile * D);
+            const int64_t b = (layer_page + x.page[0]) * p.c.heads + h;
+            tma_rows(dst, &map, (int)((b << p.c.log2T) + ((tile * kTile) & tmask)), bar);
+          } else {
+            const bool both = (x.seen >> 16) != 0;  // else the second page may not be there
+            mbar_arrive_expect_tx(bar, both ? kTile * D : 16 * D);
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+              if (k == 0 || both)
+                tma_rows(dst + k * 16 * D, &map, (int)(((layer_page + x.page[k]) * p.c.heads + h) << p.c.log2T), bar);
+          }
+        }
+      } else {
+        // a lane takes a 16-byte piece of every RPC-th row; hidden rows are not read, but become zeros
+        constexpr int LPR = D / 16, RPC = 32 / LPR;
+        const int r0 = lane / LPR, c = lane % LPR;
+#pragma unroll
+        for (int i = 0; i < LPR; ++i) {
+          const int row = i * RPC + r0;
+          const int64_t b = (layer_page + (row < 16 ? x.page[0] : x.page[1])) * p.c.heads + h;
+          copy_async16(dst + row * D + piece<D>(row, c) * 16, codes + ((b << p.c.log2T) + ((tile * kTile + row) & tmask)) * D + c * 16,
+                       (x.seen >> row) & 1);
+        }
+        cp_async_commit();
+      }
+    };
+    auto arrived = [&](uint64_t* bar) {
+      if constexpr (TMA) {
+        if (!mbar_wait(bar, (turn >> 1) & 1, kSpinLimit)) set_status(p.c.status, OCCAM_ERR_TIMEOUT);
+      } else {
+        cp_async_wait<3>();
+      }
+      __syncwarp();
+    };
+
+    // Two tiles' copies are under way ahead of the one in hand, keys and values
+    // each by themselves.
+    int tile = ta + warp;
+    TileScales cur, nxt, far;
+    TileMeta ahead;
+    const int end = tb - 1;
+    auto fetch = [&](int to) {
+      TileMeta x = ahead;
+      settle(x);
+      ahead = meta_of(min(to + kWarps, end));
+      return x;
+    };
+    if (tile < tb) {
+      ahead = meta_of(tile);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int to = tile + i * kWarps;
+        const TileMeta x = fetch(min(to, end));
+        if (i == 0) cur = scales(x); else nxt = scales(x);
+        const int slot = (turn + i) & 1;
+        if (to < tb || !TMA) {
+          TileMeta y = x;
+          if (to >= tb) y.seen = 0;
+          copy(map_k, p.c.k, y, min(to, end), k_at + slot * kSlot, bars + slot);
+          copy(map_v, p.c.v, y, min(to, end), v_at + slot * kSlot, bars + 2 + slot);
+        }
+      }
+    }
+    // (while the first copies are under way) the query rows as f16, scaled by a power of two each
     uint32_t qf[NQ][4 * KC][2];
     float qscale[NQ][2];  // of rows 2t and 2t + 1
     int limit[NQ][2];     // keys those rows see
@@ -215,103 +347,13 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
     }
     float rho = 0.f, rho_max = 0.f;  // O is held in units of rho
 
-    const int64_t layer_page = (int64_t)p.layer * p.c.pages;
-    const int tmask = p.c.T - 1;
-    auto meta_of = [&](int tile) {
-      TileMeta x;
-      const int key = tile * kTile;
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int first = key + 16 * k;
-        x.page[k] = first < s.len ? table[first >> p.c.log2T] : 0;
-      }
-      bool see = key + lane < s.len;
-      if (key + lane < n_flags) see = flags[key + lane] != 0;
-      x.seen = see;
-      return x;
-    };
-    // the ballot is taken one tile later, when the flag has arrived
-    auto settle = [&](TileMeta& x) {
-      x.seen = __ballot_sync(0xffffffffu, x.seen != 0);
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-        if ((unsigned)x.page[k] >= (unsigned)p.c.pages) {
-          set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
-          x.page[k] = 0;
-          x.seen &= k ? 0x0000ffffu : 0xffff0000u;
-        }
-    };
-    // K: rows g, g + 8, g + 16, g + 24 in KC pieces; V: rows 2t, 2t + 1, 2t + 8, 2t + 9 of each 16 keys
-    auto scales = [&](const TileMeta& x) {
-      TileScales r;
-      r.seen = x.seen;
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int64_t b = (layer_page + x.page[k]) * p.c.heads + h;
-        r.ks[k] = p.c.k_scale[b];
-        r.vs[k] = p.c.v_scale[b];
-      }
-      return r;
-    };
-    auto copy_k = [&](const TileMeta& x, int tile, int slot) {
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int64_t b = (layer_page + x.page[k]) * p.c.heads + h;
-        const uint8_t* base = p.c.k + ((b << p.c.log2T) + ((tile * kTile + 16 * k) & tmask)) * D + g * D + t * 16;
-#pragma unroll
-        for (int r = 0; r < 2; ++r)
-#pragma unroll
-          for (int c = 0; c < KC; ++c)
-            copy_async<16>(k_at + (slot * KP + (2 * k + r) * KC + c) * 512, base + 8 * r * D + 64 * c,
-                           x.seen & (1u << (16 * k + 8 * r + g)));
-      }
-    };
-    auto copy_v = [&](const TileMeta& x, int tile, int slot) {
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int64_t b = (layer_page + x.page[k]) * p.c.heads + h;
-        const uint8_t* base = p.c.v + ((b << p.c.log2T) + ((tile * kTile + 16 * k) & tmask)) * D + 2 * t * D + g * (4 * VW);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int row = (r & 1) + 8 * (r >> 1);
-          copy_async<4 * VW>(v_at + (slot * 8 + 4 * k + r) * (32 * 4 * VW), base + row * D, x.seen & (1u << (16 * k + 2 * t + row)));
-        }
-      }
-    };
-
-    // Two tiles' copies are under way ahead of the one in hand; keys and values
-    // of a tile are a group of copies each, waited for in order (a group may be empty).
-    int tile = ta + warp;
-    TileScales cur, nxt, far;
-    TileMeta ahead;
-    const int end = tb - 1;
-    auto fetch = [&](int to) {
-      TileMeta x = ahead;
-      settle(x);
-      ahead = meta_of(min(to + kWarps, end));
-      return x;
-    };
-    if (tile < tb) {
-      ahead = meta_of(tile);
-      TileMeta x = fetch(tile);
-      cur = scales(x);
-      copy_k(x, tile, 0);
-      cp_async_commit();
-      copy_v(x, tile, 0);
-      cp_async_commit();
-      x = fetch(min(tile + kWarps, end));
-      nxt = scales(x);
-      if (tile + kWarps < tb) copy_k(x, tile + kWarps, 1);
-      cp_async_commit();
-      if (tile + kWarps < tb) copy_v(x, tile + kWarps, 1);
-      cp_async_commit();
-    }
-    int slot = 0;
     for (; tile < tb; tile += kWarps) {
       const int later = tile + 2 * kWarps;
+      const int slot = turn & 1;
       TileMeta x2 = fetch(min(later, end));
+      if (later >= tb) x2.seen = 0;
       // scores
-      cp_async_wait<3>();
+      arrived(bars + slot);
       float sc[NQ][2][4];
 #pragma unroll
       for (int nq = 0; nq < NQ; ++nq)
@@ -324,8 +366,11 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
 #pragma unroll
         for (int c = 0; c < KC; ++c) {
           uint32_t kr[2][4];
-          read_codes<4>(kr[0], k_at + (slot * KP + 2 * k * KC + c) * 512);
-          read_codes<4>(kr[1], k_at + (slot * KP + (2 * k + 1) * KC + c) * 512);
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const int row = 16 * k + 8 * r + order<D>(g);
+            read_codes<4>(kr[r], k_at + slot * kSlot + row * D + piece<D>(row, t + 4 * c) * 16);
+          }
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
             const uint32_t lo = kr[0][x], hi = kr[1][x];
@@ -337,8 +382,8 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
         }
       const uint32_t seen = cur.seen;
       far = scales(x2);
-      if (later < tb) copy_k(x2, later, slot);
-      cp_async_commit();
+      __syncwarp();
+      if (later < tb || !TMA) copy(map_k, p.c.k, x2, min(later, end), k_at + slot * kSlot, bars + slot);
       // softmax: lane holds rows 2t, 2t + 1 of keys g, g + 8 of each 16
       const bool open = seen == 0xffffffffu && (tile + 1) * kTile <= common;
 #pragma unroll
@@ -352,7 +397,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
           for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const int key = 16 * k + 8 * (e >> 1) + g;
+              const int key = 16 * k + 8 * (e >> 1) + order<D>(g);
               const bool see = ((seen >> key) & 1) && tile * kTile + key < limit[nq][e & 1];
               sc[nq][k][e] = see ? sc[nq][k][e] : -INFINITY;
             }
@@ -385,7 +430,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
             for (int e = 0; e < 4; ++e) o[nq][k][e] *= grow[e & 1];
         }
       }
-      cp_async_wait<3>();
+      arrived(bars + 2 + slot);
       // O^T += V^T P^T, 16 keys at a time
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -394,11 +439,15 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
           uint32_t vr[4][VW];
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            read_codes<VW>(vr[r], v_at + (slot * 8 + 4 * k + r) * (32 * 4 * VW));
+            const int row = 16 * k + 8 * (r >> 1) + order<D>(2 * t + (r & 1));
+            read_codes<VW>(vr[r], v_at + slot * kSlot + row * D + value_place<D>(row, g));
             if (!open) {
+              // hidden rows may be anything
 #pragma unroll
-              for (int x = 0; x < VW; ++x)
-                note_nans(vr[r][x], tile * kTile + 16 * k + 2 * t + (r & 1) + 8 * (r >> 1), g * (4 * VW) + 4 * x, sh_nan);
+              for (int x = 0; x < VW; ++x) {
+                if (!((seen >> row) & 1)) vr[r][x] = 0;
+                note_nans(vr[r][x], tile * kTile + row, order<D>(g) * (4 * VW) + 4 * x, sh_nan);
+              }
             }
           }
           if (v > rho || v < rho * kRhoKeep) {  // the same in every lane
@@ -438,13 +487,13 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
           }
         }
       }
-      if (later < tb) copy_v(x2, later, slot);
-      cp_async_commit();
+      __syncwarp();
+      if (later < tb || !TMA) copy(map_v, p.c.v, x2, min(later, end), v_at + slot * kSlot, bars + 2 + slot);
       cur = nxt;
       nxt = far;
-      slot ^= 1;
+      ++turn;
     }
-    cp_async_wait<0>();
+    if (!TMA) cp_async_wait<0>();
 
     // the warps' results meet in shared memory (every lane's copies have been read)
     __syncwarp();
@@ -462,7 +511,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
           sh_l[warp][r] = x;
         }
         // dims 16 g' .. of row r: tile k holds dims D/8 g + 2k and + 2k + 1
-        float* dst = sh_o + warp * kWarpFloats + r * D + g * (D / 8);
+        float* dst = sh_o + warp * kWarpFloats + r * D + order<D>(g) * (D / 8);
 #pragma unroll
         for (int k = 0; k < MT; k += 2)
           *reinterpret_cast<float4*>(dst + 2 * k) =
@@ -471,83 +520,180 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2) attend_rows_kernel(
     __syncthreads();
     const bool whole = ta == 0 && tb == tiles;
     const int part = ta > 0 ? 0 : 1;
-    float* po = p.part_o + ((int64_t)blockIdx.x * 2 + part) * kAttendRows * D;
-    float2* pml = p.part_ml + ((int64_t)blockIdx.x * 2 + part) * kAttendRows;
+    float* po = p.part_o + ((int64_t)w.index * 2 + part) * kAttendRows * D;
+    float2* pml = p.part_ml + ((int64_t)w.index * 2 + part) * kAttendRows;
     const int live = min(rows, R);
-    for (int e = threadIdx.x; e < live * D; e += kThreads) {
-      const int r = e / D, d = e % D;
+    for (int e = threadIdx.x; e < live * D / 4; e += kThreads) {
+      const int r = e / (D / 4), d = e % (D / 4) * 4;
       float mx = -INFINITY;
 #pragma unroll
       for (int k = 0; k < kWarps; ++k) mx = fmaxf(mx, sh_m[k][r]);
       const float ref = mx == -INFINITY ? 0.f : mx;
-      float sum = 0.f, acc = 0.f;
+      float sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < kWarps; ++k) {
         const float f = fast_exp2(sh_m[k][r] - ref);
-        sum += sh_l[k][r] * f;
-        acc += sh_o[k * kWarpFloats + r * D + d] * f;
+        const float4 x = *reinterpret_cast<const float4*>(sh_o + k * kWarpFloats + r * D + d);
+        sum = fmaf(sh_l[k][r], f, sum);
+        v[0] = fmaf(x.x, f, v[0]);
+        v[1] = fmaf(x.y, f, v[1]);
+        v[2] = fmaf(x.z, f, v[2]);
+        v[3] = fmaf(x.w, f, v[3]);
       }
       const int row = rt * R + r, j = div_group(p, row);
-      if (sh_nan[d] < (p.causal ? s.len - s.rows + j + 1 : s.len)) acc = __int_as_float(0x7fc00000);
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (sh_nan[d + q] < (p.causal ? s.len - s.rows + j + 1 : s.len)) v[q] = __int_as_float(0x7fc00000);
       if (whole) {
         const int64_t to = (s.row0 + j) * p.H + h * p.G + row - j * p.G;
-        p.out[to * D + d] = out_bits(sum == 0.f ? 0.f : acc / sum, p.bf16);
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        uint16_t o[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) o[q] = out_bits(sum == 0.f ? 0.f : v[q] * inv, p.bf16);
+        *reinterpret_cast<uint2*>(p.out + to * D + d) = make_uint2(o[0] | ((uint32_t)o[1] << 16), o[2] | ((uint32_t)o[3] << 16));
         if (d == 0 && p.lse) p.lse[to] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.69314718056f;
       } else {
-        po[r * D + d] = acc;
+        *reinterpret_cast<float4*>(po + r * D + d) = make_float4(v[0], v[1], v[2], v[3]);
         if (d == 0) pml[r] = make_float2(mx, sum);
       }
     }
     if (!whole) {
       __threadfence();
       __syncthreads();
-      const int2 who = item_ctas<kOver>(w, x0);
+      const int2 who = item_stretches<kOver>(line, x0);
       const int first = who.x, last = who.y;
       if (threadIdx.x == 0) sh_last = atomicAdd(&p.counters[first], 1) == last - first;
       __syncthreads();
       if (sh_last) {
         __threadfence();
         if (threadIdx.x == 0) p.counters[first] = 0;
-        for (int e = threadIdx.x; e < live * D; e += kThreads) {
-          const int r = e / D, d = e % D;
-          float mx = -INFINITY, sum = 0.f, acc = 0.f;
-          for (int c = first; c <= last; ++c) {
-            const int64_t at = ((int64_t)c * 2 + (c == first ? 1 : 0)) * kAttendRows + r;
-            const float2 ml = __ldcg(&p.part_ml[at]);
-            const float x = __ldcg(&p.part_o[at * D + d]);
-            const float mn = fmaxf(mx, ml.x), ref = mn == -INFINITY ? 0.f : mn;
-            const float f0 = fast_exp2(mx - ref), f1 = fast_exp2(ml.x - ref);
-            sum = sum * f0 + ml.y * f1;
-            acc = acc * f0 + x * f1;
-            mx = mn;
+        // Weights of the parts (a warp a row, a lane a part), then the sums, all of a
+        // block's parts in flight; the partial sums of this CTA's warps are done with.
+        constexpr int kBlock = 256;
+        float* wt = sh_o;  // [R][kBlock]
+        for (int c0 = first; c0 <= last; c0 += kBlock) {
+          const int n = min(last - c0 + 1, kBlock);
+          for (int r = warp; r < live; r += kWarps) {
+            auto ml = [&](int c) { return __ldcg(&p.part_ml[((int64_t)c * 2 + (c == first ? 1 : 0)) * kAttendRows + r]); };
+            float mx = -INFINITY, sum = 0.f;
+            for (int c = first + lane; c <= last; c += 32) mx = fmaxf(mx, ml(c).x);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            const float ref = mx == -INFINITY ? 0.f : mx;
+            for (int c = first + lane; c <= last; c += 32) {
+              const float2 x = ml(c);
+              const float f = fast_exp2(x.x - ref);
+              sum += x.y * f;
+              if (c >= c0 && c < c0 + n) wt[r * kBlock + c - c0] = f;
+            }
+            sum = warp_sum(sum);
+            if (lane == 0) {
+              sh_m[0][r] = mx;
+              sh_l[0][r] = sum;
+            }
           }
-          const int row = rt * R + r, j = div_group(p, row);
-          const int64_t to = (s.row0 + j) * p.H + h * p.G + row - j * p.G;
-          p.out[to * D + d] = out_bits(sum == 0.f ? 0.f : acc / sum, p.bf16);
-          if (d == 0 && p.lse) p.lse[to] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.69314718056f;
+          __syncthreads();
+          for (int e = threadIdx.x; e < live * D / 4; e += kThreads) {
+            const int r = e / (D / 4), d = e % (D / 4) * 4;
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+            float4* keep = reinterpret_cast<float4*>(p.part_o + (((int64_t)first * 2 + 1) * kAttendRows + r) * D + d);
+#pragma unroll 4
+            for (int k = 0; k < n; ++k) {
+              const int c = c0 + k;
+              const float4 x = __ldcg(reinterpret_cast<const float4*>(
+                  p.part_o + (((int64_t)c * 2 + (c == first ? 1 : 0)) * kAttendRows + r) * D + d));
+              const float f = wt[r * kBlock + k];
+              acc.x = fmaf(x.x, f, acc.x);
+              acc.y = fmaf(x.y, f, acc.y);
+              acc.z = fmaf(x.z, f, acc.z);
+              acc.w = fmaf(x.w, f, acc.w);
+            }
+            if (c0 > first) {  // the blocks before, kept in the first part's place
+              const float4 x = *keep;
+              acc = make_float4(acc.x + x.x, acc.y + x.y, acc.z + x.z, acc.w + x.w);
+            }
+            if (c0 + n <= last) {
+              *keep = acc;
+            } else {
+              const float sum = sh_l[0][r], mx = sh_m[0][r], inv = sum == 0.f ? 0.f : 1.f / sum;
+              const int row = rt * R + r, j = div_group(p, row);
+              const int64_t to = (s.row0 + j) * p.H + h * p.G + row - j * p.G;
+              const float v[4] = {acc.x, acc.y, acc.z, acc.w};
+              uint16_t o[4];
+#pragma unroll
+              for (int q = 0; q < 4; ++q) o[q] = out_bits(sum == 0.f ? 0.f : v[q] * inv, p.bf16);
+              *reinterpret_cast<uint2*>(p.out + to * D + d) =
+                  make_uint2(o[0] | ((uint32_t)o[1] << 16), o[2] | ((uint32_t)o[3] << 16));
+              if (d == 0 && p.lse) p.lse[to] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.69314718056f;
+            }
+          }
+          __syncthreads();
         }
       }
     }
+    if (TMA) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the next copies come by another proxy
     __syncthreads();  // the shared results are free again
     for (int d = threadIdx.x; d < D; d += kThreads) sh_nan[d] = 0x7fffffff;
   } while (walk_next<R, kTile, kOver>(p, w, x0));
+  __syncthreads();
+  c = sh_next;
+  }
+  // the last CTA to leave puts the tickets back
+  if (threadIdx.x == 0 && line.total > line.first && atomicAdd(p.tickets + 1, 1) == (int)gridDim.x - 1) {
+    p.tickets[0] = 0;
+    p.tickets[1] = 0;
+  }
 }
 
-template <int D, int NQ>
-int launch_rows(const AttendParams& p, cudaStream_t st) {
-  constexpr int smem = kWarps * 128 * D;  // two slots of 32 keys and values a warp
+template <int D, int NQ, bool TMA>
+int launch(const AttendParams& p, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t st) {
+  constexpr int smem = kWarps * 4 * kTile * D + 1024;
   static std::atomic<uint64_t> ready{0};  // devices whose shared memory limit is raised
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return OCCAM_ERR_CUDA;
   if (!((ready.load(std::memory_order_acquire) >> dev) & 1)) {
-    if (cudaFuncSetAttribute(attend_rows_kernel<D, NQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+    if (cudaFuncSetAttribute(attend_rows_kernel<D, NQ, TMA>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
       return OCCAM_ERR_CUDA;
     ready.fetch_or(uint64_t(1) << dev, std::memory_order_release);
   }
   const int grid = std::min(cache_sms() * (NQ == 1 ? 3 : 2), kAttendCtas);
-  attend_rows_kernel<D, NQ><<<grid, kThreads, smem, st>>>(p);
+  attend_rows_kernel<D, NQ, TMA><<<grid, kThreads, smem, st>>>(p, mk, mv);
   count_launch();
   return cudaGetLastError() == cudaSuccess ? OCCAM_OK : OCCAM_ERR_CUDA;
+}
+
+// Codes as rows of D bytes; boxes of up to 32 rows of one page.
+bool encode_codes(CUtensorMap* m, const void* base, int64_t rows, int dim, int box_rows) {
+  static PFN_cuTensorMapEncodeTiled_v12000 enc = nullptr;
+  static std::once_flag once;
+  std::call_once(once, [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      enc = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
+  });
+  if (!enc) return false;
+  cuuint64_t gdim[2] = {(cuuint64_t)dim, (cuuint64_t)rows};
+  cuuint64_t gstride[1] = {(cuuint64_t)dim};
+  cuuint32_t box[2] = {(cuuint32_t)dim, (cuuint32_t)box_rows};
+  cuuint32_t es[2] = {1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), gdim, gstride, box, es,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, int NQ>
+int launch_rows(const AttendParams& p, cudaStream_t st) {
+  CUtensorMap mk{}, mv{};
+  // Tensor copies where every row of a tile is wanted; with keep flags, rows
+  // one by one (a hidden row is not read), and so too where a row's number would
+  // pass the 31 bits of a copy's coordinate.
+  const int64_t rows = (int64_t)p.c.layers * p.c.pages * p.c.heads * p.c.T;
+  if (p.keep || rows > 0x7fffffff) return launch<D, NQ, false>(p, mk, mv, st);
+  const int box = std::min(p.c.T, kTile);
+  if (!encode_codes(&mk, p.c.k, rows, D, box) || !encode_codes(&mv, p.c.v, rows, D, box)) return OCCAM_ERR_CUDA;
+  return launch<D, NQ, true>(p, mk, mv, st);
 }
 
 }  // namespace
@@ -606,6 +752,7 @@ extern "C" int occam_cache_attend(const occam_cache* cache, const occam_attend_a
   const double scale = a->scale > 0.f ? (double)a->scale : 1.0 / std::sqrt((double)cache->dim);
   p.scale_log2 = (float)(scale * 1.4426950408889634);
   p.counters = ws_at<int32_t>(workspace, w.counters);
+  p.tickets = p.counters + kAttendCtas;
   p.part_o = ws_at<float>(workspace, w.part_o);
   p.part_ml = ws_at<float2>(workspace, w.part_ml);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);

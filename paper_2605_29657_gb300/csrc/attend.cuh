@@ -30,7 +30,8 @@ struct AttendParams {
   const int64_t* keep_off;
   float scale_log2;
   uint32_t g_mul, g_shift;  // x / G = x g_mul >> g_shift for 0 <= x < 2^31
-  int32_t* counters;
+  int32_t* counters;  // per stretch: arrivals at an item that begins in it
+  int32_t* tickets;   // stretches taken beyond the first ones, CTAs that are done
   float* part_o;
   float2* part_ml;
 };
@@ -105,30 +106,46 @@ __device__ __forceinline__ int64_t head_units(const AttendParams& p, const SeqIn
   return (nrt > 1 ? units_before<R, KT, OVER>(p, s, nrt - 1) : 0) + OVER + key_tiles<R, KT>(p, s, nrt - 1);
 }
 
-// The stretch [u0, u1) of the CTA and the item its first unit is in.
-struct Stretch {
-  int64_t units, u0, u1;
-  int ctas, seq, head, row_tile, in_item;  // in_item: u0's place in the item
+// The cuts: stretch c < first begins at c head / first, the others share the rest.
+struct Line {
+  int64_t units, head;
+  int first, total;  // stretches
 };
-
-__device__ __forceinline__ int64_t cta_begin(int64_t units, int ctas, int c) { return units * c / ctas; }
-static __device__ __noinline__ int cta_of(int64_t units, int ctas, int64_t u) {
-  int c = (int)(u * ctas / units);
-  while (c + 1 < ctas && cta_begin(units, ctas, c + 1) <= u) ++c;
-  while (c > 0 && cta_begin(units, ctas, c) > u) --c;
+__device__ __forceinline__ int64_t stretch_begin(const Line& l, int c) {
+  return c <= l.first ? l.head * c / l.first : l.head + (l.units - l.head) * (c - l.first) / (l.total - l.first);
+}
+static __device__ __noinline__ int stretch_of(Line l, int64_t u) {
+  int c = u < l.head ? (int)(u * l.first / l.head) : l.first + (int)((u - l.head) * (l.total - l.first) / (l.units - l.head));
+  while (c + 1 < l.total && stretch_begin(l, c + 1) <= u) ++c;
+  while (c > 0 && stretch_begin(l, c) > u) --c;
   return c;
 }
 
-// Block-wide (NT threads, all of them); sh: NT / 32 + 4 int64 of shared memory. False: no work for this CTA.
+// A stretch [u0, u1) and the item its first unit is in (in_item: u0's place in it).
+struct Stretch {
+  int64_t u0, u1;
+  int index, seq, head, row_tile, in_item;
+};
+
+// The line's length and this thread's part of it (its sequences i0 .. i1-1 begin at `at`).
+struct LinePart {
+  int64_t at, mine;
+  int i0, i1;
+};
+// Block-wide (NT threads, all of them); sh: NT / 32 + 4 int64 of shared memory.
+// min_units: a stretch is no shorter; shared: sixteenths of the line left to the short stretches.
 template <int R, int KT, int OVER, int NT>
-__device__ __forceinline__ bool attend_stretch(const AttendParams& p, int min_units, int64_t* sh, Stretch& w) {
+__device__ __forceinline__ LinePart attend_line(const AttendParams& p, int min_units, int most_stretches, int shared, int64_t* sh,
+                                                Line& l) {
   constexpr int NWARP = NT / 32;
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   const int per = (p.n + NT - 1) / NT;
-  const int i0 = min(t * per, p.n), i1 = min(i0 + per, p.n);
-  int64_t mine = 0;
-  for (int i = i0; i < i1; ++i) mine += p.c.heads * head_units<R, KT, OVER>(p, attend_seq(p, i));
-  int64_t incl = mine;
+  LinePart w;
+  w.i0 = min(t * per, p.n);
+  w.i1 = min(w.i0 + per, p.n);
+  w.mine = 0;
+  for (int i = w.i0; i < w.i1; ++i) w.mine += p.c.heads * head_units<R, KT, OVER>(p, attend_seq(p, i));
+  int64_t incl = w.mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int64_t x = __shfl_up_sync(0xffffffffu, incl, o);
@@ -142,15 +159,26 @@ __device__ __forceinline__ bool attend_stretch(const AttendParams& p, int min_un
     if (k < warp) before += sh[k];
     total += sh[k];
   }
-  w.units = total;
-  const int64_t most = (total + min_units - 1) / min_units;
-  w.ctas = (int)min((int64_t)gridDim.x, most > 0 ? most : 1);
-  if (total == 0 || (int)blockIdx.x >= w.ctas) return false;
-  w.u0 = cta_begin(total, w.ctas, blockIdx.x);
-  w.u1 = cta_begin(total, w.ctas, blockIdx.x + 1);
-  int64_t at = before + incl - mine;
-  if (w.u0 >= at && w.u0 < at + mine) {
-    for (int i = i0; i < i1; ++i) {
+  w.at = before + incl - w.mine;
+  l.units = total;
+  const int64_t most = total / min_units;
+  l.first = (int)min((int64_t)gridDim.x, most > 0 ? most : 1);
+  l.total = (int)min(min((int64_t)most_stretches, (int64_t)3 * l.first), most > 0 ? most : 1);
+  // a few stretches in all: none are held back
+  if (l.total < 2 * l.first || shared == 0) l.total = l.first;
+  l.head = l.total > l.first ? total - total * shared / 16 : total;
+  return w;
+}
+// Stretch c, to all threads of the block.
+template <int R, int KT, int OVER, int NT>
+__device__ __forceinline__ void attend_find(const AttendParams& p, const Line& l, const LinePart& part, int c, int64_t* sh, Stretch& w) {
+  constexpr int NWARP = NT / 32;
+  w.index = c;
+  w.u0 = stretch_begin(l, c);
+  w.u1 = stretch_begin(l, c + 1);
+  int64_t at = part.at;
+  if (w.u0 >= at && w.u0 < at + part.mine) {
+    for (int i = part.i0; i < part.i1; ++i) {
       const SeqInfo s = attend_seq(p, i);
       const int64_t hu = head_units<R, KT, OVER>(p, s);
       if (w.u0 < at + p.c.heads * hu) {
@@ -175,7 +203,6 @@ __device__ __forceinline__ bool attend_stretch(const AttendParams& p, int min_un
   w.head = (int)sh[NWARP + 1];
   w.row_tile = (int)sh[NWARP + 2];
   w.in_item = (int)sh[NWARP + 3];
-  return true;
 }
 
 // The segment (an item's key tiles ta .. tb-1, those in the CTA's stretch) a role is at.
@@ -219,10 +246,10 @@ __device__ __forceinline__ bool walk_begin(const AttendParams& p, const W& w, Wa
   x.item = w.u0 - w.in_item;
   return walk_set<R, KT, OVER>(p, w, x, w.in_item) || walk_next<R, KT, OVER>(p, w, x);
 }
-// The first and the last CTA with tiles of the item.
-template <int OVER, class W>
-__device__ __forceinline__ int2 item_ctas(const W& w, const Walk& x) {
-  return make_int2(cta_of(w.units, w.ctas, x.item + OVER), cta_of(w.units, w.ctas, x.item + OVER + x.tiles - 1));
+// The first and the last stretch with tiles of the item.
+template <int OVER>
+__device__ __forceinline__ int2 item_stretches(const Line& l, const Walk& x) {
+  return make_int2(stretch_of(l, x.item + OVER), stretch_of(l, x.item + OVER + x.tiles - 1));
 }
 
 }  // namespace occam

@@ -61,8 +61,9 @@ struct Shared {
       step_free[kRing], meet, drain;
   Step step[kRing];
   int64_t scan[kThreads / 32 + 4];
-  volatile int64_t u0, u1, units;   // the CTA's stretch (see Stretch)
-  volatile int ctas, seq, head, row_tile, in_item;
+  Line line;
+  volatile int64_t u0, u1;   // the CTA's stretch (see Stretch)
+  volatile int seq, head, row_tile, in_item;
   uint32_t tmem;
   int stop;            // a wait ran out
   int last;
@@ -823,50 +824,82 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
     if (!done) {
       __threadfence();
       TC_MEET();
-      const int2 who = item_ctas<kOver>(sh, x);
+      const int2 who = item_stretches<kOver>(sh.line, x);
       const int first = who.x, last = who.y;
       if (threadIdx.x == 0) sh.last = atomicAdd(&p.counters[first], 1) == last - first;
       TC_MEET();
       if (sh.last) {
         __threadfence();
         if (threadIdx.x == 0) p.counters[first] = 0;
-        if (mine && there) {
-          float mx = -INFINITY;
+        if (mine) {
+          // Lane l has row l's maximum, sum and weights; then the warp goes through its
+          // rows, all lanes on one, the parts' loads in flight together. The weights are
+          // in the place of the warp's own queries, 32 parts at a time.
+          auto part = [&](int c, int rr) { return ((int64_t)c * 2 + (c == first ? 1 : 0)) * kR + t * 128 + (r & ~31) + rr; };
+          float* wt = reinterpret_cast<float*>(q_smem + t * kK * D * 2 + (r & ~31) * 128);  // [32 parts][32 rows]
+          const int rows = min(x.s.rows * p.G - (x.rt * kR + (row & ~31)), 32);
+          float mx = -INFINITY, sum = 0.f;
+          if (there) {
 #pragma unroll 1
-          for (int c = first; c <= last; ++c)
-            mx = fmaxf(mx, __ldcg(&p.part_ml[((int64_t)c * 2 + (c == first ? 1 : 0)) * kR + row]).x);
+            for (int c = first; c <= last; ++c) mx = fmaxf(mx, __ldcg(&p.part_ml[part(c, lane)]).x);
+          }
           const float base = mx == -INFINITY ? 0.f : mx;
-          float sum = 0.f;
+          if (there) {
 #pragma unroll 1
-          for (int c = first; c <= last; ++c) {
-            const float2 ml = __ldcg(&p.part_ml[((int64_t)c * 2 + (c == first ? 1 : 0)) * kR + row]);
-            sum += ml.y * fast_exp2(ml.x - base);
+            for (int c = first; c <= last; ++c) {
+              const float2 ml = __ldcg(&p.part_ml[part(c, lane)]);
+              sum += ml.y * fast_exp2(ml.x - base);
+            }
+            if (p.lse) p.lse[to] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.69314718056f;
           }
           const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll 1
-          for (int k = 0; k < D; k += 16) {
-            float acc[16];
-#pragma unroll
-            for (int q = 0; q < 16; ++q) acc[q] = 0.f;
+          for (int c0 = first; c0 <= last; c0 += 32) {
+            const int n = min(last - c0 + 1, 32);
+            __syncwarp();
 #pragma unroll 1
-            for (int c = first; c <= last; ++c) {
-              const int64_t from = ((int64_t)c * 2 + (c == first ? 1 : 0)) * kR + row;
-              const float g = fast_exp2(__ldcg(&p.part_ml[from]).x - base);
-              const float4* po = reinterpret_cast<const float4*>(p.part_o + from * D + k);
+            for (int k = 0; k < n; ++k)
+              wt[k * 32 + lane] = there ? fast_exp2(__ldcg(&p.part_ml[part(c0 + k, lane)]).x - base) * inv : 0.f;
+            __syncwarp();
+#pragma unroll 2
+            for (int rr = 0; rr < rows; ++rr) {
+              constexpr int V = D / 32;  // values a lane holds of a row
+              float acc[V];
 #pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                const float4 v = __ldcg(po + q);
-                acc[4 * q] = fmaf(v.x, g, acc[4 * q]);
-                acc[4 * q + 1] = fmaf(v.y, g, acc[4 * q + 1]);
-                acc[4 * q + 2] = fmaf(v.z, g, acc[4 * q + 2]);
-                acc[4 * q + 3] = fmaf(v.w, g, acc[4 * q + 3]);
+              for (int q = 0; q < V; ++q) acc[q] = 0.f;
+              float* keep = p.part_o + part(first, rr) * D + lane * V;
+#pragma unroll 2
+              for (int k = 0; k < n; ++k) {
+                const float w = wt[k * 32 + rr];
+                const float* from = p.part_o + part(c0 + k, rr) * D + lane * V;
+                float v[V];
+                if constexpr (V == 4) {
+                  const float4 y = __ldcg(reinterpret_cast<const float4*>(from));
+                  v[0] = y.x, v[1] = y.y, v[2] = y.z, v[3] = y.w;
+                } else {
+                  const float2 y = __ldcg(reinterpret_cast<const float2*>(from));
+                  v[0] = y.x, v[1] = y.y;
+                }
+#pragma unroll
+                for (int q = 0; q < V; ++q) acc[q] = fmaf(v[q], w, acc[q]);
+              }
+              if (c0 > first) {  // the blocks before, kept in the first part's place
+#pragma unroll
+                for (int q = 0; q < V; ++q) acc[q] += keep[q];
+              }
+              if (c0 + n <= last) {
+#pragma unroll
+                for (int q = 0; q < V; ++q) keep[q] = acc[q];
+              } else {
+                const float total = __shfl_sync(0xffffffffu, sum, rr);
+                const int64_t row_to = __shfl_sync(0xffffffffu, to, rr);
+                uint32_t* out = reinterpret_cast<uint32_t*>(p.out + row_to * D + lane * V);
+#pragma unroll
+                for (int q = 0; q < V; q += 2)
+                  out[q / 2] = total == 0.f ? 0u : out_pair<BF16>(acc[q], acc[q + 1]);
               }
             }
-#pragma unroll
-            for (int q = 0; q < 16; ++q) acc[q] = sum == 0.f ? 0.f : acc[q] * inv;
-            write16<BF16>(p.out + to * D + k, acc);
           }
-          if (p.lse) p.lse[to] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.69314718056f;
         }
       }
     }
@@ -889,8 +922,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(AttendParams p) 
   __shared__ Shared sh;
   unsigned char* smem = dyn + ((1024 - (tc::su32(dyn) & 1023)) & 1023);  // (an offset: the pointer stays one to shared memory)
   const int warp = threadIdx.x >> 5;
+  Line line;
+  const LinePart part = attend_line<kR, kK, kOver, kThreads>(p, kOver + 1, kAttendTcCtas, 0, sh.scan, line);
+  if (line.units == 0 || (int)blockIdx.x >= line.first) return;
   Stretch w;
-  if (!attend_stretch<kR, kK, kOver, kThreads>(p, kOver + 1, sh.scan, w)) return;
+  attend_find<kR, kK, kOver, kThreads>(p, line, part, blockIdx.x, sh.scan, w);
   {
     Walk x;
     if (!walk_begin<kR, kK, kOver>(p, w, x)) return;  // no tile in the stretch: every role has at least one from here on
@@ -898,8 +934,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(AttendParams p) 
   if (threadIdx.x == 0) {
     sh.u0 = w.u0;
     sh.u1 = w.u1;
-    sh.units = w.units;
-    sh.ctas = w.ctas;
+    sh.line = line;
     sh.seq = w.seq;
     sh.head = w.head;
     sh.row_tile = w.row_tile;

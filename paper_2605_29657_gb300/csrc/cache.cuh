@@ -9,9 +9,9 @@
 
 namespace occam {
 
-// Attention workspace: at most kAttendCtas CTAs leave two partial results of
+// Attention workspace: at most kAttendCtas stretches of work leave two partial results of
 // up to kAttendRows rows each (the tensor-core kernel: kAttendTcCtas, 256 rows).
-constexpr int kAttendCtas = 1024;
+constexpr int kAttendCtas = 2048;
 constexpr int kAttendRows = 16;
 constexpr int kAttendTcCtas = 160;
 constexpr size_t kAttendPartRows =
@@ -37,7 +37,7 @@ inline CacheWs cache_ws(const occam_cache* c, int64_t max_tokens) {
     return o;
   };
   w.status = take(8);
-  w.counters = take((size_t)kAttendCtas * 4);
+  w.counters = take((size_t)(kAttendCtas + 2) * 4);
   w.marks = take((size_t)c->max_seqs * 4);
   w.count = take((size_t)c->max_seqs * 4);
   w.lead = take((size_t)c->max_seqs * 4);
