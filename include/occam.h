@@ -462,7 +462,7 @@ int occam_rope(int32_t dtype, int64_t rows, int32_t dim, int32_t rot, int32_t pa
  * changes nothing. */
 typedef struct occam_cache {
   int32_t layers;
-  int32_t pages;       /* pages of the pool (each in all layers), at most 2^24 */
+  int32_t pages;       /* pages of the pool (each in all layers), at most 2^24; layers * pages < 2^31 */
   int32_t heads;       /* key / value heads */
   int32_t dim;         /* 64 or 128 */
   int32_t page_tokens; /* 16, 32, 64 or 128 */

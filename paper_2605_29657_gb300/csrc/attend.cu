@@ -84,11 +84,11 @@ __device__ __forceinline__ int value_place(int row, int g) {
 __device__ __forceinline__ void copy_async16(uint32_t dst, const uint8_t* src, uint32_t there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
-// a box of rows from row `row` on
-__device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, int row, uint64_t* bar) {
+// a box of rows of page `page` (of all layers) from row `row` (of all heads) on
+__device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, int row, int page, uint64_t* bar) {
   asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-      "l"(map), "r"(0), "r"(row), "r"(smem_u32(bar))
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(map), "r"(0), "r"(row), "r"(page), "r"(smem_u32(bar))
       : "memory");
 }
 template <int WORDS>
@@ -224,15 +224,14 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
         if (lane == 0) {
           if (p.c.T >= kTile) {
             mbar_arrive_expect_tx(bar, kTile * D);
-            const int64_t b = (layer_page + x.page[0]) * p.c.heads + h;
-            tma_rows(dst, &map, (int)((b << p.c.log2T) + ((tile * kTile) & tmask)), bar);
+            tma_rows(dst, &map, h * p.c.T + ((tile * kTile) & tmask), (int)layer_page + x.page[0], bar);
           } else {
             const bool both = (x.seen >> 16) != 0;  // else the second page may not be there
             mbar_arrive_expect_tx(bar, both ? kTile * D : 16 * D);
 #pragma unroll
             for (int k = 0; k < 2; ++k)
               if (k == 0 || both)
-                tma_rows(dst + k * 16 * D, &map, (int)(((layer_page + x.page[k]) * p.c.heads + h) << p.c.log2T), bar);
+                tma_rows(dst + k * 16 * D, &map, h * p.c.T, (int)layer_page + x.page[k], bar);
           }
         }
       } else {
@@ -662,8 +661,20 @@ int launch(const AttendParams& p, const CUtensorMap& mk, const CUtensorMap& mv, 
   return cudaGetLastError() == cudaSuccess ? OCCAM_OK : OCCAM_ERR_CUDA;
 }
 
-// Codes as rows of D bytes; boxes of up to 32 rows of one page.
-bool encode_codes(CUtensorMap* m, const void* base, int64_t rows, int dim, int box_rows) {
+template <int D, int NQ>
+int launch_rows(const AttendParams& p, cudaStream_t st) {
+  CUtensorMap mk{}, mv{};
+  // Tensor copies where every row of a tile is wanted; with keep flags, rows
+  // one by one (a hidden row is not read).
+  if (p.keep) return launch<D, NQ, false>(p, mk, mv, st);
+  const int box = std::min(p.c.T, kTile);
+  if (!encode_blocks(&mk, p.c, p.c.k, D, box, true) || !encode_blocks(&mv, p.c, p.c.v, D, box, true)) return OCCAM_ERR_CUDA;
+  return launch<D, NQ, true>(p, mk, mv, st);
+}
+
+}  // namespace
+
+bool occam::encode_blocks(CUtensorMap* m, const CacheDev& c, const void* codes, int dim, int box_rows, bool swizzle) {
   static PFN_cuTensorMapEncodeTiled_v12000 enc = nullptr;
   static std::once_flag once;
   std::call_once(once, [] {
@@ -674,29 +685,17 @@ bool encode_codes(CUtensorMap* m, const void* base, int64_t rows, int dim, int b
       enc = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
   });
   if (!enc) return false;
-  cuuint64_t gdim[2] = {(cuuint64_t)dim, (cuuint64_t)rows};
-  cuuint64_t gstride[1] = {(cuuint64_t)dim};
-  cuuint32_t box[2] = {(cuuint32_t)dim, (cuuint32_t)box_rows};
-  cuuint32_t es[2] = {1, 1};
-  return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), gdim, gstride, box, es,
-             CU_TENSOR_MAP_INTERLEAVE_NONE, dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
-             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const cuuint64_t rows = (cuuint64_t)c.heads * c.T;
+  cuuint64_t gdim[3] = {(cuuint64_t)dim, rows, (cuuint64_t)c.layers * c.pages};
+  cuuint64_t gstride[2] = {(cuuint64_t)dim, rows * dim};
+  cuuint32_t box[3] = {(cuuint32_t)dim, (cuuint32_t)box_rows, 1};
+  cuuint32_t es[3] = {1, 1, 1};
+  const CUtensorMapSwizzle sw =
+      !swizzle ? CU_TENSOR_MAP_SWIZZLE_NONE : dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(codes), gdim, gstride, box, es,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, sw, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-
-template <int D, int NQ>
-int launch_rows(const AttendParams& p, cudaStream_t st) {
-  CUtensorMap mk{}, mv{};
-  // Tensor copies where every row of a tile is wanted; with keep flags, rows
-  // one by one (a hidden row is not read), and so too where a row's number would
-  // pass the 31 bits of a copy's coordinate.
-  const int64_t rows = (int64_t)p.c.layers * p.c.pages * p.c.heads * p.c.T;
-  if (p.keep || rows > 0x7fffffff) return launch<D, NQ, false>(p, mk, mv, st);
-  const int box = std::min(p.c.T, kTile);
-  if (!encode_codes(&mk, p.c.k, rows, D, box) || !encode_codes(&mv, p.c.v, rows, D, box)) return OCCAM_ERR_CUDA;
-  return launch<D, NQ, true>(p, mk, mv, st);
-}
-
-}  // namespace
 
 #define OCCAM_TRY(x)                 \
   do {                               \

@@ -4,21 +4,21 @@
 // The same running softmax as attend.cu, for 256 query rows (token, head of
 // the group) against tiles of 128 keys. Bound by the tensor cores and the
 // exponentials: 4 D operations and one exponential a (row, key).
-// One CTA an SM, 16 warps in four roles:
-//  - warps 8-11 fetch the codes of a key tile, a page's rows at a time, and
-//    write them to shared memory as f16 (exact) in the matrix layout (128-byte
-//    swizzle), two stages deep, the next tile's loads in flight meanwhile;
-//  - one thread of warp 12 issues the products: S = Q K^T into tensor memory,
-//    O += P V with P read from tensor memory, for two row tiles of 128 in turn,
-//    so that one tile's softmax runs under the other's products;
+// One CTA an SM, 16 warps in five roles:
+//  - warp 13 plans: it walks the key tiles, fills a ring of step records (masks,
+//    scales, references) and has each page's block copied to shared memory as it is;
+//    tiles without a seen key are left out, and a tile whose scales of v lie
+//    more than 2^6 apart is taken 16 keys at a time;
+//  - warps 8-11 turn the codes into f16 (exact) in the matrix layout
+//    (128-byte swizzle), two stages deep;
+//  - warp 12 issues the products: S = Q K^T into tensor memory, O += P V with P
+//    read from tensor memory, for two row tiles of 128 in turn, so that one
+//    tile's softmax runs under the other's products;
 //  - warps 0-3 and 4-7 hold a row a thread: scores from tensor memory, maximum,
 //    exponentials, P back over the scores as f16.
 // O stays in tensor memory. It is rescaled only where a row's maximum grew by more than
 // 2^8 since its last reference, or where v's scale left the window that P
 // is held in; both references are undone at the end.
-// Which tile comes next is decided by the fetching warps (tiles without a seen key are left out; a tile whose
-// scales of v lie more than 2^6 apart is taken 16 keys at a time), told to the others through
-// a ring of step records.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -37,7 +37,7 @@ constexpr int kOver = 4;       // beginning and ending an item takes as long as 
 constexpr int kGroup = 16;     // keys that share a page at least
 constexpr int kThreads = 512;
 constexpr int kRing = 4;
-constexpr int kRegSoftmax = 136, kRegFetch = 160, kRegIssue = 80;  // 2 x 136 + 160 + 80 = 4 x 128
+constexpr int kRegSoftmax = 184, kRegConvert = 72, kRegIssue = 72;  // 2 x 184 + 72 + 72 = 4 x 128
 constexpr uint64_t kWaitNs = 2000000000ull;
 constexpr float kLazy = 8.f;             // log2 growth of a maximum before O is rescaled
 constexpr float kLeast = 1.2e-38f;       // a score's factor: never 0, so that a hidden key's -inf stays
@@ -46,6 +46,8 @@ constexpr float kRhoSpan = 8.6736174e-19f;  // 2^-60
 
 struct Step {
   int tile;
+  int open;           // every row of the item sees the whole tile
+  uint32_t zero;      // bit g: v's scale is 0 in group g
   int end;            // 1: no more steps of this segment (an item, or the CTA's part of one); 2: nor segments
   int row_tiles;      // 1 or 2
   uint32_t seen[4];   // bit k: key k of the tile may be seen
@@ -58,9 +60,8 @@ struct Step {
 
 struct Shared {
   uint64_t q_full, k_full[2], k_free[2], v_full[2], v_free[2], s_full[2], p_full[2], o_done[2], step_full[kRing],
-      step_free[kRing], meet, drain;
+      step_free[kRing], raw_full[2], raw_free[2], meet, drain;
   Step step[kRing];
-  int64_t scan[kThreads / 32 + 4];
   Line line;
   volatile int64_t u0, u1;   // the CTA's stretch (see Stretch)
   volatile int seq, head, row_tile, in_item;
@@ -68,8 +69,10 @@ struct Shared {
   int stop;            // a wait ran out
   int last;
   int any_nan[4];
-  int nan_first[4][128];
+  alignas(16) int nan_first[4][128];  // (first the scratch of attend_line: 8-byte words)
 };
+constexpr int kSharedBytes = 3072;
+static_assert(sizeof(Shared) <= kSharedBytes, "7 tiles of 32 KB and this are all of an SM's shared memory");
 
 __device__ __forceinline__ uint64_t desc_kmajor(uint32_t saddr) { return tc::sdesc_sw128(saddr); }
 // rows of the summed index, 64 columns (128 bytes) a block, blocks 16 KB apart
@@ -139,6 +142,16 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
       : "r"(taddr)
       : "memory");
 }
+// 128 columns of this thread's lane; they are there on return
+__device__ __forceinline__ void tmem_ld128(uint32_t taddr, uint32_t (&v)[128]) {
+  uint32_t(&a)[64] = *reinterpret_cast<uint32_t(*)[64]>(v);
+  uint32_t(&b)[64] = *reinterpret_cast<uint32_t(*)[64]>(v + 64);
+  tc::tmem_ld64(taddr, a);
+  tc::tmem_ld64(taddr + 64, b);
+  tc::tmem_wait_ld();
+  asm volatile("" : OCCAM_TC_RW64(a));
+  asm volatile("" : OCCAM_TC_RW64(b));
+}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
@@ -151,60 +164,28 @@ __device__ __forceinline__ int row_tiles(const AttendParams& p, const Walk& x) {
   return x.s.rows * p.G - x.rt * kR > 128 ? 2 : 1;
 }
 
-// ---------------------------------------------------------------- fetching warps
-// 16 bytes, or zeros if !there
-__device__ __forceinline__ uint4 load_if(const uint8_t* p, uint32_t there) {
-  uint4 r;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.u32 p, %5, 0;\n\t"
-      "mov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
-      "@p ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
-      : "=&r"(r.x), "=&r"(r.y), "=&r"(r.z), "=&r"(r.w)
-      : "l"(p), "r"(there));
-  return r;
-}
-
+// ---------------------------------------------------------------- planning
 __device__ __forceinline__ uint32_t pick(const uint32_t (&v)[4], int k) {
   const uint32_t lo = k & 1 ? v[1] : v[0], hi = k & 1 ? v[3] : v[2];
   return k & 2 ? hi : lo;
 }
 
-// What a warp knows of a key tile; lane l holds the place and scales of group l & 7 (16 keys).
+// What the planning warp knows of a key tile; lane l holds the page and scales of group l & 7 (16 keys).
 struct Tile {
-  int tile;
-  int64_t at;   // the group's first code in its page (while the tile is only looked at: the page)
+  int tile, page;
   float ks, vs;
   uint32_t seen[4];
 };
 
-// A pass of the four warps takes RPP key rows, LPR lanes a row, 16 codes a lane. Row 16 q + r
-// of every pass has the same r & 7, so a lane's swizzled places are the same in each.
-template <int D>
-struct Fetch {
-  static constexpr int LPR = D / 16;
-  static constexpr int RPP = 128 / LPR;     // 16 (D = 128) or 32 rows
-  static constexpr int PASSES = 128 / RPP;
-
+struct Plan {
   const AttendParams& p;
   const Walk& x;
-  const int lane, row0, c;  // row of pass 0, piece of the row
-  int place0, place1;       // this lane's two 16-byte pieces in a matrix, pass 0
-  uint32_t swap;            // all ones: the odd piece is written first
+  const int lane;
   const int32_t* table;
   const uint8_t* flags;
   int n_flags;
 
-  __device__ Fetch(const AttendParams& p_, const Walk& x_, int lane_, int warp)
-      : p(p_), x(x_), lane(lane_), row0(warp * (32 / LPR) + lane_ / LPR), c(lane_ % LPR) {
-    // [D / 64][128 keys][64 dims], 128-byte swizzle. The two halves of a row start at the same
-    // bank: their lanes write their even and odd pieces in opposite order.
-    const int odd = c >> 2;
-    swap = 0u - (uint32_t)odd;
-    const int base = odd * 16384 + row0 * 128, idx = 2 * (c & 3);
-    place0 = base + (((idx + odd) ^ (row0 & 7)) << 4);
-    place1 = base + (((idx + 1 - odd) ^ (row0 & 7)) << 4);
-  }
+  __device__ Plan(const AttendParams& p_, const Walk& x_, int lane_) : p(p_), x(x_), lane(lane_) {}
 
   __device__ __forceinline__ void item() {
     table = p.c.table + (int64_t)x.s.seq * p.c.max_pages;
@@ -224,9 +205,8 @@ struct Fetch {
   __device__ __forceinline__ void look(Tile& t, int tile) const {
     t.tile = tile;
     const int first = tile * kK + (lane & 7) * kGroup;
-    int page = 0;
-    if (first < x.s.len) page = table[first >> p.c.log2T];
-    t.at = page;
+    t.page = 0;
+    if (first < x.s.len) t.page = table[first >> p.c.log2T];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const int key = tile * kK + 32 * k + lane;
@@ -235,36 +215,77 @@ struct Fetch {
       t.seen[k] = see;
     }
   }
-  // masks, places, and the scales (loads in flight)
+  // masks, and the scales (loads in flight)
   __device__ __forceinline__ void settle(Tile& t) const {
-    int64_t page = t.at;
-    const bool bad = (uint64_t)page >= (uint64_t)p.c.pages;
+    const bool bad = (unsigned)t.page >= (unsigned)p.c.pages;
     const unsigned wrong = __ballot_sync(0xffffffffu, bad) & 0xff;
 #pragma unroll
     for (int k = 0; k < 4; ++k) t.seen[k] = __ballot_sync(0xffffffffu, t.seen[k] != 0);
     if (wrong) {
       set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
-      if (bad) page = 0;
+      if (bad) t.page = 0;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         if ((wrong >> (2 * k)) & 1) t.seen[k] &= 0xffff0000u;
         if ((wrong >> (2 * k + 1)) & 1) t.seen[k] &= 0x0000ffffu;
       }
     }
-    const int64_t b = ((int64_t)p.layer * p.c.pages + page) * p.c.heads + x.h;
+    const int64_t b = ((int64_t)p.layer * p.c.pages + t.page) * p.c.heads + x.h;
     t.ks = p.c.k_scale[b];
     t.vs = p.c.v_scale[b];
-    t.at = ((b << p.c.log2T) + (((lane & 7) * kGroup) & (p.c.T - 1))) * D;
   }
-  __device__ __forceinline__ void load(uint4 (&r)[PASSES], const uint8_t* codes, const Tile& t) const {
-    const uint8_t* mine = codes + (row0 & 15) * D + c * 16;
+  // whether this lane's group has a seen key
+  __device__ __forceinline__ bool has(const Tile& t) const {
+    return (pick(t.seen, (lane & 7) >> 1) >> (16 * (lane & 1))) & 0xffffu;
+  }
+  // the largest and least (positive) scale of v of groups with a seen key
+  __device__ __forceinline__ void range(const Tile& t, float& hi, float& lo) const {
+    const bool h = has(t);
+    hi = h ? t.vs : 0.f;
+    lo = h && t.vs > 0.f ? t.vs : INFINITY;
 #pragma unroll
-    for (int i = 0; i < PASSES; ++i) {
-      const int64_t at = __shfl_sync(0xffffffffu, t.at, i * (RPP / 16) + (row0 >> 4));
-      r[i] = load_if(mine + at, t.seen[i * RPP / 32] & (1u << (row0 + i * RPP % 32)));
+    for (int o = 1; o < 8; o <<= 1) {
+      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
     }
   }
-  // codes to f16 in the matrix layout
+};
+
+// ---------------------------------------------------------------- conversion
+// A pass of the four warps takes RPP key rows, LPR lanes a row, 16 codes a lane. Row r of every
+// pass has the same r & 7, so a lane's swizzled places are the same in each.
+template <int D>
+struct Convert {
+  static constexpr int LPR = D / 16;
+  static constexpr int RPP = 128 / LPR;  // 16 (D = 128) or 32 rows
+  static constexpr int PASSES = 128 / RPP;
+
+  const int row0, c;   // row of pass 0, piece of the row
+  int place0, place1;  // this lane's two 16-byte pieces in a matrix, pass 0
+  uint32_t swap;       // all ones: the odd piece is written first
+
+  __device__ Convert(int lane, int warp) : row0(warp * (32 / LPR) + lane / LPR), c(lane % LPR) {
+    // [D / 64][128 keys][64 dims], 128-byte swizzle. The two halves of a row start at the same
+    // bank: their lanes write their even and odd pieces in opposite order.
+    const int odd = c >> 2;
+    swap = 0u - (uint32_t)odd;
+    const int base = odd * 16384 + row0 * 128, idx = 2 * (c & 3);
+    place0 = base + (((idx + odd) ^ (row0 & 7)) << 4);
+    place1 = base + (((idx + 1 - odd) ^ (row0 & 7)) << 4);
+  }
+  __device__ __forceinline__ void read(uint4 (&r)[PASSES], const unsigned char* raw) const {
+    const uint4* at = reinterpret_cast<const uint4*>(raw + row0 * D + c * 16);
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) r[i] = at[i * RPP * D / 16];
+  }
+  // hidden rows may be anything: zeros
+  __device__ __forceinline__ void mask(uint4 (&r)[PASSES], const uint32_t* seen) const {
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      const uint32_t m = 0u - ((seen[i * RPP / 32] >> (row0 + i * RPP % 32)) & 1u);
+      r[i] = make_uint4(r[i].x & m, r[i].y & m, r[i].z & m, r[i].w & m);
+    }
+  }
   __device__ __forceinline__ void store(const uint4 (&r)[PASSES], unsigned char* base) const {
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
@@ -275,18 +296,6 @@ struct Fetch {
       *reinterpret_cast<uint4*>(base + place1 + i * (RPP * 128)) =
           make_uint4(e4m3x2_f16x2(w2), e4m3x2_f16x2_hi(w2), e4m3x2_f16x2(w3), e4m3x2_f16x2_hi(w3));
     }
-  }
-  // whether this lane's group has a seen key; the largest and least (positive) scale of v of such groups
-  __device__ __forceinline__ bool range(const Tile& t, float& hi, float& lo) const {
-    const bool has = (pick(t.seen, (lane & 7) >> 1) >> (16 * (lane & 1))) & 0xffffu;
-    hi = has ? t.vs : 0.f;
-    lo = has && t.vs > 0.f ? t.vs : INFINITY;
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) {
-      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    }
-    return has;
   }
   __device__ __forceinline__ bool nans(const uint4 (&r)[PASSES]) const {
     uint32_t hit = 0;
@@ -300,10 +309,10 @@ struct Fetch {
   }
   // The rare cases work on the matrix, on this lane's own pieces, in rolled loops.
   // Values of scale 0 are 0.
-  __device__ __forceinline__ void clear(const Tile& t, unsigned char* base) const {
+  __device__ __forceinline__ void clear(uint32_t zero, unsigned char* base) const {
 #pragma unroll 1
     for (int i = 0; i < PASSES; ++i) {
-      if (__shfl_sync(0xffffffffu, t.vs, i * (RPP / 16) + (row0 >> 4)) == 0.f) {
+      if ((zero >> ((row0 + i * RPP) / kGroup)) & 1) {
         *reinterpret_cast<uint4*>(base + place0 + i * (RPP * 128)) = make_uint4(0, 0, 0, 0);
         *reinterpret_cast<uint4*>(base + place1 + i * (RPP * 128)) = make_uint4(0, 0, 0, 0);
       }
@@ -326,6 +335,15 @@ struct Fetch {
   }
 };
 
+// the block of codes of one page and head
+__device__ __forceinline__ void tma_block(void* dst, const CUtensorMap* map, int row, int page, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+          tc::su32(dst)),
+      "l"(map), "r"(0), "r"(row), "r"(page), "r"(tc::su32(bar))
+      : "memory");
+}
+
 // a bounded wait on a barrier phase; false (recorded) if it ran out or another role gave up
 __device__ __forceinline__ bool wait_long(uint64_t* bar, uint32_t parity, volatile int* stop, int32_t* status) {
   const uint64_t t0 = tc::globaltimer();
@@ -338,9 +356,6 @@ __device__ __forceinline__ bool wait_long(uint64_t* bar, uint32_t parity, volati
   }
   return true;
 }
-// Hides a flag's value from the compiler, so that what follows exists once and
-// not in a copy for each case.
-#define TC_ONCE(flag) asm volatile("" : "+r"(flag))
 #define TC_WAIT(bar, parity)                                                                               \
   if (!tc::bar_try(&(bar), (parity)) && !wait_long(&(bar), (parity), &sh.stop, p.c.status)) return;
 // the 256 softmax threads meet
@@ -352,153 +367,165 @@ __device__ __forceinline__ bool wait_long(uint64_t* bar, uint32_t parity, volati
   } while (0)
 
 template <int D>
-__device__ __forceinline__ void fetch_role(const AttendParams& p, Shared& sh, unsigned char* k_smem,
-                                           unsigned char* v_smem) {
-  constexpr int kBytes = kK * D * 2;
-  const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
+__device__ __forceinline__ void plan_role(const AttendParams& p, Shared& sh, const CUtensorMap& map_k, const CUtensorMap& map_v,
+                                          unsigned char* raw) {
+  const int lane = threadIdx.x & 31;
   Walk x;
   if (!walk_begin<kR, kK, kOver>(p, sh, x)) return;
-  Fetch<D> f(p, x, lane, warp);
-  uint32_t n = 0, j = 0, seg = 0;  // step records, data steps, segments so far
+  Plan f(p, x, lane);
+  uint32_t n = 0, j = 0;  // step records, steps so far
   for (bool again = true; again;) {
     f.item();
     const int common = p.causal ? x.s.len - x.s.rows + div_group(p, x.rt * kR) + 1 : x.s.len;
-    float rho = 0.f, rho_next = 0.f, rho_max = 0.f;
-    int* first = sh.nan_first[seg & 3];
-    int* any = &sh.any_nan[seg & 3];
-    // tiles in the order of their stages: codes (cur), masks and scales (nxt), page and flags (far)
+    const int end = x.tb - 1, tiles2 = row_tiles(p, x);
+    float rho = 0.f, rho_max = 0.f;
+    // tiles in the order of their stages: in hand (cur), masks and scales (nxt), page and flags (far)
     Tile cur, nxt, far;
-    uint4 kr[Fetch<D>::PASSES], vr[Fetch<D>::PASSES];
-    const int end = x.tb - 1;
-    int groups = 0;      // groups of the present tile still to be taken one by one
-    uint32_t whole[4];   // the present tile's mask, while it is taken so
+    int groups = 0;     // groups of the present tile still to be taken one by one
+    uint32_t whole[4];  // the present tile's mask, while it is taken so
     f.look(far, x.ta);
     nxt = far;
     f.settle(nxt);
     cur = nxt;
     cur.tile = x.ta - 1;
     f.look(far, min(x.ta + 1, end));
-    float fall = 1.f;
-    int have = 0, more = 1;
-#pragma unroll 1
-    while (more) {
-      TC_ONCE(have);
-      int st = j & 1;
-      TC_ONCE(st);
-      // the step after cur (tiles without a seen key are passed over)
-      Tile next = cur;
+    for (bool none = true;; none = false) {
+      // the next step (tiles without a seen key are passed over)
       int only = -1;  // the group that is taken alone
       if (groups) {
         only = __ffs(groups) - 1;
         groups &= groups - 1;
       } else {
-        more = 0;
-        while (next.tile < end) {
-          next = nxt;
-          if (next.tile < end) {
+        bool found = false;
+        while (!found && cur.tile < end) {
+          cur = nxt;
+          if (cur.tile < end) {
             nxt = far;
             f.settle(nxt);
             f.look(far, min(nxt.tile + 1, end));
           }
-          if (next.seen[0] | next.seen[1] | next.seen[2] | next.seen[3]) {
-            more = 1;
-            break;
-          }
+          found = (cur.seen[0] | cur.seen[1] | cur.seen[2] | cur.seen[3]) != 0;
         }
-        if (!have) more = 1;  // nothing is seen: one step of hidden keys gives the rows their zeros
+        if (!found && !none) break;  // (where nothing is seen, one step of hidden keys gives the rows their zeros)
       }
-      float fall_next = 1.f;
-      if (more) {
-        float hi, lo;
-        const bool has = f.range(next, hi, lo);
-        if (only < 0 && lo < hi * kRhoKeep) {
-          // scales of v too far apart for one reference: the groups with a seen key one by one
-          const int with = (int)(__ballot_sync(0xffffffffu, has) & 0xff);
-          only = __ffs(with) - 1;
-          groups = with & (with - 1);
+      float hi, lo;
+      f.range(cur, hi, lo);
+      if (only < 0 && lo < hi * kRhoKeep) {
+        // scales of v too far apart for one reference: the groups with a seen key one by one
+        const int with = (int)(__ballot_sync(0xffffffffu, f.has(cur)) & 0xff);
+        only = __ffs(with) - 1;
+        groups = with & (with - 1);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) whole[k] = next.seen[k];
-        }
-        if (only >= 0) {
+        for (int k = 0; k < 4; ++k) whole[k] = cur.seen[k];
+      }
+      if (only >= 0) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) next.seen[k] = (only >> 1) == k ? whole[k] & (0xffffu << (16 * (only & 1))) : 0u;
-          hi = __shfl_sync(0xffffffffu, next.vs, only);
-          lo = hi > 0.f ? hi : INFINITY;
-        }
-        // v's reference of that step, and O's factor
-        if (hi > rho_next || lo < rho_next * kRhoKeep) {
-          const float to = hi > rho_next ? hi : fmaxf(hi, rho_max * kRhoSpan);
-          fall_next = rho_next / to;
-          rho_next = to;
-          rho_max = fmaxf(rho_max, to);
-        }
+        for (int k = 0; k < 4; ++k) cur.seen[k] = (only >> 1) == k ? whole[k] & (0xffffu << (16 * (only & 1))) : 0u;
+        hi = __shfl_sync(0xffffffffu, cur.vs, only);
+        lo = hi > 0.f ? hi : INFINITY;
       }
-      TC_ONCE(have);
-      if (have) {
-        // the step's record
-        TC_WAIT(sh.step_free[n % kRing], ((n / kRing) & 1) ^ 1);
-        if (warp == 0) {
-          Step& s = sh.step[n % kRing];
-          if (lane < 8) {
-            // hidden groups take no part; a scale of 0 makes values of 0 (their codes are cleared below)
-            const uint32_t word = pick(cur.seen, lane >> 1);
-            const bool has = (word >> (16 * (lane & 1))) & 0xffffu, real = has && cur.vs != 0.f;
-            s.ks[lane] = has ? cur.ks : 1.f;
-            s.lr[lane] = real ? (cur.vs == rho ? 0.f : log2f(cur.vs / rho)) : 0.f;
-            s.rr[lane] = real ? rho / cur.vs : 1.f;
-          }
-          if (lane < 4) s.seen[lane] = pick(cur.seen, lane);
-          if (lane == 0) {
-            s.tile = cur.tile;
-            s.end = 0;
-            s.row_tiles = row_tiles(p, x);
-            s.fall = fall;
-            s.rho = rho;
-          }
-          __syncwarp();
-          if (lane == 0) tc::bar_arrive(&sh.step_full[n % kRing]);
-        }
-        ++n;
-        // keys
-        TC_WAIT(sh.k_free[st], ((j >> 1) & 1) ^ 1);
-        f.store(kr, k_smem + st * kBytes);
-        tc::fence_proxy_async();
-        tc::bar_arrive(&sh.k_full[st]);
+      // v's reference, and O's factor
+      float fall = 1.f;
+      if (hi > rho || lo < rho * kRhoKeep) {
+        const float to = hi > rho ? hi : fmaxf(hi, rho_max * kRhoSpan);
+        fall = rho / to;
+        rho = to;
+        rho_max = fmaxf(rho_max, to);
       }
-      TC_ONCE(more);
-      if (more) f.load(kr, p.c.k, next);
-      TC_ONCE(have);
-      if (have) {
-        // values
-        TC_WAIT(sh.v_free[st], ((j >> 1) & 1) ^ 1);
-        unsigned char* v_at = v_smem + st * kBytes;
-        f.store(vr, v_at);
-        const bool open = (cur.seen[0] & cur.seen[1] & cur.seen[2] & cur.seen[3]) == 0xffffffffu && (cur.tile + 1) * kK <= common;
-        if (!open && f.nans(vr)) f.note(cur.tile, v_at, first, any);
-        if (__any_sync(0xffffffffu, cur.vs == 0.f)) f.clear(cur, v_at);
-        tc::fence_proxy_async();
-        tc::bar_arrive(&sh.v_full[st]);
-        ++j;
+      const bool has = f.has(cur), real = has && cur.vs != 0.f;
+      const uint32_t zero = __ballot_sync(0xffffffffu, has && !real) & 0xff;
+      TC_WAIT(sh.step_free[n % kRing], ((n / kRing) & 1) ^ 1);
+      Step& s = sh.step[n % kRing];
+      if (lane < 8) {
+        // hidden groups take no part; a scale of 0 makes values of 0
+        s.ks[lane] = has ? cur.ks : 1.f;
+        s.lr[lane] = real && cur.vs != rho ? log2f(cur.vs / rho) : 0.f;
+        s.rr[lane] = real ? rho / cur.vs : 1.f;
       }
-      TC_ONCE(more);
-      if (more) {
-        f.load(vr, p.c.v, next);
-        rho = rho_next;
-        fall = fall_next;
+      if (lane < 4) s.seen[lane] = pick(cur.seen, lane);
+      if (lane == 0) {
+        s.tile = cur.tile;
+        s.open = (cur.seen[0] & cur.seen[1] & cur.seen[2] & cur.seen[3]) == 0xffffffffu && (cur.tile + 1) * kK <= common;
+        s.zero = zero;
+        s.end = 0;
+        s.row_tiles = tiles2;
+        s.fall = fall;
       }
-      cur = next;
-      have = 1;
+      __syncwarp();
+      if (lane == 0) tc::bar_arrive(&sh.step_full[n % kRing]);
+      ++n;
+      // the blocks of the pages with a seen key: lane b takes the tile's b-th page
+      const int T = p.c.T, pages = kK >> p.c.log2T;
+      bool want = has;  // of the lane's group; of its page:
+      for (int o = 1; o < 8 / pages; o <<= 1) want |= (bool)__shfl_xor_sync(0xffffffffu, (int)want, o);
+      const int page = __shfl_sync(0xffffffffu, cur.page, (lane & 7) * (8 / pages) & 7);
+      want = __shfl_sync(0xffffffffu, (int)want, (lane & 7) * (8 / pages) & 7) != 0 && lane < pages;
+      const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, want)) * T * D;
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        TC_WAIT(sh.raw_free[kv], (j & 1) ^ 1);
+        if (lane == 0) tc::bar_expect_tx(&sh.raw_full[kv], bytes);
+        __syncwarp();
+        if (want) tma_block(raw + kv * (kK * D) + lane * T * D, kv ? &map_v : &map_k, x.h * T, p.layer * p.c.pages + page, &sh.raw_full[kv]);
+      }
+      ++j;
     }
     // the end of the segment
     TC_WAIT(sh.step_free[n % kRing], ((n / kRing) & 1) ^ 1);
     again = walk_next<kR, kK, kOver>(p, sh, x);
-    if (warp == 0 && lane == 0) {
+    if (lane == 0) {
       sh.step[n % kRing].end = again ? 1 : 2;
       sh.step[n % kRing].rho = rho;
       tc::bar_arrive(&sh.step_full[n % kRing]);
     }
     ++n;
-    ++seg;
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void convert_role(const AttendParams& p, Shared& sh, unsigned char* k_smem, unsigned char* v_smem,
+                                             const unsigned char* raw) {
+  constexpr int kBytes = kK * D * 2;
+  const int lane = threadIdx.x & 31;
+  const Convert<D> f(lane, (threadIdx.x >> 5) & 3);
+  uint32_t j = 0, seg = 0;
+#pragma unroll 1
+  for (uint32_t n = 0;; ++n) {
+    TC_WAIT(sh.step_full[n % kRing], (n / kRing) & 1);
+    const Step& s = sh.step[n % kRing];
+    const int end = s.end;
+    if (!end) {
+      const bool full = (s.seen[0] & s.seen[1] & s.seen[2] & s.seen[3]) == 0xffffffffu;
+      const int st = j & 1;
+      uint4 r[Convert<D>::PASSES];
+      TC_WAIT(sh.raw_full[0], j & 1);
+      f.read(r, raw);
+      if (!full) f.mask(r, s.seen);
+      __syncwarp();
+      if (lane == 0) tc::bar_arrive(&sh.raw_free[0]);
+      TC_WAIT(sh.k_free[st], ((j >> 1) & 1) ^ 1);
+      f.store(r, k_smem + st * kBytes);
+      tc::fence_proxy_async();
+      tc::bar_arrive(&sh.k_full[st]);
+      TC_WAIT(sh.raw_full[1], j & 1);
+      f.read(r, raw + kK * D);
+      if (!full) f.mask(r, s.seen);
+      __syncwarp();
+      if (lane == 0) tc::bar_arrive(&sh.raw_free[1]);
+      unsigned char* v_at = v_smem + st * kBytes;
+      TC_WAIT(sh.v_free[st], ((j >> 1) & 1) ^ 1);
+      f.store(r, v_at);
+      if (!s.open && f.nans(r)) f.note(s.tile, v_at, sh.nan_first[seg & 3], &sh.any_nan[seg & 3]);
+      if (s.zero) f.clear(s.zero, v_at);
+      tc::fence_proxy_async();
+      tc::bar_arrive(&sh.v_full[st]);
+      ++j;
+    } else {
+      ++seg;
+    }
+    __syncwarp();
+    if (lane == 0) tc::bar_arrive(&sh.step_free[n % kRing]);
+    if (end == 2) return;
   }
 }
 
@@ -687,31 +714,29 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
         tc::fence_after();
         const int tile = st.tile;
         const bool open = (st.seen[0] & st.seen[1] & st.seen[2] & st.seen[3]) == 0xffffffffu && (tile + 1) * kK <= common;
-        // scores of 32 keys, hidden ones -inf (rolled loops: the roles together have to stay within the instruction cache)
-        const int lim = limit - tile * kK;
-        auto chunk = [&](uint32_t(&v)[32], int q) {
-          tc::tmem_ld32(s_at + 32 * q, v);
-          wait_ld(v);
-          if (!open) {
+        // the row's scores, hidden ones -inf
+        uint32_t v[128];
+        tmem_ld128(s_at, v);
+        if (!open) {
+          const int lim = limit - tile * kK;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
             const int m = lim - 32 * q;
             const uint32_t see = st.seen[q] & (m >= 32 ? 0xffffffffu : m <= 0 ? 0u : (1u << m) - 1u);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) v[k] = (see >> k) & 1 ? v[k] : 0xff800000u;
+            for (int k = 0; k < 32; ++k) v[32 * q + k] = (see >> k) & 1 ? v[32 * q + k] : 0xff800000u;
           }
-        };
-        uint32_t v[32];
+        }
         float m = top;
-#pragma unroll 1
-        for (int q = 0; q < 4; ++q) {
-          chunk(v, q);
 #pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            float x0 = -INFINITY;
+        for (int g = 0; g < 8; ++g) {
+          float x0 = -INFINITY, x1 = -INFINITY;
 #pragma unroll
-            for (int k = 0; k < 16; k += 2)
-              x0 = tc::fmax3(x0, __uint_as_float(v[16 * g + k]), __uint_as_float(v[16 * g + k + 1]));
-            m = fmaxf(m, x0 * fmaxf(st.ks[2 * q + g] * qscale, kLeast));
+          for (int k = 0; k < 8; k += 2) {
+            x0 = tc::fmax3(x0, __uint_as_float(v[16 * g + k]), __uint_as_float(v[16 * g + k + 1]));
+            x1 = tc::fmax3(x1, __uint_as_float(v[16 * g + 8 + k]), __uint_as_float(v[16 * g + 9 + k]));
           }
+          m = fmaxf(m, fmaxf(x0, x1) * fmaxf(st.ks[g] * qscale, kLeast));
         }
         top = m;
         float fall = st.fall;
@@ -740,14 +765,13 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
           }
         }
         const float base = ref == -INFINITY ? 0.f : ref;
-        // backwards, so that P (columns 64 + 16 q) only goes over scores that have been read
-#pragma unroll 1
-        for (int q = 3; q >= 0; --q) {
-          chunk(v, q);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
           uint32_t pk[16];
 #pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            const float f = fmaxf(st.ks[2 * q + g] * qscale, kLeast), add = st.lr[2 * q + g] - base;
+          for (int h2 = 0; h2 < 2; ++h2) {
+            const int g = 2 * q + h2;
+            const float f = fmaxf(st.ks[g] * qscale, kLeast), add = st.lr[g] - base;
             const float2 ff = make_float2(f, f), aa = make_float2(add, add);
             float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
@@ -756,11 +780,11 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
               x2.x = fast_exp2(x2.x);
               x2.y = fast_exp2(x2.y);
               sum = add2(sum, x2);
-              pk[8 * g + k] = pack_f16(x2.x, x2.y);
+              pk[8 * h2 + k] = pack_f16(x2.x, x2.y);
             }
-            l = fmaf(sum.x + sum.y, st.rr[2 * q + g], l);
+            l = fmaf(sum.x + sum.y, st.rr[g], l);
           }
-          tmem_st16(s_at + 64 + 16 * q, pk);
+          tmem_st16(s_at + 64 + 16 * q, pk);  // (the scores are all in registers)
         }
         tc::tmem_wait_st();
         tc::fence_before();
@@ -916,17 +940,22 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
 }
 
 template <int D, bool BF16>
-__global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(AttendParams p) {
+__global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(AttendParams p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
   constexpr int kBytes = kK * D * 2;
-  extern __shared__ unsigned char dyn[];
-  __shared__ Shared sh;
-  unsigned char* smem = dyn + ((1024 - (tc::su32(dyn) & 1023)) & 1023);  // (an offset: the pointer stays one to shared memory)
+  // queries 2 tiles, keys and values 2 stages each, codes as they come: 7 x 32 KB (D = 128)
+  extern __shared__ __align__(1024) unsigned char smem[];
+  unsigned char* q_smem = smem;
+  unsigned char* k_smem = smem + 2 * kBytes;
+  unsigned char* v_smem = smem + 4 * kBytes;
+  unsigned char* raw = smem + 6 * kBytes;
+  Shared& sh = *reinterpret_cast<Shared*>(smem + 7 * kBytes);
+  int64_t* scan = reinterpret_cast<int64_t*>(&sh.nan_first[0][0]);
   const int warp = threadIdx.x >> 5;
   Line line;
-  const LinePart part = attend_line<kR, kK, kOver, kThreads>(p, kOver + 1, kAttendTcCtas, 0, sh.scan, line);
+  const LinePart part = attend_line<kR, kK, kOver, kThreads>(p, kOver + 1, kAttendTcCtas, 0, scan, line);
   if (line.units == 0 || (int)blockIdx.x >= line.first) return;
   Stretch w;
-  attend_find<kR, kK, kOver, kThreads>(p, line, part, blockIdx.x, sh.scan, w);
+  attend_find<kR, kK, kOver, kThreads>(p, line, part, blockIdx.x, scan, w);
   {
     Walk x;
     if (!walk_begin<kR, kK, kOver>(p, w, x)) return;  // no tile in the stretch: every role has at least one from here on
@@ -951,13 +980,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(AttendParams p) 
       tc::bar_init(&sh.s_full[k], 1);
       tc::bar_init(&sh.p_full[k], 128);
       tc::bar_init(&sh.o_done[k], 1);
+      tc::bar_init(&sh.raw_full[k], 1);
+      tc::bar_init(&sh.raw_free[k], 4);
     }
     for (int k = 0; k < kRing; ++k) {
       tc::bar_init(&sh.step_full[k], 1);
-      tc::bar_init(&sh.step_free[k], 9);  // eight softmax warps and the issuing thread
+      tc::bar_init(&sh.step_free[k], 13);  // every warp that reads it
     }
     tc::bar_fence_init();
   }
+  __syncthreads();
   if (threadIdx.x < 4) sh.any_nan[threadIdx.x] = 0;
   for (int d = threadIdx.x; d < 4 * 128; d += kThreads) (&sh.nan_first[0][0])[d] = 0x7fffffff;
   if (warp == 12) tc::tmem_alloc(&sh.tmem, 512);
@@ -965,26 +997,29 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(AttendParams p) 
   __syncthreads();
   tc::fence_after();
   const uint32_t tmem = sh.tmem;
-  unsigned char* q_smem = smem;
-  unsigned char* k_smem = smem + 2 * kBytes;
-  unsigned char* v_smem = smem + 4 * kBytes;
   // registers: 512 threads start with 128 each, four warpgroups split them
   if (warp < 8) {
     tc::setmaxnreg_inc<kRegSoftmax>();
     softmax_role<D, BF16>(p, sh, q_smem, tmem, warp >> 2);
   } else if (warp < 12) {
-    tc::setmaxnreg_inc<kRegFetch>();
-    fetch_role<D>(p, sh, k_smem, v_smem);
+    tc::setmaxnreg_dec<kRegConvert>();
+    convert_role<D>(p, sh, k_smem, v_smem, raw);
   } else {
     tc::setmaxnreg_dec<kRegIssue>();
     if (warp == 12)
       mma_role<D>(p, sh, tc::su32(q_smem), tc::su32(k_smem), tc::su32(v_smem), tmem);
+    else if (warp == 13)
+      plan_role<D>(p, sh, map_k, map_v, raw);
   }
   __syncthreads();
-  // after a wait that ran out products may still be in flight
+  // after a wait that ran out, products and copies may still be in flight
   if (sh.stop && threadIdx.x == 384) {
     tc::mma_commit(&sh.drain);
     tc::bar_wait(&sh.drain, 0, nullptr, kWaitNs);
+    for (int k = 0; k < 2; ++k) {
+      tc::bar_wait(&sh.raw_full[k], 0, nullptr, kWaitNs / 8);
+      tc::bar_wait(&sh.raw_full[k], 1, nullptr, kWaitNs / 8);
+    }
   }
   __syncthreads();
   if (warp == 12) tc::tmem_dealloc(tmem, 512);
@@ -1000,7 +1035,7 @@ int prepare(int smem) {
   if ((ready.load(std::memory_order_acquire) >> dev) & 1) return OCCAM_OK;
   cudaFuncAttributes at;
   if (cudaFuncGetAttributes(&at, attend_tc_kernel<D, BF16>) != cudaSuccess) return OCCAM_ERR_CUDA;
-  if (at.numRegs * kThreads < 256 * kRegSoftmax + 128 * (kRegFetch + kRegIssue)) return OCCAM_ERR_UNSUPPORTED;
+  if (at.numRegs * kThreads < 256 * kRegSoftmax + 128 * (kRegConvert + kRegIssue)) return OCCAM_ERR_UNSUPPORTED;
   if (cudaFuncSetAttribute(attend_tc_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
     return OCCAM_ERR_CUDA;
   ready.fetch_or(uint64_t(1) << dev, std::memory_order_release);
@@ -1008,11 +1043,11 @@ int prepare(int smem) {
 }
 
 template <int D, bool BF16>
-int launch(const AttendParams& p, cudaStream_t st) {
-  const int smem = 6 * kK * D * 2 + 1024;
+int launch(const AttendParams& p, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t st) {
+  const int smem = 7 * kK * D * 2 + kSharedBytes;
   const int rc = prepare<D, BF16>(smem);
   if (rc != OCCAM_OK) return rc;
-  attend_tc_kernel<D, BF16><<<std::min(cache_sms(), kAttendTcCtas), kThreads, smem, st>>>(p);
+  attend_tc_kernel<D, BF16><<<std::min(cache_sms(), kAttendTcCtas), kThreads, smem, st>>>(p, mk, mv);
   count_launch();
   return cudaGetLastError() == cudaSuccess ? OCCAM_OK : OCCAM_ERR_CUDA;
 }
@@ -1020,6 +1055,8 @@ int launch(const AttendParams& p, cudaStream_t st) {
 }  // namespace
 
 int occam::launch_attend_tc(const AttendParams& p, int dim, cudaStream_t st) {
-  if (dim == 128) return p.bf16 ? launch<128, true>(p, st) : launch<128, false>(p, st);
-  return p.bf16 ? launch<64, true>(p, st) : launch<64, false>(p, st);
+  CUtensorMap mk, mv;
+  if (!encode_blocks(&mk, p.c, p.c.k, dim, p.c.T, false) || !encode_blocks(&mv, p.c, p.c.v, dim, p.c.T, false)) return OCCAM_ERR_CUDA;
+  if (dim == 128) return p.bf16 ? launch<128, true>(p, mk, mv, st) : launch<128, false>(p, mk, mv, st);
+  return p.bf16 ? launch<64, true>(p, mk, mv, st) : launch<64, false>(p, mk, mv, st);
 }

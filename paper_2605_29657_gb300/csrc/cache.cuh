@@ -57,7 +57,7 @@ inline int check_cache(const occam_cache* c) {
   if (c->dim != 64 && c->dim != 128) return OCCAM_ERR_UNSUPPORTED;
   if (c->page_tokens != 16 && c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128)
     return OCCAM_ERR_UNSUPPORTED;
-  if (c->layers < 1 || c->pages < 1 || c->pages > (1 << 24) || c->heads < 1 || c->heads > 1024 || c->max_seqs < 1 ||
+  if (c->layers < 1 || c->pages < 1 || c->pages > (1 << 24) || (int64_t)c->layers * c->pages > 0x7fffffff || c->heads < 1 || c->heads > 1024 || c->max_seqs < 1 ||
       c->max_seqs > 65535 || c->layers > 65535 || c->max_pages < 1 || (int64_t)c->max_pages * c->page_tokens >= (int64_t(1) << 31) - 256)
     return OCCAM_ERR_INVALID_ARG;
   if (!c->k || !c->v || !c->k_scale || !c->v_scale || !c->table || !c->length || !c->refs) return OCCAM_ERR_INVALID_ARG;
