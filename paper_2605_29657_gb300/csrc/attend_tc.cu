@@ -12,8 +12,8 @@
 //  - warps 8-11 turn the codes into f16 (exact) in the matrix layout
 //    (128-byte swizzle), two stages deep;
 //  - warp 12 issues the products: S = Q K^T into tensor memory, O += P V with P
-//    read from tensor memory, for two row tiles of 128 in turn, so that one
-//    tile's softmax runs under the other's products;
+//    read from tensor memory, for two row tiles of 128, 64 keys at a time: while a
+//    row tile's softmax works on one half of its scores, the other half is multiplied;
 //  - warps 0-3 and 4-7 hold a row a thread: scores from tensor memory, maximum,
 //    exponentials, P back over the scores as f16.
 // O stays in tensor memory. It is rescaled only where a row's maximum grew by more than
@@ -37,7 +37,7 @@ constexpr int kOver = 4;       // beginning and ending an item takes as long as 
 constexpr int kGroup = 16;     // keys that share a page at least
 constexpr int kThreads = 512;
 constexpr int kRing = 4;
-constexpr int kRegSoftmax = 184, kRegConvert = 72, kRegIssue = 72;  // 2 x 184 + 72 + 72 = 4 x 128
+constexpr int kRegSoftmax = 168, kRegConvert = 88, kRegIssue = 88;  // 2 x 168 + 88 + 88 = 4 x 128
 constexpr uint64_t kWaitNs = 2000000000ull;
 constexpr float kLazy = 8.f;             // log2 growth of a maximum before O is rescaled
 constexpr float kLeast = 1.2e-38f;       // a score's factor: never 0, so that a hidden key's -inf stays
@@ -59,7 +59,7 @@ struct Step {
 };
 
 struct Shared {
-  uint64_t q_full, k_full[2], k_free[2], v_full[2], v_free[2], s_full[2], p_full[2], o_done[2], step_full[kRing],
+  uint64_t q_full, k_full[2], k_free[2], v_full[2], v_free[2], s_full[2][2], p_full[2][2], o_done[2][2], step_full[kRing],
       step_free[kRing], raw_full[2], raw_free[2], meet, drain;
   Step step[kRing];
   Line line;
@@ -142,15 +142,11 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
       : "r"(taddr)
       : "memory");
 }
-// 128 columns of this thread's lane; they are there on return
-__device__ __forceinline__ void tmem_ld128(uint32_t taddr, uint32_t (&v)[128]) {
-  uint32_t(&a)[64] = *reinterpret_cast<uint32_t(*)[64]>(v);
-  uint32_t(&b)[64] = *reinterpret_cast<uint32_t(*)[64]>(v + 64);
-  tc::tmem_ld64(taddr, a);
-  tc::tmem_ld64(taddr + 64, b);
+// 64 columns of this thread's lane; they are there on return
+__device__ __forceinline__ void tmem_ld64(uint32_t taddr, uint32_t (&v)[64]) {
+  tc::tmem_ld64(taddr, v);
   tc::tmem_wait_ld();
-  asm volatile("" : OCCAM_TC_RW64(a));
-  asm volatile("" : OCCAM_TC_RW64(b));
+  asm volatile("" : OCCAM_TC_RW64(v));
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
   asm volatile(
@@ -536,50 +532,49 @@ template <int D>
 __device__ __forceinline__ void mma_role(const AttendParams& p, Shared& sh, uint32_t q_smem, uint32_t k_smem,
                                          uint32_t v_smem, uint32_t tmem) {
   constexpr int kBytes = kK * D * 2;
-  constexpr uint32_t id_s = idesc_f16(128, 128, false), id_o = idesc_f16(128, D, true);
+  constexpr uint32_t id_s = idesc_f16(128, 64, false), id_o = idesc_f16(128, D, true);
   const uint64_t dq = desc_kmajor(q_smem), dk = desc_kmajor(k_smem), dv = desc_mnmajor(v_smem);
-  // (a descriptor's address field counts 16 bytes)
-  auto scores = [&](auto tt, uint32_t st) {
-    constexpr int t = decltype(tt)::value;
+  // Row tile t, half h of the step's keys (a descriptor's address field counts 16 bytes).
+  auto scores = [&](auto tt, auto hh, uint32_t st) {
+    constexpr int t = decltype(tt)::value, h = decltype(hh)::value;
     if (elect_one()) {
-      const uint64_t kd = dk + st * (kBytes >> 4), qd = dq + t * (kBytes >> 4);
+      const uint64_t kd = dk + st * (kBytes >> 4) + h * (64 * 128 >> 4), qd = dq + t * (kBytes >> 4);
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) {
-        constexpr int kBlock = 16384 >> 4;
-        const int o = (k >> 2) * kBlock + (k & 3) * 2;
-        tc::mma_bf16(tmem + t * 128, qd + o, kd + o, id_s, k > 0);
+        const int o = (k >> 2) * (16384 >> 4) + (k & 3) * 2;
+        tc::mma_bf16(tmem + t * 128 + h * 64, qd + o, kd + o, id_s, k > 0);
       }
-      tc::mma_commit(&sh.s_full[t]);
+      tc::mma_commit(&sh.s_full[t][h]);
     }
     __syncwarp();
   };
-  auto values = [&](auto tt, uint32_t st, bool begin) {
-    constexpr int t = decltype(tt)::value;
+  auto values = [&](auto tt, auto hh, uint32_t st, bool begin) {
+    constexpr int t = decltype(tt)::value, h = decltype(hh)::value;
     if (elect_one()) {
-      const uint64_t vd = dv + st * (kBytes >> 4);
+      const uint64_t vd = dv + st * (kBytes >> 4) + h * (64 * 128 >> 4);
 #pragma unroll
-      for (int k = 0; k < kK / 16; ++k)
-        mma_ts(tmem + 256 + t * 128, tmem + t * 128 + 64 + k * 8, vd + k * (2048 >> 4), id_o, k > 0 ? 1u : (begin ? 0u : 1u));
-      tc::mma_commit(&sh.o_done[t]);
+      for (int k = 0; k < 4; ++k)
+        mma_ts(tmem + 256 + t * 128, tmem + t * 128 + h * 64 + k * 8, vd + k * (2048 >> 4), id_o,
+               h > 0 || k > 0 ? 1u : (begin ? 0u : 1u));
+      tc::mma_commit(&sh.o_done[t][h]);
     }
     __syncwarp();
   };
-  using T0 = std::integral_constant<int, 0>;
-  using T1 = std::integral_constant<int, 1>;
-  uint32_t n = 0, j = 0, it0 = 0, it1 = 0;  // step records, steps, products of each row tile
+  using C0 = std::integral_constant<int, 0>;
+  using C1 = std::integral_constant<int, 1>;
+  uint32_t n = 0, j = 0, it0 = 0, it1 = 0;  // step records, steps, steps of each row tile
   int end = 0;
   for (uint32_t seg = 0; end != 2; ++seg) {
     TC_WAIT(sh.q_full, seg & 1);
     bool two = false;
     end = 0;
-    // pass k: O += P V of step k - 1, S of step k, a row tile after the other
+    // pass k: by halves and row tiles, O += P V of step k - 1, then S of step k in the place of that P
     for (uint32_t k = 0; !end; ++k) {
       if (k > 0) {
-        TC_WAIT(sh.p_full[0], it0 & 1);
-        ++it0;
+        TC_WAIT(sh.p_full[0][0], it0 & 1);
         TC_WAIT(sh.v_full[(j - 1) & 1], ((j - 1) >> 1) & 1);
         tc::fence_after();
-        values(T0{}, (j - 1) & 1, k == 1);
+        values(C0{}, C0{}, (j - 1) & 1, k == 1);
       }
       TC_WAIT(sh.step_full[n % kRing], (n / kRing) & 1);
       end = sh.step[n % kRing].end;
@@ -587,16 +582,31 @@ __device__ __forceinline__ void mma_role(const AttendParams& p, Shared& sh, uint
         two = sh.step[n % kRing].row_tiles == 2;
         TC_WAIT(sh.k_full[j & 1], (j >> 1) & 1);
         tc::fence_after();
-        scores(T0{}, j & 1);
+        scores(C0{}, C0{}, j & 1);
       }
       if (two) {
         if (k > 0) {
-          TC_WAIT(sh.p_full[1], it1 & 1);
+          TC_WAIT(sh.p_full[1][0], it1 & 1);
+          tc::fence_after();
+          values(C1{}, C0{}, (j - 1) & 1, k == 1);
+        }
+        if (!end) scores(C1{}, C0{}, j & 1);
+      }
+      if (k > 0) {
+        TC_WAIT(sh.p_full[0][1], it0 & 1);
+        ++it0;
+        tc::fence_after();
+        values(C0{}, C1{}, (j - 1) & 1, false);
+      }
+      if (!end) scores(C0{}, C1{}, j & 1);
+      if (two) {
+        if (k > 0) {
+          TC_WAIT(sh.p_full[1][1], it1 & 1);
           ++it1;
           tc::fence_after();
-          values(T1{}, (j - 1) & 1, k == 1);
+          values(C1{}, C1{}, (j - 1) & 1, false);
         }
-        if (!end) scores(T1{}, j & 1);
+        if (!end) scores(C1{}, C1{}, j & 1);
       }
       if (elect_one()) {
         if (k > 0) tc::mma_commit(&sh.v_free[(j - 1) & 1]);
@@ -710,86 +720,90 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
       const bool end = st.end != 0;
       if (end) rho = st.rho;
       if (!end && mine) {
-        TC_WAIT(sh.s_full[t], it & 1);
-        tc::fence_after();
         const int tile = st.tile;
         const bool open = (st.seen[0] & st.seen[1] & st.seen[2] & st.seen[3]) == 0xffffffffu && (tile + 1) * kK <= common;
-        // the row's scores, hidden ones -inf
-        uint32_t v[128];
-        tmem_ld128(s_at, v);
-        if (!open) {
-          const int lim = limit - tile * kK;
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int m = lim - 32 * q;
-            const uint32_t see = st.seen[q] & (m >= 32 ? 0xffffffffu : m <= 0 ? 0u : (1u << m) - 1u);
-#pragma unroll
-            for (int k = 0; k < 32; ++k) v[32 * q + k] = (see >> k) & 1 ? v[32 * q + k] : 0xff800000u;
-          }
-        }
-        float m = top;
-#pragma unroll
-        for (int g = 0; g < 8; ++g) {
-          float x0 = -INFINITY, x1 = -INFINITY;
-#pragma unroll
-          for (int k = 0; k < 8; k += 2) {
-            x0 = tc::fmax3(x0, __uint_as_float(v[16 * g + k]), __uint_as_float(v[16 * g + k + 1]));
-            x1 = tc::fmax3(x1, __uint_as_float(v[16 * g + 8 + k]), __uint_as_float(v[16 * g + 9 + k]));
-          }
-          m = fmaxf(m, fmaxf(x0, x1) * fmaxf(st.ks[g] * qscale, kLeast));
-        }
-        top = m;
-        float fall = st.fall;
-        bool move = fall != 1.f;
-        if (m > ref + kLazy || ref == -INFINITY) {
-          const float to = m;
-          if (to != ref) {
-            fall *= ref == -INFINITY ? 0.f : fast_exp2(ref - to);
-            l *= ref == -INFINITY ? 0.f : fast_exp2(ref - to);
-            move = true;
-            ref = to;
-          }
-        }
-        // O in units of the new references (nothing is there before the first product)
-        if (!begin && __any_sync(0xffffffffu, move)) {
-          TC_WAIT(sh.o_done[t], (it - 1) & 1);
-          tc::fence_after();
 #pragma unroll 1
-          for (int c = 0; c < D / 32; ++c) {
-            uint32_t o[32];
-            tc::tmem_ld32(o_at + 32 * c, o);
-            wait_ld(o);
+        for (int h = 0; h < 2; ++h, ++it) {
+          TC_WAIT(sh.s_full[t][h], (it >> 1) & 1);
+          tc::fence_after();
+          // the row's scores of 64 keys, hidden ones -inf
+          uint32_t v[64];
+          tmem_ld64(s_at + 64 * h, v);
+          if (!open) {
+            const int lim = limit - tile * kK - 64 * h;
 #pragma unroll
-            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * fall);
-            tc::tmem_st32(o_at + 32 * c, o);
-          }
-        }
-        const float base = ref == -INFINITY ? 0.f : ref;
+            for (int q = 0; q < 2; ++q) {
+              const int m = lim - 32 * q;
+              const uint32_t see = st.seen[2 * h + q] & (m >= 32 ? 0xffffffffu : m <= 0 ? 0u : (1u << m) - 1u);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          uint32_t pk[16];
-#pragma unroll
-          for (int h2 = 0; h2 < 2; ++h2) {
-            const int g = 2 * q + h2;
-            const float f = fmaxf(st.ks[g] * qscale, kLeast), add = st.lr[g] - base;
-            const float2 ff = make_float2(f, f), aa = make_float2(add, add);
-            float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              float2 x2 = fma2(make_float2(__uint_as_float(v[16 * g + 2 * k]), __uint_as_float(v[16 * g + 2 * k + 1])), ff, aa);
-              x2.x = fast_exp2(x2.x);
-              x2.y = fast_exp2(x2.y);
-              sum = add2(sum, x2);
-              pk[8 * h2 + k] = pack_f16(x2.x, x2.y);
+              for (int k = 0; k < 32; ++k) v[32 * q + k] = (see >> k) & 1 ? v[32 * q + k] : 0xff800000u;
             }
-            l = fmaf(sum.x + sum.y, st.rr[g], l);
           }
-          tmem_st16(s_at + 64 + 16 * q, pk);  // (the scores are all in registers)
+          float f[4], m = top;
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            f[g] = fmaxf(st.ks[4 * h + g] * qscale, kLeast);
+            float x0 = -INFINITY, x1 = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) {
+              x0 = tc::fmax3(x0, __uint_as_float(v[16 * g + k]), __uint_as_float(v[16 * g + k + 1]));
+              x1 = tc::fmax3(x1, __uint_as_float(v[16 * g + 8 + k]), __uint_as_float(v[16 * g + 9 + k]));
+            }
+            m = fmaxf(m, fmaxf(x0, x1) * f[g]);
+          }
+          top = m;
+          float fall = h == 0 ? st.fall : 1.f;
+          bool move = fall != 1.f;
+          if (m > ref + kLazy || ref == -INFINITY) {
+            if (m != ref) {
+              const float by = ref == -INFINITY ? 0.f : fast_exp2(ref - m);
+              fall *= by;
+              l *= by;
+              move = true;
+              ref = m;
+            }
+          }
+          // O in units of the new references (nothing is there before the first product)
+          if (!(begin && h == 0) && __any_sync(0xffffffffu, move)) {
+            // the product of the half before (the one before that is done: this half's scores came after it)
+            TC_WAIT(sh.o_done[t][h ^ 1], ((it - 1) >> 1) & 1);
+            tc::fence_after();
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+              uint32_t o[32];
+              tc::tmem_ld32(o_at + 32 * c, o);
+              wait_ld(o);
+#pragma unroll
+              for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * fall);
+              tc::tmem_st32(o_at + 32 * c, o);
+            }
+          }
+          const float base = ref == -INFINITY ? 0.f : ref;
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int g = 2 * q + e;
+              const float add = st.lr[4 * h + g] - base;
+              const float2 ff = make_float2(f[g], f[g]), aa = make_float2(add, add);
+              float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                float2 x2 = fma2(make_float2(__uint_as_float(v[16 * g + 2 * k]), __uint_as_float(v[16 * g + 2 * k + 1])), ff, aa);
+                x2.x = fast_exp2(x2.x);
+                x2.y = fast_exp2(x2.y);
+                sum = add2(sum, x2);
+                pk[8 * e + k] = pack_f16(x2.x, x2.y);
+              }
+              l = fmaf(sum.x + sum.y, st.rr[4 * h + g], l);
+            }
+            tmem_st16(s_at + 64 * h + 16 * q, pk);  // (the half's scores are all in registers)
+          }
+          tc::tmem_wait_st();
+          tc::fence_before();
+          tc::bar_arrive(&sh.p_full[t][h]);
         }
-        tc::tmem_wait_st();
-        tc::fence_before();
-        tc::bar_arrive(&sh.p_full[t]);
-        ++it;
       }
       __syncwarp();
       if (lane == 0) tc::bar_arrive(&sh.step_free[n % kRing]);
@@ -804,7 +818,7 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
     const int64_t to = (x.s.row0 + tok) * p.H + x.h * p.G + at - tok * p.G;
     const int64_t mypart = ((int64_t)blockIdx.x * 2 + slot) * kR + row;
     if (mine) {
-      TC_WAIT(sh.o_done[t], (it - 1) & 1);
+      TC_WAIT(sh.o_done[t][1], ((it >> 1) - 1) & 1);
       tc::fence_after();
       const float scale = l == 0.f ? 0.f : done ? rho / l : rho;
       uint16_t* out = p.out + to * D;
@@ -977,9 +991,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(AttendParams p, 
       tc::bar_init(&sh.v_full[k], 128);
       tc::bar_init(&sh.k_free[k], 1);
       tc::bar_init(&sh.v_free[k], 1);
-      tc::bar_init(&sh.s_full[k], 1);
-      tc::bar_init(&sh.p_full[k], 128);
-      tc::bar_init(&sh.o_done[k], 1);
+      for (int h = 0; h < 2; ++h) {
+        tc::bar_init(&sh.s_full[k][h], 1);
+        tc::bar_init(&sh.p_full[k][h], 128);
+        tc::bar_init(&sh.o_done[k][h], 1);
+      }
       tc::bar_init(&sh.raw_full[k], 1);
       tc::bar_init(&sh.raw_free[k], 4);
     }
