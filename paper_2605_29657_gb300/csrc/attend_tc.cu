@@ -21,7 +21,6 @@
 // is held in; both references are undone at the end.
 #include <algorithm>
 #include <atomic>
-#include <type_traits>
 
 #include "attend.cuh"
 #include "attend_tc.cuh"
@@ -493,28 +492,24 @@ __device__ __forceinline__ void convert_role(const AttendParams& p, Shared& sh, 
     if (!end) {
       const bool full = (s.seen[0] & s.seen[1] & s.seen[2] & s.seen[3]) == 0xffffffffu;
       const int st = j & 1;
-      uint4 r[Convert<D>::PASSES];
-      TC_WAIT(sh.raw_full[0], j & 1);
-      f.read(r, raw);
-      if (!full) f.mask(r, s.seen);
-      __syncwarp();
-      if (lane == 0) tc::bar_arrive(&sh.raw_free[0]);
-      TC_WAIT(sh.k_free[st], ((j >> 1) & 1) ^ 1);
-      f.store(r, k_smem + st * kBytes);
-      tc::fence_proxy_async();
-      tc::bar_arrive(&sh.k_full[st]);
-      TC_WAIT(sh.raw_full[1], j & 1);
-      f.read(r, raw + kK * D);
-      if (!full) f.mask(r, s.seen);
-      __syncwarp();
-      if (lane == 0) tc::bar_arrive(&sh.raw_free[1]);
-      unsigned char* v_at = v_smem + st * kBytes;
-      TC_WAIT(sh.v_free[st], ((j >> 1) & 1) ^ 1);
-      f.store(r, v_at);
-      if (!s.open && f.nans(r)) f.note(s.tile, v_at, sh.nan_first[seg & 3], &sh.any_nan[seg & 3]);
-      if (s.zero) f.clear(s.zero, v_at);
-      tc::fence_proxy_async();
-      tc::bar_arrive(&sh.v_full[st]);
+#pragma unroll 1
+      for (int kv = 0; kv < 2; ++kv) {
+        uint4 r[Convert<D>::PASSES];
+        TC_WAIT(sh.raw_full[kv], j & 1);
+        f.read(r, raw + kv * (kK * D));
+        if (!full) f.mask(r, s.seen);
+        __syncwarp();
+        if (lane == 0) tc::bar_arrive(&sh.raw_free[kv]);
+        unsigned char* to = (kv ? v_smem : k_smem) + st * kBytes;
+        TC_WAIT(*(kv ? &sh.v_free[st] : &sh.k_free[st]), ((j >> 1) & 1) ^ 1);
+        f.store(r, to);
+        if (kv) {
+          if (!s.open && f.nans(r)) f.note(s.tile, to, sh.nan_first[seg & 3], &sh.any_nan[seg & 3]);
+          if (s.zero) f.clear(s.zero, to);
+        }
+        tc::fence_proxy_async();
+        tc::bar_arrive(kv ? &sh.v_full[st] : &sh.k_full[st]);
+      }
       ++j;
     } else {
       ++seg;
@@ -534,79 +529,60 @@ __device__ __forceinline__ void mma_role(const AttendParams& p, Shared& sh, uint
   constexpr int kBytes = kK * D * 2;
   constexpr uint32_t id_s = idesc_f16(128, 64, false), id_o = idesc_f16(128, D, true);
   const uint64_t dq = desc_kmajor(q_smem), dk = desc_kmajor(k_smem), dv = desc_mnmajor(v_smem);
-  // Row tile t, half h of the step's keys (a descriptor's address field counts 16 bytes).
-  auto scores = [&](auto tt, auto hh, uint32_t st) {
-    constexpr int t = decltype(tt)::value, h = decltype(hh)::value;
-    if (elect_one()) {
-      const uint64_t kd = dk + st * (kBytes >> 4) + h * (64 * 128 >> 4), qd = dq + t * (kBytes >> 4);
-#pragma unroll
-      for (int k = 0; k < D / 16; ++k) {
-        const int o = (k >> 2) * (16384 >> 4) + (k & 3) * 2;
-        tc::mma_bf16(tmem + t * 128 + h * 64, qd + o, kd + o, id_s, k > 0);
-      }
-      tc::mma_commit(&sh.s_full[t][h]);
-    }
-    __syncwarp();
-  };
-  auto values = [&](auto tt, auto hh, uint32_t st, bool begin) {
-    constexpr int t = decltype(tt)::value, h = decltype(hh)::value;
-    if (elect_one()) {
-      const uint64_t vd = dv + st * (kBytes >> 4) + h * (64 * 128 >> 4);
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        mma_ts(tmem + 256 + t * 128, tmem + t * 128 + h * 64 + k * 8, vd + k * (2048 >> 4), id_o,
-               h > 0 || k > 0 ? 1u : (begin ? 0u : 1u));
-      tc::mma_commit(&sh.o_done[t][h]);
-    }
-    __syncwarp();
-  };
-  using C0 = std::integral_constant<int, 0>;
-  using C1 = std::integral_constant<int, 1>;
-  uint32_t n = 0, j = 0, it0 = 0, it1 = 0;  // step records, steps, steps of each row tile
+  uint32_t n = 0, j = 0, it = 0, it1 = 0;  // step records, steps, steps of row tile 0 and 1
   int end = 0;
   for (uint32_t seg = 0; end != 2; ++seg) {
     TC_WAIT(sh.q_full, seg & 1);
-    bool two = false;
+    int nt = 1;
     end = 0;
-    // pass k: by halves and row tiles, O += P V of step k - 1, then S of step k in the place of that P
+    // Pass k: by halves h and row tiles t, O += P V of step k - 1, then S of step k in the
+    // place of that P. (Rolled: the roles together have to stay within the
+    // instruction cache. A descriptor's address field counts 16 bytes.)
+#pragma unroll 1
     for (uint32_t k = 0; !end; ++k) {
-      if (k > 0) {
-        TC_WAIT(sh.p_full[0][0], it0 & 1);
-        TC_WAIT(sh.v_full[(j - 1) & 1], ((j - 1) >> 1) & 1);
-        tc::fence_after();
-        values(C0{}, C0{}, (j - 1) & 1, k == 1);
-      }
-      TC_WAIT(sh.step_full[n % kRing], (n / kRing) & 1);
-      end = sh.step[n % kRing].end;
-      if (!end) {
-        two = sh.step[n % kRing].row_tiles == 2;
-        TC_WAIT(sh.k_full[j & 1], (j >> 1) & 1);
-        tc::fence_after();
-        scores(C0{}, C0{}, j & 1);
-      }
-      if (two) {
-        if (k > 0) {
-          TC_WAIT(sh.p_full[1][0], it1 & 1);
+#pragma unroll 1
+      for (uint32_t ht = 0; ht < 4; ++ht) {
+        const uint32_t h = ht >> 1, t = ht & 1;
+        if (k > 0 && (int)t < nt) {
+          TC_WAIT(sh.p_full[t][h], (t ? it1 : it) & 1);
+          if (ht == 0) TC_WAIT(sh.v_full[(j - 1) & 1], ((j - 1) >> 1) & 1);
           tc::fence_after();
-          values(C1{}, C0{}, (j - 1) & 1, k == 1);
+          if (elect_one()) {
+            const uint64_t vd = dv + ((j - 1) & 1) * (kBytes >> 4) + h * (64 * 128 >> 4);
+            const uint32_t o_at = tmem + 256 + t * 128, p_at = tmem + t * 128 + h * 64;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              mma_ts(o_at, p_at + q * 8, vd + q * (2048 >> 4), id_o, q > 0 ? 1u : (k > 1 || h > 0 ? 1u : 0u));
+            tc::mma_commit(&sh.o_done[t][h]);
+          }
+          __syncwarp();
         }
-        if (!end) scores(C1{}, C0{}, j & 1);
+        if (ht == 0) {
+          TC_WAIT(sh.step_full[n % kRing], (n / kRing) & 1);
+          end = sh.step[n % kRing].end;
+          if (!end) {
+            nt = sh.step[n % kRing].row_tiles;
+            TC_WAIT(sh.k_full[j & 1], (j >> 1) & 1);
+            tc::fence_after();
+          }
+        }
+        if (!end && (int)t < nt) {
+          if (elect_one()) {
+            const uint64_t kd = dk + (j & 1) * (kBytes >> 4) + h * (64 * 128 >> 4), qd = dq + t * (kBytes >> 4);
+            const uint32_t s_at = tmem + t * 128 + h * 64;
+#pragma unroll
+            for (int q = 0; q < D / 16; ++q) {
+              const int o = (q >> 2) * (16384 >> 4) + (q & 3) * 2;
+              tc::mma_bf16(s_at, qd + o, kd + o, id_s, q > 0);
+            }
+            tc::mma_commit(&sh.s_full[t][h]);
+          }
+          __syncwarp();
+        }
       }
       if (k > 0) {
-        TC_WAIT(sh.p_full[0][1], it0 & 1);
-        ++it0;
-        tc::fence_after();
-        values(C0{}, C1{}, (j - 1) & 1, false);
-      }
-      if (!end) scores(C0{}, C1{}, j & 1);
-      if (two) {
-        if (k > 0) {
-          TC_WAIT(sh.p_full[1][1], it1 & 1);
-          ++it1;
-          tc::fence_after();
-          values(C1{}, C1{}, (j - 1) & 1, false);
-        }
-        if (!end) scores(C1{}, C1{}, j & 1);
+        ++it;
+        it1 += nt == 2;
       }
       if (elect_one()) {
         if (k > 0) tc::mma_commit(&sh.v_free[(j - 1) & 1]);
@@ -634,7 +610,7 @@ __device__ __forceinline__ float load_queries(const AttendParams& p, const Walk&
     const int r = (first & 127) + i * RPI + sub;
     return mine + r * 128 + (((c & 7) ^ (r & 7)) << 4);
   };
-#pragma unroll 1
+#pragma unroll 2
   for (int i = 0; i < N; ++i) {
     const int at = x.rt * kR + first + i * RPI + sub, tok = div_group(p, at);
     const uint16_t* src = at < rows ? p.q + (x.s.row0 + tok) * p.q_row + (int64_t)(x.h * p.G + at - tok * p.G) * D + c * 8 : p.q;
@@ -643,7 +619,7 @@ __device__ __forceinline__ float load_queries(const AttendParams& p, const Walk&
   cp_async_commit();
   cp_async_wait<0>();
   float scale = 0.f;
-#pragma unroll 1
+#pragma unroll 4
   for (int i = 0; i < N; ++i) {
     uint4* at = reinterpret_cast<uint4*>(piece(i));
     const uint4 v = *at;
