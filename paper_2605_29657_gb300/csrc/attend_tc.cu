@@ -378,12 +378,12 @@ __device__ __forceinline__ void plan_role(const AttendParams& p, Shared& sh, con
     Tile cur, nxt, far;
     int groups = 0;     // groups of the present tile still to be taken one by one
     uint32_t whole[4];  // the present tile's mask, while it is taken so
-    f.look(far, x.ta);
-    nxt = far;
-    f.settle(nxt);
-    cur = nxt;
-    cur.tile = x.ta - 1;
-    f.look(far, min(x.ta + 1, end));
+    cur.tile = x.ta - 3;  // (two turns of the stages bring the first tile to nxt)
+    cur.seen[0] = cur.seen[1] = cur.seen[2] = cur.seen[3] = 0;
+    nxt = far = cur;
+    nxt.tile = x.ta - 2;
+    far.tile = x.ta - 1;
+    far.page = 0;
     for (bool none = true;; none = false) {
       // the next step (tiles without a seen key are passed over)
       int only = -1;  // the group that is taken alone
@@ -392,14 +392,13 @@ __device__ __forceinline__ void plan_role(const AttendParams& p, Shared& sh, con
         groups &= groups - 1;
       } else {
         bool found = false;
+#pragma unroll 1
         while (!found && cur.tile < end) {
           cur = nxt;
-          if (cur.tile < end) {
-            nxt = far;
-            f.settle(nxt);
-            f.look(far, min(nxt.tile + 1, end));
-          }
-          found = (cur.seen[0] | cur.seen[1] | cur.seen[2] | cur.seen[3]) != 0;
+          nxt = far;
+          f.settle(nxt);
+          f.look(far, min(nxt.tile + 1, end));
+          found = cur.tile >= x.ta && (cur.seen[0] | cur.seen[1] | cur.seen[2] | cur.seen[3]) != 0;
         }
         if (!found && !none) break;  // (where nothing is seen, one step of hidden keys gives the rows their zeros)
       }
@@ -875,7 +874,7 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
             for (int k = 0; k < n; ++k)
               wt[k * 32 + lane] = there ? fast_exp2(__ldcg(&p.part_ml[part(c0 + k, lane)]).x - base) * inv : 0.f;
             __syncwarp();
-#pragma unroll 2
+#pragma unroll 1
             for (int rr = 0; rr < rows; ++rr) {
               constexpr int V = D / 32;  // values a lane holds of a row
               float acc[V];
