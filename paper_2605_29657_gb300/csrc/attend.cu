@@ -155,6 +155,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
   if (TMA && threadIdx.x < kWarps * 4) mbar_init(&sh_bar[0][0] + threadIdx.x, 1);
   if (TMA) fence_mbar_init();
   for (int d = threadIdx.x; d < D; d += kThreads) sh_nan[d] = 0x7fffffff;
+  pdl_wait();
   Line line;
   const LinePart part0 = attend_line<R, kTile, kOver, kThreads>(p, kOver + kWarps, kAttendCtas, kShared, sh, line);
   // (every CTA takes part in the last count below)
@@ -656,9 +657,7 @@ int launch(const AttendParams& p, const CUtensorMap& mk, const CUtensorMap& mv, 
     ready.fetch_or(uint64_t(1) << dev, std::memory_order_release);
   }
   const int grid = std::min(cache_sms() * (NQ == 1 ? 3 : 2), kAttendCtas);
-  attend_rows_kernel<D, NQ, TMA><<<grid, kThreads, smem, st>>>(p, mk, mv);
-  count_launch();
-  return cudaGetLastError() == cudaSuccess ? OCCAM_OK : OCCAM_ERR_CUDA;
+  return launch_after(attend_rows_kernel<D, NQ, TMA>, dim3((unsigned)grid), kThreads, smem, st, p, mk, mv) && cudaGetLastError() == cudaSuccess ? OCCAM_OK : OCCAM_ERR_CUDA;
 }
 
 template <int D, int NQ>

@@ -107,15 +107,21 @@ __device__ __forceinline__ int64_t head_units(const AttendParams& p, const SeqIn
 }
 
 // The cuts: stretch c < first begins at c head / first, the others share the rest.
+// (Units are 31-bit numbers: 2^31 key tiles are hours of work.)
 struct Line {
-  int64_t units, head;
+  int units, head;
   int first, total;  // stretches
+  int q0, r0, q1, r1;  // head = q0 first + r0, the rest = q1 (total - first) + r1
 };
-__device__ __forceinline__ int64_t stretch_begin(const Line& l, int c) {
-  return c <= l.first ? l.head * c / l.first : l.head + (l.units - l.head) * (c - l.first) / (l.total - l.first);
+__device__ __forceinline__ int stretch_begin(const Line& l, int c) {
+  if (c <= l.first) return l.q0 * c + l.r0 * c / l.first;
+  const int d = c - l.first;
+  return l.head + l.q1 * d + l.r1 * d / (l.total - l.first);
 }
-static __device__ __noinline__ int stretch_of(Line l, int64_t u) {
-  int c = u < l.head ? (int)(u * l.first / l.head) : l.first + (int)((u - l.head) * (l.total - l.first) / (l.units - l.head));
+static __device__ __noinline__ int stretch_of(const Line& l, int u) {
+  int c = u < l.head ? (int)((float)u * (float)l.first / (float)l.head)
+                     : l.first + (int)((float)(u - l.head) * (float)(l.total - l.first) / (float)(l.units - l.head));
+  c = min(max(c, 0), l.total - 1);
   while (c + 1 < l.total && stretch_begin(l, c + 1) <= u) ++c;
   while (c > 0 && stretch_begin(l, c) > u) --c;
   return c;
@@ -123,13 +129,13 @@ static __device__ __noinline__ int stretch_of(Line l, int64_t u) {
 
 // A stretch [u0, u1) and the item its first unit is in (in_item: u0's place in it).
 struct Stretch {
-  int64_t u0, u1;
+  int u0, u1;
   int index, seq, head, row_tile, in_item;
 };
 
 // The line's length and this thread's part of it (its sequences i0 .. i1-1 begin at `at`).
 struct LinePart {
-  int64_t at, mine;
+  int at, mine;
   int i0, i1;
 };
 // Block-wide (NT threads, all of them); sh: NT / 32 + 4 int64 of shared memory.
@@ -143,9 +149,9 @@ __device__ __forceinline__ LinePart attend_line(const AttendParams& p, int min_u
   LinePart w;
   w.i0 = min(t * per, p.n);
   w.i1 = min(w.i0 + per, p.n);
-  w.mine = 0;
-  for (int i = w.i0; i < w.i1; ++i) w.mine += p.c.heads * head_units<R, KT, OVER>(p, attend_seq(p, i));
-  int64_t incl = w.mine;
+  int64_t mine = 0;
+  for (int i = w.i0; i < w.i1; ++i) mine += p.c.heads * head_units<R, KT, OVER>(p, attend_seq(p, i));
+  int64_t incl = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int64_t x = __shfl_up_sync(0xffffffffu, incl, o);
@@ -159,14 +165,24 @@ __device__ __forceinline__ LinePart attend_line(const AttendParams& p, int min_u
     if (k < warp) before += sh[k];
     total += sh[k];
   }
-  w.at = before + incl - w.mine;
-  l.units = total;
-  const int64_t most = total / min_units;
-  l.first = (int)min((int64_t)gridDim.x, most > 0 ? most : 1);
-  l.total = (int)min(min((int64_t)most_stretches, (int64_t)3 * l.first), most > 0 ? most : 1);
+  if (total > 0x7fff0000) {
+    set_status(p.c.status, OCCAM_ERR_UNSUPPORTED);
+    total = 0;
+  }
+  w.at = (int)(before + incl - mine);
+  w.mine = (int)mine;
+  l.units = (int)total;
+  const int most = max(l.units / min_units, 1);
+  l.first = min((int)gridDim.x, most);
+  l.total = min(min(most_stretches, 3 * l.first), most);
   // a few stretches in all: none are held back
   if (l.total < 2 * l.first || shared == 0) l.total = l.first;
-  l.head = l.total > l.first ? total - total * shared / 16 : total;
+  l.head = l.total > l.first ? (int)(total - total * shared / 16) : l.units;
+  l.q0 = l.head / l.first;
+  l.r0 = l.head - l.q0 * l.first;
+  const int d = max(l.total - l.first, 1);
+  l.q1 = (l.units - l.head) / d;
+  l.r1 = l.units - l.head - l.q1 * d;
   return w;
 }
 // Stretch c, to all threads of the block.
@@ -176,14 +192,14 @@ __device__ __forceinline__ void attend_find(const AttendParams& p, const Line& l
   w.index = c;
   w.u0 = stretch_begin(l, c);
   w.u1 = stretch_begin(l, c + 1);
-  int64_t at = part.at;
-  if (w.u0 >= at && w.u0 < at + part.mine) {
+  int at = part.at;
+  if (w.u0 >= at && w.u0 - at < part.mine) {
     for (int i = part.i0; i < part.i1; ++i) {
       const SeqInfo s = attend_seq(p, i);
-      const int64_t hu = head_units<R, KT, OVER>(p, s);
+      const int hu = (int)head_units<R, KT, OVER>(p, s);
       if (w.u0 < at + p.c.heads * hu) {
-        const int64_t off = w.u0 - at;
-        const int64_t h = off / hu, in_head = off - h * hu;
+        const int off = w.u0 - at;
+        const int h = off / hu, in_head = off - h * hu;
         int lo = 0, hi = (s.rows * p.G + R - 1) / R;  // the last row tile that begins at or before in_head
         while (hi - lo > 1) {
           const int mid = (lo + hi) >> 1;
@@ -192,7 +208,7 @@ __device__ __forceinline__ void attend_find(const AttendParams& p, const Line& l
         sh[NWARP] = i;
         sh[NWARP + 1] = h;
         sh[NWARP + 2] = lo;
-        sh[NWARP + 3] = in_head - (lo ? units_before<R, KT, OVER>(p, s, lo) : 0);
+        sh[NWARP + 3] = in_head - (lo ? (int)units_before<R, KT, OVER>(p, s, lo) : 0);
         break;
       }
       at += p.c.heads * hu;
@@ -208,7 +224,7 @@ __device__ __forceinline__ void attend_find(const AttendParams& p, const Line& l
 // The segment (an item's key tiles ta .. tb-1, those in the CTA's stretch) a role is at.
 struct Walk {
   SeqInfo s;
-  int64_t item;  // the item's first unit
+  int item;  // the item's first unit
   int i, h, rt, tiles, ta, tb;
 };
 // False if no tile of the item lies in the stretch.
@@ -216,7 +232,7 @@ template <int R, int KT, int OVER, class W>
 __device__ __forceinline__ bool walk_set(const AttendParams& p, const W& w, Walk& x, int in_item) {
   x.tiles = key_tiles<R, KT>(p, x.s, x.rt);
   x.ta = max(in_item - OVER, 0);
-  x.tb = (int)max(min(w.u1 - x.item - OVER, (int64_t)x.tiles), (int64_t)0);
+  x.tb = max(min((int)w.u1 - x.item - OVER, x.tiles), 0);
   return x.ta < x.tb;
 }
 // The next segment; false at the end of the stretch.

@@ -62,7 +62,7 @@ struct Shared {
       step_free[kRing], raw_full[2], raw_free[2], meet, drain;
   Step step[kRing];
   Line line;
-  volatile int64_t u0, u1;   // the CTA's stretch (see Stretch)
+  volatile int u0, u1;   // the CTA's stretch (see Stretch)
   volatile int seq, head, row_tile, in_item;
   uint32_t tmem;
   int stop;            // a wait ran out
@@ -940,6 +940,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(AttendParams p, 
   Shared& sh = *reinterpret_cast<Shared*>(smem + 7 * kBytes);
   int64_t* scan = reinterpret_cast<int64_t*>(&sh.nan_first[0][0]);
   const int warp = threadIdx.x >> 5;
+  pdl_wait();
   Line line;
   const LinePart part = attend_line<kR, kK, kOver, kThreads>(p, kOver + 1, kAttendTcCtas, 0, scan, line);
   if (line.units == 0 || (int)blockIdx.x >= line.first) return;
@@ -1038,9 +1039,8 @@ int launch(const AttendParams& p, const CUtensorMap& mk, const CUtensorMap& mv, 
   const int smem = 7 * kK * D * 2 + kSharedBytes;
   const int rc = prepare<D, BF16>(smem);
   if (rc != OCCAM_OK) return rc;
-  attend_tc_kernel<D, BF16><<<std::min(cache_sms(), kAttendTcCtas), kThreads, smem, st>>>(p, mk, mv);
-  count_launch();
-  return cudaGetLastError() == cudaSuccess ? OCCAM_OK : OCCAM_ERR_CUDA;
+  const dim3 grid((unsigned)std::min(cache_sms(), kAttendTcCtas));
+  return launch_after(attend_tc_kernel<D, BF16>, grid, kThreads, smem, st, p, mk, mv) && cudaGetLastError() == cudaSuccess ? OCCAM_OK : OCCAM_ERR_CUDA;
 }
 
 }  // namespace

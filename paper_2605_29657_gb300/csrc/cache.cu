@@ -4,7 +4,7 @@
 // handed out in call order by prefix sums, so page indices do not depend on
 // timing. The codes move in grid-wide kernels behind it.
 #include <algorithm>
-#include <cstring>
+#include <utility>
 
 #include "cache.cuh"
 #include "nvtx.cuh"
@@ -31,7 +31,9 @@ constexpr int kPlanThreads = 1024;
 // ---------------------------------------------------------------- append
 // One CTA per (touched page, head, K or V): the new rows' values of the block
 // stay in registers between the block's maximum and the rounding, so they are
-// read once. Bound by HBM (2 bytes read and 1 written a value).
+// read once. Bound by HBM (2 bytes read and 1 written a value). Four heads a CTA with
+// the next head's rows under way measured slower (20 k rows: 156 us, not 121):
+// fewer CTAs fit an SM.
 struct AppendParams {
   CacheDev c;
   int layer, n;
@@ -95,19 +97,18 @@ __device__ __forceinline__ float amax8(uint4 r) {
   return BF16 ? __uint_as_float(m << 16) : __half2float(__ushort_as_half((unsigned short)m));
 }
 
-// MAXV: 8-value vectors a thread holds (128 threads; page_tokens * D / 8 / 128 at most)
+// MAXV: 8-value vectors a thread holds of a block (128 threads; page_tokens * D / 8 / 128 at most).
+// grid: x over (head, K or V), y and z over slots.
 template <bool BF16, int D, int MAXV>
 __global__ void __launch_bounds__(128) append_kernel(AppendParams p) {
-  __shared__ float red[4];
+  __shared__ float r[4];
+  pdl_wait();
   const int T = p.c.T, H = p.c.heads;
-  const int64_t item = blockIdx.x;
-  const int kv = (int)(item & 1);
-  const int64_t rest = item >> 1;
-  const int h = (int)(rest % H);
-  const int64_t w = rest / H;
+  const int kv = blockIdx.x & 1, h = (int)(blockIdx.x >> 1);
+  const int64_t w = (int64_t)blockIdx.z * gridDim.y + blockIdx.y;
   const int i = slot_sequence(p.row_off, p.n, p.c.log2T, w);
   const int64_t r0 = p.row_off[i], r1 = p.row_off[i + 1];
-  const int local = (int)(w - ((r0 >> p.c.log2T) + 2 * (int64_t)i));
+  const int64_t local = w - ((r0 >> p.c.log2T) + 2 * (int64_t)i);
   const int seq = p.seqs[i];
   int len = -1;
   if ((unsigned)seq < (unsigned)p.c.max_seqs) len = p.c.length[seq];
@@ -119,7 +120,9 @@ __global__ void __launch_bounds__(128) append_kernel(AppendParams p) {
     return;
   }
   const int start = len - (int)(r1 - r0);  // position of row r0
-  const int slot = (start >> p.c.log2T) + local;
+  if (local > (len >> p.c.log2T)) return;  // (a slot past the rows)
+  const int slot = (start >> p.c.log2T) + (int)local;
+  if (slot >= p.c.max_pages) return;
   const int t0 = max(start - slot * T, 0), t1 = min(len - slot * T, T);  // new tokens of this page
   if (t1 <= t0) return;
   const int page = p.c.table[(int64_t)seq * p.c.max_pages + slot];
@@ -127,38 +130,34 @@ __global__ void __launch_bounds__(128) append_kernel(AppendParams p) {
     if (threadIdx.x == 0) set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
     return;
   }
-  const int64_t block = ((int64_t)p.layer * p.c.pages + page) * H + h;
-  uint8_t* codes = (kv ? p.c.v : p.c.k) + block * T * D;
-  float* scale = (kv ? p.c.v_scale : p.c.k_scale) + block;
+  const int64_t block = ((int64_t)p.layer * p.c.pages + page) * H;
   const int64_t ld = kv ? p.v_row : p.k_row;
-  const uint16_t* src = static_cast<const uint16_t*>(kv ? p.v : p.k) + (r0 + (int64_t)slot * T - start) * ld + (int64_t)h * D;
   constexpr int vpr = D / 8;  // vectors of a row
-  const int nv = (t1 - t0) * vpr;
+  const int nv = (t1 - t0) * vpr, tv = threadIdx.x / vpr, c = threadIdx.x % vpr;
+  const uint16_t* src = static_cast<const uint16_t*>(kv ? p.v : p.k) + (r0 + (int64_t)slot * T - start + t0 + tv) * ld + c * 8;
+  const int64_t step = 128 / vpr * ld;
   uint4 x[MAXV];
+#pragma unroll
+  for (int q = 0; q < MAXV; ++q)
+    if (q * 128 + (int)threadIdx.x < nv) x[q] = ldg_stream(src + q * step + h * D);
+  uint8_t* codes = (kv ? p.c.v : p.c.k) + (block + h) * T * D;
+  float* scale = (kv ? p.c.v_scale : p.c.k_scale) + block + h;
   float amax = 0.f;
 #pragma unroll
-  for (int q = 0; q < MAXV; ++q) {
-    const int e = q * 128 + threadIdx.x;
-    if (e < nv) x[q] = ldg_stream(src + (int64_t)(t0 + e / vpr) * ld + (e % vpr) * 8);
-  }
-#pragma unroll
-  for (int q = 0; q < MAXV; ++q) {
-    const int e = q * 128 + threadIdx.x;
-    if (e < nv) amax = fmaxf(amax, amax8<BF16>(x[q]));
-  }
+  for (int q = 0; q < MAXV; ++q)
+    if (q * 128 + (int)threadIdx.x < nv) amax = fmaxf(amax, amax8<BF16>(x[q]));
   amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = amax;
+  if ((threadIdx.x & 31) == 0) r[threadIdx.x >> 5] = amax;
   const float was = t0 > 0 ? *scale : 0.f;
-  __syncthreads();
-  amax = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  const float need = block_scale(amax);
+  __syncthreads();  // (and every thread has `was`)
+  const float need = block_scale(fmaxf(fmaxf(r[0], r[1]), fmaxf(r[2], r[3])));
   const float now = was > need ? was : need;  // older tokens keep at least their scale
   if (t0 > 0 && now > was) {
     // the held codes, rounded again to the larger scale
     const float ratio = was / now;
     for (int e = threadIdx.x; e < t0 * D / 16; e += 128) {
-      uint4 r = reinterpret_cast<uint4*>(codes)[e];
-      uint32_t* rw = reinterpret_cast<uint32_t*>(&r);
+      uint4 y = reinterpret_cast<uint4*>(codes)[e];
+      uint32_t* rw = reinterpret_cast<uint32_t*>(&y);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         float f[4];
@@ -167,27 +166,22 @@ __global__ void __launch_bounds__(128) append_kernel(AppendParams p) {
         for (int m = 0; m < 4; ++m) f[m] *= ratio;
         rw[j] = f32_codes4(f);
       }
-      reinterpret_cast<uint4*>(codes)[e] = r;
+      reinterpret_cast<uint4*>(codes)[e] = y;
     }
   }
   const bool exact = is_pow2(now);
   const float inv = exact ? 1.f / now : 0.f;
 #pragma unroll
   for (int q = 0; q < MAXV; ++q) {
-    const int e = q * 128 + threadIdx.x;
-    if (e < nv) {
+    if (q * 128 + (int)threadIdx.x < nv) {
       float f[8];
       unpack8<BF16>(x[q], f);
 #pragma unroll
       for (int j = 0; j < 8; ++j) f[j] = exact ? f[j] * inv : f[j] / now;
       const float lo[4] = {f[0], f[1], f[2], f[3]}, hi[4] = {f[4], f[5], f[6], f[7]};
-      uint2 out;
-      out.x = f32_codes4(lo);
-      out.y = f32_codes4(hi);
-      *reinterpret_cast<uint2*>(codes + (int64_t)(t0 + e / vpr) * D + (e % vpr) * 8) = out;
+      *reinterpret_cast<uint2*>(codes + (t0 + tv + q * (128 / vpr)) * D + c * 8) = make_uint2(f32_codes4(lo), f32_codes4(hi));
     }
   }
-  __syncthreads();  // `was` has been read by every thread
   if (threadIdx.x == 0) *scale = now;
 }
 
@@ -264,6 +258,7 @@ __device__ __forceinline__ int pages_of(int tokens, const CacheDev& c) { return 
 
 __global__ void __launch_bounds__(kPlanThreads) extend_kernel(PlanParams p) {
   __shared__ int tmp[33];
+  pdl_wait();
   const CacheDev& c = p.c;
   const bool fine = mark_slots(c, p.a, p.n, p.marks);
   int bad = 0, full = 0;
@@ -324,6 +319,7 @@ __global__ void __launch_bounds__(kPlanThreads) extend_kernel(PlanParams p) {
 
 __global__ void __launch_bounds__(kPlanThreads) fork_kernel(PlanParams p) {
   __shared__ int tmp[33];
+  pdl_wait();
   const CacheDev& c = p.c;
   const bool fine = mark_slots(c, p.b, p.n, p.marks);
   int bad = 0;
@@ -397,6 +393,7 @@ __global__ void __launch_bounds__(kPlanThreads) fork_kernel(PlanParams p) {
 // Copies the pages fork_kernel listed: grid (pairs, layers, 2 * chunks), 16 KB a CTA.
 constexpr int kCopyChunk = 16384;
 __global__ void __launch_bounds__(256) copy_pages_kernel(CacheDev c, const int2* pairs, int page_bytes) {
+  pdl_wait();
   const int2 ft = pairs[blockIdx.x];
   if (ft.x < 0) return;
   const int layer = blockIdx.y, kv = blockIdx.z & 1, chunk = blockIdx.z >> 1;
@@ -419,6 +416,7 @@ __global__ void __launch_bounds__(256) copy_pages_kernel(CacheDev c, const int2*
 }
 
 __global__ void __launch_bounds__(256) release_kernel(CacheDev c, int n, const int32_t* seqs) {
+  pdl_wait();
   const int i = blockIdx.y;
   const int s = seqs[i];
   if ((unsigned)s >= (unsigned)c.max_seqs) {
@@ -461,6 +459,7 @@ struct CountParams {
 __global__ void __launch_bounds__(1024) compact_count_kernel(CountParams p) {
   __shared__ int tmp[33];
   __shared__ int first;
+  pdl_wait();
   const int i = blockIdx.x;
   const int s = p.seqs[i];
   const int64_t k0 = p.keep_off[i], k1 = p.keep_off[i + 1];
@@ -495,6 +494,7 @@ __global__ void __launch_bounds__(1024) compact_count_kernel(CountParams p) {
 // New page tables: head[i] = index of sequence i's first new page in free_list.
 __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(PlanParams p) {
   __shared__ int tmp[33];
+  pdl_wait();
   const CacheDev& c = p.c;
   const bool fine = mark_slots(c, p.a, p.n, p.marks);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -557,6 +557,22 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(PlanParams p
   unmark_slots(c, p.a, p.n, p.marks);
 }
 
+// the largest |code| of 16 (NaN codes passed over): magnitudes order as integers
+__device__ __forceinline__ float codes_amax(uint4 v) {
+  const uint32_t w[4] = {v.x & 0x7f7f7f7fu, v.y & 0x7f7f7f7fu, v.z & 0x7f7f7f7fu, v.w & 0x7f7f7f7fu};
+  uint32_t m = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t nan = __vcmpeq4(w[k], 0x7f7f7f7fu);
+    m = __vmaxu4(m, w[k] & ~nan);
+  }
+  m = __vmaxu4(m, m >> 16);
+  m = max(m & 0xffu, m >> 8 & 0xffu);
+  float f[4];
+  codes4_f32(m, f);
+  return f[0];
+}
+
 struct MoveParams {
   CacheDev c;
   int n, layer0, layers;
@@ -580,18 +596,13 @@ template <int D, int MAXV>
 __global__ void __launch_bounds__(128) compact_move_kernel(MoveParams p) {
   __shared__ int2 src[128];  // page and slot of each token
   __shared__ float red[2][4];
+  pdl_wait();
   constexpr int vpr = D / 16;
   const int T = p.c.T, H = p.c.heads;
-  const int hg = (H + kMoveHeads - 1) / kMoveHeads;
-  const int64_t items = (int64_t)p.head[p.n] * p.layers * 2 * hg;
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    int64_t rest = item;
-    const int g = (int)(rest % hg);
-    rest /= hg;
-    const int kv = (int)(rest & 1);
-    rest >>= 1;
-    const int layer = p.layer0 + (int)(rest % p.layers);
-    const int fresh = (int)(rest / p.layers);
+  const int hg = (H + kMoveHeads - 1) / kMoveHeads, per_page = p.layers * 2 * hg;
+  const int pages = p.head[p.n];
+  const int tv = threadIdx.x / vpr, c = threadIdx.x % vpr;
+  for (int fresh = blockIdx.y; fresh < pages; fresh += gridDim.y) {
     // the sequence whose new pages include this one (head is ascending)
     int lo = 0, hi = p.n;
     while (hi - lo > 1) {
@@ -600,7 +611,7 @@ __global__ void __launch_bounds__(128) compact_move_kernel(MoveParams p) {
     }
     const int i = lo;
     const int first = (p.lead[i] + fresh - p.head[i]) * T;  // new position of the page's first token
-    const int tokens = min(p.count[i] - first, T);
+    const int tokens = min(p.count[i] - first, T), nv = tokens * vpr;
     __syncthreads();
     if ((int)threadIdx.x < tokens) {
       // kept flagged tokens come from the list, tokens past the flags in order
@@ -610,68 +621,68 @@ __global__ void __launch_bounds__(128) compact_move_kernel(MoveParams p) {
       src[threadIdx.x] = make_int2(p.old_table[(int64_t)i * p.c.max_pages + (pos >> p.c.log2T)], pos & (T - 1));
     }
     __syncthreads();
-    const uint8_t* from = kv ? p.c.v : p.c.k;
-    uint8_t* to = kv ? p.c.v : p.c.k;
-    float* sc = kv ? p.c.v_scale : p.c.k_scale;
-    const int64_t layer_page = (int64_t)layer * p.c.pages;
-    const int64_t new_block = (layer_page + p.free_list[fresh]) * H;
-    const int nv = tokens * vpr;
-    for (int h = g * kMoveHeads; h < min((g + 1) * kMoveHeads, H); ++h) {
-      uint4 x[MAXV];
-      float s[MAXV];
-      float amax = 0.f;
+    const int to_page = p.free_list[fresh];
+    for (int item = blockIdx.x; item < per_page; item += gridDim.x) {
+      const int g = item % hg, kv = item / hg & 1, layer = p.layer0 + item / hg / 2;
+      const int h0 = g * kMoveHeads, h1 = min(h0 + kMoveHeads, H);
+      uint8_t* codes = kv ? p.c.v : p.c.k;
+      float* sc = kv ? p.c.v_scale : p.c.k_scale;
+      const int64_t layer_page = (int64_t)layer * p.c.pages, new_block = (layer_page + to_page) * H;
+      // this thread's vectors: block of head 0, and the place in it
+      int64_t from[MAXV];
+      int at[MAXV];
 #pragma unroll
       for (int q = 0; q < MAXV; ++q) {
-        const int e = q * 128 + threadIdx.x;
-        if (e < nv) {
-          const int2 ps = src[e / vpr];
-          const int64_t block = (layer_page + ps.x) * H + h;
-          x[q] = ldg_stream(from + (block * T + ps.y) * D + (e % vpr) * 16);
-          s[q] = sc[block];
-        }
+        const int2 ps = src[min(tv + q * (128 / vpr), 127)];
+        from[q] = (layer_page + ps.x) * H;
+        at[q] = ps.y * D + c * 16;
       }
+      auto load = [&](uint4 (&x)[MAXV], float (&s)[MAXV], int h) {
 #pragma unroll
-      for (int q = 0; q < MAXV; ++q) {
-        const int e = q * 128 + threadIdx.x;
-        if (e < nv) {
-          const uint32_t* w = reinterpret_cast<const uint32_t*>(&x[q]);
-          float m = 0.f;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            float f[4];
-            codes4_f32(w[j], f);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) m = fmaxf(m, fabsf(f[k]));  // a NaN code is passed over
+        for (int q = 0; q < MAXV; ++q)
+          if (q * 128 + (int)threadIdx.x < nv) {
+            x[q] = ldg_stream(codes + (from[q] + h) * T * D + at[q]);
+            s[q] = sc[from[q] + h];
           }
-          amax = fmaxf(amax, finite_abs(m * s[q]));
-        }
-      }
-      amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
-      if ((threadIdx.x & 31) == 0) red[h & 1][threadIdx.x >> 5] = amax;
-      __syncthreads();
-      const float* r = red[h & 1];
-      const float now = block_scale(fmaxf(fmaxf(r[0], r[1]), fmaxf(r[2], r[3])));
-      const float inv = 1.f / now;  // exact: now is a power of two
-      uint8_t* out = to + (new_block + h) * T * D;
+      };
+      auto finish = [&](uint4 (&x)[MAXV], const float (&s)[MAXV], int h) {
+        float amax = 0.f;
 #pragma unroll
-      for (int q = 0; q < MAXV; ++q) {
-        const int e = q * 128 + threadIdx.x;
-        if (e < nv) {
-          uint32_t* w = reinterpret_cast<uint32_t*>(&x[q]);
-          if (s[q] != now) {
+        for (int q = 0; q < MAXV; ++q)
+          if (q * 128 + (int)threadIdx.x < nv) amax = fmaxf(amax, finite_abs(codes_amax(x[q]) * s[q]));
+        amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
+        float* r = red[h & 1];
+        if ((threadIdx.x & 31) == 0) r[threadIdx.x >> 5] = amax;
+        __syncthreads();
+        const float now = block_scale(fmaxf(fmaxf(r[0], r[1]), fmaxf(r[2], r[3])));
+        const float inv = 1.f / now;  // exact: now is a power of two
+        uint8_t* out = codes + (new_block + h) * T * D;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              float f[4];
-              codes4_f32(w[j], f);
+        for (int q = 0; q < MAXV; ++q) {
+          if (q * 128 + (int)threadIdx.x < nv) {
+            uint32_t* w = reinterpret_cast<uint32_t*>(&x[q]);
+            if (s[q] != now) {
 #pragma unroll
-              for (int k = 0; k < 4; ++k) f[k] = f[k] * s[q] * inv;
-              w[j] = f32_codes4(f);
+              for (int j = 0; j < 4; ++j) {
+                float f[4];
+                codes4_f32(w[j], f);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) f[k] = f[k] * s[q] * inv;
+                w[j] = f32_codes4(f);
+              }
             }
+            stg_stream(out + (q * 128 + threadIdx.x) * 16, x[q]);
           }
-          stg_stream(out + e * 16, x[q]);
         }
+        if (threadIdx.x == 0) sc[new_block + h] = now;
+      };
+      for (int h = h0; h < h1; ++h) {
+        uint4 x[MAXV];
+        float s[MAXV];
+        load(x, s, h);
+        finish(x, s, h);
       }
-      if (threadIdx.x == 0) sc[new_block + h] = now;
+      __syncthreads();  // (red: an odd number of heads meets the next item's first)
     }
   }
 }
@@ -693,30 +704,29 @@ PlanParams plan_params(const occam_cache* c, void* ws, const CacheWs& w, int n) 
 }
 
 template <bool BF16, int D>
-void launch_append(const AppendParams& p, unsigned grid, cudaStream_t st) {
+bool launch_append(AppendParams& p, cudaStream_t st) {
+  const int64_t slots = p.total_rows / p.c.T + 2 * (int64_t)p.n;
+  const unsigned y = (unsigned)std::min<int64_t>(slots, 65535);
+  const dim3 grid((unsigned)p.c.heads * 2, y, (unsigned)((slots + y - 1) / y));
   const int vecs = p.c.T * D / 8 / 128;
-  if (vecs <= 2)
-    append_kernel<BF16, D, 2><<<grid, 128, 0, st>>>(p);
-  else if (vecs == 4)
-    append_kernel<BF16, D, 4><<<grid, 128, 0, st>>>(p);
-  else if (vecs == 8)
-    append_kernel<BF16, D, 8><<<grid, 128, 0, st>>>(p);
-  else
-    append_kernel<BF16, D, 16><<<grid, 128, 0, st>>>(p);
+  if (vecs <= 2) return launch_after(append_kernel<BF16, D, 2>, grid, 128, 0, st, p);
+  if (vecs == 4) return launch_after(append_kernel<BF16, D, 4>, grid, 128, 0, st, p);
+  if (vecs == 8) return launch_after(append_kernel<BF16, D, 8>, grid, 128, 0, st, p);
+  return launch_after(append_kernel<BF16, D, 16>, grid, 128, 0, st, p);
 }
 
 template <int D>
-void launch_move(const MoveParams& m, cudaStream_t st) {
+bool launch_move(const MoveParams& m, cudaStream_t st) {
   const int vecs = m.c.T * D / 16 / 128;
-  const unsigned grid = (unsigned)cache_sms() * 12;
-  if (vecs <= 1)
-    compact_move_kernel<D, 1><<<grid, 128, 0, st>>>(m);
-  else if (vecs == 2)
-    compact_move_kernel<D, 2><<<grid, 128, 0, st>>>(m);
-  else if (vecs == 4)
-    compact_move_kernel<D, 4><<<grid, 128, 0, st>>>(m);
-  else
-    compact_move_kernel<D, 8><<<grid, 128, 0, st>>>(m);
+  // how many pages move is only known on the device: CTAs share them out, all of a page's work to
+  // neighbours
+  const int work = m.layers * 2 * ((m.c.heads + kMoveHeads - 1) / kMoveHeads);
+  const unsigned x = (unsigned)std::min(work, 65535), want = (unsigned)cache_sms() * 64;
+  const dim3 grid(x, std::max(1u, std::min(want / x, 65535u)));
+  if (vecs <= 1) return launch_after(compact_move_kernel<D, 1>, grid, 128, 0, st, m);
+  if (vecs == 2) return launch_after(compact_move_kernel<D, 2>, grid, 128, 0, st, m);
+  if (vecs == 4) return launch_after(compact_move_kernel<D, 4>, grid, 128, 0, st, m);
+  return launch_after(compact_move_kernel<D, 8>, grid, 128, 0, st, m);
 }
 
 }  // namespace
@@ -748,9 +758,7 @@ int occam_cache_extend(const occam_cache* cache, int32_t n, const int32_t* seqs,
   PlanParams p = plan_params(cache, workspace, w, n);
   p.a = seqs;
   p.b = counts;
-  extend_kernel<<<1, kPlanThreads, 0, reinterpret_cast<cudaStream_t>(stream)>>>(p);
-  count_launch();
-  return last_error();
+  return launch_after(extend_kernel, dim3(1), kPlanThreads, 0, reinterpret_cast<cudaStream_t>(stream), p) ? last_error() : OCCAM_ERR_CUDA;
 }
 
 int occam_cache_append(const occam_cache* cache, int32_t layer, int32_t dtype, int64_t total_rows, const void* k,
@@ -779,15 +787,11 @@ int occam_cache_append(const occam_cache* cache, int32_t layer, int32_t dtype, i
   p.v = v;
   p.seqs = seqs;
   p.row_off = row_off;
-  const int64_t grid = (total_rows / cache->page_tokens + 2 * (int64_t)n) * cache->heads * 2;
-  if (grid > 0x7fffffff) return OCCAM_ERR_UNSUPPORTED;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  if (cache->dim == 128)
-    dtype == OCCAM_BF16 ? launch_append<true, 128>(p, (unsigned)grid, st) : launch_append<false, 128>(p, (unsigned)grid, st);
-  else
-    dtype == OCCAM_BF16 ? launch_append<true, 64>(p, (unsigned)grid, st) : launch_append<false, 64>(p, (unsigned)grid, st);
-  count_launch();
-  return last_error();
+  const bool bf16 = dtype == OCCAM_BF16;
+  const bool ok = cache->dim == 128 ? (bf16 ? launch_append<true, 128>(p, st) : launch_append<false, 128>(p, st))
+                                    : (bf16 ? launch_append<true, 64>(p, st) : launch_append<false, 64>(p, st));
+  return ok ? last_error() : OCCAM_ERR_CUDA;
 }
 
 int occam_cache_fork(const occam_cache* cache, int32_t n, const int32_t* src, const int32_t* dst, void* workspace,
@@ -803,13 +807,11 @@ int occam_cache_fork(const occam_cache* cache, int32_t n, const int32_t* src, co
   PlanParams p = plan_params(cache, workspace, w, n);
   p.a = src;
   p.b = dst;
-  fork_kernel<<<1, kPlanThreads, 0, st>>>(p);
-  count_launch();
+  if (!launch_after(fork_kernel, dim3(1), kPlanThreads, 0, st, p)) return OCCAM_ERR_CUDA;
   const int page_bytes = cache->heads * cache->page_tokens * cache->dim;
   const int chunks = (page_bytes + kCopyChunk - 1) / kCopyChunk;
-  copy_pages_kernel<<<dim3((unsigned)n, (unsigned)cache->layers, (unsigned)(2 * chunks)), 256, 0, st>>>(p.c, p.new_pages, page_bytes);
-  count_launch();
-  return last_error();
+  const dim3 grid((unsigned)n, (unsigned)cache->layers, (unsigned)(2 * chunks));
+  return launch_after(copy_pages_kernel, grid, 256, 0, st, p.c, p.new_pages, page_bytes) ? last_error() : OCCAM_ERR_CUDA;
 }
 
 int occam_cache_compact(const occam_cache* cache, int32_t layer_begin, int32_t layer_end, int32_t n,
@@ -837,10 +839,9 @@ int occam_cache_compact(const occam_cache* cache, int32_t layer_begin, int32_t l
   q.lead = p.lead;
   q.info = p.new_pages;
   q.list = ws_at<int32_t>(workspace, w.list);
-  compact_count_kernel<<<n, 1024, 0, st>>>(q);
-  count_launch();
-  compact_plan_kernel<<<1, kPlanThreads, 0, st>>>(p);
-  count_launch();
+  if (!launch_after(compact_count_kernel, dim3((unsigned)n), 1024, 0, st, q) ||
+      !launch_after(compact_plan_kernel, dim3(1), kPlanThreads, 0, st, p))
+    return OCCAM_ERR_CUDA;
   if (layer_end > layer_begin) {
     MoveParams m{};
     m.c = p.c;
@@ -855,11 +856,7 @@ int occam_cache_compact(const occam_cache* cache, int32_t layer_begin, int32_t l
     m.info = p.new_pages;
     m.list = q.list;
     m.keep_off = keep_off;
-    if (cache->dim == 128)
-      launch_move<128>(m, st);
-    else
-      launch_move<64>(m, st);
-    count_launch();
+    if (!(cache->dim == 128 ? launch_move<128>(m, st) : launch_move<64>(m, st))) return OCCAM_ERR_CUDA;
   }
   return last_error();
 }
@@ -873,10 +870,10 @@ int occam_cache_release(const occam_cache* cache, int32_t n, const int32_t* seqs
   CacheWs w;
   OCCAM_TRY(check_cache_ws(cache, 0, workspace, workspace_bytes, &w));
   if (n == 0) return OCCAM_OK;
-  release_kernel<<<dim3((unsigned)((cache->max_pages + 255) / 256), (unsigned)n), 256, 0,
-                   reinterpret_cast<cudaStream_t>(stream)>>>(cache_dev(cache, workspace, w), n, seqs);
-  count_launch();
-  return last_error();
+  const dim3 grid((unsigned)((cache->max_pages + 255) / 256), (unsigned)n);
+  return launch_after(release_kernel, grid, 256, 0, reinterpret_cast<cudaStream_t>(stream), cache_dev(cache, workspace, w), n, seqs)
+             ? last_error()
+             : OCCAM_ERR_CUDA;
 }
 
 }  // extern "C"

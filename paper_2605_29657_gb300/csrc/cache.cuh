@@ -4,6 +4,8 @@
 
 #include <cuda_fp16.h>
 
+#include <utility>
+
 #include "common.cuh"
 #include "validate.cuh"
 
@@ -78,6 +80,24 @@ T* ws_at(void* ws, size_t off) {
 
 // SMs of the current device
 int cache_sms();
+
+// Launches `kern` so that its start overlaps the end of the kernel before it in the stream; the
+// kernel itself waits for that one (pdl_wait) before it reads anything.
+template <class... P, class... A>
+bool launch_after(void (*kern)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, A&&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  count_launch();
+  return cudaLaunchKernelEx(&cfg, kern, std::forward<A>(args)...) == cudaSuccess;
+}
 
 // ---------------------------------------------------------------- device
 struct CacheDev {

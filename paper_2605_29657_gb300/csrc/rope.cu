@@ -56,6 +56,7 @@ struct alignas(sizeof(E) * V) Vec {
 template <typename E, int V, bool ADJ>
 __global__ void __launch_bounds__(256) rope_kernel(RopeParams p) {
   using VecT = Vec<E, V>;
+  pdl_wait();
   const int units = p.dim / (2 * V), turn = p.half / V;
   const int64_t at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   const int64_t row = at / units;
@@ -113,11 +114,9 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeParams p) {
 }
 
 template <typename E, int V>
-void launch_v(const RopeParams& p, int adj, dim3 grid, cudaStream_t st) {
-  if (adj)
-    rope_kernel<E, V, true><<<grid, 256, 0, st>>>(p);
-  else
-    rope_kernel<E, V, false><<<grid, 256, 0, st>>>(p);
+bool launch_v(const RopeParams& p, int adj, dim3 grid, cudaStream_t st) {
+  return adj ? launch_after(rope_kernel<E, V, true>, grid, 256, 0, st, p)
+             : launch_after(rope_kernel<E, V, false>, grid, 256, 0, st, p);
 }
 
 template <typename E>
@@ -150,17 +149,17 @@ int launch_t(RopeParams& p, int adj, int n, cudaStream_t st) {
   const int groups = p.groups0 + (n > 1 ? (p.t[1].heads + p.hpt - 1) / p.hpt : 0);
   if (groups > 65535) return OCCAM_ERR_UNSUPPORTED;
   const dim3 grid((unsigned)blocks, (unsigned)groups);
+  bool ok = false;
   if (v == 8) {
-    if constexpr (sizeof(E) == 2) launch_v<E, 8>(p, adj, grid, st);
+    if constexpr (sizeof(E) == 2) ok = launch_v<E, 8>(p, adj, grid, st);
   } else if (v == 4) {
-    launch_v<E, 4>(p, adj, grid, st);
+    ok = launch_v<E, 4>(p, adj, grid, st);
   } else if (v == 2) {
-    launch_v<E, 2>(p, adj, grid, st);
+    ok = launch_v<E, 2>(p, adj, grid, st);
   } else {
-    launch_v<E, 1>(p, adj, grid, st);
+    ok = launch_v<E, 1>(p, adj, grid, st);
   }
-  count_launch();
-  return cudaGetLastError() == cudaSuccess ? OCCAM_OK : OCCAM_ERR_CUDA;
+  return ok && cudaGetLastError() == cudaSuccess ? OCCAM_OK : OCCAM_ERR_CUDA;
 }
 
 }  // namespace
