@@ -172,18 +172,25 @@ struct Tile {
   uint32_t seen[4];
 };
 
+// (One warp runs this once a step, so its latency is the step's: reductions are votes and
+// integer redux, masks without flags are arithmetic, divisions are left out where all scales agree.)
 struct Plan {
   const AttendParams& p;
   const Walk& x;
   const int lane;
   const int32_t* table;
   const uint8_t* flags;
+  const float* ks0;  // scales of page 0 in this layer and head
+  const float* vs0;
   int n_flags;
 
   __device__ Plan(const AttendParams& p_, const Walk& x_, int lane_) : p(p_), x(x_), lane(lane_) {}
 
   __device__ __forceinline__ void item() {
     table = p.c.table + (int64_t)x.s.seq * p.c.max_pages;
+    const int64_t b = (int64_t)p.layer * p.c.pages * p.c.heads + x.h;
+    ks0 = p.c.k_scale + b;
+    vs0 = p.c.v_scale + b;
     flags = nullptr;
     n_flags = 0;
     if (p.keep) {
@@ -202,20 +209,26 @@ struct Plan {
     const int first = tile * kK + (lane & 7) * kGroup;
     t.page = 0;
     if (first < x.s.len) t.page = table[first >> p.c.log2T];
+    if (tile * kK < n_flags) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int key = tile * kK + 32 * k + lane;
-      uint32_t see = key < x.s.len;
-      if (key < n_flags) see = flags[key];
-      t.seen[k] = see;
+      for (int k = 0; k < 4; ++k) {
+        const int key = tile * kK + 32 * k + lane;
+        t.seen[k] = key < n_flags ? flags[key] : 1u;
+      }
     }
   }
   // masks, and the scales (loads in flight)
   __device__ __forceinline__ void settle(Tile& t) const {
     const bool bad = (unsigned)t.page >= (unsigned)p.c.pages;
-    const unsigned wrong = __ballot_sync(0xffffffffu, bad) & 0xff;
+    const int keys = x.s.len - t.tile * kK;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) t.seen[k] = __ballot_sync(0xffffffffu, t.seen[k] != 0);
+    for (int k = 0; k < 4; ++k) {
+      const int n = keys - 32 * k;
+      uint32_t see = n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
+      if (t.tile * kK < n_flags) see &= __ballot_sync(0xffffffffu, t.seen[k] != 0);
+      t.seen[k] = see;
+    }
+    const unsigned wrong = __ballot_sync(0xffffffffu, bad) & 0xff;
     if (wrong) {
       set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
       if (bad) t.page = 0;
@@ -225,24 +238,19 @@ struct Plan {
         if ((wrong >> (2 * k + 1)) & 1) t.seen[k] &= 0x0000ffffu;
       }
     }
-    const int64_t b = ((int64_t)p.layer * p.c.pages + t.page) * p.c.heads + x.h;
-    t.ks = p.c.k_scale[b];
-    t.vs = p.c.v_scale[b];
+    t.ks = ks0[(int64_t)t.page * p.c.heads];
+    t.vs = vs0[(int64_t)t.page * p.c.heads];
   }
-  // whether this lane's group has a seen key
-  __device__ __forceinline__ bool has(const Tile& t) const {
-    return (pick(t.seen, (lane & 7) >> 1) >> (16 * (lane & 1))) & 0xffffu;
+  // groups with a seen key, a bit each
+  __device__ __forceinline__ uint32_t groups(const Tile& t) const {
+    const bool h = (pick(t.seen, (lane & 7) >> 1) >> (16 * (lane & 1))) & 0xffffu;
+    return __ballot_sync(0xffffffffu, h) & 0xff;
   }
-  // the largest and least (positive) scale of v of groups with a seen key
-  __device__ __forceinline__ void range(const Tile& t, float& hi, float& lo) const {
-    const bool h = has(t);
-    hi = h ? t.vs : 0.f;
-    lo = h && t.vs > 0.f ? t.vs : INFINITY;
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) {
-      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    }
+  // the largest and least positive, finite scale of v in those groups (positive floats order as integers)
+  __device__ __forceinline__ void range(const Tile& t, uint32_t with, float& hi, float& lo) const {
+    const bool h = ((with >> (lane & 7)) & 1) && t.vs > 0.f && t.vs <= 3.4e38f;
+    hi = __uint_as_float(__reduce_max_sync(0xffffffffu, h ? __float_as_uint(t.vs) : 0u));
+    lo = __uint_as_float(__reduce_min_sync(0xffffffffu, h ? __float_as_uint(t.vs) : 0x7f800000u));
   }
 };
 
@@ -402,21 +410,21 @@ __device__ __forceinline__ void plan_role(const AttendParams& p, Shared& sh, con
         }
         if (!found && !none) break;  // (where nothing is seen, one step of hidden keys gives the rows their zeros)
       }
+      uint32_t with = only >= 0 ? 1u << only : f.groups(cur);
       float hi, lo;
-      f.range(cur, hi, lo);
+      f.range(cur, with, hi, lo);
       if (only < 0 && lo < hi * kRhoKeep) {
         // scales of v too far apart for one reference: the groups with a seen key one by one
-        const int with = (int)(__ballot_sync(0xffffffffu, f.has(cur)) & 0xff);
         only = __ffs(with) - 1;
         groups = with & (with - 1);
+        with = 1u << only;
+        f.range(cur, with, hi, lo);
 #pragma unroll
         for (int k = 0; k < 4; ++k) whole[k] = cur.seen[k];
       }
       if (only >= 0) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) cur.seen[k] = (only >> 1) == k ? whole[k] & (0xffffu << (16 * (only & 1))) : 0u;
-        hi = __shfl_sync(0xffffffffu, cur.vs, only);
-        lo = hi > 0.f ? hi : INFINITY;
       }
       // v's reference, and O's factor
       float fall = 1.f;
@@ -426,21 +434,31 @@ __device__ __forceinline__ void plan_role(const AttendParams& p, Shared& sh, con
         rho = to;
         rho_max = fmaxf(rho_max, to);
       }
-      const bool has = f.has(cur), real = has && cur.vs != 0.f;
-      const uint32_t zero = __ballot_sync(0xffffffffu, has && !real) & 0xff;
+      // hidden groups take no part; a scale of 0 makes values of 0
+      const bool has = (with >> (lane & 7)) & 1, real = has && cur.vs != 0.f;
+      const uint32_t zero = with & ~__ballot_sync(0xffffffffu, real);
+      float lr = 0.f, rr = 1.f;
+      if (__any_sync(0xffffffffu, real && cur.vs != rho)) {
+        if (real && cur.vs != rho) {
+          lr = log2f(cur.vs / rho);
+          rr = rho / cur.vs;
+        }
+      }
       TC_WAIT(sh.step_free[n % kRing], ((n / kRing) & 1) ^ 1);
       Step& s = sh.step[n % kRing];
       if (lane < 8) {
-        // hidden groups take no part; a scale of 0 makes values of 0
         s.ks[lane] = has ? cur.ks : 1.f;
-        s.lr[lane] = real && cur.vs != rho ? log2f(cur.vs / rho) : 0.f;
-        s.rr[lane] = real ? rho / cur.vs : 1.f;
+        s.lr[lane] = lr;
+        s.rr[lane] = rr;
       }
-      if (lane < 4) s.seen[lane] = pick(cur.seen, lane);
+      if (lane == 8) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s.seen[k] = cur.seen[k];
+        s.zero = zero;
+      }
       if (lane == 0) {
         s.tile = cur.tile;
         s.open = (cur.seen[0] & cur.seen[1] & cur.seen[2] & cur.seen[3]) == 0xffffffffu && (cur.tile + 1) * kK <= common;
-        s.zero = zero;
         s.end = 0;
         s.row_tiles = tiles2;
         s.fall = fall;
@@ -448,12 +466,10 @@ __device__ __forceinline__ void plan_role(const AttendParams& p, Shared& sh, con
       __syncwarp();
       if (lane == 0) tc::bar_arrive(&sh.step_full[n % kRing]);
       ++n;
-      // the blocks of the pages with a seen key: lane b takes the tile's b-th page
-      const int T = p.c.T, pages = kK >> p.c.log2T;
-      bool want = has;  // of the lane's group; of its page:
-      for (int o = 1; o < 8 / pages; o <<= 1) want |= (bool)__shfl_xor_sync(0xffffffffu, (int)want, o);
-      const int page = __shfl_sync(0xffffffffu, cur.page, (lane & 7) * (8 / pages) & 7);
-      want = __shfl_sync(0xffffffffu, (int)want, (lane & 7) * (8 / pages) & 7) != 0 && lane < pages;
+      // the blocks of the pages with a seen key: lane b takes the tile's b-th page, 1 << log_gp groups each
+      const int T = p.c.T, log_gp = p.c.log2T - 4;
+      const int page = __shfl_sync(0xffffffffu, cur.page, (lane << log_gp) & 7);
+      const bool want = lane < (8 >> log_gp) && ((with >> (lane << log_gp)) & ((1u << (1 << log_gp)) - 1u)) != 0;
       const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, want)) * T * D;
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv) {
