@@ -11,8 +11,8 @@
 //    more than 2^6 apart is taken 16 keys at a time;
 //  - warps 8-11 turn the codes into f16 (exact) in the matrix layout
 //    (128-byte swizzle), two stages deep;
-//  - warp 12 issues the products: S = Q K^T into tensor memory, O += P V with P
-//    read from tensor memory, for two row tiles of 128, 64 keys at a time: while a
+//  - warps 12 and 14 issue the products: S = Q K^T into tensor memory, O += P V with P
+//    read from tensor memory, each for a row tile of 128, 64 keys at a time: while a
 //    row tile's softmax works on one half of its scores, the other half is multiplied;
 //  - warps 0-3 and 4-7 hold a row a thread: scores from tensor memory, maximum,
 //    exponentials, P back over the scores as f16.
@@ -535,73 +535,73 @@ __device__ __forceinline__ void convert_role(const AttendParams& p, Shared& sh, 
   }
 }
 
-// ---------------------------------------------------------------- the issuing thread
-// The whole warp walks through the steps (so that descriptors and branches are
-// the same for every lane); one elected lane issues.
+// ---------------------------------------------------------------- issuing
+// One warp for each row tile t. The whole warp walks through the steps (so that
+// branches are the same for every lane); one elected lane issues. (A single
+// warp for both was the slowest part: about 70 cycles an instruction.)
 template <int D>
 __device__ __forceinline__ void mma_role(const AttendParams& p, Shared& sh, uint32_t q_smem, uint32_t k_smem,
-                                         uint32_t v_smem, uint32_t tmem) {
+                                         uint32_t v_smem, uint32_t tmem, int t) {
   constexpr int kBytes = kK * D * 2;
   constexpr uint32_t id_s = idesc_f16(128, 64, false), id_o = idesc_f16(128, D, true);
-  const uint64_t dq = desc_kmajor(q_smem), dk = desc_kmajor(k_smem), dv = desc_mnmajor(v_smem);
-  uint32_t n = 0, j = 0, it = 0, it1 = 0;  // step records, steps, steps of row tile 0 and 1
+  const uint64_t dq = desc_kmajor(q_smem + t * kBytes), dk = desc_kmajor(k_smem), dv = desc_mnmajor(v_smem);
+  uint32_t n = 0, j = 0, it = 0;  // step records, steps, steps of this row tile
   int end = 0;
   for (uint32_t seg = 0; end != 2; ++seg) {
     TC_WAIT(sh.q_full, seg & 1);
-    int nt = 1;
+    bool mine = true;
     end = 0;
-    // Pass k: by halves h and row tiles t, O += P V of step k - 1, then S of step k in the
-    // place of that P. (Rolled: the roles together have to stay within the
-    // instruction cache. A descriptor's address field counts 16 bytes.)
+    // Pass k: by halves h, O += P V of step k - 1, then S of step k in the place of that P.
+    // (Rolled: the roles together have to stay within the instruction cache.
+    // A descriptor's address field counts 16 bytes.)
 #pragma unroll 1
     for (uint32_t k = 0; !end; ++k) {
 #pragma unroll 1
-      for (uint32_t ht = 0; ht < 4; ++ht) {
-        const uint32_t h = ht >> 1, t = ht & 1;
-        if (k > 0 && (int)t < nt) {
-          TC_WAIT(sh.p_full[t][h], (t ? it1 : it) & 1);
-          if (ht == 0) TC_WAIT(sh.v_full[(j - 1) & 1], ((j - 1) >> 1) & 1);
-          tc::fence_after();
-          if (elect_one()) {
-            const uint64_t vd = dv + ((j - 1) & 1) * (kBytes >> 4) + h * (64 * 128 >> 4);
-            const uint32_t o_at = tmem + 256 + t * 128, p_at = tmem + t * 128 + h * 64;
+      for (uint32_t h = 0; h < 2; ++h) {
+        if (k > 0) {
+          if (h == 0) TC_WAIT(sh.v_full[(j - 1) & 1], ((j - 1) >> 1) & 1);
+          if (mine) {
+            TC_WAIT(sh.p_full[t][h], it & 1);
+            tc::fence_after();
+            if (elect_one()) {
+              const uint64_t vd = dv + ((j - 1) & 1) * (kBytes >> 4) + h * (64 * 128 >> 4);
+              const uint32_t o_at = tmem + 256 + t * 128, p_at = tmem + t * 128 + h * 64;
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-              mma_ts(o_at, p_at + q * 8, vd + q * (2048 >> 4), id_o, q > 0 ? 1u : (k > 1 || h > 0 ? 1u : 0u));
-            tc::mma_commit(&sh.o_done[t][h]);
+              for (int q = 0; q < 4; ++q)
+                mma_ts(o_at, p_at + q * 8, vd + q * (2048 >> 4), id_o, q > 0 ? 1u : (k > 1 || h > 0 ? 1u : 0u));
+              tc::mma_commit(&sh.o_done[t][h]);
+            }
+            __syncwarp();
           }
-          __syncwarp();
         }
-        if (ht == 0) {
+        if (h == 0) {
           TC_WAIT(sh.step_full[n % kRing], (n / kRing) & 1);
           end = sh.step[n % kRing].end;
           if (!end) {
-            nt = sh.step[n % kRing].row_tiles;
+            mine = t < sh.step[n % kRing].row_tiles;
             TC_WAIT(sh.k_full[j & 1], (j >> 1) & 1);
             tc::fence_after();
           }
         }
-        if (!end && (int)t < nt) {
+        if (!end && mine) {
           if (elect_one()) {
-            const uint64_t kd = dk + (j & 1) * (kBytes >> 4) + h * (64 * 128 >> 4), qd = dq + t * (kBytes >> 4);
+            const uint64_t kd = dk + (j & 1) * (kBytes >> 4) + h * (64 * 128 >> 4);
             const uint32_t s_at = tmem + t * 128 + h * 64;
 #pragma unroll
             for (int q = 0; q < D / 16; ++q) {
               const int o = (q >> 2) * (16384 >> 4) + (q & 3) * 2;
-              tc::mma_bf16(s_at, qd + o, kd + o, id_s, q > 0);
+              tc::mma_bf16(s_at, dq + o, kd + o, id_s, q > 0);
             }
             tc::mma_commit(&sh.s_full[t][h]);
           }
           __syncwarp();
         }
       }
-      if (k > 0) {
-        ++it;
-        it1 += nt == 2;
-      }
+      if (k > 0 && mine) ++it;
+      // (without products of its own the warp just arrives: it has waited for the same stages)
       if (elect_one()) {
-        if (k > 0) tc::mma_commit(&sh.v_free[(j - 1) & 1]);
-        if (!end) tc::mma_commit(&sh.k_free[j & 1]);
+        if (k > 0) mine ? tc::mma_commit(&sh.v_free[(j - 1) & 1]) : tc::bar_arrive(&sh.v_free[(j - 1) & 1]);
+        if (!end) mine ? tc::mma_commit(&sh.k_free[j & 1]) : tc::bar_arrive(&sh.k_free[j & 1]);
         tc::bar_arrive(&sh.step_free[n % kRing]);
       }
       __syncwarp();
@@ -977,12 +977,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(AttendParams p, 
     sh.stop = 0;
     tc::bar_init(&sh.q_full, 256);
     tc::bar_init(&sh.meet, 256);
-    tc::bar_init(&sh.drain, 1);
+    tc::bar_init(&sh.drain, 2);
     for (int k = 0; k < 2; ++k) {
       tc::bar_init(&sh.k_full[k], 128);
       tc::bar_init(&sh.v_full[k], 128);
-      tc::bar_init(&sh.k_free[k], 1);
-      tc::bar_init(&sh.v_free[k], 1);
+      tc::bar_init(&sh.k_free[k], 2);
+      tc::bar_init(&sh.v_free[k], 2);
       for (int h = 0; h < 2; ++h) {
         tc::bar_init(&sh.s_full[k][h], 1);
         tc::bar_init(&sh.p_full[k][h], 128);
@@ -993,7 +993,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(AttendParams p, 
     }
     for (int k = 0; k < kRing; ++k) {
       tc::bar_init(&sh.step_full[k], 1);
-      tc::bar_init(&sh.step_free[k], 13);  // every warp that reads it
+      tc::bar_init(&sh.step_free[k], 14);  // every warp that reads it
     }
     tc::bar_fence_init();
   }
@@ -1014,14 +1014,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(AttendParams p, 
     convert_role<D>(p, sh, k_smem, v_smem, raw);
   } else {
     tc::setmaxnreg_dec<kRegIssue>();
-    if (warp == 12)
-      mma_role<D>(p, sh, tc::su32(q_smem), tc::su32(k_smem), tc::su32(v_smem), tmem);
+    if (warp == 12 || warp == 14)
+      mma_role<D>(p, sh, tc::su32(q_smem), tc::su32(k_smem), tc::su32(v_smem), tmem, warp == 14);
     else if (warp == 13)
       plan_role<D>(p, sh, map_k, map_v, raw);
   }
   __syncthreads();
   // after a wait that ran out, products and copies may still be in flight
-  if (sh.stop && threadIdx.x == 384) {
+  if (sh.stop && (threadIdx.x == 384 || threadIdx.x == 448)) {
     tc::mma_commit(&sh.drain);
     tc::bar_wait(&sh.drain, 0, nullptr, kWaitNs);
     for (int k = 0; k < 2; ++k) {
