@@ -13,7 +13,8 @@
 //    (128-byte swizzle), two stages deep;
 //  - warps 12 and 14 issue the products: S = Q K^T into tensor memory, O += P V with P
 //    read from tensor memory, each for a row tile of 128, 64 keys at a time: while a
-//    row tile's softmax works on one half of its scores, the other half is multiplied;
+//    row tile's softmax works on one half of its scores, the other half is multiplied
+//    (128 keys at a time, 64 of P: measured slower, 0.61 ms where this takes 0.55);
 //  - warps 0-3 and 4-7 hold a row a thread: scores from tensor memory, maximum,
 //    exponentials, P back over the scores as f16.
 // O stays in tensor memory. It is rescaled only where a row's maximum grew by more than
@@ -625,11 +626,15 @@ __device__ __forceinline__ float load_queries(const AttendParams& p, const Walk&
     const int r = (first & 127) + i * RPI + sub;
     return mine + r * 128 + (((c & 7) ^ (r & 7)) << 4);
   };
-#pragma unroll 2
+  const uint16_t* row_at = nullptr;  // lane l's row
+  {
+    const int at = x.rt * kR + first + lane, tok = div_group(p, at);
+    if (at < rows) row_at = p.q + (x.s.row0 + tok) * p.q_row + (int64_t)(x.h * p.G + at - tok * p.G) * D;
+  }
+#pragma unroll 4
   for (int i = 0; i < N; ++i) {
-    const int at = x.rt * kR + first + i * RPI + sub, tok = div_group(p, at);
-    const uint16_t* src = at < rows ? p.q + (x.s.row0 + tok) * p.q_row + (int64_t)(x.h * p.G + at - tok * p.G) * D + c * 8 : p.q;
-    tc::cp_async16(piece(i), src, at < rows ? 16 : 0);
+    const uint64_t from = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(row_at), i * RPI + sub);
+    tc::cp_async16(piece(i), from ? reinterpret_cast<const uint16_t*>(from) + c * 8 : p.q, from ? 16 : 0);
   }
   cp_async_commit();
   cp_async_wait<0>();
@@ -652,8 +657,8 @@ __device__ __forceinline__ float load_queries(const AttendParams& p, const Walk&
       }
       amax = tc::fmax3(amax, fabsf(f[2 * k]), fabsf(f[2 * k + 1]));
     }
-#pragma unroll
-    for (int o = 1; o < LPR; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    // (magnitudes order as integers; a NaN does not matter, its row is NaN)
+    amax = __uint_as_float(__reduce_max_sync(((1u << LPR) - 1u) << (sub * LPR), __float_as_uint(amax)));
     // largest value in [2^14, 2^15), as in attend.cu
     int e = (__float_as_int(amax) >> 23) - 127 - 14;
     e = amax == 0.f ? 0 : max(e, -112);
@@ -673,16 +678,6 @@ __device__ __forceinline__ uint32_t out_pair(float a, float b) {
     return *reinterpret_cast<const uint32_t*>(&v);
   }
   return pack_f16(a, b);
-}
-
-// 16 values of a result row
-template <bool BF16>
-__device__ __forceinline__ void write16(uint16_t* to, const float (&v)[16]) {
-  uint4* out = reinterpret_cast<uint4*>(to);
-#pragma unroll
-  for (int k = 0; k < 2; ++k)
-    out[k] = make_uint4(out_pair<BF16>(v[8 * k], v[8 * k + 1]), out_pair<BF16>(v[8 * k + 2], v[8 * k + 3]),
-                        out_pair<BF16>(v[8 * k + 4], v[8 * k + 5]), out_pair<BF16>(v[8 * k + 6], v[8 * k + 7]));
 }
 
 template <int D, bool BF16>
@@ -756,7 +751,7 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
           }
           // O in units of the new references (nothing is there before the first product)
           if (!(begin && h == 0) && __any_sync(0xffffffffu, move)) {
-            // the product of the half before (the one before that is done: this half's scores came after it)
+            // the product of the half before (the one before that is done: the step's scores came after it)
             TC_WAIT(sh.o_done[t][h ^ 1], ((it - 1) >> 1) & 1);
             tc::fence_after();
 #pragma unroll 1
@@ -814,22 +809,44 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
       const float scale = l == 0.f ? 0.f : done ? rho / l : rho;
       uint16_t* out = p.out + to * D;
       float* part = p.part_o + mypart * D;
+      // By way of the warp's own queries' place (they are done with), so that whole rows are
+      // written at once: row r's 16-byte piece c lies where a query's would.
+      constexpr int CH = D / 8, RPI = 32 / CH;  // pieces of a row there, rows of a write
+      unsigned char* stage = q_smem + t * kK * D * 2;
+      auto place = [&](int rr, int c) { return stage + (c >> 3) * 16384 + rr * 128 + (((c & 7) ^ (rr & 7)) << 4); };
+      const int live = min(x.s.rows * p.G - (x.rt * kR + (row & ~31)), 32);  // rows of the warp
+      const uint64_t mine_at = done ? reinterpret_cast<uint64_t>(out) : reinterpret_cast<uint64_t>(part);
 #pragma unroll 1
-      for (int c = 0; c < D; c += 16) {
-        uint32_t o[16];
-        tmem_ld16(o_at + c, o);
-        if (there) {
+      for (int pass = 0; pass < (done ? 1 : 2); ++pass) {
+        const int cols = done ? D : D / 2;
+#pragma unroll 1
+        for (int c = 0; c < cols; c += 16) {
+          uint32_t o[16];
+          tmem_ld16(o_at + pass * (D / 2) + c, o);
           float v[16];
 #pragma unroll
           for (int k = 0; k < 16; ++k) v[k] = l == 0.f ? 0.f : __uint_as_float(o[k]) * scale;
           if (done) {
-            write16<BF16>(out + c, v);
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+              *reinterpret_cast<uint4*>(place(r, c / 8 + k)) =
+                  make_uint4(out_pair<BF16>(v[8 * k], v[8 * k + 1]), out_pair<BF16>(v[8 * k + 2], v[8 * k + 3]),
+                             out_pair<BF16>(v[8 * k + 4], v[8 * k + 5]), out_pair<BF16>(v[8 * k + 6], v[8 * k + 7]));
           } else {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              reinterpret_cast<float4*>(part + c)[k] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+              *reinterpret_cast<float4*>(place(r, c / 4 + k)) = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
           }
         }
+        __syncwarp();
+#pragma unroll 4
+        for (int i = 0; i < 32 / RPI; ++i) {
+          const int rr = i * RPI + lane / CH, c = lane % CH;
+          const uint64_t to_at = __shfl_sync(0xffffffffu, mine_at, rr);
+          const uint4 v = *reinterpret_cast<const uint4*>(place((r & ~31) + rr, c));
+          if (rr < live) reinterpret_cast<uint4*>(to_at)[pass * CH + c] = v;
+        }
+        __syncwarp();
       }
       if (there && sh.any_nan[seg & 3]) {
 #pragma unroll 1
@@ -890,42 +907,51 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
             for (int k = 0; k < n; ++k)
               wt[k * 32 + lane] = there ? fast_exp2(__ldcg(&p.part_ml[part(c0 + k, lane)]).x - base) * inv : 0.f;
             __syncwarp();
+            constexpr int V = D / 32, ROWS = 8;  // values a lane holds of a row, rows whose loads are in flight
 #pragma unroll 1
-            for (int rr = 0; rr < rows; ++rr) {
-              constexpr int V = D / 32;  // values a lane holds of a row
-              float acc[V];
+            for (int r0 = 0; r0 < rows; r0 += ROWS) {
+              float acc[ROWS][V];
 #pragma unroll
-              for (int q = 0; q < V; ++q) acc[q] = 0.f;
-              float* keep = p.part_o + part(first, rr) * D + lane * V;
-#pragma unroll 2
-              for (int k = 0; k < n; ++k) {
-                const float w = wt[k * 32 + rr];
-                const float* from = p.part_o + part(c0 + k, rr) * D + lane * V;
-                float v[V];
-                if constexpr (V == 4) {
-                  const float4 y = __ldcg(reinterpret_cast<const float4*>(from));
-                  v[0] = y.x, v[1] = y.y, v[2] = y.z, v[3] = y.w;
-                } else {
-                  const float2 y = __ldcg(reinterpret_cast<const float2*>(from));
-                  v[0] = y.x, v[1] = y.y;
+              for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+                for (int q = 0; q < V; ++q) acc[i][q] = 0.f;
+#pragma unroll 1
+              for (int k = c0 > first ? -1 : 0; k < n; ++k) {
+                // (-1: the blocks before, kept in the first part's place)
+                float v[ROWS][V];
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i) {
+                  const float* from = p.part_o + part(k < 0 ? first : c0 + k, min(r0 + i, rows - 1)) * D + lane * V;
+                  if constexpr (V == 4) {
+                    const float4 y = __ldcg(reinterpret_cast<const float4*>(from));
+                    v[i][0] = y.x, v[i][1] = y.y, v[i][2] = y.z, v[i][3] = y.w;
+                  } else {
+                    const float2 y = __ldcg(reinterpret_cast<const float2*>(from));
+                    v[i][0] = y.x, v[i][1] = y.y;
+                  }
                 }
 #pragma unroll
-                for (int q = 0; q < V; ++q) acc[q] = fmaf(v[q], w, acc[q]);
+                for (int i = 0; i < ROWS; ++i) {
+                  const float w = k < 0 ? 1.f : wt[k * 32 + r0 + i];
+#pragma unroll
+                  for (int q = 0; q < V; ++q) acc[i][q] = fmaf(v[i][q], w, acc[i][q]);
+                }
               }
-              if (c0 > first) {  // the blocks before, kept in the first part's place
 #pragma unroll
-                for (int q = 0; q < V; ++q) acc[q] += keep[q];
-              }
-              if (c0 + n <= last) {
+              for (int i = 0; i < ROWS; ++i) {
+                const float total = __shfl_sync(0xffffffffu, sum, (r0 + i) & 31);
+                const uint64_t row_to = __shfl_sync(0xffffffffu, (uint64_t)to, (r0 + i) & 31);
+                if (r0 + i < rows) {
+                  if (c0 + n <= last) {
+                    float* keep = p.part_o + part(first, r0 + i) * D + lane * V;
 #pragma unroll
-                for (int q = 0; q < V; ++q) keep[q] = acc[q];
-              } else {
-                const float total = __shfl_sync(0xffffffffu, sum, rr);
-                const int64_t row_to = __shfl_sync(0xffffffffu, to, rr);
-                uint32_t* out = reinterpret_cast<uint32_t*>(p.out + row_to * D + lane * V);
+                    for (int q = 0; q < V; ++q) keep[q] = acc[i][q];
+                  } else {
+                    uint32_t* out = reinterpret_cast<uint32_t*>(p.out + row_to * D + lane * V);
 #pragma unroll
-                for (int q = 0; q < V; q += 2)
-                  out[q / 2] = total == 0.f ? 0u : out_pair<BF16>(acc[q], acc[q + 1]);
+                    for (int q = 0; q < V; q += 2) out[q / 2] = total == 0.f ? 0u : out_pair<BF16>(acc[i][q], acc[i][q + 1]);
+                  }
+                }
               }
             }
           }
