@@ -39,7 +39,6 @@ namespace {
 
 constexpr int kTile = 32;   // keys of a unit
 constexpr int kOver = 3;    // beginning and ending an item takes as long as this many units
-constexpr int kShared = 0;  // sixteenths of the work left to CTAs that become free
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr int kFewRows = 32;  // query rows of a key head this file's kernel is used for
@@ -135,7 +134,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
   constexpr int MT = D / 16;      // tiles of 16 dims
   __shared__ int64_t sh[kWarps + 4];
   __shared__ float sh_m[kWarps][R], sh_l[kWarps][R];
-  __shared__ int sh_last, sh_next;
+  __shared__ int sh_last;
   __shared__ int sh_nan[D];  // first token with a NaN in that dim, of those taken out
   // Each warp's copies: two slots of keys and two of values, 32 rows each. At the end
   // of a segment the warp's sums take their place.
@@ -157,14 +156,12 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
   for (int d = threadIdx.x; d < D; d += kThreads) sh_nan[d] = 0x7fffffff;
   pdl_wait();
   Line line;
-  const LinePart part0 = attend_line<R, kTile, kOver, kThreads>(p, kOver + kWarps, kAttendCtas, kShared, sh, line);
-  // (every CTA takes part in the last count below)
-  for (int c = line.units > 0 ? (int)blockIdx.x : line.total; c < line.total;) {
+  const LinePart mine = attend_line<R, kTile, kOver, kThreads>(p, kOver + kWarps, sh, line);
+  if (line.units == 0 || (int)blockIdx.x >= line.stretches) return;
   Stretch w;
-  attend_find<R, kTile, kOver, kThreads>(p, line, part0, c, sh, w);
-  if (threadIdx.x == 0) sh_next = line.total > line.first ? line.first + atomicAdd(p.tickets, 1) : line.total;
+  attend_find<R, kTile, kOver, kThreads>(p, line, mine, blockIdx.x, sh, w);
   Walk x0;
-  if (walk_begin<R, kTile, kOver>(p, w, x0))
+  if (!walk_begin<R, kTile, kOver>(p, w, x0)) return;
   do {
     const SeqInfo s = x0.s;
     const int i = x0.i, h = x0.h, rt = x0.rt, tiles = x0.tiles, ta = x0.ta, tb = x0.tb;
@@ -635,14 +632,6 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
     __syncthreads();  // the shared results are free again
     for (int d = threadIdx.x; d < D; d += kThreads) sh_nan[d] = 0x7fffffff;
   } while (walk_next<R, kTile, kOver>(p, w, x0));
-  __syncthreads();
-  c = sh_next;
-  }
-  // the last CTA to leave puts the tickets back
-  if (threadIdx.x == 0 && line.total > line.first && atomicAdd(p.tickets + 1, 1) == (int)gridDim.x - 1) {
-    p.tickets[0] = 0;
-    p.tickets[1] = 0;
-  }
 }
 
 template <int D, int NQ, bool TMA>
@@ -657,7 +646,10 @@ int launch(const AttendParams& p, const CUtensorMap& mk, const CUtensorMap& mv, 
     ready.fetch_or(uint64_t(1) << dev, std::memory_order_release);
   }
   const int grid = std::min(cache_sms() * (NQ == 1 ? 3 : 2), kAttendCtas);
-  return launch_after(attend_rows_kernel<D, NQ, TMA>, dim3((unsigned)grid), kThreads, smem, st, p, mk, mv) && cudaGetLastError() == cudaSuccess ? OCCAM_OK : OCCAM_ERR_CUDA;
+  return launch_after(attend_rows_kernel<D, NQ, TMA>, dim3((unsigned)grid), kThreads, smem, st, p, mk, mv) &&
+                 cudaGetLastError() == cudaSuccess
+             ? OCCAM_OK
+             : OCCAM_ERR_CUDA;
 }
 
 template <int D, int NQ>
@@ -750,7 +742,6 @@ extern "C" int occam_cache_attend(const occam_cache* cache, const occam_attend_a
   const double scale = a->scale > 0.f ? (double)a->scale : 1.0 / std::sqrt((double)cache->dim);
   p.scale_log2 = (float)(scale * 1.4426950408889634);
   p.counters = ws_at<int32_t>(workspace, w.counters);
-  p.tickets = p.counters + kAttendCtas;
   p.part_o = ws_at<float>(workspace, w.part_o);
   p.part_ml = ws_at<float2>(workspace, w.part_ml);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);

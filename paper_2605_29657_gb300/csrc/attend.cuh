@@ -4,12 +4,14 @@
 // The work is a line of units: for each sequence, key head and tile of query
 // rows (token j, query head g of the key head's group: row j G + g) the key
 // tiles that the tile's last row can see. Every CTA takes an equal stretch of
-// the line. An item (sequence, head, row tile) that lies in one CTA's
-// stretch is finished there; one that is split leaves a partial result
-// (unnormalised sums, running maximum, sum) per CTA, and the CTA that
-// arrives last adds them in order -- always the same order, so results do not depend on timing.
-// An item's units are preceded by OVER empty ones: what beginning and ending an
+// the line. An item (sequence, head, row tile) that lies in one CTA's stretch
+// is finished there; one that is split leaves a partial result (unnormalised
+// sums, running maximum, sum) per CTA, and the CTA that arrives last adds them
+// in order -- always the same order, so results do not depend on timing. An
+// item's units are preceded by OVER empty ones: what beginning and ending an
 // item costs, in key tiles, so that CTAs with many short items get fewer tiles.
+// (Leaving 3/16 of the line in short stretches to the CTAs that are done first
+// measured slower: 64 single tokens 100 us where equal stretches take 81.)
 #pragma once
 
 #include "cache.cuh"
@@ -31,7 +33,6 @@ struct AttendParams {
   float scale_log2;
   uint32_t g_mul, g_shift;  // x / G = x g_mul >> g_shift for 0 <= x < 2^31
   int32_t* counters;  // per stretch: arrivals at an item that begins in it
-  int32_t* tickets;   // stretches taken beyond the first ones, CTAs that are done
   float* part_o;
   float2* part_ml;
 };
@@ -106,23 +107,16 @@ __device__ __forceinline__ int64_t head_units(const AttendParams& p, const SeqIn
   return (nrt > 1 ? units_before<R, KT, OVER>(p, s, nrt - 1) : 0) + OVER + key_tiles<R, KT>(p, s, nrt - 1);
 }
 
-// The cuts: stretch c < first begins at c head / first, the others share the rest.
-// (Units are 31-bit numbers: 2^31 key tiles are hours of work.)
+// Stretch c begins at c units / stretches. (Units are 31-bit numbers: 2^31 key
+// tiles are hours of work.)
 struct Line {
-  int units, head;
-  int first, total;  // stretches
-  int q0, r0, q1, r1;  // head = q0 first + r0, the rest = q1 (total - first) + r1
+  int units, stretches;
+  int q, r;  // units = q stretches + r
 };
-__device__ __forceinline__ int stretch_begin(const Line& l, int c) {
-  if (c <= l.first) return l.q0 * c + l.r0 * c / l.first;
-  const int d = c - l.first;
-  return l.head + l.q1 * d + l.r1 * d / (l.total - l.first);
-}
+__device__ __forceinline__ int stretch_begin(const Line& l, int c) { return l.q * c + l.r * c / l.stretches; }
 static __device__ __noinline__ int stretch_of(const Line& l, int u) {
-  int c = u < l.head ? (int)((float)u * (float)l.first / (float)l.head)
-                     : l.first + (int)((float)(u - l.head) * (float)(l.total - l.first) / (float)(l.units - l.head));
-  c = min(max(c, 0), l.total - 1);
-  while (c + 1 < l.total && stretch_begin(l, c + 1) <= u) ++c;
+  int c = min(max((int)((float)u * (float)l.stretches / (float)l.units), 0), l.stretches - 1);
+  while (c + 1 < l.stretches && stretch_begin(l, c + 1) <= u) ++c;
   while (c > 0 && stretch_begin(l, c) > u) --c;
   return c;
 }
@@ -139,10 +133,9 @@ struct LinePart {
   int i0, i1;
 };
 // Block-wide (NT threads, all of them); sh: NT / 32 + 4 int64 of shared memory.
-// min_units: a stretch is no shorter; shared: sixteenths of the line left to the short stretches.
+// min_units: a stretch is no shorter.
 template <int R, int KT, int OVER, int NT>
-__device__ __forceinline__ LinePart attend_line(const AttendParams& p, int min_units, int most_stretches, int shared, int64_t* sh,
-                                                Line& l) {
+__device__ __forceinline__ LinePart attend_line(const AttendParams& p, int min_units, int64_t* sh, Line& l) {
   constexpr int NWARP = NT / 32;
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   const int per = (p.n + NT - 1) / NT;
@@ -172,22 +165,15 @@ __device__ __forceinline__ LinePart attend_line(const AttendParams& p, int min_u
   w.at = (int)(before + incl - mine);
   w.mine = (int)mine;
   l.units = (int)total;
-  const int most = max(l.units / min_units, 1);
-  l.first = min((int)gridDim.x, most);
-  l.total = min(min(most_stretches, 3 * l.first), most);
-  // a few stretches in all: none are held back
-  if (l.total < 2 * l.first || shared == 0) l.total = l.first;
-  l.head = l.total > l.first ? (int)(total - total * shared / 16) : l.units;
-  l.q0 = l.head / l.first;
-  l.r0 = l.head - l.q0 * l.first;
-  const int d = max(l.total - l.first, 1);
-  l.q1 = (l.units - l.head) / d;
-  l.r1 = l.units - l.head - l.q1 * d;
+  l.stretches = min((int)gridDim.x, max(l.units / min_units, 1));
+  l.q = l.units / l.stretches;
+  l.r = l.units - l.q * l.stretches;
   return w;
 }
 // Stretch c, to all threads of the block.
 template <int R, int KT, int OVER, int NT>
-__device__ __forceinline__ void attend_find(const AttendParams& p, const Line& l, const LinePart& part, int c, int64_t* sh, Stretch& w) {
+__device__ __forceinline__ void attend_find(const AttendParams& p, const Line& l, const LinePart& part, int c, int64_t* sh,
+                                            Stretch& w) {
   constexpr int NWARP = NT / 32;
   w.index = c;
   w.u0 = stretch_begin(l, c);

@@ -63,8 +63,8 @@ struct Shared {
       step_free[kRing], raw_full[2], raw_free[2], meet, drain;
   Step step[kRing];
   Line line;
-  volatile int u0, u1;   // the CTA's stretch (see Stretch)
-  volatile int seq, head, row_tile, in_item;
+  int u0, u1;   // the CTA's stretch (see Stretch)
+  int seq, head, row_tile, in_item;
   uint32_t tmem;
   int stop;            // a wait ran out
   int last;
@@ -477,7 +477,9 @@ __device__ __forceinline__ void plan_role(const AttendParams& p, Shared& sh, con
         TC_WAIT(sh.raw_free[kv], (j & 1) ^ 1);
         if (lane == 0) tc::bar_expect_tx(&sh.raw_full[kv], bytes);
         __syncwarp();
-        if (want) tma_block(raw + kv * (kK * D) + lane * T * D, kv ? &map_v : &map_k, x.h * T, p.layer * p.c.pages + page, &sh.raw_full[kv]);
+        if (want)
+          tma_block(raw + kv * (kK * D) + lane * T * D, kv ? &map_v : &map_k, x.h * T, p.layer * p.c.pages + page,
+                    &sh.raw_full[kv]);
       }
       ++j;
     }
@@ -959,7 +961,7 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
       }
     }
     // The notes of the segment before are cleared: its other row tile has read
-    // them (it came to this segment's products), and the fetching warps, two tiles ahead
+    // them (it came to this segment's products), and the converting warps, two tiles ahead
     // at most, are not yet three segments on.
     const uint32_t old = (seg + 3) & 3;
     if (t == 0 && sh.any_nan[old]) {
@@ -971,7 +973,8 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
 }
 
 template <int D, bool BF16>
-__global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(AttendParams p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+__global__ void __launch_bounds__(kThreads, 1)
+    attend_tc_kernel(AttendParams p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
   constexpr int kBytes = kK * D * 2;
   // queries 2 tiles, keys and values 2 stages each, codes as they come: 7 x 32 KB (D = 128)
   extern __shared__ __align__(1024) unsigned char smem[];
@@ -984,8 +987,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc_kernel(AttendParams p, 
   const int warp = threadIdx.x >> 5;
   pdl_wait();
   Line line;
-  const LinePart part = attend_line<kR, kK, kOver, kThreads>(p, kOver + 1, kAttendTcCtas, 0, scan, line);
-  if (line.units == 0 || (int)blockIdx.x >= line.first) return;
+  const LinePart part = attend_line<kR, kK, kOver, kThreads>(p, kOver + 1, scan, line);
+  if (line.units == 0 || (int)blockIdx.x >= line.stretches) return;
   Stretch w;
   attend_find<kR, kK, kOver, kThreads>(p, line, part, blockIdx.x, scan, w);
   {
@@ -1082,14 +1085,17 @@ int launch(const AttendParams& p, const CUtensorMap& mk, const CUtensorMap& mv, 
   const int rc = prepare<D, BF16>(smem);
   if (rc != OCCAM_OK) return rc;
   const dim3 grid((unsigned)std::min(cache_sms(), kAttendTcCtas));
-  return launch_after(attend_tc_kernel<D, BF16>, grid, kThreads, smem, st, p, mk, mv) && cudaGetLastError() == cudaSuccess ? OCCAM_OK : OCCAM_ERR_CUDA;
+  return launch_after(attend_tc_kernel<D, BF16>, grid, kThreads, smem, st, p, mk, mv) && cudaGetLastError() == cudaSuccess
+             ? OCCAM_OK
+             : OCCAM_ERR_CUDA;
 }
 
 }  // namespace
 
 int occam::launch_attend_tc(const AttendParams& p, int dim, cudaStream_t st) {
   CUtensorMap mk, mv;
-  if (!encode_blocks(&mk, p.c, p.c.k, dim, p.c.T, false) || !encode_blocks(&mv, p.c, p.c.v, dim, p.c.T, false)) return OCCAM_ERR_CUDA;
+  if (!encode_blocks(&mk, p.c, p.c.k, dim, p.c.T, false) || !encode_blocks(&mv, p.c, p.c.v, dim, p.c.T, false))
+    return OCCAM_ERR_CUDA;
   if (dim == 128) return p.bf16 ? launch<128, true>(p, mk, mv, st) : launch<128, false>(p, mk, mv, st);
   return p.bf16 ? launch<64, true>(p, mk, mv, st) : launch<64, false>(p, mk, mv, st);
 }

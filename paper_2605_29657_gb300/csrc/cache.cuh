@@ -13,7 +13,7 @@ namespace occam {
 
 // Attention workspace: at most kAttendCtas stretches of work leave two partial results of
 // up to kAttendRows rows each (the tensor-core kernel: kAttendTcCtas, 256 rows).
-constexpr int kAttendCtas = 2048;
+constexpr int kAttendCtas = 512;
 constexpr int kAttendRows = 16;
 constexpr int kAttendTcCtas = 160;
 constexpr size_t kAttendPartRows =
@@ -39,7 +39,7 @@ inline CacheWs cache_ws(const occam_cache* c, int64_t max_tokens) {
     return o;
   };
   w.status = take(8);
-  w.counters = take((size_t)(kAttendCtas + 2) * 4);
+  w.counters = take((size_t)kAttendCtas * 4);
   w.marks = take((size_t)c->max_seqs * 4);
   w.count = take((size_t)c->max_seqs * 4);
   w.lead = take((size_t)c->max_seqs * 4);
@@ -59,8 +59,9 @@ inline int check_cache(const occam_cache* c) {
   if (c->dim != 64 && c->dim != 128) return OCCAM_ERR_UNSUPPORTED;
   if (c->page_tokens != 16 && c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128)
     return OCCAM_ERR_UNSUPPORTED;
-  if (c->layers < 1 || c->pages < 1 || c->pages > (1 << 24) || (int64_t)c->layers * c->pages > 0x7fffffff || c->heads < 1 || c->heads > 1024 || c->max_seqs < 1 ||
-      c->max_seqs > 65535 || c->layers > 65535 || c->max_pages < 1 || (int64_t)c->max_pages * c->page_tokens >= (int64_t(1) << 31) - 256)
+  if (c->layers < 1 || c->layers > 65535 || c->pages < 1 || c->pages > (1 << 24) ||
+      (int64_t)c->layers * c->pages > 0x7fffffff || c->heads < 1 || c->heads > 1024 || c->max_seqs < 1 ||
+      c->max_seqs > 65535 || c->max_pages < 1 || (int64_t)c->max_pages * c->page_tokens >= (int64_t(1) << 31) - 256)
     return OCCAM_ERR_INVALID_ARG;
   if (!c->k || !c->v || !c->k_scale || !c->v_scale || !c->table || !c->length || !c->refs) return OCCAM_ERR_INVALID_ARG;
   if (!aligned16(c->k) || !aligned16(c->v)) return OCCAM_ERR_INVALID_ARG;
