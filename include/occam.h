@@ -416,7 +416,8 @@ enum { OCCAM_ROPE_HALF = 0, OCCAM_ROPE_ADJACENT = 1 };
 
 /* One tensor of an occam_rope call: [rows, heads, dim] values, dense in dim;
  * strides in elements. dst may be src with the same strides (in place);
- * otherwise the two must not overlap. */
+ * otherwise the two must not overlap. src may be broadcast (a stride of 0);
+ * dst's rows and heads are at least dim elements apart. */
 typedef struct occam_rope_tensor {
   const void* src;
   void* dst;
@@ -442,17 +443,17 @@ int occam_rope(int32_t dtype, int64_t rows, int32_t dim, int32_t rot, int32_t pa
 
 /* ------------------------------------------------------------------ after pruning: a paged cache held in 8 bits
  * Keys and values of kept rows, held as e4m3 codes (1 sign, 4 exponent, 3
- * mantissa bits; largest value 448) with one fp32 scale for each block of
- * tokens and head: value = code * scale. A page holds page_tokens tokens of
+ * mantissa bits; largest value 448) with one fp32 scale, positive and finite, for
+ * each block of tokens and head: value = code * scale. A page holds page_tokens tokens of
  * one sequence in every layer; the block of (layer, page, head) is
  * page_tokens x dim codes, contiguous. Sequence slot s lists its pages in
  * table[s], holds length[s] tokens (token p in slot p % page_tokens of page
  * table[s][p / page_tokens]), and a page may belong to several sequences;
  * refs counts them. A page that is not full belongs to one sequence only.
- * Table entries that name no page are -1. All state is on the device and only the calls below
- * write it: nothing needs a host synchronisation, and every call can be
- * captured into a CUDA graph. Page indices are given out lowest free page
- * first, in call order, so they do not depend on timing.
+ * Table entries that name no page are -1. All state is on the device and only
+ * the calls below write it: nothing needs a host synchronisation, and every
+ * call can be captured into a CUDA graph. Page indices are given out lowest
+ * free page first, in call order, so they do not depend on timing.
  *
  * seqs (and src, dst) are device arrays of n distinct slots, n <= max_seqs.
  * A slot, offset or page outside its range, a slot listed twice (extend,
@@ -511,15 +512,18 @@ int occam_cache_append(const occam_cache* cache, int32_t layer, int32_t dtype, i
  * none; uint8, device) hides tokens: token p of sequence i is seen if
  * keep[keep_off[i] + p] != 0 or p is past the flags (keep_off[i+1] -
  * keep_off[i] of them; keep_off [n+1] int64, device), so a prefix can be
- * pruned for one question without moving it. Hidden tokens and slots past the length may hold anything.
+ * pruned for one question without moving it. Hidden tokens and slots past the
+ * length may hold anything.
  *   out [total_rows, heads, dim] (q's type, dense) = sum_k p_k v_k / sum_k p_k,
  *   p_k = exp(scale q.k - max), scale 0: 1/sqrt(dim);
  *   lse [total_rows, heads] fp32 (NULL to skip) = log sum_k exp(scale q.k).
  * A row that sees no token gives 0 and -inf. Scores, statistics and sums are
  * in fp32; probabilities are rounded to f16 for the product with the codes.
  * Scales of v within a sequence may span a factor of 2^60. max_rows: the
- * largest row_off[i+1] - row_off[i] (it chooses the kernels; results are right for any
- * value). heads <= 64 * cache heads. */
+ * largest row_off[i+1] - row_off[i] (it chooses the kernels; results are right
+ * for any value). heads <= 64 * cache heads. A call of more than 2^31 - 2^16
+ * tiles (32 keys x 16 query rows of a key head) records OCCAM_ERR_UNSUPPORTED
+ * and writes nothing. */
 typedef struct occam_attend_args {
   int32_t layer;
   int32_t dtype;
@@ -543,8 +547,8 @@ int occam_cache_attend(const occam_cache* cache, const occam_attend_args* args, 
                        size_t workspace_bytes, occam_stream_t stream);
 
 /* Sequence dst[i], which must be empty, becomes a copy of src[i] (a src may
- * be listed more than once, but not as a dst): full pages are shared, a last page that is not
- * full is copied in every layer. */
+ * be listed more than once, but not as a dst): full pages are shared, a last
+ * page that is not full is copied in every layer. */
 int occam_cache_fork(const occam_cache* cache, int32_t n, const int32_t* src, const int32_t* dst, void* workspace,
                      size_t workspace_bytes, occam_stream_t stream);
 

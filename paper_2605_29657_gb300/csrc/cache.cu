@@ -758,7 +758,9 @@ int occam_cache_extend(const occam_cache* cache, int32_t n, const int32_t* seqs,
   PlanParams p = plan_params(cache, workspace, w, n);
   p.a = seqs;
   p.b = counts;
-  return launch_after(extend_kernel, dim3(1), kPlanThreads, 0, reinterpret_cast<cudaStream_t>(stream), p) ? last_error() : OCCAM_ERR_CUDA;
+  return launch_after(extend_kernel, dim3(1), kPlanThreads, 0, reinterpret_cast<cudaStream_t>(stream), p)
+             ? last_error()
+             : OCCAM_ERR_CUDA;
 }
 
 int occam_cache_append(const occam_cache* cache, int32_t layer, int32_t dtype, int64_t total_rows, const void* k,

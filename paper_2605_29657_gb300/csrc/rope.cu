@@ -201,6 +201,8 @@ extern "C" int occam_rope(int32_t dtype, int64_t rows, int32_t dim, int32_t rot,
     if (!t.src || !t.dst || t.heads < 1 || t.heads > 65535 || t.src_row < 0 || t.src_head < 0 || t.dst_row < 0 || t.dst_head < 0)
       return OCCAM_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(t.src) | reinterpret_cast<uintptr_t>(t.dst)) & (es - 1)) return OCCAM_ERR_INVALID_ARG;
+    // no value of dst has two places to come from
+    if ((rows > 1 && t.dst_row < dim) || (t.heads > 1 && t.dst_head < dim)) return OCCAM_ERR_INVALID_ARG;
     // in place means the same strides: a row's values are read before they are written
     if (t.src == t.dst && (t.src_row != t.dst_row || t.src_head != t.dst_head)) return OCCAM_ERR_INVALID_ARG;
     p.t[i] = t;
