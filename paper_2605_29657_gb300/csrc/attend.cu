@@ -38,7 +38,7 @@ using namespace occam;
 namespace {
 
 constexpr int kTile = 32;   // keys of a unit
-constexpr int kOver = 3;    // beginning and ending an item takes as long as this many units
+constexpr int kOver = 16;    // beginning and ending an item takes as long as this many units
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr int kFewRows = 32;  // query rows of a key head this file's kernel is used for
@@ -555,14 +555,12 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
       }
     }
     if (!whole) {
-      __threadfence();
       __syncthreads();
       const int2 who = item_stretches<kOver>(line, x0);
       const int first = who.x, last = who.y;
-      if (threadIdx.x == 0) sh_last = atomicAdd(&p.counters[first], 1) == last - first;
+      if (threadIdx.x == 0) sh_last = arrive_count(&p.counters[first]) == last - first;
       __syncthreads();
       if (sh_last) {
-        __threadfence();
         if (threadIdx.x == 0) p.counters[first] = 0;
         // Weights of the parts (a warp a row, a lane a part), then the sums, all of a
         // block's parts in flight; the partial sums of this CTA's warps are done with.

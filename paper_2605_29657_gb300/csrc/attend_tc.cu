@@ -870,14 +870,12 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
       }
     }
     if (!done) {
-      __threadfence();
       TC_MEET();
       const int2 who = item_stretches<kOver>(sh.line, x);
       const int first = who.x, last = who.y;
-      if (threadIdx.x == 0) sh.last = atomicAdd(&p.counters[first], 1) == last - first;
+      if (threadIdx.x == 0) sh.last = arrive_count(&p.counters[first]) == last - first;
       TC_MEET();
       if (sh.last) {
-        __threadfence();
         if (threadIdx.x == 0) p.counters[first] = 0;
         if (mine) {
           // Lane l has row l's maximum, sum and weights; then the warp goes through its
