@@ -38,10 +38,17 @@ using namespace occam;
 namespace {
 
 constexpr int kTile = 32;   // keys of a unit
-constexpr int kOver = 16;    // beginning and ending an item takes as long as this many units
+// What beginning and ending an item costs, in units (64 single tokens, 37 k units:
+// 3: 80 us, 8: 69, 16: 65, 32: 67, 48: 74; the first copies' way through
+// the busy memory system is most of it).
+constexpr int kOver = 16;
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
-constexpr int kFewRows = 32;  // query rows of a key head this file's kernel is used for
+// Query rows of a key head this file's kernel is used for. Caches of 2,300 tokens, 8
+// key heads; here / on tcgen05 (whose tile has 256 rows whatever is in them):
+// 64 sequences 8 rows 69 / 176 us, 16: 97 / 179, 32: 169 / 180, 48: 237 / 181;
+// 8 sequences 16 rows 27 / 43 us, 32: 37 / 43, 48: 46 / 43.
+constexpr int kFewRows = 32;
 constexpr float kRhoKeep = 1.f / 64.f;           // P is scaled down by v's scales at most this far
 constexpr float kRhoSpan = 8.6736174e-19f;       // 2^-60
 
@@ -156,7 +163,9 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
   for (int d = threadIdx.x; d < D; d += kThreads) sh_nan[d] = 0x7fffffff;
   pdl_wait();
   Line line;
-  const LinePart mine = attend_line<R, kTile, kOver, kThreads>(p, kOver + kWarps, sh, line);
+  // (a stretch has a tile a warp at least: one sequence of 2,300 tokens takes 12.5 us, with two
+  // tiles a warp 13.6, with five 17.8)
+  const LinePart mine = attend_line<R, kTile, kOver, kThreads>(p, kWarps, sh, line);
   if (line.units == 0 || (int)blockIdx.x >= line.stretches) return;
   Stretch w;
   attend_find<R, kTile, kOver, kThreads>(p, line, mine, blockIdx.x, sh, w);
