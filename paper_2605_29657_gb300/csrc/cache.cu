@@ -97,6 +97,27 @@ __device__ __forceinline__ float amax8(uint4 r) {
   return BF16 ? __uint_as_float(m << 16) : __half2float(__ushort_as_half((unsigned short)m));
 }
 
+// 8 values to codes. (A scale that is no power of two comes only with a cache whose scales the
+// caller made: by division, kept out of the way of the others.)
+template <bool BF16>
+__device__ __forceinline__ uint2 codes8(uint4 r, float inv) {
+  float f[8];
+  unpack8<BF16>(r, f);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f[j] *= inv;
+  const float lo[4] = {f[0], f[1], f[2], f[3]}, hi[4] = {f[4], f[5], f[6], f[7]};
+  return make_uint2(f32_codes4(lo), f32_codes4(hi));
+}
+template <bool BF16>
+__device__ __noinline__ uint2 codes8_by_division(uint4 r, float scale) {
+  float f[8];
+  unpack8<BF16>(r, f);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f[j] /= scale;
+  const float lo[4] = {f[0], f[1], f[2], f[3]}, hi[4] = {f[4], f[5], f[6], f[7]};
+  return make_uint2(f32_codes4(lo), f32_codes4(hi));
+}
+
 // MAXV: 8-value vectors a thread holds of a block (128 threads; page_tokens * D / 8 / 128 at most).
 // grid: x over (head, K or V), y and z over slots.
 template <bool BF16, int D, int MAXV>
@@ -170,17 +191,12 @@ __global__ void __launch_bounds__(128) append_kernel(AppendParams p) {
     }
   }
   const bool exact = is_pow2(now);
-  const float inv = exact ? 1.f / now : 0.f;
+  const float inv = 1.f / now;
 #pragma unroll
   for (int q = 0; q < MAXV; ++q) {
-    if (q * 128 + (int)threadIdx.x < nv) {
-      float f[8];
-      unpack8<BF16>(x[q], f);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = exact ? f[j] * inv : f[j] / now;
-      const float lo[4] = {f[0], f[1], f[2], f[3]}, hi[4] = {f[4], f[5], f[6], f[7]};
-      *reinterpret_cast<uint2*>(codes + (t0 + tv + q * (128 / vpr)) * D + c * 8) = make_uint2(f32_codes4(lo), f32_codes4(hi));
-    }
+    if (q * 128 + (int)threadIdx.x < nv)
+      *reinterpret_cast<uint2*>(codes + (t0 + tv + q * (128 / vpr)) * D + c * 8) =
+          exact ? codes8<BF16>(x[q], inv) : codes8_by_division<BF16>(x[q], now);
   }
   if (threadIdx.x == 0) *scale = now;
 }
@@ -662,12 +678,14 @@ __global__ void __launch_bounds__(128) compact_move_kernel(MoveParams p) {
           if (q * 128 + (int)threadIdx.x < nv) {
             uint32_t* w = reinterpret_cast<uint32_t*>(&x[q]);
             if (s[q] != now) {
+              // (finite, so that a code of 0 stays 0 under any scale)
+              const float ratio = fminf(s[q] * inv, 3.4e38f);
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
                 float f[4];
                 codes4_f32(w[j], f);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) f[k] = f[k] * s[q] * inv;
+                for (int k = 0; k < 4; ++k) f[k] *= ratio;
                 w[j] = f32_codes4(f);
               }
             }
