@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
   __shared__ int64_t sh[kWarps + 4];
   __shared__ float sh_m[kWarps][R], sh_l[kWarps][R];
   __shared__ int sh_last;
-  __shared__ int sh_nan[D];  // first token with a NaN in that dim, of those taken out
+  __shared__ int sh_nan[2][D];  // first token with a NaN in that dim, of those taken out; by turns of segments
   // Each warp's copies: two slots of keys and two of values, 32 rows each. At the end
   // of a segment the warp's sums take their place.
   constexpr int kSlot = kTile * D, kWarpBytes = 4 * kSlot;
@@ -162,7 +162,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
   uint32_t turn = 0;              // tiles this warp has taken
   if (TMA && threadIdx.x < kWarps * 4) mbar_init(&sh_bar[0][0] + threadIdx.x, 1);
   if (TMA) fence_mbar_init();
-  for (int d = threadIdx.x; d < D; d += kThreads) sh_nan[d] = 0x7fffffff;
+  for (int d = threadIdx.x; d < 2 * D; d += kThreads) sh_nan[0][d] = 0x7fffffff;
   pdl_wait();
   Line line;
   // (a stretch has a tile a warp at least: one sequence of 2,300 tokens takes 12.5 us, with two
@@ -173,6 +173,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
   attend_find<R, kTile, kOver, kThreads>(p, line, mine, blockIdx.x, sh, w);
   Walk x0;
   if (!walk_begin<R, kTile, kOver>(p, w, x0)) return;
+  int* nan_first = sh_nan[0];
   do {
     const SeqInfo s = x0.s;
     const int i = x0.i, h = x0.h, rt = x0.rt, tiles = x0.tiles, ta = x0.ta, tb = x0.tb;
@@ -454,7 +455,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
 #pragma unroll
               for (int x = 0; x < VW; ++x) {
                 if (!((seen >> row) & 1)) vr[r][x] = 0;
-                note_nans(vr[r][x], tile * kTile + row, order<D>(g) * (4 * VW) + 4 * x, sh_nan);
+                note_nans(vr[r][x], tile * kTile + row, order<D>(g) * (4 * VW) + 4 * x, nan_first);
               }
             }
           }
@@ -551,7 +552,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
       const int row = rt * R + r, j = div_group(p, row);
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        if (sh_nan[d + q] < (p.causal ? s.len - s.rows + j + 1 : s.len)) v[q] = __int_as_float(0x7fc00000);
+        if (nan_first[d + q] < (p.causal ? s.len - s.rows + j + 1 : s.len)) v[q] = __int_as_float(0x7fc00000);
       if (whole) {
         const int64_t to = (s.row0 + j) * p.H + h * p.G + row - j * p.G;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -639,7 +640,9 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
     }
     if (TMA) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the next copies come by another proxy
     __syncthreads();  // the shared results are free again
-    for (int d = threadIdx.x; d < D; d += kThreads) sh_nan[d] = 0x7fffffff;
+    // (the next segment has the other notes: its first warp may be there before the last one clears these)
+    for (int d = threadIdx.x; d < D; d += kThreads) nan_first[d] = 0x7fffffff;
+    nan_first = nan_first == sh_nan[0] ? sh_nan[1] : sh_nan[0];
   } while (walk_next<R, kTile, kOver>(p, w, x0));
 }
 
