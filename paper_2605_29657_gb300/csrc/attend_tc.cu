@@ -644,36 +644,45 @@ __device__ __forceinline__ float load_queries(const AttendParams& p, const Walk&
   }
   cp_async_commit();
   cp_async_wait<0>();
-  float scale = 0.f;
+  // The largest magnitude of each row (magnitudes order as integers; a NaN does not matter, its
+  // row is NaN): this lane's share of the N = LPR rows, then exchanges that halve the rows a lane
+  // has and double the lanes it has seen, until lane c has row c's (of its `sub`).
+  static_assert(N == LPR, "");
+  uint32_t top[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint4 v = *reinterpret_cast<const uint4*>(piece(i));
+    const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+    top[i] = max(m & 0xffffu, m >> 16);
+  }
+#pragma unroll
+  for (int n = N / 2; n > 0; n >>= 1) {
+    const bool high = c & n;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const uint32_t give = high ? top[i] : top[i + n], keep = high ? top[i + n] : top[i];
+      top[i] = max(keep, __shfl_xor_sync(0xffffffffu, give, n));
+    }
+  }
+  // a row's power of two: largest value in [2^14, 2^15), as in attend.cu
+  const float amax = BF16 ? __uint_as_float(top[0] << 16) : __half2float(__ushort_as_half((unsigned short)top[0]));
+  const int e = amax == 0.f ? 0 : max((__float_as_int(amax) >> 23) - 127 - 14, -112);
 #pragma unroll 4
   for (int i = 0; i < N; ++i) {
     uint4* at = reinterpret_cast<uint4*>(piece(i));
     const uint4 v = *at;
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    float f[8], amax = 0.f;
+    const float up = __int_as_float((127 - __shfl_sync(0xffffffffu, e, sub * LPR + i)) << 23);
+    uint32_t r[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      if (BF16) {
-        f[2 * k] = bf16_lo(w[k]);
-        f[2 * k + 1] = bf16_hi(w[k]);
-      } else {
-        const float2 h2 = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
-        f[2 * k] = h2.x;
-        f[2 * k + 1] = h2.y;
-      }
-      amax = tc::fmax3(amax, fabsf(f[2 * k]), fabsf(f[2 * k + 1]));
+      const float2 f = BF16 ? make_float2(bf16_lo(w[k]), bf16_hi(w[k])) : __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
+      r[k] = pack_f16(f.x * up, f.y * up);
     }
-    // (magnitudes order as integers; a NaN does not matter, its row is NaN)
-    amax = __uint_as_float(__reduce_max_sync(((1u << LPR) - 1u) << (sub * LPR), __float_as_uint(amax)));
-    // largest value in [2^14, 2^15), as in attend.cu
-    int e = (__float_as_int(amax) >> 23) - 127 - 14;
-    e = amax == 0.f ? 0 : max(e, -112);
-    const float up = __int_as_float((127 - e) << 23);
-    *at = make_uint4(pack_f16(f[0] * up, f[1] * up), pack_f16(f[2] * up, f[3] * up), pack_f16(f[4] * up, f[5] * up),
-                     pack_f16(f[6] * up, f[7] * up));
-    const float down = __shfl_sync(0xffffffffu, __int_as_float((127 + e) << 23), (lane % RPI) * LPR);
-    if (lane / RPI == i) scale = down;
+    *at = make_uint4(r[0], r[1], r[2], r[3]);
   }
+  // lane l's own row is row l % RPI of the loop's l / RPI-th
+  const float scale = __int_as_float((127 + __shfl_sync(0xffffffffu, e, (lane % RPI) * LPR + lane / RPI)) << 23);
   return scale * p.scale_log2;
 }
 
