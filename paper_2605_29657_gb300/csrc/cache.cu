@@ -209,21 +209,22 @@ __global__ void __launch_bounds__(128, MAXV == 8 ? 9 : 1) append_kernel(AppendPa
 
 // ---------------------------------------------------------------- page bookkeeping (one CTA)
 
+// The slots a call names, a bit each.
+constexpr int kSlotWords = 65536 / 32;
+// (before the kernel waits for the one before it)
+__device__ __forceinline__ void clear_slots(const CacheDev& c, uint32_t* bits) {
+  for (int i = threadIdx.x; i < (c.max_seqs + 31) / 32; i += blockDim.x) bits[i] = 0;
+  __syncthreads();
+}
 // Marks the n slots of `seqs`; true (block-wide) if all are in range and listed once.
-__device__ bool mark_slots(const CacheDev& c, const int32_t* seqs, int n, int32_t* marks) {
+__device__ bool mark_slots(const CacheDev& c, const int32_t* seqs, int n, uint32_t* bits) {
   int bad = 0;
   for (int i = threadIdx.x; i < n; i += blockDim.x) {
     const int s = seqs[i];
-    if ((unsigned)s >= (unsigned)c.max_seqs || atomicAdd(&marks[s], 1) != 0) bad = 1;
+    const uint32_t bit = 1u << (s & 31);
+    if ((unsigned)s >= (unsigned)c.max_seqs || (atomicOr(&bits[s >> 5], bit) & bit)) bad = 1;
   }
   return __syncthreads_or(bad) == 0;
-}
-__device__ void unmark_slots(const CacheDev& c, const int32_t* seqs, int n, int32_t* marks) {
-  __syncthreads();
-  for (int i = threadIdx.x; i < n; i += blockDim.x) {
-    const int s = seqs[i];
-    if ((unsigned)s < (unsigned)c.max_seqs) marks[s] = 0;
-  }
 }
 
 // Writes the lowest `want` free pages, ascending, to list; returns how many
@@ -266,7 +267,6 @@ struct PlanParams {
   int n;
   const int32_t* a;  // extend: seqs; fork: src; compact: seqs
   const int32_t* b;  // extend: counts; fork: dst
-  int32_t* marks;
   int32_t* free_list;
   int2* new_pages;   // fork: (from, to) of a copied page, or (-1, -1)
   // compact
@@ -280,9 +280,11 @@ __device__ __forceinline__ int pages_of(int tokens, const CacheDev& c) { return 
 
 __global__ void __launch_bounds__(kPlanThreads) extend_kernel(PlanParams p) {
   __shared__ int tmp[33];
+  __shared__ uint32_t slots[kSlotWords];
+  clear_slots(p.c, slots);
   pdl_wait();
   const CacheDev& c = p.c;
-  const bool fine = mark_slots(c, p.a, p.n, p.marks);
+  const bool fine = mark_slots(c, p.a, p.n, slots);
   int bad = 0, full = 0;
   int64_t total = 0;
   if (fine) {
@@ -336,14 +338,15 @@ __global__ void __launch_bounds__(kPlanThreads) extend_kernel(PlanParams p) {
   } else if (threadIdx.x == 0) {
     set_status(c.status, bad ? OCCAM_ERR_INVALID_ARG : OCCAM_ERR_CAPACITY);
   }
-  unmark_slots(c, p.a, p.n, p.marks);
 }
 
 __global__ void __launch_bounds__(kPlanThreads) fork_kernel(PlanParams p) {
   __shared__ int tmp[33];
+  __shared__ uint32_t slots[kSlotWords];
+  clear_slots(p.c, slots);
   pdl_wait();
   const CacheDev& c = p.c;
-  const bool fine = mark_slots(c, p.b, p.n, p.marks);
+  const bool fine = mark_slots(c, p.b, p.n, slots);
   int bad = 0;
   int64_t total = 0;
   if (fine) {
@@ -353,7 +356,7 @@ __global__ void __launch_bounds__(kPlanThreads) fork_kernel(PlanParams p) {
       if (i < p.n) {
         const int a = p.a[i], b = p.b[i];
         p.new_pages[i] = make_int2(-1, -1);
-        if ((unsigned)a >= (unsigned)c.max_seqs || p.marks[a] != 0 || c.length[b] != 0 || c.length[a] < 0 ||
+        if ((unsigned)a >= (unsigned)c.max_seqs || ((slots[a >> 5] >> (a & 31)) & 1) || c.length[b] != 0 || c.length[a] < 0 ||
             c.length[a] > c.max_pages * c.T)
           bad = 1;
         else
@@ -409,7 +412,6 @@ __global__ void __launch_bounds__(kPlanThreads) fork_kernel(PlanParams p) {
     for (int i = threadIdx.x; i < p.n; i += blockDim.x) p.new_pages[i] = make_int2(-1, -1);
     if (threadIdx.x == 0) set_status(c.status, bad ? OCCAM_ERR_INVALID_ARG : OCCAM_ERR_CAPACITY);
   }
-  unmark_slots(c, p.b, p.n, p.marks);
 }
 
 // Copies the pages fork_kernel listed: grid (pairs, layers, 2 * chunks), 16 KB a CTA.
@@ -516,9 +518,11 @@ __global__ void __launch_bounds__(1024) compact_count_kernel(CountParams p) {
 // New page tables: head[i] = index of sequence i's first new page in free_list.
 __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(PlanParams p) {
   __shared__ int tmp[33];
+  __shared__ uint32_t slots[kSlotWords];
+  clear_slots(p.c, slots);
   pdl_wait();
   const CacheDev& c = p.c;
-  const bool fine = mark_slots(c, p.a, p.n, p.marks);
+  const bool fine = mark_slots(c, p.a, p.n, slots);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int bad = 0;
   int64_t total = 0;
@@ -576,7 +580,6 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(PlanParams p
       set_status(c.status, bad ? OCCAM_ERR_INVALID_ARG : OCCAM_ERR_CAPACITY);
     }
   }
-  unmark_slots(c, p.a, p.n, p.marks);
 }
 
 // the largest |code| of 16 (NaN codes passed over): magnitudes order as integers
@@ -718,7 +721,6 @@ PlanParams plan_params(const occam_cache* c, void* ws, const CacheWs& w, int n) 
   PlanParams p{};
   p.c = cache_dev(c, ws, w);
   p.n = n;
-  p.marks = ws_at<int32_t>(ws, w.marks);
   p.free_list = ws_at<int32_t>(ws, w.free_list);
   p.new_pages = ws_at<int2>(ws, w.new_pages);
   p.count = ws_at<int32_t>(ws, w.count);

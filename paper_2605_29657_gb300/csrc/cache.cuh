@@ -22,10 +22,10 @@ constexpr size_t kAttendPartRows =
 
 inline size_t cache_align(size_t x) { return (x + 255) / 256 * 256; }
 
-// Byte offsets from the workspace base. Everything but status, counters and
-// marks is written before it is read within each call.
+// Byte offsets from the workspace base. Everything but status and counters
+// is written before it is read within each call.
 struct CacheWs {
-  size_t status, counters, marks;  // zero between calls
+  size_t status, counters;  // zero between calls
   size_t count, lead, head, new_pages, free_list, old_table, list, part_o, part_ml;
   size_t total;
 };
@@ -40,7 +40,6 @@ inline CacheWs cache_ws(const occam_cache* c, int64_t max_tokens) {
   };
   w.status = take(8);
   w.counters = take((size_t)kAttendCtas * 4);
-  w.marks = take((size_t)c->max_seqs * 4);
   w.count = take((size_t)c->max_seqs * 4);
   w.lead = take((size_t)c->max_seqs * 4);
   w.head = take((size_t)(c->max_seqs + 1) * 4);
