@@ -29,7 +29,6 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
-#include <mutex>
 
 #include "attend.cuh"
 #include "attend_tc.cuh"
@@ -678,15 +677,13 @@ int launch_rows(const AttendParams& p, cudaStream_t st) {
 }  // namespace
 
 bool occam::encode_blocks(CUtensorMap* m, const CacheDev& c, const void* codes, int dim, int box_rows, bool swizzle) {
-  static PFN_cuTensorMapEncodeTiled_v12000 enc = nullptr;
-  static std::once_flag once;
-  std::call_once(once, [] {
+  static const PFN_cuTensorMapEncodeTiled_v12000 enc = [] {
     void* f = nullptr;
     cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      enc = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
-  });
+    const bool found = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) ==
+                           cudaSuccess && q == cudaDriverEntryPointSuccess;
+    return found ? reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f) : nullptr;
+  }();
   if (!enc) return false;
   const cuuint64_t rows = (cuuint64_t)c.heads * c.T;
   cuuint64_t gdim[3] = {(cuuint64_t)dim, rows, (cuuint64_t)c.layers * c.pages};

@@ -3,7 +3,7 @@
 //
 // The same running softmax as attend.cu, for 256 query rows (token, head of
 // the group) against tiles of 128 keys. 4 D operations and one exponential a
-// (row, key). A prefix of 8,257 tokens, 32 query and 8 key heads of 128 dims, takes 0.55 ms,
+// (row, key). A prefix of 8,257 tokens, 32 query and 8 key heads of 128 dims, takes 0.545 ms,
 // 1.0 PFLOP/s: 3,900 cycles a tile where the products alone need 2,050 and shared
 // memory's traffic (codes, their f16 form, operands: 384 KB) 3,070; bound by the
 // round scores -> softmax -> P -> products, of which two halves a row tile are under way.
