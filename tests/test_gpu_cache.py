@@ -288,6 +288,23 @@ def test_attend_nan_counts_for_rows_that_see_it(T, dim, G, lengths, rows):
     attend_case(c, seqs, rows, G, keep=keep, keep_off=offs(lengths))
 
 
+@pytest.mark.parametrize("T,dim", [(16, 128), (64, 128), (128, 64)])
+@pytest.mark.parametrize("rows", [1, 7, 70])
+def test_attend_long_caches_mostly_hidden(T, dim, rows):
+    """Many tiles with few seen tokens, whole tiles without one, flags that end inside the sequence."""
+    lengths, g = [1500, 700, 129], torch.Generator().manual_seed(T + rows)
+    c, seqs = filled(T, dim, 1, lengths, T)
+    keep, off = [], [0]
+    for n in lengths:
+        m = n - rows // 2
+        f = torch.rand(m, generator=g) < 0.1
+        f[m // 4:m // 2] = False
+        keep += f.int().tolist()
+        off.append(off[-1] + m)
+    for causal in (True, False):
+        attend_case(c, seqs, [rows] * 3, 4, seed=T, causal=causal, keep=keep, keep_off=off)
+
+
 @pytest.mark.parametrize("T,rows", [(16, 1), (64, 1), (16, 60), (128, 200)])
 def test_attend_scales_far_apart(T, rows):
     """Scales of v far apart, the large ones where the probabilities are 0: what is seen keeps its digits."""
