@@ -485,7 +485,10 @@ int occam_cache_workspace_size(const occam_cache* cache, int64_t max_tokens, siz
 
 /* Makes room: sequence seqs[i] grows by counts[i] >= 0 tokens (device int32). Pages
  * are taken as needed and length is raised; the new tokens' codes are to be
- * written by occam_cache_append, layer by layer. */
+ * written by occam_cache_append, layer by layer, with the same workspace.
+ * After a call that recorded an error, extend and append calls with that workspace do
+ * nothing until its status has been read: an append queued behind it would take
+ * its rows for tokens that are held already. */
 int occam_cache_extend(const occam_cache* cache, int32_t n, const int32_t* seqs, const int32_t* counts,
                        void* workspace, size_t workspace_bytes, occam_stream_t stream);
 
@@ -499,7 +502,9 @@ int occam_cache_extend(const occam_cache* cache, int32_t n, const int32_t* seqs,
  * a shift of the exponent; a block that holds older tokens keeps at least its
  * scale, and when it grows their codes are rounded again to the new one.
  * Codes are rounded to nearest, ties to even; infinities become +-448 s, NaN
- * stays NaN. Repeating a call changes nothing. Rows must be 16-byte aligned. */
+ * stays NaN. Repeating a call changes nothing. Rows must be 16-byte aligned.
+ * A page that another sequence holds too is not written (OCCAM_ERR_INVALID_ARG):
+ * append to a sequence before it is forked, and extend a fork before appending to it. */
 int occam_cache_append(const occam_cache* cache, int32_t layer, int32_t dtype, int64_t total_rows, const void* k,
                        int64_t k_row, const void* v, int64_t v_row, int32_t n, const int32_t* seqs,
                        const int64_t* row_off, void* workspace, size_t workspace_bytes, occam_stream_t stream);

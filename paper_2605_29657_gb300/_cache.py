@@ -220,7 +220,8 @@ def _vector(t, dtype, n: int | None, name: str) -> torch.Tensor:
 
 
 def occam_cache_extend(cache: PagedCache, seqs, counts, ws=None, stream=None) -> None:
-    """Sequence seqs[i] grows by counts[i] tokens: pages are taken and lengths raised."""
+    """Sequence seqs[i] grows by counts[i] tokens: pages are taken and lengths raised. After a
+    call that recorded an error, extend and append with that workspace do nothing until status() is read."""
     wp, wn = _workspace(cache, ws)
     n = _vector(seqs, torch.int32, None, "seqs").shape[0]
     _vector(counts, torch.int32, n, "counts")
@@ -231,7 +232,7 @@ def occam_cache_extend(cache: PagedCache, seqs, counts, ws=None, stream=None) ->
 def occam_cache_append(cache: PagedCache, layer: int, k, v, seqs, row_off, ws=None, stream=None) -> None:
     """Writes rows row_off[i] .. row_off[i+1] of k and v [rows, heads, dim]
     (bfloat16 or float16, rows may be strided) as the last tokens of sequence
-    seqs[i] in one layer."""
+    seqs[i] in one layer. Pages that other sequences hold too are not written."""
     wp, wn = _workspace(cache, ws)
     _rows_tensor(k, "k", _ROWS, cache.heads, cache.dim)
     _rows_tensor(v, "v", (k.dtype,), cache.heads, cache.dim)

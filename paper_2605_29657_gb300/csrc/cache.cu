@@ -130,6 +130,7 @@ template <bool BF16, int D, int MAXV>
 __global__ void __launch_bounds__(128, MAXV == 8 ? 9 : 1) append_kernel(AppendParams p) {
   __shared__ float r[4];
   pdl_wait();
+  const int refused = p.c.status[1] & kRefused;  // (no CTA of this launch sets it)
   const int T = p.c.T, H = p.c.heads;
   const int kv = blockIdx.x & 1, h = (int)(blockIdx.x >> 1);
   const int64_t w = (int64_t)blockIdx.z * gridDim.y + blockIdx.y;
@@ -139,6 +140,7 @@ __global__ void __launch_bounds__(128, MAXV == 8 ? 9 : 1) append_kernel(AppendPa
   const int seq = p.seqs[i];
   int len = -1;
   if ((unsigned)seq < (unsigned)p.c.max_seqs) len = p.c.length[seq];
+  if (refused) return;
   if (local < 0) return;  // rows before row_off[0] belong to no sequence
   const bool good = r0 >= 0 && r1 >= r0 && r1 <= p.total_rows && len >= r1 - r0 &&
                     len <= (int64_t)p.c.max_pages * T;
@@ -157,6 +159,7 @@ __global__ void __launch_bounds__(128, MAXV == 8 ? 9 : 1) append_kernel(AppendPa
     if (threadIdx.x == 0) set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
     return;
   }
+  const int holders = p.c.refs[page];
   const int64_t block = ((int64_t)p.layer * p.c.pages + page) * H;
   const int64_t ld = kv ? p.v_row : p.k_row;
   constexpr int vpr = D / 8;  // vectors of a row
@@ -167,6 +170,10 @@ __global__ void __launch_bounds__(128, MAXV == 8 ? 9 : 1) append_kernel(AppendPa
 #pragma unroll
   for (int q = 0; q < MAXV; ++q)
     if (q * 128 + (int)threadIdx.x < nv) x[q] = ldg_stream(src + q * step + h * D);
+  if (holders != 1) {  // other sequences hold the page (the same in every thread)
+    if (threadIdx.x == 0) set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
+    return;
+  }
   uint8_t* codes = (kv ? p.c.v : p.c.k) + (block + h) * T * D;
   float* scale = (kv ? p.c.v_scale : p.c.k_scale) + block + h;
   float amax = 0.f;
@@ -284,6 +291,7 @@ __global__ void __launch_bounds__(kPlanThreads) extend_kernel(PlanParams p) {
   clear_slots(p.c, slots);
   pdl_wait();
   const CacheDev& c = p.c;
+  if (c.status[1] & kRefused) return;
   const bool fine = mark_slots(c, p.a, p.n, slots);
   int bad = 0, full = 0;
   int64_t total = 0;
@@ -337,6 +345,7 @@ __global__ void __launch_bounds__(kPlanThreads) extend_kernel(PlanParams p) {
     }
   } else if (threadIdx.x == 0) {
     set_status(c.status, bad ? OCCAM_ERR_INVALID_ARG : OCCAM_ERR_CAPACITY);
+    atomicOr(&c.status[1], kRefused);
   }
 }
 

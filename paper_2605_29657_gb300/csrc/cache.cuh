@@ -112,6 +112,11 @@ struct CacheDev {
   int32_t* status;
 };
 
+// Set in the word after the status word by an extend that records an error; both are cleared
+// when the status is read. Until then nothing grows and nothing is appended: the rows
+// of an append behind it would land on the last tokens that are held.
+constexpr int32_t kRefused = 1 << 30;
+
 inline CacheDev cache_dev(const occam_cache* c, void* ws, const CacheWs& w) {
   CacheDev d;
   d.layers = c->layers;

@@ -508,3 +508,50 @@ def test_refusals():
             f()
             print("not refused", n)
     R.assert_codes(c, before)
+
+
+def rows_of(n, heads, dim, seed):
+    return torch.randn((n, heads, dim), generator=torch.Generator().manual_seed(seed)).bfloat16().cuda()
+
+
+def test_append_behind_a_refused_extend_changes_nothing():
+    """A full pool: the extend is refused for all its sequences, and the calls queued behind it write
+    nothing, whether the page at the end is a sequence's own or shared, until the status is read."""
+    import paper_2605_29657_gb300 as occ
+    c = make(layers=2, pages=5, heads=2, dim=64, T=16, seqs=4, max_pages=4)
+    ref = R.Cache(c)
+    grow(c, ref, [0, 1], [32, 20], 0)
+    occ.occam_cache_fork(c, dev([0]), dev([2]))
+    ref.fork([0], [2])
+    occ.occam_cache_extend(c, dev([3]), dev([10]))  # the last page
+    ref.extend([3], [10])
+    x, one = rows_of(3, 2, 64, 1), dev([1, 1, 1])
+    s, off = dev([0, 1, 2]), dev([0, 1, 2, 3], torch.int64)
+    for _ in range(2):  # a step that does not fit, and the next one
+        occ.occam_cache_extend(c, s, one)
+        for layer in range(2):
+            occ.occam_cache_append(c, layer, x, x, s, off)
+    occ.occam_cache_release(c, dev([3]))  # room again, but nobody has looked
+    ref.release([3])
+    occ.occam_cache_extend(c, dev([1]), dev([1]))
+    occ.occam_cache_append(c, 0, x[:1], x[:1], dev([1]), dev([0, 1], torch.int64))
+    assert c.status() == 2
+    R.assert_codes(c, ref)
+    grow(c, ref, [1, 2], [1, 1], 2)
+    R.assert_codes(c, ref)
+
+
+def test_append_writes_no_shared_page():
+    import paper_2605_29657_gb300 as occ
+    c = make(layers=1, pages=8, heads=2, dim=64, T=16, seqs=4, max_pages=4)
+    ref = R.Cache(c)
+    grow(c, ref, [0, 3], [32, 5], 0)
+    occ.occam_cache_fork(c, dev([0, 3]), dev([1, 2]))
+    ref.fork([0, 3], [1, 2])
+    x = rows_of(3, 2, 64, 1)
+    for seqs, off in (([1], [0, 1]), ([0, 1], [0, 1, 2]), ([1], [0, 3])):  # not extended: the last rows are shared
+        occ.occam_cache_append(c, 0, x[:off[-1]], x[:off[-1]], dev(seqs), dev(off, torch.int64))
+        assert c.status() == 1
+        R.assert_codes(c, ref)
+    grow(c, ref, [1, 0, 2], [1, 2, 12], 2)
+    R.assert_codes(c, ref)
