@@ -234,8 +234,21 @@ __device__ bool mark_slots(const CacheDev& c, const int32_t* seqs, int n, uint32
   return __syncthreads_or(bad) == 0;
 }
 
+// The block's sum, to every thread. A call's page counts are added in 64 bits (a sequence may want
+// up to 2^27 pages); once the sum is known to fit the pool, 32 bits do. tmp: 32 words of shared memory.
+__device__ int64_t block_sum(int64_t x, int64_t* tmp) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  if ((threadIdx.x & 31) == 0) tmp[threadIdx.x >> 5] = x;
+  __syncthreads();
+  int64_t sum = 0;
+  for (int w = 0; w < kPlanThreads / 32; ++w) sum += tmp[w];
+  __syncthreads();
+  return sum;
+}
+
 // Writes the lowest `want` free pages, ascending, to list; returns how many
-// there are (want, or fewer if the pool has fewer). tmp: 33 ints of shared memory.
+// there are (want, 0 .. c.pages, or fewer if the pool has fewer). tmp: 33 ints of shared memory.
 __device__ int find_free(const CacheDev& c, int want, int32_t* list, int* tmp) {
   int found = 0;
   const bool vec = (reinterpret_cast<uintptr_t>(c.refs) & 15) == 0;
@@ -287,6 +300,7 @@ __device__ __forceinline__ int pages_of(int tokens, const CacheDev& c) { return 
 
 __global__ void __launch_bounds__(kPlanThreads) extend_kernel(PlanParams p) {
   __shared__ int tmp[33];
+  __shared__ int64_t sums[32];
   __shared__ uint32_t slots[kSlotWords];
   clear_slots(p.c, slots);
   pdl_wait();
@@ -296,29 +310,24 @@ __global__ void __launch_bounds__(kPlanThreads) extend_kernel(PlanParams p) {
   int bad = 0, full = 0;
   int64_t total = 0;
   if (fine) {
-    for (int base = 0; base < p.n; base += kPlanThreads) {
-      const int i = base + threadIdx.x;
-      int need = 0, t = 0;
-      if (i < p.n) {
-        const int s = p.a[i], add = p.b[i], len = c.length[s];
-        const int64_t to = (int64_t)len + add;
-        if (add < 0 || len < 0 || len > c.max_pages * c.T) {
-          bad = 1;
-        } else if (to > (int64_t)c.max_pages * c.T) {
-          full = 1;
-        } else {
-          need = pages_of((int)to, c) - pages_of(len, c);
-          // tokens go into a page of the sequence's own
-          if (add > 0 && (len & (c.T - 1))) {
-            const int pg = c.table[(int64_t)s * c.max_pages + (len >> c.log2T)];
-            if ((unsigned)pg >= (unsigned)c.pages || c.refs[pg] != 1) bad = 1;
-          }
+    for (int i = threadIdx.x; i < p.n; i += kPlanThreads) {
+      const int s = p.a[i], add = p.b[i], len = c.length[s];
+      const int64_t to = (int64_t)len + add;
+      if (add < 0 || len < 0 || len > c.max_pages * c.T) {
+        bad = 1;
+      } else if (to > (int64_t)c.max_pages * c.T) {
+        full = 1;
+      } else {
+        total += pages_of((int)to, c) - pages_of(len, c);
+        // tokens go into a page of the sequence's own
+        if (add > 0 && (len & (c.T - 1))) {
+          const int pg = c.table[(int64_t)s * c.max_pages + (len >> c.log2T)];
+          if ((unsigned)pg >= (unsigned)c.pages || c.refs[pg] != 1) bad = 1;
         }
       }
-      block_exclusive_scan(need, tmp, &t);
-      total += t;
     }
   }
+  total = block_sum(total, sums);
   bad = __syncthreads_or(bad || !fine);
   full = __syncthreads_or(full) || total > c.pages;
   const bool ok = !bad && !full && find_free(c, (int)total, p.free_list, tmp) == (int)total;
@@ -527,6 +536,7 @@ __global__ void __launch_bounds__(1024) compact_count_kernel(CountParams p) {
 // New page tables: head[i] = index of sequence i's first new page in free_list.
 __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(PlanParams p) {
   __shared__ int tmp[33];
+  __shared__ int64_t sums[32];
   __shared__ uint32_t slots[kSlotWords];
   clear_slots(p.c, slots);
   pdl_wait();
@@ -535,31 +545,34 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(PlanParams p
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int bad = 0;
   int64_t total = 0;
+  auto pages_wanted = [&](int i) { return max(pages_of(p.count[i], c) - p.lead[i], 0); };
   if (fine) {
-    for (int base = 0; base < p.n; base += kPlanThreads) {
-      const int i = base + threadIdx.x;
-      int need = 0, t = 0;
-      if (i < p.n) {
-        if (p.count[i] < 0)
-          bad = 1;
-        else
-          need = max(pages_of(p.count[i], c) - p.lead[i], 0);
-      }
-      const int at = (int)min(total, (int64_t)0x3fffffff) + block_exclusive_scan(need, tmp, &t);
-      if (i < p.n) p.head[i] = at;
-      total += t;
+    for (int i = threadIdx.x; i < p.n; i += kPlanThreads) {
+      if (p.count[i] < 0)
+        bad = 1;
+      else
+        total += pages_wanted(i);
     }
-    if (!__syncthreads_or(bad)) {
-      for (int i = warp; i < p.n; i += kPlanThreads / 32) {
-        const int s = p.a[i], m = pages_of(c.length[s], c);
-        for (int j = lane; j < m; j += 32)
-          if ((unsigned)c.table[(int64_t)s * c.max_pages + j] >= (unsigned)c.pages) bad = 1;
-      }
+  }
+  total = block_sum(total, sums);
+  if (fine && !__syncthreads_or(bad) && total <= c.pages) {
+    for (int i = warp; i < p.n; i += kPlanThreads / 32) {
+      const int s = p.a[i], m = pages_of(c.length[s], c);
+      for (int j = lane; j < m; j += 32)
+        if ((unsigned)c.table[(int64_t)s * c.max_pages + j] >= (unsigned)c.pages) bad = 1;
     }
   }
   bad = __syncthreads_or(bad || !fine);
   const bool ok = !bad && total <= c.pages && find_free(c, (int)total, p.free_list, tmp) == (int)total;
   if (ok) {
+    for (int base = 0, at = 0; base < p.n; base += kPlanThreads) {
+      const int i = base + threadIdx.x;
+      int sum = 0;
+      const int before = at + block_exclusive_scan(i < p.n ? pages_wanted(i) : 0, tmp, &sum);
+      if (i < p.n) p.head[i] = before;
+      at += sum;
+    }
+    __syncthreads();
     // pages leave their sequence before new ones come in: the new ones were
     // free at the start of the call, so the two sets do not meet
     for (int i = warp; i < p.n; i += kPlanThreads / 32) {

@@ -555,3 +555,24 @@ def test_append_writes_no_shared_page():
         R.assert_codes(c, ref)
     grow(c, ref, [1, 0, 2], [1, 2, 12], 2)
     R.assert_codes(c, ref)
+
+
+def test_page_counts_past_32_bits():
+    """1024 sequences that want 2^21 pages each, as many as the pool has: more than 32 bits count. The
+    calls record that the pool is too small and change nothing (the table alone is 8.6 GB)."""
+    import paper_2605_29657_gb300 as occ
+    n, pages, T = 1 << 10, 1 << 21, 16
+    c = occ.PagedCache(1, pages, 1, 64, n, pages, page_tokens=T, max_tokens=n)
+    seqs = dev(list(range(n)))
+    occ.occam_cache_extend(c, seqs, torch.full((n,), pages * T, dtype=torch.int32, device="cuda"))
+    assert c.status() == 2
+    assert not c.length.any() and not c.refs.any() and int(c.table.max()) == -1
+    # every sequence holds the whole pool and drops its first token
+    c.table.copy_(torch.arange(pages, dtype=torch.int32, device="cuda").expand(n, -1))
+    c.length.fill_(pages * T)
+    c.refs.fill_(n)
+    occ.occam_cache_compact(c, seqs, torch.zeros(n, dtype=torch.uint8, device="cuda"),
+                            torch.arange(n + 1, dtype=torch.int64, device="cuda"))
+    assert c.status() == 2
+    assert bool((c.length == pages * T).all()) and bool((c.refs == n).all())
+    assert all(torch.equal(row, torch.arange(pages, dtype=torch.int32, device="cuda")) for row in c.table[::93])
