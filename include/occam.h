@@ -528,7 +528,8 @@ int occam_cache_append(const occam_cache* cache, int32_t layer, int32_t dtype, i
  * largest row_off[i+1] - row_off[i] (it chooses the kernels; results are right
  * for any value). heads <= 64 * cache heads. A call of more than 2^31 - 2^16
  * tiles (32 keys x 16 query rows of a key head) records OCCAM_ERR_UNSUPPORTED
- * and writes nothing. */
+ * and writes nothing. After OCCAM_ERR_TIMEOUT the call's results are undefined; the
+ * workspace stays usable. */
 typedef struct occam_attend_args {
   int32_t layer;
   int32_t dtype;

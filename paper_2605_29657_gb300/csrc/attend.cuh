@@ -32,7 +32,7 @@ struct AttendParams {
   const int64_t* keep_off;
   float scale_log2;
   uint32_t g_mul, g_shift;  // x / G = x g_mul >> g_shift for 0 <= x < 2^31
-  int32_t* counters;  // per stretch: arrivals at an item that begins in it
+  int32_t* counters;  // per stretch: arrivals at an item that begins in it; at kAttendCtas: CTAs that have left
   float* part_o;
   float2* part_ml;
 };

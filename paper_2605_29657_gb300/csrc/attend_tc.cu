@@ -72,6 +72,7 @@ struct Shared {
   uint32_t tmem;
   int stop;            // a wait ran out
   int last;
+  int left;            // the last CTA to leave
   int any_nan[4];
   alignas(16) int nan_first[4][128];  // (first the scratch of attend_line: 8-byte words)
 };
@@ -889,7 +890,6 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
       if (threadIdx.x == 0) sh.last = arrive_count(&p.counters[first]) == last - first;
       TC_MEET();
       if (sh.last) {
-        if (threadIdx.x == 0) p.counters[first] = 0;
         if (mine) {
           // Lane l has row l's maximum, sum and weights; then the warp goes through its
           // rows, all lanes on one, the parts' loads in flight together. The weights are
@@ -983,6 +983,20 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
   } while (walk_next<kR, kK, kOver>(p, sh, x));
 }
 
+// A wait that ran out leaves items without their last arrival, so the last CTA to leave clears
+// the counters whatever they are: the next call on the workspace has to find zeros.
+// count_out: by the thread that makes the CTA's arrivals, after the last of them; true for the last CTA.
+// (Relaxed: the arrivals have returned their counts by then. And not at the very end, where its way
+// through the busy memory system is waited for: 4 us of a prefix of 8,257 tokens.)
+__device__ __forceinline__ int count_out(const AttendParams& p, int stretches) {
+  return atomicAdd(&p.counters[kAttendCtas], 1) == stretches - 1;
+}
+__device__ __forceinline__ void clear_counters(const AttendParams& p) {
+  static_assert(kAttendCtas <= kThreads, "a counter a thread");
+  if (threadIdx.x < kAttendCtas) p.counters[threadIdx.x] = 0;
+  if (threadIdx.x == 0) p.counters[kAttendCtas] = 0;
+}
+
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kThreads, 1)
     attend_tc_kernel(AttendParams p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
@@ -1004,7 +1018,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   attend_find<kR, kK, kOver, kThreads>(p, line, part, blockIdx.x, scan, w);
   {
     Walk x;
-    if (!walk_begin<kR, kK, kOver>(p, w, x)) return;  // no tile in the stretch: every role has at least one from here on
+    if (!walk_begin<kR, kK, kOver>(p, w, x)) {  // no tile in the stretch: every role has at least one from here on
+      if (threadIdx.x == 0) sh.left = count_out(p, line.stretches);
+      __syncthreads();
+      if (sh.left) clear_counters(p);
+      return;
+    }
   }
   if (threadIdx.x == 0) {
     sh.u0 = w.u0;
@@ -1049,6 +1068,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp < 8) {
     tc::setmaxnreg_inc<kRegSoftmax>();
     softmax_role<D, BF16>(p, sh, q_smem, tmem, warp >> 2);
+    if (threadIdx.x == 0) sh.left = count_out(p, sh.line.stretches);
   } else if (warp < 12) {
     tc::setmaxnreg_dec<kRegConvert>();
     convert_role<D>(p, sh, k_smem, v_smem, raw);
@@ -1070,6 +1090,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   }
   __syncthreads();
+  if (sh.left) clear_counters(p);
   if (warp == 12) tc::tmem_dealloc(tmem, 512);
 }
 

@@ -25,7 +25,7 @@ inline size_t cache_align(size_t x) { return (x + 255) / 256 * 256; }
 // Byte offsets from the workspace base. Everything but status and counters
 // is written before it is read within each call.
 struct CacheWs {
-  size_t status, counters;  // zero between calls
+  size_t status, counters;  // zero between calls (attention's counters: also after a wait that ran out)
   size_t count, lead, head, new_pages, free_list, old_table, list, part_o, part_ml;
   size_t total;
 };
@@ -39,7 +39,7 @@ inline CacheWs cache_ws(const occam_cache* c, int64_t max_tokens) {
     return o;
   };
   w.status = take(8);
-  w.counters = take((size_t)kAttendCtas * 4);
+  w.counters = take((size_t)(kAttendCtas + 1) * 4);  // (the last: CTAs that have left)
   w.count = take((size_t)c->max_seqs * 4);
   w.lead = take((size_t)c->max_seqs * 4);
   w.head = take((size_t)(c->max_seqs + 1) * 4);

@@ -576,3 +576,21 @@ def test_page_counts_past_32_bits():
     assert c.status() == 2
     assert bool((c.length == pages * T).all()) and bool((c.refs == n).all())
     assert all(torch.equal(row, torch.arange(pages, dtype=torch.int32, device="cuda")) for row in c.table[::93])
+
+
+def test_attention_leaves_its_counters_zero():
+    """Arrivals that an unfinished call would leave behind: the counters (they follow the status
+    word's 256 bytes) are zero after the next call of the tensor-core kernel, and the call after it is right."""
+    import paper_2605_29657_gb300 as occ
+    c, seqs = filled(64, 128, 1, [5000, 3000], 5, gain=0.7)
+    q = torch.randn((500, 4, 128), generator=torch.Generator().manual_seed(0)).bfloat16().cuda()
+    off = dev([0, 200, 500], torch.int64)
+    want, wl = occ.occam_cache_attend(c, 0, q, dev(seqs), off, 300)
+    counters = c.ws[256:256 + 4 * 513].view(torch.int32)
+    assert not counters.any()
+    counters[:152] = 1
+    occ.occam_cache_attend(c, 0, q, dev(seqs), off, 300)
+    assert not counters.any()
+    out, lse = occ.occam_cache_attend(c, 0, q, dev(seqs), off, 300)
+    assert torch.equal(out, want) and torch.equal(lse, wl)
+    assert c.status() == 0
