@@ -523,7 +523,8 @@ int occam_cache_append(const occam_cache* cache, int32_t layer, int32_t dtype, i
  *   p_k = exp(scale q.k - max), scale 0: 1/sqrt(dim);
  *   lse [total_rows, heads] fp32 (NULL to skip) = log sum_k exp(scale q.k).
  * A row that sees no token gives 0 and -inf. Scores, statistics and sums are
- * in fp32; probabilities are rounded to f16 for the product with the codes.
+ * in fp32; probabilities are rounded to f16 for the product with the codes (11
+ * bits down to 2^-21 of a row's largest, lost below 2^-32).
  * Scales of v within a sequence may span a factor of 2^60. max_rows: the
  * largest row_off[i+1] - row_off[i] (it chooses the kernels; results are right
  * for any value). heads <= 64 * cache heads. A call of more than 2^31 - 2^16

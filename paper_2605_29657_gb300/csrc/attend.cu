@@ -52,6 +52,10 @@ constexpr int kThreads = kWarps * 32;
 constexpr int kFewRows = 32;
 constexpr float kRhoKeep = 1.f / 64.f;           // P is scaled down by v's scales at most this far
 constexpr float kRhoSpan = 8.6736174e-19f;       // 2^-60
+// P (at most 1) goes to f16 2^15 times as large: what is 2^-29 of a row's running maximum still has
+// f16's 11 bits, below 2^-40 it is lost. (As it is, 2^-14 and 2^-25: a long cache's many small
+// probabilities were missing from O, while l, summed in fp32, had them.)
+constexpr float kLift = 32768.f, kUnlift = 1.f / 32768.f;
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                         uint32_t b1) {
@@ -353,7 +357,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
       m[nq][0] = m[nq][1] = -INFINITY;
       l[nq][0] = l[nq][1] = 0.f;
     }
-    float rho = 0.f, rho_max = 0.f;  // O is held in units of rho
+    float rho = 0.f, rho_max = 0.f;  // O is held in units of rho / kLift
 
     for (; tile < tb; tile += kWarps) {
       const int later = tile + 2 * kWarps;
@@ -472,7 +476,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
               rho_max = fmaxf(rho_max, to);
             }
           }
-          const float ratio = rho > 0.f ? v / rho : 0.f;
+          const float ratio = rho > 0.f ? v / rho * kLift : 0.f;
           uint32_t b0[NQ], b1[NQ];
 #pragma unroll
           for (int nq = 0; nq < NQ; ++nq) {
@@ -505,6 +509,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
 
     // the warps' results meet in shared memory (every lane's copies have been read)
     __syncwarp();
+    auto value = [&](float x) { return x * kUnlift * rho; };
 #pragma unroll
     for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
@@ -523,7 +528,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
 #pragma unroll
         for (int k = 0; k < MT; k += 2)
           *reinterpret_cast<float4*>(dst + 2 * k) =
-              make_float4(o[nq][k][e] * rho, o[nq][k][e + 2] * rho, o[nq][k + 1][e] * rho, o[nq][k + 1][e + 2] * rho);
+              make_float4(value(o[nq][k][e]), value(o[nq][k][e + 2]), value(o[nq][k + 1][e]), value(o[nq][k + 1][e + 2]));
       }
     __syncthreads();
     const bool whole = ta == 0 && tb == tiles;

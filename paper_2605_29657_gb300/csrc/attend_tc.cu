@@ -46,6 +46,10 @@ constexpr uint64_t kWaitNs = 2000000000ull;
 constexpr float kLazy = 8.f;             // log2 growth of a maximum before O is rescaled
 constexpr float kLeast = 1.2e-38f;       // a score's factor: never 0, so that a hidden key's -inf stays
 constexpr float kRhoKeep = 1.f / 64.f;
+// P is held 2^7 times as large: at most 2^15 (f16 ends at 2^16), and what is 2^-21 of a row's
+// reference still has f16's 11 bits; below 2^-32 it is lost. l stays in true units, O's factor is taken
+// back by the last reference.
+constexpr float kLift = 7.f, kUnlift = 1.f / 128.f;
 constexpr float kRhoSpan = 8.6736174e-19f;  // 2^-60
 
 struct Step {
@@ -56,10 +60,10 @@ struct Step {
   int row_tiles;      // 1 or 2
   uint32_t seen[4];   // bit k: key k of the tile may be seen
   float ks[8];        // scale of k, per 16 keys
-  float lr[8];        // log2(scale of v / rho)
-  float rr[8];        // rho / scale of v
+  float lr[8];        // log2(scale of v / rho) + kLift
+  float rr[8];        // kUnlift rho / scale of v
   float fall;         // O's factor: rho before / rho now
-  float rho;
+  float rho;          // kUnlift rho
 };
 
 struct Shared {
@@ -448,8 +452,8 @@ __device__ __forceinline__ void plan_role(const AttendParams& p, Shared& sh, con
       Step& s = sh.step[n % kRing];
       if (lane < 8) {
         s.ks[lane] = has ? cur.ks : 1.f;
-        s.lr[lane] = lr;
-        s.rr[lane] = rr;
+        s.lr[lane] = lr + kLift;
+        s.rr[lane] = rr * kUnlift;
       }
       if (lane == 8) {
 #pragma unroll
@@ -487,7 +491,7 @@ __device__ __forceinline__ void plan_role(const AttendParams& p, Shared& sh, con
     again = walk_next<kR, kK, kOver>(p, sh, x);
     if (lane == 0) {
       sh.step[n % kRing].end = again ? 1 : 2;
-      sh.step[n % kRing].rho = rho;
+      sh.step[n % kRing].rho = rho * kUnlift;
       tc::bar_arrive(&sh.step_full[n % kRing]);
     }
     ++n;

@@ -4,6 +4,8 @@ calls exactly, attention within bounds derived from the data
 
 from __future__ import annotations
 
+import math
+
 import pytest
 import torch
 
@@ -594,3 +596,37 @@ def test_attention_leaves_its_counters_zero():
     out, lse = occ.occam_cache_attend(c, 0, q, dev(seqs), off, 300)
     assert torch.equal(out, want) and torch.equal(lse, wl)
     assert c.status() == 0
+
+
+@pytest.mark.parametrize("rows,branches", [(1, 600), (4, 200), (2048, 1)])
+def test_attend_sums_many_small_probabilities(rows, branches):
+    """One key with a probability near 1 and a value of 0, 8,191 keys with a probability of 2^-27 each and a
+    value of 1: the result is the sum of the small ones. (As many items as keep each on few CTAs, so
+    that the small ones meet the large one's maximum.)
+
+    Bound: a probability is held in f16, 2^15 (few rows) or 2^7 (many rows, whose reference is at most
+    the maximum) times as large: 2^-11 relative or 2^-32 absolute; the exponent, 27 log 2 and a
+    power of two away, is exact to 2^-20; half an ulp of the f16 result, 2^-11, or 2^-25."""
+    import paper_2605_29657_gb300 as occ
+    n, T, D, G = 1 << 13, 128, 64, 32 if rows > 4 else 1
+    c = make(layers=1, pages=n // T, heads=1, dim=D, T=T, seqs=branches, max_pages=n // T, stale=False)
+    k, v = torch.zeros((n, 1, D)), torch.zeros((n, 1, D))
+    k[0, 0, 0], v[1:] = 1.0, 1.0
+    occ.occam_cache_extend(c, dev([0]), dev([n]))
+    occ.occam_cache_append(c, 0, k.bfloat16().cuda(), v.bfloat16().cuda(), dev([0]), dev([0, n], torch.int64))
+    if branches > 1:
+        occ.occam_cache_fork(c, dev([0] * (branches - 1)), dev(list(range(1, branches))))
+    q = torch.zeros((rows * branches, G, D), device="cuda", dtype=torch.float16)
+    q[:, :, 0] = 1.0
+    off = torch.arange(branches + 1, dtype=torch.int64, device="cuda") * rows
+    p = 2.0 ** -27
+    l = 1 + (n - 1) * p
+    want = (n - 1) * p / l
+    bound = (n - 1) * ((2.0 ** -11 + 2.0 ** -20) * p + 2.0 ** -32) / l + 2.0 ** -11 * want + 2.0 ** -25
+    for keep in (None, torch.ones(n * branches, dtype=torch.uint8, device="cuda")):
+        out, lse = occ.occam_cache_attend(c, 0, q, dev(list(range(branches))), off, rows, scale=27 * math.log(2.0), causal=False,
+                                          keep=keep, keep_off=None if keep is None else torch.arange(branches + 1, device="cuda") * n)
+        assert c.status() == 0
+        assert float((out.double() - want).abs().max()) <= bound, (float(out.min()), float(out.max()), want)
+        # log l of a score of 27 log 2: its 2^-20 and the logarithm's own
+        assert float((lse.double() - 27 * math.log(2.0) - math.log(l)).abs().max()) <= 2.0 ** -19 + 2.0 ** -22 * 27
