@@ -640,6 +640,9 @@ struct MoveParams {
 // of 2 x 32 heads in 11 layers take about 95 us, 4.5 TB/s of bytes moved.
 // MAXV: 16-code vectors a thread holds (128 threads).
 constexpr int kMoveHeads = 4;
+// A code times its scale may round to 2^128 (256 x 2^120, from values near bf16's end): it counts as the
+// largest finite value, which asks for the same scale.
+constexpr float kLargest = 3.4028235e38f;
 template <int D, int MAXV>
 __global__ void __launch_bounds__(128) compact_move_kernel(MoveParams p) {
   __shared__ int2 src[128];  // page and slot of each token
@@ -697,7 +700,7 @@ __global__ void __launch_bounds__(128) compact_move_kernel(MoveParams p) {
         float amax = 0.f;
 #pragma unroll
         for (int q = 0; q < MAXV; ++q)
-          if (q * 128 + (int)threadIdx.x < nv) amax = fmaxf(amax, finite_abs(codes_amax(x[q]) * s[q]));
+          if (q * 128 + (int)threadIdx.x < nv) amax = fmaxf(amax, fminf(codes_amax(x[q]) * s[q], kLargest));
         amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
         float* r = red[h & 1];
         if ((threadIdx.x & 31) == 0) r[threadIdx.x >> 5] = amax;

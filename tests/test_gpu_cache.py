@@ -630,3 +630,27 @@ def test_attend_sums_many_small_probabilities(rows, branches):
         assert float((out.double() - want).abs().max()) <= bound, (float(out.min()), float(out.max()), want)
         # log l of a score of 27 log 2: its 2^-20 and the logarithm's own
         assert float((lse.double() - 27 * math.log(2.0) - math.log(l)).abs().max()) <= 2.0 ** -19 + 2.0 ** -22 * 27
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_compact_keeps_the_largest_values(dtype):
+    """Values near the type's end, beside ordinary ones and alone, in blocks that are moved."""
+    import paper_2605_29657_gb300 as occ
+    c = make(layers=1, T=16, dim=64, heads=2)
+    ref = R.Cache(c)
+    x = torch.randn((40, 2, 64), generator=torch.Generator().manual_seed(3))
+    big = 3.3e38 if dtype == "bf16" else 65504.0
+    x[5, 0, 6], x[20, 1, 7] = big, -big
+    x[16:24, 0] = 0.0
+    x[17, 0, 1] = big  # with zeros only
+    x = x.to(DT[dtype]).cuda()
+    occ.occam_cache_extend(c, dev([3]), dev([40]))
+    occ.occam_cache_append(c, 0, x, -x, dev([3]), dev([0, 40], torch.int64))
+    ref.extend([3], [40])
+    ref.append(0, x, -x, [3], [0, 40])
+    R.assert_codes(c, ref)
+    flags = [i % 3 != 0 for i in range(40)]
+    occ.occam_cache_compact(c, dev([3]), dev(flags, torch.uint8), dev([0, 40], torch.int64))
+    ref.compact([3], flags, [0, 40], (0, 1))
+    R.assert_codes(c, ref)
+    assert c.status() == 0
