@@ -141,7 +141,7 @@ __global__ void __launch_bounds__(128, MAXV == 8 ? 9 : 1) append_kernel(AppendPa
   int len = -1;
   if ((unsigned)seq < (unsigned)p.c.max_seqs) len = p.c.length[seq];
   if (refused) return;
-  if (local < 0) return;  // rows before row_off[0] belong to no sequence
+  if (local < 0 && r0 <= p.total_rows) return;  // rows before row_off[0] belong to no sequence
   const bool good = r0 >= 0 && r1 >= r0 && r1 <= p.total_rows && len >= r1 - r0 &&
                     len <= (int64_t)p.c.max_pages * T;
   if (!good) {

@@ -654,3 +654,18 @@ def test_compact_keeps_the_largest_values(dtype):
     ref.compact([3], flags, [0, 40], (0, 1))
     R.assert_codes(c, ref)
     assert c.status() == 0
+
+
+@pytest.mark.parametrize("off", [[1000, 1003], [4, 4], [-3, 0], [0, 2, 1], [0, 4, 4], [3, 2, 2]])
+def test_append_offsets_outside_the_rows_are_recorded(off):
+    import paper_2605_29657_gb300 as occ
+    c = make(layers=1, pages=8, heads=2, dim=64, T=16, seqs=4, max_pages=4)
+    ref = R.Cache(c)
+    grow(c, ref, [0, 1], [32, 20], 0)
+    x = rows_of(3, 2, 64, 1)
+    x[2] = float("nan")  # (only good ranges of rows may be written: [0, 2) of [0, 2, 1])
+    occ.occam_cache_append(c, 0, x, x, dev(list(range(len(off) - 1))), dev(off, torch.int64))
+    assert c.status() == 1
+    if off[:2] == [0, 2]:
+        ref.append(0, x, x, [0], [0, 2])
+    R.assert_codes(c, ref)
