@@ -415,8 +415,10 @@ enum { OCCAM_BF16 = 0, OCCAM_F16 = 1, OCCAM_F32 = 2 };
 enum { OCCAM_ROPE_HALF = 0, OCCAM_ROPE_ADJACENT = 1 };
 
 /* One tensor of an occam_rope call: [rows, heads, dim] values, dense in dim;
- * strides in elements. dst may be src with the same strides (in place);
- * otherwise the two must not overlap. src may be broadcast (a stride of 0);
+ * strides in elements. dst may be src with the same strides (in place); else
+ * no dst has an element in common with a src, with the other dst, or twice with
+ * itself: such calls are refused, and so are tensors that lie within one
+ * another with rows of different strides. src may be broadcast (a stride of 0);
  * dst's rows and heads are at least dim elements apart. */
 typedef struct occam_rope_tensor {
   const void* src;

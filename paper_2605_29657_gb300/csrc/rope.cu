@@ -12,6 +12,8 @@
 // 6.3 TB/s; 64 rows of 40 heads: 5.5 us, the chain of loads, sines and stores.
 #include <cuda_fp16.h>
 
+#include <algorithm>
+
 #include "common.cuh"
 #include "cache.cuh"
 #include "nvtx.cuh"
@@ -181,6 +183,54 @@ int launch_t(RopeParams& p, int adj, int n, cudaStream_t st) {
   return ok && cudaGetLastError() == cudaSuccess ? OCCAM_OK : OCCAM_ERR_CUDA;
 }
 
+// A tensor's values as intervals of `width` elements at base + r row + h head.
+struct Extent {
+  __int128 base, row, head, rows, heads, width;  // base in elements
+  __int128 end() const { return base + (rows - 1) * row + (heads - 1) * head + width; }
+};
+Extent extent(const void* at, int64_t rows, int64_t row, int64_t heads, int64_t head, int64_t dim, int64_t es) {
+  Extent e{(__int128)(reinterpret_cast<uintptr_t>(at) / es), row, head, rows, heads, dim};
+  if (e.rows == 1 || e.row == 0) e.rows = 1, e.row = 0;      // (a row read again is one row)
+  if (e.heads == 1 || e.head == 0) e.heads = 1, e.head = 0;
+  if (e.head == e.width) e.width *= e.heads, e.heads = 1, e.head = 0;  // heads side by side are one interval
+  return e;
+}
+// Whether c + n pitch lies in lo .. hi for some n in first .. last (pitch >= 0).
+bool reaches(__int128 c, __int128 pitch, __int128 first, __int128 last, __int128 lo, __int128 hi) {
+  if (pitch == 0) return lo <= c && c <= hi;
+  auto floor_div = [](__int128 a, __int128 b) { return a >= 0 ? a / b : -((-a + b - 1) / b); };
+  const __int128 n = std::max(first, -floor_div(c - lo, pitch));  // the least n with c + n pitch >= lo
+  return n <= last && c + n * pitch <= hi;
+}
+// Whether two tensors have an element in common. (Exact, but for tensors that lie within each other with
+// rows of different strides, or more than 2^20 pairs of heads with different strides: true.)
+bool meet(const Extent& a, const Extent& b) {
+  if (a.end() <= b.base || b.end() <= a.base) return false;
+  if (a.rows > 1 && b.rows > 1 && a.row != b.row) return true;
+  const __int128 pitch = a.rows > 1 ? a.row : b.row, at = a.base - b.base;
+  auto rows_meet = [&](__int128 c) { return reaches(c, pitch, 1 - b.rows, a.rows - 1, 1 - a.width, b.width - 1); };
+  if (a.heads == 1 || b.heads == 1 || a.head == b.head) {
+    const __int128 head = a.heads > 1 ? a.head : b.head;
+    for (__int128 h = 1 - b.heads; h < a.heads; ++h)
+      if (rows_meet(at + h * head)) return true;
+    return false;
+  }
+  if (a.heads * b.heads > (1 << 20)) return true;
+  for (__int128 h = 0; h < a.heads; ++h)
+    for (__int128 k = 0; k < b.heads; ++k)
+      if (rows_meet(at + h * a.head - k * b.head)) return true;
+  return false;
+}
+// Whether two of a tensor's own (row, head) intervals have an element in common.
+bool meets_itself(const Extent& a) {
+  if (a.row >= (a.heads - 1) * a.head + a.width || a.rows == 1) return a.heads > 1 && a.head < a.width;
+  if (a.heads == 1) return true;  // (rows closer than a row is wide)
+  if (a.head >= (a.rows - 1) * a.row + a.width) return a.row < a.width;
+  for (__int128 h = 0; h < a.heads; ++h)  // h = 0: rows 1 .. apart
+    if (reaches(h * a.head, a.row, h ? 1 - a.rows : 1, a.rows - 1, 1 - a.width, a.width - 1)) return true;
+  return false;
+}
+
 }  // namespace
 
 extern "C" int occam_rope(int32_t dtype, int64_t rows, int32_t dim, int32_t rot, int32_t pairing, int32_t inverse,
@@ -198,6 +248,7 @@ extern "C" int occam_rope(int32_t dtype, int64_t rows, int32_t dim, int32_t rot,
   if (!positions || !inv_freq || !axis) return OCCAM_ERR_INVALID_ARG;
   const uintptr_t es = dtype == OCCAM_F32 ? 4 : 2;
   RopeParams p{};
+  Extent to[2], from[2];
   for (int i = 0; i < n_tensors; ++i) {
     const occam_rope_tensor& t = tensors[i];
     if (!t.src || !t.dst || t.heads < 1 || t.heads > 65535 || t.src_row < 0 || t.src_head < 0 || t.dst_row < 0 || t.dst_head < 0)
@@ -205,10 +256,19 @@ extern "C" int occam_rope(int32_t dtype, int64_t rows, int32_t dim, int32_t rot,
     if ((reinterpret_cast<uintptr_t>(t.src) | reinterpret_cast<uintptr_t>(t.dst)) & (es - 1)) return OCCAM_ERR_INVALID_ARG;
     // no value of dst has two places to come from
     if ((rows > 1 && t.dst_row < dim) || (t.heads > 1 && t.dst_head < dim)) return OCCAM_ERR_INVALID_ARG;
+    to[i] = extent(t.dst, rows, t.dst_row, t.heads, t.dst_head, dim, es);
+    from[i] = extent(t.src, rows, t.src_row, t.heads, t.src_head, dim, es);
+    if (meets_itself(to[i])) return OCCAM_ERR_INVALID_ARG;
     // in place means the same strides: a row's values are read before they are written
     if (t.src == t.dst && (t.src_row != t.dst_row || t.src_head != t.dst_head)) return OCCAM_ERR_INVALID_ARG;
     p.t[i] = t;
   }
+  // no value is written that another thread may still read, or writes too
+  for (int i = 0; i < n_tensors; ++i)
+    for (int j = 0; j < n_tensors; ++j) {
+      if (i < j && meet(to[i], to[j])) return OCCAM_ERR_INVALID_ARG;
+      if (!(i == j && p.t[i].src == p.t[i].dst) && meet(to[i], from[j])) return OCCAM_ERR_INVALID_ARG;
+    }
   p.rows = rows;
   p.dim = dim;
   p.half = rot / 2;

@@ -148,3 +148,31 @@ def test_rope_refusals(lib):
                 dict(dst_row=256), dict(dst=PTR + 4096, dst_row=0), dict(dst=PTR + 4096, dst_head=32)):
         assert rope(**bad) == invalid, bad
     assert lib.occam_rope(0, 2, 64, 64, 0, 0, PTR, 2, 3, PTR, PTR, 1, None, None) == invalid
+
+
+def test_rope_results_that_overlap_are_refused(lib):
+    """bf16, 3 rows of 2 heads of 64 dims (4 of 2 in the last one), as [rows, heads, dim] unless said."""
+    import paper_2605_29657_gb300._lib as L
+    invalid, FAR = codes()[0], PTR + (1 << 20)
+
+    def rope(*tensors, rows=3):
+        full = [dict(dict(src=PTR, dst=FAR, heads=2, src_row=128, src_head=64, dst_row=128, dst_head=64), **t) for t in tensors]
+        x = (L.CRopeTensor * 2)(*[L.CRopeTensor(**f) for f in full])
+        return lib.occam_rope(0, rows, 64, 64, 0, 0, PTR, 4, 3, PTR, PTR, len(tensors), bytes(x), None)
+
+    other = dict(src=PTR + (1 << 21), dst=PTR + (1 << 22))
+    for bad in (
+            [dict(dst_row=64)],                                  # row r's second head is row r + 1's first
+            [dict(dst_row=64, dst_head=128)],                    # heads outside rows, rows 0 and 2 of neighbours meet
+            [dict(dst_row=100, dst_head=90)],
+            [dict(dst=PTR + 2)], [dict(dst=PTR + 128)],          # shifted by an element, by a head
+            [dict(dst=PTR + 256)], [dict(dst=PTR - 256)],        # by a row
+            [dict(dst=PTR + 64, dst_row=256)],                   # rows of other strides within the input
+            [dict(src_row=0, dst=PTR - 256)],                    # onto a row that every row reads
+            [dict(), dict(other, dst=FAR)],                      # the same result twice
+            [dict(), dict(other, dst=FAR + 128)],
+            [dict(dst_row=256), dict(other, dst=FAR + 192, dst_row=256)],  # half a head into the other's rows
+            [dict(), dict(other, dst=PTR)], [dict(dst=PTR + (1 << 21)), other],  # onto the other's input
+            [dict(dst=PTR), dict(other, src=PTR + 128, dst=PTR + 128)]):  # in place, inputs that share a head
+        assert rope(*bad) == invalid, bad
+    assert rope(dict(dst_row=200, dst_head=150), rows=4) == invalid

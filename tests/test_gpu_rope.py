@@ -147,3 +147,53 @@ def test_refusals():
     for f in bad:
         with pytest.raises(occ.OccamError):
             f()
+
+
+def test_results_in_every_layout_that_does_not_overlap():
+    """In place on views of one projection, heads outside rows, rows between the heads of another tensor, results in the
+    gaps of the input: all give what new dense tensors get."""
+    import paper_2605_29657_gb300 as occ
+    rows, hq, hk, dim = 33, 4, 2, 64
+    q, k, pos, freq, axis = case(rows, hq, hk, dim, dim, 2, "bf16")
+    want_q, want_k = occ.occam_rope(q, k, pos, freq, axis)
+
+    def empty(*shape):
+        return torch.zeros(shape, dtype=torch.bfloat16, device="cuda")
+
+    def check(q, k, out_q, out_k):
+        a, b = occ.occam_rope(q, k, pos, freq, axis, out_q=out_q, out_k=out_k)
+        assert a is out_q and b is out_k and torch.equal(a, want_q) and torch.equal(b, want_k)
+
+    fused = empty(rows, hq + 2 * hk, dim)
+    fused[:, :hq], fused[:, hq:hq + hk] = q, k
+    check(fused[:, :hq], fused[:, hq:hq + hk], fused[:, :hq], fused[:, hq:hq + hk])
+    fused[:, :hq], fused[:, hq:hq + hk] = q, k  # keys in place of the values' rows, queries in place
+    check(fused[:, :hq], fused[:, hq:hq + hk], fused[:, :hq], fused[:, hq + hk:])
+    both = empty(hq + hk, rows, dim)
+    check(q, k, both[:hq].transpose(0, 1), both[hq:].transpose(0, 1))
+    woven = empty(rows, 2 * hq, dim)
+    check(q, k, woven[:, ::2], woven[:, 1:2 * hk:2])
+    woven[:, ::2] = q
+    check(woven[:, ::2], k, woven[:, 1::2], empty(rows, hk, dim))
+    apart = empty(2 * hq, rows, dim).transpose(0, 1)  # heads outside rows, other head strides
+    apart[:, ::2] = q
+    check(apart[:, ::2], k, apart[:, 1::2], apart[:, 0:2 * hk:2].clone())
+    odd = empty(rows * 3 * dim + hq * 100 * dim)  # rows 3 and heads 34 widths apart: rows and heads cross, and no two meet
+    out = torch.as_strided(odd, (rows, hq, dim), (3 * dim, 34 * dim, 1))
+    check(q, k, out, empty(rows, hk, dim))
+
+
+def test_overlapping_results_are_refused():
+    import paper_2605_29657_gb300 as occ
+    q, k, pos, freq, axis = case(5, 4, 2, 64, 64, 2, "bf16")
+    buf = torch.zeros(4096, dtype=torch.bfloat16, device="cuda")
+    rows = torch.zeros((6, 6, 64), dtype=torch.bfloat16, device="cuda")
+    for kw in (dict(out_q=torch.as_strided(buf, (5, 4, 64), (64, 64, 1))), dict(out_q=rows[:5, :4], out_k=rows[:5, 3:5]),
+               dict(out_q=rows[:5, :4], out_k=rows[1:, :2])):
+        with pytest.raises(occ.OccamError):
+            occ.occam_rope(q, k, pos, freq, axis, **kw)
+    with pytest.raises(occ.OccamError):
+        occ.occam_rope(rows[:5, :4], k, pos, freq, axis, out_q=rows[1:, :4])
+    with pytest.raises(occ.OccamError):
+        occ.occam_rope(rows[:5, :4], rows[:5, 4:], pos, freq, axis, out_q=rows[:5, 2:])
+    assert not rows.any() and not buf.any()
