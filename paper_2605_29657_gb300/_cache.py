@@ -19,7 +19,6 @@ from ._lib import (
     _dev_tensor,
     _ptr,
     library,
-    occam_get_status,
 )
 
 _DTYPE = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
@@ -38,17 +37,37 @@ def _bad(msg: str):
     raise OccamError(OCCAM_ERR_INVALID_ARG, msg)
 
 
-def _on(stream, device) -> int:
+# A call's tensors are all on one GPU, `at` below (its index); the call is made with that one current.
+
+def _on(stream, at: int) -> int:
     """The stream's handle; the device's current one by default."""
     if stream is not None:
+        if stream.device.index != at:
+            _bad(f"the stream is on {stream.device}, the tensors on cuda:{at}")
         return stream.cuda_stream
-    return torch._C._cuda_getCurrentRawStream(device.index)
+    return torch._C._cuda_getCurrentRawStream(at)
 
 
-def _rows_tensor(t, name: str, dtypes, heads: int | None = None, dim: int | None = None) -> torch.Tensor:
+def _call(at: int, fn, *args) -> None:
+    if torch._C._cuda_getDevice() == at:
+        rc = fn(*args)
+    else:
+        with torch.cuda.device(at):
+            rc = fn(*args)
+    if rc:
+        _check(rc, fn.__name__)
+
+
+def _dense(t, dtype, name: str, at: int) -> torch.Tensor:
+    if not isinstance(t, torch.Tensor) or t.get_device() != at:
+        _bad(f"{name} must be a tensor on cuda:{at}")
+    return _dev_tensor(t, dtype, name)
+
+
+def _rows_tensor(t, name: str, dtypes, at: int, heads: int | None = None, dim: int | None = None) -> torch.Tensor:
     """A CUDA tensor [rows, heads, dim] whose heads are dense; rows may be strided."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        _bad(f"{name} must be a CUDA tensor")
+    if not isinstance(t, torch.Tensor) or t.get_device() != at:
+        _bad(f"{name} must be a tensor on cuda:{at}")
     if t.dtype not in dtypes:
         _bad(f"{name} must be one of {[str(d) for d in dtypes]}, got {t.dtype}")
     shape = t.shape
@@ -98,40 +117,37 @@ def occam_rope(q, k, positions, inv_freq, axis, pairing: str = "half", inverse: 
     if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dim() != 3 or q.dtype not in _DTYPE:
         _bad("q must be a CUDA tensor [rows, heads, dim] of bfloat16, float16 or float32")
     rows, _, dim = q.shape
-    dtype = q.dtype
-    _dev_tensor(inv_freq, torch.float32, "inv_freq")
-    _dev_tensor(axis, torch.int32, "axis")
-    if inv_freq.dim() != 1 or axis.shape != inv_freq.shape:
-        _bad("inv_freq and axis must be [pairs]")
-    if not isinstance(positions, torch.Tensor) or not positions.is_cuda or positions.dtype != torch.int32 or \
+    dtype, at = q.dtype, q.get_device()
+    pairs = _vector(inv_freq, torch.float32, None, "inv_freq", at).shape[0]
+    _vector(axis, torch.int32, pairs, "axis", at)
+    if not isinstance(positions, torch.Tensor) or positions.get_device() != at or positions.dtype != torch.int32 or \
             positions.dim() != 2 or positions.shape[1] != rows or (rows > 1 and positions.stride(1) != 1):
-        _bad("positions must be a CUDA int32 tensor [axes, rows], dense in rows")
-    packed, out_q = _rope_tensor(q, out_q, "q", rows, dim, dtype)
+        _bad(f"positions must be an int32 tensor [axes, rows] on cuda:{at}, dense in rows")
+    packed, out_q = _rope_tensor(q, out_q, "q", rows, dim, dtype, at)
     n = 1
     if k is not None:
-        more, out_k = _rope_tensor(k, out_k, "k", rows, dim, dtype)
+        more, out_k = _rope_tensor(k, out_k, "k", rows, dim, dtype, at)
         packed += more
         n = 2
     elif out_k is not None:
         _bad("out_k without k")
-    rc = library().occam_rope(_DTYPE[dtype], rows, dim, 2 * inv_freq.shape[0], _PAIRING[pairing], int(bool(inverse)),
-                              positions.data_ptr(), positions.stride(0), positions.shape[0], inv_freq.data_ptr(),
-                              axis.data_ptr(), n, packed, _on(stream, q.device))
-    _check(rc, "occam_rope")
+    _call(at, library().occam_rope, _DTYPE[dtype], rows, dim, 2 * pairs, _PAIRING[pairing], int(bool(inverse)),
+          positions.data_ptr(), positions.stride(0), positions.shape[0], inv_freq.data_ptr(), axis.data_ptr(), n, packed,
+          _on(stream, at))
     return out_q, out_k
 
 
-def _rope_tensor(x, out, name, rows, dim, dtype):
-    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dtype != dtype or x.dim() != 3 or x.shape[0] != rows or \
+def _rope_tensor(x, out, name, rows, dim, dtype, at):
+    if not isinstance(x, torch.Tensor) or x.get_device() != at or x.dtype != dtype or x.dim() != 3 or x.shape[0] != rows or \
             x.shape[2] != dim:
-        _bad(f"{name} must be a CUDA tensor [{rows}, heads, {dim}] {dtype}")
+        _bad(f"{name} must be a tensor [{rows}, heads, {dim}] {dtype} on cuda:{at}")
     row, head, one = x.stride()
     if out is None:
         out = torch.empty(x.shape, dtype=dtype, device=x.device)
         heads = x.shape[1]
         out_row, out_head, out_one = heads * dim, dim, 1
     else:
-        if not isinstance(out, torch.Tensor) or not out.is_cuda or out.shape != x.shape or out.dtype != dtype:
+        if not isinstance(out, torch.Tensor) or out.get_device() != at or out.shape != x.shape or out.dtype != dtype:
             _bad(f"out_{name} must be like {name}")
         heads = x.shape[1]
         out_row, out_head, out_one = out.stride()
@@ -171,10 +187,11 @@ class PagedCache:
         return self
 
     def _set(self, k, v, k_scale, v_scale, table, length, refs, max_tokens):
-        _dev_tensor(k, E4M3, "k"); _dev_tensor(v, E4M3, "v")
-        _dev_tensor(k_scale, torch.float32, "k_scale"); _dev_tensor(v_scale, torch.float32, "v_scale")
-        _dev_tensor(table, torch.int32, "table"); _dev_tensor(length, torch.int32, "length")
-        _dev_tensor(refs, torch.int32, "refs")
+        at = _dev_tensor(k, E4M3, "k").get_device()
+        _dense(v, E4M3, "v", at)
+        _dense(k_scale, torch.float32, "k_scale", at); _dense(v_scale, torch.float32, "v_scale", at)
+        _dense(table, torch.int32, "table", at); _dense(length, torch.int32, "length", at)
+        _dense(refs, torch.int32, "refs", at)
         if k.dim() != 5 or v.shape != k.shape or k_scale.shape != k.shape[:3] or v_scale.shape != k.shape[:3]:
             _bad("k and v must be [layers, pages, heads, page_tokens, dim], their scales [layers, pages, heads]")
         if table.dim() != 2 or length.shape != table.shape[:1] or refs.shape != k.shape[1:2]:
@@ -185,7 +202,7 @@ class PagedCache:
         self.max_seqs, self.max_pages = table.shape
         # flags one compact call may pass: by default a token of every page of the pool
         self.max_tokens = self.pages * self.page_tokens if max_tokens is None else int(max_tokens)
-        self.device = k.device
+        self.device, self.at = k.device, at
         self._c = CCache(self.layers, self.pages, self.heads, self.dim, self.page_tokens, self.max_seqs, self.max_pages,
                          _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(table), _ptr(length), _ptr(refs))
         self._ref = ctypes.byref(self._c)
@@ -203,19 +220,24 @@ class PagedCache:
 
     def status(self, stream=None, ws=None) -> int:
         """Reads and clears the status word (synchronises the stream)."""
-        return occam_get_status(self.ws if ws is None else ws, stream)
+        v = ctypes.c_int32(0)
+        _call(self.at, library().occam_get_status, _workspace(self, ws)[0], ctypes.byref(v), _on(stream, self.at))
+        return int(v.value)
 
 
 def _workspace(cache, ws):
     if not isinstance(cache, PagedCache):
         _bad("cache must be a PagedCache")
-    return cache._ws if ws is None else (ws.data_ptr(), ws.numel())
+    if ws is None:
+        return cache._ws
+    _dense(ws, torch.uint8, "ws", cache.at)
+    return ws.data_ptr(), ws.numel()
 
 
-def _vector(t, dtype, n: int | None, name: str) -> torch.Tensor:
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or t.dim() != 1 or \
+def _vector(t, dtype, n: int | None, name: str, at: int) -> torch.Tensor:
+    if not isinstance(t, torch.Tensor) or t.get_device() != at or t.dtype != dtype or t.dim() != 1 or \
             (n is not None and t.shape[0] != n) or not t.is_contiguous():
-        _bad(f"{name} must be a dense CUDA vector of {dtype}" + ("" if n is None else f" with {n} entries"))
+        _bad(f"{name} must be a dense vector of {dtype} on cuda:{at}" + ("" if n is None else f" with {n} entries"))
     return t
 
 
@@ -223,10 +245,9 @@ def occam_cache_extend(cache: PagedCache, seqs, counts, ws=None, stream=None) ->
     """Sequence seqs[i] grows by counts[i] tokens: pages are taken and lengths raised. After a
     call that recorded an error, extend and append with that workspace do nothing until status() is read."""
     wp, wn = _workspace(cache, ws)
-    n = _vector(seqs, torch.int32, None, "seqs").shape[0]
-    _vector(counts, torch.int32, n, "counts")
-    _check(library().occam_cache_extend(cache._ref, n, _ptr(seqs), _ptr(counts), wp, wn,
-                                        _on(stream, cache.device)), "occam_cache_extend")
+    n = _vector(seqs, torch.int32, None, "seqs", cache.at).shape[0]
+    _vector(counts, torch.int32, n, "counts", cache.at)
+    _call(cache.at, library().occam_cache_extend, cache._ref, n, _ptr(seqs), _ptr(counts), wp, wn, _on(stream, cache.at))
 
 
 def occam_cache_append(cache: PagedCache, layer: int, k, v, seqs, row_off, ws=None, stream=None) -> None:
@@ -234,15 +255,14 @@ def occam_cache_append(cache: PagedCache, layer: int, k, v, seqs, row_off, ws=No
     (bfloat16 or float16, rows may be strided) as the last tokens of sequence
     seqs[i] in one layer. Pages that other sequences hold too are not written."""
     wp, wn = _workspace(cache, ws)
-    _rows_tensor(k, "k", _ROWS, cache.heads, cache.dim)
-    _rows_tensor(v, "v", (k.dtype,), cache.heads, cache.dim)
+    _rows_tensor(k, "k", _ROWS, cache.at, cache.heads, cache.dim)
+    _rows_tensor(v, "v", (k.dtype,), cache.at, cache.heads, cache.dim)
     if v.shape[0] != k.shape[0]:
         _bad("k and v must have as many rows")
-    n = _vector(seqs, torch.int32, None, "seqs").shape[0]
-    _vector(row_off, torch.int64, n + 1, "row_off")
-    _check(library().occam_cache_append(cache._ref, int(layer), _DTYPE[k.dtype], k.shape[0], _ptr(k), _row_stride(k),
-                                        _ptr(v), _row_stride(v), n, _ptr(seqs), _ptr(row_off), wp, wn,
-                                        _on(stream, cache.device)), "occam_cache_append")
+    n = _vector(seqs, torch.int32, None, "seqs", cache.at).shape[0]
+    _vector(row_off, torch.int64, n + 1, "row_off", cache.at)
+    _call(cache.at, library().occam_cache_append, cache._ref, int(layer), _DTYPE[k.dtype], k.shape[0], _ptr(k), _row_stride(k),
+          _ptr(v), _row_stride(v), n, _ptr(seqs), _ptr(row_off), wp, wn, _on(stream, cache.at))
 
 
 def occam_cache_attend(cache: PagedCache, layer: int, q, seqs, row_off, max_rows: int, scale: float = 0.0,
@@ -252,24 +272,24 @@ def occam_cache_attend(cache: PagedCache, layer: int, q, seqs, row_off, max_rows
     sequence. scale 0: 1 / sqrt(dim). keep / keep_off: uint8 flags that hide
     tokens. Returns (out, lse [rows, heads] natural logarithm)."""
     wp, wn = _workspace(cache, ws)
-    _rows_tensor(q, "q", _ROWS, None, cache.dim)
+    _rows_tensor(q, "q", _ROWS, cache.at, None, cache.dim)
     rows, heads, dim = q.shape
-    n = _vector(seqs, torch.int32, None, "seqs").shape[0]
-    _vector(row_off, torch.int64, n + 1, "row_off")
+    n = _vector(seqs, torch.int32, None, "seqs", cache.at).shape[0]
+    _vector(row_off, torch.int64, n + 1, "row_off", cache.at)
     total_keep = 0
     if keep is not None:
-        _dev_tensor(keep, torch.uint8, "keep")
+        _dense(keep, torch.uint8, "keep", cache.at)
         if keep_off is None:
             _bad("keep needs keep_off")
-        _vector(keep_off, torch.int64, n + 1, "keep_off")
+        _vector(keep_off, torch.int64, n + 1, "keep_off", cache.at)
         total_keep = keep.numel()
     if out is None:
         out = torch.empty((rows, heads, dim), dtype=q.dtype, device=q.device)
-    elif _dev_tensor(out, q.dtype, "out").shape != q.shape:
+    elif _dense(out, q.dtype, "out", cache.at).shape != q.shape:
         _bad("out must be like q")
     if lse is None:
         lse = torch.empty((rows, heads), dtype=torch.float32, device=q.device)
-    elif _dev_tensor(lse, torch.float32, "lse").shape != q.shape[:2]:
+    elif _dense(lse, torch.float32, "lse", cache.at).shape != q.shape[:2]:
         _bad("lse must be [rows, heads]")
     try:
         a = _ATTEND_ARGS.pack(layer, _ROWS[q.dtype], heads, 1 if causal else 0, rows, _row_stride(q), q.data_ptr(),
@@ -278,17 +298,16 @@ def occam_cache_attend(cache: PagedCache, layer: int, q, seqs, row_off, max_rows
                               total_keep)
     except struct.error as e:
         _bad(f"layer, max_rows or scale: {e}")
-    _check(library().occam_cache_attend(cache._ref, a, wp, wn, _on(stream, cache.device)), "occam_cache_attend")
+    _call(cache.at, library().occam_cache_attend, cache._ref, a, wp, wn, _on(stream, cache.at))
     return out, lse
 
 
 def occam_cache_fork(cache: PagedCache, src, dst, ws=None, stream=None) -> None:
     """Sequence dst[i] (empty) becomes a copy of src[i]; full pages are shared."""
     wp, wn = _workspace(cache, ws)
-    n = _vector(src, torch.int32, None, "src").shape[0]
-    _vector(dst, torch.int32, n, "dst")
-    _check(library().occam_cache_fork(cache._ref, n, _ptr(src), _ptr(dst), wp, wn,
-                                      _on(stream, cache.device)), "occam_cache_fork")
+    n = _vector(src, torch.int32, None, "src", cache.at).shape[0]
+    _vector(dst, torch.int32, n, "dst", cache.at)
+    _call(cache.at, library().occam_cache_fork, cache._ref, n, _ptr(src), _ptr(dst), wp, wn, _on(stream, cache.at))
 
 
 def occam_cache_compact(cache: PagedCache, seqs, keep, keep_off, layers: tuple[int, int] | None = None, ws=None,
@@ -297,17 +316,16 @@ def occam_cache_compact(cache: PagedCache, seqs, keep, keep_off, layers: tuple[i
     set (and those past the flags), in order; layers: the range of layers whose
     codes move (default: all)."""
     wp, wn = _workspace(cache, ws)
-    n = _vector(seqs, torch.int32, None, "seqs").shape[0]
-    _dev_tensor(keep, torch.uint8, "keep")
-    _vector(keep_off, torch.int64, n + 1, "keep_off")
+    n = _vector(seqs, torch.int32, None, "seqs", cache.at).shape[0]
+    _dense(keep, torch.uint8, "keep", cache.at)
+    _vector(keep_off, torch.int64, n + 1, "keep_off", cache.at)
     l0, l1 = (0, cache.layers) if layers is None else layers
-    _check(library().occam_cache_compact(cache._ref, int(l0), int(l1), n, _ptr(seqs), _ptr(keep), _ptr(keep_off),
-                                         keep.numel(), wp, wn, _on(stream, cache.device)), "occam_cache_compact")
+    _call(cache.at, library().occam_cache_compact, cache._ref, int(l0), int(l1), n, _ptr(seqs), _ptr(keep), _ptr(keep_off),
+          keep.numel(), wp, wn, _on(stream, cache.at))
 
 
 def occam_cache_release(cache: PagedCache, seqs, ws=None, stream=None) -> None:
     """Empties sequences; their pages lose a reference."""
     wp, wn = _workspace(cache, ws)
-    n = _vector(seqs, torch.int32, None, "seqs").shape[0]
-    _check(library().occam_cache_release(cache._ref, n, _ptr(seqs), wp, wn,
-                                         _on(stream, cache.device)), "occam_cache_release")
+    n = _vector(seqs, torch.int32, None, "seqs", cache.at).shape[0]
+    _call(cache.at, library().occam_cache_release, cache._ref, n, _ptr(seqs), wp, wn, _on(stream, cache.at))
