@@ -1,6 +1,11 @@
 """What follows pruning: rotary positions with several axes, and a paged
 cache held in 8 bits with the calls that fill it, attend over it and manage
-its pages (include/occam.h). Argument marshalling only, as in _lib."""
+its pages (include/occam.h). Argument marshalling only, as in _lib.
+
+stream: the stream a call runs on (default: the current one of its tensors'
+device). New results are allocated on that stream; as with every tensor used on
+two streams, order them and keep or record (Tensor.record_stream) what the
+other one still uses."""
 
 from __future__ import annotations
 
@@ -56,6 +61,14 @@ def _call(at: int, fn, *args) -> None:
             rc = fn(*args)
     if rc:
         _check(rc, fn.__name__)
+
+
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """A new result, of the stream that writes it: another stream's freed memory may still be in use there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def _dense(t, dtype, name: str, at: int) -> torch.Tensor:
@@ -123,27 +136,27 @@ def occam_rope(q, k, positions, inv_freq, axis, pairing: str = "half", inverse: 
     if not isinstance(positions, torch.Tensor) or positions.get_device() != at or positions.dtype != torch.int32 or \
             positions.dim() != 2 or positions.shape[1] != rows or (rows > 1 and positions.stride(1) != 1):
         _bad(f"positions must be an int32 tensor [axes, rows] on cuda:{at}, dense in rows")
-    packed, out_q = _rope_tensor(q, out_q, "q", rows, dim, dtype, at)
+    on = _on(stream, at)
+    packed, out_q = _rope_tensor(q, out_q, "q", rows, dim, dtype, at, stream)
     n = 1
     if k is not None:
-        more, out_k = _rope_tensor(k, out_k, "k", rows, dim, dtype, at)
+        more, out_k = _rope_tensor(k, out_k, "k", rows, dim, dtype, at, stream)
         packed += more
         n = 2
     elif out_k is not None:
         _bad("out_k without k")
     _call(at, library().occam_rope, _DTYPE[dtype], rows, dim, 2 * pairs, _PAIRING[pairing], int(bool(inverse)),
-          positions.data_ptr(), positions.stride(0), positions.shape[0], inv_freq.data_ptr(), axis.data_ptr(), n, packed,
-          _on(stream, at))
+          positions.data_ptr(), positions.stride(0), positions.shape[0], inv_freq.data_ptr(), axis.data_ptr(), n, packed, on)
     return out_q, out_k
 
 
-def _rope_tensor(x, out, name, rows, dim, dtype, at):
+def _rope_tensor(x, out, name, rows, dim, dtype, at, stream):
     if not isinstance(x, torch.Tensor) or x.get_device() != at or x.dtype != dtype or x.dim() != 3 or x.shape[0] != rows or \
             x.shape[2] != dim:
         _bad(f"{name} must be a tensor [{rows}, heads, {dim}] {dtype} on cuda:{at}")
     row, head, one = x.stride()
     if out is None:
-        out = torch.empty(x.shape, dtype=dtype, device=x.device)
+        out = _empty(x.shape, dtype, x.device, stream)
         heads = x.shape[1]
         out_row, out_head, out_one = heads * dim, dim, 1
     else:
@@ -283,12 +296,13 @@ def occam_cache_attend(cache: PagedCache, layer: int, q, seqs, row_off, max_rows
             _bad("keep needs keep_off")
         _vector(keep_off, torch.int64, n + 1, "keep_off", cache.at)
         total_keep = keep.numel()
+    on = _on(stream, cache.at)
     if out is None:
-        out = torch.empty((rows, heads, dim), dtype=q.dtype, device=q.device)
+        out = _empty((rows, heads, dim), q.dtype, q.device, stream)
     elif _dense(out, q.dtype, "out", cache.at).shape != q.shape:
         _bad("out must be like q")
     if lse is None:
-        lse = torch.empty((rows, heads), dtype=torch.float32, device=q.device)
+        lse = _empty((rows, heads), torch.float32, q.device, stream)
     elif _dense(lse, torch.float32, "lse", cache.at).shape != q.shape[:2]:
         _bad("lse must be [rows, heads]")
     try:
@@ -298,7 +312,7 @@ def occam_cache_attend(cache: PagedCache, layer: int, q, seqs, row_off, max_rows
                               total_keep)
     except struct.error as e:
         _bad(f"layer, max_rows or scale: {e}")
-    _call(cache.at, library().occam_cache_attend, cache._ref, a, wp, wn, _on(stream, cache.at))
+    _call(cache.at, library().occam_cache_attend, cache._ref, a, wp, wn, on)
     return out, lse
 
 

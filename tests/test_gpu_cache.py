@@ -669,3 +669,34 @@ def test_append_offsets_outside_the_rows_are_recorded(off):
     if off[:2] == [0, 2]:
         ref.append(0, x, x, [0], [0, 2])
     R.assert_codes(c, ref)
+
+
+@pytest.mark.parametrize("op", ["attend", "rope"])
+def test_new_results_belong_to_the_stream_that_writes_them(op):
+    """Memory that the current stream has freed, with writes to it still queued there, is no place for
+    the results of a call on another stream."""
+    import paper_2605_29657_gb300 as occ
+    c, seqs = filled(64, 128, 2, [300, 100], 5)
+    rows = [200, 100]
+    q = torch.randn((300, 32, 128), generator=torch.Generator().manual_seed(0)).bfloat16().cuda()  # 2.4 MB
+    s, off = dev(seqs), dev(offs(rows), torch.int64)
+    pos, freq, axis = torch.zeros((1, 300), dtype=torch.int32, device="cuda"), torch.ones(64, device="cuda"), dev([0] * 64)
+    ws, st = c.alloc_workspace(), torch.cuda.Stream()
+
+    def call(stream):
+        if op == "attend":
+            return occ.occam_cache_attend(c, 0, q, s, off, 200, ws=ws, stream=stream)[0]
+        return occ.occam_rope(q, None, pos, freq, axis, stream=stream)[0]
+
+    want = call(None)
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    freed = [torch.empty_like(q) for _ in range(8)]
+    torch.cuda._sleep(200_000_000)  # about 0.1 s
+    for x in freed:
+        x.fill_(7.0)
+    del freed, x
+    got = call(st)
+    st.synchronize()
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
