@@ -1084,8 +1084,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       plan_role<D>(p, sh, map_k, map_v, raw);
   }
   __syncthreads();
-  // after a wait that ran out, products and copies may still be in flight
-  if (sh.stop && (threadIdx.x == 384 || threadIdx.x == 448)) {
+  // after a wait that ran out, products and copies may still be in flight (the lane that issued the
+  // products is the one whose commit covers them)
+  if (sh.stop && (warp == 12 || warp == 14) && elect_one()) {
     tc::mma_commit(&sh.drain);
     tc::bar_wait(&sh.drain, 0, nullptr, kWaitNs);
     for (int k = 0; k < 2; ++k) {
