@@ -202,10 +202,12 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const int first = key + 16 * k;
-        x.page[k] = first < s.len ? table[first >> p.c.log2T] : 0;
+        const bool there = first < s.len && in_bounds((first >> p.c.log2T) < p.c.max_pages, p.c.status, kSiteAttendKey);
+        x.page[k] = there ? table[first >> p.c.log2T] : 0;
       }
       bool see = key + lane < s.len;
-      if (key + lane < n_flags) see = flags[key + lane] != 0;
+      if (key + lane < n_flags && in_bounds(flags + key + lane < p.keep + p.total_keep, p.c.status, kSiteAttendKey))
+        see = flags[key + lane] != 0;
       x.seen = see;
       return x;
     };
@@ -312,7 +314,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
         uint4 v[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-        if (r < rows) {
+        if (r < rows && in_bounds(s.row0 + j < p.total_rows && h * p.G + row - j * p.G < p.H, p.c.status, kSiteAttendRow)) {
           v[0] = *reinterpret_cast<const uint4*>(q + (t + 4 * c) * 16);
           v[1] = *reinterpret_cast<const uint4*>(q + (t + 4 * c) * 16 + 8);
         }
@@ -557,6 +559,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
         if (nan_first[d + q] < (p.causal ? s.len - s.rows + j + 1 : s.len)) v[q] = __int_as_float(0x7fc00000);
+      if (!in_bounds(s.row0 + j < p.total_rows && h * p.G + row - j * p.G < p.H, p.c.status, kSiteAttendRow)) continue;
       if (whole) {
         const int64_t to = (s.row0 + j) * p.H + h * p.G + row - j * p.G;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -574,7 +577,9 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
       __syncthreads();
       const int2 who = item_stretches<kOver>(line, x0);
       const int first = who.x, last = who.y;
-      if (threadIdx.x == 0) sh_last = arrive_count(&p.counters[first]) == last - first;
+      const bool fits = in_bounds(first >= 0 && first < last && last < line.stretches && line.stretches <= kAttendCtas &&
+                                      w.index >= first && w.index <= last, p.c.status, kSiteAttendPart);
+      if (threadIdx.x == 0) sh_last = fits && arrive_count(&p.counters[first]) == last - first;
       __syncthreads();
       if (sh_last) {
         if (threadIdx.x == 0) p.counters[first] = 0;
@@ -629,6 +634,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
               const float sum = sh_l[0][r], mx = sh_m[0][r], inv = sum == 0.f ? 0.f : 1.f / sum;
               const int row = rt * R + r, j = div_group(p, row);
               const int64_t to = (s.row0 + j) * p.H + h * p.G + row - j * p.G;
+              if (!in_bounds(to < p.total_rows * p.H, p.c.status, kSiteAttendRow)) continue;
               const float v[4] = {acc.x, acc.y, acc.z, acc.w};
               uint16_t o[4];
 #pragma unroll

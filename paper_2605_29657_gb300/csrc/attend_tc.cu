@@ -212,12 +212,14 @@ struct Plan {
     t.tile = tile;
     const int first = tile * kK + (lane & 7) * kGroup;
     t.page = 0;
-    if (first < x.s.len) t.page = table[first >> p.c.log2T];
+    if (first < x.s.len && in_bounds((first >> p.c.log2T) < p.c.max_pages, p.c.status, kSiteAttendKey))
+      t.page = table[first >> p.c.log2T];
     if (tile * kK < n_flags) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int key = tile * kK + 32 * k + lane;
-        t.seen[k] = key < n_flags ? flags[key] : 1u;
+        const bool flag = key < n_flags && in_bounds(flags + key < p.keep + p.total_keep, p.c.status, kSiteAttendKey);
+        t.seen[k] = flag ? flags[key] : 1u;
       }
     }
   }
@@ -634,7 +636,8 @@ __device__ __forceinline__ float load_queries(const AttendParams& p, const Walk&
   const uint16_t* row_at = nullptr;  // lane l's row
   {
     const int at = x.rt * kR + first + lane, tok = div_group(p, at);
-    if (at < rows) row_at = p.q + (x.s.row0 + tok) * p.q_row + (int64_t)(x.h * p.G + at - tok * p.G) * D;
+    if (at < rows && in_bounds(x.s.row0 + tok < p.total_rows && x.h * p.G + at - tok * p.G < p.H, p.c.status, kSiteAttendRow))
+      row_at = p.q + (x.s.row0 + tok) * p.q_row + (int64_t)(x.h * p.G + at - tok * p.G) * D;
   }
 #pragma unroll 4
   for (int i = 0; i < N; ++i) {
@@ -835,7 +838,8 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
       unsigned char* stage = q_smem + t * kK * D * 2;
       auto place = [&](int rr, int c) { return stage + (c >> 3) * 16384 + rr * 128 + (((c & 7) ^ (rr & 7)) << 4); };
       const int live = min(x.s.rows * p.G - (x.rt * kR + (row & ~31)), 32);  // rows of the warp
-      const uint64_t mine_at = done ? reinterpret_cast<uint64_t>(out) : reinterpret_cast<uint64_t>(part);
+      const bool fits = !there || in_bounds(x.s.row0 + tok < p.total_rows && x.h * p.G + at - tok * p.G < p.H, p.c.status, kSiteAttendRow);
+      const uint64_t mine_at = !fits ? 0 : done ? reinterpret_cast<uint64_t>(out) : reinterpret_cast<uint64_t>(part);
 #pragma unroll 1
       for (int pass = 0; pass < (done ? 1 : 2); ++pass) {
         const int cols = done ? D : D / 2;
@@ -864,11 +868,11 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
           const int rr = i * RPI + lane / CH, c = lane % CH;
           const uint64_t to_at = __shfl_sync(0xffffffffu, mine_at, rr);
           const uint4 v = *reinterpret_cast<const uint4*>(place((r & ~31) + rr, c));
-          if (rr < live) reinterpret_cast<uint4*>(to_at)[pass * CH + c] = v;
+          if (rr < live && in_bounds(to_at != 0, p.c.status, kSiteAttendRow)) reinterpret_cast<uint4*>(to_at)[pass * CH + c] = v;
         }
         __syncwarp();
       }
-      if (there && sh.any_nan[seg & 3]) {
+      if (there && fits && sh.any_nan[seg & 3]) {
 #pragma unroll 1
         for (int d = 0; d < D; ++d)
           if (sh.nan_first[seg & 3][d] < limit) {
@@ -879,7 +883,7 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
           }
       }
       tc::fence_before();
-      if (there) {
+      if (there && fits) {
         if (done) {
           if (p.lse) p.lse[to] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.69314718056f;
         } else {
@@ -891,7 +895,9 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
       TC_MEET();
       const int2 who = item_stretches<kOver>(sh.line, x);
       const int first = who.x, last = who.y;
-      if (threadIdx.x == 0) sh.last = arrive_count(&p.counters[first]) == last - first;
+      const bool fits = in_bounds(first >= 0 && first < last && last < sh.line.stretches && sh.line.stretches <= kAttendTcCtas &&
+                                      (int)blockIdx.x >= first && (int)blockIdx.x <= last, p.c.status, kSiteAttendPart);
+      if (threadIdx.x == 0) sh.last = fits && arrive_count(&p.counters[first]) == last - first;
       TC_MEET();
       if (sh.last) {
         if (mine) {
@@ -913,7 +919,8 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
               const float2 ml = __ldcg(&p.part_ml[part(c, lane)]);
               sum += ml.y * fast_exp2(ml.x - base);
             }
-            if (p.lse) p.lse[to] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.69314718056f;
+            if (p.lse && in_bounds(to < p.total_rows * p.H, p.c.status, kSiteAttendRow))
+              p.lse[to] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.69314718056f;
           }
           const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll 1
@@ -958,7 +965,7 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
               for (int i = 0; i < ROWS; ++i) {
                 const float total = __shfl_sync(0xffffffffu, sum, (r0 + i) & 31);
                 const uint64_t row_to = __shfl_sync(0xffffffffu, (uint64_t)to, (r0 + i) & 31);
-                if (r0 + i < rows) {
+                if (r0 + i < rows && in_bounds((int64_t)row_to < p.total_rows * p.H, p.c.status, kSiteAttendRow)) {
                   if (c0 + n <= last) {
                     float* keep = p.part_o + part(first, r0 + i) * D + lane * V;
 #pragma unroll

@@ -154,6 +154,9 @@ __global__ void __launch_bounds__(128, MAXV == 8 ? 9 : 1) append_kernel(AppendPa
   if (slot >= p.c.max_pages) return;
   const int t0 = max(start - slot * T, 0), t1 = min(len - slot * T, T);  // new tokens of this page
   if (t1 <= t0) return;
+  if (!in_bounds(i >= 0 && i < p.n && r0 + (int64_t)slot * T - start + t0 >= r0 && r0 + (int64_t)slot * T - start + t1 <= r1,
+                 p.c.status, kSiteAppendRow))
+    return;
   const int page = p.c.table[(int64_t)seq * p.c.max_pages + slot];
   if ((unsigned)page >= (unsigned)p.c.pages) {
     if (threadIdx.x == 0) set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
@@ -273,7 +276,7 @@ __device__ int find_free(const CacheDev& c, int want, int32_t* list, int* tmp) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       if (r[j] == 0) {
-        if (at < want) list[at] = p + j;
+        if (at < want && in_bounds(at >= 0 && at < c.pages, c.status, kSiteFreeList)) list[at] = p + j;
         ++at;
       }
     found += total;
@@ -346,7 +349,9 @@ __global__ void __launch_bounds__(kPlanThreads) extend_kernel(PlanParams p) {
       int rank = at + block_exclusive_scan(need, tmp, &t);
       at += t;
       for (int j = 0; j < need; ++j) {
+        if (!in_bounds(rank >= 0 && rank + j < c.pages && have + j < c.max_pages, c.status, kSiteFreeList)) break;
         const int pg = p.free_list[rank + j];
+        if (!in_bounds((unsigned)pg < (unsigned)c.pages, c.status, kSiteTable)) break;
         c.table[(int64_t)s * c.max_pages + have + j] = pg;
         c.refs[pg] = 1;
       }
@@ -408,7 +413,8 @@ __global__ void __launch_bounds__(kPlanThreads) fork_kernel(PlanParams p) {
       }
       const int rank = at + block_exclusive_scan(need, tmp, &t);
       at += t;
-      if (need) {
+      if (need && in_bounds(rank >= 0 && rank < c.pages && (len >> c.log2T) < c.max_pages, c.status, kSiteFreeList) &&
+          in_bounds((unsigned)p.free_list[rank] < (unsigned)c.pages, c.status, kSiteTable)) {
         const int pg = p.free_list[rank], j = len >> c.log2T;
         p.new_pages[i] = make_int2(c.table[(int64_t)a * c.max_pages + j], pg);
         c.table[(int64_t)b * c.max_pages + j] = pg;
@@ -422,6 +428,7 @@ __global__ void __launch_bounds__(kPlanThreads) fork_kernel(PlanParams p) {
       const int a = p.a[i], b = p.b[i], m = c.length[a] >> c.log2T;
       for (int j = lane; j < m; j += 32) {
         const int pg = c.table[(int64_t)a * c.max_pages + j];
+        if (!in_bounds((unsigned)pg < (unsigned)c.pages && j < c.max_pages, c.status, kSiteTable)) break;
         c.table[(int64_t)b * c.max_pages + j] = pg;
         atomicAdd(&c.refs[pg], 1);
       }
@@ -438,6 +445,7 @@ __global__ void __launch_bounds__(256) copy_pages_kernel(CacheDev c, const int2*
   pdl_wait();
   const int2 ft = pairs[blockIdx.x];
   if (ft.x < 0) return;
+  if (!in_bounds(ft.x < c.pages && (unsigned)ft.y < (unsigned)c.pages, c.status, kSiteCopyPage)) return;
   const int layer = blockIdx.y, kv = blockIdx.z & 1, chunk = blockIdx.z >> 1;
   const int64_t from = (int64_t)layer * c.pages + ft.x, to = (int64_t)layer * c.pages + ft.y;
   uint8_t* base = kv ? c.v : c.k;
@@ -516,11 +524,11 @@ __global__ void __launch_bounds__(1024) compact_count_kernel(CountParams p) {
   int n = 0, mine = len;
   for (int base = 0; base < flags; base += 1024) {
     const int pos = base + threadIdx.x;
-    const int k = pos < flags && p.keep[k0 + pos] != 0;
+    const int k = pos < flags && in_bounds(k0 + pos < p.total_keep, p.c.status, kSiteKeepList) && p.keep[k0 + pos] != 0;
     if (pos < flags && !k) mine = min(mine, pos);
     int t = 0;
     const int at = n + block_exclusive_scan(k, tmp, &t);
-    if (k) p.list[k0 + at] = pos;
+    if (k && in_bounds(k0 + at < p.total_keep, p.c.status, kSiteKeepList)) p.list[k0 + at] = pos;
     n += t;
   }
   mine = __reduce_min_sync(0xffffffffu, mine);
@@ -580,14 +588,19 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(PlanParams p
       const int to = pages_of(p.count[i], c), head = p.head[i];
       for (int j = lane; j < max(m, to); j += 32) {
         int32_t* e = &c.table[(int64_t)s * c.max_pages + j];
+        if (!in_bounds(j < c.max_pages && (j < lead || j >= to || (unsigned)(head + j - lead) < (unsigned)c.pages), c.status,
+                       kSiteFreeList))
+          break;
         if (j < m) {
           const int pg = *e;
+          if (!in_bounds((unsigned)pg < (unsigned)c.pages, c.status, kSiteTable)) break;
           p.old_table[(int64_t)i * c.max_pages + j] = pg;
           if (j >= lead) atomicSub(&c.refs[pg], 1);
         }
         if (j >= lead) {
           const bool fresh = j < to;
           const int pg = fresh ? p.free_list[head + j - lead] : -1;
+          if (!in_bounds(!fresh || (unsigned)pg < (unsigned)c.pages, c.status, kSiteTable)) break;
           *e = pg;
           if (fresh) atomicAdd(&c.refs[pg], 1);
         }
@@ -664,14 +677,22 @@ __global__ void __launch_bounds__(128) compact_move_kernel(MoveParams p) {
     const int first = (p.lead[i] + fresh - p.head[i]) * T;  // new position of the page's first token
     const int tokens = min(p.count[i] - first, T), nv = tokens * vpr;
     __syncthreads();
-    if ((int)threadIdx.x < tokens) {
+    bool fits = in_bounds(i < p.n && fresh < p.c.pages && (unsigned)p.free_list[fresh] < (unsigned)p.c.pages, p.c.status, kSiteMoveToken);
+    if (fits && (int)threadIdx.x < tokens) {
       // kept flagged tokens come from the list, tokens past the flags in order
       const int q = first + threadIdx.x;
       const int2 info = p.info[i];  // listed tokens, flags
-      const int pos = q < info.x ? p.list[p.keep_off[i] + q] : info.y + q - info.x;
-      src[threadIdx.x] = make_int2(p.old_table[(int64_t)i * p.c.max_pages + (pos >> p.c.log2T)], pos & (T - 1));
+      const bool listed = in_bounds(q >= info.x || p.keep_off[i] + q < p.keep_off[i + 1], p.c.status, kSiteKeepList);
+      const int pos = q < info.x && listed ? p.list[p.keep_off[i] + q] : info.y + q - info.x;
+      fits = listed && in_bounds(pos >= 0 && (pos >> p.c.log2T) < p.c.max_pages, p.c.status, kSiteMoveToken);
+      const int page = fits ? p.old_table[(int64_t)i * p.c.max_pages + (pos >> p.c.log2T)] : 0;
+      fits = fits && in_bounds((unsigned)page < (unsigned)p.c.pages, p.c.status, kSiteMoveToken);
+      src[threadIdx.x] = make_int2(page, pos & (T - 1));
     }
     __syncthreads();
+#if OCCAM_CHECKED
+    if (!__syncthreads_and(fits)) continue;
+#endif
     const int to_page = p.free_list[fresh];
     for (int item = blockIdx.x; item < per_page; item += gridDim.x) {
       const int g = item % hg, kv = item / hg & 1, layer = p.layer0 + item / hg / 2;

@@ -26,6 +26,15 @@ enum CheckSite {
   kSiteFusedSlot = 9,      // fused Stage II: an s2(r) partial slot
   kSiteTwoPassKeyRow = 10, // two-pass Stage II: an S1 key row
   kSiteMutualRow = 11,     // mutual Stage I: a row of the segment
+  kSiteAppendRow = 12,     // cache append: the rows of a block
+  kSiteFreeList = 13,      // page calls: a place of the list of free pages
+  kSiteTable = 14,         // page calls: a new page and its table column
+  kSiteCopyPage = 15,      // fork: a copied page
+  kSiteKeepList = 16,      // compact: a keep flag, a place of the list of kept tokens
+  kSiteMoveToken = 17,     // compact: a moved token's sequence, old page and new page
+  kSiteAttendKey = 18,     // attention: a key's table column and flag
+  kSiteAttendRow = 19,     // attention: a query's or a result's row
+  kSiteAttendPart = 20,    // attention: the stretches of a split item (counters and partial results)
 };
 
 // True when ok; otherwise (checked builds) records the first violation and
