@@ -141,7 +141,9 @@ int occam_workspace_size(const occam_batch* batch, int32_t H1, int32_t H2, size_
  * (compiled with OCCAM_CHECKED=1, every computed index of the kernels'
  * gathers, lists and scans tested against its buffer) a violation records
  * OCCAM_ERR_BOUNDS, and the int32 after the status word (workspace bytes
- * 4..7) names the check site that failed first; both are cleared here. */
+ * 4..7) names the check site that failed first.
+ * That word also has a bit (2^30) that a refused occam_cache_extend sets; both
+ * words are cleared. */
 int occam_get_status(void* workspace, int32_t* status, occam_stream_t stream);
 
 /* Stage-I scores (Sec. 3.4, Eqs. 4 and 6; App. A, Eqs. 10 and 13).
@@ -526,7 +528,8 @@ int occam_cache_append(const occam_cache* cache, int32_t layer, int32_t dtype, i
  *   lse [total_rows, heads] fp32 (NULL to skip) = log sum_k exp(scale q.k).
  * A row that sees no token gives 0 and -inf. Scores, statistics and sums are
  * in fp32; probabilities are rounded to f16 for the product with the codes (11
- * bits down to 2^-21 of a row's largest, lost below 2^-32).
+ * bits down to 2^-15 of a row's largest, lost below 2^-26; without v's scales falling
+ * within a sequence 2^-21 and 2^-32).
  * Scales of v within a sequence may span a factor of 2^60. max_rows: the
  * largest row_off[i+1] - row_off[i] (it chooses the kernels; results are right
  * for any value). heads <= 64 * cache heads. A call of more than 2^31 - 2^16
@@ -568,7 +571,8 @@ int occam_cache_fork(const occam_cache* cache, int32_t n, const int32_t* src, co
  * pages, whose blocks get the scale of their own values (as in
  * occam_cache_append) in layers layer_begin .. layer_end-1 -- the other
  * layers' codes are not moved: give every layer that holds the sequence.
- * New pages are taken before the old ones are given back. */
+ * New pages are taken before the old ones are given back, and a last page that is not
+ * full always moves, also where every token is kept. */
 int occam_cache_compact(const occam_cache* cache, int32_t layer_begin, int32_t layer_end, int32_t n,
                         const int32_t* seqs, const uint8_t* keep, const int64_t* keep_off, int64_t total_keep,
                         void* workspace, size_t workspace_bytes, occam_stream_t stream);

@@ -3,11 +3,11 @@
 //
 // The same running softmax as attend.cu, for 256 query rows (token, head of
 // the group) against tiles of 128 keys. 4 D operations and one exponential a
-// (row, key). A prefix of 8,257 tokens, 32 query and 8 key heads of 128 dims, takes 0.545 ms,
-// 1.0 PFLOP/s: 3,900 cycles a tile where the products alone need 2,050 and shared
+// (row, key). A prefix of 8,257 tokens, 32 query and 8 key heads of 128 dims, takes 0.535 ms,
+// 1.04 PFLOP/s: 3,800 cycles a tile where the products alone need 2,050 and shared
 // memory's traffic (codes, their f16 form, operands: 384 KB) 3,070; bound by the
 // round scores -> softmax -> P -> products, of which two halves a row tile are under way.
-// (Without the softmax 0.47 ms, without the exponentials 0.53, without the conversion 0.55.)
+// (At 0.57 ms: without the softmax 0.47, without the exponentials 0.53, without the conversion 0.55.)
 // One CTA an SM, 16 warps in five roles:
 //  - warp 13 plans: it walks the key tiles, fills a ring of step records (masks,
 //    scales, references) and has each page's block copied to shared memory as it is;
@@ -18,12 +18,13 @@
 //  - warps 12 and 14 issue the products: S = Q K^T into tensor memory, O += P V with P
 //    read from tensor memory, each for a row tile of 128, 64 keys at a time: while a
 //    row tile's softmax works on one half of its scores, the other half is multiplied
-//    (128 keys at a time, 64 of P: measured slower, 0.61 ms where this takes 0.55);
+//    (128 keys at a time, 64 of P: measured slower, 0.61 ms where this took 0.55);
 //  - warps 0-3 and 4-7 hold a row a thread: scores from tensor memory, maximum,
 //    exponentials, P back over the scores as f16.
 // O stays in tensor memory. It is rescaled only where a row's maximum grew by more than
 // 2^8 since its last reference, or where v's scale left the window that P
-// is held in; both references are undone at the end.
+// is held in; both references are undone at the end. P is rounded to f16 (see attend.cu), l sums the
+// unrounded P.
 #include <algorithm>
 #include <atomic>
 
@@ -730,7 +731,7 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
           TC_WAIT(sh.s_full[t][h], (it >> 1) & 1);
           tc::fence_after();
           // The row's scores of 64 keys: the maximum, and hidden ones -inf. The exponentials read them
-          // again, 32 at a time in a rolled loop: 64 held in registers took 0.63 ms where this takes 0.61
+          // again, 32 at a time in a rolled loop: 64 held in registers took 0.63 ms where this took 0.61
           // (32 questions with keep flags), a rolled loop here too 0.63.
           float m = top;
 #pragma unroll

@@ -34,7 +34,7 @@ constexpr int kPlanThreads = 1024;
 // One CTA per (touched page, head, K or V): the new rows' values of the block
 // stay in registers between the block's maximum and the rounding, so they are
 // read once. Bound by HBM (2 bytes read and 1 written a value): 20 k rows of 32 heads of
-// 128 dims take 85 us, 5.8 TB/s. Four heads a CTA with the next head's rows
+// 128 dims take 86 us, 5.8 TB/s (66 % DRAM, 71 % issue active). Four heads a CTA with the next head's rows
 // under way measured slower (156 us where one took 121): fewer CTAs fit an SM. One
 // row each of 64 sequences takes 10 us, the chain of dependent loads (offsets,
 // table, rows, scale).
@@ -125,7 +125,8 @@ __device__ __noinline__ uint2 codes8_by_division(uint4 r, float scale) {
 // MAXV: 8-value vectors a thread holds of a block (128 threads; page_tokens * D / 8 / 128 at most).
 // grid: x over (head, K or V), y and z over slots.
 // (20 k rows, 64 tokens x 128 dims a block: nine CTAs an SM 85 us, eight 90, ten 95, 256 threads
-// a CTA 111.)
+// a CTA 111. 128 x 128 values a block have no bound: 160 registers and three CTAs an SM, 136 us of 20 k rows;
+// bounds of four, five and six gave 115, 105 and 105.)
 template <bool BF16, int D, int MAXV>
 __global__ void __launch_bounds__(128, MAXV == 8 ? 9 : 1) append_kernel(AppendParams p) {
   __shared__ float r[4];
@@ -649,8 +650,9 @@ struct MoveParams {
 // One CTA per (new page, layer, K or V, group of heads), a block of codes at
 // a time: the kept rows are gathered once, their common scale found, the codes
 // rounded to it (a shift of the exponent where both scales are powers of
-// two) and written once. Bound by HBM's single 128-byte rows: 8 x 240 scattered rows
-// of 2 x 32 heads in 11 layers take about 95 us, 4.5 TB/s of bytes moved.
+// two) and written once. 8 x 350 scattered rows of 2 x 32 heads in 11 layers take 95 to 102 us, 4.5 TB/s of
+// bytes moved, at 56 % DRAM and 59 % issue active with 48 % of the warps: bound by neither alone, but
+// by a head's chain (loads, maximum across a barrier, stores) before the next head's loads.
 // MAXV: 16-code vectors a thread holds (128 threads).
 constexpr int kMoveHeads = 4;
 // A code times its scale may round to 2^128 (256 x 2^120, from values near bf16's end): it counts as the
