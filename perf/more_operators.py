@@ -298,18 +298,17 @@ def run(st):
 def _own_prompt(st):
     import paper_2605_29657_gb300 as occ
 
-    out, lse = occ.occam_prompt_attend(st["q"], st["k"], st["v"], st["row_off"], st["max_rows"], st["ws"],
-                                       key_off=st["key_off"], max_keys=st["max_keys"], causal=st["case"]["causal"])
+    out, lse = occ.occam_prompt_attend(st["q"], st["k"], st["v"], st["row_off"], st["ws"], key_off=st["key_off"],
+                                       causal=st["case"]["causal"])
     return {"out": out, "lse": lse}
 
 
 def _own_train(st):
     import paper_2605_29657_gb300 as occ
 
-    keys = dict(key_off=st["key_off"], max_keys=st["max_keys"], causal=st["case"]["causal"])
-    out, lse = occ.occam_prompt_attend(st["q"], st["k"], st["v"], st["row_off"], st["max_rows"], st["ws"], **keys)
-    dq, dk, dv = occ.occam_prompt_attend_grad(st["q"], st["k"], st["v"], out, lse, st["dout"], st["row_off"], st["max_rows"],
-                                              st["ws"], **keys)
+    keys = dict(key_off=st["key_off"], causal=st["case"]["causal"])
+    out, lse = occ.occam_prompt_attend(st["q"], st["k"], st["v"], st["row_off"], st["ws"], **keys)
+    dq, dk, dv = occ.occam_prompt_attend_grad(st["q"], st["k"], st["v"], out, lse, st["dout"], st["row_off"], st["ws"], **keys)
     return {"out": out, "lse": lse, "dq": dq, "dk": dk, "dv": dv}
 
 
