@@ -582,6 +582,57 @@ int occam_cache_compact(const occam_cache* cache, int32_t layer_begin, int32_t l
 int occam_cache_release(const occam_cache* cache, int32_t n, const int32_t* seqs, void* workspace,
                         size_t workspace_bytes, occam_stream_t stream);
 
+/* ------------------------------------------------------------------ whole prompts: attention of 16-bit rows, and its gradient
+ * What the rows of a prompt (or of an image in a vision tower) do before they enter
+ * a cache: attention among themselves at full precision, for packed sequences of
+ * different lengths. */
+
+/* Sequence i's queries are rows row_off[i] .. row_off[i+1] of q ([total_rows,
+ * heads, dim]), its keys and values rows key_off[i] .. key_off[i+1] of k and v
+ * ([total_keys, kv_heads, dim]); key_off may be row_off. Offsets are int64 [n+1], device.
+ * Query head h reads key head h / (heads / kv_heads). causal: the queries are
+ * the last of their sequence's tokens, so the query at place j of r sees the keys
+ * at places 0 .. m - r + j of m (none where that is negative); else all m. Values are
+ * OCCAM_BF16 or OCCAM_F16, heads dense, rows q_row / k_row / v_row elements apart
+ * (at least heads * dim; views of one projection fit); bases 16-byte aligned, strides
+ * and dim multiples of 8, dim 8..128. heads <= 1024, n <= 2^20. Rows that belong to no
+ * sequence are not read into any result. Offsets that do not fit record
+ * OCCAM_ERR_INVALID_ARG, and that sequence is left out. */
+typedef struct occam_prompt_args {
+  int32_t dtype;
+  int32_t heads;
+  int32_t kv_heads;
+  int32_t dim;
+  int32_t causal;
+  int32_t n;
+  int64_t total_rows;
+  int64_t total_keys;
+  const void* q;
+  const void* k;
+  const void* v;
+  int64_t q_row;
+  int64_t k_row;
+  int64_t v_row;
+  const int64_t* row_off;
+  const int64_t* key_off;
+  float scale; /* 0: 1 / sqrt(dim) */
+} occam_prompt_args;
+
+/* Scratch of the two calls below for total_rows query rows (workspace convention
+ * as above: 256-byte aligned, zero-filled before first use, status word at its start). */
+int occam_prompt_workspace_size(int64_t total_rows, int32_t heads, size_t* bytes);
+
+/* out [total_rows, heads, dim] (q's type, dense, 16-byte aligned) = sum_k p_k v_k / sum_k p_k,
+ *   p_k = exp(scale q.k - max) over the keys that the row sees;
+ * lse [total_rows, heads] fp32 (NULL to skip) = log sum_k exp(scale q.k).
+ * A row that sees no key gives 0 and -inf; rows of no sequence are left as they
+ * are. Scores, statistics and sums are in fp32; p is rounded to the values' type for its
+ * product with v. A value that is not finite reaches the rows that see
+ * it and no others. out and lse overlap no input. After OCCAM_ERR_TIMEOUT the results
+ * are undefined; the workspace stays usable. */
+int occam_prompt_attend(const occam_prompt_args* args, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                        occam_stream_t stream);
+
 /* Diagnostic of the bounded device-side waits (no fault, trap or hang). One
  * warp waits, each time for about limit_ns (1 .. 1e9), on an mbarrier that
  * nothing completes (the tensor-core kernels' timer-bounded wait and the

@@ -52,3 +52,7 @@ from ._cache import (  # noqa: F401
     occam_rope,
     rope_axes,
 )
+from ._prompt import (  # noqa: F401
+    alloc_prompt_workspace,
+    occam_prompt_attend,
+)

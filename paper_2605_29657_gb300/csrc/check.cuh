@@ -35,6 +35,7 @@ enum CheckSite {
   kSiteAttendKey = 18,     // attention: a key's table column and flag
   kSiteAttendRow = 19,     // attention: a query's or a result's row
   kSiteAttendPart = 20,    // attention: the stretches of a split item (counters and partial results)
+  kSitePromptRow = 21,     // a prompt's attention: a result's row
 };
 
 // True when ok; otherwise (checked builds) records the first violation and

@@ -1,0 +1,199 @@
+// prompt.cuh -- what the kernels of a whole prompt's attention (prompt.cu) and
+// of its gradient (prompt_grad.cu) share (internal header): parameters, the list
+// of items and how CTAs take them, bounded waits.
+//
+// An item is a block of rows of one sequence and some heads. Items are taken from
+// a counter, the first ones by block index: CTAs that had short items take more of them.
+// A sequence's heaviest items come first, so that what is left at the end is short.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_fp16.h>
+
+#include "cache.cuh"
+#include "overlap.cuh"
+#include "tc5.cuh"
+
+namespace occam {
+
+struct PromptParams {
+  int n, H, Hkv, G, log2P, causal, dim;  // 2^log2P heads of a group are packed as rows of a tile
+  int64_t total_rows, total_keys;
+  const int64_t* row_off;
+  const int64_t* key_off;
+  float scale, scale_log2;
+  uint16_t* out;
+  float* lse;
+  int32_t* status;
+  int32_t* counters;  // [0] items taken beyond the first of each CTA, [1] CTAs that have left; zero between calls
+};
+
+// The smallest power of two above any factor of a score: never 0, so that a hidden key's -inf stays
+constexpr float kLeastFactor = 1.2e-38f;
+
+struct PromptSeq {
+  int64_t row0, key0;
+  int rows, keys;
+};
+// Sequence i; no rows and no keys if its offsets do not fit (recorded).
+__device__ __forceinline__ PromptSeq prompt_seq(const PromptParams& p, int i) {
+  PromptSeq s;
+  s.row0 = p.row_off[i];
+  const int64_t r1 = p.row_off[i + 1];
+  s.key0 = p.key_off[i];
+  const int64_t k1 = p.key_off[i + 1];
+  if (s.row0 >= 0 && r1 >= s.row0 && r1 <= p.total_rows && s.key0 >= 0 && k1 >= s.key0 && k1 <= p.total_keys) {
+    s.rows = (int)(r1 - s.row0);
+    s.keys = (int)(k1 - s.key0);
+    return s;
+  }
+  set_status(p.status, OCCAM_ERR_INVALID_ARG);
+  s.row0 = s.key0 = 0;
+  s.rows = s.keys = 0;
+  return s;
+}
+// Keys that the row at place tok of its sequence sees; none (never fewer) where the rows outnumber the keys.
+__device__ __forceinline__ int prompt_limit(const PromptParams& p, int rows, int keys, int tok) {
+  return p.causal ? max(keys - rows + tok + 1, 0) : keys;
+}
+
+// A CTA's item, told to its roles. Fields after `hb` are the kernel's own.
+struct PromptItem {
+  int64_t row0, key0;
+  int rows, keys;
+  int tile, hb;    // the block of rows (or keys) and the block of heads
+  int steps;       // 0: there is none, the CTA is done
+  int nk[2];       // steps of each row tile
+};
+
+// How a kernel cuts a sequence: `len` rows (or keys) in blocks of `block`, head blocks inner.
+// The prefix sums of item counts over kChunks runs of sequences are in shared memory.
+constexpr int kChunks = 128;
+struct PromptList {
+  int first[kChunks + 1];
+  int part[4];
+};
+
+// Block-wide, all threads (at least 128). COUNT(seq) gives a sequence's items.
+template <class Count>
+__device__ __forceinline__ void prompt_list(const PromptParams& p, PromptList& l, const Count& count) {
+  const int t = threadIdx.x, per = (p.n + kChunks - 1) / kChunks;
+  int mine = 0, incl = 0;
+  if (t < kChunks) {
+    for (int i = t * per; i < min((t + 1) * per, p.n); ++i) mine += count(prompt_seq(p, i));
+    incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, incl, o);
+      if ((t & 31) >= o) incl += x;
+    }
+    if ((t & 31) == 31) l.part[t >> 5] = incl;
+  }
+  __syncthreads();
+  if (t < kChunks) {
+    for (int w = 0; w < (t >> 5); ++w) incl += l.part[w];
+    l.first[t + 1] = incl;
+    if (t == 0) l.first[0] = 0;
+  }
+  __syncthreads();
+}
+// One warp: the sequence of item `at` (below first[kChunks]) and its place among that sequence's items.
+template <class Count>
+__device__ __forceinline__ PromptSeq prompt_find(const PromptParams& p, const PromptList& l, const Count& count, int at, int* place) {
+  const int lane = threadIdx.x & 31, per = (p.n + kChunks - 1) / kChunks;
+  int before = 0;
+#pragma unroll
+  for (int k = 0; k < kChunks / 32; ++k) before += l.first[k * 32 + lane + 1] <= at;
+  const int c = __reduce_add_sync(0xffffffffu, before);
+  int base = l.first[c];
+  const int end = min((c + 1) * per, p.n);
+  PromptSeq s;
+  for (int i = c * per; i < end; i += 32) {
+    s.rows = s.keys = 0;
+    s.row0 = s.key0 = 0;
+    int mine = 0;
+    if (i + lane < end) {
+      s = prompt_seq(p, i + lane);
+      mine = count(s);
+    }
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += x;
+    }
+    const unsigned past = __ballot_sync(0xffffffffu, at < base + incl);
+    if (past) {
+      const int from = __ffs(past) - 1;
+      *place = at - base - __shfl_sync(0xffffffffu, incl - mine, from);
+      s.row0 = __shfl_sync(0xffffffffu, s.row0, from);
+      s.key0 = __shfl_sync(0xffffffffu, s.key0, from);
+      s.rows = __shfl_sync(0xffffffffu, s.rows, from);
+      s.keys = __shfl_sync(0xffffffffu, s.keys, from);
+      return s;
+    }
+    base += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  *place = 0;  // (not reached)
+  s.rows = s.keys = 0;
+  return s;
+}
+
+// The last CTA to leave clears the counters, whatever happened: the next call has to find zeros. By one thread,
+// after the CTA's last item was taken.
+__device__ __forceinline__ void prompt_leave(const PromptParams& p, int ctas) {
+  if (atomicAdd(&p.counters[1], 1) == ctas - 1) {
+    p.counters[0] = 0;
+    p.counters[1] = 0;
+  }
+}
+
+constexpr uint64_t kPromptWaitNs = 2000000000ull;
+// a bounded wait on a barrier phase; false (recorded) if it ran out or another role gave up
+__device__ __forceinline__ bool prompt_wait_long(uint64_t* bar, uint32_t parity, volatile int* stop, int32_t* status) {
+  const uint64_t t0 = tc::globaltimer();
+  while (!tc::bar_try(bar, parity)) {
+    if (*stop || tc::globaltimer() - t0 > kPromptWaitNs) {
+      *stop = 1;
+      set_status(status, OCCAM_ERR_TIMEOUT);
+      return false;
+    }
+  }
+  return true;
+}
+#define PROMPT_WAIT(bar, parity) \
+  if (!tc::bar_try(&(bar), (parity)) && !prompt_wait_long(&(bar), (parity), &sh.stop, p.status)) return;
+
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
+  if (BF16) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+  return tc::pack_f16(lo, hi);
+}
+
+// Tensor map of rows [rows][heads][dim] of 16-bit values, `row` elements apart, as boxes of 64 dims x
+// box_heads x box_rows with the 128-byte swizzle; dims past the last one are read as zeros.
+bool encode_rows(CUtensorMap* m, const void* at, bool bf16, int dim, int heads, int64_t rows, int64_t row, int box_heads,
+                 int box_rows);
+
+// Byte offsets of the workspace: the status word (8 bytes) and the counters, zero between calls; then what the
+// gradient writes before it reads it.
+struct PromptWs {
+  size_t rows;  // float2 [total_rows, heads]
+  size_t total;
+};
+inline PromptWs prompt_ws(int64_t total_rows, int heads) {
+  PromptWs w;
+  w.rows = 256;
+  w.total = w.rows + cache_align((size_t)total_rows * heads * 8);
+  return w;
+}
+
+// Checks the arguments and fills in what both entry points share.
+int prompt_params(const occam_prompt_args* a, void* workspace, size_t workspace_bytes, PromptParams* p);
+// Whether a result (of 16-bit elements) shares memory with q, k or v.
+bool prompt_meets_inputs(const occam_prompt_args* a, const Extent& x);
+
+}  // namespace occam
