@@ -513,6 +513,35 @@ int occam_cache_append(const occam_cache* cache, int32_t layer, int32_t dtype, i
                        int64_t k_row, const void* v, int64_t v_row, int32_t n, const int32_t* seqs,
                        const int64_t* row_off, void* workspace, size_t workspace_bytes, occam_stream_t stream);
 
+/* occam_cache_append with occam_rope on the way, in one launch. Keys (not values) are turned by
+ * their rows' positions as in occam_rope (rot, pairing, positions, inv_freq and
+ * axis as there, rot <= dim); the turned keys stay in fp32 until they are rounded to codes, once. q (NULL:
+ * none): queries of the same rows, turned to q->dst (every row of total_rows, whatever
+ * the cache's state; in place and strides as in occam_rope, no overlap with k or v). Everything
+ * else as in occam_cache_append. */
+typedef struct occam_append_rope_args {
+  int32_t layer;
+  int32_t dtype;
+  int32_t n;
+  int32_t rot;
+  int32_t pairing;
+  int32_t axes;
+  int64_t total_rows;
+  const void* k;
+  int64_t k_row;
+  const void* v;
+  int64_t v_row;
+  const int32_t* seqs;
+  const int64_t* row_off;
+  const int32_t* positions;
+  int64_t pos_stride;
+  const float* inv_freq;
+  const int32_t* axis;
+  const occam_rope_tensor* q;
+} occam_append_rope_args;
+int occam_cache_append_rope(const occam_cache* cache, const occam_append_rope_args* args, void* workspace,
+                            size_t workspace_bytes, occam_stream_t stream);
+
 /* Attention over the cache. Rows row_off[i] .. row_off[i+1] of q ([total_rows,
  * heads, dim] bf16 or f16, rows q_row elements apart) are the queries of
  * the last tokens of sequence seqs[i], whose keys and values are in the cache

@@ -44,6 +44,7 @@ from ._lib import (  # noqa: F401
 from ._cache import (  # noqa: F401
     PagedCache,
     occam_cache_append,
+    occam_cache_append_rope,
     occam_cache_attend,
     occam_cache_compact,
     occam_cache_extend,

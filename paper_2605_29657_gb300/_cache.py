@@ -16,6 +16,7 @@ import torch
 
 from ._lib import (
     OCCAM_ERR_INVALID_ARG,
+    CAppendRopeArgs,
     CAttendArgs,
     CCache,
     CRopeTensor,
@@ -131,11 +132,7 @@ def occam_rope(q, k, positions, inv_freq, axis, pairing: str = "half", inverse: 
         _bad("q must be a CUDA tensor [rows, heads, dim] of bfloat16, float16 or float32")
     rows, _, dim = q.shape
     dtype, at = q.dtype, q.get_device()
-    pairs = _vector(inv_freq, torch.float32, None, "inv_freq", at).shape[0]
-    _vector(axis, torch.int32, pairs, "axis", at)
-    if not isinstance(positions, torch.Tensor) or positions.get_device() != at or positions.dtype != torch.int32 or \
-            positions.dim() != 2 or positions.shape[1] != rows or (rows > 1 and positions.stride(1) != 1):
-        _bad(f"positions must be an int32 tensor [axes, rows] on cuda:{at}, dense in rows")
+    pairs = _turns(positions, inv_freq, axis, rows, at)
     on = _on(stream, at)
     packed, out_q = _rope_tensor(q, out_q, "q", rows, dim, dtype, at, stream)
     n = 1
@@ -148,6 +145,16 @@ def occam_rope(q, k, positions, inv_freq, axis, pairing: str = "half", inverse: 
     _call(at, library().occam_rope, _DTYPE[dtype], rows, dim, 2 * pairs, _PAIRING[pairing], int(bool(inverse)),
           positions.data_ptr(), positions.stride(0), positions.shape[0], inv_freq.data_ptr(), axis.data_ptr(), n, packed, on)
     return out_q, out_k
+
+
+def _turns(positions, inv_freq, axis, rows: int, at: int) -> int:
+    """The number of pairs."""
+    pairs = _vector(inv_freq, torch.float32, None, "inv_freq", at).shape[0]
+    _vector(axis, torch.int32, pairs, "axis", at)
+    if not isinstance(positions, torch.Tensor) or positions.get_device() != at or positions.dtype != torch.int32 or \
+            positions.dim() != 2 or positions.shape[1] != rows or (rows > 1 and positions.stride(1) != 1):
+        _bad(f"positions must be an int32 tensor [axes, rows] on cuda:{at}, dense in rows")
+    return pairs
 
 
 def _rope_tensor(x, out, name, rows, dim, dtype, at, stream):
@@ -276,6 +283,36 @@ def occam_cache_append(cache: PagedCache, layer: int, k, v, seqs, row_off, ws=No
     _vector(row_off, torch.int64, n + 1, "row_off", cache.at)
     _call(cache.at, library().occam_cache_append, cache._ref, int(layer), _DTYPE[k.dtype], k.shape[0], _ptr(k), _row_stride(k),
           _ptr(v), _row_stride(v), n, _ptr(seqs), _ptr(row_off), wp, wn, _on(stream, cache.at))
+
+
+def occam_cache_append_rope(cache: PagedCache, layer: int, q, k, v, seqs, row_off, positions, inv_freq, axis,
+                            pairing: str = "half", out_q=None, ws=None, stream=None):
+    """occam_cache_append with the keys turned by their positions (as occam_rope, in fp32 until they
+    are rounded to codes) and the queries q [rows, heads, dim] (None: none) of the same rows
+    turned in the same launch. Returns the turned queries: a new dense tensor unless out_q is given (q
+    itself: in place)."""
+    wp, wn = _workspace(cache, ws)
+    if pairing not in _PAIRING:
+        _bad(f"pairing must be one of {sorted(_PAIRING)}")
+    _rows_tensor(k, "k", _ROWS, cache.at, cache.heads, cache.dim)
+    _rows_tensor(v, "v", (k.dtype,), cache.at, cache.heads, cache.dim)
+    rows = k.shape[0]
+    if v.shape[0] != rows:
+        _bad("k and v must have as many rows")
+    n = _vector(seqs, torch.int32, None, "seqs", cache.at).shape[0]
+    _vector(row_off, torch.int64, n + 1, "row_off", cache.at)
+    pairs = _turns(positions, inv_freq, axis, rows, cache.at)
+    on = _on(stream, cache.at)
+    packed = None
+    if q is not None:
+        packed, out_q = _rope_tensor(q, out_q, "q", rows, cache.dim, k.dtype, cache.at, stream)
+    elif out_q is not None:
+        _bad("out_q without q")
+    a = CAppendRopeArgs(int(layer), _ROWS[k.dtype], n, 2 * pairs, _PAIRING[pairing], positions.shape[0], rows, _ptr(k), _row_stride(k),
+                        _ptr(v), _row_stride(v), _ptr(seqs), _ptr(row_off), _ptr(positions), positions.stride(0), _ptr(inv_freq),
+                        _ptr(axis), packed)
+    _call(cache.at, library().occam_cache_append_rope, cache._ref, ctypes.byref(a), wp, wn, on)
+    return out_q
 
 
 def occam_cache_attend(cache: PagedCache, layer: int, q, seqs, row_off, max_rows: int, scale: float = 0.0,

@@ -1,0 +1,374 @@
+// append_rope.cu -- occam_cache_append_rope: keys turned by their positions on
+// the way into the paged 8-bit cache, values beside them, and the queries turned in the
+// same launch.
+//
+// A CTA of the first part takes one touched page and some heads of K or of V. Cosines
+// and sines of the page's tokens are computed once, into shared memory, and serve all its
+// heads of K; the turned values stay in registers as fp32 between the block's maximum and the
+// rounding, so keys are rounded once, to their codes. CTAs of the second part turn
+// the queries (rope_rows). Bound by HBM: queries 2 bytes read and written, keys and values 2 read and 1
+// written a value.
+#include <algorithm>
+#include <atomic>
+#include <type_traits>
+
+#include "append.cuh"
+#include "nvtx.cuh"
+#include "overlap.cuh"
+#include "rope.cuh"
+
+using namespace occam;
+
+namespace {
+
+constexpr int kThreads = 256;
+
+struct EnterParams {
+  AppendParams a;
+  RopeParams q;          // rows, angles and the queries (t[0]; no heads: none)
+  int k_heads, v_heads;  // heads a CTA takes of K, of V
+  int k_parts, parts;    // CTAs a page for K; in all
+  int64_t slots;
+  int64_t kv_ctas;
+  int64_t q_blocks;      // CTAs of a head group of the queries
+};
+
+template <int V>
+struct Raw;
+template <>
+struct Raw<8> {
+  uint4 w;
+  static constexpr int kWords = 4;
+};
+template <>
+struct Raw<4> {
+  uint2 w;
+  static constexpr int kWords = 2;
+};
+template <>
+struct Raw<1> {
+  uint16_t w;
+  static constexpr int kWords = 1;
+};
+template <bool BF16, int V>
+__device__ __forceinline__ void unpack(const Raw<V>& r, float (&x)[V]) {
+  if constexpr (V == 1) {
+    x[0] = BF16 ? __uint_as_float((uint32_t)r.w << 16) : __half2float(__ushort_as_half(r.w));
+  } else {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(&r.w);
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+      if (BF16) {
+        x[2 * i] = bf16_lo(w[i]);
+        x[2 * i + 1] = bf16_hi(w[i]);
+      } else {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+        x[2 * i] = f.x;
+        x[2 * i + 1] = f.y;
+      }
+    }
+  }
+}
+// V values to codes at `to`; scales that are no power of two come only with a cache whose scales the caller made
+template <int V>
+__device__ __forceinline__ void put_codes(uint8_t* to, const float* x, float scale, float inv, bool exact) {
+  float y[V < 4 ? 4 : V];
+#pragma unroll
+  for (int i = 0; i < (V < 4 ? 4 : V); ++i) y[i] = i < V ? (exact ? x[i] * inv : x[i] / scale) : 0.f;
+  if constexpr (V == 8) {
+    const float lo[4] = {y[0], y[1], y[2], y[3]}, hi[4] = {y[4], y[5], y[6], y[7]};
+    *reinterpret_cast<uint2*>(to) = make_uint2(f32_codes4(lo), f32_codes4(hi));
+  } else {
+    const float lo[4] = {y[0], y[1], y[2], y[3]};
+    if constexpr (V == 4)
+      *reinterpret_cast<uint32_t*>(to) = f32_codes4(lo);
+    else
+      *to = (uint8_t)f32_codes4(lo);
+  }
+}
+
+// V: values of a vector; a unit is two vectors (of pairs, or side by side where nothing is turned). NU: units a
+// thread holds of a block at most.
+template <bool BF16, int D, int V, bool ADJ, int NU>
+__global__ void __launch_bounds__(kThreads) enter_kernel(EnterParams e) {
+  using E = typename std::conditional<BF16, __nv_bfloat16, __half>::type;
+  extern __shared__ __align__(16) float2 turn[];  // [tokens][pairs]
+  __shared__ float sh_max[2][kThreads / 32];
+  pdl_wait();
+  if ((int64_t)blockIdx.x >= e.kv_ctas) {
+    const int64_t b = (int64_t)blockIdx.x - e.kv_ctas;
+    const int group = (int)(b / e.q_blocks);
+    rope_rows<E, V, ADJ>(e.q, (b - group * e.q_blocks) * kThreads + threadIdx.x, group);
+    return;
+  }
+  const AppendParams& p = e.a;
+  const int64_t w = (int64_t)blockIdx.x / e.parts;
+  const int part = (int)((int64_t)blockIdx.x - w * e.parts);
+  const bool is_k = part < e.k_parts;
+  const int refused = p.c.status[1] & kRefused;  // (no CTA of this launch sets it)
+  const int T = p.c.T, H = p.c.heads;
+  const int i = slot_sequence(p.row_off, p.n, p.c.log2T, w);
+  const int64_t r0 = p.row_off[i], r1 = p.row_off[i + 1];
+  const int64_t local = w - ((r0 >> p.c.log2T) + 2 * (int64_t)i);
+  const int seq = p.seqs[i];
+  int len = -1;
+  if ((unsigned)seq < (unsigned)p.c.max_seqs) len = p.c.length[seq];
+  if (refused) return;
+  if (local < 0 && r0 <= p.total_rows) return;  // rows before row_off[0] belong to no sequence
+  if (!(r0 >= 0 && r1 >= r0 && r1 <= p.total_rows && len >= r1 - r0 && len <= (int64_t)p.c.max_pages * T)) {
+    if (threadIdx.x == 0) set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
+    return;
+  }
+  const int start = len - (int)(r1 - r0);  // position of row r0
+  if (local > (len >> p.c.log2T)) return;  // (a slot past the rows)
+  const int slot = (start >> p.c.log2T) + (int)local;
+  if (slot >= p.c.max_pages) return;
+  const int t0 = max(start - slot * T, 0), t1 = min(len - slot * T, T);  // new tokens of this page
+  if (t1 <= t0) return;
+  const int64_t row0 = r0 + (int64_t)slot * T - start + t0;
+  if (!in_bounds(i >= 0 && i < p.n && row0 >= r0 && row0 + t1 - t0 <= r1, p.c.status, kSiteAppendRow)) return;
+  const int page = p.c.table[(int64_t)seq * p.c.max_pages + slot];
+  if ((unsigned)page >= (unsigned)p.c.pages || p.c.refs[page] != 1) {  // no page, or one that other sequences hold
+    if (threadIdx.x == 0) set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
+    return;
+  }
+  const int64_t block = ((int64_t)p.layer * p.c.pages + page) * H;
+  const int64_t ld = is_k ? p.k_row : p.v_row;
+  const uint16_t* src = static_cast<const uint16_t*>(is_k ? p.k : p.v) + row0 * ld;
+  const int h0 = is_k ? part * e.k_heads : (part - e.k_parts) * e.v_heads;
+  const int h1 = min(h0 + (is_k ? e.k_heads : e.v_heads), H);
+
+  constexpr int UPR = D / (2 * V);  // units of a row
+  const int half = e.q.half, turned = is_k ? half / V : 0, units = (t1 - t0) * UPR;
+  // this thread's units: token and places of the two vectors
+  auto places = [&](int n, int& tok, int& d0, int& d1, int& pair) {
+    const int x = n * kThreads + threadIdx.x, u = x % UPR;
+    tok = x / UPR;
+    pair = u < turned ? u * V : -1;
+    d0 = pair >= 0 && !ADJ ? V * u : 2 * V * u;
+    d1 = pair >= 0 && !ADJ ? d0 + half : d0 + V;
+  };
+  Raw<V> raw[NU][2];
+  auto load = [&](int h) {
+#pragma unroll
+    for (int n = 0; n < NU; ++n) {
+      if (n * kThreads + (int)threadIdx.x < units) {
+        int tok, d0, d1, pair;
+        places(n, tok, d0, d1, pair);
+        raw[n][0] = *reinterpret_cast<const Raw<V>*>(src + tok * ld + h * D + d0);
+        raw[n][1] = *reinterpret_cast<const Raw<V>*>(src + tok * ld + h * D + d1);
+      }
+    }
+  };
+  load(h0);
+  if (is_k) {
+    for (int x = threadIdx.x; x < (t1 - t0) * half; x += kThreads) {
+      const int tok = x / half, pair = x - tok * half;
+      int ax = e.q.axis[pair];
+      ax = (unsigned)ax < (unsigned)e.q.axes ? ax : 0;
+      rope_angle((float)e.q.pos[ax * e.q.pos_stride + row0 + tok], e.q.freq[pair], turn[x].x, turn[x].y);
+    }
+    __syncthreads();
+  }
+  for (int h = h0; h < h1; ++h) {
+    float x[NU][2 * V];
+    float amax = 0.f;
+#pragma unroll
+    for (int n = 0; n < NU; ++n) {
+      if (n * kThreads + (int)threadIdx.x < units) {
+        int tok, d0, d1, pair;
+        places(n, tok, d0, d1, pair);
+        float a[V], b[V];
+        unpack<BF16, V>(raw[n][0], a);
+        unpack<BF16, V>(raw[n][1], b);
+        if (pair >= 0) {
+#pragma unroll
+          for (int k = 0; k < V; ++k) {
+            const float2 cs = turn[tok * half + pair + k];
+            float& e0 = ADJ ? (2 * k < V ? a[(2 * k) % V] : b[(2 * k) % V]) : a[k];
+            float& e1 = ADJ ? (2 * k + 1 < V ? a[(2 * k + 1) % V] : b[(2 * k + 1) % V]) : b[k];
+            const float y = e0, z = e1;
+            e0 = fmaf(y, cs.x, -__fmul_rn(z, cs.y));  // (as in rope_rows)
+            e1 = fmaf(z, cs.x, __fmul_rn(y, cs.y));
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          amax = fmaxf(amax, fmaxf(finite_abs(a[k]), finite_abs(b[k])));
+          x[n][k] = a[k];
+          x[n][V + k] = b[k];
+        }
+      }
+    }
+    if (h + 1 < h1) load(h + 1);  // (under way during the maximum and the rounding)
+    amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
+    float* r = sh_max[h & 1];
+    if ((threadIdx.x & 31) == 0) r[threadIdx.x >> 5] = amax;
+    uint8_t* codes = (is_k ? p.c.k : p.c.v) + (block + h) * T * D;
+    float* scale = (is_k ? p.c.k_scale : p.c.v_scale) + block + h;
+    const float was = t0 > 0 ? *scale : 0.f;
+    __syncthreads();  // (and every thread has `was`)
+#pragma unroll
+    for (int k = 0; k < kThreads / 32; ++k) amax = fmaxf(amax, r[k]);
+    const float need = block_scale(amax);
+    const float now = was > need ? was : need;  // older tokens keep at least their scale
+    if (t0 > 0 && now > was) {
+      // the held codes, rounded again to the larger scale
+      const float ratio = was / now;
+      for (int y = threadIdx.x; y < t0 * D / 16; y += kThreads) {
+        uint4 c = reinterpret_cast<uint4*>(codes)[y];
+        uint32_t* cw = reinterpret_cast<uint32_t*>(&c);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float f[4];
+          codes4_f32(cw[j], f);
+#pragma unroll
+          for (int m = 0; m < 4; ++m) f[m] *= ratio;
+          cw[j] = f32_codes4(f);
+        }
+        reinterpret_cast<uint4*>(codes)[y] = c;
+      }
+    }
+    const bool exact = is_pow2(now);
+    const float inv = 1.f / now;
+#pragma unroll
+    for (int n = 0; n < NU; ++n) {
+      if (n * kThreads + (int)threadIdx.x < units) {
+        int tok, d0, d1, pair;
+        places(n, tok, d0, d1, pair);
+        uint8_t* to = codes + (t0 + tok) * D;
+        put_codes<V>(to + d0, x[n], now, inv, exact);
+        put_codes<V>(to + d1, x[n] + V, now, inv, exact);
+      }
+    }
+    if (threadIdx.x == 0) *scale = now;
+  }
+}
+
+template <bool BF16, int D, int V, bool ADJ, int NU>
+int launch_units(const EnterParams& e, cudaStream_t st) {
+  const int64_t tokens = std::min<int64_t>(e.a.c.T, e.a.total_rows);
+  const size_t smem = (size_t)tokens * e.q.half * sizeof(float2);
+  if (smem > 48 * 1024) {
+    static std::atomic<uint64_t> ready{0};  // devices whose shared memory limit is raised
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return OCCAM_ERR_CUDA;
+    if (!((ready.load(std::memory_order_acquire) >> dev) & 1)) {
+      if (cudaFuncSetAttribute(enter_kernel<BF16, D, V, ADJ, NU>, cudaFuncAttributeMaxDynamicSharedMemorySize, 128 * 64 * 8) != cudaSuccess)
+        return OCCAM_ERR_CUDA;
+      ready.fetch_or(uint64_t(1) << dev, std::memory_order_release);
+    }
+  }
+  const int64_t groups = e.q.t[0].heads > 0 ? e.q.groups0 : 0;
+  const int64_t grid = e.kv_ctas + groups * e.q_blocks;
+  if (grid > 0x7fffffff) return OCCAM_ERR_UNSUPPORTED;
+  return launch_after(enter_kernel<BF16, D, V, ADJ, NU>, dim3((unsigned)grid), kThreads, smem, st, e) && cudaGetLastError() == cudaSuccess
+             ? OCCAM_OK
+             : OCCAM_ERR_CUDA;
+}
+
+template <bool BF16, int D, int V, bool ADJ>
+int launch_pairing(const EnterParams& e, cudaStream_t st) {
+  // units of a block a thread: page_tokens * D / (2 V) / 256
+  constexpr int U64 = std::max(64 * D / (2 * V * kThreads), 1);
+  return e.a.c.T <= 64 ? launch_units<BF16, D, V, ADJ, U64>(e, st) : launch_units<BF16, D, V, ADJ, 2 * U64>(e, st);
+}
+
+template <bool BF16, int D>
+int launch_dim(const EnterParams& e, int v, bool adj, cudaStream_t st) {
+  if (v == 8) return adj ? launch_pairing<BF16, D, 8, true>(e, st) : launch_pairing<BF16, D, 8, false>(e, st);
+  if (v == 4) return adj ? launch_pairing<BF16, D, 4, true>(e, st) : launch_pairing<BF16, D, 4, false>(e, st);
+  return adj ? launch_pairing<BF16, D, 1, true>(e, st) : launch_pairing<BF16, D, 1, false>(e, st);
+}
+
+}  // namespace
+
+#define OCCAM_TRY(x)                 \
+  do {                               \
+    int _rc = (x);                   \
+    if (_rc != OCCAM_OK) return _rc; \
+  } while (0)
+
+extern "C" int occam_cache_append_rope(const occam_cache* cache, const occam_append_rope_args* a, void* workspace,
+                                       size_t workspace_bytes, occam_stream_t stream) {
+  const NvtxRange nvtx("occam_cache_append_rope");
+  launch_counter() = 0;
+  OCCAM_TRY(check_cache(cache));
+  if (!a) return OCCAM_ERR_INVALID_ARG;
+  if (a->dtype != OCCAM_BF16 && a->dtype != OCCAM_F16) return OCCAM_ERR_UNSUPPORTED;
+  const int dim = cache->dim;
+  if (a->layer < 0 || a->layer >= cache->layers || a->total_rows < 0 || a->total_rows > 0x7fffffff || a->n < 0 ||
+      a->n > cache->max_seqs || a->rot < 2 || a->rot > dim || (a->rot & 1) || a->axes < 1 || a->axes > 8 || a->pos_stride < 0 ||
+      (a->pairing != OCCAM_ROPE_HALF && a->pairing != OCCAM_ROPE_ADJACENT))
+    return OCCAM_ERR_INVALID_ARG;
+  CacheWs w;
+  OCCAM_TRY(check_cache_ws(cache, 0, workspace, workspace_bytes, &w));
+  if (a->total_rows == 0) return OCCAM_OK;
+  if (!a->positions || !a->inv_freq || !a->axis) return OCCAM_ERR_INVALID_ARG;
+  const int64_t row = (int64_t)cache->heads * dim;
+  if (a->n > 0 && (!a->k || !a->v || !a->seqs || !a->row_off || !aligned16(a->k) || !aligned16(a->v) || a->k_row < row ||
+                   a->v_row < row || (a->k_row & 7) || (a->v_row & 7)))
+    return OCCAM_ERR_INVALID_ARG;
+  EnterParams e{};
+  uintptr_t bits = 0;  // of the queries' addresses and strides
+  if (a->q) {
+    const occam_rope_tensor& t = *a->q;
+    if (!t.src || !t.dst || t.heads < 1 || t.heads > 65535 || t.src_row < 0 || t.src_head < 0 || t.dst_row < 0 || t.dst_head < 0)
+      return OCCAM_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(t.src) | reinterpret_cast<uintptr_t>(t.dst)) & 1) return OCCAM_ERR_INVALID_ARG;
+    if ((a->total_rows > 1 && t.dst_row < dim) || (t.heads > 1 && t.dst_head < dim)) return OCCAM_ERR_INVALID_ARG;
+    if (t.src == t.dst && (t.src_row != t.dst_row || t.src_head != t.dst_head)) return OCCAM_ERR_INVALID_ARG;
+    // no value is written that another thread may still read, or writes too
+    const Extent to = extent(t.dst, a->total_rows, t.dst_row, t.heads, t.dst_head, dim, 2);
+    if (meets_itself(to) || (t.src != t.dst && meet(to, extent(t.src, a->total_rows, t.src_row, t.heads, t.src_head, dim, 2))))
+      return OCCAM_ERR_INVALID_ARG;
+    if (a->n > 0 && (meet(to, extent(a->k, a->total_rows, a->k_row, cache->heads, dim, dim, 2)) ||
+                     meet(to, extent(a->v, a->total_rows, a->v_row, cache->heads, dim, dim, 2))))
+      return OCCAM_ERR_INVALID_ARG;
+    bits = reinterpret_cast<uintptr_t>(t.src) | reinterpret_cast<uintptr_t>(t.dst) |
+           (uintptr_t)((t.src_row | t.src_head | t.dst_row | t.dst_head) * 2);
+    e.q.t[0] = t;
+  }
+  if (a->n == 0 && !a->q) return OCCAM_OK;
+  e.a.c = cache_dev(cache, workspace, w);
+  e.a.layer = a->layer;
+  e.a.n = a->n;
+  e.a.total_rows = a->total_rows;
+  e.a.k_row = a->k_row;
+  e.a.v_row = a->v_row;
+  e.a.k = a->k;
+  e.a.v = a->v;
+  e.a.seqs = a->seqs;
+  e.a.row_off = a->row_off;
+  e.q.rows = a->total_rows;
+  e.q.dim = dim;
+  e.q.half = a->rot / 2;
+  e.q.axes = a->axes;
+  e.q.pos = a->positions;
+  e.q.pos_stride = a->pos_stride;
+  e.q.freq = a->inv_freq;
+  e.q.axis = a->axis;
+  // the widest vector that divides the turned and the copied part and that every address is a multiple of
+  int v = 8;
+  while (v > 1 && (e.q.half % v || (dim - a->rot) % (2 * v) || (bits & (2 * v - 1)))) v = v == 8 ? 4 : 1;
+  // Heads a CTA: as many as leave four CTAs an SM (K: up to 8 share a page's cosines and sines).
+  const int64_t sms = cache_sms();
+  e.slots = a->n > 0 ? (a->total_rows >> e.a.c.log2T) + 2 * (int64_t)a->n : 0;
+  auto share = [&](int64_t ctas, int heads, int most) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>({ctas * heads / (sms * 4), (int64_t)heads, (int64_t)most}));
+  };
+  e.k_heads = share(e.slots, cache->heads, 8);
+  e.v_heads = share(e.slots, cache->heads, 4);
+  e.k_parts = (cache->heads + e.k_heads - 1) / e.k_heads;
+  e.parts = e.k_parts + (cache->heads + e.v_heads - 1) / e.v_heads;
+  e.kv_ctas = e.slots * e.parts;
+  const int64_t units = dim / (2 * v);
+  e.q_blocks = (a->total_rows * units + kThreads - 1) / kThreads;
+  // queries: enough threads to fill the GPU first, then as many heads a thread as amortise the sines
+  e.q.hpt = share(e.q_blocks * 2, std::max(e.q.t[0].heads, 1), kMostHeads);
+  e.q.groups0 = (e.q.t[0].heads + e.q.hpt - 1) / e.q.hpt;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  const bool adj = a->pairing == OCCAM_ROPE_ADJACENT, bf16 = a->dtype == OCCAM_BF16;
+  if (dim == 128) return bf16 ? launch_dim<true, 128>(e, v, adj, st) : launch_dim<false, 128>(e, v, adj, st);
+  return bf16 ? launch_dim<true, 64>(e, v, adj, st) : launch_dim<false, 64>(e, v, adj, st);
+}
