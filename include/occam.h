@@ -587,6 +587,22 @@ typedef struct occam_attend_args {
 int occam_cache_attend(const occam_cache* cache, const occam_attend_args* args, void* workspace,
                        size_t workspace_bytes, occam_stream_t stream);
 
+/* occam_cache_attend for sequences that share leading pages, as occam_cache_fork leaves them:
+ * the pages that a group's sequences have in common are read once for all
+ * rows of the group. Group g is the sequences seqs[group_off[g] .. group_off[g+1]-1]
+ * (group_off int32 [n_groups+1], device, from 0 up to n; n_groups at most max_seqs, at least 1 if n is). What they
+ * share is found in the page table: leading full pages that are the same in all of them and that every
+ * row sees whole; a group may share nothing. Results are those of occam_cache_attend
+ * up to the order of sums in fp32. keep flags are not taken (OCCAM_ERR_UNSUPPORTED): prune forks
+ * with occam_cache_compact. max_group_rows: the largest number of rows of one group (it chooses
+ * the kernels; results are right for any value). workspace: of
+ * occam_cache_shared_workspace_size() for at least total_rows and heads; it serves the other cache
+ * calls too. Offsets of groups that do not go from 0 up to n record OCCAM_ERR_INVALID_ARG, and nothing is shared. */
+int occam_cache_shared_workspace_size(const occam_cache* cache, int64_t total_rows, int32_t heads, size_t* bytes);
+int occam_cache_attend_shared(const occam_cache* cache, const occam_attend_args* args, const int32_t* group_off,
+                              int32_t n_groups, int32_t max_group_rows, void* workspace, size_t workspace_bytes,
+                              occam_stream_t stream);
+
 /* Sequence dst[i], which must be empty, becomes a copy of src[i] (a src may
  * be listed more than once, but not as a dst): full pages are shared, a last
  * page that is not full is copied in every layer. */

@@ -46,6 +46,7 @@ from ._cache import (  # noqa: F401
     occam_cache_append,
     occam_cache_append_rope,
     occam_cache_attend,
+    occam_cache_attend_shared,
     occam_cache_compact,
     occam_cache_extend,
     occam_cache_fork,

@@ -229,14 +229,20 @@ class PagedCache:
         self.ws = self.alloc_workspace()
         self._ws = (self.ws.data_ptr(), self.ws.numel())
 
-    def alloc_workspace(self) -> torch.Tensor:
-        """A workspace of the cache calls, zero-filled and 256-byte aligned."""
+    def alloc_workspace(self, rows: int = 0, heads: int = 0) -> torch.Tensor:
+        """A workspace of the cache calls, zero-filled and 256-byte aligned. rows, heads: the most
+        query rows and heads of an occam_cache_attend_shared call with it (0: it serves none)."""
         n = ctypes.c_size_t(0)
         _check(library().occam_cache_workspace_size(self._ref, self.max_tokens, ctypes.byref(n)),
                "occam_cache_workspace_size")
-        ws = torch.zeros(n.value + 256, dtype=torch.uint8, device=self.device)
+        size = n.value
+        if rows:
+            _check(library().occam_cache_shared_workspace_size(self._ref, int(rows), int(heads), ctypes.byref(n)),
+                   "occam_cache_shared_workspace_size")
+            size = max(size, n.value)
+        ws = torch.zeros(size + 256, dtype=torch.uint8, device=self.device)
         off = (-ws.data_ptr()) % 256
-        return ws[off:off + n.value]
+        return ws[off:off + size]
 
     def status(self, stream=None, ws=None) -> int:
         """Reads and clears the status word (synchronises the stream)."""
@@ -315,13 +321,8 @@ def occam_cache_append_rope(cache: PagedCache, layer: int, q, k, v, seqs, row_of
     return out_q
 
 
-def occam_cache_attend(cache: PagedCache, layer: int, q, seqs, row_off, max_rows: int, scale: float = 0.0,
-                       causal: bool = True, keep=None, keep_off=None, out=None, lse=None, ws=None, stream=None):
-    """Attention of the rows of q [rows, heads, dim] (the last tokens of their
-    sequences; rows may be strided) over the cache. max_rows: the most rows of one
-    sequence. scale 0: 1 / sqrt(dim). keep / keep_off: uint8 flags that hide
-    tokens. Returns (out, lse [rows, heads] natural logarithm)."""
-    wp, wn = _workspace(cache, ws)
+def _attend_args(cache, layer, q, seqs, row_off, max_rows, scale, causal, keep, keep_off, out, lse, stream):
+    """(packed arguments, out, lse, stream handle) of an attention call."""
     _rows_tensor(q, "q", _ROWS, cache.at, None, cache.dim)
     rows, heads, dim = q.shape
     n = _vector(seqs, torch.int32, None, "seqs", cache.at).shape[0]
@@ -349,7 +350,36 @@ def occam_cache_attend(cache: PagedCache, layer: int, q, seqs, row_off, max_rows
                               total_keep)
     except struct.error as e:
         _bad(f"layer, max_rows or scale: {e}")
+    return a, out, lse, on
+
+
+def occam_cache_attend(cache: PagedCache, layer: int, q, seqs, row_off, max_rows: int, scale: float = 0.0,
+                       causal: bool = True, keep=None, keep_off=None, out=None, lse=None, ws=None, stream=None):
+    """Attention of the rows of q [rows, heads, dim] (the last tokens of their
+    sequences; rows may be strided) over the cache. max_rows: the most rows of one
+    sequence. scale 0: 1 / sqrt(dim). keep / keep_off: uint8 flags that hide
+    tokens. Returns (out, lse [rows, heads] natural logarithm)."""
+    wp, wn = _workspace(cache, ws)
+    a, out, lse, on = _attend_args(cache, layer, q, seqs, row_off, max_rows, scale, causal, keep, keep_off, out, lse, stream)
     _call(cache.at, library().occam_cache_attend, cache._ref, a, wp, wn, on)
+    return out, lse
+
+
+def occam_cache_attend_shared(cache: PagedCache, layer: int, q, seqs, row_off, max_rows: int, group_off, max_group_rows: int, ws,
+                              scale: float = 0.0, causal: bool = True, out=None, lse=None, stream=None):
+    """occam_cache_attend for sequences that share leading pages (forks): group g is seqs[group_off[g]]
+    .. seqs[group_off[g + 1] - 1] (int32, from 0 up to the number of sequences), and the full pages that its
+    sequences have in common are read once for all their rows. max_group_rows: the most rows of one group.
+    ws: alloc_workspace(rows, heads). Returns (out, lse) as occam_cache_attend."""
+    wp, wn = _workspace(cache, ws)
+    a, out, lse, on = _attend_args(cache, layer, q, seqs, row_off, max_rows, scale, causal, None, None, out, lse, stream)
+    groups = _vector(group_off, torch.int32, None, "group_off", cache.at).shape[0] - 1
+    if groups < 0:
+        _bad("group_off must have an entry more than there are groups")
+    try:
+        _call(cache.at, library().occam_cache_attend_shared, cache._ref, a, group_off.data_ptr(), groups, max_group_rows, wp, wn, on)
+    except ctypes.ArgumentError as e:
+        _bad(f"max_group_rows: {e}")
     return out, lse
 
 

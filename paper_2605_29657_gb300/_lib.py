@@ -176,9 +176,11 @@ def library() -> ctypes.CDLL:
         lib.occam_cache_compact.argtypes = [P(CCache), _i32, _i32, _i32, _p, _p, _p, _i64] + _ws
         lib.occam_cache_release.argtypes = [P(CCache), _i32, _p] + _ws
         lib.occam_cache_append_rope.argtypes = [P(CCache), P(CAppendRopeArgs)] + _ws
+        lib.occam_cache_shared_workspace_size.argtypes = [P(CCache), _i64, _i32, P(ctypes.c_size_t)]
+        lib.occam_cache_attend_shared.argtypes = [P(CCache), ctypes.c_char_p, _p, _i32, _i32] + _ws
         lib.occam_prompt_workspace_size.argtypes = [_i64, _i32, P(ctypes.c_size_t)]
         lib.occam_prompt_attend.argtypes = [ctypes.c_char_p, _p, _p] + _ws
-        for name in ("occam_cache_append_rope", "occam_prompt_workspace_size", "occam_prompt_attend", "occam_rope", "occam_cache_workspace_size", "occam_cache_extend", "occam_cache_append",
+        for name in ("occam_cache_shared_workspace_size", "occam_cache_attend_shared", "occam_cache_append_rope", "occam_prompt_workspace_size", "occam_prompt_attend", "occam_rope", "occam_cache_workspace_size", "occam_cache_extend", "occam_cache_append",
                      "occam_cache_attend", "occam_cache_fork", "occam_cache_compact", "occam_cache_release",
                      "occam_last_call_kernels", "occam_selftest_wait", "occam_pool_scores", "occam_mean_reference", "occam_budget_keep", "occam_construct_registers", "occam_calibrate_lambda2", "occam_workspace_size", "occam_get_status", "occam_score_stage1",
                      "occam_threshold",

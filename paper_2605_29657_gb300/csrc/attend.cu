@@ -137,11 +137,40 @@ __device__ __forceinline__ void note_nans(uint32_t& w, int key, int d, int* firs
   }
 }
 
+// Dims d .. d+3 of a row's result: v / sum, with sum in units of 2^mx
+template <int D, class P>
+__device__ __forceinline__ void put_row(const P& p, const SeqInfo& s, int64_t to, int d, const float (&v)[4], float mx, float sum) {
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  float x[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) x[q] = sum == 0.f ? 0.f : v[q] * inv;
+  if constexpr (P::mode == kPrefix) {
+    *reinterpret_cast<float4*>(p.pre_o + to * D + d) = make_float4(x[0], x[1], x[2], x[3]);
+    if (d == 0) p.pre_l[to] = sum == 0.f ? -INFINITY : mx + log2f(sum);
+    return;
+  }
+  float l2 = sum == 0.f ? -INFINITY : mx + log2f(sum);
+  if (P::mode == kTail && s.page0 > 0) {
+    float a, b;
+    l2 = join_prefix(p, to, l2, a, b);
+    const float4 y = __ldcg(reinterpret_cast<const float4*>(p.pre_o + to * D + d));
+    x[0] = fmaf(y.x, a, x[0] * b);
+    x[1] = fmaf(y.y, a, x[1] * b);
+    x[2] = fmaf(y.z, a, x[2] * b);
+    x[3] = fmaf(y.w, a, x[3] * b);
+  }
+  uint16_t o[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) o[q] = out_bits(x[q], p.bf16);
+  *reinterpret_cast<uint2*>(p.out + to * D + d) = make_uint2(o[0] | ((uint32_t)o[1] << 16), o[2] | ((uint32_t)o[3] << 16));
+  if (d == 0 && p.lse) p.lse[to] = l2 * 0.69314718056f;
+}
+
 // NQ: tiles of 8 query rows. TMA: whole tiles come by tensor copies; else row by
 // row, leaving out hidden rows.
-template <int D, int NQ, bool TMA>
+template <int D, int NQ, bool TMA, int MODE>
 __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
-    attend_rows_kernel(AttendParams p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+    attend_rows_kernel(AttendCall<MODE> p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
   constexpr int R = 8 * NQ;
   constexpr int KC = D / 64;      // 16-byte pieces of a key row a lane holds
   constexpr int VW = D / 32;      // 4-byte words of a value row a lane holds
@@ -183,7 +212,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
     const SeqInfo s = x0.s;
     const int i = x0.i, h = x0.h, rt = x0.rt, tiles = x0.tiles, ta = x0.ta, tb = x0.tb;
     const int rows = s.rows * p.G - rt * R;  // rows of this tile that exist, from 0
-    const int32_t* table = p.c.table + (int64_t)s.seq * p.c.max_pages;
+    const int32_t* table = p.c.table + (int64_t)s.seq * p.c.max_pages + first_page(p, s);
     const uint8_t* flags = nullptr;
     int n_flags = 0;
     if (p.keep) {
@@ -204,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const int first = key + 16 * k;
-        const bool there = first < s.len && in_bounds((first >> p.c.log2T) < p.c.max_pages, p.c.status, kSiteAttendKey);
+        const bool there = first < s.len && in_bounds(first_page(p, s) + (first >> p.c.log2T) < p.c.max_pages, p.c.status, kSiteAttendKey);
         x.page[k] = there ? table[first >> p.c.log2T] : 0;
       }
       bool see = key + lane < s.len;
@@ -563,13 +592,7 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
         if (nan_first[d + q] < (p.causal ? s.len - s.rows + j + 1 : s.len)) v[q] = __int_as_float(0x7fc00000);
       if (!in_bounds(s.row0 + j < p.total_rows && h * p.G + row - j * p.G < p.H, p.c.status, kSiteAttendRow)) continue;
       if (whole) {
-        const int64_t to = (s.row0 + j) * p.H + h * p.G + row - j * p.G;
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        uint16_t o[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) o[q] = out_bits(sum == 0.f ? 0.f : v[q] * inv, p.bf16);
-        *reinterpret_cast<uint2*>(p.out + to * D + d) = make_uint2(o[0] | ((uint32_t)o[1] << 16), o[2] | ((uint32_t)o[3] << 16));
-        if (d == 0 && p.lse) p.lse[to] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.69314718056f;
+        put_row<D>(p, s, (s.row0 + j) * p.H + h * p.G + row - j * p.G, d, v, mx, sum);
       } else {
         *reinterpret_cast<float4*>(po + r * D + d) = make_float4(v[0], v[1], v[2], v[3]);
         if (d == 0) pml[r] = make_float2(mx, sum);
@@ -633,17 +656,12 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
             if (c0 + n <= last) {
               *keep = acc;
             } else {
-              const float sum = sh_l[0][r], mx = sh_m[0][r], inv = sum == 0.f ? 0.f : 1.f / sum;
+              const float sum = sh_l[0][r], mx = sh_m[0][r];
               const int row = rt * R + r, j = div_group(p, row);
               const int64_t to = (s.row0 + j) * p.H + h * p.G + row - j * p.G;
               if (!in_bounds(to < p.total_rows * p.H, p.c.status, kSiteAttendRow)) continue;
               const float v[4] = {acc.x, acc.y, acc.z, acc.w};
-              uint16_t o[4];
-#pragma unroll
-              for (int q = 0; q < 4; ++q) o[q] = out_bits(sum == 0.f ? 0.f : v[q] * inv, p.bf16);
-              *reinterpret_cast<uint2*>(p.out + to * D + d) =
-                  make_uint2(o[0] | ((uint32_t)o[1] << 16), o[2] | ((uint32_t)o[3] << 16));
-              if (d == 0 && p.lse) p.lse[to] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.69314718056f;
+              put_row<D>(p, s, to, d, v, mx, sum);
             }
           }
           __syncthreads();
@@ -658,31 +676,32 @@ __global__ void __launch_bounds__(kThreads, NQ == 1 ? 3 : 2)
   } while (walk_next<R, kTile, kOver>(p, w, x0));
 }
 
-template <int D, int NQ, bool TMA>
-int launch(const AttendParams& p, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t st) {
+template <int D, int NQ, bool TMA, int MODE>
+int launch(const AttendCall<MODE>& p, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t st) {
   constexpr int smem = kWarps * 4 * kTile * D + 1024;
   static std::atomic<uint64_t> ready{0};  // devices whose shared memory limit is raised
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return OCCAM_ERR_CUDA;
   if (!((ready.load(std::memory_order_acquire) >> dev) & 1)) {
-    if (cudaFuncSetAttribute(attend_rows_kernel<D, NQ, TMA>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+    if (cudaFuncSetAttribute(attend_rows_kernel<D, NQ, TMA, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
       return OCCAM_ERR_CUDA;
     ready.fetch_or(uint64_t(1) << dev, std::memory_order_release);
   }
   const int grid = std::min(cache_sms() * (NQ == 1 ? 3 : 2), kAttendCtas);
-  return launch_after(attend_rows_kernel<D, NQ, TMA>, dim3((unsigned)grid), kThreads, smem, st, p, mk, mv) &&
+  return launch_after(attend_rows_kernel<D, NQ, TMA, MODE>, dim3((unsigned)grid), kThreads, smem, st, p, mk, mv) &&
                  cudaGetLastError() == cudaSuccess
              ? OCCAM_OK
              : OCCAM_ERR_CUDA;
 }
 
-template <int D, int NQ>
-int launch_rows(const AttendParams& p, cudaStream_t st) {
+template <int D, int NQ, int MODE>
+int launch_rows(const AttendCall<MODE>& p, cudaStream_t st) {
   CUtensorMap mk{}, mv{};
   // Tensor copies where every row of a tile is wanted; with keep flags, rows
   // one by one (a hidden row is not read). 64 single tokens over 2,300, of which 10 % are seen: 83 us,
   // by tensor copies 94; half 93 and 92; 90 % 94.5 and 92; without flags 65.
-  if (p.keep) return launch<D, NQ, false>(p, mk, mv, st);
+  if constexpr (MODE == kWhole)
+    if (p.keep) return launch<D, NQ, false>(p, mk, mv, st);
   const int box = std::min(p.c.T, kTile);
   if (!encode_blocks(&mk, p.c, p.c.k, D, box, true) || !encode_blocks(&mv, p.c, p.c.v, D, box, true)) return OCCAM_ERR_CUDA;
   return launch<D, NQ, true>(p, mk, mv, st);
@@ -717,11 +736,8 @@ bool occam::encode_blocks(CUtensorMap* m, const CacheDev& c, const void* codes, 
     if (_rc != OCCAM_OK) return _rc; \
   } while (0)
 
-extern "C" int occam_cache_attend(const occam_cache* cache, const occam_attend_args* a, void* workspace,
-                                  size_t workspace_bytes, occam_stream_t stream) {
-  const NvtxRange nvtx("occam_cache_attend");
-  launch_counter() = 0;
-  OCCAM_TRY(check_cache(cache));
+int occam::attend_params(const occam_cache* cache, const occam_attend_args* a, void* workspace, int ws_rc, const CacheWs& w,
+                         AttendParams* out) {
   if (!a) return OCCAM_ERR_INVALID_ARG;
   if (a->dtype != OCCAM_BF16 && a->dtype != OCCAM_F16) return OCCAM_ERR_UNSUPPORTED;
   if (a->layer < 0 || a->layer >= cache->layers || a->total_rows < 0 || a->total_rows > 0x7fffffff || a->n < 0 ||
@@ -731,13 +747,12 @@ extern "C" int occam_cache_attend(const occam_cache* cache, const occam_attend_a
   const int G = a->heads / cache->heads;
   if (G > 64 || a->total_rows * G > 0x7fffffff) return OCCAM_ERR_UNSUPPORTED;
   if (a->keep && (!a->keep_off || a->total_keep < 0)) return OCCAM_ERR_INVALID_ARG;
-  CacheWs w;
-  OCCAM_TRY(check_cache_ws(cache, 0, workspace, workspace_bytes, &w));
+  OCCAM_TRY(ws_rc);
   if (a->n == 0 || a->total_rows == 0) return OCCAM_OK;
   if (!a->q || !a->out || !a->seqs || !a->row_off || !aligned16(a->q) || !aligned16(a->out) || (a->q_row & 7) ||
       a->q_row < (int64_t)a->heads * cache->dim)
     return OCCAM_ERR_INVALID_ARG;
-  AttendParams p{};
+  AttendParams& p = *out;
   p.c = cache_dev(cache, workspace, w);
   p.layer = a->layer;
   p.n = a->n;
@@ -750,8 +765,6 @@ extern "C" int occam_cache_attend(const occam_cache* cache, const occam_attend_a
   p.g_mul = (uint32_t)(((uint64_t(1) << p.g_shift) + G - 1) / G);
   p.causal = a->causal ? 1 : 0;
   p.bf16 = a->dtype == OCCAM_BF16;
-  p.row_lo = 0;
-  p.row_hi = 0x7fffffff;
   p.total_rows = a->total_rows;
   p.q_row = a->q_row;
   p.total_keep = a->total_keep;
@@ -767,14 +780,20 @@ extern "C" int occam_cache_attend(const occam_cache* cache, const occam_attend_a
   p.counters = ws_at<int32_t>(workspace, w.counters);
   p.part_o = ws_at<float>(workspace, w.part_o);
   p.part_ml = ws_at<float2>(workspace, w.part_ml);
-  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  return OCCAM_OK;
+}
+
+template <int MODE>
+int occam::launch_attend(const AttendParams& base, int dim, int64_t most, bool one, cudaStream_t st) {
+  AttendCall<MODE> p{base};
+  p.row_lo = 0;
+  p.row_hi = 0x7fffffff;
   // Sequences with more than kFewRows query rows a key head go to the
   // tensor-core kernel, the others are this file's; one launch where the rows allow only one of them.
-  const int64_t most = (int64_t)a->max_rows * G;
   if (most > kFewRows) {
-    p.row_lo = a->n == 1 ? 0 : kFewRows;
-    OCCAM_TRY(launch_attend_tc(p, cache->dim, st));
-    if (a->n == 1) return OCCAM_OK;  // whatever its rows are
+    p.row_lo = one ? 0 : kFewRows;
+    OCCAM_TRY(launch_attend_tc(p, dim, st));
+    if (one) return OCCAM_OK;  // whatever its rows are
     p.row_lo = 0;
     p.row_hi = kFewRows;
   }
@@ -782,6 +801,22 @@ extern "C" int occam_cache_attend(const occam_cache* cache, const occam_attend_a
   // only known on the device: 63 single tokens beside a prefix of 2,000 take two column tiles, 174 us in all
   // where one would give 154; but 64 x 16 rows take 98 us with two and 116 with one.)
   const bool few = most <= 8;
-  if (cache->dim == 128) return few ? launch_rows<128, 1>(p, st) : launch_rows<128, 2>(p, st);
+  if (dim == 128) return few ? launch_rows<128, 1>(p, st) : launch_rows<128, 2>(p, st);
   return few ? launch_rows<64, 1>(p, st) : launch_rows<64, 2>(p, st);
+}
+template int occam::launch_attend<kWhole>(const AttendParams&, int, int64_t, bool, cudaStream_t);
+template int occam::launch_attend<kPrefix>(const AttendParams&, int, int64_t, bool, cudaStream_t);
+template int occam::launch_attend<kTail>(const AttendParams&, int, int64_t, bool, cudaStream_t);
+
+extern "C" int occam_cache_attend(const occam_cache* cache, const occam_attend_args* a, void* workspace,
+                                  size_t workspace_bytes, occam_stream_t stream) {
+  const NvtxRange nvtx("occam_cache_attend");
+  launch_counter() = 0;
+  OCCAM_TRY(check_cache(cache));
+  CacheWs w;
+  const int rc = check_cache_ws(cache, 0, workspace, workspace_bytes, &w);
+  AttendParams p{};
+  OCCAM_TRY(attend_params(cache, a, workspace, rc, w, &p));
+  if (a->n == 0 || a->total_rows == 0) return OCCAM_OK;
+  return launch_attend<kWhole>(p, cache->dim, (int64_t)a->max_rows * p.G, a->n == 1, reinterpret_cast<cudaStream_t>(stream));
 }

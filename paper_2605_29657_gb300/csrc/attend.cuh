@@ -32,32 +32,78 @@ struct AttendParams {
   const int64_t* keep_off;
   float scale_log2;
   uint32_t g_mul, g_shift;  // x / G = x g_mul >> g_shift for 0 <= x < 2^31
+  // attention over shared prefixes (see attend_shared.cu)
+  const int32_t* group_off;  // prefixes: the sequences of each group
+  const int32_t* shared;     // prefixes: tokens that a group's sequences have in common
+  const int32_t* skip;       // tails: leading tokens of a sequence that its group's prefix stands for
+  float* pre_o;              // results over the prefixes, normalised [total_rows, heads, dim]
+  float* pre_l;              // and log2 sum_k 2^s_k
   int32_t* counters;  // per stretch: arrivals at an item that begins in it; at kAttendCtas: CTAs that have left
   float* part_o;
   float2* part_ml;
 };
 
+// What a launch attends over: the whole of each sequence; the prefix of a group of sequences, all their rows as
+// one; or what is behind those prefixes, whose results are joined in.
+enum { kWhole = 0, kPrefix = 1, kTail = 2 };
+template <int MODE>
+struct AttendCall : AttendParams {
+  static constexpr int mode = MODE;
+};
+
 struct SeqInfo {
   int64_t row0;
   int rows, len, seq;
+  int page0;  // (kTail) the first page's column
 };
+// The column of the first page
+template <class P>
+__device__ __forceinline__ int first_page(const P&, const SeqInfo& s) {
+  return P::mode == kTail ? s.page0 : 0;
+}
 
 // Sequence i's rows and length; rows = 0 if it is not this launch's or if its offsets do
 // not fit (recorded).
-__device__ __forceinline__ SeqInfo attend_seq(const AttendParams& p, int i) {
+template <class P>
+__device__ __forceinline__ SeqInfo attend_seq(const P& p, int i) {
   SeqInfo s;
+  s.rows = 0;
+  s.len = 0;
+  s.page0 = 0;
+  if constexpr (P::mode == kPrefix) {
+    s.row0 = 0;
+    s.seq = 0;
+    const int len = p.shared[i];  // (0: nothing in common, or a group that does not fit)
+    if (len <= 0) return s;
+    const int a = p.group_off[i], b = p.group_off[i + 1];
+    s.row0 = p.row_off[a];
+    const int64_t r1 = p.row_off[b];
+    s.seq = p.seqs[a];
+    s.len = len;
+    const int64_t m = (r1 - s.row0) * p.G;
+    if (m > p.row_lo && m <= p.row_hi) s.rows = (int)(r1 - s.row0);
+    return s;
+  }
   s.row0 = p.row_off[i];
   const int64_t r1 = p.row_off[i + 1];
   s.seq = p.seqs[i];
-  s.rows = 0;
-  s.len = 0;
   if ((unsigned)s.seq < (unsigned)p.c.max_seqs) {
     const int len = p.c.length[s.seq];
     if (s.row0 >= 0 && r1 >= s.row0 && r1 <= p.total_rows && len <= p.c.max_pages * p.c.T && r1 - s.row0 <= len) {
       s.len = len;
       const int64_t m = (r1 - s.row0) * p.G;
       if (m > p.row_lo && m <= p.row_hi) s.rows = (int)(r1 - s.row0);
-      return s;
+      if constexpr (P::mode == kTail) {
+        const int skip = p.skip[i];
+        if (skip >= 0 && skip <= len - (r1 - s.row0) && (skip & (p.c.T - 1)) == 0) {
+          s.page0 = skip >> p.c.log2T;
+          s.len = len - skip;
+          return s;
+        }
+        s.rows = 0;
+      } else {
+        return s;
+      }
     }
   }
   set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
@@ -69,8 +115,8 @@ __device__ __forceinline__ int div_group(const AttendParams& p, int x) {
 }
 
 // Key tiles of KT keys that row tile rt (R rows) of a sequence can see, at least one.
-template <int R, int KT>
-__device__ __forceinline__ int key_tiles(const AttendParams& p, const SeqInfo& s, int rt) {
+template <int R, int KT, class P>
+__device__ __forceinline__ int key_tiles(const P& p, const SeqInfo& s, int rt) {
   int keys = s.len;
   if (p.causal) keys = s.len - s.rows + div_group(p, min((rt + 1) * R - 1, s.rows * p.G - 1)) + 1;
   return (keys + KT - 1) / KT;
@@ -95,13 +141,13 @@ static __device__ __noinline__ int64_t floor_sum(int64_t n, int64_t m, int64_t a
 }
 // Units of the first nrt row tiles of a sequence's head. Row tile rt < the last sees
 // base + 1 + floor(((rt + 1) R - 1) / G) keys.
-template <int R, int KT, int OVER>
-__device__ __forceinline__ int64_t units_before(const AttendParams& p, const SeqInfo& s, int nrt) {
+template <int R, int KT, int OVER, class P>
+__device__ __forceinline__ int64_t units_before(const P& p, const SeqInfo& s, int nrt) {
   if (!p.causal) return (int64_t)nrt * ((s.len + KT - 1) / KT + OVER);
   return (int64_t)nrt * OVER + floor_sum(nrt, (int64_t)p.G * KT, R, R - 1 + (int64_t)p.G * (s.len - s.rows + KT));
 }
-template <int R, int KT, int OVER>
-__device__ __forceinline__ int64_t head_units(const AttendParams& p, const SeqInfo& s) {
+template <int R, int KT, int OVER, class P>
+__device__ __forceinline__ int64_t head_units(const P& p, const SeqInfo& s) {
   if (s.rows == 0) return 0;
   const int nrt = (s.rows * p.G + R - 1) / R;
   return (nrt > 1 ? units_before<R, KT, OVER>(p, s, nrt - 1) : 0) + OVER + key_tiles<R, KT>(p, s, nrt - 1);
@@ -134,8 +180,8 @@ struct LinePart {
 };
 // Block-wide (NT threads, all of them); sh: NT / 32 + 4 int64 of shared memory.
 // min_units: a stretch is no shorter.
-template <int R, int KT, int OVER, int NT>
-__device__ __forceinline__ LinePart attend_line(const AttendParams& p, int min_units, int64_t* sh, Line& l) {
+template <int R, int KT, int OVER, int NT, class P>
+__device__ __forceinline__ LinePart attend_line(const P& p, int min_units, int64_t* sh, Line& l) {
   constexpr int NWARP = NT / 32;
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   const int per = (p.n + NT - 1) / NT;
@@ -171,8 +217,8 @@ __device__ __forceinline__ LinePart attend_line(const AttendParams& p, int min_u
   return w;
 }
 // Stretch c, to all threads of the block.
-template <int R, int KT, int OVER, int NT>
-__device__ __forceinline__ void attend_find(const AttendParams& p, const Line& l, const LinePart& part, int c, int64_t* sh,
+template <int R, int KT, int OVER, int NT, class P>
+__device__ __forceinline__ void attend_find(const P& p, const Line& l, const LinePart& part, int c, int64_t* sh,
                                             Stretch& w) {
   constexpr int NWARP = NT / 32;
   w.index = c;
@@ -214,16 +260,16 @@ struct Walk {
   int i, h, rt, tiles, ta, tb;
 };
 // False if no tile of the item lies in the stretch.
-template <int R, int KT, int OVER, class W>
-__device__ __forceinline__ bool walk_set(const AttendParams& p, const W& w, Walk& x, int in_item) {
+template <int R, int KT, int OVER, class P, class W>
+__device__ __forceinline__ bool walk_set(const P& p, const W& w, Walk& x, int in_item) {
   x.tiles = key_tiles<R, KT>(p, x.s, x.rt);
   x.ta = max(in_item - OVER, 0);
   x.tb = max(min((int)w.u1 - x.item - OVER, x.tiles), 0);
   return x.ta < x.tb;
 }
 // The next segment; false at the end of the stretch.
-template <int R, int KT, int OVER, class W>
-__device__ __forceinline__ bool walk_next(const AttendParams& p, const W& w, Walk& x) {
+template <int R, int KT, int OVER, class P, class W>
+__device__ __forceinline__ bool walk_next(const P& p, const W& w, Walk& x) {
   x.item += OVER + x.tiles;
   if (x.item + OVER >= w.u1) return false;
   const int nrt = (x.s.rows * p.G + R - 1) / R;
@@ -239,8 +285,8 @@ __device__ __forceinline__ bool walk_next(const AttendParams& p, const W& w, Wal
   return walk_set<R, KT, OVER>(p, w, x, 0);
 }
 // The first segment; false if the stretch has none.
-template <int R, int KT, int OVER, class W>
-__device__ __forceinline__ bool walk_begin(const AttendParams& p, const W& w, Walk& x) {
+template <int R, int KT, int OVER, class P, class W>
+__device__ __forceinline__ bool walk_begin(const P& p, const W& w, Walk& x) {
   x.i = w.seq;
   x.s = attend_seq(p, x.i);
   x.h = w.head;
@@ -253,5 +299,24 @@ template <int OVER>
 __device__ __forceinline__ int2 item_stretches(const Line& l, const Walk& x) {
   return make_int2(stretch_of(l, x.item + OVER), stretch_of(l, x.item + OVER + x.tiles - 1));
 }
+
+// How a row's result over its tail, log2 sum l2, joins the one over the prefix (kTail, where there is one): a and b are
+// the weights of the prefix's and the tail's normalised results, the return value is log2 of the whole sum.
+__device__ __forceinline__ float join_prefix(const AttendParams& p, int64_t row, float l2, float& a, float& b) {
+  const float pl = __ldcg(p.pre_l + row), m = fmaxf(pl, l2), base = m == -INFINITY ? 0.f : m;
+  a = fast_exp2(pl - base);
+  b = fast_exp2(l2 - base);
+  const float sum = a + b, inv = sum == 0.f ? 0.f : 1.f / sum;
+  a *= inv;
+  b *= inv;
+  return sum == 0.f ? -INFINITY : m + log2f(sum);
+}
+
+// Host side: checks a call's arguments and fills in the parameters. ws_rc: what the check of the workspace gave.
+int attend_params(const occam_cache* cache, const occam_attend_args* a, void* workspace, int ws_rc, const CacheWs& w,
+                  AttendParams* out);
+// most: query rows a key head of one item's rows at most (it chooses the kernels); one: there is one such item.
+template <int MODE>
+int launch_attend(const AttendParams& p, int dim, int64_t most, bool one, cudaStream_t st);
 
 }  // namespace occam

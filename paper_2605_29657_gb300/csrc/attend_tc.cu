@@ -125,11 +125,13 @@ struct Plan {
   const float* ks0;  // scales of page 0 in this layer and head
   const float* vs0;
   int n_flags;
+  int column;  // of the item's first page
 
   __device__ Plan(const AttendParams& p_, const Walk& x_, int lane_) : p(p_), x(x_), lane(lane_) {}
 
-  __device__ __forceinline__ void item() {
-    table = p.c.table + (int64_t)x.s.seq * p.c.max_pages;
+  __device__ __forceinline__ void item(int first_column) {
+    column = first_column;
+    table = p.c.table + (int64_t)x.s.seq * p.c.max_pages + column;
     const int64_t b = (int64_t)p.layer * p.c.pages * p.c.heads + x.h;
     ks0 = p.c.k_scale + b;
     vs0 = p.c.v_scale + b;
@@ -150,7 +152,7 @@ struct Plan {
     t.tile = tile;
     const int first = tile * kK + (lane & 7) * kGroup;
     t.page = 0;
-    if (first < x.s.len && in_bounds((first >> p.c.log2T) < p.c.max_pages, p.c.status, kSiteAttendKey))
+    if (first < x.s.len && in_bounds(column + (first >> p.c.log2T) < p.c.max_pages, p.c.status, kSiteAttendKey))
       t.page = table[first >> p.c.log2T];
     if (tile * kK < n_flags) {
 #pragma unroll
@@ -309,8 +311,8 @@ __device__ __forceinline__ bool wait_long(uint64_t* bar, uint32_t parity, volati
     ++met;                               \
   } while (0)
 
-template <int D>
-__device__ __forceinline__ void plan_role(const AttendParams& p, Shared& sh, const CUtensorMap& map_k, const CUtensorMap& map_v,
+template <int D, class P>
+__device__ __forceinline__ void plan_role(const P& p, Shared& sh, const CUtensorMap& map_k, const CUtensorMap& map_v,
                                           unsigned char* raw) {
   const int lane = threadIdx.x & 31;
   Walk x;
@@ -318,7 +320,7 @@ __device__ __forceinline__ void plan_role(const AttendParams& p, Shared& sh, con
   Plan f(p, x, lane);
   uint32_t n = 0, j = 0;  // step records, steps so far
   for (bool again = true; again;) {
-    f.item();
+    f.item(first_page(p, x.s));
     const int common = p.causal ? x.s.len - x.s.rows + div_group(p, x.rt * kR) + 1 : x.s.len;
     const int end = x.tb - 1, tiles2 = row_tiles(p, x);
     float rho = 0.f, rho_max = 0.f;
@@ -631,8 +633,8 @@ __device__ __forceinline__ uint32_t out_pair(float a, float b) {
   return pack_f16(a, b);
 }
 
-template <int D, bool BF16>
-__device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, unsigned char* q_smem,
+template <int D, bool BF16, class P>
+__device__ __forceinline__ void softmax_role(const P& p, Shared& sh, unsigned char* q_smem,
                                              uint32_t tmem, int t) {
   const int r = threadIdx.x & 127, lane = threadIdx.x & 31;
   const uint32_t lanes = (uint32_t)(r & ~31) << 16;
@@ -763,9 +765,20 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
     if (mine) {
       TC_WAIT(sh.o_done[t][1], ((it >> 1) - 1) & 1);
       tc::fence_after();
-      const float scale = l == 0.f ? 0.f : done ? rho / l : rho;
+      float scale = l == 0.f ? 0.f : done ? rho / l : rho;
+      float l2 = l == 0.f ? -INFINITY : ref + log2f(l), pre = 0.f;  // the prefix's weight
       uint16_t* out = p.out + to * D;
       float* part = p.part_o + mypart * D;
+      const bool half_out = P::mode == kPrefix ? false : done;  // 16-bit results
+      if constexpr (P::mode == kPrefix)
+        if (done) part = p.pre_o + to * D;
+      const bool joins = P::mode == kTail && done && x.s.page0 > 0 && there;
+      if constexpr (P::mode == kTail)
+        if (joins) {
+          float b;
+          l2 = join_prefix(p, to, l2, pre, b);
+          scale *= b;
+        }
       // By way of the warp's own queries' place (they are done with), so that whole rows are
       // written at once: row r's 16-byte piece c lies where a query's would.
       constexpr int CH = D / 8, RPI = 32 / CH;  // pieces of a row there, rows of a write
@@ -773,10 +786,10 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
       auto place = [&](int rr, int c) { return stage + (c >> 3) * 16384 + rr * 128 + (((c & 7) ^ (rr & 7)) << 4); };
       const int live = min(x.s.rows * p.G - (x.rt * kR + (row & ~31)), 32);  // rows of the warp
       const bool fits = !there || in_bounds(x.s.row0 + tok < p.total_rows && x.h * p.G + at - tok * p.G < p.H, p.c.status, kSiteAttendRow);
-      const uint64_t mine_at = !fits ? 0 : done ? reinterpret_cast<uint64_t>(out) : reinterpret_cast<uint64_t>(part);
+      const uint64_t mine_at = !fits ? 0 : half_out ? reinterpret_cast<uint64_t>(out) : reinterpret_cast<uint64_t>(part);
 #pragma unroll 1
-      for (int pass = 0; pass < (done ? 1 : 2); ++pass) {
-        const int cols = done ? D : D / 2;
+      for (int pass = 0; pass < (half_out ? 1 : 2); ++pass) {
+        const int cols = half_out ? D : D / 2;
 #pragma unroll 1
         for (int c = 0; c < cols; c += 16) {
           uint32_t o[16];
@@ -784,7 +797,18 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
           float v[16];
 #pragma unroll
           for (int k = 0; k < 16; ++k) v[k] = l == 0.f ? 0.f : __uint_as_float(o[k]) * scale;
-          if (done) {
+          if constexpr (P::mode == kTail)
+            if (joins) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const float4 y = __ldcg(reinterpret_cast<const float4*>(p.pre_o + to * D + c) + k);
+                v[4 * k] = fmaf(y.x, pre, v[4 * k]);
+                v[4 * k + 1] = fmaf(y.y, pre, v[4 * k + 1]);
+                v[4 * k + 2] = fmaf(y.z, pre, v[4 * k + 2]);
+                v[4 * k + 3] = fmaf(y.w, pre, v[4 * k + 3]);
+              }
+            }
+          if (half_out) {
 #pragma unroll
             for (int k = 0; k < 2; ++k)
               *reinterpret_cast<uint4*>(place(r, c / 8 + k)) =
@@ -810,7 +834,7 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
 #pragma unroll 1
         for (int d = 0; d < D; ++d)
           if (sh.nan_first[seg & 3][d] < limit) {
-            if (done)
+            if (half_out)
               out[d] = BF16 ? 0x7fc0 : 0x7e00;
             else
               part[d] = __int_as_float(0x7fc00000);
@@ -819,7 +843,10 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
       tc::fence_before();
       if (there && fits) {
         if (done) {
-          if (p.lse) p.lse[to] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.69314718056f;
+          if (P::mode == kPrefix)
+            p.pre_l[to] = l2;
+          else if (p.lse)
+            p.lse[to] = l2 * 0.69314718056f;
         } else {
           p.part_ml[mypart] = make_float2(l == 0.f ? -INFINITY : ref, l);
         }
@@ -853,10 +880,20 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
               const float2 ml = __ldcg(&p.part_ml[part(c, lane)]);
               sum += ml.y * fast_exp2(ml.x - base);
             }
-            if (p.lse && in_bounds(to < p.total_rows * p.H, p.c.status, kSiteAttendRow))
-              p.lse[to] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * 0.69314718056f;
           }
-          const float inv = sum == 0.f ? 0.f : 1.f / sum;
+          float inv = sum == 0.f ? 0.f : 1.f / sum, l2 = sum == 0.f ? -INFINITY : mx + log2f(sum), pre = 0.f;
+          if (there && in_bounds(to < p.total_rows * p.H, p.c.status, kSiteAttendRow)) {
+            if constexpr (P::mode == kPrefix) {
+              p.pre_l[to] = l2;
+            } else {
+              if (P::mode == kTail && x.s.page0 > 0) {
+                float b;
+                l2 = join_prefix(p, to, l2, pre, b);
+                inv *= b;
+              }
+              if (p.lse) p.lse[to] = l2 * 0.69314718056f;
+            }
+          }
 #pragma unroll 1
           for (int c0 = first; c0 <= last; c0 += 32) {
             const int n = min(last - c0 + 1, 32);
@@ -897,17 +934,28 @@ __device__ __forceinline__ void softmax_role(const AttendParams& p, Shared& sh, 
               }
 #pragma unroll
               for (int i = 0; i < ROWS; ++i) {
-                const float total = __shfl_sync(0xffffffffu, sum, (r0 + i) & 31);
+                const float total = __shfl_sync(0xffffffffu, P::mode == kTail ? l2 : sum, (r0 + i) & 31);
                 const uint64_t row_to = __shfl_sync(0xffffffffu, (uint64_t)to, (r0 + i) & 31);
+                const float row_pre = P::mode == kTail ? __shfl_sync(0xffffffffu, pre, (r0 + i) & 31) : 0.f;
                 if (r0 + i < rows && in_bounds((int64_t)row_to < p.total_rows * p.H, p.c.status, kSiteAttendRow)) {
                   if (c0 + n <= last) {
                     float* keep = p.part_o + part(first, r0 + i) * D + lane * V;
 #pragma unroll
                     for (int q = 0; q < V; ++q) keep[q] = acc[i][q];
+                  } else if constexpr (P::mode == kPrefix) {
+                    float* pre_o = p.pre_o + row_to * D + lane * V;
+#pragma unroll
+                    for (int q = 0; q < V; ++q) pre_o[q] = total == 0.f ? 0.f : acc[i][q];
                   } else {
+                    const bool none = P::mode == kTail ? total == -INFINITY : total == 0.f;
+                    if (P::mode == kTail && row_pre != 0.f) {
+                      const float* pre_o = p.pre_o + row_to * D + lane * V;
+#pragma unroll
+                      for (int q = 0; q < V; ++q) acc[i][q] = fmaf(__ldcg(pre_o + q), row_pre, acc[i][q]);
+                    }
                     uint32_t* out = reinterpret_cast<uint32_t*>(p.out + row_to * D + lane * V);
 #pragma unroll
-                    for (int q = 0; q < V; q += 2) out[q / 2] = total == 0.f ? 0u : out_pair<BF16>(acc[i][q], acc[i][q + 1]);
+                    for (int q = 0; q < V; q += 2) out[q / 2] = none ? 0u : out_pair<BF16>(acc[i][q], acc[i][q + 1]);
                   }
                 }
               }
@@ -942,9 +990,9 @@ __device__ __forceinline__ void clear_counters(const AttendParams& p) {
   if (threadIdx.x == 0) p.counters[kAttendCtas] = 0;
 }
 
-template <int D, bool BF16>
+template <int D, bool BF16, int MODE>
 __global__ void __launch_bounds__(kThreads, 1)
-    attend_tc_kernel(AttendParams p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+    attend_tc_kernel(AttendCall<MODE> p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
   constexpr int kBytes = kK * D * 2;
   // queries 2 tiles, keys and values 2 stages each, codes as they come: 7 x 32 KB (D = 128)
   extern __shared__ __align__(1024) unsigned char smem[];
@@ -1042,38 +1090,42 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // Once per device: the shared memory, and that the register split adds up --
 // setmaxnreg.inc waits for registers that only the launch's own can give.
-template <int D, bool BF16>
+template <int D, bool BF16, int MODE>
 int prepare(int smem) {
   static std::atomic<uint64_t> ready{0};
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return OCCAM_ERR_CUDA;
   if ((ready.load(std::memory_order_acquire) >> dev) & 1) return OCCAM_OK;
   cudaFuncAttributes at;
-  if (cudaFuncGetAttributes(&at, attend_tc_kernel<D, BF16>) != cudaSuccess) return OCCAM_ERR_CUDA;
+  if (cudaFuncGetAttributes(&at, attend_tc_kernel<D, BF16, MODE>) != cudaSuccess) return OCCAM_ERR_CUDA;
   if (at.numRegs * kThreads < 256 * kRegSoftmax + 128 * (kRegConvert + kRegIssue)) return OCCAM_ERR_UNSUPPORTED;
-  if (cudaFuncSetAttribute(attend_tc_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+  if (cudaFuncSetAttribute(attend_tc_kernel<D, BF16, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
     return OCCAM_ERR_CUDA;
   ready.fetch_or(uint64_t(1) << dev, std::memory_order_release);
   return OCCAM_OK;
 }
 
-template <int D, bool BF16>
-int launch(const AttendParams& p, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t st) {
+template <int D, bool BF16, int MODE>
+int launch(const AttendCall<MODE>& p, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t st) {
   const int smem = 7 * kK * D * 2 + kSharedBytes;
-  const int rc = prepare<D, BF16>(smem);
+  const int rc = prepare<D, BF16, MODE>(smem);
   if (rc != OCCAM_OK) return rc;
   const dim3 grid((unsigned)std::min(cache_sms(), kAttendTcCtas));
-  return launch_after(attend_tc_kernel<D, BF16>, grid, kThreads, smem, st, p, mk, mv) && cudaGetLastError() == cudaSuccess
+  return launch_after(attend_tc_kernel<D, BF16, MODE>, grid, kThreads, smem, st, p, mk, mv) && cudaGetLastError() == cudaSuccess
              ? OCCAM_OK
              : OCCAM_ERR_CUDA;
 }
 
 }  // namespace
 
-int occam::launch_attend_tc(const AttendParams& p, int dim, cudaStream_t st) {
+template <int MODE>
+int occam::launch_attend_tc(const AttendCall<MODE>& p, int dim, cudaStream_t st) {
   CUtensorMap mk, mv;
   if (!encode_blocks(&mk, p.c, p.c.k, dim, p.c.T, false) || !encode_blocks(&mv, p.c, p.c.v, dim, p.c.T, false))
     return OCCAM_ERR_CUDA;
   if (dim == 128) return p.bf16 ? launch<128, true>(p, mk, mv, st) : launch<128, false>(p, mk, mv, st);
   return p.bf16 ? launch<64, true>(p, mk, mv, st) : launch<64, false>(p, mk, mv, st);
 }
+template int occam::launch_attend_tc<kWhole>(const AttendCall<kWhole>&, int, cudaStream_t);
+template int occam::launch_attend_tc<kPrefix>(const AttendCall<kPrefix>&, int, cudaStream_t);
+template int occam::launch_attend_tc<kTail>(const AttendCall<kTail>&, int, cudaStream_t);

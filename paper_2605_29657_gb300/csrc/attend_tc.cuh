@@ -8,8 +8,8 @@
 namespace occam {
 
 // Sequences with p.row_lo < rows * G <= p.row_hi; at most kAttendTcCtas CTAs.
-int launch_attend_tc(const AttendParams& p, int dim, cudaStream_t st);
-
+template <int MODE>
+int launch_attend_tc(const AttendCall<MODE>& p, int dim, cudaStream_t st);
 
 // Tensor map of the codes as [layers * pages][heads * page_tokens][dim] bytes, boxes of
 // `box_rows` rows of one page (swizzled by the row's bytes, 128 or 64, if asked).
