@@ -195,7 +195,7 @@ def _prepare_prompt(case, st, cpu, g):
     if own:
         import paper_2605_29657_gb300 as occ
 
-        st["ws"] = occ.alloc_prompt_workspace(total, hq)
+        st["ws"] = occ.alloc_prompt_workspace(total, hq, ktotal, hkv)
 
 
 def _handle(st, **more):
