@@ -663,9 +663,9 @@ typedef struct occam_prompt_args {
   float scale; /* 0: 1 / sqrt(dim) */
 } occam_prompt_args;
 
-/* Scratch of the two calls below for total_rows query rows (workspace convention
+/* Scratch of the two calls below, for calls of up to these sizes (workspace convention
  * as above: 256-byte aligned, zero-filled before first use, status word at its start). */
-int occam_prompt_workspace_size(int64_t total_rows, int32_t heads, size_t* bytes);
+int occam_prompt_workspace_size(int64_t total_rows, int64_t total_keys, int32_t heads, int32_t kv_heads, size_t* bytes);
 
 /* out [total_rows, heads, dim] (q's type, dense, 16-byte aligned) = sum_k p_k v_k / sum_k p_k,
  *   p_k = exp(scale q.k - max) over the keys that the row sees;
@@ -677,6 +677,33 @@ int occam_prompt_workspace_size(int64_t total_rows, int32_t heads, size_t* bytes
  * are undefined; the workspace stays usable. */
 int occam_prompt_attend(const occam_prompt_args* args, void* out, float* lse, void* workspace, size_t workspace_bytes,
                         occam_stream_t stream);
+
+/* The gradient: from out and lse of occam_prompt_attend on the same arguments and
+ * the gradient dout of a loss with respect to out,
+ *   dv_k = sum_q p dout_q, dq = scale sum_k ds k, dk = scale sum_q ds q,
+ *   p = exp(scale q.k - lse), ds = p (dout.v - dout.out),
+ * sums over the rows that see the key, of all heads of its group, or the keys that the row sees. p and ds
+ * are rounded to the inputs' type for their products (f16: ds by a power of two a sequence and key
+ * head that uses its range); sums are in fp32, in an order that does not depend on timing. Rows that
+ * see nothing have gradient 0, and so have keys that nobody sees; rows and keys of no sequence are
+ * left as they are. A value that is not finite may make any gradient of its sequence not finite, but none
+ * of another's. dout, dq, dk and dv: 16-byte aligned, heads dense, rows a multiple of 8 elements apart, so
+ * that the three gradients may be views of one projection's. They overlap no input and not
+ * each other. */
+typedef struct occam_prompt_grads {
+  const void* out; /* dense */
+  const float* lse;
+  const void* dout;
+  void* dq;
+  void* dk;
+  void* dv;
+  int64_t dout_row;
+  int64_t dq_row;
+  int64_t dk_row;
+  int64_t dv_row;
+} occam_prompt_grads;
+int occam_prompt_attend_grad(const occam_prompt_args* args, const occam_prompt_grads* grads, void* workspace,
+                             size_t workspace_bytes, occam_stream_t stream);
 
 /* Diagnostic of the bounded device-side waits (no fault, trap or hang). One
  * warp waits, each time for about limit_ns (1 .. 1e9), on an mbarrier that

@@ -57,4 +57,5 @@ from ._cache import (  # noqa: F401
 from ._prompt import (  # noqa: F401
     alloc_prompt_workspace,
     occam_prompt_attend,
+    occam_prompt_attend_grad,
 )

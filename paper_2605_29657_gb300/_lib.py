@@ -122,6 +122,13 @@ class CPromptArgs(ctypes.Structure):
     ]
 
 
+class CPromptGrads(ctypes.Structure):
+    _fields_ = [
+        ("out", _p), ("lse", _p), ("dout", _p), ("dq", _p), ("dk", _p), ("dv", _p), ("dout_row", _i64), ("dq_row", _i64),
+        ("dk_row", _i64), ("dv_row", _i64),
+    ]
+
+
 _lib = None
 
 
@@ -178,9 +185,10 @@ def library() -> ctypes.CDLL:
         lib.occam_cache_append_rope.argtypes = [P(CCache), P(CAppendRopeArgs)] + _ws
         lib.occam_cache_shared_workspace_size.argtypes = [P(CCache), _i64, _i32, P(ctypes.c_size_t)]
         lib.occam_cache_attend_shared.argtypes = [P(CCache), ctypes.c_char_p, _p, _i32, _i32] + _ws
-        lib.occam_prompt_workspace_size.argtypes = [_i64, _i32, P(ctypes.c_size_t)]
+        lib.occam_prompt_workspace_size.argtypes = [_i64, _i64, _i32, _i32, P(ctypes.c_size_t)]
         lib.occam_prompt_attend.argtypes = [ctypes.c_char_p, _p, _p] + _ws
-        for name in ("occam_cache_shared_workspace_size", "occam_cache_attend_shared", "occam_cache_append_rope", "occam_prompt_workspace_size", "occam_prompt_attend", "occam_rope", "occam_cache_workspace_size", "occam_cache_extend", "occam_cache_append",
+        lib.occam_prompt_attend_grad.argtypes = [ctypes.c_char_p, P(CPromptGrads)] + _ws
+        for name in ("occam_cache_shared_workspace_size", "occam_cache_attend_shared", "occam_cache_append_rope", "occam_prompt_workspace_size", "occam_prompt_attend", "occam_prompt_attend_grad", "occam_rope", "occam_cache_workspace_size", "occam_cache_extend", "occam_cache_append",
                      "occam_cache_attend", "occam_cache_fork", "occam_cache_compact", "occam_cache_release",
                      "occam_last_call_kernels", "occam_selftest_wait", "occam_pool_scores", "occam_mean_reference", "occam_budget_keep", "occam_construct_registers", "occam_calibrate_lambda2", "occam_workspace_size", "occam_get_status", "occam_score_stage1",
                      "occam_threshold",

@@ -10,18 +10,21 @@ import struct
 import torch
 
 from ._cache import _DTYPE, _ROWS, _bad, _call, _dense, _empty, _on, _row_stride, _rows_tensor, _vector
-from ._lib import CPromptArgs, _check, library
+from ._lib import CPromptArgs, CPromptGrads, _check, library
 
 # occam_prompt_args as packed bytes (as in _cache)
 _PROMPT_ARGS = struct.Struct("@iiiiiiqqPPPqqqPPf0q")
 assert _PROMPT_ARGS.size == ctypes.sizeof(CPromptArgs)
 
 
-def alloc_prompt_workspace(rows: int, heads: int, device="cuda") -> torch.Tensor:
+def alloc_prompt_workspace(rows: int, heads: int, keys: int | None = None, kv_heads: int | None = None, device="cuda") -> torch.Tensor:
     """A workspace (zero-filled, 256-byte aligned) of occam_prompt_attend and its gradient for up to `rows`
-    query rows of `heads` heads. One workspace serves one call at a time."""
+    query rows of `heads` heads and `keys` (None: as many as rows) keys of `kv_heads` (None: heads). One workspace
+    serves one call at a time."""
     n = ctypes.c_size_t(0)
-    _check(library().occam_prompt_workspace_size(int(rows), int(heads), ctypes.byref(n)), "occam_prompt_workspace_size")
+    _check(library().occam_prompt_workspace_size(int(rows), int(rows if keys is None else keys), int(heads),
+                                                 int(heads if kv_heads is None else kv_heads), ctypes.byref(n)),
+           "occam_prompt_workspace_size")
     ws = torch.zeros(n.value + 256, dtype=torch.uint8, device=device)
     off = (-ws.data_ptr()) % 256
     return ws[off:off + n.value]
@@ -71,3 +74,36 @@ def occam_prompt_attend(q, k, v, row_off, ws, key_off=None, scale: float = 0.0, 
         _bad("lse must be [rows, heads]")
     _call(at, library().occam_prompt_attend, args, out.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel(), on)
     return out, lse
+
+
+def occam_prompt_attend_grad(q, k, v, out, lse, dout, row_off, ws, key_off=None, scale: float = 0.0, causal: bool = True, dq=None,
+                             dk=None, dv=None, stream=None):
+    """The gradient of occam_prompt_attend: from its arguments, its results out and lse, and dout [rows, heads, dim], a
+    loss's gradient with respect to out (rows may be strided). Returns (dq, dk, dv), new dense tensors unless
+    given (their rows may be strided: views of one projection's gradient). Rows and keys that belong to no
+    sequence are not written: give zeroed tensors where some are padded."""
+    at, args = _inputs(q, k, v, row_off, key_off, scale, causal)
+    _dense(ws, torch.uint8, "ws", at)
+    on = _on(stream, at)
+    if _dense(out, q.dtype, "out", at).shape != q.shape:
+        _bad("out must be like q")
+    if _dense(lse, torch.float32, "lse", at).shape != q.shape[:2]:
+        _bad("lse must be [rows, heads]")
+    _rows_like(dout, q, "dout", at)
+    grads = []
+    for name, given, like in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
+        if given is None:
+            given = _empty(like.shape, like.dtype, like.device, stream)
+        else:
+            _rows_like(given, like, name, at)
+        grads.append(given)
+    dq, dk, dv = grads
+    g = CPromptGrads(out.data_ptr(), lse.data_ptr(), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _row_stride(dout),
+                     _row_stride(dq), _row_stride(dk), _row_stride(dv))
+    _call(at, library().occam_prompt_attend_grad, args, ctypes.byref(g), ws.data_ptr(), ws.numel(), on)
+    return dq, dk, dv
+
+
+def _rows_like(t, like, name: str, at: int) -> None:
+    if _rows_tensor(t, name, (like.dtype,), at, like.shape[1], like.shape[2]).shape[0] != like.shape[0]:
+        _bad(f"{name} must have {like.shape[0]} rows")

@@ -21,7 +21,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "liboccam.so")
 LIB_CHECKED = os.path.join(HERE, "liboccam_checked.so")
-SOURCES = ["stage1.cu", "stage1_tc.cu", "stage2.cu", "stage2_tc.cu", "stage2_scores_tc.cu", "compact.cu", "rules.cu", "rope.cu", "cache.cu", "append_rope.cu", "attend.cu", "attend_tc.cu", "attend_shared.cu", "prompt.cu", "selftest.cu", "api.cu"]
+SOURCES = ["stage1.cu", "stage1_tc.cu", "stage2.cu", "stage2_tc.cu", "stage2_scores_tc.cu", "compact.cu", "rules.cu", "rope.cu", "cache.cu", "append_rope.cu", "attend.cu", "attend_tc.cu", "attend_shared.cu", "prompt.cu", "prompt_grad.cu", "selftest.cu", "api.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

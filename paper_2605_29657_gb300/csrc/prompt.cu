@@ -644,7 +644,7 @@ int occam::prompt_params(const occam_prompt_args* a, void* workspace, size_t wor
       !(a->scale < INFINITY))
     return OCCAM_ERR_INVALID_ARG;
   size_t need = 0;
-  const int rc = occam_prompt_workspace_size(a->total_rows, a->heads, &need);
+  const int rc = occam_prompt_workspace_size(a->total_rows, a->total_keys, a->heads, a->kv_heads, &need);
   if (rc != OCCAM_OK) return rc;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < need) return OCCAM_ERR_WORKSPACE;
   if (a->n == 0 || (a->total_rows == 0 && a->total_keys == 0)) return OCCAM_OK;
@@ -689,9 +689,11 @@ bool occam::prompt_meets_inputs(const occam_prompt_args* a, const Extent& x) {
     if (_rc != OCCAM_OK) return _rc; \
   } while (0)
 
-extern "C" int occam_prompt_workspace_size(int64_t total_rows, int32_t heads, size_t* bytes) {
-  if (!bytes || total_rows < 0 || total_rows > 0x7fffffff || heads < 1 || heads > 1024) return OCCAM_ERR_INVALID_ARG;
-  *bytes = prompt_ws(total_rows, heads).total;
+extern "C" int occam_prompt_workspace_size(int64_t total_rows, int64_t total_keys, int32_t heads, int32_t kv_heads, size_t* bytes) {
+  if (!bytes || total_rows < 0 || total_rows > 0x7fffffff || total_keys < 0 || total_keys > 0x7fffffff || heads < 1 ||
+      heads > 1024 || kv_heads < 1 || kv_heads > heads)
+    return OCCAM_ERR_INVALID_ARG;
+  *bytes = prompt_ws(total_rows, total_keys, heads, kv_heads).total;
   return OCCAM_OK;
 }
 

@@ -179,15 +179,17 @@ bool encode_rows(CUtensorMap* m, const void* at, bool bf16, int dim, int heads, 
                  int box_rows);
 
 // Byte offsets of the workspace: the status word (8 bytes) and the counters, zero between calls; then what the
-// gradient writes before it reads it.
+// gradient writes before it reads it (see GradParams).
 struct PromptWs {
-  size_t rows;  // float2 [total_rows, heads]
-  size_t total;
+  size_t stat, norm, power, vnorm, total;
 };
-inline PromptWs prompt_ws(int64_t total_rows, int heads) {
+inline PromptWs prompt_ws(int64_t total_rows, int64_t total_keys, int heads, int kv_heads) {
   PromptWs w;
-  w.rows = 256;
-  w.total = w.rows + cache_align((size_t)total_rows * heads * 8);
+  w.stat = 256;
+  w.norm = w.stat + cache_align((size_t)total_rows * heads * 8);
+  w.power = w.norm + cache_align((size_t)total_rows * heads * 4);
+  w.vnorm = w.power + cache_align((size_t)total_rows * kv_heads * 4);
+  w.total = w.vnorm + cache_align((size_t)total_keys * kv_heads * 4);
   return w;
 }
 

@@ -1,0 +1,1180 @@
+// prompt_grad.cu -- gradient of a whole prompt's attention: occam_prompt_attend_grad.
+//
+// With s = scale q.k, p = exp(s - lse), dP = dO V^T and delta = dO.O a row:
+//   dV = P^T dO,  dS = P (dP - delta),  dQ = scale dS K,  dK = scale dS^T Q.
+// Neither P nor dS goes to memory: two kernels on the fifth-generation tensor cores form them again, one that
+// owns keys (dK, dV; 8 D operations a (row, head, key)) and one that owns rows (dQ; 6 D). Every
+// sum has one CTA and one order, the heads of a group included, so results repeat bit for bit; a kernel that
+// owned keys alone would do with 10 D in all but add dQ across CTAs.
+// Before them a pass over dO and O forms delta; with f16, where dS has no range to spare, also the norms
+// that bound it: |dP - delta| <= |dO||V| + |delta|, and dS is held times a power of two a sequence and key head that
+// brings that bound under f16's end.
+#include <algorithm>
+#include <atomic>
+
+#include "nvtx.cuh"
+#include "prompt.cuh"
+
+using namespace occam;
+
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kItems = 3;           // items known ahead
+constexpr int kRegElement = 184, kRegWrite = 80, kRegIssue = 64;  // 2 x 184 + 80 + 64 = 4 x 128
+constexpr int kRowBytes = 128;      // of 64 dims in a block
+
+struct GradParams : PromptParams {
+  const uint16_t* o;
+  const uint16_t* dout;
+  int64_t dout_row, v_row;
+  const uint16_t* v;
+  uint16_t *dq, *dk, *dv;
+  int64_t dq_row, dk_row, dv_row;
+  float2* stat;   // [total_rows, heads] lse in log2 units, -delta
+  float* norm;    // (f16) [total_rows, heads] |dO|
+  float* vnorm;   // (f16) [total_keys, kv_heads] |V|
+  float* power;   // (f16) [total_rows, kv_heads], at a sequence's first row: what its dS is held times of
+};
+
+template <bool BF16>
+__device__ __forceinline__ float2 pair16(uint32_t w) {
+  return BF16 ? make_float2(bf16_lo(w), bf16_hi(w)) : __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+
+// ---------------------------------------------------------------- delta
+// Bound by HBM: dO and O read once.
+template <bool BF16>
+__global__ void __launch_bounds__(256) stat_kernel(GradParams p) {
+  pdl_wait();
+  const int sub = threadIdx.x & 15;
+  const int64_t at = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), rows = p.total_rows * p.H;
+  float dot = 0.f, sq = 0.f;
+  if (at < rows) {
+    const int64_t row = at / p.H;
+    if (sub * 8 < p.dim) {
+      const uint4 a = ldg_stream(p.o + at * p.dim + sub * 8);
+      const uint4 b = ldg_stream(p.dout + row * p.dout_row + (at - row * p.H) * p.dim + sub * 8);
+      const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 u = pair16<BF16>(x[k]), v = pair16<BF16>(y[k]);
+        dot = fmaf(u.x, v.x, fmaf(u.y, v.y, dot));
+        sq = fmaf(v.x, v.x, fmaf(v.y, v.y, sq));
+      }
+    }
+  } else if (!BF16 && at - rows < p.total_keys * p.Hkv) {
+    const int64_t key = (at - rows) / p.Hkv;
+    if (sub * 8 < p.dim) {
+      const uint4 b = ldg_stream(p.v + key * p.v_row + (at - rows - key * p.Hkv) * p.dim + sub * 8);
+      const uint32_t y[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 v = pair16<BF16>(y[k]);
+        sq = fmaf(v.x, v.x, fmaf(v.y, v.y, sq));
+      }
+    }
+  }
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) {
+    dot += __shfl_xor_sync(0xffffffffu, dot, o);
+    if (!BF16) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+  }
+  if (sub != 0) return;
+  if (at < rows) {
+    const float l = p.lse[at];
+    p.stat[at] = make_float2(l == -INFINITY ? INFINITY : l * 1.44269504089f, -dot);  // (a row that sees nothing: every p is 0)
+    if (!BF16) p.norm[at] = sqrtf(sq);
+  } else if (!BF16 && at - rows < p.total_keys * p.Hkv) {
+    p.vnorm[at - rows] = sqrtf(sq);
+  }
+}
+
+// (f16) One CTA a sequence and key head: the power of two that brings the bound of dS under 2^15.
+__global__ void __launch_bounds__(512) power_kernel(GradParams p) {
+  __shared__ float sh[3][16];
+  pdl_wait();
+  const PromptSeq s = prompt_seq(p, blockIdx.x);
+  const int h = blockIdx.y;
+  if (s.rows == 0) return;
+  float m[3] = {0.f, 0.f, 0.f};
+  for (int64_t e = threadIdx.x; e < (int64_t)s.rows * p.G; e += 512) {
+    const int64_t row = e / p.G, at = (s.row0 + row) * p.H + h * p.G + (e - row * p.G);
+    m[0] = fmaxf(m[0], finite_abs(p.norm[at]));
+    m[1] = fmaxf(m[1], finite_abs(p.stat[at].y));
+  }
+  for (int64_t e = threadIdx.x; e < s.keys; e += 512) m[2] = fmaxf(m[2], finite_abs(p.vnorm[(s.key0 + e) * p.Hkv + h]));
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    m[k] = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(m[k])));
+    if ((threadIdx.x & 31) == 0) sh[k][threadIdx.x >> 5] = m[k];
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int k = 0; k < 3; ++k)
+      for (int w = 0; w < 16; ++w) m[k] = fmaxf(m[k], sh[k][w]);
+    const float bound = fminf(fmaf(m[0], m[2], m[1]), 3e38f);
+    int e = 0;
+    if (bound > 0.f) e = 14 - ((__float_as_int(bound) >> 23) - 127);  // bound 2^e < 2^15
+    p.power[s.row0 * p.Hkv + h] = __int_as_float((min(max(e, -100), 100) + 127) << 23);
+  }
+}
+
+#define WAIT(bar, parity) PROMPT_WAIT(bar, parity)
+
+// f16: P is held 2^14 times as large (it is at most 1, up to the rounding of lse), so that what is 2^-28 of the
+// largest still has 11 bits.
+template <bool BF16>
+struct Lift {
+  static constexpr float kLog2 = BF16 ? 0.f : 14.f, kBack = BF16 ? 1.f : 1.f / 16384.f;
+};
+
+// The 16-bit results of 32 rows, of a lane each, over shared memory to rows of global memory: 16 values at a time are
+// put by put16, whole 64-dim blocks written by flush. to(row) gives a row's address, null if it is not there.
+struct RowWriter {
+  unsigned char* stage;  // 32 x 128 bytes of this warp
+  int lane;
+  __device__ __forceinline__ void put16(int c, const uint32_t (&w)[8]) const {
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      *reinterpret_cast<uint4*>(stage + lane * 128 + (((c / 8 + e) ^ (lane & 7)) << 4)) =
+          make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
+  }
+  template <class To>
+  __device__ __forceinline__ void flush(int block, int pieces, const To& to) const {
+    __syncwarp();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int rr = e * 4 + lane / 8, c = lane % 8;
+      const uint4 v = *reinterpret_cast<const uint4*>(stage + rr * 128 + ((c ^ (rr & 7)) << 4));
+      uint16_t* at = to(rr);
+      if (at && block * 8 + c < pieces) *reinterpret_cast<uint4*>(at + block * 64 + c * 8) = v;
+    }
+    __syncwarp();
+  }
+};
+template <bool BF16>
+__device__ __forceinline__ void scale_pack(const uint32_t (&o)[16], float f, uint32_t (&w)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) w[e] = pack16<BF16>(__uint_as_float(o[2 * e]) * f, __uint_as_float(o[2 * e + 1]) * f);
+}
+
+// ================================================================ dK and dV
+// An item is a tile of 128 keys of one key head; its steps are blocks of 64 query rows (64 / P tokens x P heads),
+// first rows that see it on, for every head of the group. Scores are taken transposed, S^T = K Q^T and dP^T = V dO^T, a
+// key a lane, so that P^T and dS^T are the first operands of dV += P^T dO and dK += dS^T Q from tensor memory.
+// Even and odd steps have tensor memory, an issuing warp and a warpgroup of their own: while one's scores are
+// turned into P and dS, the other's products run. The sums are added to in the order of the steps (a step's product
+// waits for the one before it; the scores issued in between keep the tensor cores busy).
+namespace keys {
+
+constexpr int kQ = 64;  // query rows of a step
+
+template <int DP>
+struct Shape {
+  static constexpr int kBlocks = DP > 64 ? 2 : 1;
+  static constexpr int kTile = kBlocks * 128 * kRowBytes;  // bytes of 128 rows
+  static constexpr int kHalf = kTile / 2;                  // and of 64
+  static constexpr int kStages = DP > 64 ? 4 : 6;
+};
+
+template <int STAGES>
+struct Shared {
+  uint64_t kv_full, kv_free, full[STAGES], ready[STAGES], free[STAGES], s_full[2], dp_full[2], p_full[2], ds_full[2], added[2], o_full,
+      o_free, item_full[kItems], item_free[kItems], drain;
+  PromptItem item[kItems];  // tile: of keys; hb: key head; nk[0]: the first block of rows; nk[1]: 0, or 1 at the end
+  uint32_t tmem;
+  int stop;
+  alignas(16) float2 stat[STAGES][kQ];
+  PromptList list;
+};
+
+struct Count {
+  const GradParams& p;
+  __device__ __forceinline__ int operator()(const PromptSeq& s) const { return (s.keys / 128 + (s.keys % 128 != 0)) * p.Hkv; }
+};
+
+// the step's place: head block and token block
+struct Place {
+  int head, tok;  // first head, first token
+};
+__device__ __forceinline__ Place place_of(const GradParams& p, const PromptItem& it, int log_p, int k) {
+  const int log_t = 6 - log_p, blocks = ((it.rows + (1 << log_t) - 1) >> log_t) - it.nk[0];
+  const int hb = k / blocks;
+  return Place{it.hb * p.G + (hb << log_p), (it.nk[0] + k - hb * blocks) << log_t};
+}
+
+template <int DP, class Sh>
+__device__ __forceinline__ void load_role(const GradParams& p, Sh& sh, int log_p, const CUtensorMap& map_q, const CUtensorMap& map_do,
+                                          const CUtensorMap& map_k, const CUtensorMap& map_v, unsigned char* k_smem,
+                                          unsigned char* v_smem, unsigned char* q_smem) {
+  using S = Shape<DP>;
+  const int lane = threadIdx.x & 31, total = sh.list.first[kChunks];
+  const Count count{p};
+  int next = blockIdx.x;
+  uint32_t told = 0;
+  auto tell = [&]() -> bool {
+    PromptItem& it = sh.item[told % kItems];
+    if (!tc::bar_try(&sh.item_free[told % kItems], ((told / kItems) & 1) ^ 1) &&
+        !prompt_wait_long(&sh.item_free[told % kItems], ((told / kItems) & 1) ^ 1, &sh.stop, p.status))
+      return false;
+    if (next < total) {
+      int place = 0;
+      const PromptSeq s = prompt_find(p, sh.list, count, next, &place);
+      const int tile = place / p.Hkv, log_t = 6 - log_p;
+      const int first = (p.causal ? max(tile * 128 - (s.keys - s.rows), 0) : 0) >> log_t;
+      const int blocks = ((s.rows + (1 << log_t) - 1) >> log_t) - first;
+      if (lane == 0) {
+        it.row0 = s.row0;
+        it.key0 = s.key0;
+        it.rows = s.rows;
+        it.keys = s.keys;
+        it.tile = tile;
+        it.hb = place - tile * p.Hkv;
+        it.steps = max(blocks, 0) * (p.G >> log_p);
+        it.nk[0] = first;
+        it.nk[1] = 0;
+        next = gridDim.x + atomicAdd(&p.counters[0], 1);
+      }
+      next = __shfl_sync(0xffffffffu, next, 0);
+    } else if (lane == 0) {
+      it.steps = 0;
+      it.nk[1] = 1;
+    }
+    __syncwarp();
+    if (lane == 0) tc::bar_arrive(&sh.item_full[told % kItems]);
+    __syncwarp();
+    ++told;
+    return true;
+  };
+  if (!tell()) return;
+  uint32_t j = 0, n = 0;
+  for (uint32_t i = 0;; ++i) {
+    const PromptItem it = sh.item[i % kItems];
+    if (it.nk[1]) break;
+    if (!tell()) return;
+    if (it.steps > 0) {
+      const int key = (int)(it.key0 + (int64_t)it.tile * 128);
+      WAIT(sh.kv_free, (n & 1) ^ 1);
+      ++n;
+      if (lane == 0) {
+        tc::bar_expect_tx(&sh.kv_full, 2 * S::kTile);
+        for (int b = 0; b < S::kBlocks; ++b) {
+          tc::tma_load_3d(k_smem + b * 128 * kRowBytes, &map_k, b * 64, it.hb, key, &sh.kv_full);
+          tc::tma_load_3d(v_smem + b * 128 * kRowBytes, &map_v, b * 64, it.hb, key, &sh.kv_full);
+        }
+      }
+    }
+    for (int k = 0; k < it.steps; ++k, ++j) {
+      const int st = j % S::kStages;
+      const Place at = place_of(p, it, log_p, k);
+      WAIT(sh.free[st], ((j / S::kStages) & 1) ^ 1);
+      if (lane == 0) {
+        tc::bar_expect_tx(&sh.full[st], S::kTile);  // 64 rows of Q and of dO
+        unsigned char* to = q_smem + st * S::kTile;
+        for (int b = 0; b < S::kBlocks; ++b) {
+          tc::tma_load_3d(to + b * kQ * kRowBytes, &map_q, b * 64, at.head, (int)(it.row0 + at.tok), &sh.full[st]);
+          tc::tma_load_3d(to + S::kHalf + b * kQ * kRowBytes, &map_do, b * 64, at.head, (int)(it.row0 + at.tok), &sh.full[st]);
+        }
+      }
+      __syncwarp();
+    }
+    if (lane == 0) tc::bar_arrive(&sh.item_free[i % kItems]);
+    __syncwarp();
+  }
+}
+
+// The rows' statistics, and zeros in rows past the sequence's end
+template <int DP, class Sh>
+__device__ __forceinline__ void look_role(const GradParams& p, Sh& sh, int log_p, unsigned char* q_smem) {
+  using S = Shape<DP>;
+  const int lane = threadIdx.x & 31;
+  uint32_t j = 0;
+  for (uint32_t i = 0;; ++i) {
+    WAIT(sh.item_full[i % kItems], (i / kItems) & 1);
+    const PromptItem it = sh.item[i % kItems];
+    if (it.nk[1]) return;
+#pragma unroll 1
+    for (int k = 0; k < it.steps; ++k, ++j) {
+      const int st = j % S::kStages;
+      const Place at = place_of(p, it, log_p, k);
+      float2 x[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = lane + 32 * e, tok = at.tok + (r >> log_p);
+        x[e] = make_float2(INFINITY, 0.f);
+        const int64_t from = (it.row0 + tok) * p.H + at.head + (r & ((1 << log_p) - 1));
+        if (tok < it.rows && in_bounds(from < p.total_rows * p.H, p.status, kSitePromptRow)) x[e] = p.stat[from];
+      }
+      WAIT(sh.full[st], (j / S::kStages) & 1);
+      sh.stat[st][lane] = x[0];
+      sh.stat[st][lane + 32] = x[1];
+      const int live = (it.rows - at.tok) << log_p;  // rows that exist
+      if (live < kQ) {
+#pragma unroll 1
+        for (int b = 0; b < 2 * S::kBlocks; ++b) {
+          uint4* piece = reinterpret_cast<uint4*>(q_smem + st * S::kTile + b * kQ * kRowBytes);
+          for (int e = live * 8 + lane; e < kQ * 8; e += 32) piece[e] = make_uint4(0, 0, 0, 0);
+        }
+        tc::fence_proxy_async();
+      }
+      __syncwarp();
+      if (lane == 0) tc::bar_arrive(&sh.ready[st]);
+    }
+    if (lane == 0) tc::bar_arrive(&sh.item_free[i % kItems]);
+  }
+}
+
+// The steps of parity b. After step j's P: dV += P^T dO, then S^T of step j + 2 in its place; after its dS: dK += dS^T Q and
+// dP^T of step j + 2.
+template <int DP, bool BF16, class Sh>
+__device__ __forceinline__ void issue_role(const GradParams& p, Sh& sh, uint32_t k_smem, uint32_t v_smem, uint32_t q_smem, uint32_t tmem,
+                                           uint32_t b) {
+  using S = Shape<DP>;
+  constexpr uint32_t id_s = tc::idesc16(BF16, 128, kQ, false), id_o = tc::idesc16(BF16, 128, DP, true);
+  const uint64_t dk = tc::sdesc_sw128(k_smem), dv = tc::sdesc_sw128(v_smem);
+  const uint64_t dq = tc::sdesc_sw128(q_smem), dqt = tc::sdesc_mn_sw128(q_smem, kQ * kRowBytes);
+  const uint32_t s_at = tmem + b * 128, dp_at = s_at + 64, dv_at = tmem + 256, dk_at = tmem + 384;
+  // a walk over the steps of this parity
+  uint32_t i = 0, j = b;       // items begun; the next own step
+  uint32_t base = 0, end = 0;  // the present item's steps
+  uint32_t n_kv = 0, kv = 0;   // items with steps: begun; whose keys and values were waited for
+  uint32_t done = 0;           // own steps so far
+  struct {
+    bool any, first, last;
+    uint32_t stage, j, items;
+  } was = {false, false, false, 0, 0, 0};
+  for (;;) {
+    // Step j's item: one item further at most before the products of the step before are issued (the loader
+    // knows one ahead; more may wait for those very products)
+    bool over = false, have = j < end;
+    if (!have) {
+      // the item's keys and values are done with once the scores issued so far are
+      if (end > base && tc::elect_one()) tc::mma_commit(&sh.kv_free);
+      if (i > 0 && tc::elect_one()) tc::bar_arrive(&sh.item_free[(i - 1) % kItems]);
+      __syncwarp();
+      WAIT(sh.item_full[i % kItems], (i / kItems) & 1);
+      over = sh.item[i % kItems].nk[1] != 0;
+      base = end;
+      if (!over) end = base + sh.item[i % kItems].steps;
+      if (end > base) ++n_kv;
+      ++i;
+      have = j < end;
+    }
+    const uint32_t st = j % S::kStages;
+    if (was.any) {
+      WAIT(sh.p_full[b], (done - 1) & 1);
+      if (was.j > 0) WAIT(sh.added[b ^ 1], ((was.j - 1) >> 1) & 1);  // the step before it
+      if (was.first) WAIT(sh.o_free, (was.items & 1) ^ 1);           // (after that: the items before have begun)
+      tc::fence_after();
+      if (tc::elect_one()) {
+        const uint64_t d = dqt + was.stage * (S::kTile >> 4) + (S::kHalf >> 4);
+#pragma unroll
+        for (int q = 0; q < kQ / 16; ++q)
+          tc::mma_ts(dv_at, s_at + q * 8, d + q * (16 * kRowBytes >> 4), id_o, q > 0 || !was.first ? 1u : 0u);
+      }
+      __syncwarp();
+    }
+    if (have) {
+      for (; kv < n_kv; ++kv) WAIT(sh.kv_full, kv & 1);  // (every phase, those of items without own steps too)
+      WAIT(sh.ready[st], (j / S::kStages) & 1);
+      tc::fence_after();
+      if (tc::elect_one()) {
+        const uint64_t d = dq + st * (S::kTile >> 4);
+#pragma unroll
+        for (int q = 0; q < DP / 16; ++q)
+          tc::mma_bf16(s_at, dk + (q >> 2) * (128 * kRowBytes >> 4) + (q & 3) * 2, d + (q >> 2) * (kQ * kRowBytes >> 4) + (q & 3) * 2, id_s, q > 0);
+        tc::mma_commit(&sh.s_full[b]);
+      }
+      __syncwarp();
+    }
+    if (was.any) {
+      WAIT(sh.ds_full[b], (done - 1) & 1);
+      tc::fence_after();
+      if (tc::elect_one()) {
+        const uint64_t d = dqt + was.stage * (S::kTile >> 4);
+#pragma unroll
+        for (int q = 0; q < kQ / 16; ++q)
+          tc::mma_ts(dk_at, dp_at + q * 8, d + q * (16 * kRowBytes >> 4), id_o, q > 0 || !was.first ? 1u : 0u);
+        tc::mma_commit(&sh.added[b]);
+        tc::mma_commit(&sh.free[was.stage]);
+        if (was.last) tc::mma_commit(&sh.o_full);
+      }
+      __syncwarp();
+    }
+    if (over) return;
+    if (!have) {
+      was.any = false;
+      continue;
+    }
+    if (tc::elect_one()) {
+      const uint64_t d = dq + st * (S::kTile >> 4) + (S::kHalf >> 4);
+#pragma unroll
+      for (int q = 0; q < DP / 16; ++q)
+        tc::mma_bf16(dp_at, dv + (q >> 2) * (128 * kRowBytes >> 4) + (q & 3) * 2, d + (q >> 2) * (kQ * kRowBytes >> 4) + (q & 3) * 2, id_s, q > 0);
+      tc::mma_commit(&sh.dp_full[b]);
+    }
+    __syncwarp();
+    was.any = true;
+    was.first = j == base;
+    was.last = j + 1 == end;
+    was.stage = st;
+    was.j = j;
+    was.items = n_kv - 1;  // items with steps before this one
+    ++done;
+    j += 2;
+  }
+}
+
+// A key a thread: P^T and dS^T of the steps of parity b
+template <int DP, bool BF16, class Sh>
+__device__ __forceinline__ void element_role(const GradParams& p, Sh& sh, int log_p, uint32_t tmem, uint32_t b) {
+  using S = Shape<DP>;
+  const int r = threadIdx.x & 127, lane = threadIdx.x & 31;
+  const uint32_t s_at = tmem + b * 128 + ((uint32_t)(r & ~31) << 16), dp_at = s_at + 64;
+  const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
+  uint32_t j = 0, done = 0;
+  for (uint32_t i = 0;; ++i) {
+    WAIT(sh.item_full[i % kItems], (i / kItems) & 1);
+    const PromptItem it = sh.item[i % kItems];
+    if (it.nk[1]) return;
+    const int key = it.tile * 128 + r, ahead = it.keys - it.rows;  // keys before the first row's own
+    const float power = BF16 || it.steps == 0 ? 1.f : p.power[it.row0 * p.Hkv + it.hb] * Lift<BF16>::kBack;
+#pragma unroll 1
+    for (int k = 0; k < it.steps; ++k, ++j) {
+      if ((j & 1) != b) continue;
+      const int st = j % S::kStages;
+      const Place at = place_of(p, it, log_p, k);
+      WAIT(sh.ready[st], (j / S::kStages) & 1);
+      const float4* stat = reinterpret_cast<const float4*>(sh.stat[st]);
+      WAIT(sh.s_full[b], done & 1);
+      tc::fence_after();
+      uint32_t v[64];
+      tc::tmem_ld64(s_at, v);
+      tc::wait_ld64(v);
+      float pr[64];
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        const float4 q = stat[e];
+        float2 y = tc::fma2(make_float2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), scale2,
+                            make_float2(Lift<BF16>::kLog2 - q.x, Lift<BF16>::kLog2 - q.z));
+        pr[2 * e] = fast_exp2(y.x);
+        pr[2 * e + 1] = fast_exp2(y.y);
+      }
+      // keys that some row of the block does not see (all keys past the sequence's end are nobody's: their rows are not written)
+      if (p.causal && it.tile * 128 + 127 > ahead + at.tok) {
+        const int lo = min(max(key - ahead - at.tok, 0), kQ) << log_p;  // the first row of the block that sees this key
+#pragma unroll
+        for (int e = 0; e < 64; ++e) pr[e] = e < lo ? 0.f : pr[e];
+      }
+      {
+        uint32_t pk[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) pk[e] = pack16<BF16>(pr[2 * e], pr[2 * e + 1]);
+        tc::tmem_st32(s_at, pk);
+      }
+      tc::tmem_wait_st();
+      tc::fence_before();
+      tc::bar_arrive(&sh.p_full[b]);
+      WAIT(sh.dp_full[b], done & 1);
+      tc::fence_after();
+      tc::tmem_ld64(dp_at, v);
+      tc::wait_ld64(v);
+      uint32_t pk[32];
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        const float4 q = stat[e];
+        float2 y = tc::add2(make_float2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), make_float2(q.y, q.w));
+        y.x *= pr[2 * e];
+        y.y *= pr[2 * e + 1];
+        if (!BF16) y.x *= power, y.y *= power;
+        pk[e] = pack16<BF16>(y.x, y.y);
+      }
+      tc::tmem_st32(dp_at, pk);
+      tc::tmem_wait_st();
+      tc::fence_before();
+      tc::bar_arrive(&sh.ds_full[b]);
+      ++done;
+    }
+    __syncwarp();
+    if (lane == 0) tc::bar_arrive(&sh.item_free[i % kItems]);
+  }
+}
+
+template <int DP, bool BF16, class Sh>
+__device__ __forceinline__ void write_role(const GradParams& p, Sh& sh, unsigned char* stage, uint32_t tmem) {
+  const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31;
+  const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+  const RowWriter writer{stage + warp * (32 * 128), lane};
+  uint32_t n = 0;
+  for (uint32_t i = 0;; ++i) {
+    WAIT(sh.item_full[i % kItems], (i / kItems) & 1);
+    const PromptItem it = sh.item[i % kItems];
+    if (it.nk[1]) return;
+    if (it.steps > 0) {
+      WAIT(sh.o_full, n & 1);
+      tc::fence_after();
+      ++n;
+    }
+    const float back = BF16 || it.steps == 0 ? 1.f : 1.f / p.power[it.row0 * p.Hkv + it.hb];
+#pragma unroll 1
+    for (int which = 0; which < 2; ++which) {
+      uint16_t* base = which ? p.dk : p.dv;
+      const int64_t row = which ? p.dk_row : p.dv_row;
+      const float f = which ? p.scale * back : Lift<BF16>::kBack;
+#pragma unroll 1
+      for (int blk = 0; blk < Shape<DP>::kBlocks; ++blk) {
+        const int cols = min(DP - blk * 64, 64);
+#pragma unroll 1
+        for (int c = 0; c < cols; c += 16) {
+          uint32_t o[16], w[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+          if (it.steps > 0) {
+            tc::tmem_ld16(tmem + 256 + which * 128 + lanes + blk * 64 + c, o);
+            scale_pack<BF16>(o, f, w);
+          }
+          writer.put16(c, w);
+        }
+        if (which && blk == Shape<DP>::kBlocks - 1 && it.steps > 0) {
+          tc::fence_before();
+          tc::bar_arrive(&sh.o_free);
+        }
+        writer.flush(blk, p.dim / 8, [&](int rr) -> uint16_t* {
+          const int64_t key = (int64_t)it.tile * 128 + warp * 32 + rr;
+          return key < it.keys && in_bounds(it.key0 + key < p.total_keys, p.status, kSitePromptRow)
+                     ? base + (it.key0 + key) * row + it.hb * p.dim
+                     : nullptr;
+        });
+      }
+    }
+    __syncwarp();
+    if (lane == 0) tc::bar_arrive(&sh.item_free[i % kItems]);
+  }
+}
+
+template <int DP, bool BF16>
+__global__ void __launch_bounds__(kThreads, 1)
+    prompt_keys_kernel(GradParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_do,
+                       const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+  using S = Shape<DP>;
+  using Sh = Shared<S::kStages>;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  unsigned char* k_smem = smem;
+  unsigned char* v_smem = k_smem + S::kTile;
+  unsigned char* q_smem = v_smem + S::kTile;
+  unsigned char* stage = q_smem + S::kStages * S::kTile;
+  Sh& sh = *reinterpret_cast<Sh*>(stage + 4 * 32 * 128);
+  const int warp = threadIdx.x >> 5, log_p = min(p.log2P, 6);
+  if (threadIdx.x == 0) {
+    sh.stop = 0;
+    tc::bar_init(&sh.kv_full, 1);
+    tc::bar_init(&sh.kv_free, 2);
+    for (int k = 0; k < S::kStages; ++k) {
+      tc::bar_init(&sh.full[k], 1);
+      tc::bar_init(&sh.ready[k], 1);
+      tc::bar_init(&sh.free[k], 1);
+    }
+    for (int k = 0; k < 2; ++k) {
+      tc::bar_init(&sh.s_full[k], 1);
+      tc::bar_init(&sh.dp_full[k], 1);
+      tc::bar_init(&sh.p_full[k], 128);
+      tc::bar_init(&sh.ds_full[k], 128);
+      tc::bar_init(&sh.added[k], 1);
+    }
+    tc::bar_init(&sh.o_full, 1);
+    tc::bar_init(&sh.o_free, 128);
+    for (int k = 0; k < kItems; ++k) {
+      tc::bar_init(&sh.item_full[k], 1);
+      tc::bar_init(&sh.item_free[k], 16);  // every warp
+    }
+    tc::bar_init(&sh.drain, 2);
+    tc::bar_fence_init();
+  }
+  pdl_wait();
+  if (warp == 12) tc::tmem_alloc(&sh.tmem, 512);
+  prompt_list(p, sh.list, Count{p});
+  tc::fence_before();
+  __syncthreads();
+  tc::fence_after();
+  const uint32_t tmem = sh.tmem;
+  if (warp < 8) {
+    tc::setmaxnreg_inc<kRegElement>();
+    element_role<DP, BF16>(p, sh, log_p, tmem, warp >> 2);
+  } else if (warp < 12) {
+    tc::setmaxnreg_dec<kRegWrite>();
+    write_role<DP, BF16>(p, sh, stage, tmem);
+  } else {
+    tc::setmaxnreg_dec<kRegIssue>();
+    if (warp == 13)
+      load_role<DP>(p, sh, log_p, map_q, map_do, map_k, map_v, k_smem, v_smem, q_smem);
+    else if (warp == 15)
+      look_role<DP>(p, sh, log_p, q_smem);
+    else
+      issue_role<DP, BF16>(p, sh, tc::su32(k_smem), tc::su32(v_smem), tc::su32(q_smem), tmem, warp == 14);
+  }
+  __syncthreads();
+  // after a wait that ran out, products and copies may still be in flight
+  if (sh.stop && (warp == 12 || warp == 14) && tc::elect_one()) {
+    tc::mma_commit(&sh.drain);
+    tc::bar_wait(&sh.drain, 0, nullptr, kPromptWaitNs);
+    for (int k = 0; k < 2 * (S::kStages + 1); ++k)
+      tc::bar_wait(k / 2 < S::kStages ? &sh.full[k / 2] : &sh.kv_full, k & 1, nullptr, kPromptWaitNs / 16);
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) prompt_leave(p, gridDim.x);
+  if (warp == 12) tc::tmem_dealloc(tmem, 512);
+}
+
+}  // namespace keys
+
+// ================================================================ dQ
+// An item is 256 query rows, two tiles of 128 as in the forward pass; its steps are blocks of 64 keys. S = Q K^T and
+// dP = dO V^T a row a lane, dS in the place of S, dQ += dS K. Each row tile has an issuing warp and a
+// warpgroup: while one tile's dS is formed, the other's products run.
+namespace rows {
+
+constexpr int kKeys = 64;
+
+template <int DP>
+struct Shape {
+  static constexpr int kBlocks = DP > 64 ? 2 : 1;
+  static constexpr int kTile = kBlocks * 128 * kRowBytes;  // bytes of 128 rows
+  static constexpr int kHalf = kTile / 2;                  // and of 64
+  static constexpr int kStages = DP > 64 ? 2 : 4;
+};
+
+template <int STAGES>
+struct Shared {
+  uint64_t q_full[2], q_free[2], k_full[STAGES], k_ready[STAGES], k_free[STAGES], v_full[STAGES], v_free[STAGES], s_full[2], dp_full[2],
+      ds_full[2], o_full[2], o_free[2], item_full[kItems], item_free[kItems], drain;
+  PromptItem item[kItems];
+  uint32_t tmem;
+  int stop;
+  PromptList list;
+};
+
+struct Count {
+  const GradParams& p;
+  __device__ __forceinline__ int operator()(const PromptSeq& s) const {
+    const int per = 256 >> p.log2P;
+    return (s.rows / per + (s.rows % per != 0)) * (p.H >> p.log2P);
+  }
+};
+__device__ __forceinline__ int key_steps(const GradParams& p, const PromptSeq& s, int tok_last) {
+  const int lim = min(prompt_limit(p, s.rows, s.keys, tok_last), s.keys);
+  return max((lim + kKeys - 1) / kKeys, 1);
+}
+
+template <int DP, class Sh>
+__device__ __forceinline__ void load_role(const GradParams& p, Sh& sh, const CUtensorMap& map_q, const CUtensorMap& map_do,
+                                          const CUtensorMap& map_k, const CUtensorMap& map_v, unsigned char* q_smem,
+                                          unsigned char* do_smem, unsigned char* k_smem, unsigned char* v_smem) {
+  using S = Shape<DP>;
+  const int lane = threadIdx.x & 31, total = sh.list.first[kChunks];
+  const Count count{p};
+  int next = blockIdx.x;
+  uint32_t told = 0;
+  auto tell = [&]() -> bool {
+    PromptItem& it = sh.item[told % kItems];
+    if (!tc::bar_try(&sh.item_free[told % kItems], ((told / kItems) & 1) ^ 1) &&
+        !prompt_wait_long(&sh.item_free[told % kItems], ((told / kItems) & 1) ^ 1, &sh.stop, p.status))
+      return false;
+    if (next < total) {
+      int place = 0;
+      const PromptSeq s = prompt_find(p, sh.list, count, next, &place);
+      const int hbs = p.H >> p.log2P, log_tt = 7 - p.log2P, per = 2 << log_tt;
+      const int blocks = (s.rows + per - 1) / per;
+      const int tile = blocks - 1 - place / hbs, hb = place % hbs, tok0 = tile * per;
+      const int left = s.rows - tok0;
+      const int nk0 = key_steps(p, s, tok0 + min(left, 1 << log_tt) - 1);
+      const int nk1 = left > (1 << log_tt) ? key_steps(p, s, tok0 + min(left, per) - 1) : 0;
+      if (lane == 0) {
+        it.row0 = s.row0;
+        it.key0 = s.key0;
+        it.rows = s.rows;
+        it.keys = s.keys;
+        it.tile = tile;
+        it.hb = hb;
+        it.steps = max(nk0, nk1);
+        it.nk[0] = nk0;
+        it.nk[1] = nk1;
+        next = gridDim.x + atomicAdd(&p.counters[0], 1);
+      }
+      next = __shfl_sync(0xffffffffu, next, 0);
+    } else if (lane == 0) {
+      it.steps = 0;
+    }
+    __syncwarp();
+    if (lane == 0) tc::bar_arrive(&sh.item_full[told % kItems]);
+    __syncwarp();
+    ++told;
+    return true;
+  };
+  if (!tell()) return;
+  uint32_t j = 0, nq[2] = {0, 0};
+  for (uint32_t i = 0;; ++i) {
+    const PromptItem it = sh.item[i % kItems];
+    if (it.steps == 0) break;
+    if (!tell()) return;
+    const int tt = 128 >> p.log2P, head = it.hb << p.log2P, kv = head / p.G;
+    for (int k = 0; k < it.steps; ++k, ++j) {
+      const int st = j % S::kStages;
+      const uint32_t turn = ((j / S::kStages) & 1) ^ 1;
+      const int key = (int)(it.key0 + (int64_t)k * kKeys);
+      WAIT(sh.k_free[st], turn);
+      if (lane == 0) {
+        tc::bar_expect_tx(&sh.k_full[st], S::kHalf);
+        for (int b = 0; b < S::kBlocks; ++b)
+          tc::tma_load_3d(k_smem + st * S::kHalf + b * kKeys * kRowBytes, &map_k, b * 64, kv, key, &sh.k_full[st]);
+      }
+      if (k == 0) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if (it.nk[t] == 0) continue;
+          WAIT(sh.q_free[t], (nq[t] & 1) ^ 1);
+          ++nq[t];
+          if (lane == 0) {
+            const int row = (int)(it.row0 + (int64_t)(it.tile * 2 + t) * tt);
+            tc::bar_expect_tx(&sh.q_full[t], 2 * S::kTile);
+            for (int b = 0; b < S::kBlocks; ++b) {
+              tc::tma_load_3d(q_smem + t * S::kTile + b * 128 * kRowBytes, &map_q, b * 64, head, row, &sh.q_full[t]);
+              tc::tma_load_3d(do_smem + t * S::kTile + b * 128 * kRowBytes, &map_do, b * 64, head, row, &sh.q_full[t]);
+            }
+          }
+        }
+      }
+      WAIT(sh.v_free[st], turn);
+      if (lane == 0) {
+        tc::bar_expect_tx(&sh.v_full[st], S::kHalf);
+        for (int b = 0; b < S::kBlocks; ++b)
+          tc::tma_load_3d(v_smem + st * S::kHalf + b * kKeys * kRowBytes, &map_v, b * 64, kv, key, &sh.v_full[st]);
+      }
+      __syncwarp();
+    }
+    if (lane == 0) tc::bar_arrive(&sh.item_free[i % kItems]);
+    __syncwarp();
+  }
+}
+
+// Keys past the sequence's end become zeros: dS is 0 there, but what lies behind may be anything.
+template <int DP, class Sh>
+__device__ __forceinline__ void look_role(const GradParams& p, Sh& sh, unsigned char* k_smem) {
+  using S = Shape<DP>;
+  const int lane = threadIdx.x & 31;
+  uint32_t j = 0;
+  for (uint32_t i = 0;; ++i) {
+    WAIT(sh.item_full[i % kItems], (i / kItems) & 1);
+    const int steps = sh.item[i % kItems].steps, keys = sh.item[i % kItems].keys;
+    if (steps == 0) return;
+#pragma unroll 1
+    for (int k = 0; k < steps; ++k, ++j) {
+      const int st = j % S::kStages, live = max(keys - k * kKeys, 0);
+      WAIT(sh.k_full[st], (j / S::kStages) & 1);
+      if (live < kKeys) {
+#pragma unroll 1
+        for (int b = 0; b < S::kBlocks; ++b) {
+          uint4* piece = reinterpret_cast<uint4*>(k_smem + st * S::kHalf + b * kKeys * kRowBytes);
+          for (int e = live * 8 + lane; e < kKeys * 8; e += 32) piece[e] = make_uint4(0, 0, 0, 0);
+        }
+        tc::fence_proxy_async();
+      }
+      __syncwarp();
+      if (lane == 0) tc::bar_arrive(&sh.k_ready[st]);
+    }
+    if (lane == 0) tc::bar_arrive(&sh.item_free[i % kItems]);
+  }
+}
+
+template <int DP, bool BF16, class Sh>
+__device__ __forceinline__ void issue_role(const GradParams& p, Sh& sh, uint32_t q_smem, uint32_t do_smem, uint32_t k_smem, uint32_t v_smem,
+                                           uint32_t tmem, int t) {
+  using S = Shape<DP>;
+  constexpr uint32_t id_s = tc::idesc16(BF16, 128, kKeys, false), id_o = tc::idesc16(BF16, 128, DP, true);
+  const uint64_t dq = tc::sdesc_sw128(q_smem + t * S::kTile), ddo = tc::sdesc_sw128(do_smem + t * S::kTile);
+  const uint64_t dk = tc::sdesc_sw128(k_smem), dv = tc::sdesc_sw128(v_smem), dkt = tc::sdesc_mn_sw128(k_smem, kKeys * kRowBytes);
+  const uint32_t s_at = tmem + t * 256, dp_at = s_at + 64, o_at = s_at + 128;
+  uint32_t j = 0, done = 0, n_q = 0, n_o = 0;
+  struct {
+    bool any, mine, first, last;
+  } was = {false, false, false, false};
+  uint32_t i = 0;
+  int k = 0, steps = 0, nk = 0;
+  for (;;) {
+    if (k == steps) {
+      if (i > 0 && tc::elect_one()) tc::bar_arrive(&sh.item_free[(i - 1) % kItems]);
+      __syncwarp();
+      WAIT(sh.item_full[i % kItems], (i / kItems) & 1);
+      steps = sh.item[i % kItems].steps;
+      nk = steps == 0 ? 0 : sh.item[i % kItems].nk[t];
+      k = 0;
+      ++i;
+    }
+    const bool end = steps == 0, mine = !end && k < nk;
+    const uint32_t st = j % S::kStages, before = (j - 1) % S::kStages;
+    if (was.any) {
+      if (was.mine) {
+        if (was.first) {
+          WAIT(sh.o_free[t], (n_o & 1) ^ 1);
+          ++n_o;
+        }
+        WAIT(sh.ds_full[t], (done - 1) & 1);
+        tc::fence_after();
+        if (tc::elect_one()) {
+#pragma unroll
+          for (int q = 0; q < kKeys / 16; ++q)
+            tc::mma_ts(o_at, s_at + q * 8, dkt + before * (S::kHalf >> 4) + q * (16 * kRowBytes >> 4), id_o, q > 0 || !was.first ? 1u : 0u);
+          if (was.last) tc::mma_commit(&sh.o_full[t]);
+        }
+        __syncwarp();
+      }
+      if (tc::elect_one()) was.mine ? tc::mma_commit(&sh.k_free[before]) : tc::bar_arrive(&sh.k_free[before]);
+      __syncwarp();
+    }
+    if (end) return;
+    WAIT(sh.k_ready[st], (j / S::kStages) & 1);
+    if (mine && k == 0) {
+      WAIT(sh.q_full[t], n_q & 1);
+      ++n_q;
+    }
+    tc::fence_after();
+    if (mine && tc::elect_one()) {
+#pragma unroll
+      for (int q = 0; q < DP / 16; ++q)
+        tc::mma_bf16(s_at, dq + (q >> 2) * (128 * kRowBytes >> 4) + (q & 3) * 2,
+                     dk + st * (S::kHalf >> 4) + (q >> 2) * (kKeys * kRowBytes >> 4) + (q & 3) * 2, id_s, q > 0);
+      tc::mma_commit(&sh.s_full[t]);
+    }
+    __syncwarp();
+    WAIT(sh.v_full[st], (j / S::kStages) & 1);
+    tc::fence_after();
+    if (tc::elect_one()) {
+      if (mine) {
+#pragma unroll
+        for (int q = 0; q < DP / 16; ++q)
+          tc::mma_bf16(dp_at, ddo + (q >> 2) * (128 * kRowBytes >> 4) + (q & 3) * 2,
+                       dv + st * (S::kHalf >> 4) + (q >> 2) * (kKeys * kRowBytes >> 4) + (q & 3) * 2, id_s, q > 0);
+        tc::mma_commit(&sh.dp_full[t]);
+        tc::mma_commit(&sh.v_free[st]);
+        if (k == nk - 1) tc::mma_commit(&sh.q_free[t]);
+      } else {
+        tc::bar_arrive(&sh.v_free[st]);
+      }
+    }
+    __syncwarp();
+    was.any = true;
+    was.mine = mine;
+    was.first = k == 0;
+    was.last = k == nk - 1;
+    if (mine) ++done;
+    ++j;
+    ++k;
+  }
+}
+
+// A row a thread
+template <int DP, bool BF16, class Sh>
+__device__ __forceinline__ void element_role(const GradParams& p, Sh& sh, uint32_t tmem, int t) {
+  const int r = threadIdx.x & 127, lane = threadIdx.x & 31;
+  const uint32_t s_at = tmem + t * 256 + ((uint32_t)(r & ~31) << 16), dp_at = s_at + 64;
+  const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
+  uint32_t done = 0;
+  for (uint32_t i = 0;; ++i) {
+    WAIT(sh.item_full[i % kItems], (i / kItems) & 1);
+    const PromptItem& x = sh.item[i % kItems];
+    const int steps = x.steps, nk = x.nk[t], rows = x.rows, keys = x.keys;
+    if (steps == 0) return;
+    const int first = (x.tile * 2 + t) << (7 - p.log2P), tok = first + (r >> p.log2P), head0 = x.hb << p.log2P;
+    const int64_t row0 = x.row0, at = (row0 + tok) * p.H + head0 + (r & ((1 << p.log2P) - 1));
+    __syncwarp();
+    if (lane == 0) tc::bar_arrive(&sh.item_free[i % kItems]);
+    if (nk == 0) continue;
+    const int limit = min(prompt_limit(p, rows, keys, tok), keys), common = min(prompt_limit(p, rows, keys, first), keys);
+    float2 stat = make_float2(INFINITY, 0.f);
+    if (tok < rows && in_bounds(at < p.total_rows * p.H, p.status, kSitePromptRow)) stat = p.stat[at];
+    const float power = BF16 ? 1.f : p.power[row0 * p.Hkv + head0 / p.G];
+    const float2 add2 = make_float2(-stat.x, -stat.x), delta2 = make_float2(stat.y * power, stat.y * power);
+    const float2 power2 = make_float2(power, power);
+#pragma unroll 1
+    for (int k = 0; k < nk; ++k, ++done) {
+      WAIT(sh.s_full[t], done & 1);
+      tc::fence_after();
+      uint32_t v[64];
+      tc::tmem_ld64(s_at, v);
+      tc::wait_ld64(v);
+      float pr[64];
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        const float2 y = tc::fma2(make_float2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), scale2, add2);
+        pr[2 * e] = fast_exp2(y.x);
+        pr[2 * e + 1] = fast_exp2(y.y);
+      }
+      if ((k + 1) * kKeys > common) {
+        const int lim = limit - k * kKeys;
+#pragma unroll
+        for (int e = 0; e < 64; ++e) pr[e] = e < lim ? pr[e] : 0.f;
+      }
+      WAIT(sh.dp_full[t], done & 1);
+      tc::fence_after();
+      tc::tmem_ld64(dp_at, v);
+      tc::wait_ld64(v);
+      // keys past the end: what is there may be anything
+      if (k * kKeys + kKeys > keys) {
+#pragma unroll
+        for (int e = 0; e < 64; ++e) v[e] = k * kKeys + e < keys ? v[e] : 0u;
+      }
+      uint32_t pk[32];
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        float2 y = tc::fma2(make_float2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), power2, delta2);
+        pk[e] = pack16<BF16>(y.x * pr[2 * e], y.y * pr[2 * e + 1]);
+      }
+      tc::tmem_st32(s_at, pk);
+      tc::tmem_wait_st();
+      tc::fence_before();
+      tc::bar_arrive(&sh.ds_full[t]);
+    }
+  }
+}
+
+template <int DP, bool BF16, class Sh>
+__device__ __forceinline__ void write_role(const GradParams& p, Sh& sh, unsigned char* stage, uint32_t tmem) {
+  const int warp = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31;
+  const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+  const RowWriter writer{stage + warp * (32 * 128), lane};
+  uint32_t n[2] = {0, 0};
+  for (uint32_t i = 0;; ++i) {
+    WAIT(sh.item_full[i % kItems], (i / kItems) & 1);
+    const PromptItem x = sh.item[i % kItems];
+    if (x.steps == 0) return;
+    const float f = BF16 ? p.scale : p.scale / p.power[x.row0 * p.Hkv + (x.hb << p.log2P) / p.G];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      if (x.nk[t] == 0) continue;
+      WAIT(sh.o_full[t], n[t] & 1);
+      tc::fence_after();
+      ++n[t];
+#pragma unroll 1
+      for (int blk = 0; blk < Shape<DP>::kBlocks; ++blk) {
+        const int cols = min(DP - blk * 64, 64);
+#pragma unroll 1
+        for (int c = 0; c < cols; c += 16) {
+          uint32_t o[16], w[8];
+          tc::tmem_ld16(tmem + t * 256 + 128 + lanes + blk * 64 + c, o);
+          scale_pack<BF16>(o, f, w);
+          writer.put16(c, w);
+        }
+        if (blk == Shape<DP>::kBlocks - 1) {
+          tc::fence_before();
+          tc::bar_arrive(&sh.o_free[t]);
+        }
+        writer.flush(blk, p.dim / 8, [&](int rr) -> uint16_t* {
+          const int row = warp * 32 + rr, tok = ((x.tile * 2 + t) << (7 - p.log2P)) + (row >> p.log2P);
+          return tok < x.rows && in_bounds(x.row0 + tok < p.total_rows, p.status, kSitePromptRow)
+                     ? p.dq + (x.row0 + tok) * p.dq_row + ((x.hb << p.log2P) + (row & ((1 << p.log2P) - 1))) * p.dim
+                     : nullptr;
+        });
+      }
+    }
+    __syncwarp();
+    if (lane == 0) tc::bar_arrive(&sh.item_free[i % kItems]);
+  }
+}
+
+template <int DP, bool BF16>
+__global__ void __launch_bounds__(kThreads, 1)
+    prompt_rows_kernel(GradParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_do,
+                       const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+  using S = Shape<DP>;
+  using Sh = Shared<S::kStages>;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  unsigned char* q_smem = smem;
+  unsigned char* do_smem = q_smem + 2 * S::kTile;
+  unsigned char* k_smem = do_smem + 2 * S::kTile;
+  unsigned char* v_smem = k_smem + S::kStages * S::kHalf;
+  unsigned char* stage = v_smem + S::kStages * S::kHalf;
+  Sh& sh = *reinterpret_cast<Sh*>(stage + 4 * 32 * 128);
+  const int warp = threadIdx.x >> 5;
+  if (threadIdx.x == 0) {
+    sh.stop = 0;
+    for (int k = 0; k < 2; ++k) {
+      tc::bar_init(&sh.q_full[k], 1);
+      tc::bar_init(&sh.q_free[k], 1);
+      tc::bar_init(&sh.s_full[k], 1);
+      tc::bar_init(&sh.dp_full[k], 1);
+      tc::bar_init(&sh.ds_full[k], 128);
+      tc::bar_init(&sh.o_full[k], 1);
+      tc::bar_init(&sh.o_free[k], 128);
+    }
+    for (int k = 0; k < S::kStages; ++k) {
+      tc::bar_init(&sh.k_full[k], 1);
+      tc::bar_init(&sh.k_ready[k], 1);
+      tc::bar_init(&sh.k_free[k], 2);
+      tc::bar_init(&sh.v_full[k], 1);
+      tc::bar_init(&sh.v_free[k], 2);
+    }
+    for (int k = 0; k < kItems; ++k) {
+      tc::bar_init(&sh.item_full[k], 1);
+      tc::bar_init(&sh.item_free[k], 16);  // every warp
+    }
+    tc::bar_init(&sh.drain, 2);
+    tc::bar_fence_init();
+  }
+  pdl_wait();
+  if (warp == 12) tc::tmem_alloc(&sh.tmem, 512);
+  prompt_list(p, sh.list, Count{p});
+  tc::fence_before();
+  __syncthreads();
+  tc::fence_after();
+  const uint32_t tmem = sh.tmem;
+  if (warp < 8) {
+    tc::setmaxnreg_inc<kRegElement>();
+    element_role<DP, BF16>(p, sh, tmem, warp >> 2);
+  } else if (warp < 12) {
+    tc::setmaxnreg_dec<kRegWrite>();
+    write_role<DP, BF16>(p, sh, stage, tmem);
+  } else {
+    tc::setmaxnreg_dec<kRegIssue>();
+    if (warp == 13)
+      load_role<DP>(p, sh, map_q, map_do, map_k, map_v, q_smem, do_smem, k_smem, v_smem);
+    else if (warp == 15)
+      look_role<DP>(p, sh, k_smem);
+    else
+      issue_role<DP, BF16>(p, sh, tc::su32(q_smem), tc::su32(do_smem), tc::su32(k_smem), tc::su32(v_smem), tmem, warp == 14);
+  }
+  __syncthreads();
+  // after a wait that ran out, products and copies may still be in flight
+  if (sh.stop && (warp == 12 || warp == 14) && tc::elect_one()) {
+    tc::mma_commit(&sh.drain);
+    tc::bar_wait(&sh.drain, 0, nullptr, kPromptWaitNs);
+    for (int k = 0; k < 2 * (2 * S::kStages + 2); ++k) {
+      uint64_t* bar = k / 2 < S::kStages ? &sh.k_full[k / 2] : k / 2 < 2 * S::kStages ? &sh.v_full[k / 2 - S::kStages] : &sh.q_full[k / 2 - 2 * S::kStages];
+      tc::bar_wait(bar, k & 1, nullptr, kPromptWaitNs / 16);
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) prompt_leave(p, gridDim.x);
+  if (warp == 12) tc::tmem_dealloc(tmem, 512);
+}
+
+}  // namespace rows
+
+// Once per device and kernel: the shared memory, and that the register split adds up --
+// setmaxnreg.inc waits for registers that only the launch's own can give.
+template <class Kernel>
+int launch(Kernel kern, std::atomic<uint64_t>& ready, int smem, int grid, const GradParams& p, const CUtensorMap (&m)[4], cudaStream_t st) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return OCCAM_ERR_CUDA;
+  if (!((ready.load(std::memory_order_acquire) >> dev) & 1)) {
+    cudaFuncAttributes at;
+    if (cudaFuncGetAttributes(&at, kern) != cudaSuccess) return OCCAM_ERR_CUDA;
+    if (at.numRegs * kThreads < 256 * kRegElement + 128 * (kRegWrite + kRegIssue)) return OCCAM_ERR_UNSUPPORTED;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return OCCAM_ERR_CUDA;
+    ready.fetch_or(uint64_t(1) << dev, std::memory_order_release);
+  }
+  return launch_after(kern, dim3((unsigned)grid), kThreads, smem, st, p, m[0], m[1], m[2], m[3]) && cudaGetLastError() == cudaSuccess
+             ? OCCAM_OK
+             : OCCAM_ERR_CUDA;
+}
+
+template <int DP, bool BF16>
+int launch_grad(const GradParams& p, const CUtensorMap (&mk)[4], const CUtensorMap (&mr)[4], int grid_keys, int grid_rows, cudaStream_t st) {
+  const int64_t vectors = p.total_rows * p.H + (BF16 ? 0 : p.total_keys * p.Hkv);
+  if (p.total_rows > 0) {
+    if ((vectors + 15) / 16 > 0x7fffffff) return OCCAM_ERR_UNSUPPORTED;
+    if (!launch_after(stat_kernel<BF16>, dim3((unsigned)((vectors + 15) / 16)), 256, 0, st, p)) return OCCAM_ERR_CUDA;
+    if (!BF16 && !launch_after(power_kernel, dim3((unsigned)p.n, (unsigned)p.Hkv), 512, 0, st, p)) return OCCAM_ERR_CUDA;
+  }
+  using K = keys::Shape<DP>;
+  using R = rows::Shape<DP>;
+  constexpr int smem_k = (2 + K::kStages) * K::kTile + 4 * 32 * 128 + (int)sizeof(keys::Shared<K::kStages>);
+  constexpr int smem_r = 4 * R::kTile + 2 * R::kStages * R::kHalf + 4 * 32 * 128 + (int)sizeof(rows::Shared<R::kStages>);
+  static_assert(smem_k <= 227 * 1024 && smem_r <= 227 * 1024, "an SM's shared memory");
+  static std::atomic<uint64_t> ready_k{0}, ready_r{0};
+  if (grid_keys > 0) {
+    const int rc = launch(keys::prompt_keys_kernel<DP, BF16>, ready_k, smem_k, grid_keys, p, mk, st);
+    if (rc != OCCAM_OK) return rc;
+  }
+  return grid_rows > 0 ? launch(rows::prompt_rows_kernel<DP, BF16>, ready_r, smem_r, grid_rows, p, mr, st) : OCCAM_OK;
+}
+
+}  // namespace
+
+#define OCCAM_TRY(x)                 \
+  do {                               \
+    int _rc = (x);                   \
+    if (_rc != OCCAM_OK) return _rc; \
+  } while (0)
+
+extern "C" int occam_prompt_attend_grad(const occam_prompt_args* a, const occam_prompt_grads* g, void* workspace, size_t workspace_bytes,
+                                        occam_stream_t stream) {
+  const NvtxRange nvtx("occam_prompt_attend_grad");
+  launch_counter() = 0;
+  GradParams p{};
+  OCCAM_TRY(prompt_params(a, workspace, workspace_bytes, &p));
+  if (!g) return OCCAM_ERR_INVALID_ARG;
+  const PromptWs w = prompt_ws(a->total_rows, a->total_keys, a->heads, a->kv_heads);
+  if (workspace_bytes < w.total) return OCCAM_ERR_WORKSPACE;
+  if (a->n == 0 || (a->total_rows == 0 && a->total_keys == 0)) return OCCAM_OK;
+  const int64_t R = a->total_rows, K = a->total_keys, qw = (int64_t)a->heads * a->dim, kw = (int64_t)a->kv_heads * a->dim;
+  auto fits = [&](const void* x, int64_t rows, int64_t row, int64_t width) {
+    return rows == 0 || (x && aligned16(x) && (row & 7) == 0 && row >= width && row < (int64_t(1) << 38));
+  };
+  if (!fits(g->out, R, qw, qw) || (R > 0 && !g->lse) || !fits(g->dout, R, g->dout_row, qw) || !fits(g->dq, R, g->dq_row, qw) ||
+      !fits(g->dk, K, g->dk_row, kw) || !fits(g->dv, K, g->dv_row, kw))
+    return OCCAM_ERR_INVALID_ARG;
+  // no result lies over an input or over another result
+  const Extent to[3] = {extent(g->dq, R, g->dq_row, 1, 0, qw, 2), extent(g->dk, K, g->dk_row, 1, 0, kw, 2),
+                        extent(g->dv, K, g->dv_row, 1, 0, kw, 2)};
+  const bool there[3] = {R > 0, K > 0, K > 0};
+  for (int i = 0; i < 3; ++i) {
+    if (!there[i]) continue;
+    if (prompt_meets_inputs(a, to[i])) return OCCAM_ERR_INVALID_ARG;
+    if (R > 0 && (meet(to[i], extent(g->out, R, qw, 1, 0, qw, 2)) || meet(to[i], extent(g->dout, R, g->dout_row, 1, 0, qw, 2)) ||
+                  meet(to[i], extent(g->lse, 1, 0, 1, 0, R * a->heads * 2, 2))))
+      return OCCAM_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      if (there[j] && meet(to[i], to[j])) return OCCAM_ERR_INVALID_ARG;
+  }
+  p.o = static_cast<const uint16_t*>(g->out);
+  p.lse = const_cast<float*>(g->lse);
+  p.dout = static_cast<const uint16_t*>(g->dout);
+  p.dout_row = g->dout_row;
+  p.v = static_cast<const uint16_t*>(a->v);
+  p.v_row = a->v_row;
+  p.dq = static_cast<uint16_t*>(g->dq);
+  p.dk = static_cast<uint16_t*>(g->dk);
+  p.dv = static_cast<uint16_t*>(g->dv);
+  p.dq_row = g->dq_row;
+  p.dk_row = g->dk_row;
+  p.dv_row = g->dv_row;
+  p.stat = ws_at<float2>(workspace, w.stat);
+  p.norm = ws_at<float>(workspace, w.norm);
+  p.vnorm = ws_at<float>(workspace, w.vnorm);
+  p.power = ws_at<float>(workspace, w.power);
+  const bool bf16 = a->dtype == OCCAM_BF16;
+  const int per = 256 >> p.log2P, heads = p.H >> p.log2P, log_p = std::min(p.log2P, 6);
+  const int64_t most_rows = R == 0 ? 0 : (R / per + a->n) * heads, most_keys = K == 0 ? 0 : (K / 128 + a->n) * p.Hkv;
+  if (most_rows > (1 << 30) || most_keys > (1 << 30) || (!bf16 && p.Hkv > 65535)) return OCCAM_ERR_UNSUPPORTED;
+  // (without any rows, or any keys, the copies have to come from somewhere; what they bring is not used)
+  const void* q = R > 0 ? a->q : a->k;
+  const void* dout = R > 0 ? g->dout : a->k;
+  const void* k = K > 0 ? a->k : a->q;
+  const void* v = K > 0 ? a->v : a->q;
+  const int64_t q_row = R > 0 ? a->q_row : (int64_t(1) << 20), do_row = R > 0 ? g->dout_row : (int64_t(1) << 20);
+  const int64_t k_row = K > 0 ? a->k_row : a->q_row, v_row = K > 0 ? a->v_row : a->q_row;
+  const int64_t rows = std::max<int64_t>(R, 1), keys_n = std::max<int64_t>(K, 1);
+  CUtensorMap mk[4], mr[4];
+  if (!encode_rows(&mk[0], q, bf16, p.dim, p.H, rows, q_row, 1 << log_p, 64 >> log_p) ||
+      !encode_rows(&mk[1], dout, bf16, p.dim, p.H, rows, do_row, 1 << log_p, 64 >> log_p) ||
+      !encode_rows(&mk[2], k, bf16, p.dim, p.Hkv, keys_n, k_row, 1, 128) || !encode_rows(&mk[3], v, bf16, p.dim, p.Hkv, keys_n, v_row, 1, 128) ||
+      !encode_rows(&mr[0], q, bf16, p.dim, p.H, rows, q_row, 1 << p.log2P, 128 >> p.log2P) ||
+      !encode_rows(&mr[1], dout, bf16, p.dim, p.H, rows, do_row, 1 << p.log2P, 128 >> p.log2P) ||
+      !encode_rows(&mr[2], k, bf16, p.dim, p.Hkv, keys_n, k_row, 1, 64) || !encode_rows(&mr[3], v, bf16, p.dim, p.Hkv, keys_n, v_row, 1, 64))
+    return OCCAM_ERR_CUDA;
+  const int grid_rows = (int)std::min<int64_t>(cache_sms(), most_rows), grid_keys = (int)std::min<int64_t>(cache_sms(), most_keys);
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  if (p.dim <= 64)
+    return bf16 ? launch_grad<64, true>(p, mk, mr, grid_keys, grid_rows, st) : launch_grad<64, false>(p, mk, mr, grid_keys, grid_rows, st);
+  if (p.dim <= 80)
+    return bf16 ? launch_grad<80, true>(p, mk, mr, grid_keys, grid_rows, st) : launch_grad<80, false>(p, mk, mr, grid_keys, grid_rows, st);
+  return bf16 ? launch_grad<128, true>(p, mk, mr, grid_keys, grid_rows, st) : launch_grad<128, false>(p, mk, mr, grid_keys, grid_rows, st);
+}

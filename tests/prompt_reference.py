@@ -67,3 +67,56 @@ def assert_near(got, want, tol, dtype, where=""):
     off = (g - want).abs() - (tol + UNIT[dtype] * (want.abs() + tol) + TINY[dtype])
     off = torch.where(fine, off, -1.0)
     assert off.numel() == 0 or float(off.max()) <= 0, f"{where}: {float(off.max())} past its bound at {divmod(int(off.argmax()), got.shape[-1])}"
+
+
+def grad(q, k, v, dout, row_off, key_off=None, scale=0.0, causal=True):
+    """(dq, dk, dv and the bounds of each without its last rounding) in float64, from the formulas.
+
+    The bounds. p is exp of a score less lse, both off (d and attend()'s bound of lse): e; it is rounded to the
+    inputs' type (u; f16: held 2^14 times as large, 2^-39 may be lost) for dv. ds = p (dP - delta): dP is a sum of dim fp32
+    products, delta comes from an out that is off and rounded; ds is rounded (f16: within 2^-25 of 2^14
+    times what is at least a quarter of its bound |dO||V| + |delta|, so 2^-37 of that may be lost). Sums are in fp32, 16 terms at
+    a time.
+    """
+    u, f64, f16 = UNIT[q.dtype], torch.float64, q.dtype == torch.float16
+    key_off = row_off if key_off is None else key_off
+    rows, H, D = q.shape
+    G = H // k.shape[1]
+    sc = scale or 1.0 / math.sqrt(D)
+    out, lse, out_tol, lse_tol = attend(q, k, v, row_off, key_off, scale, causal)
+    res = [torch.zeros(x.shape, dtype=f64, device=q.device) for x in (q, k, v)]
+    tol = [torch.zeros_like(x) for x in res]
+    for i in range(len(row_off) - 1):
+        a, b = slice(row_off[i], row_off[i + 1]), slice(key_off[i], key_off[i + 1])
+        r, m = a.stop - a.start, b.stop - b.start
+        if r == 0 or m == 0:
+            continue
+        see = torch.ones((r, m), dtype=torch.bool, device=q.device)
+        if causal:
+            see = see.tril(m - r)
+        add = (r * G / 8 + m / 8 + 32) * 2.0 ** -23
+        for h in range(H):
+            Q, K, V, dO = q[a, h].double(), k[b, h // G].double(), v[b, h // G].double(), dout[a, h].double()
+            O, L = out[a, h], lse[a, h][:, None]
+            p = torch.where(see, torch.exp((Q @ K.T) * sc - torch.where(L == -math.inf, 0.0, L)), 0.0)
+            delta = (dO * O).sum(-1, keepdim=True)
+            g = torch.where(see, dO @ V.T - delta, 0.0)
+            ds = p * g
+            res[0][a, h] = sc * (ds @ K)
+            res[1][b, h // G] += sc * (ds.T @ Q)
+            res[2][b, h // G] += p.T @ dO
+            mass = (Q.abs() @ K.abs().T * sc).amax(-1, keepdim=True)
+            e = 2 * ((D + 8) * 2.0 ** -23 * mass + 2.0 ** -20 + lse_tol[a, h][:, None] + 2.0 ** -22 * torch.where(L == -math.inf, 0.0, L).abs())
+            p_err = torch.where(see, p * (u + e) + (2.0 ** -39 if f16 else 0.0), 0.0)
+            dp_err = (D + 8) * 2.0 ** -23 * (dO.abs() @ V.abs().T)
+            delta_err = (dO.abs() * (u * O.abs() + (1 + u) * out_tol[a, h])).sum(-1, keepdim=True) + (D + 8) * 2.0 ** -24 * (dO * O).abs().sum(-1, keepdim=True)
+            bound = dO.norm(dim=-1).max() * V.norm(dim=-1).max() + delta.abs().max()
+            # (the group's other heads share the power of two: at most the largest of their bounds)
+            for h2 in range(h // G * G, h // G * G + G) if f16 else ():
+                d2 = dout[a, h2].double()
+                bound = torch.maximum(bound, d2.norm(dim=-1).max() * V.norm(dim=-1).max() + (d2 * out[a, h2]).sum(-1).abs().max())
+            ds_err = torch.where(see, p * ((u + 2 * e) * g.abs() + (1 + u) * (dp_err + delta_err)) + (2.0 ** -36 * bound if f16 else 0.0), 0.0)
+            tol[0][a, h] = sc * (ds_err @ K.abs()) + add * sc * (ds.abs() @ K.abs())
+            tol[1][b, h // G] += sc * (ds_err.T @ Q.abs()) + add * sc * (ds.abs().T @ Q.abs())
+            tol[2][b, h // G] += p_err.T @ dO.abs() + add * (p.T @ dO.abs())
+    return (*res, *tol)

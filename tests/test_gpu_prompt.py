@@ -45,7 +45,7 @@ def inputs(rows, keys, H, Hkv, D, dtype, seed=0, gain=1.5, fused=False, first=0,
 
 def check(q, k, v, off, koff=None, scale=0.0, causal=True, where=""):
     import paper_2605_29657_gb300 as occ
-    ws = occ.alloc_prompt_workspace(q.shape[0], q.shape[1])
+    ws = occ.alloc_prompt_workspace(q.shape[0], q.shape[1], k.shape[0], k.shape[1])
     out = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda")
     lse = torch.full(q.shape[:2], 7.0, device="cuda")
     occ.occam_prompt_attend(q, k, v, dev(off), ws, key_off=None if koff is None else dev(koff), scale=scale, causal=causal, out=out,
