@@ -68,7 +68,7 @@ struct Step {
 };
 
 struct Shared {
-  uint64_t q_full, k_full[2], k_free[2], v_full[2], v_free[2], s_full[2][2], p_full[2][2], o_done[2][2], step_full[kRing],
+  uint64_t q_full[2], k_full[2], k_free[2], v_full[2], v_free[2], s_full[2][2], p_full[2][2], o_done[2][2], step_full[kRing],
       step_free[kRing], raw_full[2], raw_free[2], meet, drain;
   Step step[kRing];
   Line line;
@@ -319,8 +319,16 @@ __device__ __forceinline__ void plan_role(const P& p, Shared& sh, const CUtensor
   if (!walk_begin<kR, kK, kOver>(p, sh, x)) return;
   Plan f(p, x, lane);
   uint32_t n = 0, j = 0;  // step records, steps so far
-  for (bool again = true; again;) {
+  uint32_t seg = 0;
+  for (bool again = true; again; ++seg) {
     f.item(first_page(p, x.s));
+    // The notes of four segments ago: a segment has two records at least, so every row tile has given back that one's last.
+    if (sh.any_nan[seg & 3]) {
+      for (int d = lane; d < D; d += 32) sh.nan_first[seg & 3][d] = 0x7fffffff;
+      __syncwarp();
+      if (lane == 0) sh.any_nan[seg & 3] = 0;
+      __syncwarp();
+    }
     const int common = p.causal ? x.s.len - x.s.rows + div_group(p, x.rt * kR) + 1 : x.s.len;
     const int end = x.tb - 1, tiles2 = row_tiles(p, x);
     float rho = 0.f, rho_max = 0.f;
@@ -491,8 +499,8 @@ __device__ __forceinline__ void mma_role(const AttendParams& p, Shared& sh, uint
   const uint64_t dq = desc_kmajor(q_smem + t * kBytes), dk = desc_kmajor(k_smem), dv = desc_mnmajor(v_smem);
   uint32_t n = 0, j = 0, it = 0;  // step records, steps, steps of this row tile
   int end = 0;
-  for (uint32_t seg = 0; end != 2; ++seg) {
-    TC_WAIT(sh.q_full, seg & 1);
+  uint32_t queries = 0;  // segments of this row tile
+  while (end != 2) {
     bool mine = true;
     end = 0;
     // Pass k: by halves h, O += P V of step k - 1, then S of step k in the place of that P.
@@ -523,6 +531,10 @@ __device__ __forceinline__ void mma_role(const AttendParams& p, Shared& sh, uint
           end = sh.step[n % kRing].end;
           if (!end) {
             mine = t < sh.step[n % kRing].row_tiles;
+            if (k == 0 && mine) {
+              TC_WAIT(sh.q_full[t], queries & 1);
+              ++queries;
+            }
             TC_WAIT(sh.k_full[j & 1], (j >> 1) & 1);
             tc::fence_after();
           }
@@ -649,7 +661,8 @@ __device__ __forceinline__ void softmax_role(const P& p, Shared& sh, unsigned ch
     float qscale = 0.f;
     if (mine) qscale = load_queries<D, BF16>(p, x, row & ~31, q_smem + t * kK * D * 2, lane);
     tc::fence_proxy_async();
-    tc::bar_arrive(&sh.q_full);
+    // (a barrier a row tile: the warps of one that has no rows in these segments are ahead of the other's)
+    if (mine) tc::bar_arrive(&sh.q_full[t]);
     const int limit = !there ? 0 : p.causal ? x.s.len - x.s.rows + div_group(p, at) + 1 : x.s.len;  // keys this row sees
     const int common = p.causal ? x.s.len - x.s.rows + div_group(p, x.rt * kR + t * 128) + 1 : x.s.len;
     float ref = -INFINITY, top = -INFINITY, l = 0.f, rho = 0.f;
@@ -750,10 +763,10 @@ __device__ __forceinline__ void softmax_role(const P& p, Shared& sh, unsigned ch
           tc::bar_arrive(&sh.p_full[t][h]);
         }
       }
+      if (end) break;
       __syncwarp();
       if (lane == 0) tc::bar_arrive(&sh.step_free[n % kRing]);
       ++n;
-      if (end) break;
     }
 
     // the row's result
@@ -964,14 +977,10 @@ __device__ __forceinline__ void softmax_role(const P& p, Shared& sh, unsigned ch
         }
       }
     }
-    // The notes of the segment before are cleared: its other row tile has read
-    // them (it came to this segment's products), and the converting warps, two tiles ahead
-    // at most, are not yet three segments on.
-    const uint32_t old = (seg + 3) & 3;
-    if (t == 0 && sh.any_nan[old]) {
-      if (r < D) sh.nan_first[old][r] = 0x7fffffff;
-      __syncwarp();
-    }
+    // (the segment's last record is given back once its notes have been read)
+    __syncwarp();
+    if (lane == 0) tc::bar_arrive(&sh.step_free[n % kRing]);
+    ++n;
     ++seg;
   } while (walk_next<kR, kK, kOver>(p, sh, x));
 }
@@ -1027,10 +1036,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     sh.row_tile = w.row_tile;
     sh.in_item = w.in_item;
     sh.stop = 0;
-    tc::bar_init(&sh.q_full, 256);
     tc::bar_init(&sh.meet, 256);
     tc::bar_init(&sh.drain, 2);
     for (int k = 0; k < 2; ++k) {
+      tc::bar_init(&sh.q_full[k], 128);
       tc::bar_init(&sh.k_full[k], 128);
       tc::bar_init(&sh.v_full[k], 128);
       tc::bar_init(&sh.k_free[k], 2);
