@@ -513,7 +513,7 @@ int occam_cache_append(const occam_cache* cache, int32_t layer, int32_t dtype, i
                        int64_t k_row, const void* v, int64_t v_row, int32_t n, const int32_t* seqs,
                        const int64_t* row_off, void* workspace, size_t workspace_bytes, occam_stream_t stream);
 
-/* occam_cache_append with occam_rope on the way, in one launch. Keys (not values) are turned by
+/* occam_cache_append with occam_rope on the way. Keys (not values) are turned by
  * their rows' positions as in occam_rope (rot, pairing, positions, inv_freq and
  * axis as there, rot <= dim); the turned keys stay in fp32 until they are rounded to codes, once. q (NULL:
  * none): queries of the same rows, turned to q->dst (every row of total_rows, whatever

@@ -2,12 +2,11 @@
 // the way into the paged 8-bit cache, values beside them, and the queries turned in the
 // same launch.
 //
-// A CTA of the first part takes one touched page and some heads of K or of V. Cosines
-// and sines of the page's tokens are computed once, into shared memory, and serve all its
-// heads of K; the turned values stay in registers as fp32 between the block's maximum and the
-// rounding, so keys are rounded once, to their codes. CTAs of the second part turn
-// the queries (rope_rows). Bound by HBM: queries 2 bytes read and written, keys and values 2 read and 1
-// written a value.
+// A CTA takes one touched page and some heads of K or of V. Cosines and sines of the page's
+// tokens are computed once, into shared memory, and serve all its heads of K; the turned values stay
+// in registers as fp32 between the block's maximum and the rounding, so keys are rounded once, to their
+// codes. The queries are turned by a launch of their own (rope_rows) that starts while this one ends. Bound by HBM:
+// queries 2 bytes read and written, keys and values 2 read and 1 written a value.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -16,6 +15,7 @@
 #include "nvtx.cuh"
 #include "overlap.cuh"
 #include "rope.cuh"
+#include "tc5.cuh"
 
 using namespace occam;
 
@@ -25,12 +25,9 @@ constexpr int kThreads = 256;
 
 struct EnterParams {
   AppendParams a;
-  RopeParams q;          // rows, angles and the queries (t[0]; no heads: none)
+  RopeParams q;          // rows and angles; the queries are t[0]
   int k_heads, v_heads;  // heads a CTA takes of K, of V
   int k_parts, parts;    // CTAs a page for K; in all
-  int64_t slots;
-  int64_t kv_ctas;
-  int64_t q_blocks;      // CTAs of a head group of the queries
 };
 
 template <int V>
@@ -51,56 +48,56 @@ struct Raw<1> {
   static constexpr int kWords = 1;
 };
 template <bool BF16, int V>
-__device__ __forceinline__ void unpack(const Raw<V>& r, float (&x)[V]) {
+__device__ __forceinline__ void unpack(const Raw<V>& r, float* x) {
   if constexpr (V == 1) {
     x[0] = BF16 ? __uint_as_float((uint32_t)r.w << 16) : __half2float(__ushort_as_half(r.w));
   } else {
     const uint32_t* w = reinterpret_cast<const uint32_t*>(&r.w);
 #pragma unroll
     for (int i = 0; i < V / 2; ++i) {
-      if (BF16) {
-        x[2 * i] = bf16_lo(w[i]);
-        x[2 * i + 1] = bf16_hi(w[i]);
-      } else {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-        x[2 * i] = f.x;
-        x[2 * i + 1] = f.y;
-      }
+      const float2 f = BF16 ? make_float2(bf16_lo(w[i]), bf16_hi(w[i])) : __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      x[2 * i] = f.x;
+      x[2 * i + 1] = f.y;
     }
   }
 }
-// V values to codes at `to`; scales that are no power of two come only with a cache whose scales the caller made
+__device__ __forceinline__ float2 at2(const float* x) { return make_float2(x[0], x[1]); }
+// V values to codes at `to`
 template <int V>
-__device__ __forceinline__ void put_codes(uint8_t* to, const float* x, float scale, float inv, bool exact) {
-  float y[V < 4 ? 4 : V];
-#pragma unroll
-  for (int i = 0; i < (V < 4 ? 4 : V); ++i) y[i] = i < V ? (exact ? x[i] * inv : x[i] / scale) : 0.f;
+__device__ __forceinline__ void put_codes(uint8_t* to, const float* x) {
   if constexpr (V == 8) {
-    const float lo[4] = {y[0], y[1], y[2], y[3]}, hi[4] = {y[4], y[5], y[6], y[7]};
+    const float lo[4] = {x[0], x[1], x[2], x[3]}, hi[4] = {x[4], x[5], x[6], x[7]};
     *reinterpret_cast<uint2*>(to) = make_uint2(f32_codes4(lo), f32_codes4(hi));
+  } else if constexpr (V == 4) {
+    const float lo[4] = {x[0], x[1], x[2], x[3]};
+    *reinterpret_cast<uint32_t*>(to) = f32_codes4(lo);
   } else {
-    const float lo[4] = {y[0], y[1], y[2], y[3]};
-    if constexpr (V == 4)
-      *reinterpret_cast<uint32_t*>(to) = f32_codes4(lo);
-    else
-      *to = (uint8_t)f32_codes4(lo);
+    *to = (uint8_t)f32x2_e4m3x2(x[0], 0.f);
   }
+}
+// (a scale that is no power of two comes only with a cache whose scales the caller made: kept out of the way of the others)
+__device__ __noinline__ float divide(float x, float s) { return x / s; }
+
+// Bytes of two heads' rows on their way, each thread its own
+template <int V, int NU>
+constexpr int kRingBytes = V > 1 ? 2 * NU * 2 * kThreads * V * 2 : 0;
+template <int V>
+__device__ __forceinline__ void copy_async(Raw<V>* to, const uint16_t* from) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_u32(to)), "l"(from), "n"(V * 2) : "memory");
 }
 
 // V: values of a vector; a unit is two vectors (of pairs, or side by side where nothing is turned). NU: units a
 // thread holds of a block at most.
 template <bool BF16, int D, int V, bool ADJ, int NU>
-__global__ void __launch_bounds__(kThreads) enter_kernel(EnterParams e) {
-  using E = typename std::conditional<BF16, __nv_bfloat16, __half>::type;
-  extern __shared__ __align__(16) float2 turn[];  // [tokens][pairs]
+__global__ void __launch_bounds__(kThreads, NU * V <= 16 ? 3 : 1) enter_kernel(EnterParams e) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  Raw<V>* ring = reinterpret_cast<Raw<V>*>(smem) + threadIdx.x;  // [heads by turns][unit][its two vectors][thread]
+  // cosines and sines [tokens][pairs], by two pairs (c, c, s, s) where pairs of vectors are turned at once, else (c, s)
+  float* turn = reinterpret_cast<float*>(smem + kRingBytes<V, NU>);
+  constexpr bool TWO = V > 1 && !ADJ;
   __shared__ float sh_max[2][kThreads / 32];
   pdl_wait();
-  if ((int64_t)blockIdx.x >= e.kv_ctas) {
-    const int64_t b = (int64_t)blockIdx.x - e.kv_ctas;
-    const int group = (int)(b / e.q_blocks);
-    rope_rows<E, V, ADJ>(e.q, (b - group * e.q_blocks) * kThreads + threadIdx.x, group);
-    return;
-  }
+  pdl_trigger();  // the queries' launch may begin
   const AppendParams& p = e.a;
   const int64_t w = (int64_t)blockIdx.x / e.parts;
   const int part = (int)((int64_t)blockIdx.x - w * e.parts);
@@ -138,69 +135,91 @@ __global__ void __launch_bounds__(kThreads) enter_kernel(EnterParams e) {
   const int h0 = is_k ? part * e.k_heads : (part - e.k_parts) * e.v_heads;
   const int h1 = min(h0 + (is_k ? e.k_heads : e.v_heads), H);
 
-  constexpr int UPR = D / (2 * V);  // units of a row
-  const int half = e.q.half, turned = is_k ? half / V : 0, units = (t1 - t0) * UPR;
-  // this thread's units: token and places of the two vectors
-  auto places = [&](int n, int& tok, int& d0, int& d1, int& pair) {
-    const int x = n * kThreads + threadIdx.x, u = x % UPR;
-    tok = x / UPR;
-    pair = u < turned ? u * V : -1;
-    d0 = pair >= 0 && !ADJ ? V * u : 2 * V * u;
-    d1 = pair >= 0 && !ADJ ? d0 + half : d0 + V;
-  };
-  Raw<V> raw[NU][2];
-  auto load = [&](int h) {
+  constexpr int UPR = D / (2 * V), STEP = kThreads / UPR;  // units of a row; rows between a thread's units
+  const int half = e.q.half, rows = t1 - t0;
+  // this thread's units: rows tok0, tok0 + STEP, ..; places of the two vectors; the first pair (-1: not turned)
+  const int u = threadIdx.x % UPR, tok0 = threadIdx.x / UPR;
+  const int pair = is_k && u < half / V ? u * V : -1;
+  const int d0 = pair >= 0 && !ADJ ? V * u : 2 * V * u, d1 = pair >= 0 && !ADJ ? d0 + half : d0 + V;
+  // A head's rows come by asynchronous copies, two heads ahead of the one in hand (single values of 2 bytes by loads).
+  auto held = [&](int h, int n, int which) { return ring + (((h & 1) * NU + n) * 2 + which) * kThreads; };
+  auto fetch = [&](int h) {
+    if constexpr (V > 1) {
+      if (h < h1) {
+        const uint16_t* from = src + tok0 * ld + h * D;
 #pragma unroll
-    for (int n = 0; n < NU; ++n) {
-      if (n * kThreads + (int)threadIdx.x < units) {
-        int tok, d0, d1, pair;
-        places(n, tok, d0, d1, pair);
-        raw[n][0] = *reinterpret_cast<const Raw<V>*>(src + tok * ld + h * D + d0);
-        raw[n][1] = *reinterpret_cast<const Raw<V>*>(src + tok * ld + h * D + d1);
+        for (int n = 0; n < NU; ++n)
+          if (tok0 + n * STEP < rows) {
+            copy_async<V>(held(h, n, 0), from + n * STEP * ld + d0);
+            copy_async<V>(held(h, n, 1), from + n * STEP * ld + d1);
+          }
       }
+      cp_async_commit();
     }
   };
-  load(h0);
+  fetch(h0);
+  fetch(h0 + 1);
   if (is_k) {
-    for (int x = threadIdx.x; x < (t1 - t0) * half; x += kThreads) {
-      const int tok = x / half, pair = x - tok * half;
-      int ax = e.q.axis[pair];
+    for (int x = threadIdx.x; x < rows * half; x += kThreads) {
+      const int tok = x / half, i = x - tok * half;
+      int ax = e.q.axis[i];
       ax = (unsigned)ax < (unsigned)e.q.axes ? ax : 0;
-      rope_angle((float)e.q.pos[ax * e.q.pos_stride + row0 + tok], e.q.freq[pair], turn[x].x, turn[x].y);
+      float* to = turn + 2 * (TWO ? x & ~1 : x) + (TWO ? x & 1 : 0);
+      rope_angle((float)e.q.pos[ax * e.q.pos_stride + row0 + tok], e.q.freq[i], to[0], to[TWO ? 2 : 1]);
     }
     __syncthreads();
   }
   for (int h = h0; h < h1; ++h) {
     float x[NU][2 * V];
     float amax = 0.f;
+    if constexpr (V > 1) cp_async_wait<1>();
 #pragma unroll
     for (int n = 0; n < NU; ++n) {
-      if (n * kThreads + (int)threadIdx.x < units) {
-        int tok, d0, d1, pair;
-        places(n, tok, d0, d1, pair);
-        float a[V], b[V];
-        unpack<BF16, V>(raw[n][0], a);
-        unpack<BF16, V>(raw[n][1], b);
-        if (pair >= 0) {
+      if (tok0 + n * STEP >= rows) continue;
+      if constexpr (V > 1) {
+        unpack<BF16, V>(*held(h, n, 0), x[n]);
+        unpack<BF16, V>(*held(h, n, 1), x[n] + V);
+      } else {
+        const uint16_t* from = src + (tok0 + n * STEP) * ld + h * D;
+        unpack<BF16, V>(Raw<V>{from[d0]}, x[n]);
+        unpack<BF16, V>(Raw<V>{from[d1]}, x[n] + V);
+      }
+      if (pair >= 0) {
+        const float* cs = turn + 2 * ((tok0 + n * STEP) * half + pair);
+        if constexpr (TWO) {
+#pragma unroll
+          for (int k = 0; k < V; k += 2) {
+            const float4 t = *reinterpret_cast<const float4*>(cs + 2 * k);
+            const float2 c = make_float2(t.x, t.y), sn = make_float2(t.z, t.w), y = at2(x[n] + k), z = at2(x[n] + V + k);
+            const float2 e0 = tc::fma2(z, make_float2(-sn.x, -sn.y), tc::mul2(y, c)), e1 = tc::fma2(z, c, tc::mul2(y, sn));
+            x[n][k] = e0.x;
+            x[n][k + 1] = e0.y;
+            x[n][V + k] = e1.x;
+            x[n][V + k + 1] = e1.y;
+          }
+        } else {
 #pragma unroll
           for (int k = 0; k < V; ++k) {
-            const float2 cs = turn[tok * half + pair + k];
-            float& e0 = ADJ ? (2 * k < V ? a[(2 * k) % V] : b[(2 * k) % V]) : a[k];
-            float& e1 = ADJ ? (2 * k + 1 < V ? a[(2 * k + 1) % V] : b[(2 * k + 1) % V]) : b[k];
-            const float y = e0, z = e1;
-            e0 = fmaf(y, cs.x, -__fmul_rn(z, cs.y));  // (as in rope_rows)
-            e1 = fmaf(z, cs.x, __fmul_rn(y, cs.y));
+            float& e0 = x[n][ADJ ? 2 * k : k];
+            float& e1 = x[n][ADJ ? 2 * k + 1 : V + k];
+            const float c = cs[2 * k], sn = cs[2 * k + 1], y = e0, z = e1;
+            e0 = fmaf(y, c, -__fmul_rn(z, sn));
+            e1 = fmaf(z, c, __fmul_rn(y, sn));
           }
         }
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-          amax = fmaxf(amax, fmaxf(finite_abs(a[k]), finite_abs(b[k])));
-          x[n][k] = a[k];
-          x[n][V + k] = b[k];
-        }
       }
+#pragma unroll
+      for (int k = 0; k < 2 * V; k += 2) amax = tc::fmax3(amax, fabsf(x[n][k]), fabsf(x[n][k + 1]));  // (passes over NaN)
     }
-    if (h + 1 < h1) load(h + 1);  // (under way during the maximum and the rounding)
+    fetch(h + 2);  // (in the place of what this thread has just read)
+    if (amax == INFINITY) {  // the largest finite value counts
+      amax = 0.f;
+#pragma unroll
+      for (int n = 0; n < NU; ++n)
+        if (tok0 + n * STEP < rows)
+#pragma unroll
+          for (int k = 0; k < 2 * V; ++k) amax = fmaxf(amax, finite_abs(x[n][k]));
+    }
     amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));
     float* r = sh_max[h & 1];
     if ((threadIdx.x & 31) == 0) r[threadIdx.x >> 5] = amax;
@@ -231,54 +250,73 @@ __global__ void __launch_bounds__(kThreads) enter_kernel(EnterParams e) {
     }
     const bool exact = is_pow2(now);
     const float inv = 1.f / now;
+    uint8_t* to = codes + (t0 + tok0) * D;
 #pragma unroll
     for (int n = 0; n < NU; ++n) {
-      if (n * kThreads + (int)threadIdx.x < units) {
-        int tok, d0, d1, pair;
-        places(n, tok, d0, d1, pair);
-        uint8_t* to = codes + (t0 + tok) * D;
-        put_codes<V>(to + d0, x[n], now, inv, exact);
-        put_codes<V>(to + d1, x[n] + V, now, inv, exact);
+      if (tok0 + n * STEP >= rows) continue;
+      if (exact) {
+#pragma unroll
+        for (int k = 0; k < 2 * V; k += 2) {
+          const float2 y = tc::mul2(at2(x[n] + k), make_float2(inv, inv));
+          x[n][k] = y.x;
+          x[n][k + 1] = y.y;
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 2 * V; ++k) x[n][k] = divide(x[n][k], now);
       }
+      put_codes<V>(to + n * STEP * D + d0, x[n]);
+      put_codes<V>(to + n * STEP * D + d1, x[n] + V);
     }
     if (threadIdx.x == 0) *scale = now;
   }
 }
 
 template <bool BF16, int D, int V, bool ADJ, int NU>
-int launch_units(const EnterParams& e, cudaStream_t st) {
+int launch_units(const EnterParams& e, int64_t grid, cudaStream_t st) {
   const int64_t tokens = std::min<int64_t>(e.a.c.T, e.a.total_rows);
-  const size_t smem = (size_t)tokens * e.q.half * sizeof(float2);
-  if (smem > 48 * 1024) {
-    static std::atomic<uint64_t> ready{0};  // devices whose shared memory limit is raised
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return OCCAM_ERR_CUDA;
-    if (!((ready.load(std::memory_order_acquire) >> dev) & 1)) {
-      if (cudaFuncSetAttribute(enter_kernel<BF16, D, V, ADJ, NU>, cudaFuncAttributeMaxDynamicSharedMemorySize, 128 * 64 * 8) != cudaSuccess)
-        return OCCAM_ERR_CUDA;
-      ready.fetch_or(uint64_t(1) << dev, std::memory_order_release);
-    }
+  const size_t smem = kRingBytes<V, NU> + (size_t)tokens * e.q.half * sizeof(float2);
+  static std::atomic<uint64_t> ready{0};  // devices whose shared memory limit is raised
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return OCCAM_ERR_CUDA;
+  if (!((ready.load(std::memory_order_acquire) >> dev) & 1)) {
+    if (cudaFuncSetAttribute(enter_kernel<BF16, D, V, ADJ, NU>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             kRingBytes<V, NU> + 128 * (D / 2) * 8) != cudaSuccess)
+      return OCCAM_ERR_CUDA;
+    ready.fetch_or(uint64_t(1) << dev, std::memory_order_release);
   }
-  const int64_t groups = e.q.t[0].heads > 0 ? e.q.groups0 : 0;
-  const int64_t grid = e.kv_ctas + groups * e.q_blocks;
-  if (grid > 0x7fffffff) return OCCAM_ERR_UNSUPPORTED;
-  return launch_after(enter_kernel<BF16, D, V, ADJ, NU>, dim3((unsigned)grid), kThreads, smem, st, e) && cudaGetLastError() == cudaSuccess
-             ? OCCAM_OK
-             : OCCAM_ERR_CUDA;
+  return launch_after(enter_kernel<BF16, D, V, ADJ, NU>, dim3((unsigned)grid), kThreads, smem, st, e) ? OCCAM_OK : OCCAM_ERR_CUDA;
+}
+
+// The queries. Behind a launch for K and V (BEHIND) they need nothing of it but that it is done when they are: what came
+// before it was complete when it let this launch begin.
+template <bool BF16, int V, bool ADJ, bool BEHIND>
+__global__ void __launch_bounds__(kThreads) queries_kernel(RopeParams p) {
+  using E = typename std::conditional<BF16, __nv_bfloat16, __half>::type;
+  if (!BEHIND) pdl_wait();
+  rope_rows<E, V, ADJ>(p, (int64_t)blockIdx.x * kThreads + threadIdx.x, blockIdx.y);
+  if (BEHIND) pdl_wait();
 }
 
 template <bool BF16, int D, int V, bool ADJ>
-int launch_pairing(const EnterParams& e, cudaStream_t st) {
-  // units of a block a thread: page_tokens * D / (2 V) / 256
-  constexpr int U64 = std::max(64 * D / (2 * V * kThreads), 1);
-  return e.a.c.T <= 64 ? launch_units<BF16, D, V, ADJ, U64>(e, st) : launch_units<BF16, D, V, ADJ, 2 * U64>(e, st);
+int launch_pairing(const EnterParams& e, int64_t grid, dim3 q_grid, cudaStream_t st) {
+  if (grid > 0x7fffffff) return OCCAM_ERR_UNSUPPORTED;
+  if (grid > 0) {
+    // units of a block a thread: page_tokens * D / (2 V) / 256
+    constexpr int U64 = std::max(64 * D / (2 * V * kThreads), 1);
+    const int rc = e.a.c.T <= 64 ? launch_units<BF16, D, V, ADJ, U64>(e, grid, st) : launch_units<BF16, D, V, ADJ, 2 * U64>(e, grid, st);
+    if (rc != OCCAM_OK) return rc;
+  }
+  const bool ok = e.q.t[0].heads == 0 || (grid > 0 ? launch_after(queries_kernel<BF16, V, ADJ, true>, q_grid, kThreads, 0, st, e.q)
+                                                   : launch_after(queries_kernel<BF16, V, ADJ, false>, q_grid, kThreads, 0, st, e.q));
+  return ok && cudaGetLastError() == cudaSuccess ? OCCAM_OK : OCCAM_ERR_CUDA;
 }
 
 template <bool BF16, int D>
-int launch_dim(const EnterParams& e, int v, bool adj, cudaStream_t st) {
-  if (v == 8) return adj ? launch_pairing<BF16, D, 8, true>(e, st) : launch_pairing<BF16, D, 8, false>(e, st);
-  if (v == 4) return adj ? launch_pairing<BF16, D, 4, true>(e, st) : launch_pairing<BF16, D, 4, false>(e, st);
-  return adj ? launch_pairing<BF16, D, 1, true>(e, st) : launch_pairing<BF16, D, 1, false>(e, st);
+int launch_dim(const EnterParams& e, int v, bool adj, int64_t grid, dim3 q, cudaStream_t st) {
+  if (v == 8) return adj ? launch_pairing<BF16, D, 8, true>(e, grid, q, st) : launch_pairing<BF16, D, 8, false>(e, grid, q, st);
+  if (v == 4) return adj ? launch_pairing<BF16, D, 4, true>(e, grid, q, st) : launch_pairing<BF16, D, 4, false>(e, grid, q, st);
+  return adj ? launch_pairing<BF16, D, 1, true>(e, grid, q, st) : launch_pairing<BF16, D, 1, false>(e, grid, q, st);
 }
 
 }  // namespace
@@ -351,24 +389,26 @@ extern "C" int occam_cache_append_rope(const occam_cache* cache, const occam_app
   // the widest vector that divides the turned and the copied part and that every address is a multiple of
   int v = 8;
   while (v > 1 && (e.q.half % v || (dim - a->rot) % (2 * v) || (bits & (2 * v - 1)))) v = v == 8 ? 4 : 1;
-  // Heads a CTA: as many as leave four CTAs an SM (K: up to 8 share a page's cosines and sines).
+  // Heads a CTA: as many as leave four CTAs an SM (K: up to 16 share a page's cosines and sines).
   const int64_t sms = cache_sms();
-  e.slots = a->n > 0 ? (a->total_rows >> e.a.c.log2T) + 2 * (int64_t)a->n : 0;
+  const int64_t slots = a->n > 0 ? (a->total_rows >> e.a.c.log2T) + 2 * (int64_t)a->n : 0;
   auto share = [&](int64_t ctas, int heads, int most) {
     return (int)std::max<int64_t>(1, std::min<int64_t>({ctas * heads / (sms * 4), (int64_t)heads, (int64_t)most}));
   };
-  e.k_heads = share(e.slots, cache->heads, 8);
-  e.v_heads = share(e.slots, cache->heads, 4);
+  e.k_heads = share(slots, cache->heads, 16);
+  e.v_heads = share(slots, cache->heads, 4);
   e.k_parts = (cache->heads + e.k_heads - 1) / e.k_heads;
   e.parts = e.k_parts + (cache->heads + e.v_heads - 1) / e.v_heads;
-  e.kv_ctas = e.slots * e.parts;
-  const int64_t units = dim / (2 * v);
-  e.q_blocks = (a->total_rows * units + kThreads - 1) / kThreads;
   // queries: enough threads to fill the GPU first, then as many heads a thread as amortise the sines
-  e.q.hpt = share(e.q_blocks * 2, std::max(e.q.t[0].heads, 1), kMostHeads);
-  e.q.groups0 = (e.q.t[0].heads + e.q.hpt - 1) / e.q.hpt;
+  const int64_t q_blocks = (a->total_rows * (dim / (2 * v)) + kThreads - 1) / kThreads;
+  const int q_heads = std::max(e.q.t[0].heads, 1);
+  if (q_blocks > 0x7fffffff) return OCCAM_ERR_UNSUPPORTED;
+  e.q.hpt = (int)std::max<int64_t>(std::min<int64_t>({q_blocks * q_heads / (sms * 8), (int64_t)q_heads, (int64_t)kMostHeads}), 1);
+  e.q.groups0 = (q_heads + e.q.hpt - 1) / e.q.hpt;
+  if (e.q.groups0 > 65535) return OCCAM_ERR_UNSUPPORTED;
+  const dim3 q_grid((unsigned)q_blocks, (unsigned)e.q.groups0);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const bool adj = a->pairing == OCCAM_ROPE_ADJACENT, bf16 = a->dtype == OCCAM_BF16;
-  if (dim == 128) return bf16 ? launch_dim<true, 128>(e, v, adj, st) : launch_dim<false, 128>(e, v, adj, st);
-  return bf16 ? launch_dim<true, 64>(e, v, adj, st) : launch_dim<false, 64>(e, v, adj, st);
+  if (dim == 128) return bf16 ? launch_dim<true, 128>(e, v, adj, slots * e.parts, q_grid, st) : launch_dim<false, 128>(e, v, adj, slots * e.parts, q_grid, st);
+  return bf16 ? launch_dim<true, 64>(e, v, adj, slots * e.parts, q_grid, st) : launch_dim<false, 64>(e, v, adj, slots * e.parts, q_grid, st);
 }

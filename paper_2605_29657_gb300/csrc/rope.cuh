@@ -57,8 +57,9 @@ __device__ __forceinline__ void rope_angle(float x, float f, float& c, float& s)
   s = fmaf(ch, e, sh);
 }
 
-// Thread `at` of (row, unit of 2V values), head group `group` of both tensors
-template <typename E, int V, bool ADJ>
+// Thread `at` of (row, unit of 2V values), head group `group` of both tensors. AHEAD heads' loads are in flight together
+// (by default: two of 16-bit values cost occam_rope more registers than they gain).
+template <typename E, int V, bool ADJ, int AHEAD = sizeof(E) == 4 ? 2 : 1>
 __device__ __forceinline__ void rope_rows(const RopeParams& p, int64_t at, int group) {
   using VecT = Vec<E, V>;
   const int units = p.dim / (2 * V), turn = p.half / V;
@@ -99,19 +100,17 @@ __device__ __forceinline__ void rope_rows(const RopeParams& p, int64_t at, int g
       }
     }
   };
-  // kAhead heads' loads are in flight together (two of 16-bit values cost more registers than they gain)
-  constexpr int kAhead = sizeof(E) == 4 ? 2 : 1;
-  for (int h = h0; h < h1; h += kAhead) {
-    VecT v0[kAhead], v1[kAhead];
+  for (int h = h0; h < h1; h += AHEAD) {
+    VecT v0[AHEAD], v1[AHEAD];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k)
+    for (int k = 0; k < AHEAD; ++k)
       if (h + k < h1) {
         const E* from = src + (h + k) * t.src_head;
         v0[k] = *reinterpret_cast<const VecT*>(from + d0);
         v1[k] = *reinterpret_cast<const VecT*>(from + d1);
       }
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k)
+    for (int k = 0; k < AHEAD; ++k)
       if (h + k < h1) {
         E* to = dst + (h + k) * t.dst_head;
         turn_pair(v0[k], v1[k]);
