@@ -78,21 +78,25 @@ __device__ __forceinline__ void put_codes(uint8_t* to, const float* x) {
 // (a scale that is no power of two comes only with a cache whose scales the caller made: kept out of the way of the others)
 __device__ __noinline__ float divide(float x, float s) { return x / s; }
 
-// Bytes of two heads' rows on their way, each thread its own
+// Bytes of a head's rows on their way, each thread its own
 template <int V, int NU>
-constexpr int kRingBytes = V > 1 ? 2 * NU * 2 * kThreads * V * 2 : 0;
+constexpr int kRingBytes = V > 1 ? NU * 2 * kThreads * V * 2 : 0;
 template <int V>
 __device__ __forceinline__ void copy_async(Raw<V>* to, const uint16_t* from) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_u32(to)), "l"(from), "n"(V * 2) : "memory");
+  if constexpr (V == 8)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_u32(to)), "l"(from), "n"(V * 2) : "memory");
 }
 
 // V: values of a vector; a unit is two vectors (of pairs, or side by side where nothing is turned). NU: units a
 // thread holds of a block at most.
 template <bool BF16, int D, int V, bool ADJ, int NU>
-__global__ void __launch_bounds__(kThreads, NU * V <= 16 ? 3 : 1) enter_kernel(EnterParams e) {
+__global__ void __launch_bounds__(kThreads, NU * V <= 16 ? 4 : 2) enter_kernel(EnterParams e) {
   extern __shared__ __align__(16) unsigned char smem[];
-  Raw<V>* ring = reinterpret_cast<Raw<V>*>(smem) + threadIdx.x;  // [heads by turns][unit][its two vectors][thread]
-  // cosines and sines [tokens][pairs], by two pairs (c, c, s, s) where pairs of vectors are turned at once, else (c, s)
+  Raw<V>* ring = reinterpret_cast<Raw<V>*>(smem) + threadIdx.x;  // [unit][its two vectors][thread]
+  // Cosines and sines of each token: (c, s) a pair; where pairs are turned by twos (c, c, s, s), those that a row's
+  // threads read together next to one another.
   float* turn = reinterpret_cast<float*>(smem + kRingBytes<V, NU>);
   constexpr bool TWO = V > 1 && !ADJ;
   __shared__ float sh_max[2][kThreads / 32];
@@ -100,16 +104,43 @@ __global__ void __launch_bounds__(kThreads, NU * V <= 16 ? 3 : 1) enter_kernel(E
   pdl_trigger();  // the queries' launch may begin
   const AppendParams& p = e.a;
   const int64_t w = (int64_t)blockIdx.x / e.parts;
-  const int part = (int)((int64_t)blockIdx.x - w * e.parts);
+  // (by turns: blocks go to SMs round robin, and an SM that always got the parts of K would be last)
+  const int part = (int)((blockIdx.x + w) % e.parts);
   const bool is_k = part < e.k_parts;
   const int refused = p.c.status[1] & kRefused;  // (no CTA of this launch sets it)
   const int T = p.c.T, H = p.c.heads;
-  const int i = slot_sequence(p.row_off, p.n, p.c.log2T, w);
-  const int64_t r0 = p.row_off[i], r1 = p.row_off[i + 1];
-  const int64_t local = w - ((r0 >> p.c.log2T) + 2 * (int64_t)i);
-  const int seq = p.seqs[i];
-  int len = -1;
-  if ((unsigned)seq < (unsigned)p.c.max_seqs) len = p.c.length[seq];
+  // The slot's sequence. Up to 255 of them are looked at at once, with their lengths: two rounds of loads instead of six.
+  __shared__ struct {
+    int64_t r0, r1;
+    int i, seq, len;
+  } at;
+  if (p.n < kThreads) {
+    const int t = threadIdx.x;
+    const int64_t r = t <= p.n ? p.row_off[t] : 0;
+    const int mine = t < p.n ? p.seqs[t] : -1;
+    const int held = (unsigned)mine < (unsigned)p.c.max_seqs ? p.c.length[mine] : -1;
+    const int before = __syncthreads_count(t <= p.n && (r >> p.c.log2T) + 2 * (int64_t)t <= w);  // those that begin at or before it
+    const int found = min(max(before - 1, 0), p.n - 1);
+    if (t == found) {
+      at.r0 = r;
+      at.i = found;
+      at.seq = mine;
+      at.len = held;
+    }
+    if (t == found + 1) at.r1 = r;
+  } else if (threadIdx.x < 32) {
+    const int found = slot_sequence(p.row_off, p.n, p.c.log2T, w);
+    if (threadIdx.x == 0) {
+      at.r0 = p.row_off[found];
+      at.r1 = p.row_off[found + 1];
+      at.i = found;
+      at.seq = p.seqs[found];
+      at.len = (unsigned)at.seq < (unsigned)p.c.max_seqs ? p.c.length[at.seq] : -1;
+    }
+  }
+  __syncthreads();
+  const int i = at.i, seq = at.seq, len = at.len;
+  const int64_t r0 = at.r0, r1 = at.r1, local = w - ((r0 >> p.c.log2T) + 2 * (int64_t)i);
   if (refused) return;
   if (local < 0 && r0 <= p.total_rows) return;  // rows before row_off[0] belong to no sequence
   if (!(r0 >= 0 && r1 >= r0 && r1 <= p.total_rows && len >= r1 - r0 && len <= (int64_t)p.c.max_pages * T)) {
@@ -124,12 +155,6 @@ __global__ void __launch_bounds__(kThreads, NU * V <= 16 ? 3 : 1) enter_kernel(E
   if (t1 <= t0) return;
   const int64_t row0 = r0 + (int64_t)slot * T - start + t0;
   if (!in_bounds(i >= 0 && i < p.n && row0 >= r0 && row0 + t1 - t0 <= r1, p.c.status, kSiteAppendRow)) return;
-  const int page = p.c.table[(int64_t)seq * p.c.max_pages + slot];
-  if ((unsigned)page >= (unsigned)p.c.pages || p.c.refs[page] != 1) {  // no page, or one that other sequences hold
-    if (threadIdx.x == 0) set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
-    return;
-  }
-  const int64_t block = ((int64_t)p.layer * p.c.pages + page) * H;
   const int64_t ld = is_k ? p.k_row : p.v_row;
   const uint16_t* src = static_cast<const uint16_t*>(is_k ? p.k : p.v) + row0 * ld;
   const int h0 = is_k ? part * e.k_heads : (part - e.k_parts) * e.v_heads;
@@ -141,8 +166,8 @@ __global__ void __launch_bounds__(kThreads, NU * V <= 16 ? 3 : 1) enter_kernel(E
   const int u = threadIdx.x % UPR, tok0 = threadIdx.x / UPR;
   const int pair = is_k && u < half / V ? u * V : -1;
   const int d0 = pair >= 0 && !ADJ ? V * u : 2 * V * u, d1 = pair >= 0 && !ADJ ? d0 + half : d0 + V;
-  // A head's rows come by asynchronous copies, two heads ahead of the one in hand (single values of 2 bytes by loads).
-  auto held = [&](int h, int n, int which) { return ring + (((h & 1) * NU + n) * 2 + which) * kThreads; };
+  // A head's rows come by asynchronous copies, the next head's while one is in hand (single values of 2 bytes by loads).
+  auto held = [&](int n, int which) { return ring + (n * 2 + which) * kThreads; };
   auto fetch = [&](int h) {
     if constexpr (V > 1) {
       if (h < h1) {
@@ -150,21 +175,27 @@ __global__ void __launch_bounds__(kThreads, NU * V <= 16 ? 3 : 1) enter_kernel(E
 #pragma unroll
         for (int n = 0; n < NU; ++n)
           if (tok0 + n * STEP < rows) {
-            copy_async<V>(held(h, n, 0), from + n * STEP * ld + d0);
-            copy_async<V>(held(h, n, 1), from + n * STEP * ld + d1);
+            copy_async<V>(held(n, 0), from + n * STEP * ld + d0);
+            copy_async<V>(held(n, 1), from + n * STEP * ld + d1);
           }
       }
       cp_async_commit();
     }
   };
   fetch(h0);
-  fetch(h0 + 1);
+  const int page = p.c.table[(int64_t)seq * p.c.max_pages + slot];
+  if ((unsigned)page >= (unsigned)p.c.pages || p.c.refs[page] != 1) {  // no page, or one that other sequences hold
+    if (threadIdx.x == 0) set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
+    return;
+  }
+  const int64_t block = ((int64_t)p.layer * p.c.pages + page) * H;
   if (is_k) {
     for (int x = threadIdx.x; x < rows * half; x += kThreads) {
       const int tok = x / half, i = x - tok * half;
       int ax = e.q.axis[i];
       ax = (unsigned)ax < (unsigned)e.q.axes ? ax : 0;
-      float* to = turn + 2 * (TWO ? x & ~1 : x) + (TWO ? x & 1 : 0);
+      float* to = turn + 2 * x;
+      if (TWO) to = turn + 2 * tok * half + 4 * (i % V / 2 * (half / V) + i / V) + (i & 1);
       rope_angle((float)e.q.pos[ax * e.q.pos_stride + row0 + tok], e.q.freq[i], to[0], to[TWO ? 2 : 1]);
     }
     __syncthreads();
@@ -172,24 +203,24 @@ __global__ void __launch_bounds__(kThreads, NU * V <= 16 ? 3 : 1) enter_kernel(E
   for (int h = h0; h < h1; ++h) {
     float x[NU][2 * V];
     float amax = 0.f;
-    if constexpr (V > 1) cp_async_wait<1>();
+    if constexpr (V > 1) cp_async_wait<0>();
 #pragma unroll
     for (int n = 0; n < NU; ++n) {
       if (tok0 + n * STEP >= rows) continue;
       if constexpr (V > 1) {
-        unpack<BF16, V>(*held(h, n, 0), x[n]);
-        unpack<BF16, V>(*held(h, n, 1), x[n] + V);
+        unpack<BF16, V>(*held(n, 0), x[n]);
+        unpack<BF16, V>(*held(n, 1), x[n] + V);
       } else {
         const uint16_t* from = src + (tok0 + n * STEP) * ld + h * D;
         unpack<BF16, V>(Raw<V>{from[d0]}, x[n]);
         unpack<BF16, V>(Raw<V>{from[d1]}, x[n] + V);
       }
       if (pair >= 0) {
-        const float* cs = turn + 2 * ((tok0 + n * STEP) * half + pair);
+        const float* cs = turn + 2 * (tok0 + n * STEP) * half + (TWO ? 4 * u : 2 * pair);
         if constexpr (TWO) {
 #pragma unroll
           for (int k = 0; k < V; k += 2) {
-            const float4 t = *reinterpret_cast<const float4*>(cs + 2 * k);
+            const float4 t = *reinterpret_cast<const float4*>(cs + 2 * k * (half / V));
             const float2 c = make_float2(t.x, t.y), sn = make_float2(t.z, t.w), y = at2(x[n] + k), z = at2(x[n] + V + k);
             const float2 e0 = tc::fma2(z, make_float2(-sn.x, -sn.y), tc::mul2(y, c)), e1 = tc::fma2(z, c, tc::mul2(y, sn));
             x[n][k] = e0.x;
@@ -211,7 +242,7 @@ __global__ void __launch_bounds__(kThreads, NU * V <= 16 ? 3 : 1) enter_kernel(E
 #pragma unroll
       for (int k = 0; k < 2 * V; k += 2) amax = tc::fmax3(amax, fabsf(x[n][k]), fabsf(x[n][k + 1]));  // (passes over NaN)
     }
-    fetch(h + 2);  // (in the place of what this thread has just read)
+    fetch(h + 1);  // (in the place of what this thread has just read)
     if (amax == INFINITY) {  // the largest finite value counts
       amax = 0.f;
 #pragma unroll
@@ -396,7 +427,7 @@ extern "C" int occam_cache_append_rope(const occam_cache* cache, const occam_app
     return (int)std::max<int64_t>(1, std::min<int64_t>({ctas * heads / (sms * 4), (int64_t)heads, (int64_t)most}));
   };
   e.k_heads = share(slots, cache->heads, 16);
-  e.v_heads = share(slots, cache->heads, 4);
+  e.v_heads = share(slots, cache->heads, 16);
   e.k_parts = (cache->heads + e.k_heads - 1) / e.k_heads;
   e.parts = e.k_parts + (cache->heads + e.v_heads - 1) / e.v_heads;
   // queries: enough threads to fill the GPU first, then as many heads a thread as amortise the sines
