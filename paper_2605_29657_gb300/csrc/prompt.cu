@@ -617,7 +617,7 @@ int launch_dtype(const PromptParams& p, bool bf16, const CUtensorMap& mq, const 
 }  // namespace
 
 bool occam::encode_rows(CUtensorMap* m, const void* at, bool bf16, int dim, int heads, int64_t rows, int64_t row, int box_heads,
-                        int box_rows) {
+                        int box_rows, int box_dims) {
   static const PFN_cuTensorMapEncodeTiled_v12000 enc = [] {
     void* f = nullptr;
     cudaDriverEntryPointQueryResult q;
@@ -628,10 +628,10 @@ bool occam::encode_rows(CUtensorMap* m, const void* at, bool bf16, int dim, int 
   if (!enc) return false;
   cuuint64_t gdim[3] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)rows};
   cuuint64_t gstride[2] = {(cuuint64_t)dim * 2, (cuuint64_t)row * 2};
-  cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows};
+  cuuint32_t box[3] = {(cuuint32_t)box_dims, (cuuint32_t)box_heads, (cuuint32_t)box_rows};
   cuuint32_t es[3] = {1, 1, 1};
   return enc(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(at), gdim, gstride,
-             box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, box_dims == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_32B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 

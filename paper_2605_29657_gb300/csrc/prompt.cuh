@@ -173,19 +173,20 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
   return tc::pack_f16(lo, hi);
 }
 
-// Tensor map of rows [rows][heads][dim] of 16-bit values, `row` elements apart, as boxes of 64 dims x
-// box_heads x box_rows with the 128-byte swizzle; dims past the last one are read as zeros.
+// Tensor map of rows [rows][heads][dim] of 16-bit values, `row` elements apart, as boxes of box_dims dims x
+// box_heads x box_rows, swizzled by 64 dims' 128 bytes or 16 dims' 32; dims past the last one are read as zeros.
 bool encode_rows(CUtensorMap* m, const void* at, bool bf16, int dim, int heads, int64_t rows, int64_t row, int box_heads,
-                 int box_rows);
+                 int box_rows, int box_dims = 64);
 
 // Byte offsets of the workspace: the status word (8 bytes) and the counters, zero between calls; then what the
 // gradient writes before it reads it (see GradParams).
 struct PromptWs {
-  size_t stat, norm, power, vnorm, total;
+  size_t terms, stat, norm, power, vnorm, total;
 };
 inline PromptWs prompt_ws(int64_t total_rows, int64_t total_keys, int heads, int kv_heads) {
   PromptWs w;
-  w.stat = 256;
+  w.terms = 256;
+  w.stat = w.terms + cache_align((size_t)total_rows * heads * 32);
   w.norm = w.stat + cache_align((size_t)total_rows * heads * 8);
   w.power = w.norm + cache_align((size_t)total_rows * heads * 4);
   w.vnorm = w.power + cache_align((size_t)total_rows * kv_heads * 4);

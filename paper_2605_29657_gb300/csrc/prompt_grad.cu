@@ -32,6 +32,7 @@ struct GradParams : PromptParams {
   uint16_t *dq, *dk, *dv;
   int64_t dq_row, dk_row, dv_row;
   float2* stat;   // [total_rows, heads] lse in log2 units, -delta
+  uint4* terms;   // [total_rows, heads, 2] 16-bit terms: four of -lse / scale, four of -delta, eight zeros
   float* norm;    // (f16) [total_rows, heads] |dO|
   float* vnorm;   // (f16) [total_keys, kv_heads] |V|
   float* power;   // (f16) [total_rows, kv_heads], at a sequence's first row: what its dS is held times of
@@ -42,51 +43,85 @@ __device__ __forceinline__ float2 pair16(uint32_t w) {
   return BF16 ? make_float2(bf16_lo(w), bf16_hi(w)) : __half22float2(*reinterpret_cast<const __half2*>(&w));
 }
 
-// ---------------------------------------------------------------- delta
-// Bound by HBM: dO and O read once.
+// A number as a sum of up to four 16-bit terms, each in a unit of its own (see the kernel of keys). f16: a value below 2^31
+// is held to 2^-39 or a relative 2^-46; bf16 (24 bits, fp32's range) needs no units.
 template <bool BF16>
+__device__ __forceinline__ uint2 units4() {
+  return BF16 ? make_uint2(pack16<true>(1.f, 1.f), pack16<true>(1.f, 0.f))
+              : make_uint2(pack16<false>(32768.f, 32.f), pack16<false>(1.f / 32.f, 1.f / 16384.f));
+}
+template <bool BF16>
+__device__ __forceinline__ uint2 terms4(float x) {
+  if (!(fabsf(x) < (BF16 ? 3.3e38f : 2147483648.f)))  // infinities and NaN as they are
+    return make_uint2(pack16<BF16>(x != x ? x : x > 0.f ? INFINITY : -INFINITY, 0.f), 0);
+  if (BF16) {
+    const float a = __bfloat162float(__float2bfloat16_rn(x)), b = __bfloat162float(__float2bfloat16_rn(x - a));
+    return make_uint2(pack16<true>(a, b), pack16<true>(x - a - b, 0.f));
+  }
+  const float a = __half2float(__float2half_rn(x * (1.f / 32768.f))), r0 = fmaf(a, -32768.f, x);
+  const float b = __half2float(__float2half_rn(r0 * (1.f / 32.f))), r1 = fmaf(b, -32.f, r0);
+  const float c = __half2float(__float2half_rn(r1 * 32.f)), r2 = fmaf(c, -1.f / 32.f, r1);
+  return make_uint2(pack16<false>(a, b), pack16<false>(c, r2 * 16384.f));
+}
+
+// ---------------------------------------------------------------- delta
+// Bound by HBM: dO and O read once. 2^LOG lanes a vector, kVectors vectors' loads of a thread in flight.
+constexpr int kVectors = 4;
+template <bool BF16, int LOG>
 __global__ void __launch_bounds__(256) stat_kernel(GradParams p) {
   pdl_wait();
-  const int sub = threadIdx.x & 15;
-  const int64_t at = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), rows = p.total_rows * p.H;
-  float dot = 0.f, sq = 0.f;
-  if (at < rows) {
-    const int64_t row = at / p.H;
-    if (sub * 8 < p.dim) {
-      const uint4 a = ldg_stream(p.o + at * p.dim + sub * 8);
-      const uint4 b = ldg_stream(p.dout + row * p.dout_row + (at - row * p.H) * p.dim + sub * 8);
-      const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+  constexpr int LANES = 1 << LOG, PER = 256 / LANES;
+  const int sub = threadIdx.x & (LANES - 1), first = threadIdx.x >> LOG;
+  const bool of_v = blockIdx.y != 0;  // (f16) norms of V
+  const int heads = of_v ? p.Hkv : p.H;
+  const int64_t vectors = (of_v ? p.total_keys : p.total_rows) * heads;
+  const int64_t base = (int64_t)blockIdx.x * (PER * kVectors);
+  if (base >= vectors) return;
+  const int64_t row0 = base / heads;
+  const int head0 = (int)(base - row0 * heads);
+  uint4 a[kVectors], b[kVectors];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float2 u = pair16<BF16>(x[k]), v = pair16<BF16>(y[k]);
-        dot = fmaf(u.x, v.x, fmaf(u.y, v.y, dot));
-        sq = fmaf(v.x, v.x, fmaf(v.y, v.y, sq));
-      }
-    }
-  } else if (!BF16 && at - rows < p.total_keys * p.Hkv) {
-    const int64_t key = (at - rows) / p.Hkv;
-    if (sub * 8 < p.dim) {
-      const uint4 b = ldg_stream(p.v + key * p.v_row + (at - rows - key * p.Hkv) * p.dim + sub * 8);
-      const uint32_t y[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float2 v = pair16<BF16>(y[k]);
-        sq = fmaf(v.x, v.x, fmaf(v.y, v.y, sq));
+  for (int k = 0; k < kVectors; ++k) {
+    const int at = head0 + k * PER + first, row = at / heads;
+    a[k] = b[k] = make_uint4(0, 0, 0, 0);
+    if (base + k * PER + first < vectors && sub * 8 < p.dim) {
+      if (of_v) {
+        b[k] = ldg_stream(p.v + (row0 + row) * p.v_row + (at - row * heads) * p.dim + sub * 8);
+      } else {
+        a[k] = ldg_stream(p.o + (base + k * PER + first) * p.dim + sub * 8);
+        b[k] = ldg_stream(p.dout + (row0 + row) * p.dout_row + (at - row * heads) * p.dim + sub * 8);
       }
     }
   }
 #pragma unroll
-  for (int o = 8; o > 0; o >>= 1) {
-    dot += __shfl_xor_sync(0xffffffffu, dot, o);
-    if (!BF16) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-  }
-  if (sub != 0) return;
-  if (at < rows) {
-    const float l = p.lse[at];
-    p.stat[at] = make_float2(l == -INFINITY ? INFINITY : l * 1.44269504089f, -dot);  // (a row that sees nothing: every p is 0)
-    if (!BF16) p.norm[at] = sqrtf(sq);
-  } else if (!BF16 && at - rows < p.total_keys * p.Hkv) {
-    p.vnorm[at - rows] = sqrtf(sq);
+  for (int k = 0; k < kVectors; ++k) {
+    const uint32_t x[4] = {a[k].x, a[k].y, a[k].z, a[k].w}, y[4] = {b[k].x, b[k].y, b[k].z, b[k].w};
+    float dot = 0.f, sq = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 u = pair16<BF16>(x[e]), v = pair16<BF16>(y[e]);
+      dot = fmaf(u.x, v.x, fmaf(u.y, v.y, dot));
+      if (!BF16) sq = fmaf(v.x, v.x, fmaf(v.y, v.y, sq));
+    }
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) {
+      dot += __shfl_xor_sync(0xffffffffu, dot, o);
+      if (!BF16) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+    }
+    const int64_t to = base + k * PER + first;
+    if (sub != 0 || to >= vectors) continue;
+    if (of_v) {
+      p.vnorm[to] = sqrtf(sq);
+    } else {
+      const float l = p.lse[to];
+      const float l2 = l == -INFINITY ? INFINITY : l * 1.44269504089f;  // (a row that sees nothing: every p is 0)
+      p.stat[to] = make_float2(l2, -dot);
+      // (finite in that row: a mask hides its keys there, and an infinity would meet the other product's units of 0)
+      const uint2 x = terms4<BF16>(l2 == INFINITY ? 0.f : -l2 / p.scale_log2), y = terms4<BF16>(-dot);
+      p.terms[2 * to] = make_uint4(x.x, x.y, y.x, y.y);
+      p.terms[2 * to + 1] = make_uint4(0, 0, 0, 0);
+      if (!BF16) p.norm[to] = sqrtf(sq);
+    }
   }
 }
 
@@ -166,9 +201,14 @@ __device__ __forceinline__ void scale_pack(const uint32_t (&o)[16], float f, uin
 // Even and odd steps have tensor memory, an issuing warp and a warpgroup of their own: while one's scores are
 // turned into P and dS, the other's products run. The sums are added to in the order of the steps (a step's product
 // waits for the one before it; the scores issued in between keep the tensor cores busy).
+// A row's lse and delta are constants of a column here. They come in as 16 more dims of both products: every row
+// brings -lse / scale and -delta as sums of up to four 16-bit terms, the first operand has those terms' units (of
+// the one in S^T, of the other in dP^T), so that S^T and dP^T arrive as what the exponential and the product want.
 namespace keys {
 
-constexpr int kQ = 64;  // query rows of a step
+constexpr int kQ = 64;                  // query rows of a step
+constexpr int kMoreBytes = kQ * 32;     // of the rows' 16 more dims
+constexpr int kUnitBytes = 128 * 32;    // of the first operand's
 
 template <int DP>
 struct Shape {
@@ -185,7 +225,6 @@ struct Shared {
   PromptItem item[kItems];  // tile: of keys; hb: key head; nk[0]: the first block of rows; nk[1]: 0, or 1 at the end
   uint32_t tmem;
   int stop;
-  alignas(16) float2 stat[STAGES][kQ];
   PromptList list;
 };
 
@@ -206,8 +245,8 @@ __device__ __forceinline__ Place place_of(const GradParams& p, const PromptItem&
 
 template <int DP, class Sh>
 __device__ __forceinline__ void load_role(const GradParams& p, Sh& sh, int log_p, const CUtensorMap& map_q, const CUtensorMap& map_do,
-                                          const CUtensorMap& map_k, const CUtensorMap& map_v, unsigned char* k_smem,
-                                          unsigned char* v_smem, unsigned char* q_smem) {
+                                          const CUtensorMap& map_k, const CUtensorMap& map_v, const CUtensorMap& map_terms,
+                                          unsigned char* k_smem, unsigned char* v_smem, unsigned char* q_smem, unsigned char* more) {
   using S = Shape<DP>;
   const int lane = threadIdx.x & 31, total = sh.list.first[kChunks];
   const Count count{p};
@@ -270,7 +309,8 @@ __device__ __forceinline__ void load_role(const GradParams& p, Sh& sh, int log_p
       const Place at = place_of(p, it, log_p, k);
       WAIT(sh.free[st], ((j / S::kStages) & 1) ^ 1);
       if (lane == 0) {
-        tc::bar_expect_tx(&sh.full[st], S::kTile);  // 64 rows of Q and of dO
+        tc::bar_expect_tx(&sh.full[st], S::kTile + kMoreBytes);  // 64 rows of Q and of dO
+        tc::tma_load_3d(more + st * kMoreBytes, &map_terms, 0, at.head, (int)(it.row0 + at.tok), &sh.full[st]);
         unsigned char* to = q_smem + st * S::kTile;
         for (int b = 0; b < S::kBlocks; ++b) {
           tc::tma_load_3d(to + b * kQ * kRowBytes, &map_q, b * 64, at.head, (int)(it.row0 + at.tok), &sh.full[st]);
@@ -284,39 +324,35 @@ __device__ __forceinline__ void load_role(const GradParams& p, Sh& sh, int log_p
   }
 }
 
-// The rows' statistics, and zeros in rows past the sequence's end
+// Rows past the sequence's end become zeros, terms and all: P is finite there, dP is 0.
 template <int DP, class Sh>
-__device__ __forceinline__ void look_role(const GradParams& p, Sh& sh, int log_p, unsigned char* q_smem) {
+__device__ __forceinline__ void look_role(const GradParams& p, Sh& sh, int log_p, unsigned char* q_smem, unsigned char* more) {
   using S = Shape<DP>;
   const int lane = threadIdx.x & 31;
   uint32_t j = 0;
   for (uint32_t i = 0;; ++i) {
     WAIT(sh.item_full[i % kItems], (i / kItems) & 1);
-    const PromptItem it = sh.item[i % kItems];
-    if (it.nk[1]) return;
+    if (sh.item[i % kItems].nk[1]) return;
+    const int steps = sh.item[i % kItems].steps, rows = sh.item[i % kItems].rows, first = sh.item[i % kItems].nk[0];
+    const int log_t = 6 - log_p, blocks = ((rows + (1 << log_t) - 1) >> log_t) - first;
+    const int last = (rows & ((1 << log_t) - 1)) << log_p;  // rows of the last block of tokens, 0: it is whole
+    int block = 0;
 #pragma unroll 1
-    for (int k = 0; k < it.steps; ++k, ++j) {
+    for (int k = 0; k < steps; ++k, ++j) {
       const int st = j % S::kStages;
-      const Place at = place_of(p, it, log_p, k);
-      float2 x[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int r = lane + 32 * e, tok = at.tok + (r >> log_p);
-        x[e] = make_float2(INFINITY, 0.f);
-        const int64_t from = (it.row0 + tok) * p.H + at.head + (r & ((1 << log_p) - 1));
-        if (tok < it.rows && in_bounds(from < p.total_rows * p.H, p.status, kSitePromptRow)) x[e] = p.stat[from];
-      }
       WAIT(sh.full[st], (j / S::kStages) & 1);
-      sh.stat[st][lane] = x[0];
-      sh.stat[st][lane + 32] = x[1];
-      const int live = (it.rows - at.tok) << log_p;  // rows that exist
-      if (live < kQ) {
+      if (++block == blocks) {
+        block = 0;
+        if (last) {
 #pragma unroll 1
-        for (int b = 0; b < 2 * S::kBlocks; ++b) {
-          uint4* piece = reinterpret_cast<uint4*>(q_smem + st * S::kTile + b * kQ * kRowBytes);
-          for (int e = live * 8 + lane; e < kQ * 8; e += 32) piece[e] = make_uint4(0, 0, 0, 0);
+          for (int b = 0; b < 2 * S::kBlocks; ++b) {
+            uint4* piece = reinterpret_cast<uint4*>(q_smem + st * S::kTile + b * kQ * kRowBytes);
+            for (int e = last * 8 + lane; e < kQ * 8; e += 32) piece[e] = make_uint4(0, 0, 0, 0);
+          }
+          uint4* row = reinterpret_cast<uint4*>(more + st * kMoreBytes);
+          for (int e = last * 2 + lane; e < kQ * 2; e += 32) row[e] = make_uint4(0, 0, 0, 0);
+          tc::fence_proxy_async();
         }
-        tc::fence_proxy_async();
       }
       __syncwarp();
       if (lane == 0) tc::bar_arrive(&sh.ready[st]);
@@ -328,12 +364,15 @@ __device__ __forceinline__ void look_role(const GradParams& p, Sh& sh, int log_p
 // The steps of parity b. After step j's P: dV += P^T dO, then S^T of step j + 2 in its place; after its dS: dK += dS^T Q and
 // dP^T of step j + 2.
 template <int DP, bool BF16, class Sh>
-__device__ __forceinline__ void issue_role(const GradParams& p, Sh& sh, uint32_t k_smem, uint32_t v_smem, uint32_t q_smem, uint32_t tmem,
-                                           uint32_t b) {
+__device__ __forceinline__ void issue_role(const GradParams& p, Sh& sh, uint32_t k_smem, uint32_t v_smem, uint32_t q_smem, uint32_t units,
+                                           uint32_t more, uint32_t tmem, uint32_t b) {
   using S = Shape<DP>;
   constexpr uint32_t id_s = tc::idesc16(BF16, 128, kQ, false), id_o = tc::idesc16(BF16, 128, DP, true);
   const uint64_t dk = tc::sdesc_sw128(k_smem), dv = tc::sdesc_sw128(v_smem);
   const uint64_t dq = tc::sdesc_sw128(q_smem), dqt = tc::sdesc_mn_sw128(q_smem, kQ * kRowBytes);
+  // (Both 16-byte pieces of a row of units are the same, and one of a row of terms is 0: the order in which the
+  // swizzle puts them does not matter.)
+  const uint64_t du = tc::sdesc_sw32(units), dm = tc::sdesc_sw32(more);
   const uint32_t s_at = tmem + b * 128, dp_at = s_at + 64, dv_at = tmem + 256, dk_at = tmem + 384;
   // a walk over the steps of this parity
   uint32_t i = 0, j = b;       // items begun; the next own step
@@ -384,6 +423,7 @@ __device__ __forceinline__ void issue_role(const GradParams& p, Sh& sh, uint32_t
 #pragma unroll
         for (int q = 0; q < DP / 16; ++q)
           tc::mma_bf16(s_at, dk + (q >> 2) * (128 * kRowBytes >> 4) + (q & 3) * 2, d + (q >> 2) * (kQ * kRowBytes >> 4) + (q & 3) * 2, id_s, q > 0);
+        tc::mma_bf16(s_at, du, dm + st * (kMoreBytes >> 4), id_s, 1);
         tc::mma_commit(&sh.s_full[b]);
       }
       __syncwarp();
@@ -412,6 +452,7 @@ __device__ __forceinline__ void issue_role(const GradParams& p, Sh& sh, uint32_t
 #pragma unroll
       for (int q = 0; q < DP / 16; ++q)
         tc::mma_bf16(dp_at, dv + (q >> 2) * (128 * kRowBytes >> 4) + (q & 3) * 2, d + (q >> 2) * (kQ * kRowBytes >> 4) + (q & 3) * 2, id_s, q > 0);
+      tc::mma_bf16(dp_at, du + (kUnitBytes >> 4), dm + st * (kMoreBytes >> 4), id_s, 1);
       tc::mma_commit(&sh.dp_full[b]);
     }
     __syncwarp();
@@ -429,7 +470,6 @@ __device__ __forceinline__ void issue_role(const GradParams& p, Sh& sh, uint32_t
 // A key a thread: P^T and dS^T of the steps of parity b
 template <int DP, bool BF16, class Sh>
 __device__ __forceinline__ void element_role(const GradParams& p, Sh& sh, int log_p, uint32_t tmem, uint32_t b) {
-  using S = Shape<DP>;
   const int r = threadIdx.x & 127, lane = threadIdx.x & 31;
   const uint32_t s_at = tmem + b * 128 + ((uint32_t)(r & ~31) << 16), dp_at = s_at + 64;
   const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
@@ -443,10 +483,7 @@ __device__ __forceinline__ void element_role(const GradParams& p, Sh& sh, int lo
 #pragma unroll 1
     for (int k = 0; k < it.steps; ++k, ++j) {
       if ((j & 1) != b) continue;
-      const int st = j % S::kStages;
       const Place at = place_of(p, it, log_p, k);
-      WAIT(sh.ready[st], (j / S::kStages) & 1);
-      const float4* stat = reinterpret_cast<const float4*>(sh.stat[st]);
       WAIT(sh.s_full[b], done & 1);
       tc::fence_after();
       uint32_t v[64];
@@ -455,9 +492,8 @@ __device__ __forceinline__ void element_role(const GradParams& p, Sh& sh, int lo
       float pr[64];
 #pragma unroll
       for (int e = 0; e < 32; ++e) {
-        const float4 q = stat[e];
-        float2 y = tc::fma2(make_float2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), scale2,
-                            make_float2(Lift<BF16>::kLog2 - q.x, Lift<BF16>::kLog2 - q.z));
+        const float2 s = make_float2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
+        const float2 y = BF16 ? tc::mul2(s, scale2) : tc::fma2(s, scale2, make_float2(Lift<BF16>::kLog2, Lift<BF16>::kLog2));
         pr[2 * e] = fast_exp2(y.x);
         pr[2 * e + 1] = fast_exp2(y.y);
       }
@@ -483,11 +519,8 @@ __device__ __forceinline__ void element_role(const GradParams& p, Sh& sh, int lo
       uint32_t pk[32];
 #pragma unroll
       for (int e = 0; e < 32; ++e) {
-        const float4 q = stat[e];
-        float2 y = tc::add2(make_float2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), make_float2(q.y, q.w));
-        y.x *= pr[2 * e];
-        y.y *= pr[2 * e + 1];
-        if (!BF16) y.x *= power, y.y *= power;
+        float2 y = tc::mul2(make_float2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), make_float2(pr[2 * e], pr[2 * e + 1]));
+        if (!BF16) y = tc::mul2(y, make_float2(power, power));
         pk[e] = pack16<BF16>(y.x, y.y);
       }
       tc::tmem_st32(dp_at, pk);
@@ -554,7 +587,8 @@ __device__ __forceinline__ void write_role(const GradParams& p, Sh& sh, unsigned
 template <int DP, bool BF16>
 __global__ void __launch_bounds__(kThreads, 1)
     prompt_keys_kernel(GradParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_do,
-                       const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+                       const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                       const __grid_constant__ CUtensorMap map_terms) {
   using S = Shape<DP>;
   using Sh = Shared<S::kStages>;
   extern __shared__ __align__(1024) unsigned char smem[];
@@ -562,8 +596,16 @@ __global__ void __launch_bounds__(kThreads, 1)
   unsigned char* v_smem = k_smem + S::kTile;
   unsigned char* q_smem = v_smem + S::kTile;
   unsigned char* stage = q_smem + S::kStages * S::kTile;
-  Sh& sh = *reinterpret_cast<Sh*>(stage + 4 * 32 * 128);
+  unsigned char* units = stage + 4 * 32 * 128;
+  unsigned char* more = units + 2 * kUnitBytes;
+  Sh& sh = *reinterpret_cast<Sh*>(more + S::kStages * kMoreBytes);
   const int warp = threadIdx.x >> 5, log_p = min(p.log2P, 6);
+  {
+    static_assert(2 * kUnitBytes == kThreads * 16, "a piece a thread");
+    const uint2 u = units4<BF16>();
+    reinterpret_cast<uint4*>(units)[threadIdx.x] = threadIdx.x < kThreads / 2 ? make_uint4(u.x, u.y, 0, 0) : make_uint4(0, 0, u.x, u.y);
+  }
+  tc::fence_proxy_async();
   if (threadIdx.x == 0) {
     sh.stop = 0;
     tc::bar_init(&sh.kv_full, 1);
@@ -605,11 +647,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else {
     tc::setmaxnreg_dec<kRegIssue>();
     if (warp == 13)
-      load_role<DP>(p, sh, log_p, map_q, map_do, map_k, map_v, k_smem, v_smem, q_smem);
+      load_role<DP>(p, sh, log_p, map_q, map_do, map_k, map_v, map_terms, k_smem, v_smem, q_smem, more);
     else if (warp == 15)
-      look_role<DP>(p, sh, log_p, q_smem);
+      look_role<DP>(p, sh, log_p, q_smem, more);
     else
-      issue_role<DP, BF16>(p, sh, tc::su32(k_smem), tc::su32(v_smem), tc::su32(q_smem), tmem, warp == 14);
+      issue_role<DP, BF16>(p, sh, tc::su32(k_smem), tc::su32(v_smem), tc::su32(q_smem), tc::su32(units), tc::su32(more), tmem,
+                           warp == 14);
   }
   __syncthreads();
   // after a wait that ran out, products and copies may still be in flight
@@ -1059,8 +1102,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // Once per device and kernel: the shared memory, and that the register split adds up --
 // setmaxnreg.inc waits for registers that only the launch's own can give.
-template <class Kernel>
-int launch(Kernel kern, std::atomic<uint64_t>& ready, int smem, int grid, const GradParams& p, const CUtensorMap (&m)[4], cudaStream_t st) {
+template <class Kernel, class... Maps>
+int launch(Kernel kern, std::atomic<uint64_t>& ready, int smem, int grid, cudaStream_t st, const GradParams& p, const Maps&... maps) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return OCCAM_ERR_CUDA;
   if (!((ready.load(std::memory_order_acquire) >> dev) & 1)) {
@@ -1070,30 +1113,34 @@ int launch(Kernel kern, std::atomic<uint64_t>& ready, int smem, int grid, const 
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return OCCAM_ERR_CUDA;
     ready.fetch_or(uint64_t(1) << dev, std::memory_order_release);
   }
-  return launch_after(kern, dim3((unsigned)grid), kThreads, smem, st, p, m[0], m[1], m[2], m[3]) && cudaGetLastError() == cudaSuccess
+  return launch_after(kern, dim3((unsigned)grid), kThreads, smem, st, p, maps...) && cudaGetLastError() == cudaSuccess
              ? OCCAM_OK
              : OCCAM_ERR_CUDA;
 }
 
 template <int DP, bool BF16>
-int launch_grad(const GradParams& p, const CUtensorMap (&mk)[4], const CUtensorMap (&mr)[4], int grid_keys, int grid_rows, cudaStream_t st) {
-  const int64_t vectors = p.total_rows * p.H + (BF16 ? 0 : p.total_keys * p.Hkv);
+int launch_grad(const GradParams& p, const CUtensorMap (&mk)[5], const CUtensorMap (&mr)[4], int grid_keys, int grid_rows, cudaStream_t st) {
   if (p.total_rows > 0) {
-    if ((vectors + 15) / 16 > 0x7fffffff) return OCCAM_ERR_UNSUPPORTED;
-    if (!launch_after(stat_kernel<BF16>, dim3((unsigned)((vectors + 15) / 16)), 256, 0, st, p)) return OCCAM_ERR_CUDA;
+    const int log_lanes = p.dim <= 64 ? 3 : 4;
+    const int64_t most = std::max(p.total_rows * p.H, BF16 ? 0 : p.total_keys * p.Hkv), per = (256 >> log_lanes) * kVectors;
+    if ((most + per - 1) / per > 0x7fffffff) return OCCAM_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)((most + per - 1) / per), BF16 ? 1 : 2);
+    if (!(log_lanes == 3 ? launch_after(stat_kernel<BF16, 3>, grid, 256, 0, st, p) : launch_after(stat_kernel<BF16, 4>, grid, 256, 0, st, p)))
+      return OCCAM_ERR_CUDA;
     if (!BF16 && !launch_after(power_kernel, dim3((unsigned)p.n, (unsigned)p.Hkv), 512, 0, st, p)) return OCCAM_ERR_CUDA;
   }
   using K = keys::Shape<DP>;
   using R = rows::Shape<DP>;
-  constexpr int smem_k = (2 + K::kStages) * K::kTile + 4 * 32 * 128 + (int)sizeof(keys::Shared<K::kStages>);
+  constexpr int smem_k = (2 + K::kStages) * K::kTile + 4 * 32 * 128 + 2 * keys::kUnitBytes + K::kStages * keys::kMoreBytes +
+                         (int)sizeof(keys::Shared<K::kStages>);
   constexpr int smem_r = 4 * R::kTile + 2 * R::kStages * R::kHalf + 4 * 32 * 128 + (int)sizeof(rows::Shared<R::kStages>);
   static_assert(smem_k <= 227 * 1024 && smem_r <= 227 * 1024, "an SM's shared memory");
   static std::atomic<uint64_t> ready_k{0}, ready_r{0};
   if (grid_keys > 0) {
-    const int rc = launch(keys::prompt_keys_kernel<DP, BF16>, ready_k, smem_k, grid_keys, p, mk, st);
+    const int rc = launch(keys::prompt_keys_kernel<DP, BF16>, ready_k, smem_k, grid_keys, st, p, mk[0], mk[1], mk[2], mk[3], mk[4]);
     if (rc != OCCAM_OK) return rc;
   }
-  return grid_rows > 0 ? launch(rows::prompt_rows_kernel<DP, BF16>, ready_r, smem_r, grid_rows, p, mr, st) : OCCAM_OK;
+  return grid_rows > 0 ? launch(rows::prompt_rows_kernel<DP, BF16>, ready_r, smem_r, grid_rows, st, p, mr[0], mr[1], mr[2], mr[3]) : OCCAM_OK;
 }
 
 }  // namespace
@@ -1147,6 +1194,7 @@ extern "C" int occam_prompt_attend_grad(const occam_prompt_args* a, const occam_
   p.dk_row = g->dk_row;
   p.dv_row = g->dv_row;
   p.stat = ws_at<float2>(workspace, w.stat);
+  p.terms = ws_at<uint4>(workspace, w.terms);
   p.norm = ws_at<float>(workspace, w.norm);
   p.vnorm = ws_at<float>(workspace, w.vnorm);
   p.power = ws_at<float>(workspace, w.power);
@@ -1162,10 +1210,11 @@ extern "C" int occam_prompt_attend_grad(const occam_prompt_args* a, const occam_
   const int64_t q_row = R > 0 ? a->q_row : (int64_t(1) << 20), do_row = R > 0 ? g->dout_row : (int64_t(1) << 20);
   const int64_t k_row = K > 0 ? a->k_row : a->q_row, v_row = K > 0 ? a->v_row : a->q_row;
   const int64_t rows = std::max<int64_t>(R, 1), keys_n = std::max<int64_t>(K, 1);
-  CUtensorMap mk[4], mr[4];
+  CUtensorMap mk[5], mr[4];
   if (!encode_rows(&mk[0], q, bf16, p.dim, p.H, rows, q_row, 1 << log_p, 64 >> log_p) ||
       !encode_rows(&mk[1], dout, bf16, p.dim, p.H, rows, do_row, 1 << log_p, 64 >> log_p) ||
       !encode_rows(&mk[2], k, bf16, p.dim, p.Hkv, keys_n, k_row, 1, 128) || !encode_rows(&mk[3], v, bf16, p.dim, p.Hkv, keys_n, v_row, 1, 128) ||
+      !encode_rows(&mk[4], p.terms, bf16, 16, p.H, rows, 16 * (int64_t)p.H, 1 << log_p, 64 >> log_p, 16) ||
       !encode_rows(&mr[0], q, bf16, p.dim, p.H, rows, q_row, 1 << p.log2P, 128 >> p.log2P) ||
       !encode_rows(&mr[1], dout, bf16, p.dim, p.H, rows, do_row, 1 << p.log2P, 128 >> p.log2P) ||
       !encode_rows(&mr[2], k, bf16, p.dim, p.Hkv, keys_n, k_row, 1, 64) || !encode_rows(&mr[3], v, bf16, p.dim, p.Hkv, keys_n, v_row, 1, 64))
