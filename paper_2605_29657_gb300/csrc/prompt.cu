@@ -36,7 +36,7 @@ constexpr int kThreads = 512;
 constexpr int kK = 128;          // keys of a tile
 constexpr int kItems = 3;        // items known ahead
 constexpr int kBlock = 128 * 128;  // bytes of 128 rows x 64 dims
-constexpr int kRegSoftmax = 176, kRegWrite = 88, kRegIssue = 72;  // 2 x 176 + 88 + 72 = 4 x 128
+constexpr int kRegSoftmax = 168, kRegWrite = 88, kRegIssue = 88;  // 2 x 168 + 88 + 88 = 4 x 128
 constexpr float kLazy = 8.f;     // log2 growth of a maximum before O is rescaled
 constexpr int kNever = 0x7fffffff;
 
@@ -75,65 +75,23 @@ __device__ __forceinline__ int key_steps(const PromptParams& p, const PromptSeq&
   return max((lim + kK - 1) / kK, 1);  // (where nothing is seen, one tile of hidden keys gives the rows their zeros)
 }
 
+// Steps whose keys every row of the item sees
+__device__ __forceinline__ int whole_steps(const PromptParams& p, const PromptItem& x) {
+  return min(prompt_limit(p, x.rows, x.keys, (x.tile * 2) << (7 - p.log2P)), x.keys) / kK;
+}
+
 #define WAIT(bar, parity) PROMPT_WAIT(bar, parity)
 
 template <int DP, class Sh>
 __device__ __forceinline__ void load_role(const PromptParams& p, Sh& sh, const CUtensorMap& map_q, const CUtensorMap& map_k,
                                           const CUtensorMap& map_v, unsigned char* q_smem, unsigned char* k_smem, unsigned char* v_smem) {
   using S = Shape<DP>;
-  const int lane = threadIdx.x & 31, total = sh.list.first[kChunks];
-  const Count count{p};
-  int next = blockIdx.x;  // the item that is told next
-  uint32_t told = 0;
-  auto tell = [&]() -> bool {
-    PromptItem& it = sh.item[told % kItems];
-    if (!tc::bar_try(&sh.item_free[told % kItems], ((told / kItems) & 1) ^ 1) &&
-        !prompt_wait_long(&sh.item_free[told % kItems], ((told / kItems) & 1) ^ 1, &sh.stop, p.status))
-      return false;
-    if (sh.odd[told % kItems]) {  // the notes of the item that was here (every role is done with it)
-      for (int d = lane; d < 3 * 128; d += 32) sh.first[told % kItems][0][d] = kNever;
-      __syncwarp();
-      if (lane == 0) sh.odd[told % kItems] = 0;
-    }
-    int steps = 0;
-    if (next < total) {
-      int place = 0;
-      const PromptSeq s = prompt_find(p, sh.list, count, next, &place);
-      const int hbs = p.H >> p.log2P, log_tt = 7 - p.log2P, per = 2 << log_tt;
-      const int blocks = (s.rows + per - 1) / per;
-      const int tile = blocks - 1 - place / hbs, hb = place % hbs, tok0 = tile * per;
-      const int left = s.rows - tok0;
-      const int nk0 = key_steps(p, s, tok0 + min(left, 1 << log_tt) - 1);
-      const int nk1 = left > (1 << log_tt) ? key_steps(p, s, tok0 + min(left, per) - 1) : 0;
-      steps = max(nk0, nk1);
-      if (lane == 0) {
-        it.row0 = s.row0;
-        it.key0 = s.key0;
-        it.rows = s.rows;
-        it.keys = s.keys;
-        it.tile = tile;
-        it.hb = hb;
-        it.steps = steps;
-        it.nk[0] = nk0;
-        it.nk[1] = nk1;
-        next = gridDim.x + atomicAdd(&p.counters[0], 1);
-      }
-      next = __shfl_sync(0xffffffffu, next, 0);
-    } else if (lane == 0) {
-      it.steps = 0;
-    }
-    __syncwarp();
-    if (lane == 0) tc::bar_arrive(&sh.item_full[told % kItems]);
-    __syncwarp();
-    ++told;
-    return true;
-  };
-  if (!tell()) return;
+  const int lane = threadIdx.x & 31;
   uint32_t j = 0, nq[2] = {0, 0};
   for (uint32_t i = 0;; ++i) {
+    WAIT(sh.item_full[i % kItems], (i / kItems) & 1);
     const PromptItem it = sh.item[i % kItems];
-    if (it.steps == 0) break;
-    if (!tell()) return;
+    if (it.steps == 0) return;
     const int tt = 128 >> p.log2P, head = it.hb << p.log2P, kv = head / p.G;
     for (int k = 0; k < it.steps; ++k, ++j) {
       const int st = j % S::kStages;
@@ -171,28 +129,34 @@ __device__ __forceinline__ void load_role(const PromptParams& p, Sh& sh, const C
 
 // ---------------------------------------------------------------- issuing
 // Row tile t. Step by step and half by half: O += P V of the step before, then S of this step in the place
-// of that P. The whole warp walks; one elected lane issues. (A descriptor's address field counts 16 bytes.)
+// of that P. One lane does it all: a turn of the whole warp with an election for every group of products took longer than
+// the products. (A descriptor's address field counts 16 bytes.)
 template <int DP, bool BF16, class Sh>
 __device__ __forceinline__ void issue_role(const PromptParams& p, Sh& sh, uint32_t q_smem, uint32_t k_smem, uint32_t v_smem,
                                            uint32_t tmem, int t) {
   using S = Shape<DP>;
   constexpr uint32_t id_s = tc::idesc16(BF16, 128, 64, false), id_o = tc::idesc16(BF16, 128, DP, true);
-  const uint64_t dq = tc::sdesc_sw128(q_smem + t * S::kTile), dk = tc::sdesc_sw128(k_smem), dv = tc::sdesc_mn_sw128(v_smem, kBlock);
+  const uint64_t kmajor = tc::sdesc_sw128(0), mnmajor = tc::sdesc_mn_sw128(0, kBlock);
+  const uint32_t km = tc::desc_hi(kmajor), mn = tc::desc_hi(mnmajor);
+  const uint32_t dq = (uint32_t)kmajor + ((q_smem + t * S::kTile) >> 4), dk = (uint32_t)kmajor + (k_smem >> 4),
+                 dv = (uint32_t)mnmajor + (v_smem >> 4);
   const uint32_t o_at = tmem + 256 + t * 128, s_at = tmem + t * 128;
   uint32_t j = 0, products = 0;  // steps; this row tile's steps whose product was issued
   uint32_t n_q = 0, n_o = 0;     // this row tile's items whose scores, whose products have begun
+  uint32_t looked = 0;           // a bit a stage: how often (mod 2) its values were looked at
   struct {
-    bool any, mine, first, last;
-  } was = {false, false, false, false};
+    bool any, mine, first, last, look;
+  } was = {false, false, false, false, false};
   uint32_t i = 0;
-  int k = 0, steps = 0, nk = 0;
+  int k = 0, steps = 0, nk = 0, whole = 0;  // whole: steps whose keys every row of the item sees
   for (;;) {
     if (k == steps) {
-      if (i > 0 && tc::elect_one()) tc::bar_arrive(&sh.item_free[(i - 1) % kItems]);
-      __syncwarp();
+      if (i > 0) tc::bar_arrive(&sh.item_free[(i - 1) % kItems]);
       WAIT(sh.item_full[i % kItems], (i / kItems) & 1);
-      steps = sh.item[i % kItems].steps;
-      nk = sh.item[i % kItems].nk[t];
+      const PromptItem& x = sh.item[i % kItems];
+      steps = x.steps;
+      nk = x.nk[t];
+      whole = whole_steps(p, x);
       k = 0;
       ++i;
     }
@@ -201,7 +165,13 @@ __device__ __forceinline__ void issue_role(const PromptParams& p, Sh& sh, uint32
 #pragma unroll 1
     for (int h = 0; h < 2; ++h) {
       if (was.any) {
-        if (h == 0) WAIT(sh.v_ready[before], ((j - 1) / S::kStages) & 1);
+        if (h == 0) {
+          WAIT(sh.v_full[before], ((j - 1) / S::kStages) & 1);
+          if (was.look) {
+            WAIT(sh.v_ready[before], (looked >> before) & 1);
+            looked ^= 1u << before;
+          }
+        }
         if (was.mine) {
           if (h == 0 && was.first) {
             WAIT(sh.o_free[t], (n_o & 1) ^ 1);
@@ -209,15 +179,14 @@ __device__ __forceinline__ void issue_role(const PromptParams& p, Sh& sh, uint32
           }
           WAIT(sh.p_full[t][h], products & 1);
           tc::fence_after();
-          if (tc::elect_one()) {
-            const uint64_t vd = dv + before * (S::kTile >> 4) + h * (64 * 128 >> 4);
+          {
+            const uint32_t vd = dv + before * (S::kTile >> 4) + h * (64 * 128 >> 4);
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-              tc::mma_ts(o_at, s_at + h * 64 + q * 8, vd + q * (2048 >> 4), id_o, q > 0 || h > 0 || !was.first ? 1u : 0u);
+              tc::mma16_ts(o_at, s_at + h * 64 + q * 8, vd + q * (2048 >> 4), mn, id_o, q > 0 || h > 0 || !was.first);
             tc::mma_commit(&sh.o_done[t][h]);
             if (h == 1 && was.last) tc::mma_commit(&sh.o_full[t]);
           }
-          __syncwarp();
         }
       }
       if (mine) {
@@ -229,32 +198,31 @@ __device__ __forceinline__ void issue_role(const PromptParams& p, Sh& sh, uint32
           WAIT(sh.k_full[st], (j / S::kStages) & 1);
           tc::fence_after();
         }
-        if (tc::elect_one()) {
-          const uint64_t kd = dk + st * (S::kTile >> 4) + h * (64 * 128 >> 4);
+        {
+          const uint32_t kd = dk + st * (S::kTile >> 4) + h * (64 * 128 >> 4);
 #pragma unroll
           for (int q = 0; q < S::kKSteps; ++q) {
             const int o = (q >> 2) * (kBlock >> 4) + (q & 3) * 2;
-            tc::mma_bf16(s_at + h * 64, dq + o, kd + o, id_s, q > 0);
+            tc::mma16_ss(s_at + h * 64, dq + o, km, kd + o, km, id_s, q > 0);
           }
           tc::mma_commit(&sh.s_full[t][h]);
         }
-        __syncwarp();
       }
     }
     if (!end && !mine) WAIT(sh.k_full[st], (j / S::kStages) & 1);  // (a stage is given back after it was filled)
     // (without products of its own the warp just arrives)
-    if (tc::elect_one()) {
+    {
       if (was.any) was.mine ? tc::mma_commit(&sh.v_free[before]) : tc::bar_arrive(&sh.v_free[before]);
       if (!end) mine ? tc::mma_commit(&sh.k_free[st]) : tc::bar_arrive(&sh.k_free[st]);
       if (mine && k == nk - 1) tc::mma_commit(&sh.q_free[t]);
     }
-    __syncwarp();
     if (was.mine) ++products;
     if (end) return;
     was.any = true;
     was.mine = mine;
     was.first = k == 0;
     was.last = k == nk - 1;
+    was.look = k >= whole;
     ++j;
     ++k;
   }
@@ -292,7 +260,7 @@ __device__ __forceinline__ void softmax_role(const PromptParams& p, Sh& sh, uint
       uint32_t v[64];
       tc::tmem_ld64(s_at + 64 * h, v);
       tc::wait_ld64(v);
-      if (key0 + 64 > common) {
+      if (PROMPT_RARE(key0 + 64 > common)) {
         const int lim = limit - key0;
 #pragma unroll
         for (int e = 0; e < 64; ++e) v[e] = e < lim ? v[e] : 0xff800000u;
@@ -318,7 +286,7 @@ __device__ __forceinline__ void softmax_role(const PromptParams& p, Sh& sh, uint
         }
       }
       // O in units of the new reference (nothing is there before the first product)
-      if (k > 0 && __any_sync(0xffffffffu, move)) {
+      if (PROMPT_RARE(k > 0 && __any_sync(0xffffffffu, move))) {
         // the product of the half before (the one before that is done: these scores came after it)
         WAIT(sh.o_done[t][h ^ 1], ((it - 1) >> 1) & 1);
         tc::fence_after();
@@ -388,28 +356,24 @@ __device__ __forceinline__ void write_role(const PromptParams& p, Sh& sh, unsign
       WAIT(sh.o_full[t], n[t] & 1);
       tc::fence_after();
       ++n[t];
-#pragma unroll 1
-      for (int b = 0; b < Shape<DP>::kBlocks; ++b) {
-        const int cols = min(DP - b * 64, 64);
-#pragma unroll 1
-        for (int c = 0; c < cols; c += 16) {
-          uint32_t o[16];
-          tc::tmem_ld16(tmem + 256 + t * 128 + lanes + b * 64 + c, o);
-          uint32_t w[8];
+      // Blocks of 64 dims go through shared memory one after the other; the second one waits in registers, so that
+      // the tensor memory is free for the next item before anything is written.
+      auto read16 = [&](int c, uint32_t* w) {
+        uint32_t o[16];
+        tc::tmem_ld16(tmem + 256 + t * 128 + lanes + c, o);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float x0 = __uint_as_float(o[2 * e]) * inv, x1 = __uint_as_float(o[2 * e + 1]) * inv;
-            w[e] = pack16<BF16>(inv == 0.f ? 0.f : x0, inv == 0.f ? 0.f : x1);
-          }
+        for (int e = 0; e < 8; ++e) {
+          const float x0 = __uint_as_float(o[2 * e]) * inv, x1 = __uint_as_float(o[2 * e + 1]) * inv;
+          w[e] = pack16<BF16>(inv == 0.f ? 0.f : x0, inv == 0.f ? 0.f : x1);
+        }
+      };
+      auto put16 = [&](int c, const uint32_t* w) {
 #pragma unroll
-          for (int e = 0; e < 2; ++e)
-            *reinterpret_cast<uint4*>(stage + lane * 128 + (((c / 8 + e) ^ (lane & 7)) << 4)) =
-                make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
-        }
-        if (b == Shape<DP>::kBlocks - 1) {
-          tc::fence_before();
-          tc::bar_arrive(&sh.o_free[t]);
-        }
+        for (int e = 0; e < 2; ++e)
+          *reinterpret_cast<uint4*>(stage + lane * 128 + (((c / 8 + e) ^ (lane & 7)) << 4)) =
+              make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
+      };
+      auto flush = [&](int b) {
         __syncwarp();
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -421,8 +385,26 @@ __device__ __forceinline__ void write_role(const PromptParams& p, Sh& sh, unsign
             *reinterpret_cast<uint4*>(p.out + at * p.dim + b * 64 + c * 8) = v;
         }
         __syncwarp();
+      };
+      constexpr int kRest = DP > 64 ? DP - 64 : 0;
+      uint32_t rest[kRest / 2 + 8];
+#pragma unroll
+      for (int c = 0; c < DP - kRest; c += 16) {
+        uint32_t w[8];
+        read16(c, w);
+        put16(c, w);
       }
-      if (*reinterpret_cast<volatile int*>(&sh.odd[i % kItems])) {
+#pragma unroll
+      for (int c = 0; c < kRest; c += 16) read16(64 + c, rest + c / 2);
+      tc::fence_before();
+      tc::bar_arrive(&sh.o_free[t]);
+      flush(0);
+      if (kRest) {
+#pragma unroll
+        for (int c = 0; c < kRest; c += 16) put16(c, rest + c / 2);
+        flush(1);
+      }
+      if (PROMPT_RARE(*reinterpret_cast<volatile int*>(&sh.odd[i % kItems]))) {
         // values that are not finite and were taken out of the product, for the rows that see them
         bool there;
         const int64_t at = row_at(t, r, there);
@@ -447,38 +429,91 @@ __device__ __forceinline__ void write_role(const PromptParams& p, Sh& sh, unsign
 }
 
 // ---------------------------------------------------------------- values that some row does not see
+// sum += 0 x, two values a word
+template <bool BF16>
+__device__ __forceinline__ void add_zero_times(uint32_t& sum, uint32_t x) {
+  if (BF16)
+    asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(sum) : "r"(x), "r"(0));
+  else
+    asm("fma.rn.f16x2 %0, %1, %2, %0;" : "+r"(sum) : "r"(x), "r"(0));
+}
 template <int DP, bool BF16, class Sh>
 __device__ __forceinline__ void look_role(const PromptParams& p, Sh& sh, unsigned char* v_smem) {
   using S = Shape<DP>;
-  constexpr uint32_t kExp = BF16 ? 0x7f807f80u : 0x7c007c00u, kOne = BF16 ? 0x00800080u : 0x04000400u;
   const int lane = threadIdx.x & 31;
+  PromptTaker taker;
+  uint32_t told = 0;
+  auto tell = [&]() -> bool {
+    PromptItem& it = sh.item[told % kItems];
+    if (!prompt_wait(&sh.item_free[told % kItems], ((told / kItems) & 1) ^ 1, &sh.stop)) return false;
+    if (sh.odd[told % kItems]) {  // the notes of the item that was here (every role is done with it)
+      for (int d = lane; d < 3 * 128; d += 32) sh.first[told % kItems][0][d] = kNever;
+      __syncwarp();
+      if (lane == 0) sh.odd[told % kItems] = 0;
+    }
+    const int place = taker.take(p, sh.list, Count{p});
+    const PromptSeq& s = taker.s;
+    if (place >= 0) {
+      const int hbs = p.H >> p.log2P, log_tt = 7 - p.log2P, per = 2 << log_tt;
+      const int blocks = (s.rows + per - 1) / per;
+      const int tile = blocks - 1 - place / hbs, hb = place % hbs, tok0 = tile * per;
+      const int left = s.rows - tok0;
+      const int nk0 = key_steps(p, s, tok0 + min(left, 1 << log_tt) - 1);
+      const int nk1 = left > (1 << log_tt) ? key_steps(p, s, tok0 + min(left, per) - 1) : 0;
+      if (lane == 0) {
+        it.row0 = s.row0;
+        it.key0 = s.key0;
+        it.rows = s.rows;
+        it.keys = s.keys;
+        it.tile = tile;
+        it.hb = hb;
+        it.steps = max(nk0, nk1);
+        it.nk[0] = nk0;
+        it.nk[1] = nk1;
+      }
+    } else if (lane == 0) {
+      it.steps = 0;
+    }
+    __syncwarp();
+    if (lane == 0) tc::bar_arrive(&sh.item_full[told % kItems]);
+    __syncwarp();
+    ++told;
+    return true;
+  };
+  if (!tell()) return;
   uint32_t j = 0;
   for (uint32_t i = 0;; ++i) {
     WAIT(sh.item_full[i % kItems], (i / kItems) & 1);
     const PromptItem x = sh.item[i % kItems];
     if (x.steps == 0) return;
-    const int common = min(prompt_limit(p, x.rows, x.keys, (x.tile * 2) << (7 - p.log2P)), x.keys);
+    if (!tell()) return;  // the next one, while the first copies are under way
+    const int whole = whole_steps(p, x);
 #pragma unroll 1
     for (int k = 0; k < x.steps; ++k, ++j) {
       const int st = j % S::kStages;
       WAIT(sh.v_full[st], (j / S::kStages) & 1);
-      if ((k + 1) * kK > common) {
+      if (k >= whole) {
         unsigned char* v = v_smem + st * S::kTile;
         const int live = min(max(x.keys - k * kK, 0), kK);
-        uint32_t hit = 0;
+        // x 0 is 0 but for infinities and NaN, whose NaN stays in the sum
+        uint32_t sum[4] = {0, 0, 0, 0};
 #pragma unroll 1
         for (int b = 0; b < S::kBlocks; ++b) {
           uint4* piece = reinterpret_cast<uint4*>(v + b * kBlock);
           // four rows a turn, a piece of 8 values a lane (pieces past the dims hold zeros)
-#pragma unroll 4
+#pragma unroll 8
           for (int e = lane; e < live * 8; e += 32) {
             const uint4 w = piece[e];
-            hit |= (((w.x & kExp) + kOne) | ((w.y & kExp) + kOne)) | (((w.z & kExp) + kOne) | ((w.w & kExp) + kOne));
+            add_zero_times<BF16>(sum[0], w.x);
+            add_zero_times<BF16>(sum[1], w.y);
+            add_zero_times<BF16>(sum[2], w.z);
+            add_zero_times<BF16>(sum[3], w.w);
           }
 #pragma unroll 4
           for (int e = live * 8 + lane; e < kK * 8; e += 32) piece[e] = make_uint4(0, 0, 0, 0);
         }
-        if (__any_sync(0xffffffffu, hit & 0x80008000u)) {
+        const bool hit = ((sum[0] | sum[1] | sum[2] | sum[3]) & 0x7fff7fffu) != 0;
+        if (PROMPT_RARE(__any_sync(0xffffffffu, hit))) {
           if (lane == 0) *reinterpret_cast<volatile int*>(&sh.odd[i % kItems]) = 1;
 #pragma unroll 1
           for (int e = lane; e < S::kBlocks * live * 8; e += 32) {
@@ -494,9 +529,11 @@ __device__ __forceinline__ void look_role(const PromptParams& p, Sh& sh, unsigne
           }
         }
         tc::fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) tc::bar_arrive(&sh.v_ready[st]);
       }
-      __syncwarp();
-      if (lane == 0) tc::bar_arrive(&sh.v_ready[st]);
+      // (the stage is not filled again before it was waited for here)
+      if (lane == 0) tc::bar_arrive(&sh.v_free[st]);
     }
     if (lane == 0) tc::bar_arrive(&sh.item_free[i % kItems]);
   }
@@ -535,7 +572,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc::bar_init(&sh.k_free[k], 2);
       tc::bar_init(&sh.v_full[k], 1);
       tc::bar_init(&sh.v_ready[k], 1);
-      tc::bar_init(&sh.v_free[k], 2);
+      tc::bar_init(&sh.v_free[k], 3);
     }
     for (int k = 0; k < kItems; ++k) {
       tc::bar_init(&sh.item_full[k], 1);
@@ -566,7 +603,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       load_role<DP>(p, sh, map_q, map_k, map_v, q_smem, k_smem, v_smem);
     else if (warp == 15)
       look_role<DP, BF16>(p, sh, v_smem);
-    else
+    else if (tc::elect_one())
       issue_role<DP, BF16>(p, sh, tc::su32(q_smem), tc::su32(k_smem), tc::su32(v_smem), tmem, warp == 14);
   }
   __syncthreads();
@@ -581,7 +618,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   }
   __syncthreads();
-  if (threadIdx.x == 0) prompt_leave(p, gridDim.x);
+  if (threadIdx.x == 0) prompt_leave(p, gridDim.x, sh.stop);
   if (warp == 12) tc::tmem_dealloc(tmem, 512);
 }
 

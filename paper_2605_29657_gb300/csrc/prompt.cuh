@@ -97,51 +97,65 @@ __device__ __forceinline__ void prompt_list(const PromptParams& p, PromptList& l
   }
   __syncthreads();
 }
-// One warp: the sequence of item `at` (below first[kChunks]) and its place among that sequence's items.
-template <class Count>
-__device__ __forceinline__ PromptSeq prompt_find(const PromptParams& p, const PromptList& l, const Count& count, int at, int* place) {
-  const int lane = threadIdx.x & 31, per = (p.n + kChunks - 1) / kChunks;
-  int before = 0;
-#pragma unroll
-  for (int k = 0; k < kChunks / 32; ++k) before += l.first[k * 32 + lane + 1] <= at;
-  const int c = __reduce_add_sync(0xffffffffu, before);
-  int base = l.first[c];
-  const int end = min((c + 1) * per, p.n);
+// A CTA's items, taken by one warp: the next one is asked for when one is taken, so that the counter's latency is hidden,
+// and the sequence is looked up only where it changes.
+struct PromptTaker {
+  int next;        // lane 0: the next item (its block's own first)
+  int begin, end;  // the present sequence's items
   PromptSeq s;
-  for (int i = c * per; i < end; i += 32) {
-    s.rows = s.keys = 0;
-    s.row0 = s.key0 = 0;
-    int mine = 0;
-    if (i + lane < end) {
-      s = prompt_seq(p, i + lane);
-      mine = count(s);
-    }
-    int incl = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int x = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += x;
-    }
-    const unsigned past = __ballot_sync(0xffffffffu, at < base + incl);
-    if (past) {
-      const int from = __ffs(past) - 1;
-      *place = at - base - __shfl_sync(0xffffffffu, incl - mine, from);
-      s.row0 = __shfl_sync(0xffffffffu, s.row0, from);
-      s.key0 = __shfl_sync(0xffffffffu, s.key0, from);
-      s.rows = __shfl_sync(0xffffffffu, s.rows, from);
-      s.keys = __shfl_sync(0xffffffffu, s.keys, from);
-      return s;
-    }
-    base += __shfl_sync(0xffffffffu, incl, 31);
+
+  __device__ __forceinline__ PromptTaker() : next(blockIdx.x), begin(0), end(0) { s.row0 = s.key0 = s.rows = s.keys = 0; }
+  // The item's place among those of sequence s; -1: there is none. COUNT(seq) gives a sequence's items.
+  template <class Count>
+  __device__ __forceinline__ int take(const PromptParams& p, const PromptList& l, const Count& count) {
+    const int lane = threadIdx.x & 31, at = __shfl_sync(0xffffffffu, next, 0);
+    if (at >= l.first[kChunks]) return -1;
+    if (lane == 0) next = gridDim.x + atomicAdd(&p.counters[0], 1);
+    if (at < begin || at >= end) find(p, l, count, at);
+    return at - begin;
   }
-  *place = 0;  // (not reached)
-  s.rows = s.keys = 0;
-  return s;
-}
+  template <class Count>
+  __device__ __forceinline__ void find(const PromptParams& p, const PromptList& l, const Count& count, int at) {
+    const int lane = threadIdx.x & 31, per = (p.n + kChunks - 1) / kChunks;
+    int before = 0;
+#pragma unroll
+    for (int k = 0; k < kChunks / 32; ++k) before += l.first[k * 32 + lane + 1] <= at;
+    const int c = __reduce_add_sync(0xffffffffu, before);
+    int base = l.first[c];
+    for (int i = c * per; i < min((c + 1) * per, p.n); i += 32) {
+      PromptSeq x;
+      x.row0 = x.key0 = x.rows = x.keys = 0;
+      int mine = 0;
+      if (i + lane < min((c + 1) * per, p.n)) {
+        x = prompt_seq(p, i + lane);
+        mine = count(x);
+      }
+      int incl = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += y;
+      }
+      const unsigned past = __ballot_sync(0xffffffffu, at < base + incl);
+      if (past) {
+        const int from = __ffs(past) - 1;
+        end = base + __shfl_sync(0xffffffffu, incl, from);
+        begin = end - __shfl_sync(0xffffffffu, mine, from);
+        s.row0 = __shfl_sync(0xffffffffu, x.row0, from);
+        s.key0 = __shfl_sync(0xffffffffu, x.key0, from);
+        s.rows = __shfl_sync(0xffffffffu, x.rows, from);
+        s.keys = __shfl_sync(0xffffffffu, x.keys, from);
+        return;
+      }
+      base += __shfl_sync(0xffffffffu, incl, 31);
+    }
+  }
+};
 
 // The last CTA to leave clears the counters, whatever happened: the next call has to find zeros. By one thread,
-// after the CTA's last item was taken.
-__device__ __forceinline__ void prompt_leave(const PromptParams& p, int ctas) {
+// after the CTA's last item was taken. stop: a wait ran out.
+__device__ __forceinline__ void prompt_leave(const PromptParams& p, int ctas, int stop) {
+  if (stop) set_status(p.status, OCCAM_ERR_TIMEOUT);
   if (atomicAdd(&p.counters[1], 1) == ctas - 1) {
     p.counters[0] = 0;
     p.counters[1] = 0;
@@ -149,20 +163,22 @@ __device__ __forceinline__ void prompt_leave(const PromptParams& p, int ctas) {
 }
 
 constexpr uint64_t kPromptWaitNs = 2000000000ull;
-// a bounded wait on a barrier phase; false (recorded) if it ran out or another role gave up
-__device__ __forceinline__ bool prompt_wait_long(uint64_t* bar, uint32_t parity, volatile int* stop, int32_t* status) {
-  const uint64_t t0 = tc::globaltimer();
-  while (!tc::bar_try(bar, parity)) {
-    if (*stop || tc::globaltimer() - t0 > kPromptWaitNs) {
+constexpr uint32_t kPromptTries = 1u << 21;  // of a wait: a second or so
+// A bounded wait on a barrier phase; false if it ran out or another role gave up. (Few instructions: the roles together have
+// to stay within the instruction cache. What went wrong is recorded when the CTA ends.)
+__device__ __forceinline__ bool prompt_wait(uint64_t* bar, uint32_t parity, volatile int* stop) {
+  if (__builtin_expect(tc::bar_try(bar, parity), 1)) return true;
+  for (uint32_t n = 0; !tc::bar_try(bar, parity); ++n)
+    if (n > kPromptTries || *stop) {
       *stop = 1;
-      set_status(status, OCCAM_ERR_TIMEOUT);
       return false;
     }
-  }
   return true;
 }
 #define PROMPT_WAIT(bar, parity) \
-  if (!tc::bar_try(&(bar), (parity)) && !prompt_wait_long(&(bar), (parity), &sh.stop, p.status)) return;
+  if (__builtin_expect(!prompt_wait(&(bar), (parity), &sh.stop), 0)) return;
+// a branch whose code is put out of the way of the loop's
+#define PROMPT_RARE(x) __builtin_expect(!!(x), 0)
 
 template <bool BF16>
 __device__ __forceinline__ uint32_t pack16(float lo, float hi) {

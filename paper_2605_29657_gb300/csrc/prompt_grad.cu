@@ -21,7 +21,7 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kItems = 3;           // items known ahead
-constexpr int kRegElement = 184, kRegWrite = 80, kRegIssue = 64;  // 2 x 184 + 80 + 64 = 4 x 128
+constexpr int kRegElement = 176, kRegWrite = 80, kRegIssue = 80;  // 2 x 176 + 80 + 80 = 4 x 128
 constexpr int kRowBytes = 128;      // of 64 dims in a block
 
 struct GradParams : PromptParams {
@@ -233,33 +233,85 @@ struct Count {
   __device__ __forceinline__ int operator()(const PromptSeq& s) const { return (s.keys / 128 + (s.keys % 128 != 0)) * p.Hkv; }
 };
 
-// the step's place: head block and token block
-struct Place {
+// A walk over an item's steps: blocks of tokens, head block by head block.
+struct Steps {
   int head, tok;  // first head, first token
+  int tok0, tokens, more;
+
+  __device__ __forceinline__ Steps(const GradParams& p, const PromptItem& it, int log_p) {
+    tokens = 1 << (6 - log_p);
+    more = it.rows;
+    tok0 = tok = it.nk[0] << (6 - log_p);
+    head = it.hb * p.G;
+  }
+  __device__ __forceinline__ void next(int log_p) {
+    tok += tokens;
+    if (tok >= more) {
+      tok = tok0;
+      head += 1 << log_p;
+    }
+  }
 };
-__device__ __forceinline__ Place place_of(const GradParams& p, const PromptItem& it, int log_p, int k) {
-  const int log_t = 6 - log_p, blocks = ((it.rows + (1 << log_t) - 1) >> log_t) - it.nk[0];
-  const int hb = k / blocks;
-  return Place{it.hb * p.G + (hb << log_p), (it.nk[0] + k - hb * blocks) << log_t};
-}
 
 template <int DP, class Sh>
 __device__ __forceinline__ void load_role(const GradParams& p, Sh& sh, int log_p, const CUtensorMap& map_q, const CUtensorMap& map_do,
                                           const CUtensorMap& map_k, const CUtensorMap& map_v, const CUtensorMap& map_terms,
                                           unsigned char* k_smem, unsigned char* v_smem, unsigned char* q_smem, unsigned char* more) {
   using S = Shape<DP>;
-  const int lane = threadIdx.x & 31, total = sh.list.first[kChunks];
-  const Count count{p};
-  int next = blockIdx.x;
+  const int lane = threadIdx.x & 31;
+  uint32_t n = 0, turn = 1;
+  int st = 0;
+  for (uint32_t i = 0;; ++i) {
+    WAIT(sh.item_full[i % kItems], (i / kItems) & 1);
+    const PromptItem it = sh.item[i % kItems];
+    if (it.nk[1]) return;
+    if (it.steps > 0) {
+      const int key = (int)(it.key0 + (int64_t)it.tile * 128);
+      WAIT(sh.kv_free, (n & 1) ^ 1);
+      ++n;
+      if (lane == 0) {
+        tc::bar_expect_tx(&sh.kv_full, 2 * S::kTile);
+        for (int b = 0; b < S::kBlocks; ++b) {
+          tc::tma_load_3d(k_smem + b * 128 * kRowBytes, &map_k, b * 64, it.hb, key, &sh.kv_full);
+          tc::tma_load_3d(v_smem + b * 128 * kRowBytes, &map_v, b * 64, it.hb, key, &sh.kv_full);
+        }
+      }
+    }
+    Steps at(p, it, log_p);
+    const int row = (int)it.row0;
+#pragma unroll 1
+    for (int k = 0; k < it.steps; ++k, at.next(log_p)) {
+      WAIT(sh.free[st], turn);
+      if (lane == 0) {
+        tc::bar_expect_tx(&sh.full[st], S::kTile + kMoreBytes);  // 64 rows of Q and of dO
+        tc::tma_load_3d(more + st * kMoreBytes, &map_terms, 0, at.head, row + at.tok, &sh.full[st]);
+        unsigned char* to = q_smem + st * S::kTile;
+        for (int b = 0; b < S::kBlocks; ++b) {
+          tc::tma_load_3d(to + b * kQ * kRowBytes, &map_q, b * 64, at.head, row + at.tok, &sh.full[st]);
+          tc::tma_load_3d(to + S::kHalf + b * kQ * kRowBytes, &map_do, b * 64, at.head, row + at.tok, &sh.full[st]);
+        }
+      }
+      __syncwarp();
+      if (++st == S::kStages) st = 0, turn ^= 1;
+    }
+    if (lane == 0) tc::bar_arrive(&sh.item_free[i % kItems]);
+    __syncwarp();
+  }
+}
+
+// Rows past the sequence's end become zeros, terms and all: P is finite there, dP is 0.
+template <int DP, class Sh>
+__device__ __forceinline__ void look_role(const GradParams& p, Sh& sh, int log_p, unsigned char* q_smem, unsigned char* more) {
+  using S = Shape<DP>;
+  const int lane = threadIdx.x & 31;
+  PromptTaker taker;
   uint32_t told = 0;
   auto tell = [&]() -> bool {
     PromptItem& it = sh.item[told % kItems];
-    if (!tc::bar_try(&sh.item_free[told % kItems], ((told / kItems) & 1) ^ 1) &&
-        !prompt_wait_long(&sh.item_free[told % kItems], ((told / kItems) & 1) ^ 1, &sh.stop, p.status))
-      return false;
-    if (next < total) {
-      int place = 0;
-      const PromptSeq s = prompt_find(p, sh.list, count, next, &place);
+    if (!prompt_wait(&sh.item_free[told % kItems], ((told / kItems) & 1) ^ 1, &sh.stop)) return false;
+    const int place = taker.take(p, sh.list, Count{p});
+    const PromptSeq& s = taker.s;
+    if (place >= 0) {
       const int tile = place / p.Hkv, log_t = 6 - log_p;
       const int first = (p.causal ? max(tile * 128 - (s.keys - s.rows), 0) : 0) >> log_t;
       const int blocks = ((s.rows + (1 << log_t) - 1) >> log_t) - first;
@@ -273,9 +325,7 @@ __device__ __forceinline__ void load_role(const GradParams& p, Sh& sh, int log_p
         it.steps = max(blocks, 0) * (p.G >> log_p);
         it.nk[0] = first;
         it.nk[1] = 0;
-        next = gridDim.x + atomicAdd(&p.counters[0], 1);
       }
-      next = __shfl_sync(0xffffffffu, next, 0);
     } else if (lane == 0) {
       it.steps = 0;
       it.nk[1] = 1;
@@ -287,52 +337,11 @@ __device__ __forceinline__ void load_role(const GradParams& p, Sh& sh, int log_p
     return true;
   };
   if (!tell()) return;
-  uint32_t j = 0, n = 0;
-  for (uint32_t i = 0;; ++i) {
-    const PromptItem it = sh.item[i % kItems];
-    if (it.nk[1]) break;
-    if (!tell()) return;
-    if (it.steps > 0) {
-      const int key = (int)(it.key0 + (int64_t)it.tile * 128);
-      WAIT(sh.kv_free, (n & 1) ^ 1);
-      ++n;
-      if (lane == 0) {
-        tc::bar_expect_tx(&sh.kv_full, 2 * S::kTile);
-        for (int b = 0; b < S::kBlocks; ++b) {
-          tc::tma_load_3d(k_smem + b * 128 * kRowBytes, &map_k, b * 64, it.hb, key, &sh.kv_full);
-          tc::tma_load_3d(v_smem + b * 128 * kRowBytes, &map_v, b * 64, it.hb, key, &sh.kv_full);
-        }
-      }
-    }
-    for (int k = 0; k < it.steps; ++k, ++j) {
-      const int st = j % S::kStages;
-      const Place at = place_of(p, it, log_p, k);
-      WAIT(sh.free[st], ((j / S::kStages) & 1) ^ 1);
-      if (lane == 0) {
-        tc::bar_expect_tx(&sh.full[st], S::kTile + kMoreBytes);  // 64 rows of Q and of dO
-        tc::tma_load_3d(more + st * kMoreBytes, &map_terms, 0, at.head, (int)(it.row0 + at.tok), &sh.full[st]);
-        unsigned char* to = q_smem + st * S::kTile;
-        for (int b = 0; b < S::kBlocks; ++b) {
-          tc::tma_load_3d(to + b * kQ * kRowBytes, &map_q, b * 64, at.head, (int)(it.row0 + at.tok), &sh.full[st]);
-          tc::tma_load_3d(to + S::kHalf + b * kQ * kRowBytes, &map_do, b * 64, at.head, (int)(it.row0 + at.tok), &sh.full[st]);
-        }
-      }
-      __syncwarp();
-    }
-    if (lane == 0) tc::bar_arrive(&sh.item_free[i % kItems]);
-    __syncwarp();
-  }
-}
-
-// Rows past the sequence's end become zeros, terms and all: P is finite there, dP is 0.
-template <int DP, class Sh>
-__device__ __forceinline__ void look_role(const GradParams& p, Sh& sh, int log_p, unsigned char* q_smem, unsigned char* more) {
-  using S = Shape<DP>;
-  const int lane = threadIdx.x & 31;
   uint32_t j = 0;
   for (uint32_t i = 0;; ++i) {
     WAIT(sh.item_full[i % kItems], (i / kItems) & 1);
     if (sh.item[i % kItems].nk[1]) return;
+    if (!tell()) return;  // the next one, while the first copies are under way
     const int steps = sh.item[i % kItems].steps, rows = sh.item[i % kItems].rows, first = sh.item[i % kItems].nk[0];
     const int log_t = 6 - log_p, blocks = ((rows + (1 << log_t) - 1) >> log_t) - first;
     const int last = (rows & ((1 << log_t) - 1)) << log_p;  // rows of the last block of tokens, 0: it is whole
@@ -352,10 +361,12 @@ __device__ __forceinline__ void look_role(const GradParams& p, Sh& sh, int log_p
           uint4* row = reinterpret_cast<uint4*>(more + st * kMoreBytes);
           for (int e = last * 2 + lane; e < kQ * 2; e += 32) row[e] = make_uint4(0, 0, 0, 0);
           tc::fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) tc::bar_arrive(&sh.ready[st]);
         }
       }
-      __syncwarp();
-      if (lane == 0) tc::bar_arrive(&sh.ready[st]);
+      // (the stage is not filled again before it was waited for here)
+      if (lane == 0) tc::bar_arrive(&sh.free[st]);
     }
     if (lane == 0) tc::bar_arrive(&sh.item_free[i % kItems]);
   }
@@ -365,20 +376,25 @@ __device__ __forceinline__ void look_role(const GradParams& p, Sh& sh, int log_p
 // dP^T of step j + 2.
 template <int DP, bool BF16, class Sh>
 __device__ __forceinline__ void issue_role(const GradParams& p, Sh& sh, uint32_t k_smem, uint32_t v_smem, uint32_t q_smem, uint32_t units,
-                                           uint32_t more, uint32_t tmem, uint32_t b) {
+                                           uint32_t more, uint32_t tmem, int log_p, uint32_t b) {
   using S = Shape<DP>;
   constexpr uint32_t id_s = tc::idesc16(BF16, 128, kQ, false), id_o = tc::idesc16(BF16, 128, DP, true);
-  const uint64_t dk = tc::sdesc_sw128(k_smem), dv = tc::sdesc_sw128(v_smem);
-  const uint64_t dq = tc::sdesc_sw128(q_smem), dqt = tc::sdesc_mn_sw128(q_smem, kQ * kRowBytes);
+  const uint64_t kmajor = tc::sdesc_sw128(0), mnmajor = tc::sdesc_mn_sw128(0, kQ * kRowBytes), narrow = tc::sdesc_sw32(0);
+  const uint32_t km = tc::desc_hi(kmajor), mn = tc::desc_hi(mnmajor), nm = tc::desc_hi(narrow);
+  const uint32_t dk = (uint32_t)kmajor + (k_smem >> 4), dv = (uint32_t)kmajor + (v_smem >> 4);
+  const uint32_t dq = (uint32_t)kmajor + (q_smem >> 4), dqt = (uint32_t)mnmajor + (q_smem >> 4);
   // (Both 16-byte pieces of a row of units are the same, and one of a row of terms is 0: the order in which the
   // swizzle puts them does not matter.)
-  const uint64_t du = tc::sdesc_sw32(units), dm = tc::sdesc_sw32(more);
+  const uint32_t du = (uint32_t)narrow + (units >> 4), dm = (uint32_t)narrow + (more >> 4);
   const uint32_t s_at = tmem + b * 128, dp_at = s_at + 64, dv_at = tmem + 256, dk_at = tmem + 384;
   // a walk over the steps of this parity
   uint32_t i = 0, j = b;       // items begun; the next own step
   uint32_t base = 0, end = 0;  // the present item's steps
   uint32_t n_kv = 0, kv = 0;   // items with steps: begun; whose keys and values were waited for
   uint32_t done = 0;           // own steps so far
+  uint32_t looked = 0;         // a bit a stage: how often (mod 2) its rows were looked at
+  int block = 0, blocks = 1;   // of the next own step; in a head block
+  bool ragged = false;         // a head block's last block has rows past the end
   struct {
     bool any, first, last;
     uint32_t stage, j, items;
@@ -389,13 +405,19 @@ __device__ __forceinline__ void issue_role(const GradParams& p, Sh& sh, uint32_t
     bool over = false, have = j < end;
     if (!have) {
       // the item's keys and values are done with once the scores issued so far are
-      if (end > base && tc::elect_one()) tc::mma_commit(&sh.kv_free);
-      if (i > 0 && tc::elect_one()) tc::bar_arrive(&sh.item_free[(i - 1) % kItems]);
-      __syncwarp();
+      if (end > base) tc::mma_commit(&sh.kv_free);
+      if (i > 0) tc::bar_arrive(&sh.item_free[(i - 1) % kItems]);
       WAIT(sh.item_full[i % kItems], (i / kItems) & 1);
       over = sh.item[i % kItems].nk[1] != 0;
       base = end;
-      if (!over) end = base + sh.item[i % kItems].steps;
+      if (!over) {
+        const PromptItem& x = sh.item[i % kItems];
+        const int log_t = 6 - log_p;
+        end = base + x.steps;
+        blocks = max(((x.rows + (1 << log_t) - 1) >> log_t) - x.nk[0], 1);
+        block = (int)(j - base);  // 0 or 1, or more where there is no own step
+        ragged = (x.rows & ((1 << log_t) - 1)) != 0;
+      }
       if (end > base) ++n_kv;
       ++i;
       have = j < end;
@@ -406,56 +428,60 @@ __device__ __forceinline__ void issue_role(const GradParams& p, Sh& sh, uint32_t
       if (was.j > 0) WAIT(sh.added[b ^ 1], ((was.j - 1) >> 1) & 1);  // the step before it
       if (was.first) WAIT(sh.o_free, (was.items & 1) ^ 1);           // (after that: the items before have begun)
       tc::fence_after();
-      if (tc::elect_one()) {
-        const uint64_t d = dqt + was.stage * (S::kTile >> 4) + (S::kHalf >> 4);
+      {
+        const uint32_t d = dqt + was.stage * (S::kTile >> 4) + (S::kHalf >> 4);
 #pragma unroll
         for (int q = 0; q < kQ / 16; ++q)
-          tc::mma_ts(dv_at, s_at + q * 8, d + q * (16 * kRowBytes >> 4), id_o, q > 0 || !was.first ? 1u : 0u);
+          tc::mma16_ts(dv_at, s_at + q * 8, d + q * (16 * kRowBytes >> 4), mn, id_o, q > 0 || !was.first);
       }
-      __syncwarp();
     }
     if (have) {
       for (; kv < n_kv; ++kv) WAIT(sh.kv_full, kv & 1);  // (every phase, those of items without own steps too)
-      WAIT(sh.ready[st], (j / S::kStages) & 1);
+      WAIT(sh.full[st], (j / S::kStages) & 1);
+      while (block >= blocks) block -= blocks;
+      if (ragged && block == blocks - 1) {
+        WAIT(sh.ready[st], (looked >> st) & 1);
+        looked ^= 1u << st;
+      }
+      block += 2;
       tc::fence_after();
-      if (tc::elect_one()) {
-        const uint64_t d = dq + st * (S::kTile >> 4);
+      {
+        const uint32_t d = dq + st * (S::kTile >> 4);
 #pragma unroll
         for (int q = 0; q < DP / 16; ++q)
-          tc::mma_bf16(s_at, dk + (q >> 2) * (128 * kRowBytes >> 4) + (q & 3) * 2, d + (q >> 2) * (kQ * kRowBytes >> 4) + (q & 3) * 2, id_s, q > 0);
-        tc::mma_bf16(s_at, du, dm + st * (kMoreBytes >> 4), id_s, 1);
+          tc::mma16_ss(s_at, dk + (q >> 2) * (128 * kRowBytes >> 4) + (q & 3) * 2, km,
+                       d + (q >> 2) * (kQ * kRowBytes >> 4) + (q & 3) * 2, km, id_s, q > 0);
+        tc::mma16_ss(s_at, du, nm, dm + st * (kMoreBytes >> 4), nm, id_s, true);
         tc::mma_commit(&sh.s_full[b]);
       }
-      __syncwarp();
     }
     if (was.any) {
       WAIT(sh.ds_full[b], (done - 1) & 1);
       tc::fence_after();
-      if (tc::elect_one()) {
-        const uint64_t d = dqt + was.stage * (S::kTile >> 4);
+      {
+        const uint32_t d = dqt + was.stage * (S::kTile >> 4);
 #pragma unroll
         for (int q = 0; q < kQ / 16; ++q)
-          tc::mma_ts(dk_at, dp_at + q * 8, d + q * (16 * kRowBytes >> 4), id_o, q > 0 || !was.first ? 1u : 0u);
+          tc::mma16_ts(dk_at, dp_at + q * 8, d + q * (16 * kRowBytes >> 4), mn, id_o, q > 0 || !was.first);
         tc::mma_commit(&sh.added[b]);
         tc::mma_commit(&sh.free[was.stage]);
         if (was.last) tc::mma_commit(&sh.o_full);
       }
-      __syncwarp();
     }
     if (over) return;
     if (!have) {
       was.any = false;
       continue;
     }
-    if (tc::elect_one()) {
-      const uint64_t d = dq + st * (S::kTile >> 4) + (S::kHalf >> 4);
+    {
+      const uint32_t d = dq + st * (S::kTile >> 4) + (S::kHalf >> 4);
 #pragma unroll
       for (int q = 0; q < DP / 16; ++q)
-        tc::mma_bf16(dp_at, dv + (q >> 2) * (128 * kRowBytes >> 4) + (q & 3) * 2, d + (q >> 2) * (kQ * kRowBytes >> 4) + (q & 3) * 2, id_s, q > 0);
-      tc::mma_bf16(dp_at, du + (kUnitBytes >> 4), dm + st * (kMoreBytes >> 4), id_s, 1);
+        tc::mma16_ss(dp_at, dv + (q >> 2) * (128 * kRowBytes >> 4) + (q & 3) * 2, km,
+                     d + (q >> 2) * (kQ * kRowBytes >> 4) + (q & 3) * 2, km, id_s, q > 0);
+      tc::mma16_ss(dp_at, du + (kUnitBytes >> 4), nm, dm + st * (kMoreBytes >> 4), nm, id_s, true);
       tc::mma_commit(&sh.dp_full[b]);
     }
-    __syncwarp();
     was.any = true;
     was.first = j == base;
     was.last = j + 1 == end;
@@ -480,10 +506,10 @@ __device__ __forceinline__ void element_role(const GradParams& p, Sh& sh, int lo
     if (it.nk[1]) return;
     const int key = it.tile * 128 + r, ahead = it.keys - it.rows;  // keys before the first row's own
     const float power = BF16 || it.steps == 0 ? 1.f : p.power[it.row0 * p.Hkv + it.hb] * Lift<BF16>::kBack;
+    Steps at(p, it, log_p);
 #pragma unroll 1
-    for (int k = 0; k < it.steps; ++k, ++j) {
+    for (int k = 0; k < it.steps; ++k, ++j, at.next(log_p)) {
       if ((j & 1) != b) continue;
-      const Place at = place_of(p, it, log_p, k);
       WAIT(sh.s_full[b], done & 1);
       tc::fence_after();
       uint32_t v[64];
@@ -498,7 +524,7 @@ __device__ __forceinline__ void element_role(const GradParams& p, Sh& sh, int lo
         pr[2 * e + 1] = fast_exp2(y.y);
       }
       // keys that some row of the block does not see (all keys past the sequence's end are nobody's: their rows are not written)
-      if (p.causal && it.tile * 128 + 127 > ahead + at.tok) {
+      if (PROMPT_RARE(p.causal && it.tile * 128 + 127 > ahead + at.tok)) {
         const int lo = min(max(key - ahead - at.tok, 0), kQ) << log_p;  // the first row of the block that sees this key
 #pragma unroll
         for (int e = 0; e < 64; ++e) pr[e] = e < lo ? 0.f : pr[e];
@@ -613,7 +639,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int k = 0; k < S::kStages; ++k) {
       tc::bar_init(&sh.full[k], 1);
       tc::bar_init(&sh.ready[k], 1);
-      tc::bar_init(&sh.free[k], 1);
+      tc::bar_init(&sh.free[k], 2);
     }
     for (int k = 0; k < 2; ++k) {
       tc::bar_init(&sh.s_full[k], 1);
@@ -650,8 +676,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       load_role<DP>(p, sh, log_p, map_q, map_do, map_k, map_v, map_terms, k_smem, v_smem, q_smem, more);
     else if (warp == 15)
       look_role<DP>(p, sh, log_p, q_smem, more);
-    else
-      issue_role<DP, BF16>(p, sh, tc::su32(k_smem), tc::su32(v_smem), tc::su32(q_smem), tc::su32(units), tc::su32(more), tmem,
+    else if (tc::elect_one())
+      issue_role<DP, BF16>(p, sh, tc::su32(k_smem), tc::su32(v_smem), tc::su32(q_smem), tc::su32(units), tc::su32(more), tmem, log_p,
                            warp == 14);
   }
   __syncthreads();
@@ -663,7 +689,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc::bar_wait(k / 2 < S::kStages ? &sh.full[k / 2] : &sh.kv_full, k & 1, nullptr, kPromptWaitNs / 16);
   }
   __syncthreads();
-  if (threadIdx.x == 0) prompt_leave(p, gridDim.x);
+  if (threadIdx.x == 0) prompt_leave(p, gridDim.x, sh.stop);
   if (warp == 12) tc::tmem_dealloc(tmem, 512);
 }
 
@@ -712,52 +738,12 @@ __device__ __forceinline__ void load_role(const GradParams& p, Sh& sh, const CUt
                                           const CUtensorMap& map_k, const CUtensorMap& map_v, unsigned char* q_smem,
                                           unsigned char* do_smem, unsigned char* k_smem, unsigned char* v_smem) {
   using S = Shape<DP>;
-  const int lane = threadIdx.x & 31, total = sh.list.first[kChunks];
-  const Count count{p};
-  int next = blockIdx.x;
-  uint32_t told = 0;
-  auto tell = [&]() -> bool {
-    PromptItem& it = sh.item[told % kItems];
-    if (!tc::bar_try(&sh.item_free[told % kItems], ((told / kItems) & 1) ^ 1) &&
-        !prompt_wait_long(&sh.item_free[told % kItems], ((told / kItems) & 1) ^ 1, &sh.stop, p.status))
-      return false;
-    if (next < total) {
-      int place = 0;
-      const PromptSeq s = prompt_find(p, sh.list, count, next, &place);
-      const int hbs = p.H >> p.log2P, log_tt = 7 - p.log2P, per = 2 << log_tt;
-      const int blocks = (s.rows + per - 1) / per;
-      const int tile = blocks - 1 - place / hbs, hb = place % hbs, tok0 = tile * per;
-      const int left = s.rows - tok0;
-      const int nk0 = key_steps(p, s, tok0 + min(left, 1 << log_tt) - 1);
-      const int nk1 = left > (1 << log_tt) ? key_steps(p, s, tok0 + min(left, per) - 1) : 0;
-      if (lane == 0) {
-        it.row0 = s.row0;
-        it.key0 = s.key0;
-        it.rows = s.rows;
-        it.keys = s.keys;
-        it.tile = tile;
-        it.hb = hb;
-        it.steps = max(nk0, nk1);
-        it.nk[0] = nk0;
-        it.nk[1] = nk1;
-        next = gridDim.x + atomicAdd(&p.counters[0], 1);
-      }
-      next = __shfl_sync(0xffffffffu, next, 0);
-    } else if (lane == 0) {
-      it.steps = 0;
-    }
-    __syncwarp();
-    if (lane == 0) tc::bar_arrive(&sh.item_full[told % kItems]);
-    __syncwarp();
-    ++told;
-    return true;
-  };
-  if (!tell()) return;
+  const int lane = threadIdx.x & 31;
   uint32_t j = 0, nq[2] = {0, 0};
   for (uint32_t i = 0;; ++i) {
+    WAIT(sh.item_full[i % kItems], (i / kItems) & 1);
     const PromptItem it = sh.item[i % kItems];
-    if (it.steps == 0) break;
-    if (!tell()) return;
+    if (it.steps == 0) return;
     const int tt = 128 >> p.log2P, head = it.hb << p.log2P, kv = head / p.G;
     for (int k = 0; k < it.steps; ++k, ++j) {
       const int st = j % S::kStages;
@@ -803,25 +789,64 @@ template <int DP, class Sh>
 __device__ __forceinline__ void look_role(const GradParams& p, Sh& sh, unsigned char* k_smem) {
   using S = Shape<DP>;
   const int lane = threadIdx.x & 31;
+  PromptTaker taker;
+  uint32_t told = 0;
+  auto tell = [&]() -> bool {
+    PromptItem& it = sh.item[told % kItems];
+    if (!prompt_wait(&sh.item_free[told % kItems], ((told / kItems) & 1) ^ 1, &sh.stop)) return false;
+    const int place = taker.take(p, sh.list, Count{p});
+    const PromptSeq& s = taker.s;
+    if (place >= 0) {
+      const int hbs = p.H >> p.log2P, log_tt = 7 - p.log2P, per = 2 << log_tt;
+      const int blocks = (s.rows + per - 1) / per;
+      const int tile = blocks - 1 - place / hbs, hb = place % hbs, tok0 = tile * per;
+      const int left = s.rows - tok0;
+      const int nk0 = key_steps(p, s, tok0 + min(left, 1 << log_tt) - 1);
+      const int nk1 = left > (1 << log_tt) ? key_steps(p, s, tok0 + min(left, per) - 1) : 0;
+      if (lane == 0) {
+        it.row0 = s.row0;
+        it.key0 = s.key0;
+        it.rows = s.rows;
+        it.keys = s.keys;
+        it.tile = tile;
+        it.hb = hb;
+        it.steps = max(nk0, nk1);
+        it.nk[0] = nk0;
+        it.nk[1] = nk1;
+      }
+    } else if (lane == 0) {
+      it.steps = 0;
+    }
+    __syncwarp();
+    if (lane == 0) tc::bar_arrive(&sh.item_full[told % kItems]);
+    __syncwarp();
+    ++told;
+    return true;
+  };
+  if (!tell()) return;
   uint32_t j = 0;
   for (uint32_t i = 0;; ++i) {
     WAIT(sh.item_full[i % kItems], (i / kItems) & 1);
     const int steps = sh.item[i % kItems].steps, keys = sh.item[i % kItems].keys;
     if (steps == 0) return;
+    if (!tell()) return;  // the next one, while the first copies are under way
+    const int whole = keys / kKeys;
 #pragma unroll 1
     for (int k = 0; k < steps; ++k, ++j) {
       const int st = j % S::kStages, live = max(keys - k * kKeys, 0);
       WAIT(sh.k_full[st], (j / S::kStages) & 1);
-      if (live < kKeys) {
+      if (k >= whole) {
 #pragma unroll 1
         for (int b = 0; b < S::kBlocks; ++b) {
           uint4* piece = reinterpret_cast<uint4*>(k_smem + st * S::kHalf + b * kKeys * kRowBytes);
           for (int e = live * 8 + lane; e < kKeys * 8; e += 32) piece[e] = make_uint4(0, 0, 0, 0);
         }
         tc::fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) tc::bar_arrive(&sh.k_ready[st]);
       }
-      __syncwarp();
-      if (lane == 0) tc::bar_arrive(&sh.k_ready[st]);
+      // (the stage is not filled again before it was waited for here)
+      if (lane == 0) tc::bar_arrive(&sh.k_free[st]);
     }
     if (lane == 0) tc::bar_arrive(&sh.item_free[i % kItems]);
   }
@@ -832,22 +857,25 @@ __device__ __forceinline__ void issue_role(const GradParams& p, Sh& sh, uint32_t
                                            uint32_t tmem, int t) {
   using S = Shape<DP>;
   constexpr uint32_t id_s = tc::idesc16(BF16, 128, kKeys, false), id_o = tc::idesc16(BF16, 128, DP, true);
-  const uint64_t dq = tc::sdesc_sw128(q_smem + t * S::kTile), ddo = tc::sdesc_sw128(do_smem + t * S::kTile);
-  const uint64_t dk = tc::sdesc_sw128(k_smem), dv = tc::sdesc_sw128(v_smem), dkt = tc::sdesc_mn_sw128(k_smem, kKeys * kRowBytes);
+  const uint64_t kmajor = tc::sdesc_sw128(0), mnmajor = tc::sdesc_mn_sw128(0, kKeys * kRowBytes);
+  const uint32_t km = tc::desc_hi(kmajor), mn = tc::desc_hi(mnmajor);
+  const uint32_t dq = (uint32_t)kmajor + ((q_smem + t * S::kTile) >> 4), ddo = (uint32_t)kmajor + ((do_smem + t * S::kTile) >> 4);
+  const uint32_t dk = (uint32_t)kmajor + (k_smem >> 4), dv = (uint32_t)kmajor + (v_smem >> 4), dkt = (uint32_t)mnmajor + (k_smem >> 4);
   const uint32_t s_at = tmem + t * 256, dp_at = s_at + 64, o_at = s_at + 128;
   uint32_t j = 0, done = 0, n_q = 0, n_o = 0;
+  uint32_t looked = 0;  // a bit a stage: how often (mod 2) its keys were looked at
   struct {
     bool any, mine, first, last;
   } was = {false, false, false, false};
   uint32_t i = 0;
-  int k = 0, steps = 0, nk = 0;
+  int k = 0, steps = 0, nk = 0, whole = 0;  // whole: steps that end before the keys do
   for (;;) {
     if (k == steps) {
-      if (i > 0 && tc::elect_one()) tc::bar_arrive(&sh.item_free[(i - 1) % kItems]);
-      __syncwarp();
+      if (i > 0) tc::bar_arrive(&sh.item_free[(i - 1) % kItems]);
       WAIT(sh.item_full[i % kItems], (i / kItems) & 1);
       steps = sh.item[i % kItems].steps;
       nk = steps == 0 ? 0 : sh.item[i % kItems].nk[t];
+      whole = sh.item[i % kItems].keys / kKeys;
       k = 0;
       ++i;
     }
@@ -861,40 +889,41 @@ __device__ __forceinline__ void issue_role(const GradParams& p, Sh& sh, uint32_t
         }
         WAIT(sh.ds_full[t], (done - 1) & 1);
         tc::fence_after();
-        if (tc::elect_one()) {
+        {
 #pragma unroll
           for (int q = 0; q < kKeys / 16; ++q)
-            tc::mma_ts(o_at, s_at + q * 8, dkt + before * (S::kHalf >> 4) + q * (16 * kRowBytes >> 4), id_o, q > 0 || !was.first ? 1u : 0u);
+            tc::mma16_ts(o_at, s_at + q * 8, dkt + before * (S::kHalf >> 4) + q * (16 * kRowBytes >> 4), mn, id_o, q > 0 || !was.first);
           if (was.last) tc::mma_commit(&sh.o_full[t]);
         }
-        __syncwarp();
       }
-      if (tc::elect_one()) was.mine ? tc::mma_commit(&sh.k_free[before]) : tc::bar_arrive(&sh.k_free[before]);
-      __syncwarp();
+      was.mine ? tc::mma_commit(&sh.k_free[before]) : tc::bar_arrive(&sh.k_free[before]);
     }
     if (end) return;
-    WAIT(sh.k_ready[st], (j / S::kStages) & 1);
+    WAIT(sh.k_full[st], (j / S::kStages) & 1);
+    if (k >= whole) {
+      WAIT(sh.k_ready[st], (looked >> st) & 1);
+      looked ^= 1u << st;
+    }
     if (mine && k == 0) {
       WAIT(sh.q_full[t], n_q & 1);
       ++n_q;
     }
     tc::fence_after();
-    if (mine && tc::elect_one()) {
+    if (mine) {
 #pragma unroll
       for (int q = 0; q < DP / 16; ++q)
-        tc::mma_bf16(s_at, dq + (q >> 2) * (128 * kRowBytes >> 4) + (q & 3) * 2,
-                     dk + st * (S::kHalf >> 4) + (q >> 2) * (kKeys * kRowBytes >> 4) + (q & 3) * 2, id_s, q > 0);
+        tc::mma16_ss(s_at, dq + (q >> 2) * (128 * kRowBytes >> 4) + (q & 3) * 2, km,
+                     dk + st * (S::kHalf >> 4) + (q >> 2) * (kKeys * kRowBytes >> 4) + (q & 3) * 2, km, id_s, q > 0);
       tc::mma_commit(&sh.s_full[t]);
     }
-    __syncwarp();
     WAIT(sh.v_full[st], (j / S::kStages) & 1);
     tc::fence_after();
-    if (tc::elect_one()) {
+    {
       if (mine) {
 #pragma unroll
         for (int q = 0; q < DP / 16; ++q)
-          tc::mma_bf16(dp_at, ddo + (q >> 2) * (128 * kRowBytes >> 4) + (q & 3) * 2,
-                       dv + st * (S::kHalf >> 4) + (q >> 2) * (kKeys * kRowBytes >> 4) + (q & 3) * 2, id_s, q > 0);
+          tc::mma16_ss(dp_at, ddo + (q >> 2) * (128 * kRowBytes >> 4) + (q & 3) * 2, km,
+                       dv + st * (S::kHalf >> 4) + (q >> 2) * (kKeys * kRowBytes >> 4) + (q & 3) * 2, km, id_s, q > 0);
         tc::mma_commit(&sh.dp_full[t]);
         tc::mma_commit(&sh.v_free[st]);
         if (k == nk - 1) tc::mma_commit(&sh.q_free[t]);
@@ -902,7 +931,6 @@ __device__ __forceinline__ void issue_role(const GradParams& p, Sh& sh, uint32_t
         tc::bar_arrive(&sh.v_free[st]);
       }
     }
-    __syncwarp();
     was.any = true;
     was.mine = mine;
     was.first = k == 0;
@@ -950,7 +978,7 @@ __device__ __forceinline__ void element_role(const GradParams& p, Sh& sh, uint32
         pr[2 * e] = fast_exp2(y.x);
         pr[2 * e + 1] = fast_exp2(y.y);
       }
-      if ((k + 1) * kKeys > common) {
+      if (PROMPT_RARE((k + 1) * kKeys > common)) {
         const int lim = limit - k * kKeys;
 #pragma unroll
         for (int e = 0; e < 64; ++e) pr[e] = e < lim ? pr[e] : 0.f;
@@ -960,7 +988,7 @@ __device__ __forceinline__ void element_role(const GradParams& p, Sh& sh, uint32
       tc::tmem_ld64(dp_at, v);
       tc::wait_ld64(v);
       // keys past the end: what is there may be anything
-      if (k * kKeys + kKeys > keys) {
+      if (PROMPT_RARE(k * kKeys + kKeys > keys)) {
 #pragma unroll
         for (int e = 0; e < 64; ++e) v[e] = k * kKeys + e < keys ? v[e] : 0u;
       }
@@ -1050,7 +1078,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int k = 0; k < S::kStages; ++k) {
       tc::bar_init(&sh.k_full[k], 1);
       tc::bar_init(&sh.k_ready[k], 1);
-      tc::bar_init(&sh.k_free[k], 2);
+      tc::bar_init(&sh.k_free[k], 3);
       tc::bar_init(&sh.v_full[k], 1);
       tc::bar_init(&sh.v_free[k], 2);
     }
@@ -1080,7 +1108,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       load_role<DP>(p, sh, map_q, map_do, map_k, map_v, q_smem, do_smem, k_smem, v_smem);
     else if (warp == 15)
       look_role<DP>(p, sh, k_smem);
-    else
+    else if (tc::elect_one())
       issue_role<DP, BF16>(p, sh, tc::su32(q_smem), tc::su32(do_smem), tc::su32(k_smem), tc::su32(v_smem), tmem, warp == 14);
   }
   __syncthreads();
@@ -1094,7 +1122,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   }
   __syncthreads();
-  if (threadIdx.x == 0) prompt_leave(p, gridDim.x);
+  if (threadIdx.x == 0) prompt_leave(p, gridDim.x, sh.stop);
   if (warp == 12) tc::tmem_dealloc(tmem, 512);
 }
 
