@@ -21,7 +21,7 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kItems = 3;           // items known ahead
-constexpr int kRegElement = 176, kRegWrite = 80, kRegIssue = 80;  // 2 x 176 + 80 + 80 = 4 x 128
+constexpr int kRegElement = 160, kRegWrite = 88, kRegIssue = 104;  // 2 x 160 + 88 + 104 = 4 x 128
 constexpr int kRowBytes = 128;      // of 64 dims in a block
 
 struct GradParams : PromptParams {
@@ -697,8 +697,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // ================================================================ dQ
 // An item is 256 query rows, two tiles of 128 as in the forward pass; its steps are blocks of 64 keys. S = Q K^T and
-// dP = dO V^T a row a lane, dS in the place of S, dQ += dS K. Each row tile has an issuing warp and a
-// warpgroup: while one tile's dS is formed, the other's products run.
+// dP = dO V^T a row a lane, dS in the place of dP, dQ += dS K. Each row tile has an issuing warp and a
+// warpgroup: the next step's scores are multiplied as soon as a step's have been read, its dP behind dQ; and while one
+// tile's dS is formed, the other's products run.
 namespace rows {
 
 constexpr int kKeys = 64;
@@ -708,12 +709,13 @@ struct Shape {
   static constexpr int kBlocks = DP > 64 ? 2 : 1;
   static constexpr int kTile = kBlocks * 128 * kRowBytes;  // bytes of 128 rows
   static constexpr int kHalf = kTile / 2;                  // and of 64
-  static constexpr int kStages = DP > 64 ? 2 : 4;
+  static constexpr int kStagesK = DP > 64 ? 3 : 4;         // (keys are held for two steps)
+  static constexpr int kStagesV = DP > 64 ? 2 : 4;
 };
 
-template <int STAGES>
+template <int KS, int VS>
 struct Shared {
-  uint64_t q_full[2], q_free[2], k_full[STAGES], k_ready[STAGES], k_free[STAGES], v_full[STAGES], v_free[STAGES], s_full[2], dp_full[2],
+  uint64_t q_full[2], q_free[2], k_full[KS], k_ready[KS], k_free[KS], v_full[VS], v_free[VS], s_full[2], s_read[2], dp_full[2],
       ds_full[2], o_full[2], o_free[2], item_full[kItems], item_free[kItems], drain;
   PromptItem item[kItems];
   uint32_t tmem;
@@ -746,10 +748,9 @@ __device__ __forceinline__ void load_role(const GradParams& p, Sh& sh, const CUt
     if (it.steps == 0) return;
     const int tt = 128 >> p.log2P, head = it.hb << p.log2P, kv = head / p.G;
     for (int k = 0; k < it.steps; ++k, ++j) {
-      const int st = j % S::kStages;
-      const uint32_t turn = ((j / S::kStages) & 1) ^ 1;
+      const int st = j % S::kStagesK, sv = j % S::kStagesV;
       const int key = (int)(it.key0 + (int64_t)k * kKeys);
-      WAIT(sh.k_free[st], turn);
+      WAIT(sh.k_free[st], ((j / S::kStagesK) & 1) ^ 1);
       if (lane == 0) {
         tc::bar_expect_tx(&sh.k_full[st], S::kHalf);
         for (int b = 0; b < S::kBlocks; ++b)
@@ -771,11 +772,11 @@ __device__ __forceinline__ void load_role(const GradParams& p, Sh& sh, const CUt
           }
         }
       }
-      WAIT(sh.v_free[st], turn);
+      WAIT(sh.v_free[sv], ((j / S::kStagesV) & 1) ^ 1);
       if (lane == 0) {
-        tc::bar_expect_tx(&sh.v_full[st], S::kHalf);
+        tc::bar_expect_tx(&sh.v_full[sv], S::kHalf);
         for (int b = 0; b < S::kBlocks; ++b)
-          tc::tma_load_3d(v_smem + st * S::kHalf + b * kKeys * kRowBytes, &map_v, b * 64, kv, key, &sh.v_full[st]);
+          tc::tma_load_3d(v_smem + sv * S::kHalf + b * kKeys * kRowBytes, &map_v, b * 64, kv, key, &sh.v_full[sv]);
       }
       __syncwarp();
     }
@@ -833,8 +834,8 @@ __device__ __forceinline__ void look_role(const GradParams& p, Sh& sh, unsigned 
     const int whole = keys / kKeys;
 #pragma unroll 1
     for (int k = 0; k < steps; ++k, ++j) {
-      const int st = j % S::kStages, live = max(keys - k * kKeys, 0);
-      WAIT(sh.k_full[st], (j / S::kStages) & 1);
+      const int st = j % S::kStagesK, live = max(keys - k * kKeys, 0);
+      WAIT(sh.k_full[st], (j / S::kStagesK) & 1);
       if (k >= whole) {
 #pragma unroll 1
         for (int b = 0; b < S::kBlocks; ++b) {
@@ -880,7 +881,27 @@ __device__ __forceinline__ void issue_role(const GradParams& p, Sh& sh, uint32_t
       ++i;
     }
     const bool end = steps == 0, mine = !end && k < nk;
-    const uint32_t st = j % S::kStages, before = (j - 1) % S::kStages;
+    const uint32_t st = j % S::kStagesK, sv = j % S::kStagesV, before = (j - 1) % S::kStagesK;
+    if (!end) {
+      WAIT(sh.k_full[st], (j / S::kStagesK) & 1);
+      if (k >= whole) {
+        WAIT(sh.k_ready[st], (looked >> st) & 1);
+        looked ^= 1u << st;
+      }
+    }
+    if (mine) {
+      if (k == 0) {
+        WAIT(sh.q_full[t], n_q & 1);
+        ++n_q;
+      }
+      if (done > 0) WAIT(sh.s_read[t], (done - 1) & 1);
+      tc::fence_after();
+#pragma unroll
+      for (int q = 0; q < DP / 16; ++q)
+        tc::mma16_ss(s_at, dq + (q >> 2) * (128 * kRowBytes >> 4) + (q & 3) * 2, km,
+                     dk + st * (S::kHalf >> 4) + (q >> 2) * (kKeys * kRowBytes >> 4) + (q & 3) * 2, km, id_s, q > 0);
+      tc::mma_commit(&sh.s_full[t]);
+    }
     if (was.any) {
       if (was.mine) {
         if (was.first) {
@@ -889,47 +910,26 @@ __device__ __forceinline__ void issue_role(const GradParams& p, Sh& sh, uint32_t
         }
         WAIT(sh.ds_full[t], (done - 1) & 1);
         tc::fence_after();
-        {
 #pragma unroll
-          for (int q = 0; q < kKeys / 16; ++q)
-            tc::mma16_ts(o_at, s_at + q * 8, dkt + before * (S::kHalf >> 4) + q * (16 * kRowBytes >> 4), mn, id_o, q > 0 || !was.first);
-          if (was.last) tc::mma_commit(&sh.o_full[t]);
-        }
+        for (int q = 0; q < kKeys / 16; ++q)
+          tc::mma16_ts(o_at, dp_at + q * 8, dkt + before * (S::kHalf >> 4) + q * (16 * kRowBytes >> 4), mn, id_o, q > 0 || !was.first);
+        if (was.last) tc::mma_commit(&sh.o_full[t]);
       }
       was.mine ? tc::mma_commit(&sh.k_free[before]) : tc::bar_arrive(&sh.k_free[before]);
     }
     if (end) return;
-    WAIT(sh.k_full[st], (j / S::kStages) & 1);
-    if (k >= whole) {
-      WAIT(sh.k_ready[st], (looked >> st) & 1);
-      looked ^= 1u << st;
-    }
-    if (mine && k == 0) {
-      WAIT(sh.q_full[t], n_q & 1);
-      ++n_q;
-    }
-    tc::fence_after();
+    WAIT(sh.v_full[sv], (j / S::kStagesV) & 1);
     if (mine) {
+      tc::fence_after();
 #pragma unroll
       for (int q = 0; q < DP / 16; ++q)
-        tc::mma16_ss(s_at, dq + (q >> 2) * (128 * kRowBytes >> 4) + (q & 3) * 2, km,
-                     dk + st * (S::kHalf >> 4) + (q >> 2) * (kKeys * kRowBytes >> 4) + (q & 3) * 2, km, id_s, q > 0);
-      tc::mma_commit(&sh.s_full[t]);
-    }
-    WAIT(sh.v_full[st], (j / S::kStages) & 1);
-    tc::fence_after();
-    {
-      if (mine) {
-#pragma unroll
-        for (int q = 0; q < DP / 16; ++q)
-          tc::mma16_ss(dp_at, ddo + (q >> 2) * (128 * kRowBytes >> 4) + (q & 3) * 2, km,
-                       dv + st * (S::kHalf >> 4) + (q >> 2) * (kKeys * kRowBytes >> 4) + (q & 3) * 2, km, id_s, q > 0);
-        tc::mma_commit(&sh.dp_full[t]);
-        tc::mma_commit(&sh.v_free[st]);
-        if (k == nk - 1) tc::mma_commit(&sh.q_free[t]);
-      } else {
-        tc::bar_arrive(&sh.v_free[st]);
-      }
+        tc::mma16_ss(dp_at, ddo + (q >> 2) * (128 * kRowBytes >> 4) + (q & 3) * 2, km,
+                     dv + sv * (S::kHalf >> 4) + (q >> 2) * (kKeys * kRowBytes >> 4) + (q & 3) * 2, km, id_s, q > 0);
+      tc::mma_commit(&sh.dp_full[t]);
+      tc::mma_commit(&sh.v_free[sv]);
+      if (k == nk - 1) tc::mma_commit(&sh.q_free[t]);
+    } else {
+      tc::bar_arrive(&sh.v_free[sv]);
     }
     was.any = true;
     was.mine = mine;
@@ -968,15 +968,23 @@ __device__ __forceinline__ void element_role(const GradParams& p, Sh& sh, uint32
     for (int k = 0; k < nk; ++k, ++done) {
       WAIT(sh.s_full[t], done & 1);
       tc::fence_after();
-      uint32_t v[64];
-      tc::tmem_ld64(s_at, v);
-      tc::wait_ld64(v);
+      // (32 columns at a time: 64 at once need registers that are not there)
       float pr[64];
 #pragma unroll
-      for (int e = 0; e < 32; ++e) {
-        const float2 y = tc::fma2(make_float2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), scale2, add2);
-        pr[2 * e] = fast_exp2(y.x);
-        pr[2 * e + 1] = fast_exp2(y.y);
+      for (int c = 0; c < 2; ++c) {
+        uint32_t v[32];
+        tc::tmem_ld32(s_at + 32 * c, v);
+        tc::wait_ld(v);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float2 y = tc::fma2(make_float2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), scale2, add2);
+          pr[32 * c + 2 * e] = fast_exp2(y.x);
+          pr[32 * c + 2 * e + 1] = fast_exp2(y.y);
+        }
+        if (c == 1) {
+          tc::fence_before();
+          tc::bar_arrive(&sh.s_read[t]);
+        }
       }
       if (PROMPT_RARE((k + 1) * kKeys > common)) {
         const int lim = limit - k * kKeys;
@@ -985,20 +993,25 @@ __device__ __forceinline__ void element_role(const GradParams& p, Sh& sh, uint32
       }
       WAIT(sh.dp_full[t], done & 1);
       tc::fence_after();
-      tc::tmem_ld64(dp_at, v);
-      tc::wait_ld64(v);
-      // keys past the end: what is there may be anything
-      if (PROMPT_RARE(k * kKeys + kKeys > keys)) {
 #pragma unroll
-        for (int e = 0; e < 64; ++e) v[e] = k * kKeys + e < keys ? v[e] : 0u;
-      }
-      uint32_t pk[32];
+      for (int c = 0; c < 2; ++c) {
+        uint32_t v[32];
+        tc::tmem_ld32(dp_at + 32 * c, v);
+        tc::wait_ld(v);
+        // keys past the end: what is there may be anything
+        if (PROMPT_RARE(k * kKeys + kKeys > keys)) {
 #pragma unroll
-      for (int e = 0; e < 32; ++e) {
-        float2 y = tc::fma2(make_float2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), power2, delta2);
-        pk[e] = pack16<BF16>(y.x * pr[2 * e], y.y * pr[2 * e + 1]);
+          for (int e = 0; e < 32; ++e) v[e] = k * kKeys + 32 * c + e < keys ? v[e] : 0u;
+        }
+        uint32_t pk[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float2 y = tc::fma2(make_float2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), power2, delta2);
+          y = tc::mul2(y, make_float2(pr[32 * c + 2 * e], pr[32 * c + 2 * e + 1]));
+          pk[e] = pack16<BF16>(y.x, y.y);
+        }
+        tc::tmem_st16(dp_at + 16 * c, pk);
       }
-      tc::tmem_st32(s_at, pk);
       tc::tmem_wait_st();
       tc::fence_before();
       tc::bar_arrive(&sh.ds_full[t]);
@@ -1055,13 +1068,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     prompt_rows_kernel(GradParams p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_do,
                        const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
   using S = Shape<DP>;
-  using Sh = Shared<S::kStages>;
+  using Sh = Shared<S::kStagesK, S::kStagesV>;
   extern __shared__ __align__(1024) unsigned char smem[];
   unsigned char* q_smem = smem;
   unsigned char* do_smem = q_smem + 2 * S::kTile;
   unsigned char* k_smem = do_smem + 2 * S::kTile;
-  unsigned char* v_smem = k_smem + S::kStages * S::kHalf;
-  unsigned char* stage = v_smem + S::kStages * S::kHalf;
+  unsigned char* v_smem = k_smem + S::kStagesK * S::kHalf;
+  unsigned char* stage = v_smem + S::kStagesV * S::kHalf;
   Sh& sh = *reinterpret_cast<Sh*>(stage + 4 * 32 * 128);
   const int warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
@@ -1070,15 +1083,18 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc::bar_init(&sh.q_full[k], 1);
       tc::bar_init(&sh.q_free[k], 1);
       tc::bar_init(&sh.s_full[k], 1);
+      tc::bar_init(&sh.s_read[k], 128);
       tc::bar_init(&sh.dp_full[k], 1);
       tc::bar_init(&sh.ds_full[k], 128);
       tc::bar_init(&sh.o_full[k], 1);
       tc::bar_init(&sh.o_free[k], 128);
     }
-    for (int k = 0; k < S::kStages; ++k) {
+    for (int k = 0; k < S::kStagesK; ++k) {
       tc::bar_init(&sh.k_full[k], 1);
       tc::bar_init(&sh.k_ready[k], 1);
       tc::bar_init(&sh.k_free[k], 3);
+    }
+    for (int k = 0; k < S::kStagesV; ++k) {
       tc::bar_init(&sh.v_full[k], 1);
       tc::bar_init(&sh.v_free[k], 2);
     }
@@ -1116,8 +1132,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (sh.stop && (warp == 12 || warp == 14) && tc::elect_one()) {
     tc::mma_commit(&sh.drain);
     tc::bar_wait(&sh.drain, 0, nullptr, kPromptWaitNs);
-    for (int k = 0; k < 2 * (2 * S::kStages + 2); ++k) {
-      uint64_t* bar = k / 2 < S::kStages ? &sh.k_full[k / 2] : k / 2 < 2 * S::kStages ? &sh.v_full[k / 2 - S::kStages] : &sh.q_full[k / 2 - 2 * S::kStages];
+    for (int k = 0; k < 2 * (S::kStagesK + S::kStagesV + 2); ++k) {
+      const int n = k / 2 - S::kStagesK;
+      uint64_t* bar = n < 0 ? &sh.k_full[k / 2] : n < S::kStagesV ? &sh.v_full[n] : &sh.q_full[n - S::kStagesV];
       tc::bar_wait(bar, k & 1, nullptr, kPromptWaitNs / 16);
     }
   }
@@ -1161,7 +1178,8 @@ int launch_grad(const GradParams& p, const CUtensorMap (&mk)[5], const CUtensorM
   using R = rows::Shape<DP>;
   constexpr int smem_k = (2 + K::kStages) * K::kTile + 4 * 32 * 128 + 2 * keys::kUnitBytes + K::kStages * keys::kMoreBytes +
                          (int)sizeof(keys::Shared<K::kStages>);
-  constexpr int smem_r = 4 * R::kTile + 2 * R::kStages * R::kHalf + 4 * 32 * 128 + (int)sizeof(rows::Shared<R::kStages>);
+  constexpr int smem_r =
+      4 * R::kTile + (R::kStagesK + R::kStagesV) * R::kHalf + 4 * 32 * 128 + (int)sizeof(rows::Shared<R::kStagesK, R::kStagesV>);
   static_assert(smem_k <= 227 * 1024 && smem_r <= 227 * 1024, "an SM's shared memory");
   static std::atomic<uint64_t> ready_k{0}, ready_r{0};
   if (grid_keys > 0) {
