@@ -227,6 +227,15 @@ struct Convert {
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) r[i] = at[i * RPP * D / 16];
   }
+  // Returns once the values are in registers: an arrival does not wait for loads under way, and the copy that it lets
+  // begin can overtake them where products take most of the shared memory's reads. (What it sleeps for changes nothing;
+  // a fence in its place did not wait for them either.)
+  __device__ __forceinline__ void landed(const uint4 (&r)[PASSES]) const {
+    uint32_t all = 0;
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) all |= r[i].x | r[i].y | r[i].z | r[i].w;
+    if (all == 0x80000001u) __nanosleep(1);
+  }
   // hidden rows may be anything: zeros
   __device__ __forceinline__ void mask(uint4 (&r)[PASSES], const uint32_t* seen) const {
 #pragma unroll
@@ -464,6 +473,7 @@ __device__ __forceinline__ void convert_role(const AttendParams& p, Shared& sh, 
         uint4 r[Convert<D>::PASSES];
         TC_WAIT(sh.raw_full[kv], j & 1);
         f.read(r, raw + kv * (kK * D));
+        f.landed(r);
         if (!full) f.mask(r, s.seen);
         __syncwarp();
         if (lane == 0) tc::bar_arrive(&sh.raw_free[kv]);

@@ -46,3 +46,25 @@ def test_attend_nan_notes_of_short_items():
         c.v.view(torch.uint8)[0, int(c.table[seqs[i], p // 16]), i % 4, p % 16, i] = 0x7f
     for _ in range(5):
         attend_case(c, seqs, rows, 16)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("length", [256, 1500])
+def test_attend_results_are_the_same_each_time(dim, length):
+    """100 rows of 16 heads over 4 key heads: items of two row tiles, whose products take most of the shared memory's reads
+    while the next pages come in. The results depend on no timing, and are those of the kernel for few rows to f16's and
+    the result's roundings (2^-8 relative at most where nothing cancels; a tenth of a row's largest value is far off)."""
+    import paper_2605_29657_gb300 as occ
+    g = torch.Generator().manual_seed(dim + length)
+    n, rows = 8, 100
+    c, seqs = filled(64, dim, 4, [length] * n, 7)
+    q = (0.2 * torch.randn((n * rows, 64, dim), generator=g)).bfloat16().cuda()
+    s, off = torch.tensor(seqs, dtype=torch.int32, device="cuda"), torch.arange(0, n * rows + 1, rows, device="cuda")
+    few, few_lse = occ.occam_cache_attend(c, 0, q, s, off, 1)
+    first, first_lse = occ.occam_cache_attend(c, 0, q, s, off, rows)
+    assert bool(((first.float() - few.float()).abs().amax(-1) <= 0.1 * few.float().abs().amax(-1)).all())
+    assert bool(((first_lse - few_lse).abs() <= 0.01).all())
+    for _ in range(60):
+        out, lse = occ.occam_cache_attend(c, 0, q, s, off, rows)
+        assert torch.equal(out, first) and torch.equal(lse, first_lse)
+    assert c.status() == 0
