@@ -592,7 +592,9 @@ int occam_cache_attend(const occam_cache* cache, const occam_attend_args* args, 
  * rows of the group. Group g is the sequences seqs[group_off[g] .. group_off[g+1]-1]
  * (group_off int32 [n_groups+1], device, from 0 up to n; n_groups at most max_seqs, at least 1 if n is). What they
  * share is found in the page table: leading full pages that are the same in all of them and that every
- * row sees whole; a group may share nothing. Results are those of occam_cache_attend
+ * row sees whole; a group may share nothing. Where reading them once would not save the time that the join of the
+ * two parts takes (few rows, short prefixes, rows that fill the tensor cores' tiles without each other), the group's
+ * sequences are read one by one: that is decided on the device, from row_off and the tables. Results are those of occam_cache_attend
  * up to the order of sums in fp32. keep flags are not taken (OCCAM_ERR_UNSUPPORTED): prune forks
  * with occam_cache_compact. max_group_rows: the largest number of rows of one group (it chooses
  * the kernels; results are right for any value). workspace: of

@@ -369,7 +369,7 @@ def occam_cache_attend_shared(cache: PagedCache, layer: int, q, seqs, row_off, m
                               scale: float = 0.0, causal: bool = True, out=None, lse=None, stream=None):
     """occam_cache_attend for sequences that share leading pages (forks): group g is seqs[group_off[g]]
     .. seqs[group_off[g + 1] - 1] (int32, from 0 up to the number of sequences), and the full pages that its
-    sequences have in common are read once for all their rows. max_group_rows: the most rows of one group.
+    sequences have in common are read once for all their rows, where that saves time. max_group_rows: the most rows of one group.
     ws: alloc_workspace(rows, heads). Returns (out, lse) as occam_cache_attend."""
     wp, wn = _workspace(cache, ws)
     a, out, lse, on = _attend_args(cache, layer, q, seqs, row_off, max_rows, scale, causal, None, None, out, lse, stream)

@@ -38,6 +38,8 @@ struct AttendParams {
   const int32_t* skip;       // tails: leading tokens of a sequence that its group's prefix stands for
   float* pre_o;              // results over the prefixes, normalised [total_rows, heads, dim]
   float* pre_l;              // and log2 sum_k 2^s_k
+  int2* ranges;              // prefixes: the CTAs with parts of an item of the tensor-core kernel [key heads, range_tiles]
+  int64_t range_tiles;
   int32_t* counters;  // per stretch: arrivals at an item that begins in it; at kAttendCtas: CTAs that have left
   float* part_o;
   float2* part_ml;

@@ -6,10 +6,13 @@
 //   o = (o_1 e^{L_1} + o_2 e^{L_2}) / (e^{L_1} + e^{L_2}).
 // The rows of a group's sequences lie next to one another and all see the whole prefix,
 // so over the prefix they are the rows of one sequence: its codes are read once a group and, from 33 rows a
-// key head on, multiplied on the tensor cores, instead of once a sequence. Three launches:
+// key head on, multiplied on the tensor cores, instead of once a sequence. Launches:
 // how many leading pages the tables of each group have in common (this file), the
-// prefixes, then the tails, whose rows take the prefix's result in as they are written
+// prefixes, the sums of prefixes that were split, then the tails, whose rows take the prefix's result in as they are written
 // (attend.cu and attend_tc.cu, as attention over whole sequences).
+// What bounds it is the chain of these launches and the parts of split prefixes, not the codes: 64 forks of one token over
+// 16,000 common ones (8 key heads of 128, 4 query heads each) take 66 us, where reading the codes once takes 9 and
+// each sequence by itself 480.
 #include <algorithm>
 
 #include "attend.cuh"
@@ -20,9 +23,15 @@ using namespace occam;
 namespace {
 
 constexpr int kThreads = 1024;
+constexpr float kChain = 15.f;    // us of the launches that sharing adds
+constexpr float kJoin = 0.0005f;  // us of a (row, head) whose two parts are joined
+
+// Row tiles' worth of time that m query rows of a key head take against the same keys
+__device__ __forceinline__ float row_tiles(float m) { return m <= 0.f ? 0.f : m <= 32.f ? 0.5f : ceilf(m / 256.f); }
 
 struct SharedWs {
-  size_t shared, skip, pre_l, pre_o, total;
+  size_t shared, skip, pre_l, pre_o, ranges, total;
+  int64_t range_tiles;
 };
 // Behind what attention itself uses (where other calls on the same workspace keep their lists: each call writes
 // before it reads)
@@ -32,13 +41,15 @@ SharedWs shared_ws(const occam_cache* c, int64_t total_rows, int heads) {
   w.skip = w.shared + cache_align((size_t)c->max_seqs * 4);
   w.pre_l = w.skip + cache_align((size_t)c->max_seqs * 4);
   w.pre_o = w.pre_l + cache_align((size_t)total_rows * heads * 4);
-  w.total = w.pre_o + cache_align((size_t)total_rows * heads * c->dim * 4);
+  w.ranges = w.pre_o + cache_align((size_t)total_rows * heads * c->dim * 4);
+  w.range_tiles = total_rows * (heads / c->heads) / 256 + c->max_seqs + 1;
+  w.total = w.ranges + cache_align((size_t)c->heads * w.range_tiles * 8);
   return w;
 }
 
 struct CommonParams {
   CacheDev c;
-  int n, groups;
+  int n, groups, G, sms;
   int64_t total_rows;
   const int32_t* seqs;
   const int64_t* row_off;
@@ -104,6 +115,37 @@ __global__ void __launch_bounds__(kThreads) common_kernel(CommonParams p) {
     __syncthreads();
     pages = sh_pages;
   }
+  // Whether it pays. In units of a row tile (256 query rows of a key head) against 128 keys on the tensor cores, 2 us of an
+  // SM's time: a sequence of up to 32 such rows takes half of one, by the few-row kernel. (64 single tokens over 16 k
+  // common tokens: 65 us shared, 480 not; three over 600: 35 and 21; 8 x 8 questions of 16 to 128 rows over 2,900, whose rows fill their
+  // tiles without each other: 420 and 314.)
+  float alone = 0.f;
+  int64_t rows = 0;
+  for (int i = a + t; i < b && pages > 0; i += kThreads) {
+    const int m = (int)(p.row_off[i + 1] - p.row_off[i]);
+    alone += row_tiles(m * p.G);
+    rows += m;
+  }
+  for (int o = 16; o > 0; o >>= 1) {
+    alone += __shfl_xor_sync(0xffffffffu, alone, o);
+    rows += __shfl_xor_sync(0xffffffffu, rows, o);
+  }
+  __shared__ float sh_alone[kThreads / 32];
+  __shared__ int64_t sh_rows[kThreads / 32];
+  if (lane == 0) {
+    sh_alone[warp] = alone;
+    sh_rows[warp] = rows;
+  }
+  __syncthreads();
+  alone = 0.f;
+  rows = 0;
+  for (int w = 0; w < kThreads / 32; ++w) {
+    alone += sh_alone[w];
+    rows += sh_rows[w];
+  }
+  const float all = (float)p.groups * c.heads;  // the other groups are taken to be alike
+  const float saved = (alone - row_tiles((float)rows * p.G)) * (float)(pages << c.log2T) / 128.f * 2.f * all / p.sms;
+  if (saved < kChain + (float)rows * p.G * all * kJoin) pages = 0;
   if (t == 0) p.shared[g] = pages << c.log2T;
   for (int i = a + t; i < b; i += kThreads) p.skip[i] = pages << c.log2T;
 }
@@ -149,7 +191,9 @@ extern "C" int occam_cache_attend_shared(const occam_cache* cache, const occam_a
   p.skip = skip;
   p.pre_l = ws_at<float>(workspace, sw.pre_l);
   p.pre_o = ws_at<float>(workspace, sw.pre_o);
-  CommonParams m{p.c, a->n, n_groups, a->total_rows, a->seqs, a->row_off, group_off, shared, skip};
+  p.ranges = ws_at<int2>(workspace, sw.ranges);
+  p.range_tiles = sw.range_tiles;
+  CommonParams m{p.c, a->n, n_groups, p.G, cache_sms(), a->total_rows, a->seqs, a->row_off, group_off, shared, skip};
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   if (!launch_after(common_kernel, dim3((unsigned)n_groups), kThreads, 0, st, m)) return OCCAM_ERR_CUDA;
   AttendParams pre = p;

@@ -97,6 +97,9 @@ using tc::tmem_ld16;
 using tc::tmem_st16;
 using tc::wait_ld;
 
+// (prefixes) an item's place among its head's
+__device__ __forceinline__ int range_at(const AttendParams& p, int64_t row0, int i, int rt) { return (int)(row0 * p.G / kR) + i + rt; }
+__device__ __forceinline__ int range_at(const AttendParams& p, const Walk& x) { return range_at(p, x.s.row0, x.i, x.rt); }
 __device__ __forceinline__ int row_tiles(const AttendParams& p, const Walk& x) {
   return x.s.rows * p.G - x.rt * kR > 128 ? 2 : 1;
 }
@@ -792,12 +795,13 @@ __device__ __forceinline__ void softmax_role(const P& p, Shared& sh, unsigned ch
       float l2 = l == 0.f ? -INFINITY : ref + log2f(l), pre = 0.f;  // the prefix's weight
       uint16_t* out = p.out + to * D;
       float* part = p.part_o + mypart * D;
-      const bool half_out = P::mode == kPrefix ? false : done;  // 16-bit results
+      const bool joins = P::mode == kTail && done && x.s.page0 > 0;  // (the same for all rows)
+      const bool out16 = P::mode != kPrefix && done;                 // 16-bit results,
+      const bool half_out = out16 && !joins;                         // and in shared memory too
       if constexpr (P::mode == kPrefix)
         if (done) part = p.pre_o + to * D;
-      const bool joins = P::mode == kTail && done && x.s.page0 > 0 && there;
       if constexpr (P::mode == kTail)
-        if (joins) {
+        if (joins && there) {
           float b;
           l2 = join_prefix(p, to, l2, pre, b);
           scale *= b;
@@ -809,7 +813,7 @@ __device__ __forceinline__ void softmax_role(const P& p, Shared& sh, unsigned ch
       auto place = [&](int rr, int c) { return stage + (c >> 3) * 16384 + rr * 128 + (((c & 7) ^ (rr & 7)) << 4); };
       const int live = min(x.s.rows * p.G - (x.rt * kR + (row & ~31)), 32);  // rows of the warp
       const bool fits = !there || in_bounds(x.s.row0 + tok < p.total_rows && x.h * p.G + at - tok * p.G < p.H, p.c.status, kSiteAttendRow);
-      const uint64_t mine_at = !fits ? 0 : half_out ? reinterpret_cast<uint64_t>(out) : reinterpret_cast<uint64_t>(part);
+      const uint64_t mine_at = !fits ? 0 : out16 ? reinterpret_cast<uint64_t>(out) : reinterpret_cast<uint64_t>(part);
 #pragma unroll 1
       for (int pass = 0; pass < (half_out ? 1 : 2); ++pass) {
         const int cols = half_out ? D : D / 2;
@@ -820,17 +824,6 @@ __device__ __forceinline__ void softmax_role(const P& p, Shared& sh, unsigned ch
           float v[16];
 #pragma unroll
           for (int k = 0; k < 16; ++k) v[k] = l == 0.f ? 0.f : __uint_as_float(o[k]) * scale;
-          if constexpr (P::mode == kTail)
-            if (joins) {
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const float4 y = __ldcg(reinterpret_cast<const float4*>(p.pre_o + to * D + c) + k);
-                v[4 * k] = fmaf(y.x, pre, v[4 * k]);
-                v[4 * k + 1] = fmaf(y.y, pre, v[4 * k + 1]);
-                v[4 * k + 2] = fmaf(y.z, pre, v[4 * k + 2]);
-                v[4 * k + 3] = fmaf(y.w, pre, v[4 * k + 3]);
-              }
-            }
           if (half_out) {
 #pragma unroll
             for (int k = 0; k < 2; ++k)
@@ -844,6 +837,35 @@ __device__ __forceinline__ void softmax_role(const P& p, Shared& sh, unsigned ch
           }
         }
         __syncwarp();
+        if constexpr (P::mode == kTail)
+          if (joins) {  // four values of a row's tail, and of its prefix: eight rows' under way together
+            constexpr int AHEAD = 8;
+#pragma unroll 1
+            for (int i0 = 0; i0 < 32 / RPI; i0 += AHEAD) {
+              float4 y[AHEAD];
+              int64_t first[AHEAD];
+#pragma unroll
+              for (int i = 0; i < AHEAD; ++i) {
+                const int rr = (i0 + i) * RPI + lane / CH;
+                const uint64_t to_at = __shfl_sync(0xffffffffu, mine_at, rr);
+                const bool ok = rr < live && in_bounds(to_at != 0, p.c.status, kSiteAttendRow);
+                first[i] = ok ? (int64_t)(to_at - reinterpret_cast<uint64_t>(p.out)) / 2 + pass * (D / 2) + lane % CH * 4 : -1;
+                y[i] = ok ? __ldcg(reinterpret_cast<const float4*>(p.pre_o + first[i])) : make_float4(0.f, 0.f, 0.f, 0.f);
+              }
+#pragma unroll
+              for (int i = 0; i < AHEAD; ++i) {
+                const int rr = (i0 + i) * RPI + lane / CH;
+                const float w = __shfl_sync(0xffffffffu, pre, rr);
+                const float4 v = *reinterpret_cast<const float4*>(place((r & ~31) + rr, lane % CH));
+                if (first[i] >= 0)
+                  *reinterpret_cast<uint2*>(p.out + first[i]) =
+                      make_uint2(out_pair<BF16>(fmaf(y[i].x, w, v.x), fmaf(y[i].y, w, v.y)),
+                                 out_pair<BF16>(fmaf(y[i].z, w, v.z), fmaf(y[i].w, w, v.w)));
+              }
+            }
+            __syncwarp();
+            continue;
+          }
 #pragma unroll 4
         for (int i = 0; i < 32 / RPI; ++i) {
           const int rr = i * RPI + lane / CH, c = lane % CH;
@@ -857,7 +879,7 @@ __device__ __forceinline__ void softmax_role(const P& p, Shared& sh, unsigned ch
 #pragma unroll 1
         for (int d = 0; d < D; ++d)
           if (sh.nan_first[seg & 3][d] < limit) {
-            if (half_out)
+            if (out16)
               out[d] = BF16 ? 0x7fc0 : 0x7e00;
             else
               part[d] = __int_as_float(0x7fc00000);
@@ -875,7 +897,14 @@ __device__ __forceinline__ void softmax_role(const P& p, Shared& sh, unsigned ch
         }
       }
     }
-    if (!done) {
+    if constexpr (P::mode == kPrefix) {
+      // A prefix's parts are joined by a launch behind this one (join_kernel): an item may have a part in every
+      // CTA, and one CTA alone would take longer over the sums than all of them over the products.
+      if (threadIdx.x == 0 && x.ta == 0) {
+        const int2 who = done ? make_int2(0, -1) : item_stretches<kOver>(sh.line, x);
+        if (in_bounds(range_at(p, x) < p.range_tiles, p.c.status, kSiteAttendPart)) p.ranges[(int64_t)x.h * p.range_tiles + range_at(p, x)] = who;
+      }
+    } else if (!done) {
       TC_MEET();
       const int2 who = item_stretches<kOver>(sh.line, x);
       const int first = who.x, last = who.y;
@@ -906,16 +935,12 @@ __device__ __forceinline__ void softmax_role(const P& p, Shared& sh, unsigned ch
           }
           float inv = sum == 0.f ? 0.f : 1.f / sum, l2 = sum == 0.f ? -INFINITY : mx + log2f(sum), pre = 0.f;
           if (there && in_bounds(to < p.total_rows * p.H, p.c.status, kSiteAttendRow)) {
-            if constexpr (P::mode == kPrefix) {
-              p.pre_l[to] = l2;
-            } else {
-              if (P::mode == kTail && x.s.page0 > 0) {
-                float b;
-                l2 = join_prefix(p, to, l2, pre, b);
-                inv *= b;
-              }
-              if (p.lse) p.lse[to] = l2 * 0.69314718056f;
+            if (P::mode == kTail && x.s.page0 > 0) {
+              float b;
+              l2 = join_prefix(p, to, l2, pre, b);
+              inv *= b;
             }
+            if (p.lse) p.lse[to] = l2 * 0.69314718056f;
           }
 #pragma unroll 1
           for (int c0 = first; c0 <= last; c0 += 32) {
@@ -965,10 +990,6 @@ __device__ __forceinline__ void softmax_role(const P& p, Shared& sh, unsigned ch
                     float* keep = p.part_o + part(first, r0 + i) * D + lane * V;
 #pragma unroll
                     for (int q = 0; q < V; ++q) keep[q] = acc[i][q];
-                  } else if constexpr (P::mode == kPrefix) {
-                    float* pre_o = p.pre_o + row_to * D + lane * V;
-#pragma unroll
-                    for (int q = 0; q < V; ++q) pre_o[q] = total == 0.f ? 0.f : acc[i][q];
                   } else {
                     const bool none = P::mode == kTail ? total == -INFINITY : total == 0.f;
                     if (P::mode == kTail && row_pre != 0.f) {
@@ -1107,6 +1128,75 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 12) tc::tmem_dealloc(tmem, 512);
 }
 
+// The parts that a prefix's items left, a warp a row: its maximum, weights and sums. A CTA takes kJoinRows rows of an
+// item; grid: y over key heads, z over groups.
+constexpr int kJoinRows = 8;
+template <int D>
+__global__ void __launch_bounds__(256) join_kernel(AttendCall<kPrefix> p) {
+  pdl_wait();
+  const SeqInfo s = attend_seq(p, blockIdx.z);
+  const int lane = threadIdx.x & 31, h = blockIdx.y, rows = s.rows * p.G;
+  constexpr int V = D / 32;
+  for (int r0 = blockIdx.x * kJoinRows; r0 < rows; r0 += gridDim.x * kJoinRows) {
+    const int tile = range_at(p, s.row0, blockIdx.z, r0 / kR);
+    if (!in_bounds(tile < p.range_tiles, p.c.status, kSiteAttendPart)) continue;
+    const int2 who = p.ranges[(int64_t)h * p.range_tiles + tile];
+    if (who.y <= who.x) continue;  // one part: it is the result
+    const int n = who.y - who.x + 1;
+    if (!in_bounds(who.x >= 0 && who.y < kAttendTcCtas, p.c.status, kSiteAttendPart)) continue;
+    for (int at = r0 + (threadIdx.x >> 5); at < min(r0 + kJoinRows, rows); at += 8) {
+      auto part = [&](int c) { return ((int64_t)(who.x + c) * 2 + (c == 0 ? 1 : 0)) * kR + at % kR; };
+      float2 ml[kAttendTcCtas / 32];
+      float mx = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int k = 0; k < kAttendTcCtas / 32; ++k) {
+        ml[k] = k * 32 + lane < n ? p.part_ml[part(k * 32 + lane)] : make_float2(-INFINITY, 0.f);
+        mx = fmaxf(mx, ml[k].x);
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+      const float base = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+      for (int k = 0; k < kAttendTcCtas / 32; ++k) {
+        ml[k].x = fast_exp2(ml[k].x - base);
+        sum = fmaf(ml[k].y, ml[k].x, sum);
+      }
+      sum = warp_sum(sum);
+      float acc[V];
+#pragma unroll
+      for (int q = 0; q < V; ++q) acc[q] = 0.f;
+#pragma unroll
+      for (int k = 0; k < kAttendTcCtas / 32; ++k) {
+#pragma unroll 1
+        for (int c0 = 0; c0 < min(n - k * 32, 32); c0 += 16) {
+          alignas(16) float y[16][V];  // (all of them under way together)
+#pragma unroll
+          for (int c = 0; c < 16; ++c) {
+            const float* from = p.part_o + part(min(k * 32 + c0 + c, n - 1)) * D + lane * V;
+            if constexpr (V == 4)
+              *reinterpret_cast<float4*>(y[c]) = *reinterpret_cast<const float4*>(from);
+            else
+              *reinterpret_cast<float2*>(y[c]) = *reinterpret_cast<const float2*>(from);
+          }
+#pragma unroll
+          for (int c = 0; c < 16; ++c) {
+            const float w = __shfl_sync(0xffffffffu, ml[k].x, c0 + c);  // (0 past the last part)
+#pragma unroll
+            for (int q = 0; q < V; ++q) acc[q] = fmaf(y[c][q], k * 32 + c0 + c < n ? w : 0.f, acc[q]);
+          }
+        }
+      }
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      const int j = div_group(p, at);
+      const int64_t to = (s.row0 + j) * p.H + h * p.G + at - j * p.G;
+      if (!in_bounds(to < p.total_rows * p.H, p.c.status, kSiteAttendRow)) continue;
+#pragma unroll
+      for (int q = 0; q < V; ++q) p.pre_o[to * D + lane * V + q] = sum == 0.f ? 0.f : acc[q] * inv;
+      if (lane == 0) p.pre_l[to] = sum == 0.f ? -INFINITY : mx + log2f(sum);
+    }
+  }
+}
+
 // Once per device: the shared memory, and that the register split adds up --
 // setmaxnreg.inc waits for registers that only the launch's own can give.
 template <int D, bool BF16, int MODE>
@@ -1142,8 +1232,17 @@ int occam::launch_attend_tc(const AttendCall<MODE>& p, int dim, cudaStream_t st)
   CUtensorMap mk, mv;
   if (!encode_blocks(&mk, p.c, p.c.k, dim, p.c.T, false) || !encode_blocks(&mv, p.c, p.c.v, dim, p.c.T, false))
     return OCCAM_ERR_CUDA;
-  if (dim == 128) return p.bf16 ? launch<128, true>(p, mk, mv, st) : launch<128, false>(p, mk, mv, st);
-  return p.bf16 ? launch<64, true>(p, mk, mv, st) : launch<64, false>(p, mk, mv, st);
+  const int rc = dim == 128 ? (p.bf16 ? launch<128, true>(p, mk, mv, st) : launch<128, false>(p, mk, mv, st))
+                            : (p.bf16 ? launch<64, true>(p, mk, mv, st) : launch<64, false>(p, mk, mv, st));
+  if constexpr (MODE == kPrefix) {
+    if (rc != OCCAM_OK) return rc;
+    static_assert(kAttendTcCtas % 32 == 0, "parts a lane");
+    const int64_t want = p.total_rows * p.G / p.n / kJoinRows + 1;
+    const dim3 grid((unsigned)std::min<int64_t>(want, 1024), (unsigned)p.c.heads, (unsigned)p.n);
+    const bool ok = dim == 128 ? launch_after(join_kernel<128>, grid, 256, 0, st, p) : launch_after(join_kernel<64>, grid, 256, 0, st, p);
+    return ok && cudaGetLastError() == cudaSuccess ? OCCAM_OK : OCCAM_ERR_CUDA;
+  }
+  return rc;
 }
 template int occam::launch_attend_tc<kWhole>(const AttendCall<kWhole>&, int, cudaStream_t);
 template int occam::launch_attend_tc<kPrefix>(const AttendCall<kPrefix>&, int, cudaStream_t);

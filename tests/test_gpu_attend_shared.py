@@ -36,7 +36,7 @@ def branches(T, dim, hkv, groups, seed=0, gain=1.0):
     return c, kids, lengths
 
 
-def check(c, seqs, rows, group_sizes, heads, dtype=torch.bfloat16, seed=0, gain=1.5, hints=None, scale=0.0, causal=True):
+def check(c, seqs, rows, group_sizes, heads, dtype=torch.bfloat16, seed=0, gain=1.5, hints=None, scale=0.0, causal=True, known=None):
     import paper_2605_29657_gb300 as occ
     off, goff = offs(rows), offs(group_sizes)
     g = torch.Generator().manual_seed(seed)
@@ -48,7 +48,10 @@ def check(c, seqs, rows, group_sizes, heads, dtype=torch.bfloat16, seed=0, gain=
     out, lse = occ.occam_cache_attend_shared(c, 0, q, dev(seqs), dev(off, torch.int64), hints[0], dev(goff), hints[1], ws, scale=scale,
                                              causal=causal)
     assert c.status(ws=ws) == 0
-    want, wlse, tol, ltol = R.Cache(c).attend(0, q, seqs, off, scale, causal)
+    if not known:  # (a list: what an earlier call with the same arguments is held against)
+        known = [] if known is None else known
+        known.extend(R.Cache(c).attend(0, q, seqs, off, scale, causal))
+    want, wlse, tol, ltol = known
     tol = tol * (1 + 2.0 ** -9 + 2.0 ** -9 * wlse.nan_to_num(0, 0, 0).abs()[..., None])
     u, got = R.UNIT[dtype], out.double().cpu()
     assert torch.equal(torch.isnan(got), torch.isnan(want))
@@ -59,6 +62,62 @@ def check(c, seqs, rows, group_sizes, heads, dtype=torch.bfloat16, seed=0, gain=
     assert torch.equal(torch.isfinite(l), fin)
     assert bool(((l - wlse).abs() <= ltol + 2.0 ** -20 + 2.0 ** -21 * wlse.abs())[fin].all())
     return q, out, lse, ws
+
+
+def shared_tokens(c, ws, groups):
+    """What the last call on a workspace shared in each group (the first thing behind the other calls' scratch)."""
+    import ctypes
+    import paper_2605_29657_gb300 as occ
+    n = ctypes.c_size_t(0)
+    assert occ.library().occam_cache_workspace_size(c._ref, 0, ctypes.byref(n)) == 0
+    return ws[n.value:n.value + 4 * groups].view(torch.int32).tolist()
+
+
+PAYS = [
+    # T, dim, key heads, group, [(prefix, own tokens of each fork)], rows of each, full pages' tokens that are shared
+    (64, 128, 8, 4, [(1100, [1, 3, 70, 2] * 10)], [1] * 40, [1088]),
+    (16, 64, 16, 1, [(700, [1, 9] * 20)], [1, 2] * 20, [688]),
+    (128, 128, 8, 2, [(1000, [20] * 24), (700, [5] * 30), (900, [2])], [20] * 24 + [1] * 30 + [2], [896, 640, 0]),
+    (32, 128, 4, 8, [(1600, [9, 40] * 24)], [9] * 48, [1600]),
+    (16, 128, 2, 7, [(4000, [1] * 50)], [1] * 50, [4000]),
+    (64, 64, 4, 16, [(2900, [12, 13, 14] * 8), (2700, [12] * 24)], [12] * 48, [0, 0]),
+    # (192 rows a fork and key head fill three quarters of a tile of 256 without the others': 24 tiles against 18 over 22.5 x 128
+    # keys, 2 us each for 8 (group, head)s over 152 SMs: 14 us saved, and the two parts' joins cost 18 beside the launches' 15)
+    (64, 64, 4, 16, [(2900, [5, 6] * 12), (2700, [4] * 24)], [3] * 48, [2880, 2688]),
+    (32, 64, 8, 1, [(2000, [40, 35, 64, 129] * 8)], [35] * 32, [1984]),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n", range(len(PAYS)))
+def test_attend_shared_where_it_pays(n, dtype):
+    """Groups large enough that the pages are read once: single tokens and rows of more than one tile, prefixes split over
+    all CTAs."""
+    T, dim, hkv, G, groups, rows, tokens = PAYS[n]
+    c, seqs, _ = branches(T, dim, hkv, groups, n)
+    sizes = [len(own) for _, own in groups]
+    known = []
+    q, out, lse, ws = check(c, seqs, rows, sizes, hkv * G, DT[dtype], n, known=known)
+    assert shared_tokens(c, ws, len(sizes)) == tokens
+    import paper_2605_29657_gb300 as occ
+    off, goff = offs(rows), dev(offs(sizes))
+    most = max(sum(rows[a:b]) for a, b in zip(offs(sizes), offs(sizes)[1:]))
+    for _ in range(3):  # the same every time
+        o, l = occ.occam_cache_attend_shared(c, 0, q, dev(seqs), dev(off, torch.int64), max(rows), goff, most, ws)
+        assert torch.equal(o, out) and torch.equal(l, lse)
+    # the hints choose kernels only
+    for hints in ((0, 0), (1, 10000), (max(rows), 1)):
+        check(c, seqs, rows, sizes, hkv * G, DT[dtype], n, hints=hints, known=known)
+    if dtype == "bf16":
+        check(c, seqs, rows, sizes, hkv * G, DT[dtype], n + 50, causal=False, scale=0.3)
+
+
+def test_attend_shared_values_that_are_nan_where_it_pays():
+    c, seqs, _ = branches(64, 128, 8, [(1100, [3, 40] * 20)], 3)
+    c.v.view(torch.uint8)[0, int(c.table[seqs[1], 17]), 2, 20, 9] = 0x7f   # an own token of the second fork
+    c.v.view(torch.uint8)[0, int(c.table[seqs[2], 5]), 3, 7, 3] = 0xff     # a token of the prefix
+    for rows in ([1] * 40, [3, 20] * 20):
+        check(c, seqs, rows, [40], 16)
 
 
 SHARED = [
