@@ -675,7 +675,7 @@ int occam_prompt_workspace_size(int64_t total_rows, int64_t total_keys, int32_t 
  * A row that sees no key gives 0 and -inf; rows of no sequence are left as they
  * are. Scores, statistics and sums are in fp32; p is rounded to the values' type for its
  * product with v. A value that is not finite reaches the rows that see
- * it and no others. out and lse overlap no input. After OCCAM_ERR_TIMEOUT the results
+ * it and no others. out and lse overlap no input and not each other. After OCCAM_ERR_TIMEOUT the results
  * are undefined; the workspace stays usable. */
 int occam_prompt_attend(const occam_prompt_args* args, void* out, float* lse, void* workspace, size_t workspace_bytes,
                         occam_stream_t stream);

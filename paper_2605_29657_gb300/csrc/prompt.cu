@@ -741,9 +741,9 @@ extern "C" int occam_prompt_attend(const occam_prompt_args* a, void* out, float*
   PromptParams p{};
   OCCAM_TRY(prompt_params(a, workspace, workspace_bytes, &p));
   if (a->n == 0 || a->total_rows == 0) return OCCAM_OK;
-  if (!out || !aligned16(out) || prompt_meets_inputs(a, extent(out, a->total_rows, (int64_t)a->heads * a->dim, 1, 0, (int64_t)a->heads * a->dim, 2)) ||
-      (lse && prompt_meets_inputs(a, extent(lse, 1, 0, 1, 0, a->total_rows * a->heads * 2, 2))))
-    return OCCAM_ERR_INVALID_ARG;
+  const int64_t width = (int64_t)a->heads * a->dim;
+  const Extent o = extent(out, a->total_rows, width, 1, 0, width, 2), l = extent(lse, 1, 0, 1, 0, a->total_rows * a->heads * 2, 2);
+  if (!out || !aligned16(out) || prompt_meets_inputs(a, o) || (lse && (prompt_meets_inputs(a, l) || meet(o, l)))) return OCCAM_ERR_INVALID_ARG;
   p.out = static_cast<uint16_t*>(out);
   p.lse = lse;
   const bool bf16 = a->dtype == OCCAM_BF16;
