@@ -36,7 +36,9 @@ E4M3 = torch.float8_e4m3fn
 # these calls once a layer, and filling a ctypes structure field by field takes longer
 _ROPE_TENSOR = struct.Struct("@PPiqqqq")
 _ATTEND_ARGS = struct.Struct("@iiiiqqPPPiiPPfPPq")
+_APPEND_ROPE_ARGS = struct.Struct("@iiiiiiqPqPqPPPqPPP")
 assert _ROPE_TENSOR.size == ctypes.sizeof(CRopeTensor) and _ATTEND_ARGS.size == ctypes.sizeof(CAttendArgs)
+assert _APPEND_ROPE_ARGS.size == ctypes.sizeof(CAppendRopeArgs)
 
 
 def _bad(msg: str):
@@ -314,9 +316,15 @@ def occam_cache_append_rope(cache: PagedCache, layer: int, q, k, v, seqs, row_of
         packed, out_q = _rope_tensor(q, out_q, "q", rows, cache.dim, k.dtype, cache.at, stream)
     elif out_q is not None:
         _bad("out_q without q")
-    a = CAppendRopeArgs(int(layer), _ROWS[k.dtype], n, 2 * pairs, _PAIRING[pairing], positions.shape[0], rows, _ptr(k), _row_stride(k),
-                        _ptr(v), _row_stride(v), _ptr(seqs), _ptr(row_off), _ptr(positions), positions.stride(0), _ptr(inv_freq),
-                        _ptr(axis), packed)
+    try:
+        a = CAppendRopeArgs.from_buffer_copy(_APPEND_ROPE_ARGS.pack(
+            layer, _ROWS[k.dtype], n, 2 * pairs, _PAIRING[pairing], positions.shape[0], rows, k.data_ptr(), _row_stride(k), v.data_ptr(),
+            _row_stride(v), seqs.data_ptr(), row_off.data_ptr(), positions.data_ptr(), positions.stride(0), inv_freq.data_ptr(),
+            axis.data_ptr(), 0))
+    except struct.error as e:
+        _bad(f"layer: {e}")
+    if packed is not None:
+        a.q = packed
     _call(cache.at, library().occam_cache_append_rope, cache._ref, ctypes.byref(a), wp, wn, on)
     return out_q
 
