@@ -1237,8 +1237,9 @@ int occam::launch_attend_tc(const AttendCall<MODE>& p, int dim, cudaStream_t st)
   if constexpr (MODE == kPrefix) {
     if (rc != OCCAM_OK) return rc;
     static_assert(kAttendTcCtas % 32 == 0, "parts a lane");
-    const int64_t want = p.total_rows * p.G / p.n / kJoinRows + 1;
-    const dim3 grid((unsigned)std::min<int64_t>(want, 1024), (unsigned)p.c.heads, (unsigned)p.n);
+    // (eight CTAs an SM; more of them, most with nothing to join, took 17 us)
+    const int64_t want = p.total_rows * p.G / p.n / kJoinRows + 1, most = cache_sms() * 8 / ((int64_t)p.c.heads * p.n);
+    const dim3 grid((unsigned)std::max<int64_t>(std::min(want, most), 1), (unsigned)p.c.heads, (unsigned)p.n);
     const bool ok = dim == 128 ? launch_after(join_kernel<128>, grid, 256, 0, st, p) : launch_after(join_kernel<64>, grid, 256, 0, st, p);
     return ok && cudaGetLastError() == cudaSuccess ? OCCAM_OK : OCCAM_ERR_CUDA;
   }

@@ -77,12 +77,19 @@ __global__ void __launch_bounds__(256) stat_kernel(GradParams p) {
   const int64_t vectors = (of_v ? p.total_keys : p.total_rows) * heads;
   const int64_t base = (int64_t)blockIdx.x * (PER * kVectors);
   if (base >= vectors) return;
-  const int64_t row0 = base / heads;
+  const int64_t row0 = base >> 32 ? base / heads : (uint32_t)base / (uint32_t)heads;
   const int head0 = (int)(base - row0 * heads);
+  const float inv = 1.f / heads;
+  // The vector that this lane writes (sub < 4): the reduction below leaves it there.
+  const int mine = ((sub & 1) << 1) | ((sub >> 1) & 1);
+  const int64_t to = base + mine * PER + first;
+  const bool writes = sub < kVectors && to < vectors;
+  const float l = writes && !of_v ? p.lse[to] : 0.f;
   uint4 a[kVectors], b[kVectors];
 #pragma unroll
   for (int k = 0; k < kVectors; ++k) {
-    const int at = head0 + k * PER + first, row = at / heads;
+    // (at < heads + 128 <= 1152: the product is off by 2^-22 of at / heads, a 1 / (2 heads) from the next integer)
+    const int at = head0 + k * PER + first, row = (int)((at + 0.5f) * inv);
     a[k] = b[k] = make_uint4(0, 0, 0, 0);
     if (base + k * PER + first < vectors && sub * 8 < p.dim) {
       if (of_v) {
@@ -93,35 +100,46 @@ __global__ void __launch_bounds__(256) stat_kernel(GradParams p) {
       }
     }
   }
+  float dot[kVectors], sq[kVectors];
 #pragma unroll
   for (int k = 0; k < kVectors; ++k) {
     const uint32_t x[4] = {a[k].x, a[k].y, a[k].z, a[k].w}, y[4] = {b[k].x, b[k].y, b[k].z, b[k].w};
-    float dot = 0.f, sq = 0.f;
+    dot[k] = sq[k] = 0.f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float2 u = pair16<BF16>(x[e]), v = pair16<BF16>(y[e]);
-      dot = fmaf(u.x, v.x, fmaf(u.y, v.y, dot));
-      if (!BF16) sq = fmaf(v.x, v.x, fmaf(v.y, v.y, sq));
+      dot[k] = fmaf(u.x, v.x, fmaf(u.y, v.y, dot[k]));
+      if (!BF16) sq[k] = fmaf(v.x, v.x, fmaf(v.y, v.y, sq[k]));
+    }
+  }
+  // Exchanges that halve the vectors a lane has and double the lanes it has seen, then the rest of the lanes.
+  auto sum = [&](float (&x)[kVectors]) {
+#pragma unroll
+    for (int n = kVectors / 2, o = 1; n > 0; n >>= 1, o <<= 1) {
+#pragma unroll
+      for (int k = 0; k < n; ++k) {
+        const bool high = sub & o;
+        const float give = high ? x[k] : x[k + n], keep = high ? x[k + n] : x[k];
+        x[k] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+      }
     }
 #pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) {
-      dot += __shfl_xor_sync(0xffffffffu, dot, o);
-      if (!BF16) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-    }
-    const int64_t to = base + k * PER + first;
-    if (sub != 0 || to >= vectors) continue;
-    if (of_v) {
-      p.vnorm[to] = sqrtf(sq);
-    } else {
-      const float l = p.lse[to];
-      const float l2 = l == -INFINITY ? INFINITY : l * 1.44269504089f;  // (a row that sees nothing: every p is 0)
-      p.stat[to] = make_float2(l2, -dot);
-      // (finite in that row: a mask hides its keys there, and an infinity would meet the other product's units of 0)
-      const uint2 x = terms4<BF16>(l2 == INFINITY ? 0.f : -l2 / p.scale_log2), y = terms4<BF16>(-dot);
-      p.terms[2 * to] = make_uint4(x.x, x.y, y.x, y.y);
-      p.terms[2 * to + 1] = make_uint4(0, 0, 0, 0);
-      if (!BF16) p.norm[to] = sqrtf(sq);
-    }
+    for (int o = kVectors; o < LANES; o <<= 1) x[0] += __shfl_xor_sync(0xffffffffu, x[0], o);
+  };
+  static_assert(kVectors == 4 && LANES >= 4, "mine");
+  sum(dot);
+  if (!BF16) sum(sq);
+  if (!writes) return;
+  if (of_v) {
+    p.vnorm[to] = sqrtf(sq[0]);
+  } else {
+    const float l2 = l == -INFINITY ? INFINITY : l * 1.44269504089f;  // (a row that sees nothing: every p is 0)
+    p.stat[to] = make_float2(l2, -dot[0]);
+    // (finite in that row: a mask hides its keys there, and an infinity would meet the other product's units of 0)
+    const uint2 x = terms4<BF16>(l2 == INFINITY ? 0.f : -l2 / p.scale_log2), y = terms4<BF16>(-dot[0]);
+    p.terms[2 * to] = make_uint4(x.x, x.y, y.x, y.y);
+    p.terms[2 * to + 1] = make_uint4(0, 0, 0, 0);
+    if (!BF16) p.norm[to] = sqrtf(sq[0]);
   }
 }
 
