@@ -297,7 +297,7 @@ def occam_cache_append_rope(cache: PagedCache, layer: int, q, k, v, seqs, row_of
                             pairing: str = "half", out_q=None, ws=None, stream=None):
     """occam_cache_append with the keys turned by their positions (as occam_rope, in fp32 until they
     are rounded to codes) and the queries q [rows, heads, dim] (None: none) of the same rows
-    turned in the same launch. Returns the turned queries: a new dense tensor unless out_q is given (q
+    turned beside them. Returns the turned queries: a new dense tensor unless out_q is given (q
     itself: in place)."""
     wp, wn = _workspace(cache, ws)
     if pairing not in _PAIRING:

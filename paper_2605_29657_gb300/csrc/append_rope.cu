@@ -1,12 +1,14 @@
 // append_rope.cu -- occam_cache_append_rope: keys turned by their positions on
-// the way into the paged 8-bit cache, values beside them, and the queries turned in the
-// same launch.
+// the way into the paged 8-bit cache, values beside them, and the queries turned by a second launch
+// that overlaps with the first.
 //
 // A CTA takes one touched page and some heads of K or of V. Cosines and sines of the page's
 // tokens are computed once, into shared memory, and serve all its heads of K; the turned values stay
 // in registers as fp32 between the block's maximum and the rounding, so keys are rounded once, to their
 // codes. The queries are turned by a launch of their own (rope_rows) that starts while this one ends. Bound by HBM:
-// queries 2 bytes read and written, keys and values 2 read and 1 written a value.
+// queries 2 bytes read and written, keys and values 2 read and 1 written a value: 20 k rows of 32 + 32 + 32 heads of 128 in
+// 178 us, 0.70 of a plain copy (keys and values 117 us of it: partly filled pages, and a maximum before the first store).
+// A single row a sequence: 12 us, a chain of offsets, table, row, scale.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>

