@@ -642,9 +642,11 @@ int occam_cache_release(const occam_cache* cache, int32_t n, const int32_t* seqs
  * at places 0 .. m - r + j of m (none where that is negative); else all m. Values are
  * OCCAM_BF16 or OCCAM_F16, heads dense, rows q_row / k_row / v_row elements apart
  * (at least heads * dim; views of one projection fit); bases 16-byte aligned, strides
- * and dim multiples of 8, dim 8..128. heads <= 1024, n <= 2^20. Rows that belong to no
+ * and dim multiples of 8, dim 8..128. heads <= 1024, n <= 2^20, at
+ * most 2^31 - 1024 rows and keys. Rows that belong to no
  * sequence are not read into any result. Offsets that do not fit record
- * OCCAM_ERR_INVALID_ARG, and that sequence is left out. */
+ * OCCAM_ERR_INVALID_ARG, and that sequence is left out; offsets that go over the same rows more often than the tensors
+ * have rows record it, and nothing is done. */
 typedef struct occam_prompt_args {
   int32_t dtype;
   int32_t heads;

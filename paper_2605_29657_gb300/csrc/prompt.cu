@@ -589,7 +589,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   for (int e = threadIdx.x; e < kItems * 3 * 128; e += kThreads) (&sh.first[0][0][0])[e] = kNever;
   pdl_wait();
   if (warp == 12) tc::tmem_alloc(&sh.tmem, 512);
-  prompt_list(p, sh.list, Count{p});
+  prompt_list(p, sh.list, Count{p}, p.most);
   tc::fence_before();
   __syncthreads();
   tc::fence_after();
@@ -680,7 +680,7 @@ int occam::prompt_params(const occam_prompt_args* a, void* workspace, size_t wor
   if (!a) return OCCAM_ERR_INVALID_ARG;
   if (a->dtype != OCCAM_BF16 && a->dtype != OCCAM_F16) return OCCAM_ERR_UNSUPPORTED;
   if (a->dim < 8 || a->dim > 128 || a->dim % 8 != 0) return OCCAM_ERR_UNSUPPORTED;
-  if (a->total_rows < 0 || a->total_rows > 0x7fffffff || a->total_keys < 0 || a->total_keys > 0x7fffffff || a->n < 0 ||
+  if (a->total_rows < 0 || a->total_rows > kPromptRows || a->total_keys < 0 || a->total_keys > kPromptRows || a->n < 0 ||
       a->n > (1 << 20) || a->kv_heads < 1 || a->heads < 1 || a->heads > 1024 || a->heads % a->kv_heads != 0 || !(a->scale >= 0.f) ||
       !(a->scale < INFINITY))
     return OCCAM_ERR_INVALID_ARG;
@@ -731,7 +731,7 @@ bool occam::prompt_meets_inputs(const occam_prompt_args* a, const Extent& x) {
   } while (0)
 
 extern "C" int occam_prompt_workspace_size(int64_t total_rows, int64_t total_keys, int32_t heads, int32_t kv_heads, size_t* bytes) {
-  if (!bytes || total_rows < 0 || total_rows > 0x7fffffff || total_keys < 0 || total_keys > 0x7fffffff || heads < 1 ||
+  if (!bytes || total_rows < 0 || total_rows > kPromptRows || total_keys < 0 || total_keys > kPromptRows || heads < 1 ||
       heads > 1024 || kv_heads < 1 || kv_heads > heads)
     return OCCAM_ERR_INVALID_ARG;
   *bytes = prompt_ws(total_rows, total_keys, heads, kv_heads).total;
@@ -754,6 +754,7 @@ extern "C" int occam_prompt_attend(const occam_prompt_args* a, void* out, float*
   const int per = 256 >> p.log2P, heads = p.H >> p.log2P;
   const int64_t most = (a->total_rows / per + a->n) * heads;
   if (most > (1 << 30)) return OCCAM_ERR_UNSUPPORTED;
+  p.most = (int)most;
   CUtensorMap mq, mk, mv;
   // (without any keys the copies have to come from somewhere; what they bring is hidden)
   const bool none = a->total_keys == 0;

@@ -18,6 +18,7 @@ namespace occam {
 
 struct PromptParams {
   int n, H, Hkv, G, log2P, causal, dim;  // 2^log2P heads of a group are packed as rows of a tile
+  int most;                              // items of blocks of rows, of sequences that do not overlap
   int64_t total_rows, total_keys;
   const int64_t* row_off;
   const int64_t* key_off;
@@ -27,6 +28,8 @@ struct PromptParams {
   int32_t* status;
   int32_t* counters;  // [0] items taken beyond the first of each CTA, [1] CTAs that have left; zero between calls
 };
+
+constexpr int64_t kPromptRows = 0x7fffffff - 1023;  // places in a tile behind the last row still fit 32 bits
 
 // The smallest power of two above any factor of a score: never 0, so that a hidden key's -inf stays
 constexpr float kLeastFactor = 1.2e-38f;
@@ -70,21 +73,22 @@ struct PromptItem {
 // The prefix sums of item counts over kChunks runs of sequences are in shared memory.
 constexpr int kChunks = 128;
 struct PromptList {
+  long long part[4];
   int first[kChunks + 1];
-  int part[4];
 };
 
-// Block-wide, all threads (at least 128). COUNT(seq) gives a sequence's items.
+// Block-wide, all threads (at least 128). COUNT(seq) gives a sequence's items; most: what sequences that do not overlap have
+// at most. More (offsets that go back and forth over the same rows) is recorded, and there are no items.
 template <class Count>
-__device__ __forceinline__ void prompt_list(const PromptParams& p, PromptList& l, const Count& count) {
+__device__ __forceinline__ void prompt_list(const PromptParams& p, PromptList& l, const Count& count, int most) {
   const int t = threadIdx.x, per = (p.n + kChunks - 1) / kChunks;
-  int mine = 0, incl = 0;
+  long long mine = 0, incl = 0;
   if (t < kChunks) {
     for (int i = t * per; i < min((t + 1) * per, p.n); ++i) mine += count(prompt_seq(p, i));
     incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int x = __shfl_up_sync(0xffffffffu, incl, o);
+      const long long x = __shfl_up_sync(0xffffffffu, incl, o);
       if ((t & 31) >= o) incl += x;
     }
     if ((t & 31) == 31) l.part[t >> 5] = incl;
@@ -92,8 +96,12 @@ __device__ __forceinline__ void prompt_list(const PromptParams& p, PromptList& l
   __syncthreads();
   if (t < kChunks) {
     for (int w = 0; w < (t >> 5); ++w) incl += l.part[w];
-    l.first[t + 1] = incl;
-    if (t == 0) l.first[0] = 0;
+    const bool over = l.part[0] + l.part[1] + l.part[2] + l.part[3] > most;
+    l.first[t + 1] = over ? 0 : (int)incl;
+    if (t == 0) {
+      l.first[0] = 0;
+      if (over) set_status(p.status, OCCAM_ERR_INVALID_ARG);
+    }
   }
   __syncthreads();
 }

@@ -28,6 +28,7 @@ constexpr int kRegElement = 160, kRegWrite = 88, kRegIssue = 104;  // 2 x 160 + 
 constexpr int kRowBytes = 128;      // of 64 dims in a block
 
 struct GradParams : PromptParams {
+  int most_keys;  // items of tiles of keys, as `most`
   const uint16_t* o;
   const uint16_t* dout;
   int64_t dout_row, v_row;
@@ -680,7 +681,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   pdl_wait();
   if (warp == 12) tc::tmem_alloc(&sh.tmem, 512);
-  prompt_list(p, sh.list, Count{p});
+  prompt_list(p, sh.list, Count{p}, p.most_keys);
   tc::fence_before();
   __syncthreads();
   tc::fence_after();
@@ -1128,7 +1129,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   pdl_wait();
   if (warp == 12) tc::tmem_alloc(&sh.tmem, 512);
-  prompt_list(p, sh.list, Count{p});
+  prompt_list(p, sh.list, Count{p}, p.most);
   tc::fence_before();
   __syncthreads();
   tc::fence_after();
@@ -1269,6 +1270,8 @@ extern "C" int occam_prompt_attend_grad(const occam_prompt_args* a, const occam_
   const int per = 256 >> p.log2P, heads = p.H >> p.log2P, log_p = std::min(p.log2P, 6);
   const int64_t most_rows = R == 0 ? 0 : (R / per + a->n) * heads, most_keys = K == 0 ? 0 : (K / 128 + a->n) * p.Hkv;
   if (most_rows > (1 << 30) || most_keys > (1 << 30) || (!bf16 && p.Hkv > 65535)) return OCCAM_ERR_UNSUPPORTED;
+  p.most = (int)most_rows;
+  p.most_keys = (int)most_keys;
   // (without any rows, or any keys, the copies have to come from somewhere; what they bring is not used)
   const void* q = R > 0 ? a->q : a->k;
   const void* dout = R > 0 ? g->dout : a->k;

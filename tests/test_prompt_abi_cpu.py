@@ -61,7 +61,8 @@ def test_prompt_workspace_size(lib):
     assert prompt_size(lib, 0, 0, 1, 1)[0] == 0
     assert prompt_size(lib, 100000, 1000, 8, 2)[1] > n and prompt_size(lib, 1000, 1000, 16, 2)[1] > n
     assert prompt_size(lib, 1000, 100000, 8, 2)[1] >= n
-    for bad in ((-1, 1, 1, 1), (1, -1, 1, 1), (1 << 31, 1, 1, 1), (1, 1 << 31, 1, 1), (1, 1, 0, 1), (1, 1, 1025, 1), (1, 1, 2, 0),
+    assert prompt_size(lib, (1 << 31) - 1024, (1 << 31) - 1024, 1, 1)[0] == 0
+    for bad in ((-1, 1, 1, 1), (1, -1, 1, 1), ((1 << 31) - 1023, 1, 1, 1), (1 << 31, 1, 1, 1), (1, 1 << 31, 1, 1), (1, 1, 0, 1), (1, 1, 1025, 1), (1, 1, 2, 0),
                 (1, 1, 2, 3)):
         assert prompt_size(lib, *bad)[0] == invalid, bad
     assert lib.occam_prompt_workspace_size(1, 1, 1, 1, None) == invalid
@@ -70,7 +71,7 @@ def test_prompt_workspace_size(lib):
 @pytest.mark.parametrize("change,kind", [
     (dict(dtype=2), 1), (dict(dtype=-1), 1), (dict(dim=0), 1), (dict(dim=4), 1), (dict(dim=68), 1), (dict(dim=136), 1),
     (dict(heads=0), 0), (dict(heads=3), 0), (dict(heads=1026), 0), (dict(kv_heads=0), 0), (dict(kv_heads=8), 0), (dict(n=-1), 0),
-    (dict(n=(1 << 20) + 1), 0), (dict(rows=-1), 0), (dict(rows=1 << 31), 0), (dict(keys=-1), 0), (dict(keys=1 << 31), 0),
+    (dict(n=(1 << 20) + 1), 0), (dict(rows=-1), 0), (dict(rows=(1 << 31) - 1023), 0), (dict(keys=-1), 0), (dict(keys=(1 << 31) - 1023), 0),
     (dict(scale=-1.0), 0), (dict(scale=float("inf")), 0), (dict(scale=float("nan")), 0), (dict(row_off=None), 0),
     (dict(key_off=None), 0), (dict(q=None), 0), (dict(k=None), 0), (dict(v=None), 0), (dict(q=PTR + 8), 0), (dict(k=PTR + 2), 0),
     (dict(v=PTR + 4), 0), (dict(q_row=252), 0), (dict(q_row=248), 0), (dict(k_row=120), 0), (dict(v_row=132), 0),
