@@ -1141,9 +1141,9 @@ __global__ void __launch_bounds__(256) join_kernel(AttendCall<kPrefix> p) {
     const int tile = range_at(p, s.row0, blockIdx.z, r0 / kR);
     if (!in_bounds(tile < p.range_tiles, p.c.status, kSiteAttendPart)) continue;
     const int2 who = p.ranges[(int64_t)h * p.range_tiles + tile];
-    if (who.y <= who.x) continue;  // one part: it is the result
+    // one part: it is the result. (Whatever is there where the items were given up, which is recorded: no part to join.)
+    if (who.y <= who.x || who.x < 0 || who.y >= kAttendTcCtas) continue;
     const int n = who.y - who.x + 1;
-    if (!in_bounds(who.x >= 0 && who.y < kAttendTcCtas, p.c.status, kSiteAttendPart)) continue;
     for (int at = r0 + (threadIdx.x >> 5); at < min(r0 + kJoinRows, rows); at += 8) {
       auto part = [&](int c) { return ((int64_t)(who.x + c) * 2 + (c == 0 ? 1 : 0)) * kR + at % kR; };
       float2 ml[kAttendTcCtas / 32];
