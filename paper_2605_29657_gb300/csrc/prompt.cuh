@@ -10,6 +10,8 @@
 #include <cuda.h>
 #include <cuda_fp16.h>
 
+#include <algorithm>
+
 #include "cache.cuh"
 #include "overlap.cuh"
 #include "tc5.cuh"
@@ -27,6 +29,7 @@ struct PromptParams {
   float* lse;
   int32_t* status;
   int32_t* counters;  // [0] items taken beyond the first of each CTA, [1] CTAs that have left; zero between calls
+                      // [2] (the gradient's keys) whether there are items, for the launch that adds up their parts
 };
 
 constexpr int64_t kPromptRows = 0x7fffffff - 1023;  // places in a tile behind the last row still fit 32 bits
@@ -67,6 +70,7 @@ struct PromptItem {
   int tile, hb;    // the block of rows (or keys) and the block of heads
   int steps;       // 0: there is none, the CTA is done
   int nk[2];       // steps of each row tile
+  int step0, part; // (the gradient's keys) the first step; the part of a divided item, -1: it is whole, -2: there is no such part
 };
 
 // How a kernel cuts a sequence: `len` rows (or keys) in blocks of `block`, head blocks inner.
@@ -205,8 +209,14 @@ bool encode_rows(CUtensorMap* m, const void* at, bool bf16, int dim, int heads, 
 // Byte offsets of the workspace: the status word (8 bytes) and the counters, zero between calls; then what the
 // gradient writes before it reads it (see GradParams).
 struct PromptWs {
-  size_t terms, stat, norm, power, vnorm, total;
+  size_t terms, stat, norm, power, vnorm, split, total;
 };
+// How many parts an item of the gradient's keys may be divided into: where there are fewer items than two an SM, one of them
+// would be a CTA's whole time.
+constexpr int kPartItems = 304, kMostParts = 8;
+inline int prompt_parts(int64_t items) {
+  return items < 1 ? 1 : (int)std::min<int64_t>(std::max<int64_t>(kPartItems / items, 1), kMostParts);
+}
 inline PromptWs prompt_ws(int64_t total_rows, int64_t total_keys, int heads, int kv_heads) {
   PromptWs w;
   w.terms = 256;
@@ -214,7 +224,10 @@ inline PromptWs prompt_ws(int64_t total_rows, int64_t total_keys, int heads, int
   w.norm = w.stat + cache_align((size_t)total_rows * heads * 8);
   w.power = w.norm + cache_align((size_t)total_rows * heads * 4);
   w.vnorm = w.power + cache_align((size_t)total_rows * kv_heads * 4);
-  w.total = w.vnorm + cache_align((size_t)total_keys * kv_heads * 4);
+  w.split = w.vnorm + cache_align((size_t)total_keys * kv_heads * 4);
+  // (parts x keys is at most kPartItems tiles' keys; never less for more keys or heads: a workspace serves smaller calls)
+  const size_t split = std::min<size_t>((size_t)kMostParts * total_keys * kv_heads, kPartItems * 128);
+  w.total = w.split + cache_align(split * 2 * 128 * 4);
   return w;
 }
 

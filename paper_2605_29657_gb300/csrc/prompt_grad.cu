@@ -4,8 +4,10 @@
 //   dV = P^T dO,  dS = P (dP - delta),  dQ = scale dS K,  dK = scale dS^T Q.
 // Neither P nor dS goes to memory: two kernels on the fifth-generation tensor cores form them again, one that
 // owns keys (dK, dV; 8 D operations a (row, head, key)) and one that owns rows (dQ; 6 D). Every
-// sum has one CTA and one order, the heads of a group included, so results repeat bit for bit; a kernel that
-// owned keys alone would do with 10 D in all but add dQ across CTAs.
+// sum has one order, the heads of a group included, so results repeat bit for bit; a kernel that
+// owned keys alone would do with 10 D in all but add dQ across CTAs. Where there are few tiles of keys their rows are
+// divided into up to 8 parts of 16 steps or more, whose sums in fp32 a last launch adds up in order (1,000 rows, 8 heads on one
+// key head: 119 -> 64 us; 3,500 rows, 5 on one: 264 -> 134; 2,400 rows, 28 on 4: 265 -> 177).
 // Before them a pass over dO and O forms delta; with f16, where dS has no range to spare, also the norms
 // that bound it: |dP - delta| <= |dO||V| + |delta|, and dS is held times a power of two a sequence and key head that
 // brings that bound under f16's end.
@@ -15,6 +17,7 @@
 #include <algorithm>
 #include <atomic>
 
+#include "append.cuh"
 #include "nvtx.cuh"
 #include "prompt.cuh"
 
@@ -29,6 +32,8 @@ constexpr int kRowBytes = 128;      // of 64 dims in a block
 
 struct GradParams : PromptParams {
   int most_keys;  // items of tiles of keys, as `most`
+  int parts;      // of an item of keys, at most
+  float* split;   // [parts, 2, total_keys, kv_heads, dim] sums of dV and dK of divided items
   const uint16_t* o;
   const uint16_t* dout;
   int64_t dout_row, v_row;
@@ -252,7 +257,20 @@ struct Shared {
 
 struct Count {
   const GradParams& p;
-  __device__ __forceinline__ int operator()(const PromptSeq& s) const { return (s.keys / 128 + (s.keys % 128 != 0)) * p.Hkv; }
+  __device__ __forceinline__ int operator()(const PromptSeq& s) const { return (s.keys / 128 + (s.keys % 128 != 0)) * p.Hkv * p.parts; }
+};
+// A tile's first block of rows, blocks of a head block, and steps; parts of so many steps.
+constexpr int kPartSteps = 16;
+struct Tile {
+  int first, blocks, steps, parts;
+
+  __device__ __forceinline__ Tile(const GradParams& p, const PromptSeq& s, int tile, int log_p) {
+    const int log_t = 6 - log_p;
+    first = (p.causal ? max(tile * 128 - (s.keys - s.rows), 0) : 0) >> log_t;
+    blocks = max(((s.rows + (1 << log_t) - 1) >> log_t) - first, 0);
+    steps = blocks * (p.G >> log_p);
+    parts = min(max(steps / kPartSteps, 1), p.parts);
+  }
 };
 
 // A walk over an item's steps: blocks of tokens, head block by head block.
@@ -263,8 +281,10 @@ struct Steps {
   __device__ __forceinline__ Steps(const GradParams& p, const PromptItem& it, int log_p) {
     tokens = 1 << (6 - log_p);
     more = it.rows;
-    tok0 = tok = it.nk[0] << (6 - log_p);
-    head = it.hb * p.G;
+    tok0 = it.nk[0] << (6 - log_p);
+    const int blocks = max(((it.rows + tokens - 1) >> (6 - log_p)) - it.nk[0], 1), skip = it.step0 / blocks;
+    tok = tok0 + (it.step0 - skip * blocks) * tokens;
+    head = it.hb * p.G + (skip << log_p);
   }
   __device__ __forceinline__ void next(int log_p) {
     tok += tokens;
@@ -334,19 +354,21 @@ __device__ __forceinline__ void look_role(const GradParams& p, Sh& sh, int log_p
     const int place = taker.take(p, sh.list, Count{p});
     const PromptSeq& s = taker.s;
     if (place >= 0) {
-      const int tile = place / p.Hkv, log_t = 6 - log_p;
-      const int first = (p.causal ? max(tile * 128 - (s.keys - s.rows), 0) : 0) >> log_t;
-      const int blocks = ((s.rows + (1 << log_t) - 1) >> log_t) - first;
+      const int tile = place / (p.Hkv * p.parts), at = place - tile * (p.Hkv * p.parts), hb = at / p.parts, part = at - hb * p.parts;
+      const Tile x(p, s, tile, log_p);
+      const int a = (int)((int64_t)x.steps * part / x.parts), b = (int)((int64_t)x.steps * (part + 1) / x.parts);
       if (lane == 0) {
         it.row0 = s.row0;
         it.key0 = s.key0;
         it.rows = s.rows;
         it.keys = s.keys;
         it.tile = tile;
-        it.hb = place - tile * p.Hkv;
-        it.steps = max(blocks, 0) * (p.G >> log_p);
-        it.nk[0] = first;
+        it.hb = hb;
+        it.steps = part < x.parts ? b - a : 0;
+        it.nk[0] = x.first;
         it.nk[1] = 0;
+        it.step0 = part < x.parts ? a : 0;
+        it.part = part >= x.parts ? -2 : x.parts > 1 ? part : -1;
       }
     } else if (lane == 0) {
       it.steps = 0;
@@ -367,7 +389,7 @@ __device__ __forceinline__ void look_role(const GradParams& p, Sh& sh, int log_p
     const int steps = sh.item[i % kItems].steps, rows = sh.item[i % kItems].rows, first = sh.item[i % kItems].nk[0];
     const int log_t = 6 - log_p, blocks = ((rows + (1 << log_t) - 1) >> log_t) - first;
     const int last = (rows & ((1 << log_t) - 1)) << log_p;  // rows of the last block of tokens, 0: it is whole
-    int block = 0;
+    int block = sh.item[i % kItems].step0 % max(blocks, 1);
 #pragma unroll 1
     for (int k = 0; k < steps; ++k, ++j) {
       const int st = j % S::kStages;
@@ -437,7 +459,7 @@ __device__ __forceinline__ void issue_role(const GradParams& p, Sh& sh, uint32_t
         const int log_t = 6 - log_p;
         end = base + x.steps;
         blocks = max(((x.rows + (1 << log_t) - 1) >> log_t) - x.nk[0], 1);
-        block = (int)(j - base);  // 0 or 1, or more where there is no own step
+        block = (int)(j - base) + x.step0 % blocks;  // (past the last one: below)
         ragged = (x.rows & ((1 << log_t) - 1)) != 0;
       }
       if (end > base) ++n_kv;
@@ -598,8 +620,33 @@ __device__ __forceinline__ void write_role(const GradParams& p, Sh& sh, unsigned
       ++n;
     }
     const float back = BF16 || it.steps == 0 ? 1.f : 1.f / p.power[it.row0 * p.Hkv + it.hb];
+    if (it.part >= 0) {
+      // a part's sums as they are, a key a lane (added up and rounded by split_kernel)
+      const int64_t key = (int64_t)it.tile * 128 + warp * 32 + lane;
+      const bool there = key < it.keys && in_bounds(it.key0 + key < p.total_keys && it.part < p.parts, p.status, kSitePromptRow);
 #pragma unroll 1
-    for (int which = 0; which < 2; ++which) {
+      for (int which = 0; which < 2; ++which) {
+        float* to = p.split + ((((int64_t)it.part * 2 + which) * p.total_keys + it.key0 + key) * p.Hkv + it.hb) * p.dim;
+        const float f = which ? p.scale * back : Lift<BF16>::kBack;
+#pragma unroll 1
+        for (int c = 0; c < DP; c += 16) {
+          uint32_t o[16];
+          tc::tmem_ld16(tmem + 256 + which * 128 + lanes + c, o);
+          if (there) {
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+              if (c + e < p.dim)
+                *reinterpret_cast<float4*>(to + c + e) = make_float4(__uint_as_float(o[e]) * f, __uint_as_float(o[e + 1]) * f,
+                                                                     __uint_as_float(o[e + 2]) * f, __uint_as_float(o[e + 3]) * f);
+          }
+          __syncwarp();
+        }
+      }
+      tc::fence_before();
+      tc::bar_arrive(&sh.o_free);
+    }
+#pragma unroll 1
+    for (int which = it.part == -1 ? 0 : 2; which < 2; ++which) {
       uint16_t* base = which ? p.dk : p.dv;
       const int64_t row = which ? p.dk_row : p.dv_row;
       const float f = which ? p.scale * back : Lift<BF16>::kBack;
@@ -682,6 +729,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   pdl_wait();
   if (warp == 12) tc::tmem_alloc(&sh.tmem, 512);
   prompt_list(p, sh.list, Count{p}, p.most_keys);
+  if (blockIdx.x == 0 && threadIdx.x == 0) p.counters[2] = sh.list.first[kChunks];
   tc::fence_before();
   __syncthreads();
   tc::fence_after();
@@ -1169,6 +1217,46 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // Once per device and kernel: the shared memory, and that the register split adds up --
 // setmaxnreg.inc waits for registers that only the launch's own can give.
+// dV and dK of the items that were divided: their parts' sums in order. A CTA takes 32 keys of a tile: grid x over slots of
+// sequences' tiles, y over key heads and the two gradients, z over quarters.
+template <bool BF16>
+__global__ void __launch_bounds__(256) split_kernel(GradParams p, int log_p) {
+  __shared__ int sh_seq;
+  pdl_wait();
+  if (p.counters[2] == 0) return;  // (offsets that were refused)
+  if (threadIdx.x < 32) {
+    const int i = slot_sequence(p.key_off, p.n, 7, blockIdx.x);
+    if (threadIdx.x == 0) sh_seq = i;
+  }
+  __syncthreads();
+  const PromptSeq s = prompt_seq(p, sh_seq);
+  const int64_t tile = (int64_t)blockIdx.x - ((s.key0 >> 7) + 2 * (int64_t)sh_seq), first = tile * 128 + blockIdx.z * 32;
+  if (tile < 0 || first >= s.keys) return;
+  const keys::Tile x(p, s, (int)tile, log_p);
+  if (x.parts < 2) return;
+  const int hb = blockIdx.y >> 1, which = blockIdx.y & 1, pieces = p.dim / 4, keys = (int)min((int64_t)32, s.keys - first);
+  uint16_t* base = which ? p.dk : p.dv;
+  const int64_t row = which ? p.dk_row : p.dv_row, part = 2 * p.total_keys * p.Hkv * p.dim;
+  for (int e = threadIdx.x; e < keys * pieces; e += 256) {
+    const int r = e / pieces, c = (e - r * pieces) * 4;
+    const int64_t key = s.key0 + first + r;
+    if (!in_bounds(key < p.total_keys, p.status, kSitePromptRow)) continue;
+    const float* from = p.split + ((which * p.total_keys + key) * p.Hkv + hb) * p.dim + c;
+    float4 y[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) y[k] = k < x.parts ? *reinterpret_cast<const float4*>(from + k * part) : make_float4(0.f, 0.f, 0.f, 0.f);
+    float4 sum = y[0];
+#pragma unroll
+    for (int k = 1; k < 8; ++k) {
+      sum.x += y[k].x;
+      sum.y += y[k].y;
+      sum.z += y[k].z;
+      sum.w += y[k].w;
+    }
+    *reinterpret_cast<uint2*>(base + key * row + hb * p.dim + c) = make_uint2(pack16<BF16>(sum.x, sum.y), pack16<BF16>(sum.z, sum.w));
+  }
+}
+
 template <class Kernel, class... Maps>
 int launch(Kernel kern, std::atomic<uint64_t>& ready, int smem, int grid, cudaStream_t st, const GradParams& p, const Maps&... maps) {
   int dev = 0;
@@ -1208,7 +1296,15 @@ int launch_grad(const GradParams& p, const CUtensorMap (&mk)[5], const CUtensorM
     const int rc = launch(keys::prompt_keys_kernel<DP, BF16>, ready_k, smem_k, grid_keys, st, p, mk[0], mk[1], mk[2], mk[3], mk[4]);
     if (rc != OCCAM_OK) return rc;
   }
-  return grid_rows > 0 ? launch(rows::prompt_rows_kernel<DP, BF16>, ready_r, smem_r, grid_rows, st, p, mr[0], mr[1], mr[2], mr[3]) : OCCAM_OK;
+  if (grid_rows > 0) {
+    const int rc = launch(rows::prompt_rows_kernel<DP, BF16>, ready_r, smem_r, grid_rows, st, p, mr[0], mr[1], mr[2], mr[3]);
+    if (rc != OCCAM_OK) return rc;
+  }
+  if (p.parts > 1) {
+    const dim3 grid((unsigned)(p.total_keys / 128 + 2 * (int64_t)p.n), (unsigned)p.Hkv * 2, 4);
+    if (!launch_after(split_kernel<BF16>, grid, 256, 0, st, p, std::min(p.log2P, 6)) || cudaGetLastError() != cudaSuccess) return OCCAM_ERR_CUDA;
+  }
+  return OCCAM_OK;
 }
 
 }  // namespace
@@ -1270,8 +1366,12 @@ extern "C" int occam_prompt_attend_grad(const occam_prompt_args* a, const occam_
   const int per = 256 >> p.log2P, heads = p.H >> p.log2P, log_p = std::min(p.log2P, 6);
   const int64_t most_rows = R == 0 ? 0 : (R / per + a->n) * heads, most_keys = K == 0 ? 0 : (K / 128 + a->n) * p.Hkv;
   if (most_rows > (1 << 30) || most_keys > (1 << 30) || (!bf16 && p.Hkv > 65535)) return OCCAM_ERR_UNSUPPORTED;
+  // Few items of keys are divided, where one may have the steps for it: a group's heads by blocks of 64 rows.
+  p.parts = prompt_parts(std::max<int64_t>((K + 127) / 128, a->n) * p.Hkv);
+  if ((R / (64 >> log_p) + 1) * (p.G >> log_p) < 2 * keys::kPartSteps) p.parts = 1;
+  p.split = ws_at<float>(workspace, w.split);
   p.most = (int)most_rows;
-  p.most_keys = (int)most_keys;
+  p.most_keys = (int)(most_keys * p.parts);
   // (without any rows, or any keys, the copies have to come from somewhere; what they bring is not used)
   const void* q = R > 0 ? a->q : a->k;
   const void* dout = R > 0 ? g->dout : a->k;
@@ -1289,7 +1389,7 @@ extern "C" int occam_prompt_attend_grad(const occam_prompt_args* a, const occam_
       !encode_rows(&mr[1], dout, bf16, p.dim, p.H, rows, do_row, 1 << p.log2P, 128 >> p.log2P) ||
       !encode_rows(&mr[2], k, bf16, p.dim, p.Hkv, keys_n, k_row, 1, 64) || !encode_rows(&mr[3], v, bf16, p.dim, p.Hkv, keys_n, v_row, 1, 64))
     return OCCAM_ERR_CUDA;
-  const int grid_rows = (int)std::min<int64_t>(cache_sms(), most_rows), grid_keys = (int)std::min<int64_t>(cache_sms(), most_keys);
+  const int grid_rows = (int)std::min<int64_t>(cache_sms(), most_rows), grid_keys = (int)std::min<int64_t>(cache_sms(), p.most_keys);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   if (p.dim <= 64)
     return bf16 ? launch_grad<64, true>(p, mk, mr, grid_keys, grid_rows, st) : launch_grad<64, false>(p, mk, mr, grid_keys, grid_rows, st);

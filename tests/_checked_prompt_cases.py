@@ -22,11 +22,13 @@ def main() -> int:
     import test_gpu_cache_short as C
     import test_gpu_prompt as P
     import test_gpu_prompt_grad as G
+    import test_gpu_prompt_grad_parts as GP
     import test_gpu_prompt_serving as V
 
     assert "liboccam_checked.so" in occ.library()._name
     cases = [(P.test_prompt, (n, ("bf16", "f16")[n % 2])) for n in range(len(P.CASES))]
     cases += [(G.test_grad, (n, ("f16", "bf16")[n % 2])) for n in range(len(P.CASES))]
+    cases += [(GP.test_grad_of_few_key_heads, (n, ("bf16", "f16")[n % 2])) for n in range(len(GP.PARTS))]
     cases += [(S.test_attend_shared, (n, "bf16")) for n in range(len(S.SHARED))]
     cases += [(S.test_attend_shared_where_it_pays, (n, "f16")) for n in range(len(S.PAYS))]
     cases += [
