@@ -212,7 +212,8 @@ struct PromptWs {
   size_t terms, stat, norm, power, vnorm, split, total;
 };
 // How many parts an item of the gradient's keys may be divided into: where there are fewer items than two an SM, one of them
-// would be a CTA's whole time.
+// would be a CTA's whole time. (2,400 rows of 28 heads on 4: 178 us; parts for 228 items: 190, for 608: 196. 4,177 of 32
+// on 8, whole: 404, in two: 424.)
 constexpr int kPartItems = 304, kMostParts = 8;
 inline int prompt_parts(int64_t items) {
   return items < 1 ? 1 : (int)std::min<int64_t>(std::max<int64_t>(kPartItems / items, 1), kMostParts);
