@@ -690,7 +690,8 @@ int occam_prompt_attend(const occam_prompt_args* args, void* out, float* lse, vo
  * sums over the rows that see the key, of all heads of its group, or the keys that the row sees. p and ds
  * are rounded to the inputs' type for their products (f16: ds by a power of two a sequence and key
  * head that uses its range; |lse / scale| and |dout.out| below 2^31); sums are in fp32, in an order that does not depend on timing. Rows that
- * see nothing have gradient 0, and so have keys that nobody sees; rows and keys of no sequence are
+ * see nothing have gradient 0, and so have keys that nobody sees; a row that sees one key has dq 0 and adds nothing to dk,
+ * exactly (its softmax is 1 whatever q and k are); rows and keys of no sequence are
  * left as they are. A value that is not finite may make any gradient of its sequence not finite, but none
  * of another's. dout, dq, dk and dv: 16-byte aligned, heads dense, rows a multiple of 8 elements apart, so
  * that the three gradients may be views of one projection's. They overlap no input and not

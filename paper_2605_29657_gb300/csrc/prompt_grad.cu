@@ -583,6 +583,14 @@ __device__ __forceinline__ void element_role(const GradParams& p, Sh& sh, int lo
       tc::tmem_wait_st();
       tc::fence_before();
       tc::bar_arrive(&sh.p_full[b]);
+      // Rows that see one key (the first one): p is 1 whatever the score, so dS is 0, not what two sums of the same products
+      // leave of one another.
+      const int one = -(ahead + at.tok);  // the block's token that sees one key of a causal sequence
+      if (PROMPT_RARE(p.causal ? it.tile == 0 && one >= 0 && one < at.tokens : it.keys == 1)) {
+        const int lo = p.causal ? one << log_p : 0, hi = p.causal ? (one + 1) << log_p : kQ;
+#pragma unroll
+        for (int e = 0; e < 64; ++e) pr[e] = e >= lo && e < hi ? 0.f : pr[e];
+      }
       WAIT(sh.dp_full[b], done & 1);
       tc::fence_after();
       tc::tmem_ld64(dp_at, v);
@@ -1058,7 +1066,7 @@ __device__ __forceinline__ void element_role(const GradParams& p, Sh& sh, uint32
         }
       }
       if (PROMPT_RARE((k + 1) * kKeys > common)) {
-        const int lim = limit - k * kKeys;
+        const int lim = (limit == 1 ? 0 : limit) - k * kKeys;  // (a row that sees one key: dS is 0, as in the kernel of keys)
 #pragma unroll
         for (int e = 0; e < 64; ++e) pr[e] = e < lim ? pr[e] : 0.f;
       }

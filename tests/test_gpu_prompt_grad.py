@@ -229,3 +229,38 @@ def test_grad_refusals():
         with pytest.raises(occ.OccamError):
             call(**bad)
     call(dq=whole[:, :4], dk=whole[:, 4:6], dv=whole[:, 6:])
+
+
+# rows, keys (None: the same), heads, key heads, dims
+ONE_KEY = [
+    ([1], None, 8, 1, 128), ([1], None, 3, 3, 64), ([1] * 70, None, 32, 8, 128), ([300, 1, 2], None, 5, 1, 72), ([5, 300, 70], [1, 1, 3], 8, 2, 128),
+    ([200, 129], [70, 129], 128, 1, 16), ([1000], None, 8, 1, 64),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n", range(len(ONE_KEY)))
+def test_grad_of_rows_that_see_one_key(n, dtype):
+    """Their softmax is 1 whatever q and k are: dq is 0, and dk does not depend on them. Exactly."""
+    import paper_2605_29657_gb300 as occ
+    rows, keys, H, Hkv, D = ONE_KEY[n]
+    q, k, v = inputs(rows, keys, H, Hkv, D, DT[dtype], n)
+    dout = gradient_of(q, DT[dtype], n)
+    keys = rows if keys is None else keys
+    off, koff, ws = offs(rows), offs(keys), occ.alloc_prompt_workspace(sum(rows), H, sum(keys), Hkv)
+    for causal in (True, False):
+        check(q, k, v, dout, off, koff, causal=causal, where=str(causal))
+        sees = [max(m - r + j + 1, 0) if causal else m for r, m in zip(rows, keys) for j in range(r)]
+        one = torch.tensor([s == 1 for s in sees], device="cuda")
+        most = [max([min(sees[a + j], m) for j in range(r)]) for a, r, m in zip(off, rows, keys)]
+        kw = dict(key_off=dev(koff), causal=causal)
+        got = []
+        for x in (q, torch.where(one[:, None, None], -0.5 * q, q)):
+            out, lse = occ.occam_prompt_attend(x, k, v, dev(off), ws, **kw)
+            got.append(occ.occam_prompt_attend_grad(x, k, v, out, lse, dout, dev(off), ws, **kw))
+        for dq, dk, _ in got:
+            assert not dq[one].any()
+            for i, s in enumerate(most):
+                assert s > 1 or not dk[koff[i]:koff[i + 1]].any()
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    assert occ.occam_get_status(ws) == 0
