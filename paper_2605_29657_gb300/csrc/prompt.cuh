@@ -29,7 +29,6 @@ struct PromptParams {
   float* lse;
   int32_t* status;
   int32_t* counters;  // [0] items taken beyond the first of each CTA, [1] CTAs that have left; zero between calls
-                      // [2] (the gradient's keys) whether there are items, for the launch that adds up their parts
 };
 
 constexpr int64_t kPromptRows = 0x7fffffff - 1023;  // places in a tile behind the last row still fit 32 bits

@@ -17,7 +17,6 @@
 #include <algorithm>
 #include <atomic>
 
-#include "append.cuh"
 #include "nvtx.cuh"
 #include "prompt.cuh"
 
@@ -738,7 +737,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   pdl_wait();
   if (warp == 12) tc::tmem_alloc(&sh.tmem, 512);
   prompt_list(p, sh.list, Count{p}, p.most_keys);
-  if (blockIdx.x == 0 && threadIdx.x == 0) p.counters[2] = sh.list.first[kChunks];
   tc::fence_before();
   __syncthreads();
   tc::fence_after();
@@ -1224,24 +1222,33 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 }  // namespace rows
 
-// Once per device and kernel: the shared memory, and that the register split adds up --
-// setmaxnreg.inc waits for registers that only the launch's own can give.
-// dV and dK of the items that were divided: their parts' sums in order. A CTA takes 32 keys of a tile: grid x over slots of
-// sequences' tiles, y over key heads and the two gradients, z over quarters.
+// dV and dK of the items that were divided: their parts' sums in order. A CTA takes 32 keys of a tile: grid x over the
+// sequences' tiles, found as the kernel of keys finds its items (offsets may go back behind a sequence that does not
+// fit), y over key heads and the two gradients, z over quarters.
+struct Tiles {
+  __device__ __forceinline__ int operator()(const PromptSeq& s) const { return s.keys / 128 + (s.keys % 128 != 0); }
+};
 template <bool BF16>
 __global__ void __launch_bounds__(256) split_kernel(GradParams p, int log_p) {
-  __shared__ int sh_seq;
+  __shared__ PromptList list;
+  __shared__ PromptSeq sh_seq;
+  __shared__ int sh_tile;
   pdl_wait();
-  if (p.counters[2] == 0) return;  // (offsets that were refused)
+  prompt_list(p, list, Tiles{}, p.most_keys / (p.Hkv * p.parts));
+  if ((int)blockIdx.x >= list.first[kChunks]) return;
   if (threadIdx.x < 32) {
-    const int i = slot_sequence(p.key_off, p.n, 7, blockIdx.x);
-    if (threadIdx.x == 0) sh_seq = i;
+    PromptTaker at;
+    at.find(p, list, Tiles{}, blockIdx.x);
+    if (threadIdx.x == 0) {
+      sh_seq = at.s;
+      sh_tile = (int)blockIdx.x - at.begin;
+    }
   }
   __syncthreads();
-  const PromptSeq s = prompt_seq(p, sh_seq);
-  const int64_t tile = (int64_t)blockIdx.x - ((s.key0 >> 7) + 2 * (int64_t)sh_seq), first = tile * 128 + blockIdx.z * 32;
-  if (tile < 0 || first >= s.keys) return;
-  const keys::Tile x(p, s, (int)tile, log_p);
+  const PromptSeq s = sh_seq;
+  const int64_t first = (int64_t)sh_tile * 128 + blockIdx.z * 32;
+  if (first >= s.keys) return;
+  const keys::Tile x(p, s, sh_tile, log_p);
   if (x.parts < 2) return;
   const int hb = blockIdx.y >> 1, which = blockIdx.y & 1, pieces = p.dim / 4, keys = (int)min((int64_t)32, s.keys - first);
   uint16_t* base = which ? p.dk : p.dv;
@@ -1266,6 +1273,8 @@ __global__ void __launch_bounds__(256) split_kernel(GradParams p, int log_p) {
   }
 }
 
+// Once per device and kernel: the shared memory, and that the register split adds up --
+// setmaxnreg.inc waits for registers that only the launch's own can give.
 template <class Kernel, class... Maps>
 int launch(Kernel kern, std::atomic<uint64_t>& ready, int smem, int grid, cudaStream_t st, const GradParams& p, const Maps&... maps) {
   int dev = 0;
@@ -1309,8 +1318,8 @@ int launch_grad(const GradParams& p, const CUtensorMap (&mk)[5], const CUtensorM
     const int rc = launch(rows::prompt_rows_kernel<DP, BF16>, ready_r, smem_r, grid_rows, st, p, mr[0], mr[1], mr[2], mr[3]);
     if (rc != OCCAM_OK) return rc;
   }
-  if (p.parts > 1) {
-    const dim3 grid((unsigned)(p.total_keys / 128 + 2 * (int64_t)p.n), (unsigned)p.Hkv * 2, 4);
+  if (p.parts > 1 && grid_keys > 0) {
+    const dim3 grid((unsigned)(p.most_keys / (p.Hkv * p.parts)), (unsigned)p.Hkv * 2, 4);
     if (!launch_after(split_kernel<BF16>, grid, 256, 0, st, p, std::min(p.log2P, 6)) || cudaGetLastError() != cudaSuccess) return OCCAM_ERR_CUDA;
   }
   return OCCAM_OK;

@@ -39,3 +39,37 @@ def test_grad_of_few_key_heads(n, dtype):
             o = off if i == 0 or koff is None else koff
             assert torch.equal(x[o[0]:o[-1]], y[o[0]:o[-1]])
     assert occ.occam_get_status(ws) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("off,koff", [([1000, 2000, 0, 1000], None), ([0, 700, 1 << 40, 700, 2000], None),
+                                      ([1000, 2000, 0, 1000], [1100, 2200, 0, 1100]), ([0, 1000, 1000, 2000], [900, 1900, 0, 900])])
+def test_grad_parts_beside_a_sequence_that_does_not_fit(off, koff, dtype):
+    """Offsets that go back leave out their own sequence only: the others' divided gradients are those of a call without it."""
+    import paper_2605_29657_gb300 as occ
+    from paper_2605_29657_gb300 import _lib as L
+    ko = off if koff is None else koff
+    q, k, v = inputs([2000], [max(x for x in ko if x < 1 << 40)], 8, 1, 64, DT[dtype], 7, gain=0.8)
+    dout, ws = gradient_of(q, DT[dtype], 7), occ.alloc_prompt_workspace(2000, 8, k.shape[0], 1)
+    good = [i for i in range(len(off) - 1) if off[i] <= off[i + 1] <= 2000 and ko[i] <= ko[i + 1] <= k.shape[0]]
+    assert 0 < len(good) < len(off) - 1
+    out, lse = torch.zeros_like(q), torch.zeros(q.shape[:2], device="cuda")
+    got, want = ([torch.full_like(x, 7.0) for x in (q, k, v)] for _ in range(2))
+    kw = dict(out=out, lse=lse)
+    occ.occam_prompt_attend(q, k, v, dev(off), ws, key_off=dev(ko), **kw)
+    occ.occam_prompt_attend_grad(q, k, v, out, lse, dout, dev(off), ws, key_off=dev(ko), dq=got[0], dk=got[1], dv=got[2])
+    assert occ.occam_get_status(ws) == L.OCCAM_ERR_INVALID_ARG
+    for i in good:
+        a, b = dev([off[i], off[i + 1]]), dev([ko[i], ko[i + 1]])
+        occ.occam_prompt_attend(q, k, v, a, ws, key_off=b, **kw)
+        occ.occam_prompt_attend_grad(q, k, v, out, lse, dout, a, ws, key_off=b, dq=want[0], dk=want[1], dv=want[2])
+    assert occ.occam_get_status(ws) == 0
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
+
+
+def test_grad_of_many_rows_without_keys():
+    """Nothing to divide."""
+    q, k, v = inputs([3000], [0], 8, 1, 64, torch.bfloat16, 1)
+    dq, dk, dv = check(q, k, v, gradient_of(q, torch.bfloat16), [0, 3000], [0, 0])
+    assert not dq.any() and dk.shape[0] == dv.shape[0] == 0
