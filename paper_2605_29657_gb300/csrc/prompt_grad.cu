@@ -448,7 +448,9 @@ __device__ __forceinline__ void issue_role(const GradParams& p, Sh& sh, uint32_t
     // knows one ahead; more may wait for those very products)
     bool over = false, have = j < end;
     if (!have) {
-      // the item's keys and values are done with once the scores issued so far are
+      // The item's keys and values are done with once the scores issued so far are -- and have come: given back before, by the
+      // warp without a step here, the next ones could come before it looked for these, and two phases on a wait does not end.
+      for (; kv < n_kv; ++kv) WAIT(sh.kv_full, kv & 1);
       if (end > base) tc::mma_commit(&sh.kv_free);
       if (i > 0) tc::bar_arrive(&sh.item_free[(i - 1) % kItems]);
       WAIT(sh.item_full[i % kItems], (i / kItems) & 1);
@@ -480,7 +482,7 @@ __device__ __forceinline__ void issue_role(const GradParams& p, Sh& sh, uint32_t
       }
     }
     if (have) {
-      for (; kv < n_kv; ++kv) WAIT(sh.kv_full, kv & 1);  // (every phase, those of items without own steps too)
+      for (; kv < n_kv; ++kv) WAIT(sh.kv_full, kv & 1);
       WAIT(sh.full[st], (j / S::kStages) & 1);
       while (block >= blocks) block -= blocks;
       if (ragged && block == blocks - 1) {

@@ -264,3 +264,22 @@ def test_grad_of_rows_that_see_one_key(n, dtype):
                 assert s > 1 or not dk[koff[i]:koff[i + 1]].any()
         assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
     assert occ.occam_get_status(ws) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("H,Hkv,D", [(4, 2, 64), (3, 3, 128), (8, 1, 72)])
+def test_grad_of_many_items_of_one_step(H, Hkv, D, dtype):
+    """Each of the two issuing warps passes by every second item: no wait runs out, and results repeat."""
+    import paper_2605_29657_gb300 as occ
+    rows = [1 + (5 * i) % 8 for i in range(3000)]
+    q, k, v = inputs(rows, None, H, Hkv, D, DT[dtype], 6)
+    dout, off, ws = gradient_of(q, DT[dtype]), dev(offs(rows)), occ.alloc_prompt_workspace(sum(rows), H, sum(rows), Hkv)
+    out, lse = occ.occam_prompt_attend(q, k, v, off, ws)
+    want = occ.occam_prompt_attend_grad(q, k, v, out, lse, dout, off, ws)
+    for _ in range(30):
+        got = occ.occam_prompt_attend_grad(q, k, v, out, lse, dout, off, ws)
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+    assert occ.occam_get_status(ws) == 0
+    first = offs(rows[:100])
+    for x, y, tol in zip(want, *(lambda r: (r[:3], r[3:]))(P.grad(*(t[:first[-1]] for t in (q, k, v, dout)), first))):
+        P.assert_near(x[:first[-1]], y, tol, DT[dtype])
