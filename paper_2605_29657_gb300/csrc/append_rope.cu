@@ -224,7 +224,8 @@ __global__ void __launch_bounds__(kThreads, NU * V <= 16 ? 4 : 2) enter_kernel(E
           for (int k = 0; k < V; k += 2) {
             const float4 t = *reinterpret_cast<const float4*>(cs + 2 * k * (half / V));
             const float2 c = make_float2(t.x, t.y), sn = make_float2(t.z, t.w), y = at2(x[n] + k), z = at2(x[n] + V + k);
-            const float2 e0 = tc::fma2(z, make_float2(-sn.x, -sn.y), tc::mul2(y, c)), e1 = tc::fma2(z, c, tc::mul2(y, sn));
+            // (rounded as below and in rope_rows: every vector width, which the queries' alignment chooses too, gives the same codes)
+            const float2 e0 = tc::fma2(y, c, tc::mul2(z, make_float2(-sn.x, -sn.y))), e1 = tc::fma2(z, c, tc::mul2(y, sn));
             x[n][k] = e0.x;
             x[n][k + 1] = e0.y;
             x[n][V + k] = e1.x;

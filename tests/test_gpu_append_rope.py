@@ -256,3 +256,29 @@ def test_append_rope_refusals():
     ):
         with pytest.raises(occ.OccamError):
             call(**bad)
+
+
+@pytest.mark.parametrize("dim,rot,pairing", [(128, 128, "half"), (64, 64, "half"), (128, 24, "half"), (128, 128, "adjacent")])
+def test_append_rope_codes_do_not_depend_on_the_queries(dim, rot, pairing):
+    """The same keys beside queries of every alignment, and none: the same codes, and queries turned to the same bits."""
+    import paper_2605_29657_gb300 as occ
+    rows, heads = 4096, 16
+    c = make(layers=1, pages=rows // 64 + 1, heads=heads, dim=dim, T=64, seqs=1, max_pages=rows // 64, stale=False)
+    seqs, off = dev([0]), dev([0, rows], I64)
+    occ.occam_cache_extend(c, seqs, dev([rows]))
+    q, k, v, pos, freq, axis = case(rows, 2, heads, dim, rot, 3, "f16", 4)
+    odd = torch.zeros(rows * (2 * dim + 6) + 1, dtype=torch.float16, device="cuda")
+    some = [None, q, odd[1:].view(rows, 2 * dim + 6)[:, :2 * dim].unflatten(1, (2, dim)), odd[:-1].view(rows, 2 * dim + 6)[:, 4:2 * dim + 4].unflatten(1, (2, dim))]
+    codes, turned = [], []
+    for x in some:
+        if x is not None:
+            x.copy_(q)
+        c.k_scale.fill_(1.0), c.v_scale.fill_(1.0)
+        out = occ.occam_cache_append_rope(c, 0, x, k, v, seqs, off, pos, freq, axis, pairing=pairing)
+        codes.append((c.k.view(torch.uint8).clone(), c.v.view(torch.uint8).clone(), c.k_scale.clone(), c.v_scale.clone()))
+        if x is not None:
+            turned.append(out)
+    assert c.status() == 0
+    for x in codes[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(x, codes[0]))
+    assert all(torch.equal(x, turned[0]) for x in turned[1:])
