@@ -36,6 +36,7 @@ def main() -> int:
         (G.test_grad_without_keys, ()), (G.test_grad_many_sequences, ()), (G.test_grad_offsets_that_do_not_fit_are_recorded, ()),
         (A.test_append_rope, (16, 64, 2, 2, 64, "half", "bf16")), (A.test_append_rope, (64, 128, 3, 6, 64, "adjacent", "f16")),
         (A.test_append_rope, (128, 128, 1, 1, 128, "half", "bf16")), (A.test_append_rope_many_sequences_and_rows_outside, ()),
+        (A.test_append_rope_of_many_conversations, (256,)), (A.test_append_rope_of_many_conversations, (700,)),
         (A.test_append_rope_many_heads_share_a_page, ()), (A.test_append_rope_errors_change_nothing, ()),
         (S.test_attend_shared_whatever_the_groups, ()), (S.test_attend_shared_device_errors, ()),
         (C.test_attend_many_short_items, (30, 150, 9, 32)), (V.test_prompts_enter_fork_and_answer, (64, 128, 2, 4, [150, 70, 301], 3, "bf16")),

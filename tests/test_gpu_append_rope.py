@@ -282,3 +282,17 @@ def test_append_rope_codes_do_not_depend_on_the_queries(dim, rot, pairing):
     for x in codes[1:]:
         assert all(torch.equal(a, b) for a, b in zip(x, codes[0]))
     assert all(torch.equal(x, turned[0]) for x in turned[1:])
+
+
+@pytest.mark.parametrize("n", [255, 256, 700])
+def test_append_rope_of_many_conversations(n):
+    """Fewer sequences than a CTA has threads, as many, and more; empty ones, rows before and behind."""
+    c = make(layers=1, pages=2 * n, heads=1, dim=64, T=16, seqs=n, max_pages=3)
+    ref = R.Cache(c)
+    g = torch.Generator().manual_seed(n)
+    seqs = torch.randperm(n, generator=g).tolist()
+    for _ in range(2):
+        counts = torch.randint(-3, 10, (n,), generator=g).clamp(min=0).tolist()
+        q, k, v, pos, freq, axis = case(sum(counts) + 30, 2, 1, 64, 64, 2, "bf16", n)
+        out = append(c, ref, 0, q, k, v, pos, freq, axis, "half", seqs, counts, first=19)
+        close(out, q, pos, freq, axis, "half", False)
