@@ -236,8 +236,10 @@ __device__ __forceinline__ void issue_role(const PromptParams& p, Sh& sh, uint32
 template <int DP, bool BF16, class Sh>
 __device__ __forceinline__ void softmax_role(const PromptParams& p, Sh& sh, uint32_t tmem, int t) {
   // P of f16 values is held 2^7 times as large: at most 2^15 (f16 ends at 2^16), and what is 2^-21 of a row's
-  // reference still has f16's 11 bits; bf16 has fp32's range.
-  constexpr float kLift = BF16 ? 0.f : 7.f;
+  // reference still has f16's 11 bits. bf16 has fp32's range: P is held 2^-16 times as large, at most 2^-8, so that sums
+  // of values near bf16's end stay finite (those of 65,536 keys, 256 where a reference lags as far as it may) and
+  // values down to 2^-110 keep their bits.
+  constexpr float kLift = BF16 ? -16.f : 7.f;
   const int r = threadIdx.x & 127, lane = threadIdx.x & 31;
   const uint32_t lanes = (uint32_t)(r & ~31) << 16;
   const uint32_t s_at = tmem + t * 128 + lanes, o_at = tmem + 256 + t * 128 + lanes;
@@ -326,7 +328,7 @@ __device__ __forceinline__ void softmax_role(const PromptParams& p, Sh& sh, uint
     tc::bar_arrive(&sh.inv_full[t]);
     ++n;
     if (p.lse && tok < rows && in_bounds(at < p.total_rows * p.H, p.status, kSitePromptRow))
-      p.lse[at] = l == 0.f ? -INFINITY : (ref + log2f(l) - kLift) * 0.69314718056f;
+      p.lse[at] = l == 0.f ? -INFINITY : (BF16 ? ref + log2f(l * 65536.f) : ref + log2f(l) - kLift) * 0.69314718056f;
   }
 }
 

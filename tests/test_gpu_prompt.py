@@ -236,3 +236,16 @@ def test_prompt_refusals():
             call()
     none = occ.occam_prompt_attend(q[:0], k[:0], v[:0], dev([0]), ws)
     assert none[0].shape == (0, 4, 64)
+
+
+def test_prompt_values_near_the_end_of_bf16():
+    """Sums before their division stay finite: results are means of the values."""
+    q, k, v = (x.clone() for x in inputs([300, 40, 2], None, 4, 2, 128, torch.bfloat16, 12))
+    v[:300] = v[:300].sign() * 3.3e38
+    v[300:] = 3.3e38
+    k[:300] = 0.0  # all weights the same
+    q[300:340], k[300:340] = 1.0, (torch.arange(40, device="cuda")[:, None, None] / 80).bfloat16()  # scores that climb by 5.5
+    check(q, k, v, [0, 300, 340, 342])
+    check(q, k, v, [0, 300, 340, 342], causal=False)
+    # and small ones are what they were
+    check(q, k, torch.where(v > 0, 1e-30, -3e-31).bfloat16(), [0, 300, 340, 342])
