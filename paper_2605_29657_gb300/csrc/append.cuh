@@ -15,6 +15,14 @@ struct AppendParams {
   const int64_t* row_off;
 };
 
+// Offsets that go back are recorded, by one CTA: sequences at such a place take each other's slots, and their pages
+// may be looked at by nobody.
+__device__ __forceinline__ void record_backward(const AppendParams& p) {
+  bool back = false;
+  for (int i = threadIdx.x; i < p.n; i += blockDim.x) back |= p.row_off[i + 1] < p.row_off[i];
+  if (back) set_status(p.c.status, OCCAM_ERR_INVALID_ARG);
+}
+
 // The first index whose slot count passes w: sequence i's pages occupy slots
 // [row_off[i] / T + 2 i, row_off[i+1] / T + 2 (i + 1)), at least as many as
 // the pages its rows can touch. One warp searches 32 ways at a time.

@@ -109,6 +109,7 @@ __global__ void __launch_bounds__(kThreads, NU * V <= 16 ? 4 : 2) enter_kernel(E
   // (by turns: blocks go to SMs round robin, and an SM that always got the parts of K would be last)
   const int part = (int)((blockIdx.x + w) % e.parts);
   const bool is_k = part < e.k_parts;
+  if ((int)blockIdx.x == e.parts) record_backward(p);  // (the second slot: an early CTA, and idle where every sequence has a token)
   const int refused = p.c.status[1] & kRefused;  // (no CTA of this launch sets it)
   const int T = p.c.T, H = p.c.heads;
   // The slot's sequence. Up to 255 of them are looked at at once, with their lengths: two rounds of loads instead of six.

@@ -51,6 +51,7 @@ __global__ void __launch_bounds__(128, MAXV == 8 ? 9 : 1) append_kernel(AppendPa
   const int T = p.c.T, H = p.c.heads;
   const int kv = blockIdx.x & 1, h = (int)(blockIdx.x >> 1);
   const int64_t w = (int64_t)blockIdx.z * gridDim.y + blockIdx.y;
+  if (w == 1 && blockIdx.x == 0) record_backward(p);  // (an early CTA, and idle where every sequence has a token)
   const int i = slot_sequence(p.row_off, p.n, p.c.log2T, w);
   const int64_t r0 = p.row_off[i], r1 = p.row_off[i + 1];
   const int64_t local = w - ((r0 >> p.c.log2T) + 2 * (int64_t)i);

@@ -296,3 +296,22 @@ def test_append_rope_of_many_conversations(n):
         q, k, v, pos, freq, axis = case(sum(counts) + 30, 2, 1, 64, 64, 2, "bf16", n)
         out = append(c, ref, 0, q, k, v, pos, freq, axis, "half", seqs, counts, first=19)
         close(out, q, pos, freq, axis, "half", False)
+
+
+@pytest.mark.parametrize("more", [0, 300])
+@pytest.mark.parametrize("off", [[0, 640, 0, 640], [0, 320, 192, 400], [300, 640, 0, 300]])
+def test_append_offsets_that_go_back_are_recorded(off, more):
+    """Also where no page of the sequence between them is looked at, or sequences take each other's places."""
+    import paper_2605_29657_gb300 as occ
+    n = 3 + more
+    c = make(layers=1, pages=64, heads=1, dim=64, T=64, seqs=n, max_pages=10, stale=False)
+    seqs = dev(list(range(n)))
+    counts = [max(b - a, 0) for a, b in zip(off, off[1:])]
+    occ.occam_cache_extend(c, dev([0, 1, 2]), dev(counts))
+    assert c.status() == 0
+    q, k, v, pos, freq, axis = case(640, 1, 1, 64, 64, 1, "bf16")
+    all_off = dev(off + off[-1:] * more, I64)
+    occ.occam_cache_append_rope(c, 0, q, k, v, seqs, all_off, pos, freq, axis)
+    assert c.status() == 1
+    occ.occam_cache_append(c, 0, k, v, seqs, all_off)
+    assert c.status() == 1
