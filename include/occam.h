@@ -668,8 +668,8 @@ typedef struct occam_prompt_args {
 } occam_prompt_args;
 
 /* Scratch of the two calls below, for calls of up to these sizes (workspace convention
- * as above: 256-byte aligned, zero-filled before first use, status word at its start): 44 bytes a row and head, and up to
- * 40 MB for the gradient's parts. One call at a time. */
+ * as above: 256-byte aligned, zero-filled before first use, status word at its start): 44 bytes a row and head, 4 a row and
+ * key head, 4 a key and key head, and up to 40 MB for the gradient's parts. Both calls ask for all of it. One call at a time. */
 int occam_prompt_workspace_size(int64_t total_rows, int64_t total_keys, int32_t heads, int32_t kv_heads, size_t* bytes);
 
 /* out [total_rows, heads, dim] (q's type, dense, 16-byte aligned) = sum_k p_k v_k / sum_k p_k,

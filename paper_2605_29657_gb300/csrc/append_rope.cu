@@ -8,7 +8,7 @@
 // codes. The queries are turned by a launch of their own (rope_rows) that starts while this one ends. Bound by HBM:
 // queries 2 bytes read and written, keys and values 2 read and 1 written a value: 20 k rows of 32 + 32 + 32 heads of 128 in
 // 178 us, 0.70 of a plain copy (keys and values 117 us of it: partly filled pages, and a maximum before the first store).
-// A single row a sequence: 12 us, a chain of offsets, table, row, scale.
+// A single row a sequence: 13 us, a chain of offsets, table, row, scale.
 #include <algorithm>
 #include <atomic>
 #include <type_traits>

@@ -720,7 +720,7 @@ int launch_rows(const AttendCall<MODE>& p, cudaStream_t st) {
   CUtensorMap mk{}, mv{};
   // Tensor copies where every row of a tile is wanted; with keep flags, rows
   // one by one (a hidden row is not read). 64 single tokens over 2,300, of which 10 % are seen: 83 us,
-  // by tensor copies 94; half 93 and 92; 90 % 94.5 and 92; without flags 65.
+  // by tensor copies 94; half 93 and 92; 90 % 94.5 and 92; without flags 68.
   if constexpr (MODE == kWhole)
     if (p.keep) return launch<D, NQ, false>(p, mk, mv, st);
   const int box = std::min(p.c.T, kTile);

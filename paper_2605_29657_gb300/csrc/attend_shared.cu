@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(kThreads) common_kernel(CommonParams p) {
   // Whether it pays. In units of a row tile (256 query rows of a key head) against 128 keys on the tensor cores, 2 us of an
   // SM's time: a sequence of up to 32 such rows takes half of one, by the few-row kernel. (64 single tokens over 16 k
   // common tokens: 65 us shared, 480 not; three over 600: 35 and 21; 8 x 8 questions of 16 to 128 rows over 2,900, whose rows fill their
-  // tiles without each other: 420 and 314.)
+  // tiles without each other: 446 and 338.)
   float alone = 0.f;
   int64_t rows = 0;
   for (int i = a + t; i < b && pages > 0; i += kThreads) {

@@ -9,17 +9,18 @@
 // (P: the group's largest power of two, so that grouped heads read their keys
 // once and a causal tile spans few tokens). One CTA an SM takes items from a counter; 16 warps in six roles
 // that run through the items one after the other without a barrier between them:
-//  - warp 13 takes items and copies queries, keys and values to shared memory (TMA);
+//  - warp 13 copies queries, keys and values to shared memory (TMA);
 //  - warps 12 and 14 issue the products of a row tile each: S = Q K^T into tensor memory, 64 keys at a
 //    time, O += P V with P read from tensor memory. While one half of the scores is in the
 //    softmax, the other is multiplied; the next item's scores follow the last product of the one before;
 //  - warps 0-3 and 4-7 hold a row a thread: scores, maximum, exponentials, P back as 16 bits;
 //  - warps 8-11 write the results: O from tensor memory over shared memory as whole rows;
-//  - warp 15 looks values over that some row does not see: rows past the sequence's
+//  - warp 15 takes items and tells the others of them; it looks values over that some row does not see: rows past the sequence's
 //    end become zeros, and so do values that are not finite, which are noted and put back into
 //    the results of the rows that see them.
 // P is rounded to the type of the values (both operands of a product have one type), l sums the unrounded P.
-// Bound at 128 dims by the products: 8,257 causal rows of 32 heads in 353 us, 1,570 TFLOP/s (0.83 of cuBLAS' measured rate);
+// Bound at 128 dims by the products: 8,257 causal rows of 32 heads in 353 us, 1,580 TFLOP/s (0.84 of cuBLAS' measured rate),
+// 378 us where every pass has other inputs;
 // at 64 to 80 by the softmax's chain (scores, maximum, exponentials, P; two warps a scheduler do not hide its
 // latencies): 27 k full rows (12 images) of 16 heads of 72 in 370 us, tensor pipe 48 % busy, issue 48 %, exponentials 38 %. Many short prompts
 // (64 of about 310, 32 key heads) are bound by HBM: 154 us, 0.65 of a plain copy.

@@ -67,7 +67,7 @@ struct PromptItem {
   int64_t row0, key0;
   int rows, keys;
   int tile, hb;    // the block of rows (or keys) and the block of heads
-  int steps;       // 0: there is none, the CTA is done
+  int steps;       // 0: there is none, the CTA is done (the gradient's keys: an item without work; nk[1] says that there is none)
   int nk[2];       // steps of each row tile
   int step0, part; // (the gradient's keys) the first step; the part of a divided item, -1: it is whole, -2: there is no such part
 };
@@ -210,9 +210,10 @@ bool encode_rows(CUtensorMap* m, const void* at, bool bf16, int dim, int heads, 
 struct PromptWs {
   size_t terms, stat, norm, power, vnorm, split, total;
 };
-// How many parts an item of the gradient's keys may be divided into: where there are fewer items than two an SM, one of them
-// would be a CTA's whole time. (2,400 rows of 28 heads on 4: 178 us; parts for 228 items: 190, for 608: 196. 4,177 of 32
-// on 8, whole: 404, in two: 424.)
+// How many parts an item of the gradient's keys may be divided into: kPartItems / items, whole, so that nothing is divided
+// where there are more than half as many items (tiles x key heads), one an SM or so, and all parts together are kPartItems
+// tiles at most, for which the workspace has room. An item would be a CTA's whole time there. (2,400 rows of 28 heads on 4,
+// 76 items: 178 us; with parts for 228 items 190, for 608 196. 4,177 of 32 on 8, 264 items, whole 404, in two 424.)
 constexpr int kPartItems = 304, kMostParts = 8;
 inline int prompt_parts(int64_t items) {
   return items < 1 ? 1 : (int)std::min<int64_t>(std::max<int64_t>(kPartItems / items, 1), kMostParts);

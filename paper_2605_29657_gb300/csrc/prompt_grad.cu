@@ -7,7 +7,7 @@
 // sum has one order, the heads of a group included, so results repeat bit for bit; a kernel that
 // owned keys alone would do with 10 D in all but add dQ across CTAs. Where there are few tiles of keys their rows are
 // divided into up to 8 parts of 12 steps or more, whose sums in fp32 a last launch adds up in order (1,000 rows, 8 heads on one
-// key head: 119 -> 58 us; 3,500 rows, 5 on one: 264 -> 130; 2,400 rows, 28 on 4: 265 -> 178).
+// key head: 119 -> 61 us; 3,500 rows, 5 on one: 264 -> 134; 2,400 rows, 28 on 4: 265 -> 180).
 // Before them a pass over dO and O forms delta; with f16, where dS has no range to spare, also the norms
 // that bound it: |dP - delta| <= |dO||V| + |delta|, and dS is held times a power of two a sequence and key head that
 // brings that bound under f16's end.
@@ -259,7 +259,8 @@ struct Count {
   __device__ __forceinline__ int operator()(const PromptSeq& s) const { return (s.keys / 128 + (s.keys % 128 != 0)) * p.Hkv * p.parts; }
 };
 // A tile's first block of rows, blocks of a head block, and steps; parts of so many steps at least (1,000 rows of 8 heads
-// on one key head: 58 us, 64 with 16, 83 with 32; 300 rows of 32 on 8: 39, 43 with 8).
+// on one key head: 58 us, 64 with 16, 83 with 32; 300 rows of 32 on 8: 39, 43 with 8; finding the tiles to add up by their
+// items takes 1 us more since).
 constexpr int kPartSteps = 12;
 struct Tile {
   int first, blocks, steps, parts;
