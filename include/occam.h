@@ -460,7 +460,7 @@ int occam_rope(int32_t dtype, int64_t rows, int32_t dim, int32_t rot, int32_t pa
  * free page first, in call order, so they do not depend on timing.
  *
  * seqs (and src, dst) are device arrays of n distinct slots, n <= max_seqs.
- * A slot, offset or page outside its range, a slot listed twice (extend,
+ * A slot, offset or page outside its range, offsets that go back, a slot listed twice (extend,
  * fork, compact) or a count that does not fit records OCCAM_ERR_INVALID_ARG
  * in the status word, too few free pages (or table columns) record
  * OCCAM_ERR_CAPACITY; an extend, fork or compact call that records an error

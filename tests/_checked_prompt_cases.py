@@ -36,6 +36,9 @@ def main() -> int:
         (G.test_grad_without_keys, ()), (G.test_grad_many_sequences, ()), (G.test_grad_offsets_that_do_not_fit_are_recorded, ()),
         (A.test_append_rope, (16, 64, 2, 2, 64, "half", "bf16")), (A.test_append_rope, (64, 128, 3, 6, 64, "adjacent", "f16")),
         (A.test_append_rope, (128, 128, 1, 1, 128, "half", "bf16")), (A.test_append_rope_many_sequences_and_rows_outside, ()),
+        (G.test_grad_of_many_items_of_one_step, (4, 2, 64, "bf16")), (G.test_grad_of_many_items_of_one_step, (3, 3, 128, "f16")),
+        (G.test_grad_of_rows_that_see_one_key, (3, "bf16")), (GP.test_grad_parts_beside_a_sequence_that_does_not_fit, ([1000, 2000, 0, 1000], None, "f16")),
+        (A.test_append_offsets_that_go_back_are_recorded, ([0, 640, 0, 640], 300)),
         (A.test_append_rope_of_many_conversations, (256,)), (A.test_append_rope_of_many_conversations, (700,)),
         (A.test_append_rope_many_heads_share_a_page, ()), (A.test_append_rope_errors_change_nothing, ()),
         (S.test_attend_shared_whatever_the_groups, ()), (S.test_attend_shared_device_errors, ()),
